@@ -544,6 +544,142 @@ mtgnn_status mtgnn_time_projection_bwd(const int32_t* q_node, const float* q_t, 
                                        const int32_t* n_rows, int64_t max_rows, const mtgnn_dims* dims, float* dW_p,
                                        float* db_p, float* d_mem, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------ a state-space layer over sequences
+ * A third kind of memory update beside the GRU (mtgnn_gru_update) and the recurrent cell (mtgnn_rnn_update):
+ * instead of a node's last message it takes all of them, in time order.  Its operators are a linear layer, a
+ * short causal convolution per channel and a selective state space scan; a layer is
+ *   linear -> conv -> linear (delta, B, C) -> scan with gate -> linear with residual.
+ * Activations, weights of products and of the convolution, and the convolution's states are in the dims'
+ * dtype; biases, A, D, the scan's states and every gradient are float32; every sum and state is held in
+ * float32, and an output is rounded to the dtype once (nearest even).  Matrices of rows have a row stride
+ * in elements (>= their width), so that an operand may be a column range of a wider matrix.  Per-channel
+ * parameters and states are laid out like rows, channels fastest.
+ *
+ * The rows of several sequences stand one after the other: sequence s < n has rows off[s] .. off[s + 1] - 1
+ * (none where the two are equal), with off non-decreasing and off[n] <= max_rows.  Rows outside them are
+ * neither read into a result nor written.  A sequence goes on from the state of its slot and leaves its last
+ * one there: slot s of a table where slot is NULL, else slot[s].  A slot outside [0, n_slots) stands for no
+ * slot: the sequence starts from zeros and its last state is dropped.  Two sequences of a call must not share
+ * a slot.  A sequence without rows leaves its slot as it was.  The state a call starts from is an input that is
+ * not differentiated, as the memory table is not across steps. */
+typedef enum { MTGNN_ACT_NONE = 0, MTGNN_ACT_RELU = 1, MTGNN_ACT_SILU = 2, MTGNN_ACT_GELU = 3 } mtgnn_act;
+
+typedef struct {
+  int64_t max_rows, max_seq; /* rows of the matrices; the most sequences (max_seq <= 2^30, max_rows < 2^31 - 1) */
+  int64_t n_slots;           /* rows of the state tables (0 where no state is given) */
+  const int32_t* off;        /* [max_seq + 1] device */
+  const int32_t* n_seq;      /* device count n of sequences, or NULL: max_seq */
+  const int32_t* slot;       /* [max_seq] device, or NULL */
+} mtgnn_seqs;
+
+/* y = act(pre) + residual, pre = x W^T + b, for rows r < n_rows (device count, or NULL: max_rows).
+ *   x [max_rows, d_in], W [d_out, d_in] (rows dense), residual [max_rows, d_out] or NULL, y [max_rows, d_out]
+ *   (dtype); b [d_out] float32 or NULL;
+ *   pre -- [max_rows, d_out] float32 out for mtgnn_linear_bwd, or NULL.
+ * act: silu(p) = p / (1 + e^-p), gelu(p) = p (1 + erf(p / sqrt 2)) / 2.  y may be residual (same stride); it
+ * may not overlap x.  A product is exact to float32: bfloat16 operands multiply on the bfloat16 matrix
+ * instructions; float32 ones there too, as three bfloat16 parts each.
+ * Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too.  Rows at or beyond n_rows are left untouched. */
+typedef struct {
+  int32_t d_in, d_out, dtype, act; /* mtgnn_dtype, mtgnn_act */
+} mtgnn_linear_dims;
+size_t mtgnn_linear_ws_bytes(const mtgnn_linear_dims* dims, int64_t max_rows, int32_t backward);
+mtgnn_status mtgnn_linear(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W,
+                          const float* b, const void* residual, int64_t ldr, const mtgnn_linear_dims* dims, void* y,
+                          int64_t ldy, float* pre, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Backward of mtgnn_linear for dy [max_rows, d_out] float32 (also the residual's gradient): with
+ * g = dy act'(pre), dx = g W [max_rows, d_in] (or NULL), dW = g^T x [d_out, d_in] (or NULL), db = sum of g [d_out]
+ * (or NULL), each over the rows below n_rows; dW and db are overwritten (zero without rows).
+ *   pre -- the forward call's; may be NULL where act is none.
+ * Sums over rows run in a fixed order (deterministic).  Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 1). */
+mtgnn_status mtgnn_linear_bwd(const float* dy, int64_t lddy, const float* pre, const void* x, int64_t ldx,
+                              const int32_t* n_rows, int64_t max_rows, const void* W, const mtgnn_linear_dims* dims,
+                              float* dx, int64_t lddx, float* dW, float* db, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+
+/* Short causal convolution over each sequence, channel by channel (width 2 to 4):
+ *   y_t = act(pre_t),  pre_t = b + sum_j w[j] x_(t - width + 1 + j),  act none or silu,
+ * where rows before the sequence's first are its slot's state, the last width - 1 inputs, oldest first.
+ *   x, y [max_rows, d] (dtype; y may not overlap x), w [width, d] (dtype), b [d] float32 or NULL;
+ *   state_in, state_out -- [n_slots, width - 1, d] (dtype) tables, each or NULL (NULL state_in: zeros); they are one
+ *           table or do not overlap;
+ *   save -- mtgnn_causal_conv_save_bytes bytes for the backward (it keeps the states the sequences started
+ *           from), or NULL where state_in is NULL or no backward follows. */
+typedef struct {
+  int32_t d, width, dtype, act;
+} mtgnn_conv_dims;
+size_t mtgnn_causal_conv_save_bytes(const mtgnn_conv_dims* dims, int64_t max_seq);
+mtgnn_status mtgnn_causal_conv(const mtgnn_seqs* seqs, const void* x, int64_t ldx, const void* w, const float* b,
+                               const mtgnn_conv_dims* dims, const void* state_in, void* state_out, void* y,
+                               int64_t ldy, void* save, hipStream_t stream);
+
+/* Backward of mtgnn_causal_conv for dy [max_rows, d] float32: with g_t = dy_t act'(pre_t) (pre is computed again),
+ *   dx_t = sum_j w[j] g_(t + width - 1 - j) over the sequence's rows,  dw[j] = sum_t g_t x_(t - width + 1 + j),
+ *   db = sum_t g_t (or NULL);  dw, db overwritten.  save: the forward's (NULL: the sequences started from zeros).
+ * Deterministic.  Workspace: mtgnn_causal_conv_ws_bytes(dims, max_rows). */
+size_t mtgnn_causal_conv_ws_bytes(const mtgnn_conv_dims* dims, int64_t max_rows);
+mtgnn_status mtgnn_causal_conv_bwd(const mtgnn_seqs* seqs, const float* dy, int64_t lddy, const void* x, int64_t ldx,
+                                   const void* w, const float* b, const mtgnn_conv_dims* dims, const void* save,
+                                   float* dx, int64_t lddx, float* dw, float* db, void* ws, size_t ws_bytes,
+                                   hipStream_t stream);
+
+/* mtgnn_causal_conv for sequences of one row each, in one launch: row r < n_rows (device count, or NULL: max_rows)
+ * is the next row of slot[r] (NULL: slot r).  state_in and state_out as there, either may be NULL. */
+mtgnn_status mtgnn_causal_conv_step(const int32_t* slot, const int32_t* n_rows, int64_t max_rows, int64_t n_slots,
+                                    const void* x, int64_t ldx, const void* w, const float* b,
+                                    const mtgnn_conv_dims* dims, const void* state_in, void* state_out, void* y,
+                                    int64_t ldy, hipStream_t stream);
+
+/* Selective state space scan over each sequence: for channel c of group c / (d / groups), state i < n,
+ *   dt_t = softplus(delta_t + delta_bias)   (softplus 0 in the dims: delta_t + delta_bias),
+ *   h_t[i] = exp(dt_t A[i]) h_(t-1)[i] + dt_t B_t[i] x_t,
+ *   y_t = (sum_i C_t[i] h_t[i] + D x_t) silu(z_t),
+ * h before the sequence's first row being its slot's state.  n <= 64; groups divides d.
+ *   x, delta, z (or NULL: no gate), y -- [max_rows, d] (dtype); y may be x, delta or z (same stride) where no
+ *           backward follows, and may not overlap them otherwise;
+ *   B, C -- [max_rows, groups * n] (dtype), each group's n columns together;
+ *   A [n, d], D [d] or NULL (no skip), delta_bias [d] or NULL -- float32;
+ *   state_in, state_out -- [n_slots, n, d] float32 tables, as for mtgnn_causal_conv;
+ *   save -- mtgnn_selective_scan_save_bytes bytes for the backward, or NULL.
+ * Workspace: mtgnn_selective_scan_ws_bytes(dims, max_rows, max_seq, 0), or with 1 enough for the backward too. */
+typedef struct {
+  int32_t d, n, groups, dtype, softplus;
+} mtgnn_scan_dims;
+typedef struct {
+  const void *x, *delta, *B, *C, *z;
+  int64_t ldx, lddelta, ldB, ldC, ldz;
+  const float *A, *D, *delta_bias;
+} mtgnn_scan_inputs;
+size_t mtgnn_selective_scan_ws_bytes(const mtgnn_scan_dims* dims, int64_t max_rows, int64_t max_seq, int32_t backward);
+/* carried: whether state_in is given. */
+size_t mtgnn_selective_scan_save_bytes(const mtgnn_scan_dims* dims, int64_t max_rows, int64_t max_seq, int32_t carried);
+mtgnn_status mtgnn_selective_scan(const mtgnn_seqs* seqs, const mtgnn_scan_inputs* in, const mtgnn_scan_dims* dims,
+                                  const float* state_in, float* state_out, void* y, int64_t ldy, void* save, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/* Backward of mtgnn_selective_scan for dy [max_rows, d] float32, with the forward's inputs and save.
+ *   dx, ddelta, dz [max_rows, d] (dz NULL iff z is), dB, dC [max_rows, groups * n], all float32 with row strides:
+ *           rows of the sequences are overwritten, others left untouched;
+ *   dA [n, d], dD [d] (NULL iff D is), ddelta_bias [d] (NULL iff delta_bias is): overwritten.
+ * Deterministic (sums over channels and rows in a fixed order).
+ * Workspace: mtgnn_selective_scan_ws_bytes(dims, max_rows, max_seq, 1). */
+typedef struct {
+  float *dx, *ddelta, *dB, *dC, *dz;
+  int64_t lddx, ldddelta, lddB, lddC, lddz;
+  float *dA, *dD, *ddelta_bias;
+} mtgnn_scan_grads;
+mtgnn_status mtgnn_selective_scan_bwd(const mtgnn_seqs* seqs, const float* dy, int64_t lddy,
+                                      const mtgnn_scan_inputs* in, const mtgnn_scan_dims* dims, const void* save,
+                                      const mtgnn_scan_grads* grads, void* ws, size_t ws_bytes,
+                                      hipStream_t stream);
+
+/* mtgnn_selective_scan for sequences of one row each, in one launch, as mtgnn_causal_conv_step. */
+mtgnn_status mtgnn_selective_scan_step(const int32_t* slot, const int32_t* n_rows, int64_t max_rows, int64_t n_slots,
+                                       const mtgnn_scan_inputs* in, const mtgnn_scan_dims* dims,
+                                       const float* state_in, float* state_out, void* y, int64_t ldy,
+                                       hipStream_t stream);
+
 /* ------------------------------------------------------------------ adaptive runtime controller
  * The decisions of one worker's runtime controller (Section V, Algorithm 2), kept on the host:
  *   gradient-norm EMA (Eq. 6):   g_bar = g_r if g_bar was 0, else alpha g_r + (1 - alpha) g_bar;

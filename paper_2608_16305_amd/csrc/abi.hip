@@ -14,7 +14,7 @@ void set_hip_error(hipError_t e, const char* where) {
   g_err = std::string(where) + ": " + hipGetErrorString(e);
 }
 
-static mtgnn_status fail(mtgnn_status s, const char* what) {
+mtgnn_status fail(mtgnn_status s, const char* what) {
   g_err = what;
   return s;
 }

@@ -5,6 +5,9 @@
 
 namespace mtgnn {
 
+// Keeps `what` for mtgnn_last_error() and returns s.
+mtgnn_status fail(mtgnn_status s, const char* what);
+
 // batch intake / memory phase
 size_t build_queries_ws(int64_t n);
 mtgnn_status build_queries_impl(const mtgnn_batch* b, const int32_t* neg, int32_t* q_node, float* q_t, int32_t* n_q,
@@ -246,5 +249,36 @@ mtgnn_status attn_bwd_impl(const int32_t* q_node, const float* q_t, const int32_
 mtgnn_status attn_bwd_group_impl(const int32_t* q_node, const int32_t* n_q, int64_t max_q, const int32_t* nbr,
                                  const void* save, const int32_t* uniq, const int32_t* n_rows, int64_t max_rows,
                                  const mtgnn_dims* d, void* ws, size_t ws_bytes, hipStream_t s);
+
+// state-space layer (linear.hip, conv.hip, scan.hip; arguments as in mtgnn.h, validated)
+size_t linear_ws(const mtgnn_linear_dims* d, int64_t rows, bool back);
+mtgnn_status linear_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W,
+                         const float* b, const void* res, int64_t ldr, const mtgnn_linear_dims* d, void* y,
+                         int64_t ldy, float* pre, void* ws, size_t ws_bytes, hipStream_t s);
+mtgnn_status linear_bwd_impl(const float* dy, int64_t lddy, const float* pre, const void* x, int64_t ldx,
+                             const int32_t* n_rows, int64_t max_rows, const void* W, const mtgnn_linear_dims* d,
+                             float* dx, int64_t lddx, float* dW, float* db, void* ws, size_t ws_bytes, hipStream_t s);
+size_t conv_save(const mtgnn_conv_dims* d, int64_t max_seq);
+size_t conv_ws(const mtgnn_conv_dims* d, int64_t rows);
+mtgnn_status conv_impl(const mtgnn_seqs* q, const void* x, int64_t ldx, const void* w, const float* b,
+                       const mtgnn_conv_dims* d, const void* state_in, void* state_out, void* y, int64_t ldy,
+                       void* save, hipStream_t s);
+mtgnn_status conv_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, const void* x, int64_t ldx,
+                           const void* w, const float* b, const mtgnn_conv_dims* d, const void* save, float* dx,
+                           int64_t lddx, float* dw, float* db, void* ws, hipStream_t s);
+mtgnn_status conv_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t max_rows, int64_t n_slots,
+                            const void* x, int64_t ldx, const void* w, const float* b, const mtgnn_conv_dims* d,
+                            const void* state_in, void* state_out, void* y, int64_t ldy, hipStream_t s);
+size_t scan_ws(const mtgnn_scan_dims* d, int64_t rows, bool back);
+size_t scan_save(const mtgnn_scan_dims* d, int64_t rows, int64_t max_seq, bool carried);
+mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d,
+                       const float* state_in, float* state_out, void* y, int64_t ldy, void* save, void* ws,
+                       hipStream_t s);
+mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, const mtgnn_scan_inputs* in,
+                           const mtgnn_scan_dims* d, const void* save, const mtgnn_scan_grads* g, void* ws,
+                           hipStream_t s);
+mtgnn_status scan_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t max_rows, int64_t n_slots,
+                            const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d, const float* state_in,
+                            float* state_out, void* y, int64_t ldy, hipStream_t s);
 
 }  // namespace mtgnn

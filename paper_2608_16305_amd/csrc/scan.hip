@@ -1,0 +1,882 @@
+// Selective state space scan over ragged sequences: whole sequences, their backward, and single rows.
+//
+//   dt = softplus(delta + delta_bias),  h_t = exp(dt A) h_(t-1) + dt B x,  y = (C . h + D x) silu(z)
+//
+// per channel and state.  The recurrence is linear in h, so rows are cut into chunks that are worked on at once:
+//   k_scan_local   each chunk's last state from zeros (or from the last start of a sequence in it) and the decay
+//                  over the chunk, exp(A sum dt): one exponential per chunk, not a product of many;
+//   k_scan_carry   the state that enters each chunk, over the chunks in order;
+//   k_scan_out     each chunk again from the state that enters it, now with y.
+// A chunk is a range of rows, whatever sequences they belong to: a start of a sequence inside it replaces the
+// state, so one sequence of 100,000 rows and 100,000 sequences of one row are the same amount of work per wave.
+// One chunk (few rows) needs k_scan_out alone.
+//
+// A block holds 64 channels of one group and all states: wave w the states 16 w .. 16 w + 15 (4 SPL of them, SPL = 4
+// where there is more than one wave), lane l the channels 4 (l / 4) .. + 3 and SPL states.  So the sum over the
+// states is one over four lanes (and the waves), the backward's sums over channels are over registers first,
+// and after the first of these lane l holds the value of channel l, as rows are read and written.
+// Rows are staged in LDS eight at a time: dt and dt x by the lane of their channel, B and C as they are.
+//
+// Vector instructions bound it: per row, channel and state the exponential takes a wave 16 cycles, the rest of
+// the recurrence and the sum over states 16, against 8 bytes per row and channel in bfloat16.
+#include <algorithm>
+
+#include "ops.h"
+#include "seq.h"
+
+namespace mtgnn {
+
+namespace {
+
+constexpr int TT = 8;      // rows of a tile, and of a checkpoint of the forward
+constexpr int CT = 64;     // channels of a block
+
+struct ScanP {
+  Seqs q;
+  const void *x, *delta, *B, *C, *z;
+  int64_t ldx, ldd, ldB, ldC, ldz;
+  const float *A, *D, *bias;
+  int d, n, groups, per, tpg, nct, softplus;   // per: channels of a group; tpg: tiles of a group; nct: tiles in all
+  int ch, nchunk, vec;                         // rows of a chunk; vec: four channels of a state row are 16-byte aligned
+  const float* st_in;
+  float* st_out;
+  void* y;
+  int64_t ldy;
+  float *hs, *init;                            // saved: checkpoints [rows / 8][n][d], first states [max_seq][n][d]
+  int32_t* carried;                            // saved: whether there are first states
+  float *E, *sumdt;                            // [nchunk][n][d], [nchunk][d]
+  int32_t* flag;                               // [nchunk]
+  // [nchunk][n][d] or NULL: where one table is read and written, the first state of a sequence that goes on in the
+  // next chunk.  Another block writes its slot, maybe before this one has read it; a sequence that ends in
+  // its chunk is read and written by the same threads.
+  float* first;
+};
+struct ScanG {
+  const float* dy;
+  int64_t lddy;
+  float *dx, *ddelta, *dB, *dC, *dz;
+  int64_t lddx, lddd, lddB, lddC, lddz;
+  float *part, *bc;                            // [nchunk][n + 2][d]; [nct][rows][2][n] (one tile per group: unused)
+};
+
+// What a chunk hands on: its own state plus the decayed one that enters; its own alone (a sequence starts in
+// it); nothing (the next chunk starts with a sequence, or there are no rows).
+enum { CARRY_ADD = 0, CARRY_OWN = 1, CARRY_NONE = 2 };
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int QUAD_XOR1 = 0xB1, QUAD_XOR2 = 0x4E, ROW_ROR4 = 0x124, ROW_ROR8 = 0x128;
+
+// Lane j of each four lanes gets the sum of v[j] over the four.
+__device__ __forceinline__ float quad_sums(const float (&v)[4]) {
+  const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
+  const float r0 = (b0 ? v[1] : v[0]) + dpp<QUAD_XOR1>(b0 ? v[0] : v[1]);
+  const float r1 = (b0 ? v[3] : v[2]) + dpp<QUAD_XOR1>(b0 ? v[2] : v[3]);
+  return (b1 ? r1 : r0) + dpp<QUAD_XOR2>(b1 ? r0 : r1);
+}
+
+// Four channels' values of one state row.  vec: p is 16-byte aligned wherever all four exist.
+__device__ __forceinline__ void load4(const float* p, int left, bool vec, float (&v)[4]) {
+  if (vec && left >= 4) {
+    const float4 f = *(const float4*)p;
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] = c < left ? p[c] : 0.f;
+}
+__device__ __forceinline__ void store4(float* p, int left, bool vec, float a, float b, float c, float d) {
+  if (vec && left >= 4) {
+    *(float4*)p = make_float4(a, b, c, d);
+    return;
+  }
+  if (left > 0) p[0] = a;
+  if (left > 1) p[1] = b;
+  if (left > 2) p[2] = c;
+  if (left > 3) p[3] = d;
+}
+
+// Where a thread stands.
+template <int SPL, int NB>
+struct Place {
+  static constexpr int NP = 4 * SPL * NB;
+  int lane, wid, cb, n0, g, ch0, left;   // cb: first of its channels in the block; left: channels of the group from ch0
+  __device__ __forceinline__ Place(const ScanP& p, int tile) {
+    lane = threadIdx.x & 63;
+    wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    cb = lane & ~3;
+    n0 = wid * 4 * SPL + (lane & 3) * SPL;
+    g = tile / p.tpg;
+    const int in = (tile % p.tpg) * CT;
+    ch0 = g * p.per + in;
+    left = min(CT, p.per - in);
+  }
+  // h of state table row `row` (of n x d floats)
+  __device__ __forceinline__ void load(const ScanP& p, const float* tab, int64_t row, float (&h)[4][SPL]) const {
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (n0 + s < p.n) load4(tab + (row * p.n + n0 + s) * p.d + ch0 + cb, left - cb, p.vec, v);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) h[c][s] = v[c];
+    }
+  }
+  __device__ __forceinline__ void store(const ScanP& p, float* tab, int64_t row, const float (&h)[4][SPL]) const {
+#pragma unroll
+    for (int s = 0; s < SPL; ++s)
+      if (n0 + s < p.n)
+        store4(tab + (row * p.n + n0 + s) * p.d + ch0 + cb, left - cb, p.vec, h[0][s], h[1][s], h[2][s], h[3][s]);
+  }
+  __device__ __forceinline__ void decay(const ScanP& p, float (&A2)[4][SPL]) const {   // A log2 e
+    load(p, p.A, 0, A2);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int s = 0; s < SPL; ++s) A2[c][s] *= LOG2E;
+  }
+};
+
+__device__ __forceinline__ void zero_state(float* h, int n) {
+  for (int i = 0; i < n; ++i) h[i] = 0.f;
+}
+
+// A tile's B or C rows (float, zero past the n states) into dst[TT][NP]; rows clamped to the last.
+template <typename T, int NP, int NT>
+__device__ __forceinline__ void stage_states(const void* src, int64_t ld, int n, int col0, int row, int last,
+                                             float* dst) {
+  for (int e = threadIdx.x; e < TT * NP; e += NT) {
+    const int i = e / NP, s = e % NP;
+    const float v = Elem<T>::load((const T*)src, (int64_t)min(row + i, last) * ld + col0 + min(s, n - 1));
+    dst[e] = s < n ? v : 0.f;
+  }
+}
+
+__device__ __forceinline__ float step_size(const ScanP& p, float u) { return p.softplus ? softplus_(u) : u; }
+
+template <int SPL>
+__device__ __forceinline__ void lds_get(const float* p, float (&v)[SPL]) {
+  if constexpr (SPL == 4) {
+    const float4 f = *(const float4*)p;
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else if constexpr (SPL == 2) {
+    const float2 f = *(const float2*)p;
+    v[0] = f.x; v[1] = f.y;
+  } else {
+    v[0] = p[0];
+  }
+}
+
+// Which rows of chunk c exist.
+__device__ __forceinline__ void chunk_rows(const ScanP& p, const SeqRange& r, int c, int& t0, int& t1) {
+  const int64_t a = (int64_t)c * p.ch;
+  t0 = (int)(a > r.lo ? a : r.lo);
+  t1 = (int)(a + p.ch < r.hi ? a + p.ch : r.hi);
+}
+
+// ------------------------------------------------------------------ forward
+
+template <typename T, int SPL, int NB>
+__global__ __launch_bounds__(64 * NB) void k_scan_local(ScanP p) {
+  using P = Place<SPL, NB>;
+  constexpr int NP = P::NP;
+  __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT];
+  __shared__ __align__(16) float s_B[TT * NP];
+  const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
+  const P me(p, tile);
+  const SeqRange r = seq_range(p.q);
+  int t0, t1;
+  chunk_rows(p, r, c, t0, t1);
+  int flag = CARRY_NONE;
+  SeqAt at{0, 0, 0};
+  if (t0 < t1) {
+    at = seq_find(p.q.off, r.n, t1 - 1);
+    if (at.end > t1) flag = at.beg >= t0 ? CARRY_OWN : CARRY_ADD;
+  }
+  if (tile == 0 && threadIdx.x == 0) p.flag[c] = flag;
+  if (flag == CARRY_NONE) return;
+  float A2[4][SPL], h[4][SPL];
+  me.decay(p, A2);
+  zero_state(&h[0][0], 4 * SPL);
+  int t = t0;
+  if (flag == CARRY_OWN) {
+    t = at.beg;
+    const int64_t k = p.st_in ? seq_slot(p.q.slot, p.q.n_slots, at.s) : -1;
+    if (k >= 0) me.load(p, p.st_in, k, h);
+    if (p.first) me.store(p, p.first, c, h);
+  }
+  const bool mine = me.lane < me.left;
+  const int col = me.ch0 + (mine ? me.lane : 0);
+  const float bias = p.bias ? p.bias[col] : 0.f;
+  float sum = 0.f;
+  for (; t < t1; t += TT) {
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (i % NB != me.wid) continue;
+      const int64_t row = min(t + i, t1 - 1);
+      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
+      const float x = Elem<T>::load((const T*)p.x, row * p.ldx + col);
+      const bool on = mine && t + i < t1;   // no row: dt = 0 leaves the state as it is
+      const float dt = on ? step_size(p, u + bias) : 0.f;
+      s_dt[i][me.lane] = dt;
+      s_dx[i][me.lane] = on ? dt * x : 0.f;
+      sum += dt;
+    }
+    stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, t, t1 - 1, s_B);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      float dt[4], dx[4], b[SPL];
+      lds_get<4>(&s_dt[i][me.cb], dt);
+      lds_get<4>(&s_dx[i][me.cb], dx);
+      lds_get<SPL>(&s_B[i * NP + me.n0], b);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int s = 0; s < SPL; ++s)
+          h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
+    }
+    __syncthreads();
+  }
+  me.store(p, p.E, c, h);
+  if constexpr (NB > 1) {
+    s_dt[me.wid][me.lane] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int w = 0; w < NB; ++w) sum += s_dt[w][me.lane];
+  }
+  if (me.wid == 0 && mine) p.sumdt[(int64_t)c * p.d + col] = sum;
+}
+
+// The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
+// first.  A thread per state and channel; eight chunks are requested at a time.
+__global__ __launch_bounds__(64) void k_scan_carry(ScanP p, int back) {
+  const int64_t nd = (int64_t)p.n * p.d, i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  if (i >= nd) return;
+  const int ch = (int)(i % p.d);
+  const float A2 = p.A[i] * LOG2E;
+  float h = 0.f;
+  constexpr int U = 8;
+  for (int c0 = 0; c0 < p.nchunk; c0 += U) {
+    float e[U], sd[U];
+    int f[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(c0 + u, p.nchunk - 1), c = back ? p.nchunk - 1 - k : k;
+      e[u] = p.E[c * nd + i];
+      sd[u] = p.sumdt[(int64_t)c * p.d + ch];
+      f[u] = p.flag[c];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c0 + u >= p.nchunk) break;
+      const int c = back ? p.nchunk - 1 - (c0 + u) : c0 + u;
+      p.E[c * nd + i] = h;
+      const float next = fmaf(__builtin_amdgcn_exp2f(A2 * sd[u]), h, e[u]);
+      h = f[u] == CARRY_ADD ? next : f[u] == CARRY_OWN ? e[u] : 0.f;
+    }
+  }
+}
+
+template <typename T, int SPL, int NB>
+__global__ __launch_bounds__(64 * NB) void k_scan_out(ScanP p) {
+  using P = Place<SPL, NB>;
+  constexpr int NP = P::NP;
+  __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT];
+  __shared__ __align__(16) float s_B[TT * NP], s_C[TT * NP];
+  __shared__ float s_y[NB > 1 ? NB : 1][TT][CT];
+  const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
+  const P me(p, tile);
+  if (p.carried && blockIdx.x == 0 && threadIdx.x == 0) *p.carried = p.st_in != nullptr;
+  const SeqRange r = seq_range(p.q);
+  int t0, t1;
+  chunk_rows(p, r, c, t0, t1);
+  if (t0 >= t1) return;
+  SeqWalk at(p.q, r, t0);
+  float A2[4][SPL], h[4][SPL];
+  me.decay(p, A2);
+  zero_state(&h[0][0], 4 * SPL);
+  if (at.beg < t0) me.load(p, p.E, c, h);
+  const bool mine = me.lane < me.left;
+  const int col = me.ch0 + (mine ? me.lane : 0);
+  const float bias = p.bias ? p.bias[col] : 0.f, D = p.D ? p.D[col] : 0.f;
+  for (int tb = t0 / TT * TT; tb < t1; tb += TT) {
+    float xr[TT], zr[TT], yr[TT];
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (i % NB != me.wid) continue;
+      const int64_t row = min(max(tb + i, t0), t1 - 1);
+      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
+      xr[i] = Elem<T>::load((const T*)p.x, row * p.ldx + col);
+      zr[i] = p.z ? Elem<T>::load((const T*)p.z, row * p.ldz + col) : 0.f;
+      const float dt = mine ? step_size(p, u + bias) : 0.f;
+      s_dt[i][me.lane] = dt;
+      s_dx[i][me.lane] = mine ? dt * xr[i] : 0.f;
+    }
+    stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, tb, t1 - 1, s_B);
+    stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, t1 - 1, s_C);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      const int t = tb + i;
+      if (t < t0) continue;
+      if (t >= t1) break;
+      if (t == at.beg) {
+        const int64_t k = p.st_in ? at.row() : -1;
+        if (k >= 0) me.load(p, p.first && at.end > t1 ? p.first : p.st_in, p.first && at.end > t1 ? c : k, h);
+        else zero_state(&h[0][0], 4 * SPL);
+        if (p.init) me.store(p, p.init, at.s, h);
+      } else if (i == 0 && p.hs) {
+        me.store(p, p.hs, tb / TT, h);
+      }
+      float dt[4], dx[4], b[SPL], cc[SPL], y[4];
+      lds_get<4>(&s_dt[i][me.cb], dt);
+      lds_get<4>(&s_dx[i][me.cb], dx);
+      lds_get<SPL>(&s_B[i * NP + me.n0], b);
+      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        y[k] = 0.f;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) {
+          h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
+          y[k] = fmaf(h[k][s], cc[s], y[k]);
+        }
+      }
+      yr[i] = quad_sums(y);
+      if constexpr (NB > 1) s_y[me.wid][i][me.lane] = yr[i];
+      if (t + 1 == at.end) {
+        if (p.st_out) {
+          const int64_t k = at.row();
+          if (k >= 0) me.store(p, p.st_out, k, h);
+        }
+        at.next();
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (i % NB != me.wid || tb + i < t0 || tb + i >= t1) continue;
+      float v = yr[i];
+      if constexpr (NB > 1) {
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < NB; ++w) v += s_y[w][i][me.lane];
+      }
+      v = fmaf(D, xr[i], v);
+      if (p.z) v *= silu_(zr[i]);
+      if (mine) Elem<T>::store((T*)p.y, (int64_t)(tb + i) * p.ldy + col, v);
+    }
+    if constexpr (NB > 1) __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ backward
+//
+// With e = dy silu(z): g_t = C_t e_t + a_(t+1) g_(t+1), the gradient of h_t; what a chunk hands to the one before
+// it is r = a_t g_t at its first row, again a linear recurrence (k_scan_back_local, k_scan_carry).
+// k_scan_back then goes over a chunk's tiles from the last to the first: each tile's states forwards from the
+// forward's checkpoint, kept in registers (eight rows of them, why a checkpoint is every eight), then g backwards.
+
+template <typename T, int SPL, int NB>
+__global__ __launch_bounds__(64 * NB) void k_scan_back_local(ScanP p, ScanG o) {
+  using P = Place<SPL, NB>;
+  constexpr int NP = P::NP;
+  __shared__ __align__(16) float s_dt[TT][CT], s_e[TT][CT];
+  __shared__ __align__(16) float s_C[TT * NP];
+  const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
+  const P me(p, tile);
+  const SeqRange r = seq_range(p.q);
+  int t0, t1;
+  chunk_rows(p, r, c, t0, t1);
+  int flag = CARRY_NONE;
+  SeqAt at{0, 0, 0};
+  if (t0 < t1) {
+    at = seq_find(p.q.off, r.n, t0);
+    if (at.beg < t0) flag = at.end <= t1 ? CARRY_OWN : CARRY_ADD;
+  }
+  if (tile == 0 && threadIdx.x == 0) p.flag[c] = flag;
+  if (flag == CARRY_NONE) return;
+  const int stop = min(at.end, t1);
+  float A2[4][SPL], g[4][SPL];
+  me.decay(p, A2);
+  zero_state(&g[0][0], 4 * SPL);
+  const bool mine = me.lane < me.left;
+  const int col = me.ch0 + (mine ? me.lane : 0);
+  const float bias = p.bias ? p.bias[col] : 0.f;
+  float sum = 0.f;
+  for (int tb = t0 + (stop - 1 - t0) / TT * TT; tb >= t0; tb -= TT) {
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (i % NB != me.wid) continue;
+      const int64_t row = min(tb + i, stop - 1);
+      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
+      const float z = p.z ? Elem<T>::load((const T*)p.z, row * p.ldz + col) : 0.f;
+      float e = o.dy[row * o.lddy + col];
+      if (p.z) e *= silu_(z);
+      const bool on = mine && tb + i < stop;
+      const float dt = on ? step_size(p, u + bias) : 0.f;
+      s_dt[i][me.lane] = dt;
+      s_e[i][me.lane] = on ? e : 0.f;
+      sum += dt;
+    }
+    stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, stop - 1, s_C);
+    __syncthreads();
+#pragma unroll
+    for (int i = TT - 1; i >= 0; --i) {
+      float dt[4], e[4], cc[SPL];
+      lds_get<4>(&s_dt[i][me.cb], dt);
+      lds_get<4>(&s_e[i][me.cb], e);
+      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int s = 0; s < SPL; ++s)
+          g[k][s] = __builtin_amdgcn_exp2f(dt[k] * A2[k][s]) * fmaf(e[k], cc[s], g[k][s]);
+    }
+    __syncthreads();
+  }
+  me.store(p, p.E, c, g);
+  if constexpr (NB > 1) {
+    s_dt[me.wid][me.lane] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int w = 0; w < NB; ++w) sum += s_dt[w][me.lane];
+  }
+  if (me.wid == 0 && mine) p.sumdt[(int64_t)c * p.d + col] = sum;
+}
+
+template <typename T, int SPL, int NB>
+__global__ __launch_bounds__(64 * NB, 1) void k_scan_back(ScanP p, ScanG o) {
+  using P = Place<SPL, NB>;
+  constexpr int NP = P::NP;
+  __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT], s_e[TT][CT];
+  __shared__ float s_x[TT][CT], s_s[TT][CT], s_z[TT][CT];     // x, d dt / d delta, dy silu'(z)
+  __shared__ __align__(16) float s_B[TT * NP], s_C[TT * NP];
+  __shared__ __align__(16) float s_bc[TT][4][2][NP];          // dB, dC of a tile, from each 16 lanes
+  __shared__ float s_red[NB > 1 ? NB : 1][3][NB > 1 ? TT : 1][CT];
+  const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
+  const P me(p, tile);
+  const SeqRange r = seq_range(p.q);
+  int t0, t1;
+  chunk_rows(p, r, c, t0, t1);
+  if (t0 >= t1) return;
+  SeqWalk at(p.q, r, t1 - 1);
+  const float* init = *p.carried ? p.init : nullptr;
+  float A2[4][SPL], f[4][SPL], dA[4][SPL];   // f: what flows from the row behind
+  me.decay(p, A2);
+  zero_state(&f[0][0], 4 * SPL);
+  zero_state(&dA[0][0], 4 * SPL);
+  if (p.nchunk > 1 && at.end > t1) me.load(p, p.E, c, f);
+  const bool mine = me.lane < me.left;
+  const int col = me.ch0 + (mine ? me.lane : 0);
+  const float bias = p.bias ? p.bias[col] : 0.f, D = p.D ? p.D[col] : 0.f;
+  float dD = 0.f, db = 0.f;
+  for (int tb = (t1 - 1) / TT * TT; tb + TT > t0; tb -= TT) {
+    const int tlo = max(tb, t0), thi = min(tb + TT, t1);
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (i % NB != me.wid) continue;
+      const int64_t row = min(max(tb + i, t0), t1 - 1);
+      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col) + bias;
+      const float x = Elem<T>::load((const T*)p.x, row * p.ldx + col);
+      const float dy = o.dy[row * o.lddy + col];
+      float e = dy;
+      if (p.z) {
+        const float z = Elem<T>::load((const T*)p.z, row * p.ldz + col);
+        const float sg = sigmoid_exact(z);
+        e = dy * (z * sg);
+        s_z[i][me.lane] = dy * (sg * fmaf(z, 1.f - sg, 1.f));
+      }
+      s_x[i][me.lane] = x;
+      s_s[i][me.lane] = p.softplus ? sigmoid_exact(u) : 1.f;
+      const float dt = mine ? step_size(p, u) : 0.f;
+      s_dt[i][me.lane] = dt;
+      s_dx[i][me.lane] = mine ? dt * x : 0.f;
+      s_e[i][me.lane] = mine ? e : 0.f;
+    }
+    stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, tb, t1 - 1, s_B);
+    stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, t1 - 1, s_C);
+    __syncthreads();
+    // the states that enter each row of the tile
+    float hb[TT][4][SPL];
+    while (at.beg > tlo) at.prev();
+    {
+      float h[4][SPL];
+      zero_state(&h[0][0], 4 * SPL);
+      if (at.beg < tlo) me.load(p, p.hs, tb / TT, h);
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const int t = tb + i;
+        if (t >= tlo && t < thi) {
+          if (t == at.end) at.next();
+          if (t == at.beg) {
+            if (init && at.row() >= 0) me.load(p, init, at.s, h);
+            else zero_state(&h[0][0], 4 * SPL);
+          }
+        }
+        float dt[4], dx[4], b[SPL];
+        lds_get<4>(&s_dt[i][me.cb], dt);
+        lds_get<4>(&s_dx[i][me.cb], dx);
+        lds_get<SPL>(&s_B[i * NP + me.n0], b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int s = 0; s < SPL; ++s) {
+            hb[i][k][s] = h[k][s];
+            h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
+          }
+      }
+    }
+    // the decays and inputs are formed again below: kept from above they would be hundreds of registers
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int s = 0; s < SPL; ++s) keep_live(A2[k][s]);
+    // what a row's channel gets (lane l: channel l) once its sums over the states are complete
+    const auto finish = [&](int i, float y, float sx, float su) {
+      const int64_t t = tb + i;
+      const float x = s_x[i][me.lane], e = s_e[i][me.lane];
+      const float du = fmaf(sx, x, su * LN2) * s_s[i][me.lane];
+      if (mine) {
+        o.dx[t * o.lddx + col] = fmaf(D, e, sx * s_dt[i][me.lane]);
+        o.ddelta[t * o.lddd + col] = du;
+        if (p.z) o.dz[t * o.lddz + col] = s_z[i][me.lane] * fmaf(D, x, y);
+      }
+      dD = fmaf(e, x, dD);
+      db += du;
+    };
+#pragma unroll
+    for (int i = TT - 1; i >= 0; --i) {
+      const int t = tb + i;
+      if (t < tlo || t >= thi) continue;
+      while (at.beg > t) at.prev();
+      if (t + 1 == at.end) zero_state(&f[0][0], 4 * SPL);
+      float dt[4], dx[4], e[4], b[SPL], cc[SPL], y4[4], x4[4], u4[4], vB[SPL], vC[SPL];
+      lds_get<4>(&s_dt[i][me.cb], dt);
+      lds_get<4>(&s_dx[i][me.cb], dx);
+      lds_get<4>(&s_e[i][me.cb], e);
+      lds_get<SPL>(&s_B[i * NP + me.n0], b);
+      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+#pragma unroll
+      for (int s = 0; s < SPL; ++s) vB[s] = vC[s] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        y4[k] = x4[k] = u4[k] = 0.f;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) {
+          const float a = __builtin_amdgcn_exp2f(dt[k] * A2[k][s]);
+          const float h = fmaf(a, hb[i][k][s], dx[k] * b[s]);
+          const float g = fmaf(e[k], cc[s], f[k][s]);
+          f[k][s] = a * g;
+          const float w = f[k][s] * hb[i][k][s];
+          y4[k] = fmaf(h, cc[s], y4[k]);
+          x4[k] = fmaf(g, b[s], x4[k]);
+          u4[k] = fmaf(w, A2[k][s], u4[k]);
+          dA[k][s] = fmaf(w, dt[k], dA[k][s]);
+          vB[s] = fmaf(g, dx[k], vB[s]);
+          vC[s] = fmaf(h, e[k], vC[s]);
+        }
+      }
+      const float y = quad_sums(y4), sx = quad_sums(x4), su = quad_sums(u4);
+      if constexpr (NB > 1) {
+        s_red[me.wid][0][i][me.lane] = y;
+        s_red[me.wid][1][i][me.lane] = sx;
+        s_red[me.wid][2][i][me.lane] = su;
+      } else {
+        finish(i, y, sx, su);
+      }
+#pragma unroll
+      for (int s = 0; s < SPL; ++s) {
+        vB[s] += dpp<ROW_ROR4>(vB[s]);
+        vC[s] += dpp<ROW_ROR4>(vC[s]);
+        vB[s] += dpp<ROW_ROR8>(vB[s]);
+        vC[s] += dpp<ROW_ROR8>(vC[s]);
+      }
+      if ((me.lane & 12) == 0) {
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) {
+          s_bc[i][me.lane >> 4][0][me.n0 + s] = vB[s];
+          s_bc[i][me.lane >> 4][1][me.n0 + s] = vC[s];
+        }
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < TT * 2 * NP; e += 64 * NB) {
+      const int i = e / (2 * NP), w = e / NP & 1, s = e % NP, t = tb + i;
+      if (t < tlo || t >= thi || s >= p.n) continue;
+      const float v = (s_bc[i][0][w][s] + s_bc[i][1][w][s]) + (s_bc[i][2][w][s] + s_bc[i][3][w][s]);
+      if (p.tpg > 1) o.bc[(((int64_t)tile * p.q.max_rows + t) * 2 + w) * p.n + s] = v;
+      else if (w == 0) o.dB[(int64_t)t * o.lddB + me.g * p.n + s] = v;
+      else o.dC[(int64_t)t * o.lddC + me.g * p.n + s] = v;
+    }
+    if constexpr (NB > 1) {
+      for (int i = me.wid; i < TT; i += NB) {
+        if (tb + i < tlo || tb + i >= thi) continue;
+        float v[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NB; ++w)
+#pragma unroll
+          for (int k = 0; k < 3; ++k) v[k] += s_red[w][k][i][me.lane];
+        finish(i, v[0], v[1], v[2]);
+      }
+    }
+    __syncthreads();
+  }
+  float* part = o.part + (int64_t)c * (p.n + 2) * p.d;
+  me.store(p, part, 0, dA);
+  if constexpr (NB > 1) {
+    s_dt[me.wid][me.lane] = dD;
+    s_dx[me.wid][me.lane] = db;
+    __syncthreads();
+    dD = db = 0.f;
+    for (int w = 0; w < NB; ++w) {
+      dD += s_dt[w][me.lane];
+      db += s_dx[w][me.lane];
+    }
+  }
+  if (me.wid == 0 && mine) {
+    part[(int64_t)p.n * p.d + col] = dD;
+    part[(int64_t)(p.n + 1) * p.d + col] = db;
+  }
+}
+
+// dB, dC from the tiles' shares: a thread per row, operand, group and state.
+__global__ __launch_bounds__(256) void k_scan_sum_bc(ScanP p, ScanG o) {
+  const SeqRange r = seq_range(p.q);
+  const int gn = p.groups * p.n;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = e / (2 * gn);
+  if (t < r.lo || t >= r.hi) return;
+  const int w = (int)(e / gn & 1), j = (int)(e % gn), g = j / p.n, s = j % p.n;
+  float v = 0.f;
+  for (int k = 0; k < p.tpg; ++k) v += o.bc[(((int64_t)(g * p.tpg + k) * p.q.max_rows + t) * 2 + w) * p.n + s];
+  if (w == 0) o.dB[t * o.lddB + j] = v;
+  else o.dC[t * o.lddC + j] = v;
+}
+
+// ------------------------------------------------------------------ single rows
+
+// A thread per row and channel: its states, strided by d, are n independent reads and writes (256 bytes a wave
+// each); state traffic bounds it.
+template <typename T>
+__global__ __launch_bounds__(256) void k_scan_step(ScanP p, const int32_t* n_rows, int64_t max_rows) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = e / p.d;
+  if (row >= eff_count(max_rows, n_rows)) return;
+  const int ch = (int)(e % p.d), g = ch / p.per;
+  const int64_t k = seq_slot(p.q.slot, p.q.n_slots, row);
+  const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + ch) + (p.bias ? p.bias[ch] : 0.f);
+  const float x = Elem<T>::load((const T*)p.x, row * p.ldx + ch);
+  const float dt = step_size(p, u), dx = dt * x;
+  const T *B = (const T*)p.B + row * p.ldB + g * p.n, *C = (const T*)p.C + row * p.ldC + g * p.n;
+  const float* in = p.st_in && k >= 0 ? p.st_in + k * p.n * p.d + ch : nullptr;
+  float* out = p.st_out && k >= 0 ? p.st_out + k * p.n * p.d + ch : nullptr;
+  float y = 0.f;
+  for (int i = 0; i < p.n; ++i) {
+    const float a = __builtin_amdgcn_exp2f(dt * (p.A[(int64_t)i * p.d + ch] * LOG2E));
+    const float h0 = in ? in[(int64_t)i * p.d] : 0.f;
+    const float h = fmaf(a, h0, dx * Elem<T>::load(B, i));
+    if (out) out[(int64_t)i * p.d] = h;
+    y = fmaf(h, Elem<T>::load(C, i), y);
+  }
+  if (p.D) y = fmaf(p.D[ch], x, y);
+  if (p.z) y *= silu_(Elem<T>::load((const T*)p.z, row * p.ldz + ch));
+  Elem<T>::store((T*)p.y, row * p.ldy + ch, y);
+}
+
+// ------------------------------------------------------------------ host
+
+int scan_tiles(const mtgnn_scan_dims* d) { return d->groups * (int)cdiv(d->d / d->groups, CT); }
+
+// Rows of a chunk (a multiple of TT): enough chunks for `waves` waves.
+int scan_chunk(const mtgnn_scan_dims* d, int64_t rows, int64_t waves) {
+  const int64_t blocks = std::max<int64_t>(1, waves / (scan_tiles(d) * cdiv(d->n, 16)));
+  const int64_t ch = cdiv(cdiv(std::max<int64_t>(rows, 1), blocks), TT) * TT;
+  return (int)std::min<int64_t>(ch, int64_t(1) << 30);
+}
+constexpr int64_t FWD_WAVES = 4096, BWD_WAVES = 2048;
+
+size_t al(size_t b) { return (b + 255) & ~size_t(255); }
+
+ScanP scan_params(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d) {
+  ScanP p{};
+  if (q) p.q = seqs_of(q);
+  p.x = in->x; p.delta = in->delta; p.B = in->B; p.C = in->C; p.z = in->z;
+  p.ldx = in->ldx; p.ldd = in->lddelta; p.ldB = in->ldB; p.ldC = in->ldC; p.ldz = in->ldz;
+  p.A = in->A; p.D = in->D; p.bias = in->delta_bias;
+  p.d = d->d; p.n = d->n; p.groups = d->groups; p.per = d->d / d->groups;
+  p.tpg = (int)cdiv(p.per, CT); p.nct = d->groups * p.tpg; p.softplus = d->softplus;
+  return p;
+}
+// Every state row's groups of four channels that a thread takes are 16-byte aligned.
+int scan_vec(const ScanP& p, const void* a, const void* b) {
+  return p.d % 4 == 0 && p.per % 4 == 0 && ((uintptr_t)a | (uintptr_t)b | (uintptr_t)p.A) % 16 == 0;
+}
+
+struct ScanWs {
+  size_t E, sumdt, flag, first, part, bc, total;
+};
+ScanWs scan_ws_layout(const mtgnn_scan_dims* d, int64_t rows, bool back) {
+  const int64_t nchunk = cdiv(std::max<int64_t>(rows, 1), scan_chunk(d, rows, back ? BWD_WAVES : FWD_WAVES));
+  const size_t nd = (size_t)d->n * d->d;
+  ScanWs w{};
+  size_t o = 0;
+  w.E = o; o += al(nchunk * nd * 4);
+  w.sumdt = o; o += al(nchunk * (size_t)d->d * 4);
+  w.flag = o; o += al(nchunk * 4);
+  w.first = o; if (!back) o += al(nchunk * nd * 4);
+  w.part = o; if (back) o += al(nchunk * (nd + 2 * (size_t)d->d) * 4);
+  w.bc = o;
+  const int nct = scan_tiles(d);
+  if (back && nct > d->groups) o += al((size_t)nct * rows * 2 * d->n * 4);
+  w.total = o;
+  return w;
+}
+
+template <typename F>
+void scan_variant(int dtype, int n, F f) {
+  const auto by = [&](auto t) {
+    using T = decltype(t);
+    if (n <= 4) f.template operator()<T, 1, 1>();
+    else if (n <= 8) f.template operator()<T, 2, 1>();
+    else if (n <= 16) f.template operator()<T, 4, 1>();
+    else if (n <= 32) f.template operator()<T, 4, 2>();
+    else if (n <= 48) f.template operator()<T, 4, 3>();
+    else f.template operator()<T, 4, 4>();
+  };
+  if (dtype == MTGNN_BF16) by(uint16_t{});
+  else by(float{});
+}
+
+struct LaunchLocal {
+  const ScanP& p;
+  unsigned grid;
+  hipStream_t s;
+  template <typename T, int SPL, int NB> void operator()() const { k_scan_local<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p); }
+};
+struct LaunchOut {
+  const ScanP& p;
+  unsigned grid;
+  hipStream_t s;
+  template <typename T, int SPL, int NB> void operator()() const { k_scan_out<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p); }
+};
+struct LaunchBackLocal {
+  const ScanP& p;
+  const ScanG& g;
+  unsigned grid;
+  hipStream_t s;
+  template <typename T, int SPL, int NB> void operator()() const {
+    k_scan_back_local<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p, g);
+  }
+};
+struct LaunchBack {
+  const ScanP& p;
+  const ScanG& g;
+  unsigned grid;
+  hipStream_t s;
+  template <typename T, int SPL, int NB> void operator()() const { k_scan_back<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p, g); }
+};
+
+}  // namespace
+
+size_t scan_ws(const mtgnn_scan_dims* d, int64_t rows, bool back) { return scan_ws_layout(d, rows, back).total; }
+
+// Saved: a flag (whether there are first states), the checkpoints, the first states.
+size_t scan_save(const mtgnn_scan_dims* d, int64_t rows, int64_t max_seq, bool carried) {
+  const size_t nd = (size_t)d->n * d->d * 4;
+  return 256 + al(cdiv(std::max<int64_t>(rows, 1), TT) * nd) + (carried ? al(max_seq * nd) : 0);
+}
+static void scan_save_at(ScanP& p, const mtgnn_scan_dims* d, int64_t rows, void* save) {
+  char* b = (char*)save;
+  p.carried = (int32_t*)b;
+  p.hs = (float*)(b + 256);
+  p.init = (float*)(b + 256 + al(cdiv(std::max<int64_t>(rows, 1), TT) * ((size_t)d->n * d->d * 4)));
+}
+
+mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d,
+                       const float* state_in, float* state_out, void* y, int64_t ldy, void* save, void* ws,
+                       hipStream_t s) {
+  ScanP p = scan_params(q, in, d);
+  const int64_t rows = q->max_rows;
+  p.ch = scan_chunk(d, rows, FWD_WAVES);
+  p.nchunk = (int)cdiv(rows, p.ch);
+  p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
+  p.vec = scan_vec(p, state_in, state_out);
+  if (save) {
+    scan_save_at(p, d, rows, save);
+    if (!state_in) p.init = nullptr;
+  }
+  const ScanWs w = scan_ws_layout(d, rows, false);
+  p.E = (float*)((char*)ws + w.E);
+  p.sumdt = (float*)((char*)ws + w.sumdt);
+  p.flag = (int32_t*)((char*)ws + w.flag);
+  if (state_in && state_in == state_out && p.nchunk > 1) p.first = (float*)((char*)ws + w.first);
+  const unsigned grid = (unsigned)((int64_t)p.nchunk * p.nct);
+  if (p.nchunk > 1) {
+    scan_variant(d->dtype, d->n, LaunchLocal{p, grid, s});
+    MTGNN_CHECK_LAUNCH("scan_local");
+    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, 64), 64, 0, s>>>(p, 0);
+    MTGNN_CHECK_LAUNCH("scan_carry");
+  }
+  scan_variant(d->dtype, d->n, LaunchOut{p, grid, s});
+  MTGNN_CHECK_LAUNCH("scan_out");
+  return MTGNN_OK;
+}
+
+mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, const mtgnn_scan_inputs* in,
+                           const mtgnn_scan_dims* d, const void* save, const mtgnn_scan_grads* g, void* ws,
+                           hipStream_t s) {
+  ScanP p = scan_params(q, in, d);
+  const int64_t rows = q->max_rows;
+  p.ch = scan_chunk(d, rows, BWD_WAVES);
+  p.nchunk = (int)cdiv(rows, p.ch);
+  p.vec = scan_vec(p, nullptr, nullptr);
+  scan_save_at(p, d, rows, const_cast<void*>(save));
+  const ScanWs w = scan_ws_layout(d, rows, true);
+  p.E = (float*)((char*)ws + w.E);
+  p.sumdt = (float*)((char*)ws + w.sumdt);
+  p.flag = (int32_t*)((char*)ws + w.flag);
+  ScanG o{};
+  o.dy = dy; o.lddy = lddy;
+  o.dx = g->dx; o.ddelta = g->ddelta; o.dB = g->dB; o.dC = g->dC; o.dz = g->dz;
+  o.lddx = g->lddx; o.lddd = g->ldddelta; o.lddB = g->lddB; o.lddC = g->lddC; o.lddz = g->lddz;
+  o.part = (float*)((char*)ws + w.part);
+  o.bc = (float*)((char*)ws + w.bc);
+  const unsigned grid = (unsigned)((int64_t)p.nchunk * p.nct);
+  if (p.nchunk > 1) {
+    scan_variant(d->dtype, d->n, LaunchBackLocal{p, o, grid, s});
+    MTGNN_CHECK_LAUNCH("scan_back_local");
+    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, 64), 64, 0, s>>>(p, 1);
+    MTGNN_CHECK_LAUNCH("scan_carry");
+  }
+  scan_variant(d->dtype, d->n, LaunchBack{p, o, grid, s});
+  MTGNN_CHECK_LAUNCH("scan_back");
+  if (p.tpg > 1) {
+    k_scan_sum_bc<<<(unsigned)cdiv(rows * 2 * d->groups * d->n, 256), 256, 0, s>>>(p, o);
+    MTGNN_CHECK_LAUNCH("scan_sum_bc");
+  }
+  const int64_t nd = (int64_t)d->n * d->d;
+  k_sum_parts<<<(unsigned)cdiv(nd + 2 * d->d, 16), 256, 0, s>>>(p.q, p.ch, o.part, nd + 2 * d->d, nd, g->dA, d->d,
+                                                                g->dD, g->ddelta_bias);
+  MTGNN_CHECK_LAUNCH("scan_sum_parts");
+  return MTGNN_OK;
+}
+
+mtgnn_status scan_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t max_rows, int64_t n_slots,
+                            const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d, const float* state_in,
+                            float* state_out, void* y, int64_t ldy, hipStream_t s) {
+  ScanP p = scan_params(nullptr, in, d);
+  p.q.slot = slot;
+  p.q.n_slots = n_slots;
+  p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
+  const unsigned grid = (unsigned)cdiv(max_rows * d->d, 256);
+  if (d->dtype == MTGNN_BF16) k_scan_step<uint16_t><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+  else k_scan_step<float><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+  MTGNN_CHECK_LAUNCH("scan_step");
+  return MTGNN_OK;
+}
+
+}  // namespace mtgnn

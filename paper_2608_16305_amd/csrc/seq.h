@@ -1,0 +1,187 @@
+// Sequences laid one after the other in the rows of a matrix (mtgnn_seqs), as the convolution and the scan walk them.
+#pragma once
+
+#include "common.h"
+
+namespace mtgnn {
+
+// 2^(v log2 e) and the like on the hardware's exponential, and the activations built on it.
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// softplus(u) = max(u, 0) + log1p(e^-|u|).  log1p(v) = 2 atanh(s) with s = v / (2 + v) <= 1/3, by its series to s^17
+// (the rest is below 2^-27 of it): exact to a few units of the last place for every v, small ones too, where
+// log(1 + v) has lost v's low bits.
+__device__ __forceinline__ float softplus_(float u) {
+  const float v = expf(-fabsf(u));
+  const float s = v * __builtin_amdgcn_rcpf(2.f + v), q = s * s;
+  float p = 1.f / 17.f;
+  p = fmaf(p, q, 1.f / 15.f);
+  p = fmaf(p, q, 1.f / 13.f);
+  p = fmaf(p, q, 1.f / 11.f);
+  p = fmaf(p, q, 1.f / 9.f);
+  p = fmaf(p, q, 1.f / 7.f);
+  p = fmaf(p, q, 1.f / 5.f);
+  p = fmaf(p, q, 1.f / 3.f);
+  p = fmaf(p, q, 1.f);
+  return fmaxf(u, 0.f) + 2.f * s * p;   // a NaN stays one through v
+}
+__device__ __forceinline__ float sigmoid_exact(float u) { return __builtin_amdgcn_rcpf(1.f + expf(-u)); }
+__device__ __forceinline__ float silu_(float p) { return p * sigmoid_exact(p); }
+__device__ __forceinline__ float dsilu_(float p) {
+  const float s = sigmoid_exact(p);
+  return s * fmaf(p, 1.f - s, 1.f);
+}
+// act and its derivative for mtgnn_act `act` (uniform).
+__device__ __forceinline__ float act_(int act, float p) {
+  if (act == MTGNN_ACT_SILU) return silu_(p);
+  if (act == MTGNN_ACT_RELU) return p < 0.f ? 0.f : p;   // a NaN stays one
+  if (act == MTGNN_ACT_GELU) return 0.5f * p * (1.f + erff(p * 0.70710678118654752f));
+  return p;
+}
+__device__ __forceinline__ float dact_(int act, float p) {
+  if (act == MTGNN_ACT_SILU) return dsilu_(p);
+  if (act == MTGNN_ACT_RELU) return p > 0.f ? 1.f : 0.f;
+  if (act == MTGNN_ACT_GELU)
+    return 0.5f * (1.f + erff(p * 0.70710678118654752f)) + p * expf(-0.5f * p * p) * 0.3989422804014327f;
+  return 1.f;
+}
+
+struct Seqs {
+  const int32_t *off, *n_seq, *slot;
+  int64_t max_seq, max_rows, n_slots;
+};
+inline Seqs seqs_of(const mtgnn_seqs* q) {
+  return Seqs{q->off, q->n_seq, q->slot, q->max_seq, q->max_rows, q->n_slots};
+}
+
+// The rows of all sequences: [lo, hi), and the number of sequences.
+struct SeqRange {
+  int n, lo, hi;
+};
+__device__ __forceinline__ SeqRange seq_range(const Seqs& q) {
+  SeqRange r{(int)q.max_seq, 0, 0};
+  if (q.n_seq) {
+    const int c = *q.n_seq;
+    r.n = c < 0 ? 0 : c < r.n ? c : r.n;
+  }
+  if (r.n > 0) {
+    const int lo = q.off[0], hi = q.off[r.n];
+    r.lo = lo < 0 ? 0 : lo;
+    r.hi = hi < (int)q.max_rows ? hi : (int)q.max_rows;
+  }
+  return r;
+}
+
+// The sequence that holds row t (lo <= t < hi) and its rows [beg, end).  Found by the whole wave: each round
+// compares 64 evenly spaced starts at once, so 262,144 sequences take three dependent reads, not eighteen.
+struct SeqAt {
+  int s, beg, end;
+};
+__device__ __forceinline__ SeqAt seq_find(const int32_t* off, int n, int t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, cnt = n;
+  while (cnt > 1) {
+    const int step = (cnt + 63) >> 6, i = lane * step;
+    const bool le = i < cnt && off[lo + (i < cnt ? i : 0)] <= t;
+    const int k = __popcll(__ballot(le));
+    const int j = (k > 0 ? k - 1 : 0) * step;
+    lo += j;
+    cnt = cnt - j < step ? cnt - j : step;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  return SeqAt{lo, off[lo], off[lo + 1]};
+}
+// A walk over the sequences.  The wave holds 64 consecutive starts (lane l: off[w0 + l]) and their slots and reads
+// them from its lanes: a start costs a register read, not a dependent trip to memory.
+struct SeqWalk {
+  const int32_t *off, *slot;
+  int64_t n_slots;
+  int n, s, beg, end, w0, v_off, v_slot;
+  __device__ __forceinline__ SeqWalk(const Seqs& q, const SeqRange& r, int t) : off(q.off), slot(q.slot), n_slots(q.n_slots), n(r.n) {
+    const SeqAt a = seq_find(off, n, t);
+    s = a.s;
+    beg = a.beg;
+    end = a.end;
+    window(s);
+  }
+  __device__ __forceinline__ void window(int at) {
+    const int lane = threadIdx.x & 63;
+    w0 = at < 0 ? 0 : at;
+    v_off = off[min(w0 + lane, n)];
+    v_slot = slot ? slot[min(w0 + lane, n - 1)] : w0 + lane;
+  }
+  __device__ __forceinline__ int off_at(int i, bool back) {   // off[i], 0 <= i <= n
+    if (i < w0 || i > w0 + 63) window(back ? i - 63 : i - 1);
+    return __builtin_amdgcn_readlane(v_off, i - w0);
+  }
+  // To the next (previous) sequence that has rows; stays at the last (first) one.
+  __device__ __forceinline__ void next() {
+    do {
+      if (s + 1 >= n) {
+        beg = end;
+        return;
+      }
+      ++s;
+      beg = end;
+      end = off_at(s + 1, false);
+    } while (end <= beg);
+  }
+  __device__ __forceinline__ void prev() {
+    do {
+      if (s == 0) {
+        end = beg;
+        return;
+      }
+      --s;
+      end = beg;
+      beg = off_at(s, true);
+    } while (end <= beg);
+  }
+  // The table row of the sequence, or -1: no carried state.
+  __device__ __forceinline__ int64_t row() {
+    if (s < w0 || s > w0 + 63) window(s - 32);
+    const int k = __builtin_amdgcn_readlane(v_slot, s - w0);
+    return k >= 0 && k < n_slots ? k : -1;
+  }
+};
+// The table row of sequence (or single row) s, or -1: no carried state.
+__device__ __forceinline__ int64_t seq_slot(const int32_t* slot, int64_t n_slots, int64_t s) {
+  const int64_t k = slot ? (int64_t)slot[s] : s;
+  return k >= 0 && k < n_slots ? k : -1;
+}
+
+namespace {
+
+// Column sums of the chunks' shares part[chunk][cols] in order, into up to three tensors of n0, n1, cols - n0 - n1
+// columns (each may be NULL); a chunk is `ch` rows, and only those with rows have a share.  16 columns a
+// block, 16 threads to each.
+__global__ __launch_bounds__(256) void k_sum_parts(Seqs q, int ch, const float* part, int64_t cols, int64_t n0,
+                                                   float* out0, int64_t n1, float* out1, float* out2) {
+  __shared__ float s[16][17];
+  const SeqRange r = seq_range(q);
+  const int j = threadIdx.x & 15, k = threadIdx.x >> 4;
+  const int64_t col = (int64_t)blockIdx.x * 16 + j;
+  const int c0 = r.lo < r.hi ? r.lo / ch : 0, c1 = r.lo < r.hi ? (r.hi - 1) / ch + 1 : 0;
+  float v = 0.f;
+  if (col < cols)
+    for (int c = c0 + k; c < c1; c += 16) v += part[c * cols + col];
+  s[k][j] = v;
+  __syncthreads();
+  if (k == 0 && col < cols) {
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += s[i][j];
+    if (col < n0) {
+      if (out0) out0[col] = v;
+    } else if (col < n0 + n1) {
+      if (out1) out1[col - n0] = v;
+    } else if (out2) {
+      out2[col - n0 - n1] = v;
+    }
+  }
+}
+
+}  // namespace
+
+}  // namespace mtgnn

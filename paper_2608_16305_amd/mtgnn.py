@@ -33,6 +33,10 @@ ENTRY_POINTS = (
     "mtgnn_time_projection", "mtgnn_time_projection_bwd", "mtgnn_controller_create", "mtgnn_controller_destroy",
     "mtgnn_controller_decide", "mtgnn_controller_observe", "mtgnn_controller_state", "mtgnn_grad_norm_ws_bytes",
     "mtgnn_grad_norm", "mtgnn_prune_aux", "mtgnn_cache_refresh", "mtgnn_adam_step", "mtgnn_workspace_bytes", "mtgnn_save_bytes",
+    "mtgnn_linear_ws_bytes", "mtgnn_linear", "mtgnn_linear_bwd", "mtgnn_causal_conv_save_bytes",
+    "mtgnn_causal_conv_ws_bytes", "mtgnn_causal_conv", "mtgnn_causal_conv_bwd", "mtgnn_causal_conv_step",
+    "mtgnn_selective_scan_ws_bytes", "mtgnn_selective_scan_save_bytes", "mtgnn_selective_scan",
+    "mtgnn_selective_scan_bwd", "mtgnn_selective_scan_step",
     "mtgnn_status_string", "mtgnn_last_error", "mtgnn_version", "mtgnn_timer_start", "mtgnn_timer_stop",
 )
 
@@ -81,6 +85,39 @@ class LinkParams(C.Structure):
 
 class LinkGrads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _LINK]
+
+
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+
+
+class Seqs(C.Structure):
+    _fields_ = [("max_rows", C.c_int64), ("max_seq", C.c_int64), ("n_slots", C.c_int64), ("off", C.c_void_p),
+                ("n_seq", C.c_void_p), ("slot", C.c_void_p)]
+
+
+class LinearDims(C.Structure):
+    _fields_ = [("d_in", C.c_int32), ("d_out", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32)]
+
+
+class ConvDims(C.Structure):
+    _fields_ = [("d", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32)]
+
+
+class ScanDims(C.Structure):
+    _fields_ = [("d", C.c_int32), ("n", C.c_int32), ("groups", C.c_int32), ("dtype", C.c_int32),
+                ("softplus", C.c_int32)]
+
+
+class ScanInputs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "delta", "B", "C", "z")]
+                + [(n, C.c_int64) for n in ("ldx", "lddelta", "ldB", "ldC", "ldz")]
+                + [(n, C.c_void_p) for n in ("A", "D", "delta_bias")])
+
+
+class ScanGrads(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("dx", "ddelta", "dB", "dC", "dz")]
+                + [(n, C.c_int64) for n in ("lddx", "ldddelta", "lddB", "lddC", "lddz")]
+                + [(n, C.c_void_p) for n in ("dA", "dD", "ddelta_bias")])
 
 
 _P = C.c_void_p
@@ -141,6 +178,23 @@ _SIGS = {
     "mtgnn_cache_refresh": [_P, _I64, _P, _P, C.POINTER(Dims), _P, _P, _P],
     "mtgnn_adam_step": [C.POINTER(C.c_void_p)] * 5 + [C.POINTER(C.c_int64), _I32, C.POINTER(AdamConfig), _P],
     "mtgnn_mixed_batches": [_P, _I64, _I64, _P, _P, _P, _P, _SZ, _P],
+    "mtgnn_linear_ws_bytes": [C.POINTER(LinearDims), _I64, _I32],
+    "mtgnn_linear": [_P, _I64, _P, _I64, _P, _P, _P, _I64, C.POINTER(LinearDims), _P, _I64, _P, _P, _SZ, _P],
+    "mtgnn_linear_bwd": [_P, _I64, _P, _P, _I64, _P, _I64, _P, C.POINTER(LinearDims), _P, _I64, _P, _P, _P, _SZ, _P],
+    "mtgnn_causal_conv_save_bytes": [C.POINTER(ConvDims), _I64],
+    "mtgnn_causal_conv_ws_bytes": [C.POINTER(ConvDims), _I64],
+    "mtgnn_causal_conv": [C.POINTER(Seqs), _P, _I64, _P, _P, C.POINTER(ConvDims), _P, _P, _P, _I64, _P, _P],
+    "mtgnn_causal_conv_bwd": [C.POINTER(Seqs), _P, _I64, _P, _I64, _P, _P, C.POINTER(ConvDims), _P, _P, _I64, _P, _P,
+                              _P, _SZ, _P],
+    "mtgnn_causal_conv_step": [_P, _P, _I64, _I64, _P, _I64, _P, _P, C.POINTER(ConvDims), _P, _P, _P, _I64, _P],
+    "mtgnn_selective_scan_ws_bytes": [C.POINTER(ScanDims), _I64, _I64, _I32],
+    "mtgnn_selective_scan_save_bytes": [C.POINTER(ScanDims), _I64, _I64, _I32],
+    "mtgnn_selective_scan": [C.POINTER(Seqs), C.POINTER(ScanInputs), C.POINTER(ScanDims), _P, _P, _P, _I64, _P, _P,
+                             _SZ, _P],
+    "mtgnn_selective_scan_bwd": [C.POINTER(Seqs), _P, _I64, C.POINTER(ScanInputs), C.POINTER(ScanDims), _P,
+                                 C.POINTER(ScanGrads), _P, _SZ, _P],
+    "mtgnn_selective_scan_step": [_P, _P, _I64, _I64, C.POINTER(ScanInputs), C.POINTER(ScanDims), _P, _P, _P, _I64,
+                                  _P],
     "mtgnn_workspace_bytes": [C.c_int, C.POINTER(Dims), _I64, _I64],
     "mtgnn_save_bytes": [C.c_int, C.POINTER(Dims), _I64, _I64],
     "mtgnn_status_string": [C.c_int],
@@ -150,6 +204,8 @@ _SIGS = {
     "mtgnn_timer_stop": [C.POINTER(C.c_double), C.POINTER(C.c_int)],
 }
 _RES = {"mtgnn_workspace_bytes": _SZ, "mtgnn_save_bytes": _SZ, "mtgnn_grad_norm_ws_bytes": _SZ,
+        "mtgnn_linear_ws_bytes": _SZ, "mtgnn_causal_conv_save_bytes": _SZ, "mtgnn_causal_conv_ws_bytes": _SZ,
+        "mtgnn_selective_scan_ws_bytes": _SZ, "mtgnn_selective_scan_save_bytes": _SZ,
         "mtgnn_controller_destroy": None, "mtgnn_status_string": C.c_char_p,
         "mtgnn_last_error": C.c_char_p, "mtgnn_version": C.c_int}
 
@@ -664,6 +720,222 @@ def mtgnn_adam_step(params, grads, m, v, shadow, lr, beta1, beta2, eps, t, strea
                                  _ptr_array(m, torch.float32, "m"), _ptr_array(v, torch.float32, "v"), sh,
                                  _sizes(params), len(params), C.byref(AdamConfig(lr, beta1, beta2, eps, int(t))),
                                  _stream(stream)), "mtgnn_adam_step")
+
+
+# ----------------------------------------------------------------------------- state-space layer
+
+def _rows(t, dtype, name, rows, cols, optional=False):
+    """(pointer, row stride) of a [rows or more, cols] matrix whose rows are dense."""
+    if t is None:
+        if optional:
+            return None, cols
+        raise MtgnnError(f"{name} is required")
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise MtgnnError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise MtgnnError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols:
+        raise MtgnnError(f"{name} must be [{rows}, {cols}], got {tuple(t.shape)}")
+    if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
+        raise MtgnnError(f"{name} must have dense rows, got strides {t.stride()}")
+    if t.device.index != torch.cuda.current_device():
+        raise MtgnnError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return C.c_void_p(t.data_ptr()), max(int(t.stride(0)), cols)
+
+
+def _table(t, dtype, name, shape, optional=False):
+    """Pointer of a dense tensor of the given shape."""
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise MtgnnError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype, name, optional)
+
+
+def _count(t, n, name):
+    """Pointer of an int32 tensor of n entries or more, or NULL."""
+    if t is not None and t.numel() < n:
+        raise MtgnnError(f"{name} must have {n} entries, got {t.numel()}")
+    return _ptr(t, torch.int32, name, optional=True)
+
+
+def _bytes(t, need, name, optional=False):
+    if t is not None and t.numel() < need:
+        raise MtgnnError(f"{name} must have {need} bytes, got {t.numel()}")
+    return _ptr(t, torch.uint8, name, optional)
+
+
+def seqs(off, max_rows, n_seq=None, slot=None, n_slots=0) -> Seqs:
+    """Sequences in the rows of a matrix: sequence s has rows off[s] .. off[s + 1] - 1 (off int32, one entry more
+    than there are sequences at most)."""
+    max_seq = int(off.numel()) - 1
+    if max_seq < 0:
+        raise MtgnnError("off must have one entry more than there are sequences")
+    return Seqs(int(max_rows), max_seq, int(n_slots), _ptr(off, torch.int32, "off"), _count(n_seq, 1, "n_seq"),
+                _count(slot, max_seq, "slot"))
+
+
+def linear_dims(d_in, d_out, dtype=F32, act=ACT_NONE) -> LinearDims:
+    return LinearDims(int(d_in), int(d_out), int(dtype), int(act))
+
+
+def conv_dims(d, width, dtype=F32, act=ACT_SILU) -> ConvDims:
+    return ConvDims(int(d), int(width), int(dtype), int(act))
+
+
+def scan_dims(d, n, groups=1, dtype=F32, softplus=True) -> ScanDims:
+    return ScanDims(int(d), int(n), int(groups), int(dtype), int(softplus))
+
+
+def linear_ws_bytes(d: LinearDims, max_rows, backward=False) -> int:
+    return int(lib().mtgnn_linear_ws_bytes(C.byref(d), int(max_rows), int(backward)))
+
+
+def causal_conv_ws_bytes(d: ConvDims, max_rows) -> int:
+    return int(lib().mtgnn_causal_conv_ws_bytes(C.byref(d), int(max_rows)))
+
+
+def causal_conv_save_bytes(d: ConvDims, max_seq) -> int:
+    return int(lib().mtgnn_causal_conv_save_bytes(C.byref(d), int(max_seq)))
+
+
+def selective_scan_ws_bytes(d: ScanDims, max_rows, max_seq, backward=False) -> int:
+    return int(lib().mtgnn_selective_scan_ws_bytes(C.byref(d), int(max_rows), int(max_seq), int(backward)))
+
+
+def selective_scan_save_bytes(d: ScanDims, max_rows, max_seq, carried) -> int:
+    return int(lib().mtgnn_selective_scan_save_bytes(C.byref(d), int(max_rows), int(max_seq), int(carried)))
+
+
+def mtgnn_linear(x, W, b, residual, d: LinearDims, y, pre=None, n_rows=None, ws=None, stream=None):
+    """y = act(x W^T + b) + residual; pre: where the backward will find x W^T + b."""
+    md, R = _DT[d.dtype], int(x.shape[0])
+    xp, ldx = _rows(x, md, "x", R, d.d_in)
+    rp, ldr = _rows(residual, md, "residual", R, d.d_out, optional=True)
+    yp, ldy = _rows(y, md, "y", R, d.d_out)
+    wp, wb = _ws(ws)
+    _check(lib().mtgnn_linear(xp, ldx, _count(n_rows, 1, "n_rows"), R, _table(W, md, "W", (d.d_out, d.d_in)),
+                              _table(b, torch.float32, "b", (d.d_out,), True), rp, ldr, C.byref(d), yp, ldy,
+                              _table(pre, torch.float32, "pre", (R, d.d_out), True), wp, wb, _stream(stream)),
+           "mtgnn_linear")
+
+
+def mtgnn_linear_bwd(dy, pre, x, W, d: LinearDims, dx, dW, db, n_rows=None, ws=None, stream=None):
+    md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
+    gp, lddy = _rows(dy, f32, "dy", R, d.d_out)
+    xp, ldx = _rows(x, md, "x", R, d.d_in)
+    dp, lddx = _rows(dx, f32, "dx", R, d.d_in, optional=True)
+    wp, wb = _ws(ws)
+    _check(lib().mtgnn_linear_bwd(gp, lddy, _table(pre, f32, "pre", (R, d.d_out), d.act == ACT_NONE), xp, ldx,
+                                  _count(n_rows, 1, "n_rows"), R, _table(W, md, "W", (d.d_out, d.d_in)), C.byref(d),
+                                  dp, lddx, _table(dW, f32, "dW", (d.d_out, d.d_in)),
+                                  _table(db, f32, "db", (d.d_out,), True), wp, wb, _stream(stream)),
+           "mtgnn_linear_bwd")
+
+
+def mtgnn_causal_conv(q: Seqs, x, w, b, d: ConvDims, state_in, state_out, y, save=None, stream=None):
+    md = _DT[d.dtype]
+    xp, ldx = _rows(x, md, "x", q.max_rows, d.d)
+    yp, ldy = _rows(y, md, "y", q.max_rows, d.d)
+    st = (q.n_slots, d.width - 1, d.d)
+    _check(lib().mtgnn_causal_conv(C.byref(q), xp, ldx, _table(w, md, "w", (d.width, d.d)),
+                                   _table(b, torch.float32, "b", (d.d,), True), C.byref(d),
+                                   _table(state_in, md, "state_in", st, True),
+                                   _table(state_out, md, "state_out", st, True), yp, ldy,
+                                   _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True),
+                                   _stream(stream)), "mtgnn_causal_conv")
+
+
+def mtgnn_causal_conv_bwd(q: Seqs, dy, x, w, b, d: ConvDims, save, dx, dw, db, ws, stream=None):
+    md, f32 = _DT[d.dtype], torch.float32
+    gp, lddy = _rows(dy, f32, "dy", q.max_rows, d.d)
+    xp, ldx = _rows(x, md, "x", q.max_rows, d.d)
+    dp, lddx = _rows(dx, f32, "dx", q.max_rows, d.d)
+    wp, wb = _ws(ws)
+    _check(lib().mtgnn_causal_conv_bwd(C.byref(q), gp, lddy, xp, ldx, _table(w, md, "w", (d.width, d.d)),
+                                       _table(b, f32, "b", (d.d,), True), C.byref(d),
+                                       _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True), dp, lddx,
+                                       _table(dw, f32, "dw", (d.width, d.d)), _table(db, f32, "db", (d.d,), True), wp,
+                                       wb, _stream(stream)), "mtgnn_causal_conv_bwd")
+
+
+def mtgnn_causal_conv_step(slot, x, w, b, d: ConvDims, state_in, state_out, y, n_rows=None, stream=None):
+    """One row each: x[r] is the next row of slot[r] (None: slot r)."""
+    md, R = _DT[d.dtype], int(x.shape[0])
+    xp, ldx = _rows(x, md, "x", R, d.d)
+    yp, ldy = _rows(y, md, "y", R, d.d)
+    n = _n_slots(state_in, state_out)
+    st = (n, d.width - 1, d.d)
+    _check(lib().mtgnn_causal_conv_step(_count(slot, R, "slot"), _count(n_rows, 1, "n_rows"), R, n, xp, ldx,
+                                        _table(w, md, "w", (d.width, d.d)),
+                                        _table(b, torch.float32, "b", (d.d,), True), C.byref(d),
+                                        _table(state_in, md, "state_in", st, True),
+                                        _table(state_out, md, "state_out", st, True), yp, ldy, _stream(stream)),
+           "mtgnn_causal_conv_step")
+
+
+def _n_slots(state_in, state_out):
+    t = state_in if state_in is not None else state_out
+    return 0 if t is None else int(t.shape[0])
+
+
+def scan_inputs(d: ScanDims, x, delta, A, B, C_, D=None, z=None, delta_bias=None) -> ScanInputs:
+    """The scan's inputs; the tensors must live as long as this is used."""
+    md, f32, R, gn = _DT[d.dtype], torch.float32, int(x.shape[0]), d.groups * d.n
+    r = [_rows(x, md, "x", R, d.d), _rows(delta, md, "delta", R, d.d), _rows(B, md, "B", R, gn),
+         _rows(C_, md, "C", R, gn), _rows(z, md, "z", R, d.d, optional=True)]
+    s = ScanInputs(*[p for p, _ in r], *[ld for _, ld in r], _table(A, f32, "A", (d.n, d.d)),
+                   _table(D, f32, "D", (d.d,), True), _table(delta_bias, f32, "delta_bias", (d.d,), True))
+    s.rows = R
+    return s
+
+
+def scan_grads(d: ScanDims, dx, ddelta, dA, dB, dC, dD=None, dz=None, ddelta_bias=None) -> ScanGrads:
+    f32, R, gn = torch.float32, int(dx.shape[0]), d.groups * d.n
+    r = [_rows(dx, f32, "dx", R, d.d), _rows(ddelta, f32, "ddelta", R, d.d), _rows(dB, f32, "dB", R, gn),
+         _rows(dC, f32, "dC", R, gn), _rows(dz, f32, "dz", R, d.d, optional=True)]
+    s = ScanGrads(*[p for p, _ in r], *[ld for _, ld in r], _table(dA, f32, "dA", (d.n, d.d)),
+                  _table(dD, f32, "dD", (d.d,), True), _table(ddelta_bias, f32, "ddelta_bias", (d.d,), True))
+    s.rows = R
+    return s
+
+
+def _enough(what, rows, name):
+    if what.rows < rows:
+        raise MtgnnError(f"{name} have {what.rows} rows, the sequences {rows}")
+
+
+def mtgnn_selective_scan(q: Seqs, inp: ScanInputs, d: ScanDims, state_in, state_out, y, save=None, ws=None,
+                         stream=None):
+    _enough(inp, q.max_rows, "the scan's inputs")
+    yp, ldy = _rows(y, _DT[d.dtype], "y", q.max_rows, d.d)
+    st, f32 = (q.n_slots, d.n, d.d), torch.float32
+    need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, state_in is not None)
+    wp, wb = _ws(ws)
+    _check(lib().mtgnn_selective_scan(C.byref(q), C.byref(inp), C.byref(d), _table(state_in, f32, "state_in", st, True),
+                                      _table(state_out, f32, "state_out", st, True), yp, ldy,
+                                      _bytes(save, need, "save", True), wp, wb, _stream(stream)),
+           "mtgnn_selective_scan")
+
+
+def mtgnn_selective_scan_bwd(q: Seqs, dy, inp: ScanInputs, d: ScanDims, save, grads: ScanGrads, ws, stream=None):
+    _enough(inp, q.max_rows, "the scan's inputs")
+    _enough(grads, q.max_rows, "the scan's gradients")
+    gp, lddy = _rows(dy, torch.float32, "dy", q.max_rows, d.d)
+    need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, False)
+    wp, wb = _ws(ws)
+    _check(lib().mtgnn_selective_scan_bwd(C.byref(q), gp, lddy, C.byref(inp), C.byref(d), _bytes(save, need, "save"),
+                                          C.byref(grads), wp, wb, _stream(stream)), "mtgnn_selective_scan_bwd")
+
+
+def mtgnn_selective_scan_step(slot, inp: ScanInputs, d: ScanDims, state_in, state_out, y, n_rows=None, stream=None):
+    """One row each: row r of the inputs is the next row of slot[r] (None: slot r)."""
+    R, f32 = inp.rows, torch.float32
+    yp, ldy = _rows(y, _DT[d.dtype], "y", R, d.d)
+    n = _n_slots(state_in, state_out)
+    st = (n, d.n, d.d)
+    _check(lib().mtgnn_selective_scan_step(_count(slot, R, "slot"), _count(n_rows, 1, "n_rows"), R, n, C.byref(inp),
+                                           C.byref(d), _table(state_in, f32, "state_in", st, True),
+                                           _table(state_out, f32, "state_out", st, True), yp, ldy, _stream(stream)),
+           "mtgnn_selective_scan_step")
 
 
 def timer_start(kernel: str, max_launches: int):

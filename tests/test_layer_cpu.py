@@ -1,0 +1,212 @@
+"""The state-space layer's operators without a GPU: the 64-bit oracle's gradients against differences, and the
+C entry points' refusals (none of these calls reaches a launch)."""
+
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer
+from paper_2608_16305_amd import mtgnn as M
+
+built = pytest.mark.skipif(not os.path.exists(M.LIB_PATH), reason="libmtgnn.so not built")
+
+
+def _slope(f, v, direction, h=1e-6):
+    return (f(v + h * direction) - f(v - h * direction)) / (2 * h)
+
+
+def _check_gradients(call, inputs, names, seed=0):
+    """Each gradient in a random direction against the difference of sum(dy y)."""
+    rs = np.random.RandomState(seed)
+    y0 = call(**inputs)["y"]
+    dy = rs.randn(*y0.shape)
+    grads = call(dy=dy, **inputs)
+    for name, grad in names.items():
+        v = np.asarray(inputs[name], np.float64)
+        dirn = rs.randn(*v.shape)
+        num = _slope(lambda a, name=name: (call(**dict(inputs, **{name: a}))["y"] * dy).sum(), v, dirn)
+        ana = (grads[grad] * dirn).sum()
+        # central differences: h^2 times the third derivative, and rounding of the sums over 2h
+        assert abs(num - ana) <= 1e-6 * (1 + abs(ana)), (name, num, ana)
+
+
+@pytest.mark.parametrize("name", ["none", "silu", "gelu"])
+def test_linear_gradients(name):
+    rs = np.random.RandomState(1)
+    i = dict(x=rs.randn(7, 5), W=rs.randn(4, 5), b=rs.randn(4), residual=rs.randn(7, 4))
+    _check_gradients(lambda dy=None, **k: layer.linear(name=name, dy=dy, **k), i, dict(x="dx", W="dW", b="db"))
+
+
+@pytest.mark.parametrize("name,width", [("none", 2), ("silu", 3), ("silu", 4)])
+def test_conv_gradients(name, width):
+    rs = np.random.RandomState(2)
+    lens = [3, 0, 1, 6, 2]
+    i = dict(x=rs.randn(12, 3), w=rs.randn(width, 3), b=rs.randn(3), first=rs.randn(5, width - 1, 3))
+    _check_gradients(lambda dy=None, **k: layer.conv(lens, name=name, dy=dy, **k), i, dict(x="dx", w="dw", b="db"))
+
+
+@pytest.mark.parametrize("softplus,groups", [(True, 1), (False, 2)])
+def test_scan_gradients(softplus, groups):
+    rs = np.random.RandomState(3)
+    lens = [4, 1, 0, 5]
+    i = dict(x=rs.randn(10, 4), delta=rs.rand(10, 4), A=-rs.rand(3, 4) * 2, B=rs.randn(10, 3 * groups),
+             C=rs.randn(10, 3 * groups), D=rs.randn(4), z=rs.randn(10, 4), bias=0.1 * rs.rand(4))
+    first = rs.randn(4, 3, 4)
+    _check_gradients(lambda dy=None, **k: layer.scan(lens, softplus=softplus, groups=groups, first=first, dy=dy, **k), i,
+                     dict(x="dx", delta="ddelta", A="dA", B="dB", C="dC", D="dD", z="dz", bias="ddelta_bias"))
+
+
+def test_a_sequence_is_its_pieces():
+    """A sequence cut in two, the second piece from the first one's state, gives the whole one's rows."""
+    rs = np.random.RandomState(4)
+    x, delta, A, B, C_ = rs.randn(9, 2), rs.randn(9, 2), -rs.rand(3, 2), rs.randn(9, 3), rs.randn(9, 3)
+    whole = layer.scan([9], x, delta, A, B, C_)
+    one = layer.scan([4], x[:4], delta[:4], A, B[:4], C_[:4])
+    two = layer.scan([5], x[4:], delta[4:], A, B[4:], C_[4:], first=one["state"])
+    assert np.allclose(np.concatenate([one["y"], two["y"]]), whole["y"], rtol=1e-13, atol=1e-13)
+    w = rs.randn(4, 2)
+    whole = layer.conv([9], x, w, None, "silu")
+    one = layer.conv([2], x[:2], w, None, "silu")
+    two = layer.conv([7], x[2:], w, None, "silu", first=one["state"])
+    assert np.allclose(np.concatenate([one["y"], two["y"]]), whole["y"], rtol=1e-13, atol=1e-13)
+
+
+P = C.c_void_p(256)
+BIG = 1 << 40
+
+
+def _q(max_rows=10, max_seq=3, n_slots=4, off=P):
+    return C.byref(M.Seqs(max_rows, max_seq, n_slots, off, None, None))
+
+
+@built
+def test_linear_refusals():
+    L = M.lib()
+
+    def fwd(d=(8, 4, 0, 2), rows=10, x=P, ldx=8, W=P, res=None, ldr=0, y=P, ldy=4, ws=P, wb=BIG):
+        dims = C.byref(M.LinearDims(*d)) if d else None
+        return L.mtgnn_linear(x, ldx, None, rows, W, None, res, ldr, dims, y, ldy, None, ws, wb, None)
+
+    assert fwd(d=None) == -1 and fwd(d=(0, 4, 0, 2)) == -1 and fwd(d=(8, -1, 0, 2)) == -1
+    assert fwd(d=(8, 4, 5, 2)) == -2 and fwd(d=(8, 4, 0, 4)) == -2 and fwd(d=(8, 4, 0, -1)) == -2
+    assert fwd(rows=-1) == -1 and fwd(rows=(1 << 31) - 1) == -1
+    assert fwd(x=None) == -1 and fwd(W=None) == -1 and fwd(y=None) == -1
+    assert fwd(ldx=7) == -1 and fwd(ldy=3) == -1 and fwd(res=P, ldr=3) == -1
+    assert fwd(rows=0) == 0
+    need = L.mtgnn_linear_ws_bytes(C.byref(M.LinearDims(8, 4, 0, 2)), 10, 0)
+    assert need == 0 or fwd(wb=need - 1) == -3
+    assert L.mtgnn_linear_ws_bytes(C.byref(M.LinearDims(8, 4, 0, 9)), 10, 0) == 0
+
+    def bwd(d=(8, 4, 0, 2), rows=10, dy=P, lddy=4, pre=P, x=P, ldx=8, W=P, dx=P, lddx=8, dW=P, ws=P, wb=BIG):
+        return L.mtgnn_linear_bwd(dy, lddy, pre, x, ldx, None, rows, W, C.byref(M.LinearDims(*d)), dx, lddx, dW, None,
+                                  ws, wb, None)
+
+    assert bwd(rows=0) == -1 and bwd(dy=None) == -1 and bwd(pre=None) == -1 and bwd(dW=None) == -1
+    assert bwd(lddy=3) == -1 and bwd(ldx=2) == -1 and bwd(lddx=7) == -1 and bwd(x=None) == -1 and bwd(W=None) == -1
+    need = L.mtgnn_linear_ws_bytes(C.byref(M.LinearDims(8, 4, 0, 2)), 10, 1)
+    assert need > 0 and bwd(wb=need - 1) == -3 and bwd(ws=None) == -1
+
+
+@built
+def test_conv_refusals():
+    L = M.lib()
+
+    def fwd(d=(8, 4, 0, 2), q=None, x=P, ldx=8, w=P, y=P, ldy=8):
+        return L.mtgnn_causal_conv(q or _q(), x, ldx, w, None, C.byref(M.ConvDims(*d)), None, None, y, ldy, None, None)
+
+    assert fwd(d=(0, 4, 0, 2)) == -1 and fwd(d=(8, 1, 0, 2)) == -2 and fwd(d=(8, 5, 0, 2)) == -2
+    assert fwd(d=(8, 4, 2, 2)) == -2 and fwd(d=(8, 4, 0, 1)) == -2
+    assert fwd(q=_q(off=None)) == -1 and fwd(q=_q(max_rows=-1)) == -1 and fwd(q=_q(max_seq=-1)) == -1
+    assert fwd(q=_q(n_slots=-1)) == -1
+    assert fwd(x=None) == -1 and fwd(w=None) == -1 and fwd(y=None) == -1 and fwd(ldx=7) == -1 and fwd(ldy=7) == -1
+    assert fwd(q=_q(max_rows=0)) == 0 and fwd(q=_q(max_seq=0, off=None)) == 0
+    assert L.mtgnn_causal_conv(None, P, 8, P, None, C.byref(M.ConvDims(8, 4, 0, 2)), None, None, P, 8, None, None) == -1
+
+    def bwd(q=None, dy=P, lddy=8, x=P, ldx=8, w=P, dx=P, lddx=8, dw=P, ws=P, wb=BIG):
+        return L.mtgnn_causal_conv_bwd(q or _q(), dy, lddy, x, ldx, w, None, C.byref(M.ConvDims(8, 4, 0, 2)), None, dx,
+                                       lddx, dw, None, ws, wb, None)
+
+    assert bwd(q=_q(max_rows=0)) == -1 and bwd(dy=None) == -1 and bwd(dx=None) == -1 and bwd(dw=None) == -1
+    assert bwd(lddy=7) == -1 and bwd(lddx=7) == -1 and bwd(ws=None) == -1 and bwd(wb=16) == -3
+
+    def step(rows=10, n_slots=4, x=P, y=P, ldx=8):
+        return L.mtgnn_causal_conv_step(None, None, rows, n_slots, x, ldx, P, None, C.byref(M.ConvDims(8, 4, 0, 2)),
+                                        None, None, y, 8, None)
+
+    assert step(rows=-1) == -1 and step(n_slots=-1) == -1 and step(x=None) == -1 and step(y=None) == -1
+    assert step(ldx=7) == -1 and step(rows=0) == 0
+
+
+def _inp(**kw):
+    v = dict(x=P, delta=P, B=P, C=P, z=None, ldx=8, lddelta=8, ldB=4, ldC=4, ldz=0, A=P, D=None, delta_bias=None)
+    v.update(kw)
+    return C.byref(M.ScanInputs(*[v[f] for f, _ in M.ScanInputs._fields_]))
+
+
+@built
+def test_scan_refusals():
+    L = M.lib()
+
+    def fwd(d=(8, 4, 1, 0, 1), q=None, inp=None, y=P, ldy=8, ws=P, wb=BIG):
+        return L.mtgnn_selective_scan(q or _q(), inp or _inp(), C.byref(M.ScanDims(*d)), None, None, y, ldy, None, ws,
+                                      wb, None)
+
+    assert fwd(d=(0, 4, 1, 0, 1)) == -1 and fwd(d=(8, 0, 1, 0, 1)) == -1 and fwd(d=(8, 4, 3, 0, 1)) == -1
+    assert fwd(d=(8, 65, 1, 0, 1)) == -2 and fwd(d=(8, 4, 1, 3, 1)) == -2
+    for name in ("x", "delta", "B", "C", "A"):
+        assert fwd(inp=_inp(**{name: None})) == -1
+    for name in ("ldx", "lddelta"):
+        assert fwd(inp=_inp(**{name: 7})) == -1
+    for name in ("ldB", "ldC"):
+        assert fwd(inp=_inp(**{name: 3})) == -1
+    assert fwd(inp=_inp(z=P, ldz=7)) == -1 and fwd(y=None) == -1 and fwd(ldy=7) == -1
+    assert fwd(ws=None) == -1 and fwd(wb=16) == -3 and fwd(q=_q(off=None)) == -1
+    assert fwd(q=_q(max_rows=0)) == 0 and fwd(q=_q(max_seq=0, off=None)) == 0
+
+    def bwd(d=(8, 4, 1, 0, 1), q=None, inp=None, dy=P, lddy=8, save=P, ws=P, wb=BIG, **kw):
+        v = dict(dx=P, ddelta=P, dB=P, dC=P, dz=None, lddx=8, ldddelta=8, lddB=4, lddC=4, lddz=8, dA=P, dD=None,
+                 ddelta_bias=None)
+        v.update(kw)
+        g = M.ScanGrads(*[v[f] for f, _ in M.ScanGrads._fields_])
+        return L.mtgnn_selective_scan_bwd(q or _q(), dy, lddy, inp or _inp(), C.byref(M.ScanDims(*d)), save, C.byref(g),
+                                          ws, wb, None)
+
+    for name in ("dx", "ddelta", "dB", "dC", "dA"):
+        assert bwd(**{name: None}) == -1
+    for name in ("lddx", "ldddelta"):
+        assert bwd(**{name: 7}) == -1
+    for name in ("lddB", "lddC"):
+        assert bwd(**{name: 3}) == -1
+    assert bwd(dz=P) == -1 and bwd(dD=P) == -1 and bwd(ddelta_bias=P) == -1
+    assert bwd(inp=_inp(z=P, ldz=8)) == -1 and bwd(inp=_inp(z=P, ldz=8), dz=P, lddz=7) == -1
+    assert bwd(dy=None) == -1 and bwd(save=None) == -1 and bwd(lddy=7) == -1
+    assert bwd(ws=None) == -1 and bwd(wb=16) == -3 and bwd(q=_q(max_rows=0)) == -1
+
+    def step(rows=10, n_slots=4, inp=None, y=P):
+        return L.mtgnn_selective_scan_step(None, None, rows, n_slots, inp or _inp(), C.byref(M.ScanDims(8, 4, 1, 0, 1)),
+                                           None, None, y, 8, None)
+
+    assert step(rows=-1) == -1 and step(n_slots=-1) == -1 and step(y=None) == -1 and step(inp=_inp(A=None)) == -1
+    assert step(rows=0) == 0
+
+
+@built
+def test_sizes():
+    d = M.scan_dims(100, 16)
+    assert 0 < M.selective_scan_ws_bytes(d, 100, 5) <= M.selective_scan_ws_bytes(d, 100, 5, True)
+    a, b = M.selective_scan_save_bytes(d, 100, 5, False), M.selective_scan_save_bytes(d, 100, 5, True)
+    assert a >= 100 // 8 * 16 * 100 * 4 and b - a >= 5 * 16 * 100 * 4
+    assert M.selective_scan_ws_bytes(M.scan_dims(100, 16, 3), 100, 5) == 0
+    c = M.conv_dims(100, 4, M.BF16)
+    assert M.causal_conv_save_bytes(c, 7) == 7 * 3 * 100 * 2 and M.causal_conv_ws_bytes(c, 100) > 0
+
+
+@built
+def test_binding_refuses_host_tensors():
+    with pytest.raises(M.MtgnnError):
+        M.mtgnn_linear(torch.zeros(3, 4), torch.zeros(5, 4), None, None, M.linear_dims(4, 5), torch.zeros(3, 5))
+    with pytest.raises(M.MtgnnError):
+        M.seqs(torch.zeros(3, dtype=torch.int32), 4)
