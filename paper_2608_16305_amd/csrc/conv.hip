@@ -399,7 +399,7 @@ mtgnn_status conv_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
   conv_variant(d, two, LaunchConvBack{p, (unsigned)(cdiv(cdiv(q->max_rows, p.ch), 4) * p.tiles), s});
   MTGNN_CHECK_LAUNCH("conv_back");
   const int64_t wd = (int64_t)d->width * d->d;
-  k_sum_parts<<<(unsigned)cdiv(wd + d->d, 16), 256, 0, s>>>(p.q, p.ch, p.part, wd + d->d, wd, dw, d->d, db, nullptr);
+  k_sum_parts<<<(unsigned)cdiv(wd + d->d, 16), 256, 0, s>>>(p.q, p.ch, 0, p.part, wd + d->d, wd, dw, d->d, db, nullptr);
   MTGNN_CHECK_LAUNCH("conv_sum_parts");
   return MTGNN_OK;
 }

@@ -1,4 +1,21 @@
-// Linear layer with bias, activation and residual, and its backward.
+// Linear layer with bias, activation and residual, and its backward:
+//   y = act(x W^T + b) + residual;   g = dy act'(pre),  dx = g W,  dW = g^T x,  db = sum of g.
+//
+// All three products run in one kernel, out[r][c] = sum_k R(r, k) C(c, k), on the bfloat16 matrix instructions.  A
+// bfloat16 operand enters as it is; a float32 one as three bfloat16 parts (24 bits, bf16_split.h), split as its tile is
+// staged: three products for one such operand, six for two (the three smallest, below 2^-26 of the
+// whole, are left out), which is still 2.6 times the rate of the float32 matrix instructions.  Results are
+// exact to float32 either way.
+//
+// A block of four waves makes a T x T tile (T = 128 or 64), each wave a quarter of it.  Operands pass through
+// registers into LDS in 16-byte units of eight k, from rows that are contiguous along k or across it; the next
+// step's loads are in flight while the matrix instructions work on this one.  A unit's place in its row is
+// swizzled by the row, so that eight lanes' reads and writes of 16 bytes meet every bank once.  The matrix instruction's
+// first operand is C: a lane then holds four neighbouring columns of a row.  Tiles leave through LDS, so that
+// rows are written in 128 to 256 bytes, and the epilogue is a loop and not 64 copies of it.
+#include <algorithm>
+
+#include "bf16_split.h"
 #include "gemm.h"
 #include "ops.h"
 #include "seq.h"
@@ -7,65 +24,414 @@ namespace mtgnn {
 
 namespace {
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_linear_out(const float* pre, const T* res, int64_t ldr, const int32_t* n_rows,
-                                                    int64_t max_rows, int n, int act, T* y, int64_t ldy) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / n;
-  if (row >= eff_count(max_rows, n_rows)) return;
-  const int64_t col = e % n;
-  float v = act_(act, pre[row * n + col]);
-  if (res) v += Elem<T>::load(res, row * ldr + col);
-  Elem<T>::store(y, row * ldy + col, v);
+constexpr int NT = 256;
+
+struct ProdP {
+  const void *R, *C;
+  int64_t ldR, ldC;
+  int64_t rows, cols, K;           // rows of R and C, length of the sums
+  const int32_t *rows_dev, *K_dev; // device counts that bound them, or NULL
+  int vecR, vecC;                  // contiguous along k: 16-byte loads are aligned
+  int64_t tc, tiles;               // tiles of a row of tiles, tiles in all
+  int split;                       // blocks that share a tile's sum
+  // output: float32 sums (o, split x rows x cols of them where split > 1), or the layer's epilogue (y given)
+  float* o;
+  int64_t ldo;
+  const float* b;
+  const void* res;
+  int64_t ldr;
+  void* y;
+  int64_t ldy;
+  float* pre;
+  int act;
+};
+
+// One operand's share of a tile in a thread's registers: U units of eight k.
+template <bool F32, bool KC, int T, int KS>
+struct Stage {
+  static constexpr int U = T * KS / 8 / NT, CH = KS / 8, PL = F32 ? 3 : 1;
+  static_assert(U >= 1, "a unit per thread");
+  uint32_t v[U][F32 ? 8 : 4];
+  __device__ __forceinline__ static int row(int u) {
+    const int id = u * NT + threadIdx.x;
+    return KC ? id / CH : id % T;
+  }
+  __device__ __forceinline__ static int chunk(int u) {
+    const int id = u * NT + threadIdx.x;
+    return KC ? id % CH : id / T;
+  }
+  // rows r0 .. of the operand (the last one stands for those past it), k0 .. k0 + KS - 1 (zeros from K on)
+  __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t rows, int64_t r0, int64_t k0, int64_t K,
+                                       bool vec) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = min(r0 + row(u), rows - 1), k = k0 + chunk(u) * 8;
+      if constexpr (KC) {
+        if (vec && k + 8 <= K) {
+          if constexpr (F32) {
+            const uint4* q = (const uint4*)((const float*)p + r * ld + k);
+            const uint4 a = q[0], b = q[1];
+            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
+            v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
+          } else {
+            const uint4 a = *(const uint4*)((const uint16_t*)p + r * ld + k);
+            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
+          }
+        } else {
+          uint32_t e[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int64_t at = r * ld + min(k + i, K - 1);
+            e[i] = F32 ? ((const uint32_t*)p)[at] : (uint32_t)((const uint16_t*)p)[at];
+          }
+          put(u, e, k, K);
+        }
+      } else {
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int64_t at = min(k + i, K - 1) * ld + r;
+          e[i] = F32 ? ((const uint32_t*)p)[at] : (uint32_t)((const uint16_t*)p)[at];
+        }
+        put(u, e, k, K);
+      }
+    }
+  }
+  __device__ __forceinline__ void put(int u, const uint32_t (&e)[8], int64_t k, int64_t K) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = k + i < K ? e[i] : 0u;
+      if constexpr (F32) v[u][i] = w;
+      else if (i % 2 == 0) v[u][i / 2] = w;
+      else v[u][i / 2] |= w << 16;
+    }
+  }
+  // dst: [plane][T][KS] bfloat16, units swizzled
+  __device__ __forceinline__ void store(uint32_t* dst) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t* d = dst + at(row(u), chunk(u));
+      if constexpr (F32) {
+        float x[8];
+        uint32_t h[4], m[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[u][i]);
+        split_words<false>(x, h, m, l);
+        *(uint4*)d = make_uint4(h[0], h[1], h[2], h[3]);
+        *(uint4*)(d + T * KS / 2) = make_uint4(m[0], m[1], m[2], m[3]);
+        *(uint4*)(d + T * KS) = make_uint4(l[0], l[1], l[2], l[3]);
+      } else {
+        *(uint4*)d = make_uint4(v[u][0], v[u][1], v[u][2], v[u][3]);
+      }
+    }
+  }
+  // Word of unit c of row r in a plane.
+  __device__ __forceinline__ static int at(int r, int c) {
+    const int s = CH == 4 ? c ^ (r >> 1 & 3) : c ^ (r & 7);
+    return r * (KS / 2) + s * 4;
+  }
+  __device__ __forceinline__ static bf16x8_t frag(const uint32_t* src, int plane, int r, int c) {
+    return __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + plane * (T * KS / 2) + at(r, c)));
+  }
+};
+
+// Which tile and share of the sum this block makes.  Blocks run on the 8 XCDs in turn, each with its own L2: a
+// contiguous eighth of the tiles to each, so the blocks of an XCD share rows of R.
+__device__ __forceinline__ void my_tile(const ProdP& p, int64_t& tr, int64_t& tcol, int& share) {
+  const int64_t L = blockIdx.x, n = p.tiles * p.split, full = n & ~int64_t(7);
+  const int64_t V = L < full ? (L & 7) * (full >> 3) + (L >> 3) : L;
+  share = (int)(V % p.split);
+  const int64_t t = V / p.split;
+  tr = t / p.tc;
+  tcol = t % p.tc;
 }
 
+// One output by float32 products: what a sum that is not finite is made by again (a part of an infinite operand, or of
+// one past the largest bfloat16, is infinite or NaN and meets the others' zeros).
+template <bool RF, bool CF, bool RK, bool CK>
+__device__ __attribute__((noinline)) float plain_sum(const void* R, int64_t ldR, const void* C, int64_t ldC, int64_t r,
+                                                     int64_t c, int64_t k0, int64_t k1) {
+  float v = 0.f;
+  for (int64_t k = k0; k < k1; ++k) {
+    const int64_t a = RK ? r * ldR + k : k * ldR + r, b = CK ? c * ldC + k : k * ldC + c;
+    const float x = RF ? ((const float*)R)[a] : bf16_to_f32(((const uint16_t*)R)[a]);
+    const float w = CF ? ((const float*)C)[b] : bf16_to_f32(((const uint16_t*)C)[b]);
+    v = fmaf(x, w, v);
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish4(const ProdP& p, int64_t r, int64_t c, int n, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= n) break;
+    float a = v[i] + (p.b ? p.b[c + i] : 0.f);
+    if (p.pre) p.pre[r * p.cols + c + i] = a;
+    a = act_(p.act, a);
+    if (p.res) a += Elem<T>::load((const T*)p.res, r * p.ldr + c + i);
+    Elem<T>::store((T*)p.y, r * p.ldy + c + i, a);
+  }
+}
+
+// RF, CF: float32 operands; RK, CK: contiguous along k.  Y: the type of y.
+template <bool RF, bool CF, bool RK, bool CK, int T>
+__global__ __launch_bounds__(NT) void k_product(ProdP p) {
+  constexpr int KS = RF || CF ? 32 : 64;
+  constexpr int W = T / 32;                      // 16-wide tiles of a wave, each way
+  using SR = Stage<RF, RK, T, KS>;
+  using SC = Stage<CF, CK, T, KS>;
+  using Y = std::conditional_t<CF, float, uint16_t>;
+  constexpr int PLANE = T * KS / 2;              // words
+  constexpr int WORDS = (SR::PL + SC::PL) * PLANE, OUT = 4 * 16 * (T / 2 + 4);
+  __shared__ __align__(16) uint32_t lds[WORDS > OUT ? WORDS : OUT];
+  uint32_t *sR = lds, *sC = lds + SR::PL * PLANE;
+  int64_t tr, tcol;
+  int share;
+  my_tile(p, tr, tcol, share);
+  const int64_t rows = eff_count(p.rows, p.rows_dev), K = eff_count(p.K, p.K_dev);
+  const int64_t r0 = tr * T, c0 = tcol * T;
+  if (r0 >= rows) return;
+  const int64_t per = cdiv(cdiv(K, KS), p.split) * KS;
+  const int64_t kb = min(K, share * per), ke = min(K, kb + per);
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = (wid >> 1) * (T / 2), wc = (wid & 1) * (T / 2), fr = lane & 15, fg = lane >> 4;
+  f32x4 acc[W][W];
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+#pragma unroll
+    for (int j = 0; j < W; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  SR a;
+  SC b;
+  if (kb < ke) {
+    a.load(p.R, p.ldR, rows, r0, kb, ke, p.vecR);
+    b.load(p.C, p.ldC, p.cols, c0, kb, ke, p.vecC);
+  }
+  for (int64_t k = kb; k < ke; k += KS) {
+    a.store(sR);
+    b.store(sC);
+    __syncthreads();
+    if (k + KS < ke) {
+      a.load(p.R, p.ldR, rows, r0, k + KS, ke, p.vecR);
+      b.load(p.C, p.ldC, p.cols, c0, k + KS, ke, p.vecC);
+    }
+#pragma unroll
+    for (int kk = 0; kk < KS / 32; ++kk) {
+      bf16x8_t cf[W][SC::PL];
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+#pragma unroll
+        for (int q = 0; q < SC::PL; ++q) cf[j][q] = SC::frag(sC, q, wc + 16 * j + fr, 4 * kk + fg);
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        bf16x8_t rf[SR::PL];
+#pragma unroll
+        for (int q = 0; q < SR::PL; ++q) rf[q] = SR::frag(sR, q, wr + 16 * i + fr, 4 * kk + fg);
+        const auto mul = [&](int qc, int qr) {
+#pragma unroll
+          for (int j = 0; j < W; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cf[j][qc], rf[qr], acc[i][j], 0, 0, 0);
+        };
+        if constexpr (RF && CF) {
+          mul(1, 1);
+          mul(2, 0);
+          mul(0, 2);
+          mul(1, 0);
+          mul(0, 1);
+        } else if constexpr (RF) {
+          mul(0, 2);
+          mul(0, 1);
+        }
+        mul(0, 0);
+      }
+    }
+    __syncthreads();
+  }
+  // sixteen rows at a time through LDS: lane l then has row l / (T / 8) of a few and four columns
+  constexpr int LD = T / 2 + 4, LPR = T / 8;     // words of a row; lanes of a row
+  float* s = (float*)lds + wid * 16 * LD;
+  float* out = p.o + (p.split > 1 ? (int64_t)share * p.rows * p.cols : 0);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) *(f32x4*)(s + fr * LD + 16 * j + 4 * fg) = acc[i][j];
+    __syncthreads();
+#pragma unroll 1
+    for (int e = lane; e < 16 * LPR; e += 64) {
+      const int64_t r = r0 + wr + 16 * i + e / LPR, c = c0 + wc + 4 * (e % LPR);
+      if (r >= rows || c >= p.cols) continue;
+      const f32x4 f = *(const f32x4*)(s + (e / LPR) * LD + 4 * (e % LPR));
+      float v[4] = {f.x, f.y, f.z, f.w};
+      const int n = (int)min((int64_t)4, p.cols - c);
+      if constexpr (RF || CF) {
+        if (!(fabsf(f.x) + fabsf(f.y) + fabsf(f.z) + fabsf(f.w) < INFINITY)) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (u < n && !(fabsf(v[u]) < INFINITY))
+              v[u] = plain_sum<RF, CF, RK, CK>(p.R, p.ldR, p.C, p.ldC, r, c + u, kb, ke);
+        }
+      }
+      if (p.y) {
+        finish4<Y>(p, r, c, n, v);
+      } else if (n == 4 && ((uintptr_t)(out + r * p.ldo + c) & 15) == 0) {
+        *(float4*)(out + r * p.ldo + c) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (u < n) out[r * p.ldo + c + u] = v[u];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The sums of the shares of a split product, and what is left of the call.
+template <typename Y>
+__global__ __launch_bounds__(256) void k_product_sum(ProdP p, const float* part, int64_t total) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= total) return;
+  const int64_t r = e / p.cols, c = e % p.cols;
+  if (r >= eff_count(p.rows, p.rows_dev)) return;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < p.split; ++s) v[0] += part[s * total + e];
+  if (p.y) finish4<Y>(p, r, c, 1, v);
+  else p.o[r * p.ldo + c] = v[0];
+}
+
+// g = dy act'(pre), rows dense, and the column sums of each 64 rows (rows < n_rows; zeros without any).
+constexpr int SLOPE_ROWS = 64;
 __global__ __launch_bounds__(256) void k_linear_slope(const float* dy, int64_t lddy, const float* pre,
                                                       const int32_t* n_rows, int64_t max_rows, int n, int act,
-                                                      float* g) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / n;
-  if (row >= eff_count(max_rows, n_rows)) return;
-  const int64_t col = e % n;
-  const float d = dy[row * lddy + col];
-  g[e] = act == MTGNN_ACT_NONE ? d : d * dact_(act, pre[e]);
+                                                      float* g, float* part) {
+  __shared__ float s[4][64];
+  const int64_t rows = eff_count(max_rows, n_rows);
+  const int64_t cb = cdiv(n, 64), c = (blockIdx.x % cb) * 64 + (threadIdx.x & 63), blk = blockIdx.x / cb;
+  const int64_t r0 = blk * SLOPE_ROWS + (threadIdx.x >> 6);
+  float sum = 0.f;
+  if (c < n) {
+#pragma unroll 4
+    for (int i = 0; i < SLOPE_ROWS / 4; ++i) {
+      const int64_t r = r0 + 4 * i;
+      if (r >= rows) break;
+      float v = dy[r * lddy + c];
+      if (act != MTGNN_ACT_NONE) v *= dact_(act, pre[r * n + c]);
+      if (g) g[r * n + c] = v;
+      sum += v;
+    }
+  }
+  s[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+  __syncthreads();
+  if (part && threadIdx.x < 64 && c < n)
+    part[blk * n + c] = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
 }
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
+// Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64; with
+// fewer than about a tile per CU the smaller ones fill the card, and then shares of the sum (256 k or more each).
+struct Plan {
+  int T, split;
+  int64_t tr, tc;
+};
+Plan plan(int64_t rows, int64_t cols, int64_t K) {
+  Plan p;
+  p.T = cdiv(rows, 128) * cdiv(cols, 128) >= 192 ? 128 : 64;
+  if (p.T == 64 && rows > 64 && cols > 64 && K >= 4096) p.T = 128;   // long sums (dW): shares fill the card
+  p.tr = cdiv(rows, p.T);
+  p.tc = cdiv(cols, p.T);
+  const int64_t t = p.tr * p.tc;
+  p.split = (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, K / 256));
+  return p;
+}
+size_t split_bytes(int64_t rows, int64_t cols, int64_t K) {
+  const Plan q = plan(rows, cols, K);
+  return q.split > 1 ? al((size_t)q.split * rows * cols * 4) : 0;
+}
+
+// out = R C^T; the rest of p is set.
+template <bool RF, bool CF, bool RK, bool CK>
+mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
+  const Plan q = plan(p.rows, p.cols, p.K);
+  p.tc = q.tc;
+  p.tiles = q.tr * q.tc;
+  p.split = q.split;
+  const ProdP fin = p;
+  if (q.split > 1) {
+    p.o = (float*)ws;
+    p.ldo = p.cols;
+    p.y = nullptr;
+  }
+  const unsigned grid = (unsigned)(p.tiles * p.split);
+  {
+    TimedScope ts("linear", s);
+    if (q.T == 128) k_product<RF, CF, RK, CK, 128><<<grid, NT, 0, s>>>(p);
+    else k_product<RF, CF, RK, CK, 64><<<grid, NT, 0, s>>>(p);
+  }
+  MTGNN_CHECK_LAUNCH("product");
+  if (q.split > 1) {
+    const int64_t total = p.rows * p.cols;
+    k_product_sum<std::conditional_t<CF, float, uint16_t>><<<(unsigned)cdiv(total, 256), 256, 0, s>>>(
+        fin, (const float*)ws, total);
+    MTGNN_CHECK_LAUNCH("product_sum");
+  }
+  return MTGNN_OK;
+}
+
 }  // namespace
 
 size_t linear_ws(const mtgnn_linear_dims* d, int64_t rows, bool back) {
-  const size_t m = al((size_t)rows * d->d_out * 4);
-  return back ? m + al(linear_dw_ws_bytes(rows, d->d_out, d->d_in)) : m;
+  if (!back) return split_bytes(rows, d->d_out, d->d_in);
+  const size_t g = al((size_t)rows * d->d_out * 4) + al((size_t)cdiv(rows, SLOPE_ROWS) * d->d_out * 4);
+  return g + std::max(split_bytes(rows, d->d_in, d->d_out), split_bytes(d->d_out, d->d_in, rows));
 }
 
 mtgnn_status linear_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W,
                          const float* b, const void* res, int64_t ldr, const mtgnn_linear_dims* d, void* y,
                          int64_t ldy, float* pre, void* ws, size_t ws_bytes, hipStream_t s) {
-  float* p = pre ? pre : (float*)ws;
-  MTGNN_TRY((linear_fwd(x, d->dtype, ldx, W, d->dtype, d->d_in, b, p, d->d_out, max_rows, n_rows, d->d_out, d->d_in,
-                        false, s)));
-  const unsigned grid = (unsigned)cdiv(max_rows * d->d_out, 256);
-  if (d->dtype == MTGNN_BF16)
-    k_linear_out<uint16_t><<<grid, 256, 0, s>>>(p, (const uint16_t*)res, ldr, n_rows, max_rows, d->d_out, d->act,
-                                                (uint16_t*)y, ldy);
-  else
-    k_linear_out<float><<<grid, 256, 0, s>>>(p, (const float*)res, ldr, n_rows, max_rows, d->d_out, d->act, (float*)y,
-                                             ldy);
-  MTGNN_CHECK_LAUNCH("linear_out");
-  return MTGNN_OK;
+  const bool bf = d->dtype == MTGNN_BF16;
+  const int64_t per = bf ? 8 : 4;
+  ProdP p{};
+  p.R = x; p.ldR = ldx; p.C = W; p.ldC = d->d_in;
+  p.rows = max_rows; p.cols = d->d_out; p.K = d->d_in; p.rows_dev = n_rows;
+  p.vecR = ldx % per == 0 && (uintptr_t)x % 16 == 0;
+  p.vecC = d->d_in % per == 0 && (uintptr_t)W % 16 == 0;
+  p.b = b; p.res = res; p.ldr = ldr; p.y = y; p.ldy = ldy; p.pre = pre; p.act = d->act;
+  return bf ? product<false, false, true, true>(p, ws, s) : product<true, true, true, true>(p, ws, s);
 }
 
 mtgnn_status linear_bwd_impl(const float* dy, int64_t lddy, const float* pre, const void* x, int64_t ldx,
                              const int32_t* n_rows, int64_t max_rows, const void* W, const mtgnn_linear_dims* d,
                              float* dx, int64_t lddx, float* dW, float* db, void* ws, size_t ws_bytes, hipStream_t s) {
-  float* g = (float*)ws;
-  const size_t m = al((size_t)max_rows * d->d_out * 4);
-  k_linear_slope<<<(unsigned)cdiv(max_rows * d->d_out, 256), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, d->d_out,
-                                                                         d->act, g);
-  MTGNN_CHECK_LAUNCH("linear_slope");
-  if (dx)
-    MTGNN_TRY((linear_dx(g, d->d_out, W, d->dtype, d->d_in, dx, lddx, max_rows, n_rows, d->d_out, d->d_in, false, s)));
-  return linear_dw(g, d->d_out, x, d->dtype, ldx, dW, d->d_in, max_rows, n_rows, d->d_out, d->d_in, (char*)ws + m,
-                   ws_bytes - m, s, db);
+  const bool bf = d->dtype == MTGNN_BF16, direct = d->act == MTGNN_ACT_NONE;
+  const int n = d->d_out;
+  float* gbuf = (float*)ws;
+  float* part = (float*)((char*)ws + al((size_t)max_rows * n * 4));
+  void* rest = (char*)part + al((size_t)cdiv(max_rows, SLOPE_ROWS) * n * 4);
+  const float* g = direct ? dy : gbuf;   // without an activation dy is the slope
+  const int64_t ldg = direct ? lddy : n, blks = cdiv(max_rows, SLOPE_ROWS);
+  if (!direct || db) {
+    k_linear_slope<<<(unsigned)(blks * cdiv(n, 64)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act,
+                                                                  direct ? nullptr : gbuf, db ? part : nullptr);
+    MTGNN_CHECK_LAUNCH("linear_slope");
+  }
+  if (db) {
+    k_sum_parts<<<(unsigned)cdiv(n, 16), 256, 0, s>>>(Seqs{}, 0, (int)blks, part, n, n, db, 0, nullptr, nullptr);
+    MTGNN_CHECK_LAUNCH("linear_sum_parts");
+  }
+  if (dx) {
+    ProdP p{};
+    p.R = g; p.ldR = ldg; p.C = W; p.ldC = d->d_in;
+    p.rows = max_rows; p.cols = d->d_in; p.K = n; p.rows_dev = n_rows;
+    p.vecR = ldg % 4 == 0 && (uintptr_t)g % 16 == 0;
+    p.o = dx; p.ldo = lddx;
+    MTGNN_TRY((bf ? product<true, false, true, false>(p, rest, s) : product<true, true, true, false>(p, rest, s)));
+  }
+  ProdP p{};
+  p.R = g; p.ldR = ldg; p.C = x; p.ldC = ldx;
+  p.rows = n; p.cols = d->d_in; p.K = max_rows; p.K_dev = n_rows;
+  p.o = dW; p.ldo = d->d_in;
+  return bf ? product<true, false, false, false>(p, rest, s) : product<true, true, false, false>(p, rest, s);
 }
 
 }  // namespace mtgnn

@@ -859,7 +859,7 @@ mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
     MTGNN_CHECK_LAUNCH("scan_sum_bc");
   }
   const int64_t nd = (int64_t)d->n * d->d;
-  k_sum_parts<<<(unsigned)cdiv(nd + 2 * d->d, 16), 256, 0, s>>>(p.q, p.ch, o.part, nd + 2 * d->d, nd, g->dA, d->d,
+  k_sum_parts<<<(unsigned)cdiv(nd + 2 * d->d, 16), 256, 0, s>>>(p.q, p.ch, 0, o.part, nd + 2 * d->d, nd, g->dA, d->d,
                                                                 g->dD, g->ddelta_bias);
   MTGNN_CHECK_LAUNCH("scan_sum_parts");
   return MTGNN_OK;

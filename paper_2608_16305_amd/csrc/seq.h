@@ -154,15 +154,19 @@ __device__ __forceinline__ int64_t seq_slot(const int32_t* slot, int64_t n_slots
 namespace {
 
 // Column sums of the chunks' shares part[chunk][cols] in order, into up to three tensors of n0, n1, cols - n0 - n1
-// columns (each may be NULL); a chunk is `ch` rows, and only those with rows have a share.  16 columns a
-// block, 16 threads to each.
-__global__ __launch_bounds__(256) void k_sum_parts(Seqs q, int ch, const float* part, int64_t cols, int64_t n0,
-                                                   float* out0, int64_t n1, float* out1, float* out2) {
+// columns (each may be NULL); a chunk is `ch` rows, and only those with rows have a share (q.off NULL: `n_parts` shares
+// all have one).  16 columns a block, 16 threads to each.
+__global__ __launch_bounds__(256) void k_sum_parts(Seqs q, int ch, int n_parts, const float* part, int64_t cols,
+                                                   int64_t n0, float* out0, int64_t n1, float* out1, float* out2) {
   __shared__ float s[16][17];
-  const SeqRange r = seq_range(q);
+  int c0 = 0, c1 = n_parts;
+  if (q.off) {
+    const SeqRange r = seq_range(q);
+    c0 = r.lo < r.hi ? r.lo / ch : 0;
+    c1 = r.lo < r.hi ? (r.hi - 1) / ch + 1 : 0;
+  }
   const int j = threadIdx.x & 15, k = threadIdx.x >> 4;
   const int64_t col = (int64_t)blockIdx.x * 16 + j;
-  const int c0 = r.lo < r.hi ? r.lo / ch : 0, c1 = r.lo < r.hi ? (r.hi - 1) / ch + 1 : 0;
   float v = 0.f;
   if (col < cols)
     for (int c = c0 + k; c < c1; c += 16) v += part[c * cols + col];
