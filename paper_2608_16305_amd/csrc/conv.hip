@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <initializer_list>
 
+#include "bf16_split.h"
 #include "ops.h"
 #include "seq.h"
 
@@ -49,7 +50,7 @@ __device__ __forceinline__ void get(const void* p, int64_t i, float (&v)[V]) {
 template <typename T, int V>
 __device__ __forceinline__ void put(void* p, int64_t i, const float (&v)[V]) {
   if constexpr (V == 2 && sizeof(T) == 2) {
-    *(uint32_t*)((T*)p + i) = (uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16;
+    *(uint32_t*)((T*)p + i) = cvt2_bf16(v[0], v[1]);
   } else if constexpr (V == 2) {
     *(float2*)((T*)p + i) = make_float2(v[0], v[1]);
   } else {
@@ -123,30 +124,38 @@ __global__ __launch_bounds__(256) void k_conv(ConvP p) {
   for (int j = 0; j < W; ++j) get<T, V>(p.w, (int64_t)j * p.d + me.col, w[j]);
 #pragma unroll
   for (int v = 0; v < V; ++v) b[v] = p.b ? p.b[me.col + v] : 0.f;
-  for (int tb = me.t0; tb < me.t1; tb += TR) {
-    float xr[TR + W - 1][V], sv[TR][W - 1][V];
+  const auto tile = [&](int tb, auto inside) {
+    constexpr bool INSIDE = decltype(inside)::value;
+    float xr[TR + W - 1][V], sv[INSIDE ? 1 : TR][W - 1][V];
 #pragma unroll
     for (int i = 0; i < TR + W - 1; ++i)
       get<T, V>(p.x, (int64_t)min(max(tb + i - (W - 1), r.lo), me.t1 - 1) * p.ldx + me.col, xr[i]);
     int pos[TR];
     int64_t st[TR];
-    places<TR, false>(at, tb, me.t0, me.t1, pos, st);
+    if constexpr (!INSIDE) {
+      places<TR, false>(at, tb, me.t0, me.t1, pos, st);
 #pragma unroll
-    for (int i = 0; i < TR; ++i) first_states<T, W, V>(p, pos[i], tb + i < me.t1 ? st[i] : -1, me.col, sv[i]);
+      for (int i = 0; i < TR; ++i) first_states<T, W, V>(p, pos[i], tb + i < me.t1 ? st[i] : -1, me.col, sv[i]);
+    }
 #pragma unroll
     for (int i = 0; i < TR; ++i) {
       if (tb + i >= me.t1) break;
       float win[W][V], y[V];
-      window<W, V>(xr, sv[i], i, pos[i], win);
+      window<W, V>(xr, sv[INSIDE ? 0 : i], i, INSIDE ? W : pos[i], win);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float a = b[v];
 #pragma unroll
         for (int j = 0; j < W; ++j) a = fmaf(w[j][v], win[j][v], a);
-        y[v] = act_(p.act, a);
+        y[v] = p.act ? silu_(a) : a;
       }
       if (me.mine) put<T, V>(p.y, (int64_t)(tb + i) * p.ldy + me.col, y);
     }
+  };
+  for (int tb = me.t0; tb < me.t1; tb += TR) {
+    while (tb >= at.end && at.s + 1 < at.n) at.next();
+    if (tb - at.beg >= W - 1 && tb + TR <= at.end) tile(tb, std::true_type{});
+    else tile(tb, std::false_type{});
   }
 }
 
@@ -205,8 +214,9 @@ __global__ __launch_bounds__(256) void k_conv_back(ConvP p) {
     b[v] = p.b ? p.b[me.col + v] : 0.f;
     db[v] = 0.f;
   }
-  for (int tb = me.t0; tb < me.t1; tb += TR) {
-    float xr[N + W - 1][V], g[N][V];
+  const auto tile = [&](int tb, auto inside) {
+    constexpr bool INSIDE = decltype(inside)::value;
+    float xr[N + W - 1][V], g[N][V], sv[INSIDE ? 1 : N][W - 1][V];
 #pragma unroll
     for (int i = 0; i < N + W - 1; ++i)
       get<T, V>(p.x, (int64_t)min(max(tb + i - (W - 1), r.lo), r.hi - 1) * p.ldx + me.col, xr[i]);
@@ -214,22 +224,23 @@ __global__ __launch_bounds__(256) void k_conv_back(ConvP p) {
     for (int i = 0; i < N; ++i) get<float, V>(p.dy, (int64_t)min(tb + i, r.hi - 1) * p.lddy + me.col, g[i]);
     int pos[N];
     int64_t st[N];
-    while (at.beg > tb) at.prev();
-    places<N, true>(at, tb, tb, r.hi, pos, st);
-    float sv[N][W - 1][V];
+    if constexpr (!INSIDE) {
+      places<N, true>(at, tb, tb, r.hi, pos, st);
 #pragma unroll
-    for (int i = 0; i < N; ++i) first_states<T, W, V>(p, pos[i], st[i], me.col, sv[i]);
+      for (int i = 0; i < N; ++i) first_states<T, W, V>(p, pos[i], st[i], me.col, sv[i]);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float win[W][V];
-      window<W, V>(xr, sv[i], i, pos[i], win);
+      window<W, V>(xr, sv[INSIDE ? 0 : i], i, INSIDE ? W : pos[i], win);
       const bool on = i < TR && tb + i < me.t1;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float a = b[v];
 #pragma unroll
         for (int j = 0; j < W; ++j) a = fmaf(w[j][v], win[j][v], a);
-        g[i][v] = tb + i < r.hi ? g[i][v] * dact_(p.act, a) : 0.f;
+        const float s = p.act ? dsilu_(a) : 1.f;
+        g[i][v] = INSIDE || tb + i < r.hi ? g[i][v] * s : 0.f;
         if (on) {
           db[v] += g[i][v];
 #pragma unroll
@@ -245,10 +256,19 @@ __global__ __launch_bounds__(256) void k_conv_back(ConvP p) {
       for (int v = 0; v < V; ++v) {
         dx[v] = w[W - 1][v] * g[i][v];
 #pragma unroll
-        for (int k = 1; k < W; ++k) dx[v] += tb + i + k < r.hi && pos[i + k] >= k ? w[W - 1 - k][v] * g[i + k][v] : 0.f;
+        for (int k = 1; k < W; ++k) {
+          const bool same = INSIDE || (tb + i + k < r.hi && pos[i + k] >= k);
+          dx[v] = same ? fmaf(w[W - 1 - k][v], g[i + k][v], dx[v]) : dx[v];
+        }
       }
       if (me.mine) put<float, V>(p.dx, (int64_t)(tb + i) * p.lddx + me.col, dx);
     }
+  };
+  for (int tb = me.t0; tb < me.t1; tb += TR) {
+    while (at.beg > tb) at.prev();
+    while (tb >= at.end && at.s + 1 < at.n) at.next();
+    if (tb - at.beg >= W - 1 && tb + N <= at.end) tile(tb, std::true_type{});
+    else tile(tb, std::false_type{});
   }
   if (me.mine) {
     float* part = p.part + (int64_t)me.chunk * (W + 1) * p.d + me.col;
@@ -281,7 +301,7 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvP p, const int32_t* n_row
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) ((T*)p.st_out)[(k * (W - 1) + j) * p.d + ch] = v[j + 1];
   }
-  Elem<T>::store((T*)p.y, row * p.ldy + ch, act_(p.act, a));
+  Elem<T>::store((T*)p.y, row * p.ldy + ch, p.act ? silu_(a) : a);
 }
 
 // ------------------------------------------------------------------ host

@@ -250,33 +250,58 @@ __global__ __launch_bounds__(64 * NB) void k_scan_local(ScanP p) {
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
-// first.  A thread per state and channel; eight chunks are requested at a time.
-__global__ __launch_bounds__(64) void k_scan_carry(ScanP p, int back) {
-  const int64_t nd = (int64_t)p.n * p.d, i = (int64_t)blockIdx.x * 64 + threadIdx.x;
-  if (i >= nd) return;
+// first.  A block has 16 states and channels; each of 64 threads to one takes a run of chunks, once for
+// what the run hands on, h -> own + decay h, and, after a scan over the runs, once with what enters it.  (One
+// thread over all chunks waited for memory 127 times in turn at 1,013 chunks: 144 us, against ten.)
+constexpr int RUNS = 64, RUN_COLS = 16;
+__global__ __launch_bounds__(RUNS * RUN_COLS) void k_scan_carry(ScanP p, int back) {
+  __shared__ float s_h[RUNS][RUN_COLS + 1], s_d[RUNS][RUN_COLS + 1];   // a decay of -1: nothing passes
+  const int64_t nd = (int64_t)p.n * p.d;
+  const int j = threadIdx.x % RUN_COLS, run = threadIdx.x / RUN_COLS;
+  const int64_t i = min((int64_t)blockIdx.x * RUN_COLS + j, nd - 1);
+  const bool mine = (int64_t)blockIdx.x * RUN_COLS + j < nd;
   const int ch = (int)(i % p.d);
   const float A2 = p.A[i] * LOG2E;
-  float h = 0.f;
-  constexpr int U = 8;
-  for (int c0 = 0; c0 < p.nchunk; c0 += U) {
-    float e[U], sd[U];
-    int f[U];
+  const int len = (p.nchunk + RUNS - 1) / RUNS, k0 = run * len, k1 = min(p.nchunk, k0 + len);
+  const auto walk = [&](float& h, float& d, bool write) {
+    constexpr int U = 8;
+    for (int k = k0; k < k1; k += U) {
+      float e[U], sd[U];
+      int f[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = min(c0 + u, p.nchunk - 1), c = back ? p.nchunk - 1 - k : k;
-      e[u] = p.E[c * nd + i];
-      sd[u] = p.sumdt[(int64_t)c * p.d + ch];
-      f[u] = p.flag[c];
-    }
+      for (int u = 0; u < U; ++u) {
+        const int v = min(k + u, k1 - 1), c = back ? p.nchunk - 1 - v : v;
+        e[u] = p.E[c * nd + i];
+        sd[u] = p.sumdt[(int64_t)c * p.d + ch];
+        f[u] = p.flag[c];
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (c0 + u >= p.nchunk) break;
-      const int c = back ? p.nchunk - 1 - (c0 + u) : c0 + u;
-      p.E[c * nd + i] = h;
-      const float next = fmaf(__builtin_amdgcn_exp2f(A2 * sd[u]), h, e[u]);
-      h = f[u] == CARRY_ADD ? next : f[u] == CARRY_OWN ? e[u] : 0.f;
+      for (int u = 0; u < U; ++u) {
+        if (k + u >= k1) break;
+        const int c = back ? p.nchunk - 1 - (k + u) : k + u;
+        if (write && mine) p.E[c * nd + i] = h;
+        const float a = __builtin_amdgcn_exp2f(A2 * sd[u]), next = fmaf(a, h, e[u]);
+        h = f[u] == CARRY_ADD ? next : f[u] == CARRY_OWN ? e[u] : 0.f;
+        d = f[u] == CARRY_ADD && d >= 0.f ? d * a : -1.f;
+      }
     }
+  };
+  float h = 0.f, d = 1.f;
+  walk(h, d, false);
+  s_h[run][j] = h;
+  s_d[run][j] = d;
+  __syncthreads();
+  for (int o = 1; o < RUNS; o <<= 1) {
+    const float ph = run >= o ? s_h[run - o][j] : 0.f, pd = run >= o ? s_d[run - o][j] : 1.f;
+    __syncthreads();
+    h = d < 0.f ? h : fmaf(d, ph, h);
+    d = d < 0.f || pd < 0.f ? -1.f : d * pd;
+    s_h[run][j] = h;
+    s_d[run][j] = d;
+    __syncthreads();
   }
+  h = run > 0 ? s_h[run - 1][j] : 0.f;
+  walk(h, d, true);
 }
 
 template <typename T, int SPL, int NB>
@@ -485,12 +510,12 @@ __global__ __launch_bounds__(64 * NB, 1) void k_scan_back(ScanP p, ScanG o) {
       float e = dy;
       if (p.z) {
         const float z = Elem<T>::load((const T*)p.z, row * p.ldz + col);
-        const float sg = sigmoid_exact(z);
+        const float sg = sigmoid_hw(z);
         e = dy * (z * sg);
         s_z[i][me.lane] = dy * (sg * fmaf(z, 1.f - sg, 1.f));
       }
       s_x[i][me.lane] = x;
-      s_s[i][me.lane] = p.softplus ? sigmoid_exact(u) : 1.f;
+      s_s[i][me.lane] = p.softplus ? sigmoid_hw(u) : 1.f;
       const float dt = mine ? step_size(p, u) : 0.f;
       s_dt[i][me.lane] = dt;
       s_dx[i][me.lane] = mine ? dt * x : 0.f;
@@ -659,32 +684,71 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(ScanP p, ScanG o) {
 
 // ------------------------------------------------------------------ single rows
 
-// A thread per row and channel: its states, strided by d, are n independent reads and writes (256 bytes a wave
-// each); state traffic bounds it.
-template <typename T>
+// A thread per row and V neighbouring channels.  Its states are n reads and writes a row of the table apart (a
+// wave's are 1 KB together for V = 4), eight of them in flight; that traffic bounds it.
+template <int V>
+__device__ __forceinline__ void get_f(const float* p, float (&v)[V]) {
+  if constexpr (V == 4) {
+    const float4 f = *(const float4*)p;
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    v[0] = p[0];
+  }
+}
+template <typename T, int V>
 __global__ __launch_bounds__(256) void k_scan_step(ScanP p, const int32_t* n_rows, int64_t max_rows) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = e / p.d;
+  const int dv = p.d / V;
+  const int64_t row = e / dv;
   if (row >= eff_count(max_rows, n_rows)) return;
-  const int ch = (int)(e % p.d), g = ch / p.per;
+  const int ch = (int)(e % dv) * V, g = ch / p.per;
   const int64_t k = seq_slot(p.q.slot, p.q.n_slots, row);
-  const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + ch) + (p.bias ? p.bias[ch] : 0.f);
-  const float x = Elem<T>::load((const T*)p.x, row * p.ldx + ch);
-  const float dt = step_size(p, u), dx = dt * x;
   const T *B = (const T*)p.B + row * p.ldB + g * p.n, *C = (const T*)p.C + row * p.ldC + g * p.n;
   const float* in = p.st_in && k >= 0 ? p.st_in + k * p.n * p.d + ch : nullptr;
   float* out = p.st_out && k >= 0 ? p.st_out + k * p.n * p.d + ch : nullptr;
-  float y = 0.f;
-  for (int i = 0; i < p.n; ++i) {
-    const float a = __builtin_amdgcn_exp2f(dt * (p.A[(int64_t)i * p.d + ch] * LOG2E));
-    const float h0 = in ? in[(int64_t)i * p.d] : 0.f;
-    const float h = fmaf(a, h0, dx * Elem<T>::load(B, i));
-    if (out) out[(int64_t)i * p.d] = h;
-    y = fmaf(h, Elem<T>::load(C, i), y);
+  float x[V], z[V], dt[V], y[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + ch + v) + (p.bias ? p.bias[ch + v] : 0.f);
+    x[v] = Elem<T>::load((const T*)p.x, row * p.ldx + ch + v);
+    z[v] = p.z ? Elem<T>::load((const T*)p.z, row * p.ldz + ch + v) : 0.f;
+    dt[v] = step_size(p, u);
+    y[v] = 0.f;
   }
-  if (p.D) y = fmaf(p.D[ch], x, y);
-  if (p.z) y *= silu_(Elem<T>::load((const T*)p.z, row * p.ldz + ch));
-  Elem<T>::store((T*)p.y, row * p.ldy + ch, y);
+  constexpr int G = 8;
+  for (int i0 = 0; i0 < p.n; i0 += G) {
+    float h[G][V], A[G][V], b[G], c[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int64_t s = min(i0 + i, p.n - 1);
+#pragma unroll
+      for (int v = 0; v < V; ++v) h[i][v] = 0.f;
+      if (in) get_f<V>(in + s * p.d, h[i]);
+      get_f<V>(p.A + s * p.d + ch, A[i]);
+      b[i] = Elem<T>::load(B, s);
+      c[i] = Elem<T>::load(C, s);
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      if (i0 + i >= p.n) break;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        h[i][v] = fmaf(__builtin_amdgcn_exp2f(dt[v] * (A[i][v] * LOG2E)), h[i][v], dt[v] * x[v] * b[i]);
+        y[v] = fmaf(h[i][v], c[i], y[v]);
+      }
+      if (out) {
+        float* o = out + (int64_t)(i0 + i) * p.d;
+        if constexpr (V == 4) *(float4*)o = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
+        else o[0] = h[i][0];
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if (p.D) y[v] = fmaf(p.D[ch + v], x[v], y[v]);
+    if (p.z) y[v] *= silu_(z[v]);
+    Elem<T>::store((T*)p.y, row * p.ldy + ch + v, y[v]);
+  }
 }
 
 // ------------------------------------------------------------------ host
@@ -818,7 +882,7 @@ mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const m
   if (p.nchunk > 1) {
     scan_variant(d->dtype, d->n, LaunchLocal{p, grid, s});
     MTGNN_CHECK_LAUNCH("scan_local");
-    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, 64), 64, 0, s>>>(p, 0);
+    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 0);
     MTGNN_CHECK_LAUNCH("scan_carry");
   }
   scan_variant(d->dtype, d->n, LaunchOut{p, grid, s});
@@ -849,7 +913,7 @@ mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
   if (p.nchunk > 1) {
     scan_variant(d->dtype, d->n, LaunchBackLocal{p, o, grid, s});
     MTGNN_CHECK_LAUNCH("scan_back_local");
-    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, 64), 64, 0, s>>>(p, 1);
+    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 1);
     MTGNN_CHECK_LAUNCH("scan_carry");
   }
   scan_variant(d->dtype, d->n, LaunchBack{p, o, grid, s});
@@ -872,9 +936,15 @@ mtgnn_status scan_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t 
   p.q.slot = slot;
   p.q.n_slots = n_slots;
   p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
-  const unsigned grid = (unsigned)cdiv(max_rows * d->d, 256);
-  if (d->dtype == MTGNN_BF16) k_scan_step<uint16_t><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
-  else k_scan_step<float><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+  const bool four = scan_vec(p, state_in, state_out);
+  const unsigned grid = (unsigned)cdiv(max_rows * (d->d / (four ? 4 : 1)), 256);
+  const auto launch = [&](auto t) {
+    using T = decltype(t);
+    if (four) k_scan_step<T, 4><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+    else k_scan_step<T, 1><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+  };
+  if (d->dtype == MTGNN_BF16) launch(uint16_t{});
+  else launch(float{});
   MTGNN_CHECK_LAUNCH("scan_step");
   return MTGNN_OK;
 }

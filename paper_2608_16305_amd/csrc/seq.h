@@ -5,15 +5,22 @@
 
 namespace mtgnn {
 
-// 2^(v log2 e) and the like on the hardware's exponential, and the activations built on it.
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
+// e^x on the hardware's base-2 exponential, with the part of x log2 e that its float32 product loses: exact to a unit
+// of the last place or two (the product alone is off by |x| units).  x <= 0.
+__device__ __forceinline__ float exp_neg(float x) {
+  const float y = x < -150.f ? -150.f : x;   // e^-150 is 0; a NaN stays one
+  const float t = y * LOG2E, r = fmaf(y, 1.9259629911266175e-8f, fmaf(y, LOG2E, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, r * LN2, e);
+}
 // softplus(u) = max(u, 0) + log1p(e^-|u|).  log1p(v) = 2 atanh(s) with s = v / (2 + v) <= 1/3, by its series to s^17
 // (the rest is below 2^-27 of it): exact to a few units of the last place for every v, small ones too, where
 // log(1 + v) has lost v's low bits.
 __device__ __forceinline__ float softplus_(float u) {
-  const float v = expf(-fabsf(u));
+  const float v = exp_neg(-fabsf(u));
   const float s = v * __builtin_amdgcn_rcpf(2.f + v), q = s * s;
   float p = 1.f / 17.f;
   p = fmaf(p, q, 1.f / 15.f);
@@ -24,12 +31,11 @@ __device__ __forceinline__ float softplus_(float u) {
   p = fmaf(p, q, 1.f / 5.f);
   p = fmaf(p, q, 1.f / 3.f);
   p = fmaf(p, q, 1.f);
-  return fmaxf(u, 0.f) + 2.f * s * p;   // a NaN stays one through v
+  return fmaf(2.f * s, p, fmaxf(u, 0.f));   // a NaN stays one through v
 }
-__device__ __forceinline__ float sigmoid_exact(float u) { return __builtin_amdgcn_rcpf(1.f + expf(-u)); }
-__device__ __forceinline__ float silu_(float p) { return p * sigmoid_exact(p); }
+__device__ __forceinline__ float silu_(float p) { return p * sigmoid_hw(p); }
 __device__ __forceinline__ float dsilu_(float p) {
-  const float s = sigmoid_exact(p);
+  const float s = sigmoid_hw(p);
   return s * fmaf(p, 1.f - s, 1.f);
 }
 // act and its derivative for mtgnn_act `act` (uniform).
