@@ -11,14 +11,16 @@
 // state, so one sequence of 100,000 rows and 100,000 sequences of one row are the same amount of work per wave.
 // One chunk (few rows) needs k_scan_out alone.
 //
-// A block holds 64 channels of one group and all states: wave w the states 16 w .. 16 w + 15 (4 SPL of them, SPL = 4
-// where there is more than one wave), lane l the channels 4 (l / 4) .. + 3 and SPL states.  So the sum over the
-// states is one over four lanes (and the waves), the backward's sums over channels are over registers first,
-// and after the first of these lane l holds the value of channel l, as rows are read and written.
-// Rows are staged in LDS eight at a time: dt and dt x by the lane of their channel, B and C as they are.
+// Forward kernels: a wave has 64 channels of one group, a lane one channel and all its states, so the sum over the states
+// and everything of a row and channel stay in its lane.  B and C are the same for all lanes: read by scalar loads
+// into scalar registers, which the products take as they are, where a row is whole words of a supported
+// number of states, else staged in LDS and read by all lanes at once.
+// Backward: the sums that dB and dC need are over channels.  There a lane has four channels and 4 (2, 1) states, lane l the
+// channels 4 (l / 4) .. + 3, wave w the states 16 w .. 16 w + 15: sums over states are over four lanes, those over
+// channels over registers first and then 16 lanes, 48 lane moves a row together (192 with a channel a lane).
 //
-// Vector instructions bound it: per row, channel and state the exponential takes a wave 16 cycles, the rest of
-// the recurrence and the sum over states 16, against 8 bytes per row and channel in bfloat16.
+// Vector instructions bound it: per row, channel and state an exponential and four products and sums, against 8
+// bytes per row and channel in bfloat16.
 #include <algorithm>
 
 #include "ops.h"
@@ -177,14 +179,114 @@ __device__ __forceinline__ void chunk_rows(const ScanP& p, const SeqRange& r, in
 
 // ------------------------------------------------------------------ forward
 
-template <typename T, int SPL, int NB>
-__global__ __launch_bounds__(64 * NB) void k_scan_local(ScanP p) {
-  using P = Place<SPL, NB>;
-  constexpr int NP = P::NP;
-  __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT];
-  __shared__ __align__(16) float s_B[TT * NP];
+// The value, but not one that is known outside: the addresses that are made from it are made where they are used,
+// where otherwise a loop's 2 N of them would be kept in scalar registers that B and C need.
+__device__ __forceinline__ int64_t opaque(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
+// A lane's channel and its states.
+struct Lane {
+  int g, col0;
+  uint32_t col;     // of the lane, in its tile's first .. last channel
+  bool mine;
+  __device__ __forceinline__ Lane(const ScanP& p, int tile) {
+    const int lane = threadIdx.x & 63;
+    g = tile / p.tpg;
+    const int in = (tile % p.tpg) * CT;
+    col0 = g * p.per + in;
+    mine = in + lane < p.per;
+    col = mine ? lane : 0;
+  }
+  template <typename T>
+  __device__ __forceinline__ float at(const void* m, int64_t ld, int64_t row) const {   // m[row][channel]
+    return Elem<T>::load((const T*)m + row * ld + col0, col);
+  }
+  template <int N>
+  __device__ __forceinline__ void load(const ScanP& p, const float* tab, int64_t row, float (&h)[N]) const {
+    const int64_t step = opaque(p.d);
+    const float* q = tab + row * p.n * step + col0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = i < p.n ? q[i * step + col] : 0.f;
+  }
+  template <int N>
+  __device__ __forceinline__ void store(const ScanP& p, float* tab, int64_t row, const float (&h)[N]) const {
+    const int64_t step = opaque(p.d);
+    float* q = tab + row * p.n * step + col0;
+    if (!mine) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < p.n) q[i * step + col] = h[i];
+  }
+  template <int N>
+  __device__ __forceinline__ void decay(const ScanP& p, float (&A2)[N]) const {   // A log2 e
+    load(p, p.A, 0, A2);
+#pragma unroll
+    for (int i = 0; i < N; ++i) A2[i] *= LOG2E;
+  }
+};
+
+// B or C of a row, the same in every lane.  SC: by scalar loads (N words of float, or N / 2 of bfloat16 pairs; the matrix
+// is not written while the kernel runs); else from the tile staged in LDS.
+template <typename T, int N, bool SC>
+struct States {
+  static constexpr int WORDS = SC ? 4 : TT * N;
+  const T* m;
+  int64_t ld;
+  int n;
+  float* lds;
+  __device__ __forceinline__ States(const void* src, int64_t ld_, int n_, int g, float* lds_)
+      : m((const T*)src + g * n_), ld(ld_), n(n_), lds(lds_) {}
+  __device__ __forceinline__ void stage(int row, int last) const {
+    if constexpr (!SC) {
+      for (int e = threadIdx.x; e < TT * N; e += 64) {
+        const int i = e / N, s = e % N;
+        const float v = Elem<T>::load(m, (int64_t)min(row + i, last) * ld + min(s, n - 1));
+        lds[e] = s < n ? v : 0.f;
+      }
+    }
+  }
+  template <int M>
+  __device__ __forceinline__ void get(int i, int row, int s0, float (&v)[M]) const {   // states s0 .. of the tile's row i
+    if constexpr (SC) {
+      const auto q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)(m + row * ld + s0);
+#pragma unroll
+      for (int k = 0; k < M; ++k) {
+        if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(q[k]);
+        else v[k] = __uint_as_float(k % 2 ? q[k / 2] & 0xffff0000u : q[k / 2] << 16);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < M; k += 4) {
+        const float4 f = *(const float4*)(lds + i * N + s0 + k);
+        v[k] = f.x; v[k + 1] = f.y; v[k + 2] = f.z; v[k + 3] = f.w;
+      }
+    }
+  }
+};
+// f(first state, number of states) over N states, sixteen at a time (more of B and C have no registers).
+template <int N, class F>
+__device__ __forceinline__ void by_sixteen(F f) {
+  constexpr int M = N < 16 ? N : 16;
+#pragma unroll
+  for (int s0 = 0; s0 < N; s0 += M) {
+    if (N > 16) __builtin_amdgcn_sched_barrier(0);
+    f(s0, std::integral_constant<int, M>{});
+  }
+}
+template <int N>
+__device__ __forceinline__ void zero(float (&h)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) h[i] = 0.f;
+}
+
+template <typename T, int N, bool SC>
+__global__ __launch_bounds__(64) void k_scan_local(ScanP p) {
+  __shared__ __align__(16) float s_B[States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const P me(p, tile);
+  const Lane me(p, tile);
+  const States<T, N, SC> B(p.B, p.ldB, p.n, me.g, s_B);
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
@@ -196,9 +298,9 @@ __global__ __launch_bounds__(64 * NB) void k_scan_local(ScanP p) {
   }
   if (tile == 0 && threadIdx.x == 0) p.flag[c] = flag;
   if (flag == CARRY_NONE) return;
-  float A2[4][SPL], h[4][SPL];
+  float A2[N], h[N];
   me.decay(p, A2);
-  zero_state(&h[0][0], 4 * SPL);
+  zero(h);
   int t = t0;
   if (flag == CARRY_OWN) {
     t = at.beg;
@@ -206,47 +308,35 @@ __global__ __launch_bounds__(64 * NB) void k_scan_local(ScanP p) {
     if (k >= 0) me.load(p, p.st_in, k, h);
     if (p.first) me.store(p, p.first, c, h);
   }
-  const bool mine = me.lane < me.left;
-  const int col = me.ch0 + (mine ? me.lane : 0);
-  const float bias = p.bias ? p.bias[col] : 0.f;
+  const float bias = p.bias ? p.bias[me.col0 + me.col] : 0.f;
   float sum = 0.f;
   for (; t < t1; t += TT) {
+    float u[TT], x[TT];
 #pragma unroll
     for (int i = 0; i < TT; ++i) {
-      if (i % NB != me.wid) continue;
-      const int64_t row = min(t + i, t1 - 1);
-      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
-      const float x = Elem<T>::load((const T*)p.x, row * p.ldx + col);
-      const bool on = mine && t + i < t1;   // no row: dt = 0 leaves the state as it is
-      const float dt = on ? step_size(p, u + bias) : 0.f;
-      s_dt[i][me.lane] = dt;
-      s_dx[i][me.lane] = on ? dt * x : 0.f;
+      const int row = min(t + i, t1 - 1);
+      u[i] = me.at<T>(p.delta, p.ldd, row);
+      x[i] = me.at<T>(p.x, p.ldx, row);
+    }
+    B.stage(t, t1 - 1);
+    if constexpr (!SC) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      if (t + i >= t1) break;
+      const float dt = step_size(p, u[i] + bias), dx = dt * x[i];
       sum += dt;
+      by_sixteen<N>([&](int s0, auto m) {
+        constexpr int M = decltype(m)::value;
+        float b[M];
+        B.get(i, t + i, s0, b);
+#pragma unroll
+        for (int s = 0; s < M; ++s) h[s0 + s] = fmaf(__builtin_amdgcn_exp2f(dt * A2[s0 + s]), h[s0 + s], dx * b[s]);
+      });
     }
-    stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, t, t1 - 1, s_B);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      float dt[4], dx[4], b[SPL];
-      lds_get<4>(&s_dt[i][me.cb], dt);
-      lds_get<4>(&s_dx[i][me.cb], dx);
-      lds_get<SPL>(&s_B[i * NP + me.n0], b);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int s = 0; s < SPL; ++s)
-          h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
-    }
-    __syncthreads();
+    if constexpr (!SC) __syncthreads();
   }
   me.store(p, p.E, c, h);
-  if constexpr (NB > 1) {
-    s_dt[me.wid][me.lane] = sum;
-    __syncthreads();
-    sum = 0.f;
-    for (int w = 0; w < NB; ++w) sum += s_dt[w][me.lane];
-  }
-  if (me.wid == 0 && mine) p.sumdt[(int64_t)c * p.d + col] = sum;
+  if (me.mine) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
@@ -304,96 +394,84 @@ __global__ __launch_bounds__(RUNS * RUN_COLS) void k_scan_carry(ScanP p, int bac
   walk(h, d, true);
 }
 
-template <typename T, int SPL, int NB>
-__global__ __launch_bounds__(64 * NB) void k_scan_out(ScanP p) {
-  using P = Place<SPL, NB>;
-  constexpr int NP = P::NP;
-  __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT];
-  __shared__ __align__(16) float s_B[TT * NP], s_C[TT * NP];
-  __shared__ float s_y[NB > 1 ? NB : 1][TT][CT];
+template <typename T, int N, bool SC>
+__global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
+  __shared__ __align__(16) float s_B[States<T, N, SC>::WORDS], s_C[States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const P me(p, tile);
+  const Lane me(p, tile);
+  const States<T, N, SC> B(p.B, p.ldB, p.n, me.g, s_B), C(p.C, p.ldC, p.n, me.g, s_C);
   if (p.carried && blockIdx.x == 0 && threadIdx.x == 0) *p.carried = p.st_in != nullptr;
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
   if (t0 >= t1) return;
   SeqWalk at(p.q, r, t0);
-  float A2[4][SPL], h[4][SPL];
+  float A2[N], h[N];
   me.decay(p, A2);
-  zero_state(&h[0][0], 4 * SPL);
+  zero(h);
   if (at.beg < t0) me.load(p, p.E, c, h);
-  const bool mine = me.lane < me.left;
-  const int col = me.ch0 + (mine ? me.lane : 0);
-  const float bias = p.bias ? p.bias[col] : 0.f, D = p.D ? p.D[col] : 0.f;
+  const float bias = p.bias ? p.bias[me.col0 + me.col] : 0.f, D = p.D ? p.D[me.col0 + me.col] : 0.f;
   for (int tb = t0 / TT * TT; tb < t1; tb += TT) {
-    float xr[TT], zr[TT], yr[TT];
+    float u[TT], x[TT], z[TT];
 #pragma unroll
     for (int i = 0; i < TT; ++i) {
-      if (i % NB != me.wid) continue;
-      const int64_t row = min(max(tb + i, t0), t1 - 1);
-      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
-      xr[i] = Elem<T>::load((const T*)p.x, row * p.ldx + col);
-      zr[i] = p.z ? Elem<T>::load((const T*)p.z, row * p.ldz + col) : 0.f;
-      const float dt = mine ? step_size(p, u + bias) : 0.f;
-      s_dt[i][me.lane] = dt;
-      s_dx[i][me.lane] = mine ? dt * xr[i] : 0.f;
+      const int row = min(max(tb + i, t0), t1 - 1);
+      u[i] = me.at<T>(p.delta, p.ldd, row);
+      x[i] = me.at<T>(p.x, p.ldx, row);
+      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 0.f;
     }
-    stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, tb, t1 - 1, s_B);
-    stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, t1 - 1, s_C);
-    __syncthreads();
+    B.stage(tb, t1 - 1);
+    C.stage(tb, t1 - 1);
+    if constexpr (!SC) __syncthreads();
+    const auto row = [&](int i) {
+      const float dt = step_size(p, u[i] + bias), dx = dt * x[i];
+      float y[2] = {D * x[i], 0.f};
+      by_sixteen<N>([&](int s0, auto m) {
+        constexpr int M = decltype(m)::value;
+        float b[M], cc[M];
+        B.get(i, tb + i, s0, b);
+        C.get(i, tb + i, s0, cc);
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      const int t = tb + i;
-      if (t < t0) continue;
-      if (t >= t1) break;
-      if (t == at.beg) {
-        const int64_t k = p.st_in ? at.row() : -1;
-        if (k >= 0) me.load(p, p.first && at.end > t1 ? p.first : p.st_in, p.first && at.end > t1 ? c : k, h);
-        else zero_state(&h[0][0], 4 * SPL);
-        if (p.init) me.store(p, p.init, at.s, h);
-      } else if (i == 0 && p.hs) {
-        me.store(p, p.hs, tb / TT, h);
-      }
-      float dt[4], dx[4], b[SPL], cc[SPL], y[4];
-      lds_get<4>(&s_dt[i][me.cb], dt);
-      lds_get<4>(&s_dx[i][me.cb], dx);
-      lds_get<SPL>(&s_B[i * NP + me.n0], b);
-      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        y[k] = 0.f;
-#pragma unroll
-        for (int s = 0; s < SPL; ++s) {
-          h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
-          y[k] = fmaf(h[k][s], cc[s], y[k]);
+        for (int s = 0; s < M; ++s) {
+          h[s0 + s] = fmaf(__builtin_amdgcn_exp2f(dt * A2[s0 + s]), h[s0 + s], dx * b[s]);
+          y[s & 1] = fmaf(h[s0 + s], cc[s], y[s & 1]);
         }
+      });
+      float v = y[0] + y[1];
+      if (p.z) v *= silu_(z[i]);
+      if (me.mine) Elem<T>::store((T*)p.y + (int64_t)(tb + i) * p.ldy + me.col0, me.col, v);
+    };
+    const auto leave = [&] {   // after a sequence's last row
+      if (p.st_out) {
+        const int64_t k = at.row();
+        if (k >= 0) me.store(p, p.st_out, k, h);
       }
-      yr[i] = quad_sums(y);
-      if constexpr (NB > 1) s_y[me.wid][i][me.lane] = yr[i];
-      if (t + 1 == at.end) {
-        if (p.st_out) {
-          const int64_t k = at.row();
-          if (k >= 0) me.store(p, p.st_out, k, h);
+      at.next();
+    };
+    if (tb >= t0 && tb > at.beg && tb + TT <= at.end && tb + TT <= t1) {   // all of one sequence
+      if (p.hs) me.store(p, p.hs, tb / TT, h);
+#pragma unroll
+      for (int i = 0; i < TT; ++i) row(i);
+      if (tb + TT == at.end) leave();
+    } else {
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const int t = tb + i;
+        if (t < t0) continue;
+        if (t >= t1) break;
+        if (t == at.beg) {
+          const int64_t k = p.st_in ? at.row() : -1;
+          if (k >= 0) me.load(p, p.first && at.end > t1 ? p.first : p.st_in, p.first && at.end > t1 ? c : k, h);
+          else zero(h);
+          if (p.init) me.store(p, p.init, at.s, h);
+        } else if (i == 0 && p.hs) {
+          me.store(p, p.hs, tb / TT, h);
         }
-        at.next();
+        row(i);
+        if (t + 1 == at.end) leave();
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      if (i % NB != me.wid || tb + i < t0 || tb + i >= t1) continue;
-      float v = yr[i];
-      if constexpr (NB > 1) {
-        v = 0.f;
-#pragma unroll
-        for (int w = 0; w < NB; ++w) v += s_y[w][i][me.lane];
-      }
-      v = fmaf(D, xr[i], v);
-      if (p.z) v *= silu_(zr[i]);
-      if (mine) Elem<T>::store((T*)p.y, (int64_t)(tb + i) * p.ldy + col, v);
-    }
-    if constexpr (NB > 1) __syncthreads();
+    if constexpr (!SC) __syncthreads();
   }
 }
 
@@ -404,14 +482,12 @@ __global__ __launch_bounds__(64 * NB) void k_scan_out(ScanP p) {
 // k_scan_back then goes over a chunk's tiles from the last to the first: each tile's states forwards from the
 // forward's checkpoint, kept in registers (eight rows of them, why a checkpoint is every eight), then g backwards.
 
-template <typename T, int SPL, int NB>
-__global__ __launch_bounds__(64 * NB) void k_scan_back_local(ScanP p, ScanG o) {
-  using P = Place<SPL, NB>;
-  constexpr int NP = P::NP;
-  __shared__ __align__(16) float s_dt[TT][CT], s_e[TT][CT];
-  __shared__ __align__(16) float s_C[TT * NP];
+template <typename T, int N, bool SC>
+__global__ __launch_bounds__(64) void k_scan_back_local(ScanP p, ScanG o) {
+  __shared__ __align__(16) float s_C[States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const P me(p, tile);
+  const Lane me(p, tile);
+  const States<T, N, SC> C(p.C, p.ldC, p.n, me.g, s_C);
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
@@ -424,52 +500,40 @@ __global__ __launch_bounds__(64 * NB) void k_scan_back_local(ScanP p, ScanG o) {
   if (tile == 0 && threadIdx.x == 0) p.flag[c] = flag;
   if (flag == CARRY_NONE) return;
   const int stop = min(at.end, t1);
-  float A2[4][SPL], g[4][SPL];
+  float A2[N], g[N];
   me.decay(p, A2);
-  zero_state(&g[0][0], 4 * SPL);
-  const bool mine = me.lane < me.left;
-  const int col = me.ch0 + (mine ? me.lane : 0);
-  const float bias = p.bias ? p.bias[col] : 0.f;
+  zero(g);
+  const float bias = p.bias ? p.bias[me.col0 + me.col] : 0.f;
   float sum = 0.f;
   for (int tb = t0 + (stop - 1 - t0) / TT * TT; tb >= t0; tb -= TT) {
+    float u[TT], z[TT], e[TT];
 #pragma unroll
     for (int i = 0; i < TT; ++i) {
-      if (i % NB != me.wid) continue;
-      const int64_t row = min(tb + i, stop - 1);
-      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col);
-      const float z = p.z ? Elem<T>::load((const T*)p.z, row * p.ldz + col) : 0.f;
-      float e = o.dy[row * o.lddy + col];
-      if (p.z) e *= silu_(z);
-      const bool on = mine && tb + i < stop;
-      const float dt = on ? step_size(p, u + bias) : 0.f;
-      s_dt[i][me.lane] = dt;
-      s_e[i][me.lane] = on ? e : 0.f;
-      sum += dt;
+      const int row = min(tb + i, stop - 1);
+      u[i] = me.at<T>(p.delta, p.ldd, row);
+      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 0.f;
+      e[i] = me.at<float>(o.dy, o.lddy, row);
     }
-    stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, stop - 1, s_C);
-    __syncthreads();
+    C.stage(tb, stop - 1);
+    if constexpr (!SC) __syncthreads();
 #pragma unroll
     for (int i = TT - 1; i >= 0; --i) {
-      float dt[4], e[4], cc[SPL];
-      lds_get<4>(&s_dt[i][me.cb], dt);
-      lds_get<4>(&s_e[i][me.cb], e);
-      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+      if (tb + i >= stop) continue;
+      const float dt = step_size(p, u[i] + bias), ee = p.z ? e[i] * silu_(z[i]) : e[i];
+      sum += dt;
+      by_sixteen<N>([&](int s0, auto m) {
+        constexpr int M = decltype(m)::value;
+        float cc[M];
+        C.get(i, tb + i, s0, cc);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int s = 0; s < SPL; ++s)
-          g[k][s] = __builtin_amdgcn_exp2f(dt[k] * A2[k][s]) * fmaf(e[k], cc[s], g[k][s]);
+        for (int s = 0; s < M; ++s)
+          g[s0 + s] = __builtin_amdgcn_exp2f(dt * A2[s0 + s]) * fmaf(ee, cc[s], g[s0 + s]);
+      });
     }
-    __syncthreads();
+    if constexpr (!SC) __syncthreads();
   }
   me.store(p, p.E, c, g);
-  if constexpr (NB > 1) {
-    s_dt[me.wid][me.lane] = sum;
-    __syncthreads();
-    sum = 0.f;
-    for (int w = 0; w < NB; ++w) sum += s_dt[w][me.lane];
-  }
-  if (me.wid == 0 && mine) p.sumdt[(int64_t)c * p.d + col] = sum;
+  if (me.mine) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
 }
 
 template <typename T, int SPL, int NB>
@@ -815,26 +879,47 @@ void scan_variant(int dtype, int n, F f) {
   else by(float{});
 }
 
+// The lane-per-channel kernels: n rounded up, and whether B's and C's rows are whole words (n of a supported number).
+template <typename F>
+void scan_lane_variant(const ScanP& p, int dtype, F f) {
+  const int N = p.n <= 4 ? 4 : p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+  const bool words = p.n == N && (dtype == MTGNN_F32 || (p.ldB % 2 == 0 && p.ldC % 2 == 0 && (uintptr_t)p.B % 4 == 0 &&
+                                                         (uintptr_t)p.C % 4 == 0));
+  const auto by = [&](auto t) {
+    using T = decltype(t);
+    const auto with = [&](auto sc) {
+      constexpr bool SC = decltype(sc)::value;
+      if (N == 4) f.template operator()<T, 4, SC>();
+      else if (N == 8) f.template operator()<T, 8, SC>();
+      else if (N == 16) f.template operator()<T, 16, SC>();
+      else if (N == 32) f.template operator()<T, 32, SC>();
+      else f.template operator()<T, 64, SC>();
+    };
+    if (words) with(std::true_type{});
+    else with(std::false_type{});
+  };
+  if (dtype == MTGNN_BF16) by(uint16_t{});
+  else by(float{});
+}
+
 struct LaunchLocal {
   const ScanP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int SPL, int NB> void operator()() const { k_scan_local<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p); }
+  template <typename T, int N, bool SC> void operator()() const { k_scan_local<T, N, SC><<<grid, 64, 0, s>>>(p); }
 };
 struct LaunchOut {
   const ScanP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int SPL, int NB> void operator()() const { k_scan_out<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p); }
+  template <typename T, int N, bool SC> void operator()() const { k_scan_out<T, N, SC><<<grid, 64, 0, s>>>(p); }
 };
 struct LaunchBackLocal {
   const ScanP& p;
   const ScanG& g;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int SPL, int NB> void operator()() const {
-    k_scan_back_local<T, SPL, NB><<<grid, 64 * NB, 0, s>>>(p, g);
-  }
+  template <typename T, int N, bool SC> void operator()() const { k_scan_back_local<T, N, SC><<<grid, 64, 0, s>>>(p, g); }
 };
 struct LaunchBack {
   const ScanP& p;
@@ -880,12 +965,12 @@ mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const m
   if (state_in && state_in == state_out && p.nchunk > 1) p.first = (float*)((char*)ws + w.first);
   const unsigned grid = (unsigned)((int64_t)p.nchunk * p.nct);
   if (p.nchunk > 1) {
-    scan_variant(d->dtype, d->n, LaunchLocal{p, grid, s});
+    scan_lane_variant(p, d->dtype, LaunchLocal{p, grid, s});
     MTGNN_CHECK_LAUNCH("scan_local");
     k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 0);
     MTGNN_CHECK_LAUNCH("scan_carry");
   }
-  scan_variant(d->dtype, d->n, LaunchOut{p, grid, s});
+  scan_lane_variant(p, d->dtype, LaunchOut{p, grid, s});
   MTGNN_CHECK_LAUNCH("scan_out");
   return MTGNN_OK;
 }
@@ -911,7 +996,7 @@ mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
   o.bc = (float*)((char*)ws + w.bc);
   const unsigned grid = (unsigned)((int64_t)p.nchunk * p.nct);
   if (p.nchunk > 1) {
-    scan_variant(d->dtype, d->n, LaunchBackLocal{p, o, grid, s});
+    scan_lane_variant(p, d->dtype, LaunchBackLocal{p, o, grid, s});
     MTGNN_CHECK_LAUNCH("scan_back_local");
     k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 1);
     MTGNN_CHECK_LAUNCH("scan_carry");
