@@ -23,6 +23,7 @@
 // bytes per row and channel in bfloat16.
 #include <algorithm>
 
+#include "bf16_split.h"
 #include "ops.h"
 #include "seq.h"
 
@@ -156,6 +157,22 @@ __device__ __forceinline__ void stage_states(const void* src, int64_t ld, int n,
 }
 
 __device__ __forceinline__ float step_size(const ScanP& p, float u) { return p.softplus ? softplus_(u) : u; }
+// A tile's step sizes, and its gates, in place.  One branch for all of them, so that the rows after it are one run of
+// instructions in which B and C are requested ahead.
+__device__ __forceinline__ void step_sizes(const ScanP& p, float bias, float (&u)[TT]) {
+#pragma unroll
+  for (int i = 0; i < TT; ++i) u[i] += bias;
+  if (p.softplus) {
+#pragma unroll
+    for (int i = 0; i < TT; ++i) u[i] = softplus_(u[i]);
+  }
+}
+__device__ __forceinline__ void gates(const ScanP& p, float (&z)[TT]) {
+  if (p.z) {
+#pragma unroll
+    for (int i = 0; i < TT; ++i) z[i] = silu_(z[i]);
+  }
+}
 
 template <int SPL>
 __device__ __forceinline__ void lds_get(const float* p, float (&v)[SPL]) {
@@ -186,13 +203,15 @@ __device__ __forceinline__ int64_t opaque(int v) {
   return v;
 }
 
-// A lane's channel and its states.
+// A lane's channel and its N states (of more than 32, each of two waves has half).
 struct Lane {
-  int g, col0;
+  int g, col0, n0, wave;
   uint32_t col;     // of the lane, in its tile's first .. last channel
   bool mine;
-  __device__ __forceinline__ Lane(const ScanP& p, int tile) {
+  __device__ __forceinline__ Lane(const ScanP& p, int tile, int N) {
     const int lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    n0 = wave * N;
     g = tile / p.tpg;
     const int in = (tile % p.tpg) * CT;
     col0 = g * p.per + in;
@@ -206,18 +225,18 @@ struct Lane {
   template <int N>
   __device__ __forceinline__ void load(const ScanP& p, const float* tab, int64_t row, float (&h)[N]) const {
     const int64_t step = opaque(p.d);
-    const float* q = tab + row * p.n * step + col0;
+    const float* q = tab + (row * p.n + n0) * step + col0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) h[i] = i < p.n ? q[i * step + col] : 0.f;
+    for (int i = 0; i < N; ++i) h[i] = n0 + i < p.n ? q[i * step + col] : 0.f;
   }
   template <int N>
   __device__ __forceinline__ void store(const ScanP& p, float* tab, int64_t row, const float (&h)[N]) const {
     const int64_t step = opaque(p.d);
-    float* q = tab + row * p.n * step + col0;
+    float* q = tab + (row * p.n + n0) * step + col0;
     if (!mine) return;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (i < p.n) q[i * step + col] = h[i];
+      if (n0 + i < p.n) q[i * step + col] = h[i];
   }
   template <int N>
   __device__ __forceinline__ void decay(const ScanP& p, float (&A2)[N]) const {   // A log2 e
@@ -236,44 +255,70 @@ struct States {
   int64_t ld;
   int n;
   float* lds;
-  __device__ __forceinline__ States(const void* src, int64_t ld_, int n_, int g, float* lds_)
-      : m((const T*)src + g * n_), ld(ld_), n(n_), lds(lds_) {}
+  __device__ __forceinline__ States(const void* src, int64_t ld_, int n_, const Lane& me, float* lds_)
+      : m((const T*)src + me.g * n_ + me.n0), ld(ld_), n(n_ - me.n0), lds(lds_ + me.wave * WORDS) {}
   __device__ __forceinline__ void stage(int row, int last) const {
     if constexpr (!SC) {
-      for (int e = threadIdx.x; e < TT * N; e += 64) {
+      for (int e = threadIdx.x & 63; e < TT * N; e += 64) {
         const int i = e / N, s = e % N;
         const float v = Elem<T>::load(m, (int64_t)min(row + i, last) * ld + min(s, n - 1));
         lds[e] = s < n ? v : 0.f;
       }
     }
   }
-  template <int M>
-  __device__ __forceinline__ void get(int i, int row, int s0, float (&v)[M]) const {   // states s0 .. of the tile's row i
+  // Sixteen states at a time (more of B and C have no registers): their words as read, and their values.
+  static constexpr int M = N < 16 ? N : 16, PARTS = N / M;
+  struct Raw {
+    uint32_t w[SC ? M * sizeof(T) / 4 : 1];
+  };
+  __device__ __forceinline__ Raw fetch(int row, int part) const {
+    Raw r;
     if constexpr (SC) {
-      const auto q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)(m + row * ld + s0);
+      const auto q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)(m + row * ld + part * M);
+#pragma unroll
+      for (int k = 0; k < (int)(M * sizeof(T) / 4); ++k) r.w[k] = q[k];
+    }
+    return r;
+  }
+  __device__ __forceinline__ void values(const Raw& r, int i, int part, float (&v)[M]) const {   // row i of the tile
+    if constexpr (SC) {
 #pragma unroll
       for (int k = 0; k < M; ++k) {
-        if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(q[k]);
-        else v[k] = __uint_as_float(k % 2 ? q[k / 2] & 0xffff0000u : q[k / 2] << 16);
+        if constexpr (sizeof(T) == 4) v[k] = __uint_as_float(r.w[k]);
+        else v[k] = __uint_as_float(k % 2 ? r.w[k / 2] & 0xffff0000u : r.w[k / 2] << 16);
       }
     } else {
 #pragma unroll
       for (int k = 0; k < M; k += 4) {
-        const float4 f = *(const float4*)(lds + i * N + s0 + k);
+        const float4 f = *(const float4*)(lds + i * N + part * M + k);
         v[k] = f.x; v[k + 1] = f.y; v[k + 2] = f.z; v[k + 3] = f.w;
       }
     }
   }
 };
-// f(first state, number of states) over N states, sixteen at a time (more of B and C have no registers).
-template <int N, class F>
-__device__ __forceinline__ void by_sixteen(F f) {
-  constexpr int M = N < 16 ? N : 16;
+// f(row of the tile, part of the states, words of B (and C) for it), over all rows of a tile from FIRST in steps of
+// STEP (1 or -1), the next part's words requested before this one's work: the compiler would wait for each where it
+// is used, or bring all of a tile forward and run out of registers.
+template <int STEP, class S, class F>
+__device__ __forceinline__ void over_tile(const S& a, const S& b, bool two, int tb, F f) {
+  constexpr int FIRST = STEP > 0 ? 0 : TT - 1;
+  typename S::Raw ra = a.fetch(tb + FIRST, 0), rb = two ? b.fetch(tb + FIRST, 0) : ra;
 #pragma unroll
-  for (int s0 = 0; s0 < N; s0 += M) {
-    if (N > 16) __builtin_amdgcn_sched_barrier(0);
-    f(s0, std::integral_constant<int, M>{});
+  for (int q = 0; q < TT * S::PARTS; ++q) {
+    const int i = FIRST + STEP * (q / S::PARTS), part = q % S::PARTS;
+    const int qn = q + 1 < TT * S::PARTS ? q + 1 : q;
+    const int in = FIRST + STEP * (qn / S::PARTS), pn = qn % S::PARTS;
+    const typename S::Raw na = a.fetch(tb + in, pn), nb = two ? b.fetch(tb + in, pn) : na;
+    f(i, part, ra, rb);
+    __builtin_amdgcn_sched_barrier(0);
+    ra = na;
+    rb = nb;
   }
+}
+template <typename T>
+__device__ __forceinline__ void put(T* row, uint32_t col, float v) {
+  if constexpr (sizeof(T) == 2) row[col] = (uint16_t)cvt2_bf16(v, v);
+  else row[col] = v;
 }
 template <int N>
 __device__ __forceinline__ void zero(float (&h)[N]) {
@@ -281,12 +326,12 @@ __device__ __forceinline__ void zero(float (&h)[N]) {
   for (int i = 0; i < N; ++i) h[i] = 0.f;
 }
 
-template <typename T, int N, bool SC>
-__global__ __launch_bounds__(64) void k_scan_local(ScanP p) {
-  __shared__ __align__(16) float s_B[States<T, N, SC>::WORDS];
+template <typename T, int N, int NW, bool SC>
+__global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
+  __shared__ __align__(16) float s_B[NW * States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const Lane me(p, tile);
-  const States<T, N, SC> B(p.B, p.ldB, p.n, me.g, s_B);
+  const Lane me(p, tile, N);
+  const States<T, N, SC> B(p.B, p.ldB, p.n, me, s_B);
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
@@ -320,23 +365,36 @@ __global__ __launch_bounds__(64) void k_scan_local(ScanP p) {
     }
     B.stage(t, t1 - 1);
     if constexpr (!SC) __syncthreads();
+    step_sizes(p, bias, u);
+    using S = States<T, N, SC>;
+    const auto part = [&](int i, int k, const typename S::Raw& rb, const typename S::Raw&) {
+      const float dt = u[i], dx = dt * x[i];
+      if (k == 0) sum += dt;
+      float b[S::M];
+      B.values(rb, i, k, b);
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      if (t + i >= t1) break;
-      const float dt = step_size(p, u[i] + bias), dx = dt * x[i];
-      sum += dt;
-      by_sixteen<N>([&](int s0, auto m) {
-        constexpr int M = decltype(m)::value;
-        float b[M];
-        B.get(i, t + i, s0, b);
+      for (int s = 0; s < S::M; ++s) {
+        float& hs = h[k * S::M + s];
+        hs = fmaf(__builtin_amdgcn_exp2f(dt * A2[k * S::M + s]), hs, dx * b[s]);
+      }
+    };
+    if (t + TT <= t1) {
+      over_tile<1>(B, B, false, t, part);
+    } else {
 #pragma unroll
-        for (int s = 0; s < M; ++s) h[s0 + s] = fmaf(__builtin_amdgcn_exp2f(dt * A2[s0 + s]), h[s0 + s], dx * b[s]);
-      });
+      for (int i = 0; i < TT; ++i) {
+        if (t + i >= t1) break;
+#pragma unroll
+        for (int k = 0; k < S::PARTS; ++k) {
+          const typename S::Raw rb = B.fetch(t + i, k);
+          part(i, k, rb, rb);
+        }
+      }
     }
     if constexpr (!SC) __syncthreads();
   }
   me.store(p, p.E, c, h);
-  if (me.mine) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
+  if (me.mine && me.wave == 0) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
@@ -394,12 +452,13 @@ __global__ __launch_bounds__(RUNS * RUN_COLS) void k_scan_carry(ScanP p, int bac
   walk(h, d, true);
 }
 
-template <typename T, int N, bool SC>
-__global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
-  __shared__ __align__(16) float s_B[States<T, N, SC>::WORDS], s_C[States<T, N, SC>::WORDS];
+template <typename T, int N, int NW, bool SC>
+__global__ __launch_bounds__(64 * NW) void k_scan_out(ScanP p) {
+  __shared__ __align__(16) float s_B[NW * States<T, N, SC>::WORDS], s_C[NW * States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const Lane me(p, tile);
-  const States<T, N, SC> B(p.B, p.ldB, p.n, me.g, s_B), C(p.C, p.ldC, p.n, me.g, s_C);
+  const Lane me(p, tile, N);
+  const States<T, N, SC> B(p.B, p.ldB, p.n, me, s_B), C(p.C, p.ldC, p.n, me, s_C);
+  __shared__ float s_y[NW > 1 ? NW : 1][NW > 1 ? TT : 1][64];
   if (p.carried && blockIdx.x == 0 && threadIdx.x == 0) *p.carried = p.st_in != nullptr;
   const SeqRange r = seq_range(p.q);
   int t0, t1;
@@ -418,28 +477,36 @@ __global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
       const int row = min(max(tb + i, t0), t1 - 1);
       u[i] = me.at<T>(p.delta, p.ldd, row);
       x[i] = me.at<T>(p.x, p.ldx, row);
-      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 0.f;
+      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 1.f;
     }
+    if constexpr (NW > 1) __syncthreads();   // the last tile's s_y is read, and every wave has its rows: y may be one of them
     B.stage(tb, t1 - 1);
     C.stage(tb, t1 - 1);
     if constexpr (!SC) __syncthreads();
-    const auto row = [&](int i) {
-      const float dt = step_size(p, u[i] + bias), dx = dt * x[i];
-      float y[2] = {D * x[i], 0.f};
-      by_sixteen<N>([&](int s0, auto m) {
-        constexpr int M = decltype(m)::value;
-        float b[M], cc[M];
-        B.get(i, tb + i, s0, b);
-        C.get(i, tb + i, s0, cc);
+    step_sizes(p, bias, u);
+    gates(p, z);
+    using S = States<T, N, SC>;
+    float y[2];
+    const auto part = [&](int i, int k, const typename S::Raw& rb, const typename S::Raw& rc) {   // z[i] becomes y
+      const float dt = u[i], dx = dt * x[i];
+      if (k == 0) {
+        y[0] = NW > 1 && me.wave ? 0.f : D * x[i];
+        y[1] = 0.f;
+      }
+      float b[S::M], cc[S::M];
+      B.values(rb, i, k, b);
+      C.values(rc, i, k, cc);
 #pragma unroll
-        for (int s = 0; s < M; ++s) {
-          h[s0 + s] = fmaf(__builtin_amdgcn_exp2f(dt * A2[s0 + s]), h[s0 + s], dx * b[s]);
-          y[s & 1] = fmaf(h[s0 + s], cc[s], y[s & 1]);
-        }
-      });
-      float v = y[0] + y[1];
-      if (p.z) v *= silu_(z[i]);
-      if (me.mine) Elem<T>::store((T*)p.y + (int64_t)(tb + i) * p.ldy + me.col0, me.col, v);
+      for (int s = 0; s < S::M; ++s) {
+        float& hs = h[k * S::M + s];
+        hs = fmaf(__builtin_amdgcn_exp2f(dt * A2[k * S::M + s]), hs, dx * b[s]);
+        y[s & 1] = fmaf(hs, cc[s], y[s & 1]);
+      }
+      if (k == S::PARTS - 1) {
+        if constexpr (NW > 1) s_y[me.wave][i][threadIdx.x & 63] = y[0] + y[1];
+        else z[i] *= y[0] + y[1];
+        keep_live(z[i]);   // made here, not where it is stored: the states of all rows would have to wait for it
+      }
     };
     const auto leave = [&] {   // after a sequence's last row
       if (p.st_out) {
@@ -450,8 +517,7 @@ __global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
     };
     if (tb >= t0 && tb > at.beg && tb + TT <= at.end && tb + TT <= t1) {   // all of one sequence
       if (p.hs) me.store(p, p.hs, tb / TT, h);
-#pragma unroll
-      for (int i = 0; i < TT; ++i) row(i);
+      over_tile<1>(B, C, true, tb, part);
       if (tb + TT == at.end) leave();
     } else {
 #pragma unroll
@@ -467,9 +533,20 @@ __global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
         } else if (i == 0 && p.hs) {
           me.store(p, p.hs, tb / TT, h);
         }
-        row(i);
+#pragma unroll
+        for (int k = 0; k < S::PARTS; ++k) part(i, k, B.fetch(t, k), C.fetch(t, k));
         if (t + 1 == at.end) leave();
       }
+    }
+    if constexpr (NW > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TT; ++i) z[i] *= s_y[0][i][threadIdx.x & 63] + s_y[1][i][threadIdx.x & 63];
+    }
+    if (me.mine) {
+#pragma unroll
+      for (int i = 0; i < TT; ++i)
+        if (i % NW == me.wave && tb + i >= t0 && tb + i < t1) put<T>((T*)p.y + (int64_t)(tb + i) * p.ldy + me.col0, me.col, z[i]);
     }
     if constexpr (!SC) __syncthreads();
   }
@@ -482,12 +559,12 @@ __global__ __launch_bounds__(64) void k_scan_out(ScanP p) {
 // k_scan_back then goes over a chunk's tiles from the last to the first: each tile's states forwards from the
 // forward's checkpoint, kept in registers (eight rows of them, why a checkpoint is every eight), then g backwards.
 
-template <typename T, int N, bool SC>
-__global__ __launch_bounds__(64) void k_scan_back_local(ScanP p, ScanG o) {
-  __shared__ __align__(16) float s_C[States<T, N, SC>::WORDS];
+template <typename T, int N, int NW, bool SC>
+__global__ __launch_bounds__(64 * NW) void k_scan_back_local(ScanP p, ScanG o) {
+  __shared__ __align__(16) float s_C[NW * States<T, N, SC>::WORDS];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const Lane me(p, tile);
-  const States<T, N, SC> C(p.C, p.ldC, p.n, me.g, s_C);
+  const Lane me(p, tile, N);
+  const States<T, N, SC> C(p.C, p.ldC, p.n, me, s_C);
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
@@ -511,29 +588,42 @@ __global__ __launch_bounds__(64) void k_scan_back_local(ScanP p, ScanG o) {
     for (int i = 0; i < TT; ++i) {
       const int row = min(tb + i, stop - 1);
       u[i] = me.at<T>(p.delta, p.ldd, row);
-      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 0.f;
+      z[i] = p.z ? me.at<T>(p.z, p.ldz, row) : 1.f;
       e[i] = me.at<float>(o.dy, o.lddy, row);
     }
     C.stage(tb, stop - 1);
     if constexpr (!SC) __syncthreads();
+    step_sizes(p, bias, u);
+    gates(p, z);
+    using S = States<T, N, SC>;
+    const auto part = [&](int i, int k, const typename S::Raw& rc, const typename S::Raw&) {
+      const float dt = u[i], ee = e[i] * z[i];
+      if (k == 0) sum += dt;
+      float cc[S::M];
+      C.values(rc, i, k, cc);
 #pragma unroll
-    for (int i = TT - 1; i >= 0; --i) {
-      if (tb + i >= stop) continue;
-      const float dt = step_size(p, u[i] + bias), ee = p.z ? e[i] * silu_(z[i]) : e[i];
-      sum += dt;
-      by_sixteen<N>([&](int s0, auto m) {
-        constexpr int M = decltype(m)::value;
-        float cc[M];
-        C.get(i, tb + i, s0, cc);
+      for (int s = 0; s < S::M; ++s) {
+        float& gs = g[k * S::M + s];
+        gs = __builtin_amdgcn_exp2f(dt * A2[k * S::M + s]) * fmaf(ee, cc[s], gs);
+      }
+    };
+    if (tb + TT <= stop) {
+      over_tile<-1>(C, C, false, tb, part);
+    } else {
 #pragma unroll
-        for (int s = 0; s < M; ++s)
-          g[s0 + s] = __builtin_amdgcn_exp2f(dt * A2[s0 + s]) * fmaf(ee, cc[s], g[s0 + s]);
-      });
+      for (int i = TT - 1; i >= 0; --i) {
+        if (tb + i >= stop) continue;
+#pragma unroll
+        for (int k = 0; k < S::PARTS; ++k) {
+          const typename S::Raw rc = C.fetch(tb + i, k);
+          part(i, k, rc, rc);
+        }
+      }
     }
     if constexpr (!SC) __syncthreads();
   }
   me.store(p, p.E, c, g);
-  if (me.mine) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
+  if (me.mine && me.wave == 0) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
 }
 
 template <typename T, int SPL, int NB>
@@ -882,18 +972,18 @@ void scan_variant(int dtype, int n, F f) {
 // The lane-per-channel kernels: n rounded up, and whether B's and C's rows are whole words (n of a supported number).
 template <typename F>
 void scan_lane_variant(const ScanP& p, int dtype, F f) {
-  const int N = p.n <= 4 ? 4 : p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+  const int N = p.n <= 4 ? 4 : p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;   // 64: two waves of 32
   const bool words = p.n == N && (dtype == MTGNN_F32 || (p.ldB % 2 == 0 && p.ldC % 2 == 0 && (uintptr_t)p.B % 4 == 0 &&
                                                          (uintptr_t)p.C % 4 == 0));
   const auto by = [&](auto t) {
     using T = decltype(t);
     const auto with = [&](auto sc) {
       constexpr bool SC = decltype(sc)::value;
-      if (N == 4) f.template operator()<T, 4, SC>();
-      else if (N == 8) f.template operator()<T, 8, SC>();
-      else if (N == 16) f.template operator()<T, 16, SC>();
-      else if (N == 32) f.template operator()<T, 32, SC>();
-      else f.template operator()<T, 64, SC>();
+      if (N == 4) f.template operator()<T, 4, 1, SC>();
+      else if (N == 8) f.template operator()<T, 8, 1, SC>();
+      else if (N == 16) f.template operator()<T, 16, 1, SC>();
+      else if (N == 32) f.template operator()<T, 32, 1, SC>();
+      else f.template operator()<T, 32, 2, SC>();
     };
     if (words) with(std::true_type{});
     else with(std::false_type{});
@@ -906,20 +996,22 @@ struct LaunchLocal {
   const ScanP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int N, bool SC> void operator()() const { k_scan_local<T, N, SC><<<grid, 64, 0, s>>>(p); }
+  template <typename T, int N, int NW, bool SC> void operator()() const { k_scan_local<T, N, NW, SC><<<grid, 64 * NW, 0, s>>>(p); }
 };
 struct LaunchOut {
   const ScanP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int N, bool SC> void operator()() const { k_scan_out<T, N, SC><<<grid, 64, 0, s>>>(p); }
+  template <typename T, int N, int NW, bool SC> void operator()() const { k_scan_out<T, N, NW, SC><<<grid, 64 * NW, 0, s>>>(p); }
 };
 struct LaunchBackLocal {
   const ScanP& p;
   const ScanG& g;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int N, bool SC> void operator()() const { k_scan_back_local<T, N, SC><<<grid, 64, 0, s>>>(p, g); }
+  template <typename T, int N, int NW, bool SC> void operator()() const {
+    k_scan_back_local<T, N, NW, SC><<<grid, 64 * NW, 0, s>>>(p, g);
+  }
 };
 struct LaunchBack {
   const ScanP& p;
