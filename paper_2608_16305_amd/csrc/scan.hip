@@ -101,6 +101,13 @@ __device__ __forceinline__ void store4(float* p, int left, bool vec, float a, fl
   if (left > 3) p[3] = d;
 }
 
+// The value, but not one that is known outside: the addresses that are made from it are made where they are used,
+// where otherwise a loop's 2 N of them would be kept in scalar registers that B and C need.
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
 // Where a thread stands.
 template <int SPL, int NB>
 struct Place {
@@ -108,7 +115,7 @@ struct Place {
   int lane, wid, cb, n0, g, ch0, left;   // cb: first of its channels in the block; left: channels of the group from ch0
   __device__ __forceinline__ Place(const ScanP& p, int tile) {
     lane = threadIdx.x & 63;
-    wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wid = NB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     cb = lane & ~3;
     n0 = wid * 4 * SPL + (lane & 3) * SPL;
     g = tile / p.tpg;
@@ -116,21 +123,25 @@ struct Place {
     ch0 = g * p.per + in;
     left = min(CT, p.per - in);
   }
-  // h of state table row `row` (of n x d floats)
+  // h of state table row `row` (of n x d floats, fewer than 2^26)
   __device__ __forceinline__ void load(const ScanP& p, const float* tab, int64_t row, float (&h)[4][SPL]) const {
+    const int d = opaque(p.d);
+    const float* q = tab + row * p.n * d + ch0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
       float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (n0 + s < p.n) load4(tab + (row * p.n + n0 + s) * p.d + ch0 + cb, left - cb, p.vec, v);
+      if (n0 + s < p.n) load4(q + (uint32_t)((n0 + s) * d + cb), left - cb, p.vec, v);
 #pragma unroll
       for (int c = 0; c < 4; ++c) h[c][s] = v[c];
     }
   }
   __device__ __forceinline__ void store(const ScanP& p, float* tab, int64_t row, const float (&h)[4][SPL]) const {
+    const int d = opaque(p.d);
+    float* q = tab + row * p.n * d + ch0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s)
       if (n0 + s < p.n)
-        store4(tab + (row * p.n + n0 + s) * p.d + ch0 + cb, left - cb, p.vec, h[0][s], h[1][s], h[2][s], h[3][s]);
+        store4(q + (uint32_t)((n0 + s) * d + cb), left - cb, p.vec, h[0][s], h[1][s], h[2][s], h[3][s]);
   }
   __device__ __forceinline__ void decay(const ScanP& p, float (&A2)[4][SPL]) const {   // A log2 e
     load(p, p.A, 0, A2);
@@ -187,6 +198,13 @@ __device__ __forceinline__ void lds_get(const float* p, float (&v)[SPL]) {
   }
 }
 
+template <int SPL>
+__device__ __forceinline__ void lds_put(float* p, const float (&v)[SPL]) {
+  if constexpr (SPL == 4) *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
+  else if constexpr (SPL == 2) *(float2*)p = make_float2(v[0], v[1]);
+  else p[0] = v[0];
+}
+
 // Which rows of chunk c exist.
 __device__ __forceinline__ void chunk_rows(const ScanP& p, const SeqRange& r, int c, int& t0, int& t1) {
   const int64_t a = (int64_t)c * p.ch;
@@ -195,13 +213,6 @@ __device__ __forceinline__ void chunk_rows(const ScanP& p, const SeqRange& r, in
 }
 
 // ------------------------------------------------------------------ forward
-
-// The value, but not one that is known outside: the addresses that are made from it are made where they are used,
-// where otherwise a loop's 2 N of them would be kept in scalar registers that B and C need.
-__device__ __forceinline__ int64_t opaque(int v) {
-  asm volatile("" : "+s"(v));
-  return v;
-}
 
 // A lane's channel and its N states (of more than 32, each of two waves has half).
 struct Lane {
@@ -398,11 +409,12 @@ __global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
-// first.  A block has 16 states and channels; each of 64 threads to one takes a run of chunks, once for
+// first.  A block has 1024 / RUNS states and channels; each of RUNS threads to one takes a run of chunks, once for
 // what the run hands on, h -> own + decay h, and, after a scan over the runs, once with what enters it.  (One
-// thread over all chunks waited for memory 127 times in turn at 1,013 chunks: 144 us, against ten.)
-constexpr int RUNS = 64, RUN_COLS = 16;
-__global__ __launch_bounds__(RUNS * RUN_COLS) void k_scan_carry(ScanP p, int back) {
+// thread over all chunks waited for memory 127 times in turn at 1,013 chunks: 144 us, against 16.)
+template <int RUNS>
+__global__ __launch_bounds__(1024) void k_scan_carry(ScanP p, int back) {
+  constexpr int RUN_COLS = 1024 / RUNS;
   __shared__ float s_h[RUNS][RUN_COLS + 1], s_d[RUNS][RUN_COLS + 1];   // a decay of -1: nothing passes
   const int64_t nd = (int64_t)p.n * p.d;
   const int j = threadIdx.x % RUN_COLS, run = threadIdx.x / RUN_COLS;
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(64 * NW) void k_scan_out(ScanP p) {
 // With e = dy silu(z): g_t = C_t e_t + a_(t+1) g_(t+1), the gradient of h_t; what a chunk hands to the one before
 // it is r = a_t g_t at its first row, again a linear recurrence (k_scan_back_local, k_scan_carry).
 // k_scan_back then goes over a chunk's tiles from the last to the first: each tile's states forwards from the
-// forward's checkpoint, kept in registers (eight rows of them, why a checkpoint is every eight), then g backwards.
+// forward's checkpoint, kept in registers half a tile at a time, then g backwards.
 
 template <typename T, int N, int NW, bool SC>
 __global__ __launch_bounds__(64 * NW) void k_scan_back_local(ScanP p, ScanG o) {
@@ -627,16 +639,16 @@ __global__ __launch_bounds__(64 * NW) void k_scan_back_local(ScanP p, ScanG o) {
 }
 
 template <typename T, int SPL, int NB>
-__global__ __launch_bounds__(64 * NB, 1) void k_scan_back(ScanP p, ScanG o) {
+__global__ __launch_bounds__(64 * NB, 2) void k_scan_back(ScanP p, ScanG o) {
   using P = Place<SPL, NB>;
-  constexpr int NP = P::NP;
+  constexpr int NP = P::NP, HT = TT / 2;
   __shared__ __align__(16) float s_dt[TT][CT], s_dx[TT][CT], s_e[TT][CT];
   __shared__ float s_x[TT][CT], s_s[TT][CT], s_z[TT][CT];     // x, d dt / d delta, dy silu'(z)
   __shared__ __align__(16) float s_B[TT * NP], s_C[TT * NP];
   __shared__ __align__(16) float s_bc[TT][4][2][NP];          // dB, dC of a tile, from each 16 lanes
   __shared__ float s_red[NB > 1 ? NB : 1][3][NB > 1 ? TT : 1][CT];
   const int c = blockIdx.x / p.nct, tile = blockIdx.x % p.nct;
-  const P me(p, tile);
+  P me(p, tile);
   const SeqRange r = seq_range(p.q);
   int t0, t1;
   chunk_rows(p, r, c, t0, t1);
@@ -649,140 +661,190 @@ __global__ __launch_bounds__(64 * NB, 1) void k_scan_back(ScanP p, ScanG o) {
   zero_state(&dA[0][0], 4 * SPL);
   if (p.nchunk > 1 && at.end > t1) me.load(p, p.E, c, f);
   const bool mine = me.lane < me.left;
-  const int col = me.ch0 + (mine ? me.lane : 0);
-  const float bias = p.bias ? p.bias[col] : 0.f, D = p.D ? p.D[col] : 0.f;
+  uint32_t col = mine ? me.lane : 0;
+  const float bias = p.bias ? p.bias[me.ch0 + col] : 0.f, D = p.D ? p.D[me.ch0 + col] : 0.f;
   float dD = 0.f, db = 0.f;
   for (int tb = (t1 - 1) / TT * TT; tb + TT > t0; tb -= TT) {
     const int tlo = max(tb, t0), thi = min(tb + TT, t1);
+    // addresses are formed in the tile, not kept over all of them (opaque)
+    asm volatile("" : "+v"(me.lane), "+v"(col));
+    me.cb = me.lane & ~3;
+    me.n0 = me.wid * 4 * SPL + (me.lane & 3) * SPL;
+    float* my_bc = &s_bc[0][me.lane >> 4][me.lane >> 2 & 1][me.n0];   // (two lanes write each value, the same)
+    const bool is_C = me.lane & 4;
+    {
+      constexpr int U = (TT + NB - 1) / NB;
+      float u[U], x[U], z[U], dy[U];
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      if (i % NB != me.wid) continue;
-      const int64_t row = min(max(tb + i, t0), t1 - 1);
-      const float u = Elem<T>::load((const T*)p.delta, row * p.ldd + col) + bias;
-      const float x = Elem<T>::load((const T*)p.x, row * p.ldx + col);
-      const float dy = o.dy[row * o.lddy + col];
-      float e = dy;
-      if (p.z) {
-        const float z = Elem<T>::load((const T*)p.z, row * p.ldz + col);
-        const float sg = sigmoid_hw(z);
-        e = dy * (z * sg);
-        s_z[i][me.lane] = dy * (sg * fmaf(z, 1.f - sg, 1.f));
+      for (int k = 0; k < U; ++k) {
+        const int64_t row = min(max(tb + k * NB + me.wid, t0), t1 - 1);
+        u[k] = Elem<T>::load((const T*)p.delta + row * p.ldd + me.ch0, col) + bias;
+        x[k] = Elem<T>::load((const T*)p.x + row * p.ldx + me.ch0, col);
+        z[k] = p.z ? Elem<T>::load((const T*)p.z + row * p.ldz + me.ch0, col) : 0.f;
+        dy[k] = (o.dy + row * o.lddy + me.ch0)[col];
       }
-      s_x[i][me.lane] = x;
-      s_s[i][me.lane] = p.softplus ? sigmoid_hw(u) : 1.f;
-      const float dt = mine ? step_size(p, u) : 0.f;
-      s_dt[i][me.lane] = dt;
-      s_dx[i][me.lane] = mine ? dt * x : 0.f;
-      s_e[i][me.lane] = mine ? e : 0.f;
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int i = k * NB + me.wid;
+        if (NB > 1 && i >= TT) break;
+        float e = dy[k];
+        if (p.z) {
+          const float sg = sigmoid_hw(z[k]);
+          e = dy[k] * (z[k] * sg);
+          s_z[i][me.lane] = dy[k] * (sg * fmaf(z[k], 1.f - sg, 1.f));
+        }
+        const float dt = mine ? step_size(p, u[k]) : 0.f;
+        s_x[i][me.lane] = x[k];
+        s_s[i][me.lane] = p.softplus ? sigmoid_hw(u[k]) : 1.f;
+        s_dt[i][me.lane] = dt;
+        s_dx[i][me.lane] = mine ? dt * x[k] : 0.f;
+        s_e[i][me.lane] = mine ? e : 0.f;
+      }
     }
     stage_states<T, NP, 64 * NB>(p.B, p.ldB, p.n, me.g * p.n, tb, t1 - 1, s_B);
     stage_states<T, NP, 64 * NB>(p.C, p.ldC, p.n, me.g * p.n, tb, t1 - 1, s_C);
     __syncthreads();
-    // the states that enter each row of the tile
-    float hb[TT][4][SPL];
     while (at.beg > tlo) at.prev();
-    {
-      float h[4][SPL];
-      zero_state(&h[0][0], 4 * SPL);
-      if (at.beg < tlo) me.load(p, p.hs, tb / TT, h);
-#pragma unroll
-      for (int i = 0; i < TT; ++i) {
-        const int t = tb + i;
-        if (t >= tlo && t < thi) {
-          if (t == at.end) at.next();
-          if (t == at.beg) {
-            if (init && at.row() >= 0) me.load(p, init, at.s, h);
-            else zero_state(&h[0][0], 4 * SPL);
-          }
-        }
-        float dt[4], dx[4], b[SPL];
-        lds_get<4>(&s_dt[i][me.cb], dt);
-        lds_get<4>(&s_dx[i][me.cb], dx);
-        lds_get<SPL>(&s_B[i * NP + me.n0], b);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int s = 0; s < SPL; ++s) {
-            hb[i][k][s] = h[k][s];
-            h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
-          }
-      }
-    }
-    // the decays and inputs are formed again below: kept from above they would be hundreds of registers
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int s = 0; s < SPL; ++s) keep_live(A2[k][s]);
     // what a row's channel gets (lane l: channel l) once its sums over the states are complete
     const auto finish = [&](int i, float y, float sx, float su) {
       const int64_t t = tb + i;
       const float x = s_x[i][me.lane], e = s_e[i][me.lane];
       const float du = fmaf(sx, x, su * LN2) * s_s[i][me.lane];
       if (mine) {
-        o.dx[t * o.lddx + col] = fmaf(D, e, sx * s_dt[i][me.lane]);
-        o.ddelta[t * o.lddd + col] = du;
-        if (p.z) o.dz[t * o.lddz + col] = s_z[i][me.lane] * fmaf(D, x, y);
+        (o.dx + t * o.lddx + me.ch0)[col] = fmaf(D, e, sx * s_dt[i][me.lane]);
+        (o.ddelta + t * o.lddd + me.ch0)[col] = du;
+        if (p.z) (o.dz + t * o.lddz + me.ch0)[col] = s_z[i][me.lane] * fmaf(D, x, y);
       }
       dD = fmaf(e, x, dD);
       db += du;
     };
+    // Half a tile: the states that enter its rows (hb), forwards from the checkpoint, then its rows backwards.  Eight
+    // rows' states would be 128 registers and leave one wave a SIMD; so the first half's rows are gone over twice.
+    const auto half = [&](auto first_row, auto one_sequence) {
+      constexpr int I0 = decltype(first_row)::value;
+      constexpr bool ONE = decltype(one_sequence)::value;
+      float hb[HT][4][SPL];
+      {
+        float h[4][SPL];
+        zero_state(&h[0][0], 4 * SPL);
+        if (ONE || at.beg < tlo) me.load(p, p.hs, tb / TT, h);
 #pragma unroll
-    for (int i = TT - 1; i >= 0; --i) {
-      const int t = tb + i;
-      if (t < tlo || t >= thi) continue;
-      while (at.beg > t) at.prev();
-      if (t + 1 == at.end) zero_state(&f[0][0], 4 * SPL);
-      float dt[4], dx[4], e[4], b[SPL], cc[SPL], y4[4], x4[4], u4[4], vB[SPL], vC[SPL];
-      lds_get<4>(&s_dt[i][me.cb], dt);
-      lds_get<4>(&s_dx[i][me.cb], dx);
-      lds_get<4>(&s_e[i][me.cb], e);
-      lds_get<SPL>(&s_B[i * NP + me.n0], b);
-      lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+        for (int i = 0; i < I0 + HT; ++i) {
+          const int t = tb + i;
+          if (!ONE && t >= tlo && t < thi) {
+            if (t == at.end) at.next();
+            if (t == at.beg) {
+              if (init && at.row() >= 0) me.load(p, init, at.s, h);
+              else zero_state(&h[0][0], 4 * SPL);
+            }
+          }
+          if (i >= I0) {
 #pragma unroll
-      for (int s = 0; s < SPL; ++s) vB[s] = vC[s] = 0.f;
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        y4[k] = x4[k] = u4[k] = 0.f;
+              for (int s = 0; s < SPL; ++s) hb[i - I0 < 0 ? 0 : i - I0][k][s] = h[k][s];
+          }
+          if (i + 1 < I0 + HT) {
+            float dt[4], dx[4], b[SPL];
+            lds_get<4>(&s_dt[i][me.cb], dt);
+            lds_get<4>(&s_dx[i][me.cb], dx);
+            lds_get<SPL>(&s_B[i * NP + me.n0], b);
 #pragma unroll
-        for (int s = 0; s < SPL; ++s) {
-          const float a = __builtin_amdgcn_exp2f(dt[k] * A2[k][s]);
-          const float h = fmaf(a, hb[i][k][s], dx[k] * b[s]);
-          const float g = fmaf(e[k], cc[s], f[k][s]);
-          f[k][s] = a * g;
-          const float w = f[k][s] * hb[i][k][s];
-          y4[k] = fmaf(h, cc[s], y4[k]);
-          x4[k] = fmaf(g, b[s], x4[k]);
-          u4[k] = fmaf(w, A2[k][s], u4[k]);
-          dA[k][s] = fmaf(w, dt[k], dA[k][s]);
-          vB[s] = fmaf(g, dx[k], vB[s]);
-          vC[s] = fmaf(h, e[k], vC[s]);
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int s = 0; s < SPL; ++s)
+                h[k][s] = fmaf(__builtin_amdgcn_exp2f(dt[k] * A2[k][s]), h[k][s], dx[k] * b[s]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
       }
-      const float y = quad_sums(y4), sx = quad_sums(x4), su = quad_sums(u4);
-      if constexpr (NB > 1) {
-        s_red[me.wid][0][i][me.lane] = y;
-        s_red[me.wid][1][i][me.lane] = sx;
-        s_red[me.wid][2][i][me.lane] = su;
-      } else {
-        finish(i, y, sx, su);
-      }
+      // the decays and inputs are formed again below: kept from above they would be hundreds of registers
+      asm volatile("" ::: "memory");
+      float yv[HT], gx[HT], gu[HT];
 #pragma unroll
-      for (int s = 0; s < SPL; ++s) {
-        vB[s] += dpp<ROW_ROR4>(vB[s]);
-        vC[s] += dpp<ROW_ROR4>(vC[s]);
-        vB[s] += dpp<ROW_ROR8>(vB[s]);
-        vC[s] += dpp<ROW_ROR8>(vC[s]);
-      }
-      if ((me.lane & 12) == 0) {
+      for (int j = HT - 1; j >= 0; --j) {
+        const int i = I0 + j, t = tb + i;
+        yv[j] = gx[j] = gu[j] = 0.f;
+        if (!ONE) {
+          if (t < tlo || t >= thi) continue;
+          while (at.beg > t) at.prev();
+          if (t + 1 == at.end) zero_state(&f[0][0], 4 * SPL);
+        }
+        float dt[4], dx[4], e[4], b[SPL], cc[SPL], y4[4], x4[4], u4[4], vB[SPL], vC[SPL];
+        lds_get<4>(&s_dt[i][me.cb], dt);
+        lds_get<4>(&s_dx[i][me.cb], dx);
+        lds_get<4>(&s_e[i][me.cb], e);
+        lds_get<SPL>(&s_B[i * NP + me.n0], b);
+        lds_get<SPL>(&s_C[i * NP + me.n0], cc);
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) vB[s] = vC[s] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          y4[k] = x4[k] = u4[k] = 0.f;
+#pragma unroll
+          for (int s = 0; s < SPL; ++s) {
+            const float a = __builtin_amdgcn_exp2f(dt[k] * A2[k][s]);
+            const float h = ONE && j + 1 < HT ? hb[j + 1 < HT ? j + 1 : j][k][s] : fmaf(a, hb[j][k][s], dx[k] * b[s]);
+            const float g = fmaf(e[k], cc[s], f[k][s]);
+            f[k][s] = a * g;
+            const float w = f[k][s] * hb[j][k][s];
+            y4[k] = fmaf(h, cc[s], y4[k]);
+            x4[k] = fmaf(g, b[s], x4[k]);
+            u4[k] = fmaf(w, A2[k][s], u4[k]);
+            dA[k][s] = fmaf(w, dt[k], dA[k][s]);
+            vB[s] = fmaf(g, dx[k], vB[s]);
+            vC[s] = fmaf(h, e[k], vC[s]);
+          }
+        }
+        yv[j] = quad_sums(y4);
+        gx[j] = quad_sums(x4);
+        gu[j] = quad_sums(u4);
+        if constexpr (NB > 1) {
+          s_red[me.wid][0][i][me.lane] = yv[j];
+          s_red[me.wid][1][i][me.lane] = gx[j];
+          s_red[me.wid][2][i][me.lane] = gu[j];
+        } else {
+          keep_live(yv[j]);
+          keep_live(gx[j]);
+          keep_live(gu[j]);
+        }
+        float v[SPL];
 #pragma unroll
         for (int s = 0; s < SPL; ++s) {
-          s_bc[i][me.lane >> 4][0][me.n0 + s] = vB[s];
-          s_bc[i][me.lane >> 4][1][me.n0 + s] = vC[s];
+          vB[s] += dpp<ROW_ROR4>(vB[s]);
+          vC[s] += dpp<ROW_ROR4>(vC[s]);
+          vB[s] += dpp<ROW_ROR8>(vB[s]);
+          vC[s] += dpp<ROW_ROR8>(vC[s]);
+          v[s] = is_C ? vC[s] : vB[s];
         }
+        lds_put<SPL>(my_bc + i * 8 * NP, v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)   // added now, not at the end of the rows with all their terms kept
+#pragma unroll
+          for (int s = 0; s < SPL; ++s) keep_live(dA[k][s]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (NB == 1) {
+#pragma unroll
+        for (int j = HT - 1; j >= 0; --j)
+          if (ONE || (tb + I0 + j >= tlo && tb + I0 + j < thi)) finish(I0 + j, yv[j], gx[j], gu[j]);
+      }
+    };
+    const auto both = [&](auto one) {
+      half(std::integral_constant<int, HT>{}, one);
+      if (!decltype(one)::value) {
+        while (at.beg > tlo) at.prev();
+      }
+      half(std::integral_constant<int, 0>{}, one);
+    };
+    if (at.beg < tb && tlo == tb && thi == tb + TT && tb + TT <= at.end) {   // all of one sequence
+      if (tb + TT == at.end) zero_state(&f[0][0], 4 * SPL);
+      both(std::true_type{});
+    } else {
+      both(std::false_type{});
     }
     __syncthreads();
+#pragma unroll 1
     for (int e = threadIdx.x; e < TT * 2 * NP; e += 64 * NB) {
       const int i = e / (2 * NP), w = e / NP & 1, s = e % NP, t = tb + i;
       if (t < tlo || t >= thi || s >= p.n) continue;
@@ -817,8 +879,8 @@ __global__ __launch_bounds__(64 * NB, 1) void k_scan_back(ScanP p, ScanG o) {
     }
   }
   if (me.wid == 0 && mine) {
-    part[(int64_t)p.n * p.d + col] = dD;
-    part[(int64_t)(p.n + 1) * p.d + col] = db;
+    (part + (int64_t)p.n * p.d + me.ch0)[col] = dD;
+    (part + (int64_t)(p.n + 1) * p.d + me.ch0)[col] = db;
   }
 }
 
@@ -1037,6 +1099,14 @@ static void scan_save_at(ScanP& p, const mtgnn_scan_dims* d, int64_t rows, void*
   p.init = (float*)(b + 256 + al(cdiv(std::max<int64_t>(rows, 1), TT) * ((size_t)d->n * d->d * 4)));
 }
 
+static mtgnn_status scan_carry(const ScanP& p, int back, hipStream_t s) {
+  const int64_t nd = (int64_t)p.n * p.d;
+  if (p.nchunk > 256) k_scan_carry<64><<<(unsigned)cdiv(nd, 16), 1024, 0, s>>>(p, back);
+  else k_scan_carry<16><<<(unsigned)cdiv(nd, 64), 1024, 0, s>>>(p, back);
+  MTGNN_CHECK_LAUNCH("scan_carry");
+  return MTGNN_OK;
+}
+
 mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d,
                        const float* state_in, float* state_out, void* y, int64_t ldy, void* save, void* ws,
                        hipStream_t s) {
@@ -1059,8 +1129,7 @@ mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const m
   if (p.nchunk > 1) {
     scan_lane_variant(p, d->dtype, LaunchLocal{p, grid, s});
     MTGNN_CHECK_LAUNCH("scan_local");
-    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 0);
-    MTGNN_CHECK_LAUNCH("scan_carry");
+    MTGNN_TRY(scan_carry(p, 0, s));
   }
   scan_lane_variant(p, d->dtype, LaunchOut{p, grid, s});
   MTGNN_CHECK_LAUNCH("scan_out");
@@ -1090,8 +1159,7 @@ mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
   if (p.nchunk > 1) {
     scan_lane_variant(p, d->dtype, LaunchBackLocal{p, o, grid, s});
     MTGNN_CHECK_LAUNCH("scan_back_local");
-    k_scan_carry<<<(unsigned)cdiv((int64_t)d->n * d->d, RUN_COLS), RUNS * RUN_COLS, 0, s>>>(p, 1);
-    MTGNN_CHECK_LAUNCH("scan_carry");
+    MTGNN_TRY(scan_carry(p, 1, s));
   }
   scan_variant(d->dtype, d->n, LaunchBack{p, o, grid, s});
   MTGNN_CHECK_LAUNCH("scan_back");
