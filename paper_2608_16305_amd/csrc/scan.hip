@@ -977,7 +977,7 @@ int scan_chunk(const mtgnn_scan_dims* d, int64_t rows, int64_t waves) {
   const int64_t ch = cdiv(cdiv(std::max<int64_t>(rows, 1), blocks), TT) * TT;
   return (int)std::min<int64_t>(ch, int64_t(1) << 30);
 }
-constexpr int64_t FWD_WAVES = 4096, BWD_WAVES = 2048;
+constexpr int64_t FWD_WAVES = 4096, BWD_WAVES = 4096;
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
