@@ -161,16 +161,94 @@ __device__ __attribute__((noinline)) float plain_sum(const void* R, int64_t ldR,
   return v;
 }
 
+// Four columns (n of them) of a row: bias, activation, residual.  wide: y's and the residual's are aligned together.
 template <typename T>
 __device__ __forceinline__ void finish4(const ProdP& p, int64_t r, int64_t c, int n, float (&v)[4]) {
+  const T* res = p.res ? (const T*)p.res + r * p.ldr + c : nullptr;
+  T* y = (T*)p.y + r * p.ldy + c;
+  float* pre = p.pre ? p.pre + r * p.cols + c : nullptr;
+  constexpr uintptr_t A = 4 * sizeof(T) - 1;
+  const bool wide = n == 4 && ((uintptr_t)y & A) == 0 && ((uintptr_t)res & A) == 0 && ((uintptr_t)pre & 15) == 0;
+  float q[4] = {0.f, 0.f, 0.f, 0.f};
+  if (res) {
+    if (wide) {
+      if constexpr (sizeof(T) == 2) {
+        const uint2 w = *(const uint2*)res;
+        q[0] = lo_bf16(w.x); q[1] = hi_bf16(w.x); q[2] = lo_bf16(w.y); q[3] = hi_bf16(w.y);
+      } else {
+        const float4 w = *(const float4*)res;
+        q[0] = w.x; q[1] = w.y; q[2] = w.z; q[3] = w.w;
+      }
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i >= n) break;
-    float a = v[i] + (p.b ? p.b[c + i] : 0.f);
-    if (p.pre) p.pre[r * p.cols + c + i] = a;
-    a = act_(p.act, a);
-    if (p.res) a += Elem<T>::load((const T*)p.res, r * p.ldr + c + i);
-    Elem<T>::store((T*)p.y, r * p.ldy + c + i, a);
+      for (int i = 0; i < 4; ++i)
+        if (i < n) q[i] = Elem<T>::load(res, i);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] += p.b && i < n ? p.b[c + i] : 0.f;
+  if (pre) {
+    if (wide) {
+      *(float4*)pre = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) pre[i] = v[i];
+    }
+  }
+  if (p.act != MTGNN_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = act_(p.act, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] += q[i];
+  if (wide) {
+    if constexpr (sizeof(T) == 2) *(uint2*)y = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+    else *(float4*)y = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) Elem<T>::store(y, i, v[i]);
+  }
+}
+
+// A wave's WR x WC tiles of 16 x 16, rows from ra, columns from ca: sixteen rows at a time through LDS (s: the block's),
+// so that lane l then has row l / (4 WC) of a few and four columns.  again(r, c, v): the value to take for v.
+template <int WR, int WC, typename Y, class Again>
+__device__ __forceinline__ void leave(const ProdP& p, const f32x4 (&acc)[WR][WC], float* lds, int64_t ra, int64_t ca,
+                                      int64_t rows, int share, Again again) {
+  constexpr int LD = 16 * WC + 4, LPR = 4 * WC;     // words of a row; lanes of a row
+  const int lane = threadIdx.x & 63, fr = lane & 15, fg = lane >> 4;
+  float* s = lds + (threadIdx.x >> 6) * 16 * LD;
+  float* out = p.o + (p.split > 1 ? (int64_t)share * p.rows * p.cols : 0);
+#pragma unroll
+  for (int i = 0; i < WR; ++i) {
+#pragma unroll
+    for (int j = 0; j < WC; ++j) *(f32x4*)(s + fr * LD + 16 * j + 4 * fg) = acc[i][j];
+    __syncthreads();
+#pragma unroll 1
+    for (int e = lane; e < 16 * LPR; e += 64) {
+      const int64_t r = ra + 16 * i + e / LPR, c = ca + 4 * (e % LPR);
+      if (r >= rows || c >= p.cols) continue;
+      const f32x4 f = *(const f32x4*)(s + (e / LPR) * LD + 4 * (e % LPR));
+      float v[4] = {f.x, f.y, f.z, f.w};
+      const int n = (int)min((int64_t)4, p.cols - c);
+      if (!(fabsf(f.x) + fabsf(f.y) + fabsf(f.z) + fabsf(f.w) < INFINITY)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (u < n) v[u] = again(r, c + u, v[u]);
+      }
+      if (p.y) {
+        finish4<Y>(p, r, c, n, v);
+      } else if (n == 4 && ((uintptr_t)(out + r * p.ldo + c) & 15) == 0) {
+        *(float4*)(out + r * p.ldo + c) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (u < n) out[r * p.ldo + c + u] = v[u];
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -183,7 +261,7 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
   using SC = Stage<CF, CK, T, KS>;
   using Y = std::conditional_t<CF, float, uint16_t>;
   constexpr int PLANE = T * KS / 2;              // words
-  constexpr int WORDS = (SR::PL + SC::PL) * PLANE, OUT = 4 * 16 * (T / 2 + 4);
+  constexpr int WORDS = (SR::PL + SC::PL) * PLANE, OUT = 4 * 16 * (T / 2 + 4);   // words of the operands, of leave()
   __shared__ __align__(16) uint32_t lds[WORDS > OUT ? WORDS : OUT];
   uint32_t *sR = lds, *sC = lds + SR::PL * PLANE;
   int64_t tr, tcol;
@@ -247,42 +325,89 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
     }
     __syncthreads();
   }
-  // sixteen rows at a time through LDS: lane l then has row l / (T / 8) of a few and four columns
-  constexpr int LD = T / 2 + 4, LPR = T / 8;     // words of a row; lanes of a row
-  float* s = (float*)lds + wid * 16 * LD;
-  float* out = p.o + (p.split > 1 ? (int64_t)share * p.rows * p.cols : 0);
+  leave<W, W, Y>(p, acc, (float*)lds, r0 + wr, c0 + wc, rows, share, [&](int64_t r, int64_t c, float v) {
+    if constexpr (RF || CF) {
+      if (!(fabsf(v) < INFINITY)) return plain_sum<RF, CF, RK, CK>(p.R, p.ldR, p.C, p.ldC, r, c, kb, ke);
+    }
+    return v;
+  });
+}
+
+// The same for bfloat16 operands that are contiguous along k, K a multiple of 64, where there are enough tiles of
+// 256 x 256 for the card.  Eight waves, 128 rows x 64 columns each: a matrix instruction needs 0.75 of the LDS bytes
+// that it needs with 64 x 64.  Rows go straight to LDS, lane l of a load to unit l % 8 of row l / 8; the units'
+// swizzle is in the address that the lane reads.  Two buffers, which are two objects, so that the compiler knows that the
+// reads of one do not wait for the loads into the other; a step's loads are a whole step's work ahead.
+constexpr int BIG = 256, BIG_KS = 64;
+__global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
+  constexpr int WR = 8, WC = 4, OP = BIG * BIG_KS / 2;   // words of an operand's tile
+  __shared__ __align__(1024) uint32_t bufA[2 * OP], bufB[2 * OP];
+  int64_t tr, tcol;
+  int share;
+  my_tile(p, tr, tcol, share);
+  const int64_t rows = eff_count(p.rows, p.rows_dev), K = p.K;
+  const int64_t r0 = tr * BIG, c0 = tcol * BIG;
+  if (r0 >= rows) return;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = (wid >> 2) * 128, wc = (wid & 3) * 64, fr = lane & 15, fg = lane >> 4;
+  // this wave's loads: rows 32 wid + 8 i + lane / 8 of each operand
+  const uint16_t* src[2][4];
 #pragma unroll
-  for (int i = 0; i < W; ++i) {
+  for (int i = 0; i < 4; ++i) {
+    const int row = 32 * wid + 8 * i + (lane >> 3), unit = (lane & 7) ^ (row & 7);
+    src[0][i] = (const uint16_t*)p.R + min(r0 + row, rows - 1) * p.ldR + 8 * unit;
+    src[1][i] = (const uint16_t*)p.C + min(c0 + row, p.cols - 1) * p.ldC + 8 * unit;
+  }
+  typedef __attribute__((address_space(3))) void* lds_ptr;
+  const auto fill = [&](uint32_t* buf, int64_t k) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) *(f32x4*)(s + fr * LD + 16 * j + 4 * fg) = acc[i][j];
-    __syncthreads();
-#pragma unroll 1
-    for (int e = lane; e < 16 * LPR; e += 64) {
-      const int64_t r = r0 + wr + 16 * i + e / LPR, c = c0 + wc + 4 * (e % LPR);
-      if (r >= rows || c >= p.cols) continue;
-      const f32x4 f = *(const f32x4*)(s + (e / LPR) * LD + 4 * (e % LPR));
-      float v[4] = {f.x, f.y, f.z, f.w};
-      const int n = (int)min((int64_t)4, p.cols - c);
-      if constexpr (RF || CF) {
-        if (!(fabsf(f.x) + fabsf(f.y) + fabsf(f.z) + fabsf(f.w) < INFINITY)) {
+    for (int o = 0; o < 2; ++o)
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (u < n && !(fabsf(v[u]) < INFINITY))
-              v[u] = plain_sum<RF, CF, RK, CK>(p.R, p.ldR, p.C, p.ldC, r, c + u, kb, ke);
-        }
-      }
-      if (p.y) {
-        finish4<Y>(p, r, c, n, v);
-      } else if (n == 4 && ((uintptr_t)(out + r * p.ldo + c) & 15) == 0) {
-        *(float4*)(out + r * p.ldo + c) = make_float4(v[0], v[1], v[2], v[3]);
-      } else {
+      for (int i = 0; i < 4; ++i)
+        __builtin_amdgcn_global_load_lds((void*)(src[o][i] + k), (lds_ptr)(buf + o * OP + (32 * wid + 8 * i) * (BIG_KS / 2)),
+                                         16, 0, 0);
+  };
+  f32x4 acc[WR][WC];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (u < n) out[r * p.ldo + c + u] = v[u];
+  for (int i = 0; i < WR; ++i)
+#pragma unroll
+    for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  using S = Stage<false, true, BIG, BIG_KS>;
+  const auto multiply = [&](const uint32_t* buf) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      bf16x8_t cf[WC];
+#pragma unroll
+      for (int j = 0; j < WC; ++j) cf[j] = S::frag(buf + OP, 0, wc + 16 * j + fr, 4 * kk + fg);
+#pragma unroll
+      for (int i = 0; i < WR; ++i) {
+        const bf16x8_t rf = S::frag(buf, 0, wr + 16 * i + fr, 4 * kk + fg);
+#pragma unroll
+        for (int j = 0; j < WC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cf[j], rf, acc[i][j], 0, 0, 0);
       }
     }
-    __syncthreads();
+  };
+  const auto ready = [] {   // this wave's loads have arrived, then everybody's, and the other buffer has been read
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    __builtin_amdgcn_s_barrier();
+  };
+  fill(bufA, 0);
+  const int steps = (int)(K / BIG_KS);
+  int step = 0;
+  for (; step + 1 < steps; step += 2) {
+    ready();
+    fill(bufB, (int64_t)(step + 1) * BIG_KS);
+    multiply(bufA);
+    ready();
+    if (step + 2 < steps) fill(bufA, (int64_t)(step + 2) * BIG_KS);
+    multiply(bufB);
   }
+  if (step < steps) {
+    ready();
+    multiply(bufA);
+  }
+  __syncthreads();
+  leave<WR, WC, uint16_t>(p, acc, (float*)bufA, r0 + wr, c0 + wc, rows, 0, [](int64_t, int64_t, float v) { return v; });
 }
 
 // The sums of the shares of a split product, and what is left of the call.
@@ -352,6 +477,17 @@ size_t split_bytes(int64_t rows, int64_t cols, int64_t K) {
 // out = R C^T; the rest of p is set.
 template <bool RF, bool CF, bool RK, bool CK>
 mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
+  if constexpr (!RF && !CF && RK && CK) {
+    if (p.vecR && p.vecC && p.K % BIG_KS == 0 && cdiv(p.rows, BIG) * cdiv(p.cols, BIG) >= 192) {
+      p.tc = cdiv(p.cols, BIG);
+      p.tiles = cdiv(p.rows, BIG) * p.tc;
+      p.split = 1;
+      TimedScope ts("linear", s);
+      k_product_big<<<(unsigned)p.tiles, 512, 0, s>>>(p);
+      MTGNN_CHECK_LAUNCH("product_big");
+      return MTGNN_OK;
+    }
+  }
   const Plan q = plan(p.rows, p.cols, p.K);
   p.tc = q.tc;
   p.tiles = q.tr * q.tc;

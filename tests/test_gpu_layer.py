@@ -76,7 +76,15 @@ LINEAR = [  # rows, extra rows behind, d_in, d_out, act, bias, residual, wide op
     (300, 0, 1, 70, "silu", True, False, False),
     (300, 1, 70, 1, "relu", True, False, True),
     (1030, 0, 96, 40, "silu", True, True, False),
+    # few rows and long sums: a sum shared by several blocks
+    (3, 0, 2100, 300, "silu", True, True, False),
+    (70, 5, 1000, 40, "gelu", True, True, True),
+    # tiles of 128, and in the weight gradient long sums over rows
+    (2500, 20, 70, 1300, "silu", True, True, False),
+    (4200, 0, 100, 130, "none", True, False, False),
 ]
+# enough tiles of 256 for the widest kernel (an even and an odd number of its steps), whole and ragged
+LINEAR_BIG = [(3333, 40, 192, 3337, "silu", True, True, False), (3584, 0, 128, 3584, "none", False, False, False)]
 
 
 def _linear_case(case, bf16, seed=0):
@@ -91,6 +99,15 @@ def _linear_case(case, bf16, seed=0):
 @pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
 @pytest.mark.parametrize("case", LINEAR, ids=str)
 def test_linear(case, bf16):
+    _check_linear(case, bf16)
+
+
+@pytest.mark.parametrize("case", LINEAR_BIG, ids=str)
+def test_linear_many_tiles(case):
+    _check_linear(case, True)
+
+
+def _check_linear(case, bf16):
     rows, pad, d_in, d_out, act, bias, residual, wide = case
     x, W, b, res, dy = _linear_case(case, bf16)
     behind = lambda v: np.concatenate([v, np.full((pad, v.shape[1]), np.nan, np.float32)])   # noqa: E731
@@ -140,6 +157,36 @@ def test_linear_without_rows_and_optional_outputs():
     M.mtgnn_linear_bwd(dy, None, x, W, d, None, dW, None, ws=ws)
     want = _np(dy).T @ _np(x)
     _close("dW", dW, want, U * 11 * (np.abs(_np(dy)).T @ np.abs(_np(x))))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+def test_linear_past_the_largest_bfloat16(bf16):
+    """Infinite operands, and finite ones past the largest bfloat16, give what products of float32 give."""
+    rs = _gen(4)
+    x, W, dy = _vals(rs, bf16, 70, 40), _vals(rs, bf16, 24, 40), _vals(rs, False, 70, 24)
+    x[3, 5], x[9, 0] = np.inf, -np.inf
+    W[:, 0] = np.abs(W[:, 0]) + 0.5
+    W[:, 5] = np.abs(W[:, 5]) + 0.5
+    if not bf16:
+        x[20, 2], W[:, 2] = 3.4e38, 2.0 ** -20 * (1 + np.abs(W[:, 2]))   # past 3.3895e38
+    if bf16:
+        W = round_bf16(W)   # what the device holds
+    dy[11, 3] = np.inf
+    d = M.linear_dims(40, 24, M.BF16 if bf16 else M.F32)
+    ws = M.alloc_bytes(M.linear_ws_bytes(d, 70, True))
+    X, Wd = _dev(x, bf16), _dev(W, bf16)
+    y, dx, dW = _marked(70, 24, bf16), _marked(70, 40), _marked(24, 40)
+    M.mtgnn_linear(X, Wd, None, None, d, y, ws=ws)
+    M.mtgnn_linear_bwd(_dev(dy), None, X, Wd, d, dx, dW, None, ws=ws)
+    with np.errstate(invalid="ignore"):
+        x64, W64 = x.astype(np.float64), W.astype(np.float64)
+        for name, got, a, b in (("y", y, x64, W64.T), ("dx", dx, dy.astype(np.float64), W64), ("dW", dW, dy.T.astype(np.float64), x64)):
+            want = np.stack([(row[:, None] * b).sum(0) for row in a])
+            mag = np.stack([np.abs(row[:, None] * b).sum(0) for row in a])
+            want[np.abs(want) > np.finfo(np.float32).max] *= np.inf   # no float32 holds it
+            g, fin = _np(got), np.isfinite(want)
+            assert np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[~fin & ~np.isnan(want)], want[~fin & ~np.isnan(want)]), name
+            _close(name, g[fin], want[fin], U * (a.shape[1] + 2) * mag[fin], bf16 and name == "y")
 
 
 def test_linear_residual_in_place_and_nonfinite_rows():
