@@ -281,27 +281,36 @@ __global__ __launch_bounds__(256) void k_conv_back(ConvP p) {
   }
 }
 
-// Single rows: a thread per row and channel.
-template <typename T, int W>
+// Single rows: a thread per row and V channels.
+template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void k_conv_step(ConvP p, const int32_t* n_rows, int64_t max_rows) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = e / p.d;
+  const int dv = p.d / V;
+  const int64_t row = e / dv;
   if (row >= eff_count(max_rows, n_rows)) return;
-  const int ch = (int)(e % p.d);
+  const int ch = (int)(e % dv) * V;
   const int64_t k = seq_slot(p.q.slot, p.q.n_slots, row);
-  T v[W];
+  float v[W][V], w[W][V], a[V];
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j)
-    v[j] = p.st_in && k >= 0 ? ((const T*)p.st_in)[(k * (W - 1) + j) * p.d + ch] : T(0);
-  v[W - 1] = ((const T*)p.x)[row * p.ldx + ch];
-  float a = p.b ? p.b[ch] : 0.f;
+  for (int j = 0; j < W; ++j) {
 #pragma unroll
-  for (int j = 0; j < W; ++j) a = fmaf(Elem<T>::load((const T*)p.w, (int64_t)j * p.d + ch), Elem<T>::load(v, j), a);
+    for (int u = 0; u < V; ++u) v[j][u] = 0.f;
+    if (j == W - 1) get<T, V>(p.x, row * p.ldx + ch, v[j]);
+    else if (p.st_in && k >= 0) get<T, V>(p.st_in, (k * (W - 1) + j) * p.d + ch, v[j]);
+    get<T, V>(p.w, (int64_t)j * p.d + ch, w[j]);
+  }
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    a[u] = p.b ? p.b[ch + u] : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) a[u] = fmaf(w[j][u], v[j][u], a[u]);
+    if (p.act) a[u] = silu_(a[u]);
+  }
   if (p.st_out && k >= 0) {
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) ((T*)p.st_out)[(k * (W - 1) + j) * p.d + ch] = v[j + 1];
+    for (int j = 0; j < W - 1; ++j) put<T, V>(p.st_out, (k * (W - 1) + j) * p.d + ch, v[j + 1]);
   }
-  Elem<T>::store((T*)p.y, row * p.ldy + ch, p.act ? silu_(a) : a);
+  put<T, V>(p.y, row * p.ldy + ch, a);
 }
 
 // ------------------------------------------------------------------ host
@@ -370,7 +379,7 @@ struct LaunchConvStep {
   unsigned grid;
   hipStream_t s;
   template <typename T, int W, int V> void operator()() const {
-    if constexpr (V == 1) k_conv_step<T, W><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
+    k_conv_step<T, W, V><<<grid, 256, 0, s>>>(p, n_rows, max_rows);
   }
 };
 
@@ -430,7 +439,8 @@ mtgnn_status conv_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t 
   ConvP p = conv_params(nullptr, x, ldx, w, b, d);
   p.q.slot = slot; p.q.n_slots = n_slots;
   p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
-  conv_variant(d, false, LaunchConvStep{p, n_rows, max_rows, (unsigned)cdiv(max_rows * d->d, 256), s});
+  const bool two = pairs(d, {x, w, y, state_in, state_out}, {}, {ldx, ldy});
+  conv_variant(d, two, LaunchConvStep{p, n_rows, max_rows, (unsigned)cdiv(max_rows * (d->d / (two ? 2 : 1)), 256), s});
   MTGNN_CHECK_LAUNCH("conv_step");
   return MTGNN_OK;
 }

@@ -255,15 +255,15 @@ __device__ __forceinline__ void leave(const ProdP& p, const f32x4 (&acc)[WR][WC]
 // RF, CF: float32 operands; RK, CK: contiguous along k.  Y: the type of y.
 template <bool RF, bool CF, bool RK, bool CK, int T>
 __global__ __launch_bounds__(NT) void k_product(ProdP p) {
-  constexpr int KS = RF || CF ? 32 : 64;
+  constexpr int KS = T == 128 && (RF || CF) ? 32 : 64;
   constexpr int W = T / 32;                      // 16-wide tiles of a wave, each way
   using SR = Stage<RF, RK, T, KS>;
   using SC = Stage<CF, CK, T, KS>;
   using Y = std::conditional_t<CF, float, uint16_t>;
   constexpr int PLANE = T * KS / 2;              // words
   constexpr int WORDS = (SR::PL + SC::PL) * PLANE, OUT = 4 * 16 * (T / 2 + 4);   // words of the operands, of leave()
-  __shared__ __align__(16) uint32_t lds[WORDS > OUT ? WORDS : OUT];
-  uint32_t *sR = lds, *sC = lds + SR::PL * PLANE;
+  constexpr int BUF = 2 * 4 * WORDS <= 65536 ? 2 : 1;   // two buffers (a barrier less) where two blocks of a CU can have them
+  __shared__ __align__(16) uint32_t lds[BUF * WORDS > OUT ? BUF * WORDS : OUT];
   int64_t tr, tcol;
   int share;
   my_tile(p, tr, tcol, share);
@@ -286,6 +286,8 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
     b.load(p.C, p.ldC, p.cols, c0, kb, ke, p.vecC);
   }
   for (int64_t k = kb; k < ke; k += KS) {
+    uint32_t* sR = lds + (BUF > 1 && (k - kb) / KS % 2 ? WORDS : 0);
+    uint32_t* sC = sR + SR::PL * PLANE;
     a.store(sR);
     b.store(sC);
     __syncthreads();
@@ -323,8 +325,9 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
         mul(0, 0);
       }
     }
-    __syncthreads();
+    if constexpr (BUF == 1) __syncthreads();
   }
+  if constexpr (BUF > 1) __syncthreads();
   leave<W, W, Y>(p, acc, (float*)lds, r0 + wr, c0 + wc, rows, share, [&](int64_t r, int64_t c, float v) {
     if constexpr (RF || CF) {
       if (!(fabsf(v) < INFINITY)) return plain_sum<RF, CF, RK, CK>(p.R, p.ldR, p.C, p.ldC, r, c, kb, ke);
@@ -424,37 +427,64 @@ __global__ __launch_bounds__(256) void k_product_sum(ProdP p, const float* part,
   else p.o[r * p.ldo + c] = v[0];
 }
 
-// g = dy act'(pre), rows dense, and the column sums of each 64 rows (rows < n_rows; zeros without any).
-constexpr int SLOPE_ROWS = 64;
+// g = dy act'(pre), rows dense, and the column sums of each 16 rows (rows < n_rows; zeros without any).  A thread has V
+// columns of 4 rows, all requested before the first is used.
+constexpr int SLOPE_ROWS = 16;
+template <int V>
 __global__ __launch_bounds__(256) void k_linear_slope(const float* dy, int64_t lddy, const float* pre,
                                                       const int32_t* n_rows, int64_t max_rows, int n, int act,
                                                       float* g, float* part) {
-  __shared__ float s[4][64];
-  const int64_t rows = eff_count(max_rows, n_rows);
-  const int64_t cb = cdiv(n, 64), c = (blockIdx.x % cb) * 64 + (threadIdx.x & 63), blk = blockIdx.x / cb;
-  const int64_t r0 = blk * SLOPE_ROWS + (threadIdx.x >> 6);
-  float sum = 0.f;
-  if (c < n) {
-#pragma unroll 4
-    for (int i = 0; i < SLOPE_ROWS / 4; ++i) {
-      const int64_t r = r0 + 4 * i;
-      if (r >= rows) break;
-      float v = dy[r * lddy + c];
-      if (act != MTGNN_ACT_NONE) v *= dact_(act, pre[r * n + c]);
-      if (g) g[r * n + c] = v;
-      sum += v;
+  constexpr int M = SLOPE_ROWS / 4;
+  __shared__ float s[4][64 * V];
+  const int64_t rows = eff_count(max_rows, n_rows), cb = cdiv(n, 64 * V), blk = blockIdx.x / cb;
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int64_t c = ((blockIdx.x % cb) * 64 + lane) * V, r0 = blk * SLOPE_ROWS + wid * M;
+  float sum[V];
+#pragma unroll
+  for (int u = 0; u < V; ++u) sum[u] = 0.f;
+  if (c < n && r0 < rows) {
+    const auto get = [](const float* p, float (&v)[V]) {
+      if constexpr (V == 4) {
+        const float4 f = *(const float4*)p;
+        v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+      } else {
+        v[0] = p[0];
+      }
+    };
+    float d[M][V], q[M][V];
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int64_t r = min(r0 + i, rows - 1);
+      get(dy + r * lddy + c, d[i]);
+      if (act != MTGNN_ACT_NONE) get(pre + r * n + c, q[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      if (r0 + i >= rows) break;
+#pragma unroll
+      for (int u = 0; u < V; ++u) {
+        if (act != MTGNN_ACT_NONE) d[i][u] *= dact_(act, q[i][u]);
+        sum[u] += d[i][u];
+      }
+      if (!g) continue;
+      float* o = g + (r0 + i) * n + c;
+      if constexpr (V == 4) *(float4*)o = make_float4(d[i][0], d[i][1], d[i][2], d[i][3]);
+      else o[0] = d[i][0];
     }
   }
-  s[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+#pragma unroll
+  for (int u = 0; u < V; ++u) s[wid][lane * V + u] = sum[u];
   __syncthreads();
-  if (part && threadIdx.x < 64 && c < n)
-    part[blk * n + c] = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
+  if (!part || wid) return;
+#pragma unroll
+  for (int u = 0; u < V; ++u)
+    if (c < n) part[blk * n + c + u] = (s[0][lane * V + u] + s[1][lane * V + u]) + (s[2][lane * V + u] + s[3][lane * V + u]);
 }
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
 // Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64; with
-// fewer than about a tile per CU the smaller ones fill the card, and then shares of the sum (256 k or more each).
+// fewer than about a tile per CU the smaller ones fill the card, and then shares of the sum (128 k or more each).
 struct Plan {
   int T, split;
   int64_t tr, tc;
@@ -466,7 +496,7 @@ Plan plan(int64_t rows, int64_t cols, int64_t K) {
   p.tr = cdiv(rows, p.T);
   p.tc = cdiv(cols, p.T);
   const int64_t t = p.tr * p.tc;
-  p.split = (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, K / 256));
+  p.split = (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, K / 128));
   return p;
 }
 size_t split_bytes(int64_t rows, int64_t cols, int64_t K) {
@@ -547,8 +577,11 @@ mtgnn_status linear_bwd_impl(const float* dy, int64_t lddy, const float* pre, co
   const float* g = direct ? dy : gbuf;   // without an activation dy is the slope
   const int64_t ldg = direct ? lddy : n, blks = cdiv(max_rows, SLOPE_ROWS);
   if (!direct || db) {
-    k_linear_slope<<<(unsigned)(blks * cdiv(n, 64)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act,
-                                                                  direct ? nullptr : gbuf, db ? part : nullptr);
+    float *to = direct ? nullptr : gbuf, *sums = db ? part : nullptr;
+    if (n % 4 == 0 && lddy % 4 == 0 && ((uintptr_t)dy | (uintptr_t)pre | (uintptr_t)to) % 16 == 0)
+      k_linear_slope<4><<<(unsigned)(blks * cdiv(n, 256)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act, to, sums);
+    else
+      k_linear_slope<1><<<(unsigned)(blks * cdiv(n, 64)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act, to, sums);
     MTGNN_CHECK_LAUNCH("linear_slope");
   }
   if (db) {
