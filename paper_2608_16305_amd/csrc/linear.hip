@@ -31,7 +31,7 @@ struct ProdP {
   int64_t ldR, ldC;
   int64_t rows, cols, K;           // rows of R and C, length of the sums
   const int32_t *rows_dev, *K_dev; // device counts that bound them, or NULL
-  int vecR, vecC;                  // contiguous along k: 16-byte loads are aligned
+  int aligned;                     // every row of both operands starts at a multiple of 16 bytes
   int64_t tc, tiles;               // tiles of a row of tiles, tiles in all
   int split;                       // blocks that share a tile's sum
   // output: float32 sums (o, split x rows x cols of them where split > 1), or the layer's epilogue (y given)
@@ -45,6 +45,11 @@ struct ProdP {
   float* pre;
   int act;
 };
+
+// Sixteen bytes at any element's address (the loads take it; a row of an odd length is at no other).
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef words4 words4_at4 __attribute__((aligned(4)));
+typedef words4 words4_at2 __attribute__((aligned(2)));
 
 // One operand's share of a tile in a thread's registers: U units of eight k.
 template <bool F32, bool KC, int T, int KS>
@@ -61,20 +66,19 @@ struct Stage {
     return KC ? id % CH : id / T;
   }
   // rows r0 .. of the operand (the last one stands for those past it), k0 .. k0 + KS - 1 (zeros from K on)
-  __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t rows, int64_t r0, int64_t k0, int64_t K,
-                                       bool vec) {
+  __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t rows, int64_t r0, int64_t k0, int64_t K) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t r = min(r0 + row(u), rows - 1), k = k0 + chunk(u) * 8;
       if constexpr (KC) {
-        if (vec && k + 8 <= K) {
+        if (k + 8 <= K) {
           if constexpr (F32) {
-            const uint4* q = (const uint4*)((const float*)p + r * ld + k);
-            const uint4 a = q[0], b = q[1];
+            const words4_at4* q = (const words4_at4*)((const float*)p + r * ld + k);
+            const words4 a = q[0], b = q[1];
             v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
             v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
           } else {
-            const uint4 a = *(const uint4*)((const uint16_t*)p + r * ld + k);
+            const words4 a = *(const words4_at2*)((const uint16_t*)p + r * ld + k);
             v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
           }
         } else {
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
   using Y = std::conditional_t<CF, float, uint16_t>;
   constexpr int PLANE = T * KS / 2;              // words
   constexpr int WORDS = (SR::PL + SC::PL) * PLANE, OUT = 4 * 16 * (T / 2 + 4);   // words of the operands, of leave()
-  constexpr int BUF = 2 * 4 * WORDS <= 65536 ? 2 : 1;   // two buffers (a barrier less) where two blocks of a CU can have them
+  constexpr int BUF = T == 128 && 2 * 4 * WORDS <= 65536 ? 2 : 1;   // two buffers (a barrier less) where they cost no block of a CU
   __shared__ __align__(16) uint32_t lds[BUF * WORDS > OUT ? BUF * WORDS : OUT];
   int64_t tr, tcol;
   int share;
@@ -282,8 +286,8 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
   SR a;
   SC b;
   if (kb < ke) {
-    a.load(p.R, p.ldR, rows, r0, kb, ke, p.vecR);
-    b.load(p.C, p.ldC, p.cols, c0, kb, ke, p.vecC);
+    a.load(p.R, p.ldR, rows, r0, kb, ke);
+    b.load(p.C, p.ldC, p.cols, c0, kb, ke);
   }
   for (int64_t k = kb; k < ke; k += KS) {
     uint32_t* sR = lds + (BUF > 1 && (k - kb) / KS % 2 ? WORDS : 0);
@@ -292,8 +296,8 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
     b.store(sC);
     __syncthreads();
     if (k + KS < ke) {
-      a.load(p.R, p.ldR, rows, r0, k + KS, ke, p.vecR);
-      b.load(p.C, p.ldC, p.cols, c0, k + KS, ke, p.vecC);
+      a.load(p.R, p.ldR, rows, r0, k + KS, ke);
+      b.load(p.C, p.ldC, p.cols, c0, k + KS, ke);
     }
 #pragma unroll
     for (int kk = 0; kk < KS / 32; ++kk) {
@@ -483,15 +487,15 @@ __global__ __launch_bounds__(256) void k_linear_slope(const float* dy, int64_t l
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
-// Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64; with
-// fewer than about a tile per CU the smaller ones fill the card, and then shares of the sum (128 k or more each).
+// Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64, and
+// needs two blocks a CU to hide a step's loads: with fewer than about 400 the smaller ones fill the card, and then shares of the sum (128 k or more each).
 struct Plan {
   int T, split;
   int64_t tr, tc;
 };
 Plan plan(int64_t rows, int64_t cols, int64_t K) {
   Plan p;
-  p.T = cdiv(rows, 128) * cdiv(cols, 128) >= 192 ? 128 : 64;
+  p.T = cdiv(rows, 128) * cdiv(cols, 128) >= 400 ? 128 : 64;
   if (p.T == 64 && rows > 64 && cols > 64 && K >= 4096) p.T = 128;   // long sums (dW): shares fill the card
   p.tr = cdiv(rows, p.T);
   p.tc = cdiv(cols, p.T);
@@ -508,7 +512,7 @@ size_t split_bytes(int64_t rows, int64_t cols, int64_t K) {
 template <bool RF, bool CF, bool RK, bool CK>
 mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
   if constexpr (!RF && !CF && RK && CK) {
-    if (p.vecR && p.vecC && p.K % BIG_KS == 0 && cdiv(p.rows, BIG) * cdiv(p.cols, BIG) >= 192) {
+    if (p.aligned && p.K % BIG_KS == 0 && cdiv(p.rows, BIG) * cdiv(p.cols, BIG) >= 192) {
       p.tc = cdiv(p.cols, BIG);
       p.tiles = cdiv(p.rows, BIG) * p.tc;
       p.split = 1;
@@ -560,8 +564,7 @@ mtgnn_status linear_impl(const void* x, int64_t ldx, const int32_t* n_rows, int6
   ProdP p{};
   p.R = x; p.ldR = ldx; p.C = W; p.ldC = d->d_in;
   p.rows = max_rows; p.cols = d->d_out; p.K = d->d_in; p.rows_dev = n_rows;
-  p.vecR = ldx % per == 0 && (uintptr_t)x % 16 == 0;
-  p.vecC = d->d_in % per == 0 && (uintptr_t)W % 16 == 0;
+  p.aligned = ldx % per == 0 && d->d_in % per == 0 && ((uintptr_t)x | (uintptr_t)W) % 16 == 0;
   p.b = b; p.res = res; p.ldr = ldr; p.y = y; p.ldy = ldy; p.pre = pre; p.act = d->act;
   return bf ? product<false, false, true, true>(p, ws, s) : product<true, true, true, true>(p, ws, s);
 }
@@ -592,7 +595,6 @@ mtgnn_status linear_bwd_impl(const float* dy, int64_t lddy, const float* pre, co
     ProdP p{};
     p.R = g; p.ldR = ldg; p.C = W; p.ldC = d->d_in;
     p.rows = max_rows; p.cols = d->d_in; p.K = n; p.rows_dev = n_rows;
-    p.vecR = ldg % 4 == 0 && (uintptr_t)g % 16 == 0;
     p.o = dx; p.ldo = lddx;
     MTGNN_TRY((bf ? product<true, false, true, false>(p, rest, s) : product<true, true, true, false>(p, rest, s)));
   }
