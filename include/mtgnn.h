@@ -565,7 +565,7 @@ mtgnn_status mtgnn_time_projection_bwd(const int32_t* q_node, const float* q_t, 
 typedef enum { MTGNN_ACT_NONE = 0, MTGNN_ACT_RELU = 1, MTGNN_ACT_SILU = 2, MTGNN_ACT_GELU = 3 } mtgnn_act;
 
 typedef struct {
-  int64_t max_rows, max_seq; /* rows of the matrices; the most sequences (max_seq <= 2^30, max_rows < 2^31 - 1) */
+  int64_t max_rows, max_seq; /* rows of the matrices; the most sequences (max_seq <= 2^30, max_rows < 2^31 - 64) */
   int64_t n_slots;           /* rows of the state tables (0 where no state is given) */
   const int32_t* off;        /* [max_seq + 1] device */
   const int32_t* n_seq;      /* device count n of sequences, or NULL: max_seq */

@@ -10,7 +10,7 @@ using namespace mtgnn;
 
 namespace {
 
-constexpr int64_t MAX_ROWS = (int64_t(1) << 31) - 1;
+constexpr int64_t MAX_ROWS = (int64_t(1) << 31) - 64;   // a tile past the last row is still an int32
 constexpr int MAX_WIDTH = 1 << 20;   // channels, columns
 
 bool dtype_ok(int t) { return t == MTGNN_F32 || t == MTGNN_BF16; }

@@ -1115,7 +1115,6 @@ mtgnn_status scan_impl(const mtgnn_seqs* q, const mtgnn_scan_inputs* in, const m
   p.ch = scan_chunk(d, rows, FWD_WAVES);
   p.nchunk = (int)cdiv(rows, p.ch);
   p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
-  p.vec = scan_vec(p, state_in, state_out);
   if (save) {
     scan_save_at(p, d, rows, save);
     if (!state_in) p.init = nullptr;
@@ -1143,7 +1142,7 @@ mtgnn_status scan_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
   const int64_t rows = q->max_rows;
   p.ch = scan_chunk(d, rows, BWD_WAVES);
   p.nchunk = (int)cdiv(rows, p.ch);
-  p.vec = scan_vec(p, nullptr, nullptr);
+  p.vec = scan_vec(p, ws, save);
   scan_save_at(p, d, rows, const_cast<void*>(save));
   const ScanWs w = scan_ws_layout(d, rows, true);
   p.E = (float*)((char*)ws + w.E);

@@ -677,6 +677,66 @@ def test_calls_captured_and_replayed():
             assert torch.equal(a, b), i
 
 
+@pytest.mark.parametrize("n_seq", [0, -3])
+def test_no_sequences(n_seq):
+    """A device count of no sequences: no row and no slot is written, parameter gradients are zero."""
+    q = Layout(LENS["ragged"], 0, 3)
+    v = _scan_case(q, 70, 16, 1, True, True, True, True, False)
+    dims, dc = M.scan_dims(70, 16), M.conv_dims(70, 4)
+    n = torch.tensor([n_seq], dtype=torch.int32, device="cuda")
+    q.q = M.seqs(q.off_, q.total, n_seq=n, slot=q.slot_, n_slots=q.n_slots)
+    y, st, g, (t, _, _) = _scan_run(q, v, dims, False, True, False)
+    assert bool((y == MARK).all()) and bool((st == MARK).all())
+    for k in g:
+        assert bool((g[k] == (0.0 if k in ("dA", "dD", "ddelta_bias") else MARK)).all()), k
+    w, cst = torch.ones(4, 70, device="cuda"), torch.zeros(q.n_slots, 3, 70, device="cuda")
+    out, dx, dw = torch.full_like(cst, MARK), _marked(q.total, 70), _marked(4, 70)
+    M.mtgnn_causal_conv(q.q, t["x"], w, None, dc, cst, out, y)
+    M.mtgnn_causal_conv_bwd(q.q, t["x"], t["x"], w, None, dc, None, dx, dw, None,
+                            M.alloc_bytes(M.causal_conv_ws_bytes(dc, q.total)))
+    assert bool((y == MARK).all()) and bool((out == MARK).all()) and bool((dx == MARK).all()) and not bool(dw.any())
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^20 elements apart, and a slot at the far end of a state table of 2^31 elements."""
+    rows, ld, d = 2100, 1 << 20, 40
+    big = torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda")
+    x = big[:, ld - d:]
+    x.copy_(torch.randn(rows, d, device="cuda"))
+    near = x.contiguous()
+    off = torch.tensor([0, 700, rows], dtype=torch.int32, device="cuda")
+    q = M.seqs(off, rows)
+    w = torch.randn(4, d, device="cuda").bfloat16()
+    dc, dl, ds = M.conv_dims(d, 4, M.BF16), M.linear_dims(d, 24, M.BF16), M.scan_dims(d, 8, 1, M.BF16)
+    W, A = torch.randn(24, d, device="cuda").bfloat16(), -torch.rand(8, d, device="cuda")
+    BC = torch.randn(rows, 16, device="cuda").bfloat16()
+    ws = M.alloc_bytes(max(M.linear_ws_bytes(dl, rows, True), M.selective_scan_ws_bytes(ds, rows, 2, True)))
+    res = []
+    for m in (x, near):
+        y, l, s = (torch.zeros(rows, c, dtype=torch.bfloat16, device="cuda") for c in (d, 24, d))
+        M.mtgnn_causal_conv(q, m, w, None, dc, None, None, y)
+        M.mtgnn_linear(m, W, None, None, dl, l, ws=ws)
+        M.mtgnn_selective_scan(q, M.scan_inputs(ds, m, m, A, BC[:, :8], BC[:, 8:], z=m), ds, None, None, s, ws=ws)
+        res.append((y, l, s))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+    del big, x
+    far, n = (1 << 31) // (8 * d) + 3, 4
+    table = torch.zeros(far + n, 8, d, device="cuda")
+    table[far:] = torch.randn(n, 8, d, device="cuda")
+    small = table[far:].clone()
+    ys = []
+    for t, base in ((table, far), (small, 0)):
+        y = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+        slot = torch.arange(base, base + n, dtype=torch.int32, device="cuda")
+        inp = M.scan_inputs(ds, near[:n], near[:n], A, BC[:n, :8], BC[:n, 8:])
+        M.mtgnn_selective_scan_step(slot, inp, ds, t, t, y)
+        qs = M.seqs(torch.tensor([0, 3, 3, 4], dtype=torch.int32, device="cuda"), n, slot=slot[:3].contiguous(), n_slots=t.shape[0])
+        M.mtgnn_selective_scan(qs, inp, ds, t, t, y, ws=ws)
+        ys.append(y)
+    assert torch.equal(*ys) and torch.equal(table[far:], small)
+    assert not bool(table[:n].any())
+
+
 def test_layer_on_another_stream():
     q = Layout(LENS["two"], 0, 0)
     v = _scan_case(q, 64, 16, 1, True, True, True, True, True)
