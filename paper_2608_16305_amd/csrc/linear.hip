@@ -395,8 +395,10 @@ __global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
     }
   };
   const auto ready = [] {   // this wave's loads have arrived, then everybody's, and the other buffer has been read
+    asm volatile("" ::: "memory");        // reads of LDS stay on their side
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
   fill(bufA, 0);
   const int steps = (int)(K / BIG_KS);
