@@ -30,6 +30,10 @@ mtgnn_status check_seqs(const mtgnn_seqs* q, int64_t width) {
   if (q->max_seq > 0 && q->max_rows > 0) REQ(q->off, "off");
   return MTGNN_OK;
 }
+// A launch with a thread to each of rows x width (work items are a 32-bit number).
+mtgnn_status check_items(int64_t rows, int64_t width, const char* what) {
+  return rows * width > (int64_t(1) << 32) - 256 ? fail(MTGNN_EUNSUPPORTED, what) : MTGNN_OK;
+}
 bool no_rows(const mtgnn_seqs* q) { return q->max_rows == 0 || q->max_seq == 0; }
 
 #define STRIDE(ld, width, name) \
@@ -101,6 +105,7 @@ mtgnn_status mtgnn_linear(const void* x, int64_t ldx, const int32_t* n_rows, int
   STRIDE(ldx, d->d_in, "ldx");
   STRIDE(ldy, d->d_out, "ldy");
   if (residual) STRIDE(ldr, d->d_out, "ldr");
+  if (!linear_fits(d, max_rows, false)) return fail(MTGNN_EUNSUPPORTED, "max_rows times width");
   const size_t need = linear_ws(d, max_rows, false);
   if (ws_bytes < need) return fail(MTGNN_EWORKSPACE, "linear ws");
   if (need) REQ(ws, "ws");
@@ -122,6 +127,7 @@ mtgnn_status mtgnn_linear_bwd(const float* dy, int64_t lddy, const float* pre, c
   STRIDE(lddy, d->d_out, "lddy");
   STRIDE(ldx, d->d_in, "ldx");
   if (dx) STRIDE(lddx, d->d_in, "lddx");
+  if (!linear_fits(d, max_rows, true)) return fail(MTGNN_EUNSUPPORTED, "max_rows times width");
   const size_t need = linear_ws(d, max_rows, true);
   if (ws_bytes < need) return fail(MTGNN_EWORKSPACE, "linear_bwd ws");
   if (need) REQ(ws, "ws");
@@ -149,6 +155,7 @@ mtgnn_status mtgnn_causal_conv(const mtgnn_seqs* q, const void* x, int64_t ldx, 
   REQ(y, "y");
   STRIDE(ldx, d->d, "ldx");
   STRIDE(ldy, d->d, "ldy");
+  if (state_out || save) MTGNN_TRY(check_items(q->max_seq, d->d, "max_seq times d >= 2^32"));
   return conv_impl(q, x, ldx, w, b, d, state_in, state_out, y, ldy, save, stream);
 }
 
@@ -185,6 +192,7 @@ mtgnn_status mtgnn_causal_conv_step(const int32_t* slot, const int32_t* n_rows, 
   REQ(y, "y");
   STRIDE(ldx, d->d, "ldx");
   STRIDE(ldy, d->d, "ldy");
+  MTGNN_TRY(check_items(max_rows, d->d, "max_rows times d >= 2^32"));
   return conv_step_impl(slot, n_rows, max_rows, n_slots, x, ldx, w, b, d, state_in, state_out, y, ldy, stream);
 }
 
@@ -240,6 +248,7 @@ mtgnn_status mtgnn_selective_scan_bwd(const mtgnn_seqs* q, const float* dy, int6
   STRIDE(g->lddB, (int64_t)d->groups * d->n, "lddB");
   STRIDE(g->lddC, (int64_t)d->groups * d->n, "lddC");
   if (g->dz) STRIDE(g->lddz, d->d, "lddz");
+  MTGNN_TRY(check_items(q->max_rows, 2 * (int64_t)d->groups * d->n, "max_rows times 2 groups n >= 2^32"));
   if (ws_bytes < scan_ws(d, q->max_rows, true)) return fail(MTGNN_EWORKSPACE, "selective_scan_bwd ws");
   REQ(ws, "ws");
   return scan_bwd_impl(q, dy, lddy, in, d, save, g, ws, stream);
@@ -255,6 +264,7 @@ mtgnn_status mtgnn_selective_scan_step(const int32_t* slot, const int32_t* n_row
   MTGNN_TRY(check_inputs(in, d));
   REQ(y, "y");
   STRIDE(ldy, d->d, "ldy");
+  MTGNN_TRY(check_items(max_rows, d->d, "max_rows times d >= 2^32"));
   return scan_step_impl(slot, n_rows, max_rows, n_slots, in, d, state_in, state_out, y, ldy, stream);
 }
 

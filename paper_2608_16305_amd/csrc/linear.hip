@@ -501,7 +501,7 @@ Plan plan(int64_t rows, int64_t cols, int64_t K) {
   if (p.T == 64 && rows > 64 && cols > 64 && K >= 4096) p.T = 128;   // long sums (dW): shares fill the card
   p.tr = cdiv(rows, p.T);
   p.tc = cdiv(cols, p.T);
-  const int64_t t = p.tr * p.tc;
+  const int64_t t = std::max<int64_t>(1, p.tr * p.tc);   // (sizes are asked for no rows too)
   p.split = (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, K / 128));
   return p;
 }

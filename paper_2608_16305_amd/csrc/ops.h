@@ -251,6 +251,7 @@ mtgnn_status attn_bwd_group_impl(const int32_t* q_node, const int32_t* n_q, int6
                                  const mtgnn_dims* d, void* ws, size_t ws_bytes, hipStream_t s);
 
 // state-space layer (linear.hip, conv.hip, scan.hip; arguments as in mtgnn.h, validated)
+bool linear_fits(const mtgnn_linear_dims* d, int64_t rows, bool back);
 size_t linear_ws(const mtgnn_linear_dims* d, int64_t rows, bool back);
 mtgnn_status linear_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W,
                          const float* b, const void* res, int64_t ldr, const mtgnn_linear_dims* d, void* y,

@@ -210,3 +210,13 @@ def test_binding_refuses_host_tensors():
         M.mtgnn_linear(torch.zeros(3, 4), torch.zeros(5, 4), None, None, M.linear_dims(4, 5), torch.zeros(3, 5))
     with pytest.raises(M.MtgnnError):
         M.seqs(torch.zeros(3, dtype=torch.int32), 4)
+
+
+@built
+def test_sizes_without_rows():
+    for act in (M.ACT_NONE, M.ACT_SILU):
+        d = M.linear_dims(64, 64, act=act)
+        assert M.linear_ws_bytes(d, 0) == 0 and M.linear_ws_bytes(d, 0, True) >= 0
+    assert M.causal_conv_ws_bytes(M.conv_dims(8, 4), 0) >= 0 and M.causal_conv_save_bytes(M.conv_dims(8, 4), 0) == 0
+    s = M.scan_dims(8, 4)
+    assert M.selective_scan_ws_bytes(s, 0, 0, True) >= 0 and M.selective_scan_save_bytes(s, 0, 0, True) >= 0
