@@ -156,11 +156,15 @@ template <bool RF, bool CF, bool RK, bool CK>
 __device__ __attribute__((noinline)) float plain_sum(const void* R, int64_t ldR, const void* C, int64_t ldC, int64_t r,
                                                      int64_t c, int64_t k0, int64_t k1) {
   float v = 0.f;
-  for (int64_t k = k0; k < k1; ++k) {
-    const int64_t a = RK ? r * ldR + k : k * ldR + r, b = CK ? c * ldC + k : k * ldC + c;
-    const float x = RF ? ((const float*)R)[a] : bf16_to_f32(((const uint16_t*)R)[a]);
-    const float w = CF ? ((const float*)C)[b] : bf16_to_f32(((const uint16_t*)C)[b]);
-    v = fmaf(x, w, v);
+  for (int64_t k = k0; k < k1 && v == v; k += 16) {   // a NaN stays one: the rest need not be read
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const int64_t at = min(k + u, k1 - 1);
+      const int64_t a = RK ? r * ldR + at : at * ldR + r, b = CK ? c * ldC + at : at * ldC + c;
+      const float x = RF ? ((const float*)R)[a] : bf16_to_f32(((const uint16_t*)R)[a]);
+      const float w = CF ? ((const float*)C)[b] : bf16_to_f32(((const uint16_t*)C)[b]);
+      v = k + u < k1 ? fmaf(x, w, v) : v;
+    }
   }
   return v;
 }
@@ -394,9 +398,9 @@ __global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
       }
     }
   };
-  const auto ready = [] {   // this wave's loads have arrived, then everybody's, and the other buffer has been read
+  const auto ready = [] {   // this wave's loads have arrived and its reads are done, then everybody's
     asm volatile("" ::: "memory");        // reads of LDS stay on their side
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
