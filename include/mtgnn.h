@@ -561,7 +561,9 @@ mtgnn_status mtgnn_time_projection_bwd(const int32_t* q_node, const float* q_t, 
  * one there: slot s of a table where slot is NULL, else slot[s].  A slot outside [0, n_slots) stands for no
  * slot: the sequence starts from zeros and its last state is dropped.  Two sequences of a call must not share
  * a slot.  A sequence without rows leaves its slot as it was.  The state a call starts from is an input that is
- * not differentiated, as the memory table is not across steps. */
+ * not differentiated, as the memory table is not across steps.  Calls whose launches would have 2^32 threads or
+ * more are refused (MTGNN_EUNSUPPORTED): a thread to each row and channel of single rows and of the convolution's
+ * states, to each dB and dC, to 16 outputs of a linear layer; 16 to a row for each 64 columns of its backward. */
 typedef enum { MTGNN_ACT_NONE = 0, MTGNN_ACT_RELU = 1, MTGNN_ACT_SILU = 2, MTGNN_ACT_GELU = 3 } mtgnn_act;
 
 typedef struct {
@@ -579,7 +581,8 @@ typedef struct {
  * act: silu(p) = p / (1 + e^-p), gelu(p) = p (1 + erf(p / sqrt 2)) / 2.  y may be residual (same stride); it
  * may not overlap x.  A product is exact to float32: bfloat16 operands multiply on the bfloat16 matrix
  * instructions; float32 ones there too, as three bfloat16 parts each.
- * Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too.  Rows at or beyond n_rows are left untouched. */
+ * Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too.  Rows at or beyond
+ * n_rows are left untouched. */
 typedef struct {
   int32_t d_in, d_out, dtype, act; /* mtgnn_dtype, mtgnn_act */
 } mtgnn_linear_dims;
@@ -635,7 +638,9 @@ mtgnn_status mtgnn_causal_conv_step(const int32_t* slot, const int32_t* n_rows, 
  *   dt_t = softplus(delta_t + delta_bias)   (softplus 0 in the dims: delta_t + delta_bias),
  *   h_t[i] = exp(dt_t A[i]) h_(t-1)[i] + dt_t B_t[i] x_t,
  *   y_t = (sum_i C_t[i] h_t[i] + D x_t) silu(z_t),
- * h before the sequence's first row being its slot's state.  n <= 64; groups divides d.
+ * h before the sequence's first row being its slot's state.  n <= 64; groups divides d.  dt_t A[i] is a decay (A <= 0
+ * with softplus): rows are worked on in pieces that meet by exp(A[i] sum of dt over a piece), which a growth over
+ * some hundred rows takes past float32.
  *   x, delta, z (or NULL: no gate), y -- [max_rows, d] (dtype); y may be x, delta or z (same stride) where no
  *           backward follows, and may not overlap them otherwise;
  *   B, C -- [max_rows, groups * n] (dtype), each group's n columns together;

@@ -556,6 +556,18 @@ mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
 
 }  // namespace
 
+// Work items of a launch are a 32-bit number.
+bool linear_fits(const mtgnn_linear_dims* d, int64_t rows, bool back) {
+  constexpr int64_t MAX = int64_t(1) << 32;
+  const auto fits = [](int64_t r, int64_t c, int64_t K) {
+    const Plan q = plan(r, c, K);
+    return q.tr * q.tc * q.split * NT < MAX;
+  };
+  if (!back) return fits(rows, d->d_out, d->d_in);
+  return fits(rows, d->d_in, d->d_out) && fits(d->d_out, d->d_in, rows) &&
+         cdiv(rows, SLOPE_ROWS) * cdiv(d->d_out, 64) * 256 < MAX;
+}
+
 size_t linear_ws(const mtgnn_linear_dims* d, int64_t rows, bool back) {
   if (!back) return split_bytes(rows, d->d_out, d->d_in);
   const size_t g = al((size_t)rows * d->d_out * 4) + al((size_t)cdiv(rows, SLOPE_ROWS) * d->d_out * 4);

@@ -220,3 +220,18 @@ def test_sizes_without_rows():
     assert M.causal_conv_ws_bytes(M.conv_dims(8, 4), 0) >= 0 and M.causal_conv_save_bytes(M.conv_dims(8, 4), 0) == 0
     s = M.scan_dims(8, 4)
     assert M.selective_scan_ws_bytes(s, 0, 0, True) >= 0 and M.selective_scan_save_bytes(s, 0, 0, True) >= 0
+
+
+@built
+def test_launches_of_too_many_threads_are_refused():
+    """Refused with EUNSUPPORTED before anything is launched; the sizes just below are not tried."""
+    L = M.lib()
+    many = 1 << 29   # rows of eight channels
+    conv, scan, lin = C.byref(M.ConvDims(8, 4, 0, 2)), C.byref(M.ScanDims(8, 4, 1, 0, 1)), C.byref(M.LinearDims(8, 1, 0, 0))
+    assert L.mtgnn_causal_conv_step(None, None, many, 4, P, 8, P, None, conv, P, P, P, 8, None) == -2
+    assert L.mtgnn_causal_conv(_q(max_seq=many), P, 8, P, None, conv, P, P, P, 8, None, None) == -2
+    assert L.mtgnn_causal_conv(_q(max_seq=many), P, 8, P, None, conv, P, None, P, 8, P, None) == -2
+    assert L.mtgnn_selective_scan_step(None, None, many, 4, _inp(), scan, P, P, P, 8, None) == -2
+    g = M.ScanGrads(P, P, P, P, None, 8, 8, 4, 4, 0, P, None, None)
+    assert L.mtgnn_selective_scan_bwd(_q(max_rows=many), P, 8, _inp(), scan, P, C.byref(g), P, 1 << 62, None) == -2
+    assert L.mtgnn_linear_bwd(P, 1, None, P, 8, None, many, P, lin, P, 8, P, P, P, 1 << 62, None) == -2
