@@ -65,37 +65,44 @@ struct Stage {
     const int id = u * NT + threadIdx.x;
     return KC ? id % CH : id / T;
   }
-  // rows r0 .. of the operand (the last one stands for those past it), k0 .. k0 + KS - 1 (zeros from K on)
-  __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t rows, int64_t r0, int64_t k0, int64_t K) {
+  using E = std::conditional_t<F32, uint32_t, uint16_t>;
+  const E* q[U];   // of each unit: its row at the step's first k
+  int64_t ld;
+  // rows r0 .. of the operand (the last one stands for those past it)
+  __device__ __forceinline__ void at_rows(const void* p, int64_t ld_, int64_t rows, int64_t r0) {
+    ld = ld_;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t r = min(r0 + row(u), rows - 1), k = k0 + chunk(u) * 8;
-      if constexpr (KC) {
-        if (k + 8 <= K) {
-          if constexpr (F32) {
-            const words4_at4* q = (const words4_at4*)((const float*)p + r * ld + k);
-            const words4 a = q[0], b = q[1];
-            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
-            v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
-          } else {
-            const words4 a = *(const words4_at2*)((const uint16_t*)p + r * ld + k);
-            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
-          }
-        } else {
-          uint32_t e[8];
+      const int64_t r = min(r0 + row(u), rows - 1);
+      q[u] = (const E*)p + (KC ? r * ld : r);
+    }
+  }
+  // k0 .. k0 + KS - 1 (zeros from K on)
+  __device__ __forceinline__ void load(int64_t k0, int64_t K) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int64_t at = r * ld + min(k + i, K - 1);
-            e[i] = F32 ? ((const uint32_t*)p)[at] : (uint32_t)((const uint16_t*)p)[at];
-          }
-          put(u, e, k, K);
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + chunk(u) * 8;
+      uint32_t e[8];
+      if ((KC ? k + 8 : k0 + KS) <= K) {
+        if constexpr (KC && F32) {
+          const words4_at4* w = (const words4_at4*)(q[u] + k);
+          const words4 a = w[0], b = w[1];
+          v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
+          v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
+        } else if constexpr (KC) {
+          const words4 a = *(const words4_at2*)(q[u] + k);
+          v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
+        } else {
+          const E* w = q[u] + k * ld;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) e[i] = w[i * ld];
+          put(u, e, 0, 8);
         }
       } else {
-        uint32_t e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int64_t at = min(k + i, K - 1) * ld + r;
-          e[i] = F32 ? ((const uint32_t*)p)[at] : (uint32_t)((const uint16_t*)p)[at];
+          const int64_t at = min(k + i, K - 1);
+          e[i] = q[u][KC ? at : at * ld];
         }
         put(u, e, k, K);
       }
@@ -289,9 +296,11 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
     for (int j = 0; j < W; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   SR a;
   SC b;
+  a.at_rows(p.R, p.ldR, rows, r0);
+  b.at_rows(p.C, p.ldC, p.cols, c0);
   if (kb < ke) {
-    a.load(p.R, p.ldR, rows, r0, kb, ke);
-    b.load(p.C, p.ldC, p.cols, c0, kb, ke);
+    a.load(kb, ke);
+    b.load(kb, ke);
   }
   for (int64_t k = kb; k < ke; k += KS) {
     uint32_t* sR = lds + (BUF > 1 && (k - kb) / KS % 2 ? WORDS : 0);
@@ -300,8 +309,8 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
     b.store(sC);
     __syncthreads();
     if (k + KS < ke) {
-      a.load(p.R, p.ldR, rows, r0, k + KS, ke);
-      b.load(p.C, p.ldC, p.cols, c0, k + KS, ke);
+      a.load(k + KS, ke);
+      b.load(k + KS, ke);
     }
 #pragma unroll
     for (int kk = 0; kk < KS / 32; ++kk) {
