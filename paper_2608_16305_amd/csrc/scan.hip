@@ -1031,12 +1031,16 @@ void scan_variant(int dtype, int n, F f) {
   else by(float{});
 }
 
-// The lane-per-channel kernels: n rounded up, and whether B's and C's rows are whole words (n of a supported number).
+// The lane-per-channel kernels: n rounded up, and whether B and C come by scalar loads: their rows are whole words (n of
+// a supported number), and sequences of a tile's rows or more leave most tiles inside one, where the next words are
+// requested ahead.  k_scan_out and k_scan_local by scalar loads against LDS: 370 and 234 us against 540 and 231
+// (5 sequences, 32,768 rows x 2,048, bfloat16); 31.5 and 15.2 against 28.5 and 14.0 (6,000 sequences of 8,000 rows x 100).
 template <typename F>
 void scan_lane_variant(const ScanP& p, int dtype, F f) {
   const int N = p.n <= 4 ? 4 : p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;   // 64: two waves of 32
-  const bool words = p.n == N && (dtype == MTGNN_F32 || (p.ldB % 2 == 0 && p.ldC % 2 == 0 && (uintptr_t)p.B % 4 == 0 &&
-                                                         (uintptr_t)p.C % 4 == 0));
+  const bool words = p.n == N && p.q.max_rows >= TT * p.q.max_seq &&
+                     (dtype == MTGNN_F32 || (p.ldB % 2 == 0 && p.ldC % 2 == 0 && (uintptr_t)p.B % 4 == 0 &&
+                                            (uintptr_t)p.C % 4 == 0));
   const auto by = [&](auto t) {
     using T = decltype(t);
     const auto with = [&](auto sc) {
@@ -1180,7 +1184,9 @@ mtgnn_status scan_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t 
   p.q.slot = slot;
   p.q.n_slots = n_slots;
   p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
-  const bool four = scan_vec(p, state_in, state_out);
+  // Four channels a thread where that leaves four blocks a CU: 119 against 122 us (16,000 rows x 256); with few rows one
+  // channel a thread has the more loads in flight: 5.5 against 7.3 us (400 x 32).
+  const bool four = max_rows * d->d >= (int64_t(1) << 20) && scan_vec(p, state_in, state_out);
   const unsigned grid = (unsigned)cdiv(max_rows * (d->d / (four ? 4 : 1)), 256);
   const auto launch = [&](auto t) {
     using T = decltype(t);

@@ -492,6 +492,19 @@ def test_scan_step(rows, pad, d, n, groups, slots, bf16):
         assert torch.equal(y, y2) and torch.equal(st[moved], out[moved])
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+def test_scan_step_many_rows(bf16):
+    """Rows times channels past 2^20: four channels a thread; an odd row stride of x, and a table of its own out."""
+    q = Layout([1] * 8200)
+    v = _scan_case(q, 128, 3, 2, True, True, True, True, bf16)
+    dims = M.scan_dims(128, 3, 2, M.BF16 if bf16 else M.F32)
+    keep, inp = _scan_inputs(q, v, dims, bf16, True)
+    st = _dev(v["table"])
+    out, y = torch.full_like(st, MARK), _marked(q.total, 128, bf16, True)
+    M.mtgnn_selective_scan_step(q.slot_, inp, dims, st, out, y)
+    _scan_check(q, v, dims, y, out, None, bf16, True)
+
+
 def test_scan_in_place_and_output_over_an_input():
     """The table read and written in one, and y over the gate, give the same bits."""
     q = Layout(LENS["ragged"], 1, 2)
