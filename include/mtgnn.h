@@ -561,9 +561,10 @@ mtgnn_status mtgnn_time_projection_bwd(const int32_t* q_node, const float* q_t, 
  * one there: slot s of a table where slot is NULL, else slot[s].  A slot outside [0, n_slots) stands for no
  * slot: the sequence starts from zeros and its last state is dropped.  Two sequences of a call must not share
  * a slot.  A sequence without rows leaves its slot as it was.  The state a call starts from is an input that is
- * not differentiated, as the memory table is not across steps.  Calls whose launches would have 2^32 threads or
- * more are refused (MTGNN_EUNSUPPORTED): a thread to each row and channel of single rows and of the convolution's
- * states, to each dB and dC, to 16 outputs of a linear layer; 16 to a row for each 64 columns of its backward. */
+ * not differentiated, as the memory table is not across steps.  Workspaces and the scan's save are 16-byte aligned.
+ * Calls whose launches would have 2^32 threads or more are refused (MTGNN_EUNSUPPORTED): a thread to each row and
+ * channel of single rows and of the convolution's states, to each dB and dC, to 16 outputs of a linear layer; 16 to
+ * a row for each 64 columns of its backward. */
 typedef enum { MTGNN_ACT_NONE = 0, MTGNN_ACT_RELU = 1, MTGNN_ACT_SILU = 2, MTGNN_ACT_GELU = 3 } mtgnn_act;
 
 typedef struct {

@@ -34,6 +34,9 @@ mtgnn_status check_seqs(const mtgnn_seqs* q, int64_t width) {
 mtgnn_status check_items(int64_t rows, int64_t width, const char* what) {
   return rows * width > (int64_t(1) << 32) - 256 ? fail(MTGNN_EUNSUPPORTED, what) : MTGNN_OK;
 }
+mtgnn_status check_aligned(const void* p, const char* what) {   // (read by whole words, by the scalar unit too)
+  return (uintptr_t)p % 16 ? fail(MTGNN_EINVAL, what) : MTGNN_OK;
+}
 bool no_rows(const mtgnn_seqs* q) { return q->max_rows == 0 || q->max_seq == 0; }
 
 #define STRIDE(ld, width, name) \
@@ -109,6 +112,7 @@ mtgnn_status mtgnn_linear(const void* x, int64_t ldx, const int32_t* n_rows, int
   const size_t need = linear_ws(d, max_rows, false);
   if (ws_bytes < need) return fail(MTGNN_EWORKSPACE, "linear ws");
   if (need) REQ(ws, "ws");
+  MTGNN_TRY(check_aligned(need ? ws : nullptr, "ws is not 16-byte aligned"));
   return linear_impl(x, ldx, n_rows, max_rows, W, b, residual, ldr, d, y, ldy, pre, ws, ws_bytes, stream);
 }
 
@@ -131,6 +135,7 @@ mtgnn_status mtgnn_linear_bwd(const float* dy, int64_t lddy, const float* pre, c
   const size_t need = linear_ws(d, max_rows, true);
   if (ws_bytes < need) return fail(MTGNN_EWORKSPACE, "linear_bwd ws");
   if (need) REQ(ws, "ws");
+  MTGNN_TRY(check_aligned(need ? ws : nullptr, "ws is not 16-byte aligned"));
   return linear_bwd_impl(dy, lddy, pre, x, ldx, n_rows, max_rows, W, d, dx, lddx, dW, db, ws, ws_bytes, stream);
 }
 
@@ -176,6 +181,7 @@ mtgnn_status mtgnn_causal_conv_bwd(const mtgnn_seqs* q, const float* dy, int64_t
   STRIDE(lddx, d->d, "lddx");
   if (ws_bytes < conv_ws(d, q->max_rows)) return fail(MTGNN_EWORKSPACE, "causal_conv_bwd ws");
   REQ(ws, "ws");
+  MTGNN_TRY(check_aligned(ws, "ws is not 16-byte aligned"));
   return conv_bwd_impl(q, dy, lddy, x, ldx, w, b, d, save, dx, lddx, dw, db, ws, stream);
 }
 
@@ -220,6 +226,8 @@ mtgnn_status mtgnn_selective_scan(const mtgnn_seqs* q, const mtgnn_scan_inputs* 
   STRIDE(ldy, d->d, "ldy");
   if (ws_bytes < scan_ws(d, q->max_rows, false)) return fail(MTGNN_EWORKSPACE, "selective_scan ws");
   REQ(ws, "ws");
+  MTGNN_TRY(check_aligned(ws, "ws is not 16-byte aligned"));
+  MTGNN_TRY(check_aligned(save, "save is not 16-byte aligned"));
   return scan_impl(q, in, d, state_in, state_out, y, ldy, save, ws, stream);
 }
 
@@ -251,6 +259,8 @@ mtgnn_status mtgnn_selective_scan_bwd(const mtgnn_seqs* q, const float* dy, int6
   MTGNN_TRY(check_items(q->max_rows, 2 * (int64_t)d->groups * d->n, "max_rows times 2 groups n >= 2^32"));
   if (ws_bytes < scan_ws(d, q->max_rows, true)) return fail(MTGNN_EWORKSPACE, "selective_scan_bwd ws");
   REQ(ws, "ws");
+  MTGNN_TRY(check_aligned(ws, "ws is not 16-byte aligned"));
+  MTGNN_TRY(check_aligned(save, "save is not 16-byte aligned"));
   return scan_bwd_impl(q, dy, lddy, in, d, save, g, ws, stream);
 }
 

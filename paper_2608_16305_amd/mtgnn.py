@@ -884,7 +884,7 @@ def scan_inputs(d: ScanDims, x, delta, A, B, C_, D=None, z=None, delta_bias=None
          _rows(C_, md, "C", R, gn), _rows(z, md, "z", R, d.d, optional=True)]
     s = ScanInputs(*[p for p, _ in r], *[ld for _, ld in r], _table(A, f32, "A", (d.n, d.d)),
                    _table(D, f32, "D", (d.d,), True), _table(delta_bias, f32, "delta_bias", (d.d,), True))
-    s.rows = R
+    s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
     return s
 
 
@@ -894,18 +894,21 @@ def scan_grads(d: ScanDims, dx, ddelta, dA, dB, dC, dD=None, dz=None, ddelta_bia
          _rows(dC, f32, "dC", R, gn), _rows(dz, f32, "dz", R, d.d, optional=True)]
     s = ScanGrads(*[p for p, _ in r], *[ld for _, ld in r], _table(dA, f32, "dA", (d.n, d.d)),
                   _table(dD, f32, "dD", (d.d,), True), _table(ddelta_bias, f32, "ddelta_bias", (d.d,), True))
-    s.rows = R
+    s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
     return s
 
 
-def _enough(what, rows, name):
+def _fit(what, d, rows, name):
+    """The tensors were checked against the dims of this call, and have its rows."""
+    if what.dims != (d.d, d.n, d.groups, d.dtype):
+        raise MtgnnError(f"{name} were made for (d, n, groups, dtype) = {what.dims}")
     if what.rows < rows:
         raise MtgnnError(f"{name} have {what.rows} rows, the sequences {rows}")
 
 
 def mtgnn_selective_scan(q: Seqs, inp: ScanInputs, d: ScanDims, state_in, state_out, y, save=None, ws=None,
                          stream=None):
-    _enough(inp, q.max_rows, "the scan's inputs")
+    _fit(inp, d, q.max_rows, "the scan's inputs")
     yp, ldy = _rows(y, _DT[d.dtype], "y", q.max_rows, d.d)
     st, f32 = (q.n_slots, d.n, d.d), torch.float32
     need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, state_in is not None)
@@ -917,8 +920,8 @@ def mtgnn_selective_scan(q: Seqs, inp: ScanInputs, d: ScanDims, state_in, state_
 
 
 def mtgnn_selective_scan_bwd(q: Seqs, dy, inp: ScanInputs, d: ScanDims, save, grads: ScanGrads, ws, stream=None):
-    _enough(inp, q.max_rows, "the scan's inputs")
-    _enough(grads, q.max_rows, "the scan's gradients")
+    _fit(inp, d, q.max_rows, "the scan's inputs")
+    _fit(grads, d, q.max_rows, "the scan's gradients")
     gp, lddy = _rows(dy, torch.float32, "dy", q.max_rows, d.d)
     need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, False)
     wp, wb = _ws(ws)
@@ -929,6 +932,7 @@ def mtgnn_selective_scan_bwd(q: Seqs, dy, inp: ScanInputs, d: ScanDims, save, gr
 def mtgnn_selective_scan_step(slot, inp: ScanInputs, d: ScanDims, state_in, state_out, y, n_rows=None, stream=None):
     """One row each: row r of the inputs is the next row of slot[r] (None: slot r)."""
     R, f32 = inp.rows, torch.float32
+    _fit(inp, d, R, "the scan's inputs")
     yp, ldy = _rows(y, _DT[d.dtype], "y", R, d.d)
     n = _n_slots(state_in, state_out)
     st = (n, d.n, d.d)

@@ -235,3 +235,35 @@ def test_launches_of_too_many_threads_are_refused():
     g = M.ScanGrads(P, P, P, P, None, 8, 8, 4, 4, 0, P, None, None)
     assert L.mtgnn_selective_scan_bwd(_q(max_rows=many), P, 8, _inp(), scan, P, C.byref(g), P, 1 << 62, None) == -2
     assert L.mtgnn_linear_bwd(P, 1, None, P, 8, None, many, P, lin, P, 8, P, P, P, 1 << 62, None) == -2
+
+
+@built
+def test_workspaces_that_are_not_aligned_are_refused():
+    L, off = M.lib(), C.c_void_p(260)
+    lin, conv, scan = M.LinearDims(8, 4, 0, 2), M.ConvDims(8, 4, 0, 2), M.ScanDims(8, 4, 1, 0, 1)
+    few = M.LinearDims(1024, 4, 0, 2)   # a sum in shares: the forward has a workspace
+    assert L.mtgnn_linear_ws_bytes(C.byref(few), 10, 0) > 0
+    assert L.mtgnn_linear(P, 1024, None, 10, P, None, None, 0, C.byref(few), P, 4, None, off, BIG, None) == -1
+    assert L.mtgnn_linear_bwd(P, 4, P, P, 8, None, 10, P, C.byref(lin), P, 8, P, None, off, BIG, None) == -1
+    assert L.mtgnn_causal_conv_bwd(_q(), P, 8, P, 8, P, None, C.byref(conv), None, P, 8, P, None, off, BIG, None) == -1
+    g = M.ScanGrads(P, P, P, P, None, 8, 8, 4, 4, 0, P, None, None)
+    for ws, save in ((off, P), (P, off)):
+        assert L.mtgnn_selective_scan(_q(), _inp(), C.byref(scan), None, None, P, 8, save, ws, BIG, None) == -1
+        assert L.mtgnn_selective_scan_bwd(_q(), P, 8, _inp(), C.byref(scan), save, C.byref(g), ws, BIG, None) == -1
+
+
+@built
+def test_inputs_of_other_dims_are_refused():
+    d, q = M.scan_dims(8, 4), M.Seqs(10, 3, 4, P, None, None)
+    inp, g = M.ScanInputs(), M.ScanGrads()
+    for other in ((16, 4, 1, M.F32), (8, 5, 1, M.F32), (8, 4, 2, M.F32), (8, 4, 1, M.BF16)):
+        inp.rows, inp.dims = 10, other
+        g.rows, g.dims = 10, other
+        for call in (lambda: M.mtgnn_selective_scan(q, inp, d, None, None, None),
+                     lambda: M.mtgnn_selective_scan_step(None, inp, d, None, None, None),
+                     lambda: M.mtgnn_selective_scan_bwd(q, None, inp, d, None, g, None)):
+            with pytest.raises(M.MtgnnError, match="made for"):
+                call()
+        inp.dims = (8, 4, 1, M.F32)
+        with pytest.raises(M.MtgnnError, match="gradients were made for"):
+            M.mtgnn_selective_scan_bwd(q, None, inp, d, None, g, None)
