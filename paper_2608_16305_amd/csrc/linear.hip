@@ -13,6 +13,11 @@
 // swizzled by the row, so that eight lanes' reads and writes of 16 bytes meet every bank once.  The matrix instruction's
 // first operand is C: a lane then holds four neighbouring columns of a row.  Tiles leave through LDS, so that
 // rows are written in 128 to 256 bytes, and the epilogue is a loop and not 64 copies of it.
+//
+// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 152, 678
+// TFLOP/s of products; weight gradient 171 + 11 for the shares; there the LDS traffic of the three parts (reads and
+// writes as long as the matrix instructions) bounds it.  Float32 8,000 x 300 -> 200: 20 us, five dependent steps of
+// 500 blocks, so latency.
 #include <algorithm>
 
 #include "bf16_split.h"
@@ -354,7 +359,10 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
 }
 
 // The same for bfloat16 operands that are contiguous along k, K a multiple of 64, where there are enough tiles of
-// 256 x 256 for the card.  Eight waves, 128 rows x 64 columns each: a matrix instruction needs 0.75 of the LDS bytes
+// 256 x 256 for the card: 326 us alone, 844 TFLOP/s, at 16,384 x 4,096 -> 2,048 with a residual (512 tiles), 452 in tiles of
+// 128; 68 against 82 us at 8,192 x 1,024 -> 2,048 with pre (256 tiles: one a CU, 96 MB written at its end).  What is
+// left: waits for LDS, whose reads take 0.75 of the cycles of the matrix instructions, and the epilogue, which no other block
+// of the CU hides.  Eight waves, 128 rows x 64 columns each: a matrix instruction needs 0.75 of the LDS bytes
 // that it needs with 64 x 64.  Rows go straight to LDS, lane l of a load to unit l % 8 of row l / 8; the units'
 // swizzle is in the address that the lane reads.  Two buffers, which are two objects, so that the compiler knows that the
 // reads of one do not wait for the loads into the other; a step's loads are a whole step's work ahead.
@@ -447,7 +455,9 @@ __global__ __launch_bounds__(256) void k_product_sum(ProdP p, const float* part,
 }
 
 // g = dy act'(pre), rows dense, and the column sums of each 16 rows (rows < n_rows; zeros without any).  A thread has V
-// columns of 4 rows, all requested before the first is used.
+// columns of 4 rows, all requested before the first is used.  Reading and writing bounds it: 33 us, 6.1 TB/s, at 8,192 x
+// 2,048.  16 rows a block: 64 leave a quarter of the blocks, 46 us there and 25 us instead of 8 at 2,399 x 100; the
+// column sums of the shares cost 12 us with 16 and 5 with 64.
 constexpr int SLOPE_ROWS = 16;
 template <int V>
 __global__ __launch_bounds__(256) void k_linear_slope(const float* dy, int64_t lddy, const float* pre,
@@ -503,7 +513,11 @@ __global__ __launch_bounds__(256) void k_linear_slope(const float* dy, int64_t l
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
 // Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64, and
-// needs two blocks a CU to hide a step's loads: with fewer than about 400 the smaller ones fill the card, and then shares of the sum (128 k or more each).
+// needs two blocks a CU to hide a step's loads; with fewer than about 400 the smaller ones fill the card better.
+// Sides of 128 against 64: 35 against 44 us at 1,092 tiles of 128, 152 against 207 at 512 (data gradients), 50
+// against 46 at 272, 36 against 20 at 126.  Long sums with few tiles (weight gradients) take 128 and share the sum:
+// 171 + 11 us against 280 (2,048 x 1,024 from 8,192 rows).  Shares have 128 k or more: 2,399 x 472 -> 100 takes 11 + 4.5 us
+// in shares of 157, 13 + 5 in shares of 67, 22 without.
 struct Plan {
   int T, split;
   int64_t tr, tc;
@@ -608,7 +622,9 @@ mtgnn_status linear_bwd_impl(const float* dy, int64_t lddy, const float* pre, co
   const int64_t ldg = direct ? lddy : n, blks = cdiv(max_rows, SLOPE_ROWS);
   if (!direct || db) {
     float *to = direct ? nullptr : gbuf, *sums = db ? part : nullptr;
-    if (n % 4 == 0 && lddy % 4 == 0 && ((uintptr_t)dy | (uintptr_t)pre | (uintptr_t)to) % 16 == 0)
+    // Four columns a thread where that leaves four blocks a CU: 33 against 37 us (8,192 x 2,048); with fewer blocks one
+    // column has the more waves: 4.7 against 8 us (2,399 x 100).
+    if (blks * cdiv(n, 256) >= 1024 && n % 4 == 0 && lddy % 4 == 0 && ((uintptr_t)dy | (uintptr_t)pre | (uintptr_t)to) % 16 == 0)
       k_linear_slope<4><<<(unsigned)(blks * cdiv(n, 256)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act, to, sums);
     else
       k_linear_slope<1><<<(unsigned)(blks * cdiv(n, 64)), 256, 0, s>>>(dy, lddy, pre, n_rows, max_rows, n, d->act, to, sums);

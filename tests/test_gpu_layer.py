@@ -82,6 +82,8 @@ LINEAR = [  # rows, extra rows behind, d_in, d_out, act, bias, residual, wide op
     # tiles of 128, and in the weight gradient long sums over rows
     (2500, 20, 70, 1300, "silu", True, True, False),
     (4200, 0, 100, 130, "none", True, False, False),
+    # many rows: the slopes four columns a thread
+    (16401, 15, 24, 20, "silu", True, False, False),
 ]
 # enough tiles of 256 for the widest kernel (an even and an odd number of its steps), whole and ragged
 LINEAR_BIG = [(3333, 40, 192, 3337, "silu", True, True, False), (3584, 0, 128, 3584, "none", False, False, False)]
