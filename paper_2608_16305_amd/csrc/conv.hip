@@ -7,7 +7,7 @@
 // the caches).  Where a sequence starts, its first W - 1 rows take the values that are missing from its slot's
 // state instead of from the rows above.  Reading and writing the rows bounds it: 32,768 rows x 2,048 in bfloat16 take
 // 75 us forward (3.6 TB/s) and 173 us backward (3.9 TB/s: x, dy in, dx out); 4,000 single rows 28 us with their
-// states in the caches.  8,000 rows x 100 of 6,000 sequences take 15 us, a chain of dependent reads (offsets, slot, state)
+// states in the caches, 38 without.  8,000 rows x 100 of 6,000 sequences take 15 us, a chain of dependent reads (offsets, slot, state)
 // in one wave a SIMD, and 4 us for the new states.
 #include <algorithm>
 #include <initializer_list>
@@ -38,7 +38,13 @@ struct ConvP {
 
 template <typename T, int V>
 __device__ __forceinline__ void get(const void* p, int64_t i, float (&v)[V]) {
-  if constexpr (V == 2 && sizeof(T) == 2) {
+  if constexpr (V == 4 && sizeof(T) == 2) {
+    const uint2 u = *(const uint2*)((const T*)p + i);
+    v[0] = lo_bf16(u.x); v[1] = hi_bf16(u.x); v[2] = lo_bf16(u.y); v[3] = hi_bf16(u.y);
+  } else if constexpr (V == 4) {
+    const float4 f = *(const float4*)((const T*)p + i);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else if constexpr (V == 2 && sizeof(T) == 2) {
     const uint32_t u = *(const uint32_t*)((const T*)p + i);
     v[0] = __uint_as_float(u << 16);
     v[1] = __uint_as_float(u & 0xffff0000u);
@@ -52,7 +58,11 @@ __device__ __forceinline__ void get(const void* p, int64_t i, float (&v)[V]) {
 }
 template <typename T, int V>
 __device__ __forceinline__ void put(void* p, int64_t i, const float (&v)[V]) {
-  if constexpr (V == 2 && sizeof(T) == 2) {
+  if constexpr (V == 4 && sizeof(T) == 2) {
+    *(uint2*)((T*)p + i) = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+  } else if constexpr (V == 4) {
+    *(float4*)((T*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+  } else if constexpr (V == 2 && sizeof(T) == 2) {
     *(uint32_t*)((T*)p + i) = cvt2_bf16(v[0], v[1]);
   } else if constexpr (V == 2) {
     *(float2*)((T*)p + i) = make_float2(v[0], v[1]);
@@ -325,23 +335,24 @@ int conv_chunk(int64_t rows, int d) {
   return (int)(cdiv(cdiv(std::max<int64_t>(rows, 1), waves), TR) * TR);
 }
 
-// Two channels a lane where every pair is aligned: forward 75 us against 124 with one, backward 173 against 168, single
-// rows 29 against 52 (32,768 and 4,000 rows x 2,048, bfloat16).
-bool pairs(const mtgnn_conv_dims* d, std::initializer_list<const void*> ps, std::initializer_list<const float*> fs,
-           std::initializer_list<int64_t> lds) {
-  const uintptr_t a = d->dtype == MTGNN_BF16 ? 4 : 8;
-  if (d->d % 2) return false;
+// Whether groups of V channels are aligned.  A lane has two where they are: forward 75 us against 124 with one (77 with
+// four), backward 173 against 168 (32,768 rows x 2,048, bfloat16).  Single rows take four channels a thread from 2^20 of
+// them on: 4,000 x 2,048 38 us against 46 with two, 52 and more with one.
+bool aligned(int V, const mtgnn_conv_dims* d, std::initializer_list<const void*> ps, std::initializer_list<const float*> fs,
+             std::initializer_list<int64_t> lds) {
+  const uintptr_t a = V * (d->dtype == MTGNN_BF16 ? 2 : 4);
+  if (d->d % V) return false;
   for (const void* p : ps)
     if ((uintptr_t)p % a) return false;
   for (const float* p : fs)
-    if ((uintptr_t)p % 8) return false;
+    if ((uintptr_t)p % (4 * V)) return false;
   for (int64_t l : lds)
-    if (l % 2) return false;
+    if (l % V) return false;
   return true;
 }
 
 template <typename F>
-void conv_variant(const mtgnn_conv_dims* d, bool two, F f) {
+void conv_variant(const mtgnn_conv_dims* d, int V, F f) {
   const auto by = [&](auto t) {
     using T = decltype(t);
     const auto wide = [&](auto v) {
@@ -350,7 +361,8 @@ void conv_variant(const mtgnn_conv_dims* d, bool two, F f) {
       else if (d->width == 3) f.template operator()<T, 3, V>();
       else f.template operator()<T, 4, V>();
     };
-    if (two) wide(std::integral_constant<int, 2>{});
+    if (V == 4) wide(std::integral_constant<int, 4>{});
+    else if (V == 2) wide(std::integral_constant<int, 2>{});
     else wide(std::integral_constant<int, 1>{});
   };
   if (d->dtype == MTGNN_BF16) by(uint16_t{});
@@ -361,7 +373,9 @@ struct LaunchConv {
   const ConvP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int W, int V> void operator()() const { k_conv<T, W, V><<<grid, 256, 0, s>>>(p); }
+  template <typename T, int W, int V> void operator()() const {
+    if constexpr (V < 4) k_conv<T, W, V><<<grid, 256, 0, s>>>(p);
+  }
 };
 struct LaunchState {
   const ConvP& p;
@@ -375,7 +389,9 @@ struct LaunchConvBack {
   const ConvP& p;
   unsigned grid;
   hipStream_t s;
-  template <typename T, int W, int V> void operator()() const { k_conv_back<T, W, V><<<grid, 256, 0, s>>>(p); }
+  template <typename T, int W, int V> void operator()() const {
+    if constexpr (V < 4) k_conv_back<T, W, V><<<grid, 256, 0, s>>>(p);
+  }
 };
 struct LaunchConvStep {
   const ConvP& p;
@@ -410,13 +426,13 @@ mtgnn_status conv_impl(const mtgnn_seqs* q, const void* x, int64_t ldx, const vo
                        void* save, hipStream_t s) {
   ConvP p = conv_params(q, x, ldx, w, b, d);
   p.st_in = state_in; p.st_out = state_out; p.save = save; p.y = y; p.ldy = ldy;
-  const bool two = pairs(d, {x, w, y, state_in}, {}, {ldx, ldy});
+  const int V = aligned(2, d, {x, w, y, state_in}, {}, {ldx, ldy}) ? 2 : 1;
   p.ch = conv_chunk(q->max_rows, d->d);
-  p.tiles = (int)cdiv(d->d, two ? 128 : 64);
-  conv_variant(d, two, LaunchConv{p, (unsigned)(cdiv(cdiv(q->max_rows, p.ch), 4) * p.tiles), s});
+  p.tiles = (int)cdiv(d->d, 64 * V);
+  conv_variant(d, V, LaunchConv{p, (unsigned)(cdiv(cdiv(q->max_rows, p.ch), 4) * p.tiles), s});
   MTGNN_CHECK_LAUNCH("conv");
   if (state_out || save) {
-    conv_variant(d, false, LaunchState{p, (unsigned)cdiv(q->max_seq * d->d, 256), s});
+    conv_variant(d, 1, LaunchState{p, (unsigned)cdiv(q->max_seq * d->d, 256), s});
     MTGNN_CHECK_LAUNCH("conv_state");
   }
   return MTGNN_OK;
@@ -427,10 +443,10 @@ mtgnn_status conv_bwd_impl(const mtgnn_seqs* q, const float* dy, int64_t lddy, c
                            int64_t lddx, float* dw, float* db, void* ws, hipStream_t s) {
   ConvP p = conv_params(q, x, ldx, w, b, d);
   p.st_in = save; p.dy = dy; p.lddy = lddy; p.dx = dx; p.lddx = lddx; p.part = (float*)ws;
-  const bool two = pairs(d, {x, w, save}, {dy, dx}, {ldx, lddy, lddx});
+  const int V = aligned(2, d, {x, w, save}, {dy, dx}, {ldx, lddy, lddx}) ? 2 : 1;
   p.ch = conv_chunk(q->max_rows, d->d);
-  p.tiles = (int)cdiv(d->d, two ? 128 : 64);
-  conv_variant(d, two, LaunchConvBack{p, (unsigned)(cdiv(cdiv(q->max_rows, p.ch), 4) * p.tiles), s});
+  p.tiles = (int)cdiv(d->d, 64 * V);
+  conv_variant(d, V, LaunchConvBack{p, (unsigned)(cdiv(cdiv(q->max_rows, p.ch), 4) * p.tiles), s});
   MTGNN_CHECK_LAUNCH("conv_back");
   const int64_t wd = (int64_t)d->width * d->d;
   k_sum_parts<<<(unsigned)cdiv(wd + d->d, 16), 256, 0, s>>>(p.q, p.ch, 0, p.part, wd + d->d, wd, dw, d->d, db, nullptr);
@@ -444,8 +460,9 @@ mtgnn_status conv_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t 
   ConvP p = conv_params(nullptr, x, ldx, w, b, d);
   p.q.slot = slot; p.q.n_slots = n_slots;
   p.st_in = state_in; p.st_out = state_out; p.y = y; p.ldy = ldy;
-  const bool two = pairs(d, {x, w, y, state_in, state_out}, {}, {ldx, ldy});
-  conv_variant(d, two, LaunchConvStep{p, n_rows, max_rows, (unsigned)cdiv(max_rows * (d->d / (two ? 2 : 1)), 256), s});
+  const auto by = [&](int V) { return aligned(V, d, {x, w, y, state_in, state_out}, {}, {ldx, ldy}); };
+  const int V = max_rows * d->d >= (int64_t(1) << 20) && by(4) ? 4 : by(2) ? 2 : 1;
+  conv_variant(d, V, LaunchConvStep{p, n_rows, max_rows, (unsigned)cdiv(max_rows * (d->d / V), 256), s});
   MTGNN_CHECK_LAUNCH("conv_step");
   return MTGNN_OK;
 }

@@ -360,6 +360,25 @@ def test_conv_step(rows, pad, d, width, slots, bf16):
         assert torch.equal(st[moved], out[0][moved]) and torch.equal(y[0], y[1])
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,width", [(300, 100, 4), (300, 101, 4), (8200, 128, 4), (8200, 132, 2), (8200, 130, 3)])
+def test_conv_step_aligned(rows, d, width, bf16):
+    """Dense rows, by one, two or four channels a thread: the bits of sequences of one row."""
+    q = Layout([1] * rows)
+    rs = _gen(8)
+    dims = M.conv_dims(d, width, M.BF16 if bf16 else M.F32, M.ACT_SILU)
+    X, Wd, bd = _dev(_vals(rs, bf16, rows, d), bf16), _dev(_vals(rs, bf16, width, d), bf16), _dev(_vals(rs, False, d))
+    st = _dev(_vals(rs, bf16, q.n_slots, width - 1, d), bf16)
+    out = [torch.full_like(st, MARK) for _ in range(2)]
+    y = [_marked(rows, d, bf16) for _ in range(2)]
+    M.mtgnn_causal_conv(q.q, X, Wd, bd, dims, st, out[0], y[0])
+    M.mtgnn_causal_conv_step(q.slot_, X, Wd, bd, dims, st, out[1], y[1])
+    assert torch.equal(y[0], y[1]) and torch.equal(out[0], out[1])
+    M.mtgnn_causal_conv_step(q.slot_, X, Wd, bd, dims, st, st, y[1])
+    moved = torch.from_numpy(q.slot[q.has]).cuda()
+    assert torch.equal(st[moved], out[0][moved]) and torch.equal(y[0], y[1])
+
+
 # --------------------------------------------------------------------------- scan
 
 SCAN = [  # lens, lead, pad, extra, slots, d, n, groups, gate, skip, bias, softplus, wide
