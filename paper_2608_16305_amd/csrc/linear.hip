@@ -55,23 +55,27 @@ struct ProdP {
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef words4 words4_at4 __attribute__((aligned(4)));
 typedef words4 words4_at2 __attribute__((aligned(2)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+typedef words2 words2_at4 __attribute__((aligned(4)));
+typedef uint32_t word_at2 __attribute__((aligned(2)));
 
-// One operand's share of a tile in a thread's registers: U units of eight k.
+// One operand's share of a tile in a thread's registers: U units of eight k.  Where rows are contiguous across k, a thread's
+// units are of two neighbouring rows, whose values at one k come by one load.
 template <bool F32, bool KC, int T, int KS>
 struct Stage {
   static constexpr int U = T * KS / 8 / NT, CH = KS / 8, PL = F32 ? 3 : 1;
-  static_assert(U >= 1, "a unit per thread");
+  static_assert(U >= 1 && (KC || U % 2 == 0), "a unit, or two rows of them, per thread");
   uint32_t v[U][F32 ? 8 : 4];
   __device__ __forceinline__ static int row(int u) {
-    const int id = u * NT + threadIdx.x;
-    return KC ? id / CH : id % T;
+    const int id = u * NT + threadIdx.x, pair = u / 2 * NT + threadIdx.x;
+    return KC ? id / CH : pair % (T / 2) * 2 + u % 2;
   }
   __device__ __forceinline__ static int chunk(int u) {
-    const int id = u * NT + threadIdx.x;
-    return KC ? id % CH : id / T;
+    const int id = u * NT + threadIdx.x, pair = u / 2 * NT + threadIdx.x;
+    return KC ? id % CH : pair / (T / 2);
   }
   using E = std::conditional_t<F32, uint32_t, uint16_t>;
-  const E* q[U];   // of each unit: its row at the step's first k
+  const E* q[U];   // of each unit: its row at k = 0
   int64_t ld;
   // rows r0 .. of the operand (the last one stands for those past it)
   __device__ __forceinline__ void at_rows(const void* p, int64_t ld_, int64_t rows, int64_t r0) {
@@ -84,34 +88,60 @@ struct Stage {
   }
   // k0 .. k0 + KS - 1 (zeros from K on)
   __device__ __forceinline__ void load(int64_t k0, int64_t K) {
+    if constexpr (KC) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + chunk(u) * 8;
-      uint32_t e[8];
-      if ((KC ? k + 8 : k0 + KS) <= K) {
-        if constexpr (KC && F32) {
+      for (int u = 0; u < U; ++u) {
+        const int64_t k = k0 + chunk(u) * 8;
+        if (k + 8 > K) {
+          load_each(u, k, K);
+        } else if constexpr (F32) {
           const words4_at4* w = (const words4_at4*)(q[u] + k);
           const words4 a = w[0], b = w[1];
           v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
           v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
-        } else if constexpr (KC) {
+        } else {
           const words4 a = *(const words4_at2*)(q[u] + k);
           v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; u += 2) {
+        const int64_t k = k0 + chunk(u) * 8;
+        if (k0 + KS > K || q[u] == q[u + 1]) {   // (the last row is both where the row behind it does not exist)
+          load_each(u, k, K);
+          load_each(u + 1, k, K);
+          continue;
+        }
+        const E* w = q[u] + k * ld;
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const words2 a = *(const words2_at4*)(w + i * ld);
+            v[u][i] = a.x;
+            v[u + 1][i] = a.y;
+          }
         } else {
-          const E* w = q[u] + k * ld;
+          uint32_t e[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) e[i] = w[i * ld];
-          put(u, e, 0, 8);
-        }
-      } else {
+          for (int i = 0; i < 8; ++i) e[i] = *(const word_at2*)(w + i * ld);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int64_t at = min(k + i, K - 1);
-          e[i] = q[u][KC ? at : at * ld];
+          for (int i = 0; i < 4; ++i) {
+            v[u][i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x05040100);
+            v[u + 1][i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x07060302);
+          }
         }
-        put(u, e, k, K);
       }
     }
+  }
+  __device__ __forceinline__ void load_each(int u, int64_t k, int64_t K) {
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t at = min(k + i, K - 1);
+      e[i] = q[u][KC ? at : at * ld];
+    }
+    put(u, e, k, K);
   }
   __device__ __forceinline__ void put(int u, const uint32_t (&e)[8], int64_t k, int64_t K) {
 #pragma unroll
@@ -141,10 +171,11 @@ struct Stage {
       }
     }
   }
+  // The swizzle: eight rows in turn, and eight even ones, meet every bank once.
+  __device__ __forceinline__ static int turn(int r) { return CH == 4 ? (r >> 1 & 3) ^ (r >> 3 & 1) : (r & 7) ^ (r >> 3 & 1); }
   // Word of unit c of row r in a plane.
   __device__ __forceinline__ static int at(int r, int c) {
-    const int s = CH == 4 ? c ^ (r >> 1 & 3) : c ^ (r & 7);
-    return r * (KS / 2) + s * 4;
+    return r * (KS / 2) + (c ^ turn(r)) * 4;
   }
   __device__ __forceinline__ static bf16x8_t frag(const uint32_t* src, int plane, int r, int c) {
     return __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + plane * (T * KS / 2) + at(r, c)));
@@ -379,10 +410,11 @@ __global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = (wid >> 2) * 128, wc = (wid & 3) * 64, fr = lane & 15, fg = lane >> 4;
   // this wave's loads: rows 32 wid + 8 i + lane / 8 of each operand
+  using S = Stage<false, true, BIG, BIG_KS>;
   const uint16_t* src[2][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int row = 32 * wid + 8 * i + (lane >> 3), unit = (lane & 7) ^ (row & 7);
+    const int row = 32 * wid + 8 * i + (lane >> 3), unit = (lane & 7) ^ S::turn(row);
     src[0][i] = (const uint16_t*)p.R + min(r0 + row, rows - 1) * p.ldR + 8 * unit;
     src[1][i] = (const uint16_t*)p.C + min(c0 + row, p.cols - 1) * p.ldC + 8 * unit;
   }
@@ -400,7 +432,6 @@ __global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
   for (int i = 0; i < WR; ++i)
 #pragma unroll
     for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  using S = Stage<false, true, BIG, BIG_KS>;
   const auto multiply = [&](const uint32_t* buf) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
