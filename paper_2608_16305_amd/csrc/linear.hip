@@ -171,8 +171,11 @@ struct Stage {
       }
     }
   }
-  // The swizzle: eight rows in turn, and eight even ones, meet every bank once.
-  __device__ __forceinline__ static int turn(int r) { return CH == 4 ? (r >> 1 & 3) ^ (r >> 3 & 1) : (r & 7) ^ (r >> 3 & 1); }
+  // The swizzle: eight rows in turn meet every bank once, and eight even ones where units are stored by pairs of rows.
+  __device__ __forceinline__ static int turn(int r) {
+    const int t = CH == 4 ? r >> 1 & 3 : r & 7;
+    return KC ? t : t ^ (r >> 3 & 1);
+  }
   // Word of unit c of row r in a plane.
   __device__ __forceinline__ static int at(int r, int c) {
     return r * (KS / 2) + (c ^ turn(r)) * 4;
