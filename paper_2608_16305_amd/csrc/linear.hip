@@ -14,8 +14,8 @@
 // first operand is C: a lane then holds four neighbouring columns of a row.  Tiles leave through LDS, so that
 // rows are written in 128 to 256 bytes, and the epilogue is a loop and not 64 copies of it.
 //
-// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 152, 678
-// TFLOP/s of products; weight gradient 171 + 11 for the shares; there the LDS traffic of the three parts (reads and
+// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 135, 763
+// TFLOP/s of products; weight gradient 145 + 11 for the shares; there the LDS traffic of the three parts (reads and
 // writes as long as the matrix instructions) bounds it.  Float32 8,000 x 300 -> 200: 20 us, five dependent steps of
 // 500 blocks, so latency.
 #include <algorithm>
@@ -60,19 +60,22 @@ typedef words2 words2_at4 __attribute__((aligned(4)));
 typedef uint32_t word_at2 __attribute__((aligned(2)));
 
 // One operand's share of a tile in a thread's registers: U units of eight k.  Where rows are contiguous across k, a thread's
-// units are of two neighbouring rows, whose values at one k come by one load.
+// units are of two neighbouring rows, whose values at one k come by one load: weight gradient 145 us against 172 (8,192
+// rows, 2,048 x 1,024, tiles of 128).  Not of float32 in tiles of 64, where half a wave's 256 bytes are a row's already: 51
+// against 54 us with pairs (1,968 rows, 445 x 2,101).
 template <bool F32, bool KC, int T, int KS>
 struct Stage {
   static constexpr int U = T * KS / 8 / NT, CH = KS / 8, PL = F32 ? 3 : 1;
-  static_assert(U >= 1 && (KC || U % 2 == 0), "a unit, or two rows of them, per thread");
+  static constexpr bool PAIR = !KC && (T == 128 || !F32);
+  static_assert(U >= 1 && (!PAIR || U % 2 == 0), "a unit, or two rows of them, per thread");
   uint32_t v[U][F32 ? 8 : 4];
   __device__ __forceinline__ static int row(int u) {
     const int id = u * NT + threadIdx.x, pair = u / 2 * NT + threadIdx.x;
-    return KC ? id / CH : pair % (T / 2) * 2 + u % 2;
+    return KC ? id / CH : PAIR ? pair % (T / 2) * 2 + u % 2 : id % T;
   }
   __device__ __forceinline__ static int chunk(int u) {
     const int id = u * NT + threadIdx.x, pair = u / 2 * NT + threadIdx.x;
-    return KC ? id % CH : pair / (T / 2);
+    return KC ? id % CH : PAIR ? pair / (T / 2) : id / T;
   }
   using E = std::conditional_t<F32, uint32_t, uint16_t>;
   const E* q[U];   // of each unit: its row at k = 0
@@ -103,6 +106,20 @@ struct Stage {
           const words4 a = *(const words4_at2*)(q[u] + k);
           v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w;
         }
+      }
+    } else if constexpr (!PAIR) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t k = k0 + chunk(u) * 8;
+        if (k0 + KS > K) {
+          load_each(u, k, K);
+          continue;
+        }
+        const E* w = q[u] + k * ld;
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = w[i * ld];
+        put(u, e, 0, 8);
       }
     } else {
 #pragma unroll
@@ -174,7 +191,7 @@ struct Stage {
   // The swizzle: eight rows in turn meet every bank once, and eight even ones where units are stored by pairs of rows.
   __device__ __forceinline__ static int turn(int r) {
     const int t = CH == 4 ? r >> 1 & 3 : r & 7;
-    return KC ? t : t ^ (r >> 3 & 1);
+    return PAIR ? t ^ (r >> 3 & 1) : t;
   }
   // Word of unit c of row r in a plane.
   __device__ __forceinline__ static int at(int r, int c) {
@@ -548,9 +565,9 @@ size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
 // Tile side and blocks per tile's sum.  A tile of 128 takes half the operand traffic per product of one of 64, and
 // needs two blocks a CU to hide a step's loads; with fewer than about 400 the smaller ones fill the card better.
-// Sides of 128 against 64: 35 against 44 us at 1,092 tiles of 128, 152 against 207 at 512 (data gradients), 50
+// Sides of 128 against 64: 35 against 44 us at 1,092 tiles of 128, 147 against 207 at 512 (data gradients), 50
 // against 46 at 272, 36 against 20 at 126.  Long sums with few tiles (weight gradients) take 128 and share the sum:
-// 171 + 11 us against 280 (2,048 x 1,024 from 8,192 rows).  Shares have 128 k or more: 2,399 x 472 -> 100 takes 11 + 4.5 us
+// 170 + 11 us against 280 (2,048 x 1,024 from 8,192 rows).  Shares have 128 k or more: 2,399 x 472 -> 100 takes 11 + 4.5 us
 // in shares of 157, 13 + 5 in shares of 67, 22 without.
 struct Plan {
   int T, split;
