@@ -14,7 +14,7 @@
 // first operand is C: a lane then holds four neighbouring columns of a row.  Tiles leave through LDS, so that
 // rows are written in 128 to 256 bytes, and the epilogue is a loop and not 64 copies of it.
 //
-// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 135, 763
+// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 138, 747
 // TFLOP/s of products; weight gradient 145 + 11 for the shares; there the LDS traffic of the three parts (reads and
 // writes as long as the matrix instructions) bounds it.  Float32 8,000 x 300 -> 200: 20 us, five dependent steps of
 // 500 blocks, so latency.
