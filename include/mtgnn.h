@@ -639,9 +639,9 @@ mtgnn_status mtgnn_causal_conv_step(const int32_t* slot, const int32_t* n_rows, 
  *   dt_t = softplus(delta_t + delta_bias)   (softplus 0 in the dims: delta_t + delta_bias),
  *   h_t[i] = exp(dt_t A[i]) h_(t-1)[i] + dt_t B_t[i] x_t,
  *   y_t = (sum_i C_t[i] h_t[i] + D x_t) silu(z_t),
- * h before the sequence's first row being its slot's state.  n <= 64; groups divides d.  dt_t A[i] is a decay (A <= 0
- * with softplus): rows are worked on in pieces that meet by exp(A[i] sum of dt over a piece), which a growth over
- * some hundred rows takes past float32.
+ * h before the sequence's first row being its slot's state.  n <= 64; groups divides d.  Rows are worked on in pieces that
+ * meet by exp(A[i] sum of dt over a piece).  States may grow (dt_t A[i] > 0) as far as float32 holds them, and what such
+ * an exponential leaves uncertain grows with its exponent: about 2^-24 of it times |A[i] sum of dt|.
  *   x, delta, z (or NULL: no gate), y -- [max_rows, d] (dtype); y may be x, delta or z (same stride) where no
  *           backward follows, and may not overlap them otherwise;
  *   B, C -- [max_rows, groups * n] (dtype), each group's n columns together;

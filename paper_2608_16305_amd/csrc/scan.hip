@@ -412,6 +412,18 @@ __global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
   if (me.mine && me.wave == 0) p.sumdt[(int64_t)c * p.d + me.col0 + me.col] = sum;
 }
 
+// own + 2^s h.  The power's whole part goes to h's exponent: past float32's range it still meets a small h as it would row
+// after row, and a zero one stays zero (an infinite decay times zero is NaN).  Past +-1000 s is as at it, since h spans
+// 2^277; an infinite s is what an infinite step makes, and stays one.
+__device__ __forceinline__ float carried(float s, float h, float own) {
+  float i = 0.f;
+  if (fabsf(s) < INFINITY) {
+    s = fminf(fmaxf(s, -1000.f), 1000.f);
+    i = floorf(s);
+  }
+  return fmaf(__builtin_amdgcn_exp2f(s - i), ldexpf(h, (int)i), own);
+}
+
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
 // first.  A block has 1024 / RUNS states and channels; each of RUNS threads to one takes a run of chunks, once for
 // what the run hands on, h -> own + decay h, and, after a scan over the runs, once with what enters it.  (One
@@ -420,7 +432,9 @@ __global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
 template <int RUNS>
 __global__ __launch_bounds__(1024) void k_scan_carry(ScanP p, int back) {
   constexpr int RUN_COLS = 1024 / RUNS;
-  __shared__ float s_h[RUNS][RUN_COLS + 1], s_d[RUNS][RUN_COLS + 1];   // a decay of -1: nothing passes
+  // s_t: the sum of dt over a run, whose decay what enters the run passes with.  NaN: nothing passes (a NaN of the inputs'
+  // own: nothing that matters, since the run's state is NaN then).
+  __shared__ float s_h[RUNS][RUN_COLS + 1], s_t[RUNS][RUN_COLS + 1];
   const int64_t nd = (int64_t)p.n * p.d;
   const int j = threadIdx.x % RUN_COLS, run = threadIdx.x / RUN_COLS;
   const int64_t i = min((int64_t)blockIdx.x * RUN_COLS + j, nd - 1);
@@ -428,7 +442,7 @@ __global__ __launch_bounds__(1024) void k_scan_carry(ScanP p, int back) {
   const int ch = (int)(i % p.d);
   const float A2 = p.A[i] * LOG2E;
   const int len = (p.nchunk + RUNS - 1) / RUNS, k0 = run * len, k1 = min(p.nchunk, k0 + len);
-  const auto walk = [&](float& h, float& d, bool write) {
+  const auto walk = [&](float& h, float& t, bool write) {
     constexpr int U = 8;
     for (int k = k0; k < k1; k += U) {
       float e[U], sd[U];
@@ -445,28 +459,28 @@ __global__ __launch_bounds__(1024) void k_scan_carry(ScanP p, int back) {
         if (k + u >= k1) break;
         const int c = back ? p.nchunk - 1 - (k + u) : k + u;
         if (write && mine) p.E[c * nd + i] = h;
-        const float a = __builtin_amdgcn_exp2f(A2 * sd[u]), next = fmaf(a, h, e[u]);
+        const float next = carried(A2 * sd[u], h, e[u]);
         h = f[u] == CARRY_ADD ? next : f[u] == CARRY_OWN ? e[u] : 0.f;
-        d = f[u] == CARRY_ADD && d >= 0.f ? d * a : -1.f;
+        t = f[u] == CARRY_ADD ? t + sd[u] : NAN;
       }
     }
   };
-  float h = 0.f, d = 1.f;
-  walk(h, d, false);
+  float h = 0.f, t = 0.f;
+  walk(h, t, false);
   s_h[run][j] = h;
-  s_d[run][j] = d;
+  s_t[run][j] = t;
   __syncthreads();
   for (int o = 1; o < RUNS; o <<= 1) {
-    const float ph = run >= o ? s_h[run - o][j] : 0.f, pd = run >= o ? s_d[run - o][j] : 1.f;
+    const float ph = run >= o ? s_h[run - o][j] : 0.f, pt = run >= o ? s_t[run - o][j] : 0.f;
     __syncthreads();
-    h = d < 0.f ? h : fmaf(d, ph, h);
-    d = d < 0.f || pd < 0.f ? -1.f : d * pd;
+    h = t == t ? carried(A2 * t, ph, h) : h;
+    t += pt;
     s_h[run][j] = h;
-    s_d[run][j] = d;
+    s_t[run][j] = t;
     __syncthreads();
   }
   h = run > 0 ? s_h[run - 1][j] : 0.f;
-  walk(h, d, true);
+  walk(h, t, true);
 }
 
 template <typename T, int N, int NW, bool SC>

@@ -824,3 +824,43 @@ def test_binding_refusals():
         small = M.alloc_bytes(M.selective_scan_save_bytes(ds, 5, 2, False))
         M.mtgnn_selective_scan(M.seqs(off, 5, n_slots=2), inp, ds, torch.zeros(2, 4, 8, device="cuda"), None, x, save=small,
                                ws=ws)
+
+
+# --------------------------------------------------------------------------- chunks: what one hands to the next
+
+@pytest.mark.parametrize("d", [20, 1024], ids=["64 runs", "16 runs"])
+@pytest.mark.parametrize("grown_by", ["A", "dt"])
+@pytest.mark.parametrize("way", ["forward", "backward"])
+def test_scan_of_states_that_grow(way, grown_by, d):
+    """Growth past float32 over the second half of the rows, in the way's order, meets a zero state (flow), or one small
+    enough for the product to be finite: what row after row gives.
+
+    Every second state grows, by e^84 to e^120 over those 1,200 rows: from 1e-30 to some 1e22, or from the 400 last rows' own
+    values, by e^40.  A chunk's exponent adds to the tolerance of the rows what its sum of dt is off, at most 16 rows, 11
+    chunks of a run and 6 steps over the runs, so 33 u of an exponent of 120: 4,000 u, next to 3 u for each of the
+    2,600 rows; both are within the 8 T u = 20,800 u of the rows."""
+    rows, n = 2600, 4
+    q = Layout([rows, 40])
+    rs = _gen(21)
+    v = _scan_case(q, d, n, 1, True, True, False, False, False)
+    sign = np.where(np.arange(n) % 2, 1.0, -1.0)[:, None]
+    v["A"] = ((0.7 + 0.3 * rs.rand(n, d)) * sign * (1 if grown_by == "A" else -1)).astype(np.float32)
+    dt = np.full((q.rows, d), 1e-3, np.float32)
+    v["x"][:rows] = 0.0
+    v["dy"][:rows] = 0.0
+    v["table"][q.slot[0]] = 0.0
+    some = slice(0, d // 2)                       # these channels start from a state (flow) of 1e-30, the others from none
+    if way == "forward":
+        dt[rows - 1200:rows] = 0.1
+        v["x"][rows - 400:rows] = rs.randn(400, d)
+        v["dy"][:400] = rs.randn(400, d)
+        v["table"][q.slot[0], :, some] = 1e-30
+    else:
+        dt[:1200] = 0.1
+        v["x"][1200:1600] = rs.randn(400, d)      # behind the growth, which float32 would not hold
+        v["dy"][:400] = rs.randn(400, d)
+        v["dy"][rows - 200:rows, some] = 1e-30 * rs.randn(200, d // 2)
+    v["delta"] = dt if grown_by == "A" else -dt
+    dims = M.scan_dims(d, n, 1, M.F32, False)
+    y, st, g, _ = _scan_run(q, v, dims, False, True, False)
+    _scan_check(q, v, dims, y, st, g, False, True)
