@@ -521,7 +521,7 @@ __global__ __launch_bounds__(64 * NW) void k_scan_out(ScanP p) {
     const auto part = [&](int i, int k, const typename S::Raw& rb, const typename S::Raw& rc) {   // z[i] becomes y
       const float dt = u[i], dx = dt * x[i];
       if (k == 0) {
-        y[0] = NW > 1 && me.wave ? 0.f : D * x[i];
+        y[0] = p.D && (NW == 1 || me.wave == 0) ? D * x[i] : 0.f;   // (no skip: not 0 times an x that may be infinite)
         y[1] = 0.f;
       }
       float b[S::M], cc[S::M];
@@ -730,9 +730,10 @@ __global__ __launch_bounds__(64 * NB, 2) void k_scan_back(ScanP p, ScanG o) {
       const float x = s_x[i][me.lane], e = s_e[i][me.lane];
       const float du = fmaf(sx, x, su * LN2) * s_s[i][me.lane];
       if (mine) {
-        (o.dx + t * o.lddx + me.ch0)[col] = fmaf(D, e, sx * s_dt[i][me.lane]);
+        const float dxr = sx * s_dt[i][me.lane];
+        (o.dx + t * o.lddx + me.ch0)[col] = p.D ? fmaf(D, e, dxr) : dxr;
         (o.ddelta + t * o.lddd + me.ch0)[col] = du;
-        if (p.z) (o.dz + t * o.lddz + me.ch0)[col] = s_z[i][me.lane] * fmaf(D, x, y);
+        if (p.z) (o.dz + t * o.lddz + me.ch0)[col] = s_z[i][me.lane] * (p.D ? fmaf(D, x, y) : y);
       }
       dD = fmaf(e, x, dD);
       db += du;

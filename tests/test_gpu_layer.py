@@ -559,6 +559,71 @@ def test_scan_values_at_the_ends():
     assert np.array_equal(got[~hit], clean[~hit]) and np.isnan(got[22:25, 7]).all()
 
 
+def _ends(name, got, want, tol, bf16=False):
+    """NaN and infinities where the oracle has them, and no others; the rest close to it."""
+    got = _np(got)
+    fin = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), (name, np.argwhere(np.isnan(got) != np.isnan(want))[:4].tolist())
+    assert np.array_equal(got[~fin & ~np.isnan(want)], want[~fin & ~np.isnan(want)]), name
+    _close(name, got[fin], want[fin], tol[fin], bf16)
+
+
+def _ends_case(n, skip, bf16, seed=17):
+    """Infinite inputs: x in channel 9, a step in channel 30, an output gradient in channel 50, x in the second tile of
+    channels.  Positive B, C and gate, so that few infinities are met by one of the other sign; decays that float32 does
+    not round to zero (at least e^-5: steps below 3.5, A above -1.5), which would make NaN of an infinite state."""
+    q = Layout([20, 30, 11])
+    q.slot[:], q.has[:] = np.arange(3), True
+    q.slot_.copy_(torch.arange(3, dtype=torch.int32))
+    d = 70
+    v = _scan_case(q, d, n, 1, True, skip, False, True, bf16, seed)
+    for k in ("B", "C", "z"):
+        v[k] = np.abs(v[k]) + np.float32(0.125)
+        v[k] = round_bf16(v[k]) if bf16 else v[k]
+    v["A"] = -(0.1 + 1.4 * _gen(seed).rand(n, d)).astype(np.float32)
+    v["x"][21, 9] = np.inf
+    v["delta"][33, 30] = np.inf
+    v["dy"][40, 50] = -np.inf
+    v["x"][5, 68] = -np.inf
+    return q, v, M.scan_dims(d, n, 1, M.BF16 if bf16 else M.F32)
+
+
+def _check_ends(q, v, dims, bf16, skip):
+    args = [v[k] for k in ("x", "delta", "A", "B", "C", "D", "z", "bias")]
+    kw = dict(first=q.first(v["table"]), dy=v["dy"])
+    with np.errstate(invalid="ignore", over="ignore"):
+        want, mag = layer.scan(q.lens, *args, **kw), layer.scan(q.lens, *args, magnitude=True, **kw)
+    y, st, g, (_, st_in, _) = _scan_run(q, v, dims, bf16, True, False)
+    k = (64 + 8 * max(q.lens)) * U
+    _ends("y", y, want["y"], k * mag["y"], bf16)
+    last = np.arange(len(q.lens))[q.has]
+    _ends("state", st[q.slot[q.has]], want["state"][last], k * mag["state"][last])
+    for name in ("dx", "ddelta", "dB", "dC", "dz", "dA") + (("dD",) if skip else ()):
+        _ends(name, g[name], want[name], (k + (dims.d + q.rows) * U) * mag[name])
+    # row by row through the single-row form: its rows are the sequences' rows
+    ys, table = torch.zeros_like(y), st_in.clone()
+    off = np.concatenate([[0], np.cumsum(q.lens)])
+    for t in range(max(q.lens)):
+        live = [i for i in range(len(q.lens)) if q.lens[i] > t]
+        at = [int(off[i]) + t for i in live]
+        w = dict(v, **{f: v[f][at] for f in ("x", "delta", "B", "C", "z")})
+        one = Layout([1] * len(live))
+        keep, inp = _scan_inputs(one, w, dims, bf16, False)
+        out = _marked(len(live), dims.d, bf16)
+        M.mtgnn_selective_scan_step(torch.tensor(q.slot[live].astype(np.int32)).cuda(), inp, dims, table, table, out)
+        ys[at] = out
+    _ends("y by rows", ys, want["y"], k * mag["y"], bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 16, 32, 64])
+@pytest.mark.parametrize("skip", [False, True], ids=["no skip", "skip"])
+def test_scan_of_infinite_inputs(skip, n, bf16):
+    """Infinite inputs give what row after row gives, with and without D: an absent one is no factor of 0."""
+    q, v, dims = _ends_case(n, skip, bf16)
+    _check_ends(q, v, dims, bf16, skip)
+
+
 # --------------------------------------------------------------------------- as a layer
 
 def _layer(seed=11, bf16=False, d_msg=36, d=40, n=16, width=4):
