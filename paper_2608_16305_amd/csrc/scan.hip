@@ -413,15 +413,11 @@ __global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
 }
 
 // own + 2^s h.  The power's whole part goes to h's exponent: past float32's range it still meets a small h as it would row
-// after row, and a zero one stays zero (an infinite decay times zero is NaN).  Past +-1000 s is as at it, since h spans
-// 2^277; an infinite s is what an infinite step makes, and stays one.
+// after row, and a zero one stays zero (an infinite decay times zero is NaN).  h spans 2^277, so s past +-1000 is as at
+// it; where s is NaN own is too.  1 us of k_scan_carry's 14 against a product with exp2(s).
 __device__ __forceinline__ float carried(float s, float h, float own) {
-  float i = 0.f;
-  if (fabsf(s) < INFINITY) {
-    s = fminf(fmaxf(s, -1000.f), 1000.f);
-    i = floorf(s);
-  }
-  return fmaf(__builtin_amdgcn_exp2f(s - i), ldexpf(h, (int)i), own);
+  s = __builtin_amdgcn_fmed3f(s, -1000.f, 1000.f);
+  return fmaf(__builtin_amdgcn_exp2f(__builtin_amdgcn_fractf(s)), ldexpf(h, (int)floorf(s)), own);
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the
