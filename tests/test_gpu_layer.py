@@ -624,6 +624,14 @@ def test_scan_of_infinite_inputs(skip, n, bf16):
     _check_ends(q, v, dims, bf16, skip)
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 5, 12, 15, 17, 24, 33, 47, 50])
+def test_scan_of_infinite_inputs_with_fewer_states(n, bf16):
+    """The same with numbers of states that no kernel has as its own: what is past the last takes no part."""
+    q, v, dims = _ends_case(n, n % 2 == 0, bf16)
+    _check_ends(q, v, dims, bf16, n % 2 == 0)
+
+
 # --------------------------------------------------------------------------- as a layer
 
 def _layer(seed=11, bf16=False, d_msg=36, d=40, n=16, width=4):
