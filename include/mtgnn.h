@@ -595,7 +595,8 @@ mtgnn_status mtgnn_linear(const void* x, int64_t ldx, const int32_t* n_rows, int
 /* Backward of mtgnn_linear for dy [max_rows, d_out] float32 (also the residual's gradient): with
  * g = dy act'(pre), dx = g W [max_rows, d_in] (or NULL), dW = g^T x [d_out, d_in], db = sum of g [d_out]
  * (or NULL), each over the rows below n_rows; dW and db are overwritten (zero without rows).
- *   pre -- the forward call's; may be NULL where act is none.
+ *   pre -- the forward call's; may be NULL where act is none;
+ *   dx -- may not overlap x, nor dy where act is none (EINVAL); with an activation it may be in dy's place.
  * Sums over rows run in a fixed order (deterministic).  Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 1). */
 mtgnn_status mtgnn_linear_bwd(const float* dy, int64_t lddy, const float* pre, const void* x, int64_t ldx,
                               const int32_t* n_rows, int64_t max_rows, const void* W, const mtgnn_linear_dims* dims,
@@ -621,6 +622,7 @@ mtgnn_status mtgnn_causal_conv(const mtgnn_seqs* seqs, const void* x, int64_t ld
 /* Backward of mtgnn_causal_conv for dy [max_rows, d] float32: with g_t = dy_t act'(pre_t) (pre is computed again),
  *   dx_t = sum_j w[j] g_(t + width - 1 - j) over the sequence's rows,  dw[j] = sum_t g_t x_(t - width + 1 + j),
  *   db = sum_t g_t (or NULL);  dw, db overwritten.  save: the forward's (NULL: the sequences started from zeros).
+ * dx may not overlap dy or x (EINVAL).
  * Deterministic.  Workspace: mtgnn_causal_conv_ws_bytes(dims, max_rows). */
 size_t mtgnn_causal_conv_ws_bytes(const mtgnn_conv_dims* dims, int64_t max_rows);
 mtgnn_status mtgnn_causal_conv_bwd(const mtgnn_seqs* seqs, const float* dy, int64_t lddy, const void* x, int64_t ldx,
@@ -666,7 +668,8 @@ mtgnn_status mtgnn_selective_scan(const mtgnn_seqs* seqs, const mtgnn_scan_input
 
 /* Backward of mtgnn_selective_scan for dy [max_rows, d] float32, with the forward's inputs and save.
  *   dx, ddelta, dz [max_rows, d] (dz NULL iff z is), dB, dC [max_rows, groups * n], all float32 with row strides:
- *           rows of the sequences are overwritten, others left untouched;
+ *           rows of the sequences are overwritten, others left untouched.  One of dx, ddelta and dz may be in dy's
+ *           place (same stride); otherwise they may not overlap dy, the inputs or one another;
  *   dA [n, d], dD [d] (NULL iff D is), ddelta_bias [d] (NULL iff delta_bias is): overwritten.
  * Deterministic (sums over channels and rows in a fixed order).
  * Workspace: mtgnn_selective_scan_ws_bytes(dims, max_rows, max_seq, 1). */

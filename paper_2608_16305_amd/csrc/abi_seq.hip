@@ -37,6 +37,21 @@ mtgnn_status check_items(int64_t rows, int64_t width, const char* what) {
 mtgnn_status check_aligned(const void* p, const char* what) {   // (read by whole words, by the scalar unit too)
   return (uintptr_t)p % 16 ? fail(MTGNN_EINVAL, what) : MTGNN_OK;
 }
+// A matrix of rows in memory, in bytes.
+struct Rows {
+  const void* p;
+  int64_t ld, width;
+};
+// Whether two of `rows` rows share a byte.  Exact where their rows are as far apart (column ranges of one matrix may lie side
+// by side); else whether the memory from the first row to the last does.
+bool overlap(const Rows& a, const Rows& b, int64_t rows) {
+  const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+  if (!a.p || !b.p || d >= (rows - 1) * a.ld + a.width || -d >= (rows - 1) * b.ld + b.width) return false;
+  if (a.ld != b.ld) return true;
+  const int64_t c = (d % a.ld + a.ld) % a.ld;   // b's first column, seen from a's
+  return c < a.width || c + b.width > a.ld;
+}
+int64_t bytes_of(int dtype) { return dtype == MTGNN_BF16 ? 2 : 4; }
 bool no_rows(const mtgnn_seqs* q) { return q->max_rows == 0 || q->max_seq == 0; }
 
 #define STRIDE(ld, width, name) \
@@ -136,6 +151,12 @@ mtgnn_status mtgnn_linear_bwd(const float* dy, int64_t lddy, const float* pre, c
   if (ws_bytes < need) return fail(MTGNN_EWORKSPACE, "linear_bwd ws");
   if (need) REQ(ws, "ws");
   MTGNN_TRY(check_aligned(need ? ws : nullptr, "ws is not 16-byte aligned"));
+  // dW is made from x, and from dy where that is the slope, after dx is written
+  const int64_t e = bytes_of(d->dtype);
+  const Rows to{dx, lddx * 4, (int64_t)d->d_in * 4};
+  if (overlap(to, Rows{x, ldx * e, d->d_in * e}, max_rows)) return fail(MTGNN_EINVAL, "dx overlaps x");
+  if (d->act == MTGNN_ACT_NONE && overlap(to, Rows{dy, lddy * 4, (int64_t)d->d_out * 4}, max_rows))
+    return fail(MTGNN_EINVAL, "dx overlaps dy (without an activation)");
   return linear_bwd_impl(dy, lddy, pre, x, ldx, n_rows, max_rows, W, d, dx, lddx, dW, db, ws, ws_bytes, stream);
 }
 
@@ -182,6 +203,11 @@ mtgnn_status mtgnn_causal_conv_bwd(const mtgnn_seqs* q, const float* dy, int64_t
   if (ws_bytes < conv_ws(d, q->max_rows)) return fail(MTGNN_EWORKSPACE, "causal_conv_bwd ws");
   REQ(ws, "ws");
   MTGNN_TRY(check_aligned(ws, "ws is not 16-byte aligned"));
+  // a chunk reads rows of its neighbours, which may have written their dx by then
+  const int64_t e = bytes_of(d->dtype), w4 = (int64_t)d->d * 4;
+  const Rows to{dx, lddx * 4, w4};
+  if (overlap(to, Rows{dy, lddy * 4, w4}, q->max_rows)) return fail(MTGNN_EINVAL, "dx overlaps dy");
+  if (overlap(to, Rows{x, ldx * e, d->d * e}, q->max_rows)) return fail(MTGNN_EINVAL, "dx overlaps x");
   return conv_bwd_impl(q, dy, lddy, x, ldx, w, b, d, save, dx, lddx, dw, db, ws, stream);
 }
 

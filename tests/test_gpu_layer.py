@@ -632,6 +632,58 @@ def test_scan_of_infinite_inputs_with_fewer_states(n, bf16):
     _check_ends(q, v, dims, bf16, n % 2 == 0)
 
 
+@pytest.mark.parametrize("n", [4, 16, 33])
+@pytest.mark.parametrize("name", ["dx", "ddelta", "dz"])
+def test_scan_gradient_in_the_place_of_dy(name, n):
+    """One gradient of the rows' width may be written over dy: the same bits, in chunks of several tiles and of one."""
+    for d, lens in ((70, LENS["ragged"]), (1024, [1000, 700])):
+        q = Layout(lens, 0, 3)
+        v = _scan_case(q, d, n, 1, True, True, True, True, False)
+        dims = M.scan_dims(d, n)
+        _, _, want, (t, st_in, ws) = _scan_run(q, v, dims, False, True, False)
+        y, save = _marked(q.total, d), M.alloc_bytes(M.selective_scan_save_bytes(dims, q.total, q.max_seq, True))
+        inp = M.scan_inputs(dims, t["x"], t["delta"], t["A"], t["B"], t["C"], D=t["D"], z=t["z"], delta_bias=t["bias"])
+        M.mtgnn_selective_scan(q.q, inp, dims, st_in, None, y, save=save, ws=ws)
+        dy = _dev(q.rows_of(v["dy"]))
+        g, _ = _scan_grads(q, v, dims, False)
+        g[name] = dy
+        M.mtgnn_selective_scan_bwd(q.q, dy, inp, dims, save, M.scan_grads(dims, **g), ws)
+        for k in g:
+            assert torch.equal(q.cut(g[k]) if g[k].shape[0] == q.total else g[k],
+                               q.cut(want[k]) if want[k].shape[0] == q.total else want[k]), k
+
+
+def test_linear_gradient_in_the_place_of_dy():
+    """With an activation dx may be written over dy; without one it is refused, and over x always."""
+    rs = _gen(31)
+    R, k = 300, 96
+    x, W, dy = _dev(_vals(rs, False, R, k)), _dev(_vals(rs, False, k, k)), _dev(_vals(rs, False, R, k))
+    d = M.linear_dims(k, k, M.F32, M.ACT_SILU)
+    ws = M.alloc_bytes(max(M.linear_ws_bytes(d, R), M.linear_ws_bytes(d, R, True)))
+    y, pre, dx, dW, db = _marked(R, k), _marked(R, k), _marked(R, k), _marked(k, k), _marked(1, k)[0]
+    M.mtgnn_linear(x, W, None, None, d, y, pre=pre, ws=ws)
+    M.mtgnn_linear_bwd(dy, pre, x, W, d, dx, dW, db, ws=ws)
+    over, dW2, db2 = dy.clone(), _marked(k, k), _marked(1, k)[0]
+    M.mtgnn_linear_bwd(over, pre, x, W, d, over, dW2, db2, ws=ws)
+    assert torch.equal(over, dx) and torch.equal(dW2, dW) and torch.equal(db2, db)
+    none = M.linear_dims(k, k)
+    for a, b in ((dy, dy), (dy, x)):
+        with pytest.raises(M.MtgnnError, match="overlaps"):
+            M.mtgnn_linear_bwd(a, None, x, W, none, b, dW, db, ws=ws)
+    dc = M.conv_dims(k, 4)
+    q = Layout([R], slots=False)
+    w, dw = _dev(_vals(rs, False, 4, k)), _marked(4, k)
+    wide = torch.zeros(R, 2 * k, device="cuda")
+    cw = M.alloc_bytes(M.causal_conv_ws_bytes(dc, R))
+    for a in (dy, x):
+        with pytest.raises(M.MtgnnError, match="overlaps"):
+            M.mtgnn_causal_conv_bwd(q.q, dy, x, w, None, dc, None, a, dw, None, cw)
+    wide[:, :k] = dy
+    M.mtgnn_causal_conv_bwd(q.q, wide[:, :k], x, w, None, dc, None, wide[:, k:], dw, None, cw)   # side by side: no overlap
+    M.mtgnn_causal_conv_bwd(q.q, dy, x, w, None, dc, None, dx, dw, None, cw)
+    assert torch.equal(wide[:, k:], dx)
+
+
 # --------------------------------------------------------------------------- as a layer
 
 def _layer(seed=11, bf16=False, d_msg=36, d=40, n=16, width=4):

@@ -267,3 +267,31 @@ def test_inputs_of_other_dims_are_refused():
         inp.dims = (8, 4, 1, M.F32)
         with pytest.raises(M.MtgnnError, match="gradients were made for"):
             M.mtgnn_selective_scan_bwd(q, None, inp, d, None, g, None)
+
+
+@built
+def test_gradients_over_what_is_still_read_are_refused():
+    """dx over operands that other blocks, or the product after it, read: refused, by the bytes that rows share."""
+    L = M.lib()
+    at = lambda b: C.c_void_p(1 << 20 | b)   # noqa: E731
+    far = C.c_void_p(1 << 30)
+
+    def conv(dy, x, dx, ld=8, dtype=M.F32, ws=far):
+        d = M.ConvDims(8, 4, dtype, 2)
+        return L.mtgnn_causal_conv_bwd(_q(), dy, ld, x, ld, P, None, C.byref(d), None, dx, ld, P, None, ws,
+                                       BIG, None)
+
+    for dx in (0, 4, 32, 9 * 32 + 28, -28):            # the same rows, shifted by an element, by a row, the last and first element
+        assert conv(at(4096), far, at(4096 + dx)) == -1 and b"overlaps dy" in L.mtgnn_last_error()
+        assert conv(far, at(4096), at(4096 + dx)) == -1 and b"overlaps x" in L.mtgnn_last_error()
+    assert conv(far, at(4096), at(4096 + 9 * 16 + 12), dtype=M.BF16) == -1    # the strides differ: the last row's second half
+    assert conv(at(4096), far, at(4096 + 28), ld=16) == -1 and conv(at(4096), far, at(4096 + 36), ld=16) == -1
+
+    def lin(dy, x, dx, act=0, d_in=8, d_out=8, ldd=8, ldx=8):
+        d = M.LinearDims(d_in, d_out, M.F32, act)
+        return L.mtgnn_linear_bwd(dy, ldd, far, x, ldx, None, 10, P, C.byref(d), dx, ldx, P, None, far, BIG, None)
+
+    assert lin(at(4096), far, at(4096)) == -1 and b"overlaps dy" in L.mtgnn_last_error()
+    assert lin(far, at(4096), at(4096)) == -1 and b"overlaps x" in L.mtgnn_last_error()
+    assert lin(at(4096), at(4096), at(4096), act=2) == -1 and b"overlaps x" in L.mtgnn_last_error()
+    assert lin(at(4096), far, at(4096 + 300), d_out=9, ldd=9) == -1
