@@ -765,12 +765,14 @@ def _bytes(t, need, name, optional=False):
 
 def seqs(off, max_rows, n_seq=None, slot=None, n_slots=0) -> Seqs:
     """Sequences in the rows of a matrix: sequence s has rows off[s] .. off[s + 1] - 1 (off int32, one entry more
-    than there are sequences at most)."""
+    than there are sequences at most).  It keeps its tensors."""
     max_seq = int(off.numel()) - 1
     if max_seq < 0:
         raise MtgnnError("off must have one entry more than there are sequences")
-    return Seqs(int(max_rows), max_seq, int(n_slots), _ptr(off, torch.int32, "off"), _count(n_seq, 1, "n_seq"),
-                _count(slot, max_seq, "slot"))
+    s = Seqs(int(max_rows), max_seq, int(n_slots), _ptr(off, torch.int32, "off"), _count(n_seq, 1, "n_seq"),
+             _count(slot, max_seq, "slot"))
+    s.tensors = (off, n_seq, slot)
+    return s
 
 
 def linear_dims(d_in, d_out, dtype=F32, act=ACT_NONE) -> LinearDims:
@@ -878,13 +880,14 @@ def _n_slots(state_in, state_out):
 
 
 def scan_inputs(d: ScanDims, x, delta, A, B, C_, D=None, z=None, delta_bias=None) -> ScanInputs:
-    """The scan's inputs; the tensors must live as long as this is used."""
+    """The scan's inputs; it keeps its tensors."""
     md, f32, R, gn = _DT[d.dtype], torch.float32, int(x.shape[0]), d.groups * d.n
     r = [_rows(x, md, "x", R, d.d), _rows(delta, md, "delta", R, d.d), _rows(B, md, "B", R, gn),
          _rows(C_, md, "C", R, gn), _rows(z, md, "z", R, d.d, optional=True)]
     s = ScanInputs(*[p for p, _ in r], *[ld for _, ld in r], _table(A, f32, "A", (d.n, d.d)),
                    _table(D, f32, "D", (d.d,), True), _table(delta_bias, f32, "delta_bias", (d.d,), True))
     s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
+    s.tensors = (x, delta, A, B, C_, D, z, delta_bias)
     return s
 
 
@@ -895,6 +898,7 @@ def scan_grads(d: ScanDims, dx, ddelta, dA, dB, dC, dD=None, dz=None, ddelta_bia
     s = ScanGrads(*[p for p, _ in r], *[ld for _, ld in r], _table(dA, f32, "dA", (d.n, d.d)),
                   _table(dD, f32, "dD", (d.d,), True), _table(ddelta_bias, f32, "ddelta_bias", (d.d,), True))
     s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
+    s.tensors = (dx, ddelta, dA, dB, dC, dD, dz, ddelta_bias)
     return s
 
 

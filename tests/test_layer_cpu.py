@@ -295,3 +295,30 @@ def test_gradients_over_what_is_still_read_are_refused():
     assert lin(far, at(4096), at(4096)) == -1 and b"overlaps x" in L.mtgnn_last_error()
     assert lin(at(4096), at(4096), at(4096), act=2) == -1 and b"overlaps x" in L.mtgnn_last_error()
     assert lin(at(4096), far, at(4096 + 300), d_out=9, ldd=9) == -1
+
+
+def test_descriptors_keep_their_tensors(monkeypatch):
+    """seqs, scan_inputs and scan_grads hold addresses: the tensors live as long as they do."""
+    import gc
+    import weakref
+    monkeypatch.setattr(M, "_ptr", lambda t, *a, **k: None if t is None else C.c_void_p(t.data_ptr()))
+    monkeypatch.setattr(M, "_rows", lambda t, *a, **k: (None, 8) if t is None else (C.c_void_p(t.data_ptr()), 8))
+    alive = []
+
+    def new(*shape, dtype=torch.float32):
+        t = torch.zeros(*shape, dtype=dtype)
+        alive.append(weakref.ref(t))
+        return t
+
+    i32 = torch.int32
+    q = M.seqs(new(4, dtype=i32), 10, n_seq=new(1, dtype=i32), slot=new(3, dtype=i32), n_slots=2)
+    d = M.scan_dims(8, 4)
+    inp = M.scan_inputs(d, new(10, 8), new(10, 8), new(4, 8), new(10, 4), new(10, 4), D=new(8), z=new(10, 8),
+                        delta_bias=new(8))
+    g = M.scan_grads(d, new(10, 8), new(10, 8), new(4, 8), new(10, 4), new(10, 4), dD=new(8), dz=new(10, 8),
+                     ddelta_bias=new(8))
+    gc.collect()
+    assert len(alive) == 19 and all(r() is not None for r in alive)
+    del q, inp, g
+    gc.collect()
+    assert all(r() is None for r in alive)
