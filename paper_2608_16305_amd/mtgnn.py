@@ -724,7 +724,23 @@ def mtgnn_adam_step(params, grads, m, v, shadow, lr, beta1, beta2, eps, t, strea
 
 # ----------------------------------------------------------------------------- state-space layer
 
-def _rows(t, dtype, name, rows, cols, optional=False):
+def _device() -> int:
+    """The current device, on which all tensors of a call have to be (-1: no GPU tensor can exist yet)."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+
+
+def _elsewhere(t, name, dev):
+    if t.is_cuda:
+        raise MtgnnError(f"{name} is on {t.device}, the current device is {dev}")
+
+
+def _made_here(what, name, dev):
+    """Refuses what holds the addresses of another device's tensors (a bare structure has its own)."""
+    if getattr(what, "device", dev) != dev:
+        raise MtgnnError(f"{name} are on device {what.device}, the current device is {dev}")
+
+
+def _rows(t, dtype, name, rows, cols, optional=False, dev=-1):
     """(pointer, row stride) of a [rows or more, cols] matrix whose rows are dense."""
     if t is None:
         if optional:
@@ -738,40 +754,55 @@ def _rows(t, dtype, name, rows, cols, optional=False):
         raise MtgnnError(f"{name} must be [{rows}, {cols}], got {tuple(t.shape)}")
     if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
         raise MtgnnError(f"{name} must have dense rows, got strides {t.stride()}")
-    if t.device.index != torch.cuda.current_device():
-        raise MtgnnError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    if t.get_device() != dev:
+        _elsewhere(t, name, dev)
     return C.c_void_p(t.data_ptr()), max(int(t.stride(0)), cols)
 
 
-def _table(t, dtype, name, shape, optional=False):
+def _table(t, dtype, name, shape, optional=False, dev=-1):
     """Pointer of a dense tensor of the given shape."""
     if t is not None and tuple(t.shape) != tuple(shape):
         raise MtgnnError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return _ptr(t, dtype, name, optional)
+    p = _ptr(t, dtype, name, optional)
+    if t is not None and t.get_device() != dev:
+        _elsewhere(t, name, dev)
+    return p
 
 
-def _count(t, n, name):
+def _count(t, n, name, dev=-1):
     """Pointer of an int32 tensor of n entries or more, or NULL."""
     if t is not None and t.numel() < n:
         raise MtgnnError(f"{name} must have {n} entries, got {t.numel()}")
-    return _ptr(t, torch.int32, name, optional=True)
+    p = _ptr(t, torch.int32, name, optional=True)
+    if t is not None and t.get_device() != dev:
+        _elsewhere(t, name, dev)
+    return p
 
 
-def _bytes(t, need, name, optional=False):
+def _bytes(t, need, name, optional=False, dev=-1):
     if t is not None and t.numel() < need:
         raise MtgnnError(f"{name} must have {need} bytes, got {t.numel()}")
-    return _ptr(t, torch.uint8, name, optional)
+    p = _ptr(t, torch.uint8, name, optional)
+    if t is not None and t.get_device() != dev:
+        _elsewhere(t, name, dev)
+    return p
+
+
+def _work(ws, dev):
+    """(pointer, bytes) of a workspace, or (None, 0)."""
+    return (None, 0) if ws is None else (_bytes(ws, 0, "ws", dev=dev), ws.numel())
 
 
 def seqs(off, max_rows, n_seq=None, slot=None, n_slots=0) -> Seqs:
     """Sequences in the rows of a matrix: sequence s has rows off[s] .. off[s + 1] - 1 (off int32, one entry more
     than there are sequences at most).  It keeps its tensors."""
+    dev = _device()
     max_seq = int(off.numel()) - 1
     if max_seq < 0:
         raise MtgnnError("off must have one entry more than there are sequences")
-    s = Seqs(int(max_rows), max_seq, int(n_slots), _ptr(off, torch.int32, "off"), _count(n_seq, 1, "n_seq"),
-             _count(slot, max_seq, "slot"))
-    s.tensors = (off, n_seq, slot)
+    s = Seqs(int(max_rows), max_seq, int(n_slots), _count(off, 1, "off", dev=dev), _count(n_seq, 1, "n_seq", dev=dev),
+             _count(slot, max_seq, "slot", dev=dev))
+    s.tensors, s.device = (off, n_seq, slot), dev
     return s
 
 
@@ -809,68 +840,79 @@ def selective_scan_save_bytes(d: ScanDims, max_rows, max_seq, carried) -> int:
 
 def mtgnn_linear(x, W, b, residual, d: LinearDims, y, pre=None, n_rows=None, ws=None, stream=None):
     """y = act(x W^T + b) + residual; pre: where the backward will find x W^T + b."""
+    dev = _device()
     md, R = _DT[d.dtype], int(x.shape[0])
-    xp, ldx = _rows(x, md, "x", R, d.d_in)
-    rp, ldr = _rows(residual, md, "residual", R, d.d_out, optional=True)
-    yp, ldy = _rows(y, md, "y", R, d.d_out)
-    wp, wb = _ws(ws)
-    _check(lib().mtgnn_linear(xp, ldx, _count(n_rows, 1, "n_rows"), R, _table(W, md, "W", (d.d_out, d.d_in)),
-                              _table(b, torch.float32, "b", (d.d_out,), True), rp, ldr, C.byref(d), yp, ldy,
-                              _table(pre, torch.float32, "pre", (R, d.d_out), True), wp, wb, _stream(stream)),
+    xp, ldx = _rows(x, md, "x", R, d.d_in, dev=dev)
+    rp, ldr = _rows(residual, md, "residual", R, d.d_out, optional=True, dev=dev)
+    yp, ldy = _rows(y, md, "y", R, d.d_out, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_linear(xp, ldx, _count(n_rows, 1, "n_rows", dev=dev), R,
+                              _table(W, md, "W", (d.d_out, d.d_in), dev=dev),
+                              _table(b, torch.float32, "b", (d.d_out,), True, dev=dev), rp, ldr, C.byref(d), yp, ldy,
+                              _table(pre, torch.float32, "pre", (R, d.d_out), True, dev=dev), wp, wb, _stream(stream)),
            "mtgnn_linear")
 
 
 def mtgnn_linear_bwd(dy, pre, x, W, d: LinearDims, dx, dW, db, n_rows=None, ws=None, stream=None):
+    dev = _device()
     md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
-    gp, lddy = _rows(dy, f32, "dy", R, d.d_out)
-    xp, ldx = _rows(x, md, "x", R, d.d_in)
-    dp, lddx = _rows(dx, f32, "dx", R, d.d_in, optional=True)
-    wp, wb = _ws(ws)
-    _check(lib().mtgnn_linear_bwd(gp, lddy, _table(pre, f32, "pre", (R, d.d_out), d.act == ACT_NONE), xp, ldx,
-                                  _count(n_rows, 1, "n_rows"), R, _table(W, md, "W", (d.d_out, d.d_in)), C.byref(d),
-                                  dp, lddx, _table(dW, f32, "dW", (d.d_out, d.d_in)),
-                                  _table(db, f32, "db", (d.d_out,), True), wp, wb, _stream(stream)),
+    gp, lddy = _rows(dy, f32, "dy", R, d.d_out, dev=dev)
+    xp, ldx = _rows(x, md, "x", R, d.d_in, dev=dev)
+    dp, lddx = _rows(dx, f32, "dx", R, d.d_in, optional=True, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_linear_bwd(gp, lddy, _table(pre, f32, "pre", (R, d.d_out), d.act == ACT_NONE, dev=dev), xp, ldx,
+                                  _count(n_rows, 1, "n_rows", dev=dev), R,
+                                  _table(W, md, "W", (d.d_out, d.d_in), dev=dev), C.byref(d), dp, lddx,
+                                  _table(dW, f32, "dW", (d.d_out, d.d_in), dev=dev),
+                                  _table(db, f32, "db", (d.d_out,), True, dev=dev), wp, wb, _stream(stream)),
            "mtgnn_linear_bwd")
 
 
 def mtgnn_causal_conv(q: Seqs, x, w, b, d: ConvDims, state_in, state_out, y, save=None, stream=None):
+    dev = _device()
     md = _DT[d.dtype]
-    xp, ldx = _rows(x, md, "x", q.max_rows, d.d)
-    yp, ldy = _rows(y, md, "y", q.max_rows, d.d)
+    _made_here(q, "seqs", dev)
+    xp, ldx = _rows(x, md, "x", q.max_rows, d.d, dev=dev)
+    yp, ldy = _rows(y, md, "y", q.max_rows, d.d, dev=dev)
     st = (q.n_slots, d.width - 1, d.d)
-    _check(lib().mtgnn_causal_conv(C.byref(q), xp, ldx, _table(w, md, "w", (d.width, d.d)),
-                                   _table(b, torch.float32, "b", (d.d,), True), C.byref(d),
-                                   _table(state_in, md, "state_in", st, True),
-                                   _table(state_out, md, "state_out", st, True), yp, ldy,
-                                   _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True),
+    _check(lib().mtgnn_causal_conv(C.byref(q), xp, ldx, _table(w, md, "w", (d.width, d.d), dev=dev),
+                                   _table(b, torch.float32, "b", (d.d,), True, dev=dev), C.byref(d),
+                                   _table(state_in, md, "state_in", st, True, dev=dev),
+                                   _table(state_out, md, "state_out", st, True, dev=dev), yp, ldy,
+                                   _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True, dev=dev),
                                    _stream(stream)), "mtgnn_causal_conv")
 
 
 def mtgnn_causal_conv_bwd(q: Seqs, dy, x, w, b, d: ConvDims, save, dx, dw, db, ws, stream=None):
+    dev = _device()
     md, f32 = _DT[d.dtype], torch.float32
-    gp, lddy = _rows(dy, f32, "dy", q.max_rows, d.d)
-    xp, ldx = _rows(x, md, "x", q.max_rows, d.d)
-    dp, lddx = _rows(dx, f32, "dx", q.max_rows, d.d)
-    wp, wb = _ws(ws)
-    _check(lib().mtgnn_causal_conv_bwd(C.byref(q), gp, lddy, xp, ldx, _table(w, md, "w", (d.width, d.d)),
-                                       _table(b, f32, "b", (d.d,), True), C.byref(d),
-                                       _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True), dp, lddx,
-                                       _table(dw, f32, "dw", (d.width, d.d)), _table(db, f32, "db", (d.d,), True), wp,
-                                       wb, _stream(stream)), "mtgnn_causal_conv_bwd")
+    _made_here(q, "seqs", dev)
+    gp, lddy = _rows(dy, f32, "dy", q.max_rows, d.d, dev=dev)
+    xp, ldx = _rows(x, md, "x", q.max_rows, d.d, dev=dev)
+    dp, lddx = _rows(dx, f32, "dx", q.max_rows, d.d, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_causal_conv_bwd(C.byref(q), gp, lddy, xp, ldx, _table(w, md, "w", (d.width, d.d), dev=dev),
+                                       _table(b, f32, "b", (d.d,), True, dev=dev), C.byref(d),
+                                       _bytes(save, causal_conv_save_bytes(d, q.max_seq), "save", True, dev=dev), dp, lddx,
+                                       _table(dw, f32, "dw", (d.width, d.d), dev=dev),
+                                       _table(db, f32, "db", (d.d,), True, dev=dev), wp, wb, _stream(stream)),
+           "mtgnn_causal_conv_bwd")
 
 
 def mtgnn_causal_conv_step(slot, x, w, b, d: ConvDims, state_in, state_out, y, n_rows=None, stream=None):
     """One row each: x[r] is the next row of slot[r] (None: slot r)."""
+    dev = _device()
     md, R = _DT[d.dtype], int(x.shape[0])
-    xp, ldx = _rows(x, md, "x", R, d.d)
-    yp, ldy = _rows(y, md, "y", R, d.d)
+    xp, ldx = _rows(x, md, "x", R, d.d, dev=dev)
+    yp, ldy = _rows(y, md, "y", R, d.d, dev=dev)
     n = _n_slots(state_in, state_out)
     st = (n, d.width - 1, d.d)
-    _check(lib().mtgnn_causal_conv_step(_count(slot, R, "slot"), _count(n_rows, 1, "n_rows"), R, n, xp, ldx,
-                                        _table(w, md, "w", (d.width, d.d)),
-                                        _table(b, torch.float32, "b", (d.d,), True), C.byref(d),
-                                        _table(state_in, md, "state_in", st, True),
-                                        _table(state_out, md, "state_out", st, True), yp, ldy, _stream(stream)),
+    _check(lib().mtgnn_causal_conv_step(_count(slot, R, "slot", dev=dev), _count(n_rows, 1, "n_rows", dev=dev), R, n,
+                                        xp, ldx,
+                                        _table(w, md, "w", (d.width, d.d), dev=dev),
+                                        _table(b, torch.float32, "b", (d.d,), True, dev=dev), C.byref(d),
+                                        _table(state_in, md, "state_in", st, True, dev=dev),
+                                        _table(state_out, md, "state_out", st, True, dev=dev), yp, ldy, _stream(stream)),
            "mtgnn_causal_conv_step")
 
 
@@ -881,68 +923,82 @@ def _n_slots(state_in, state_out):
 
 def scan_inputs(d: ScanDims, x, delta, A, B, C_, D=None, z=None, delta_bias=None) -> ScanInputs:
     """The scan's inputs; it keeps its tensors."""
+    dev = _device()
     md, f32, R, gn = _DT[d.dtype], torch.float32, int(x.shape[0]), d.groups * d.n
-    r = [_rows(x, md, "x", R, d.d), _rows(delta, md, "delta", R, d.d), _rows(B, md, "B", R, gn),
-         _rows(C_, md, "C", R, gn), _rows(z, md, "z", R, d.d, optional=True)]
-    s = ScanInputs(*[p for p, _ in r], *[ld for _, ld in r], _table(A, f32, "A", (d.n, d.d)),
-                   _table(D, f32, "D", (d.d,), True), _table(delta_bias, f32, "delta_bias", (d.d,), True))
+    r = [_rows(x, md, "x", R, d.d, dev=dev), _rows(delta, md, "delta", R, d.d, dev=dev),
+         _rows(B, md, "B", R, gn, dev=dev), _rows(C_, md, "C", R, gn, dev=dev),
+         _rows(z, md, "z", R, d.d, optional=True, dev=dev)]
+    s = ScanInputs(*[p for p, _ in r], *[ld for _, ld in r], _table(A, f32, "A", (d.n, d.d), dev=dev),
+                   _table(D, f32, "D", (d.d,), True, dev=dev),
+                   _table(delta_bias, f32, "delta_bias", (d.d,), True, dev=dev))
     s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
-    s.tensors = (x, delta, A, B, C_, D, z, delta_bias)
+    s.tensors, s.device = (x, delta, A, B, C_, D, z, delta_bias), dev
     return s
 
 
 def scan_grads(d: ScanDims, dx, ddelta, dA, dB, dC, dD=None, dz=None, ddelta_bias=None) -> ScanGrads:
+    dev = _device()
     f32, R, gn = torch.float32, int(dx.shape[0]), d.groups * d.n
-    r = [_rows(dx, f32, "dx", R, d.d), _rows(ddelta, f32, "ddelta", R, d.d), _rows(dB, f32, "dB", R, gn),
-         _rows(dC, f32, "dC", R, gn), _rows(dz, f32, "dz", R, d.d, optional=True)]
-    s = ScanGrads(*[p for p, _ in r], *[ld for _, ld in r], _table(dA, f32, "dA", (d.n, d.d)),
-                  _table(dD, f32, "dD", (d.d,), True), _table(ddelta_bias, f32, "ddelta_bias", (d.d,), True))
+    r = [_rows(dx, f32, "dx", R, d.d, dev=dev), _rows(ddelta, f32, "ddelta", R, d.d, dev=dev),
+         _rows(dB, f32, "dB", R, gn, dev=dev), _rows(dC, f32, "dC", R, gn, dev=dev),
+         _rows(dz, f32, "dz", R, d.d, optional=True, dev=dev)]
+    s = ScanGrads(*[p for p, _ in r], *[ld for _, ld in r], _table(dA, f32, "dA", (d.n, d.d), dev=dev),
+                  _table(dD, f32, "dD", (d.d,), True, dev=dev),
+                  _table(ddelta_bias, f32, "ddelta_bias", (d.d,), True, dev=dev))
     s.rows, s.dims = R, (d.d, d.n, d.groups, d.dtype)
-    s.tensors = (dx, ddelta, dA, dB, dC, dD, dz, ddelta_bias)
+    s.tensors, s.device = (dx, ddelta, dA, dB, dC, dD, dz, ddelta_bias), dev
     return s
 
 
-def _fit(what, d, rows, name):
+def _fit(what, d, rows, name, dev):
     """The tensors were checked against the dims of this call, and have its rows."""
     if what.dims != (d.d, d.n, d.groups, d.dtype):
         raise MtgnnError(f"{name} were made for (d, n, groups, dtype) = {what.dims}")
     if what.rows < rows:
         raise MtgnnError(f"{name} have {what.rows} rows, the sequences {rows}")
+    _made_here(what, name, dev)
 
 
 def mtgnn_selective_scan(q: Seqs, inp: ScanInputs, d: ScanDims, state_in, state_out, y, save=None, ws=None,
                          stream=None):
-    _fit(inp, d, q.max_rows, "the scan's inputs")
-    yp, ldy = _rows(y, _DT[d.dtype], "y", q.max_rows, d.d)
+    dev = _device()
+    _fit(inp, d, q.max_rows, "the scan's inputs", dev)
+    _made_here(q, "seqs", dev)
+    yp, ldy = _rows(y, _DT[d.dtype], "y", q.max_rows, d.d, dev=dev)
     st, f32 = (q.n_slots, d.n, d.d), torch.float32
     need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, state_in is not None)
-    wp, wb = _ws(ws)
-    _check(lib().mtgnn_selective_scan(C.byref(q), C.byref(inp), C.byref(d), _table(state_in, f32, "state_in", st, True),
-                                      _table(state_out, f32, "state_out", st, True), yp, ldy,
-                                      _bytes(save, need, "save", True), wp, wb, _stream(stream)),
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_selective_scan(C.byref(q), C.byref(inp), C.byref(d),
+                                      _table(state_in, f32, "state_in", st, True, dev=dev),
+                                      _table(state_out, f32, "state_out", st, True, dev=dev), yp, ldy,
+                                      _bytes(save, need, "save", True, dev=dev), wp, wb, _stream(stream)),
            "mtgnn_selective_scan")
 
 
 def mtgnn_selective_scan_bwd(q: Seqs, dy, inp: ScanInputs, d: ScanDims, save, grads: ScanGrads, ws, stream=None):
-    _fit(inp, d, q.max_rows, "the scan's inputs")
-    _fit(grads, d, q.max_rows, "the scan's gradients")
-    gp, lddy = _rows(dy, torch.float32, "dy", q.max_rows, d.d)
+    dev = _device()
+    _fit(inp, d, q.max_rows, "the scan's inputs", dev)
+    _fit(grads, d, q.max_rows, "the scan's gradients", dev)
+    _made_here(q, "seqs", dev)
+    gp, lddy = _rows(dy, torch.float32, "dy", q.max_rows, d.d, dev=dev)
     need = selective_scan_save_bytes(d, q.max_rows, q.max_seq, False)
-    wp, wb = _ws(ws)
-    _check(lib().mtgnn_selective_scan_bwd(C.byref(q), gp, lddy, C.byref(inp), C.byref(d), _bytes(save, need, "save"),
-                                          C.byref(grads), wp, wb, _stream(stream)), "mtgnn_selective_scan_bwd")
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_selective_scan_bwd(C.byref(q), gp, lddy, C.byref(inp), C.byref(d),
+                                          _bytes(save, need, "save", dev=dev), C.byref(grads), wp, wb,
+                                          _stream(stream)), "mtgnn_selective_scan_bwd")
 
 
 def mtgnn_selective_scan_step(slot, inp: ScanInputs, d: ScanDims, state_in, state_out, y, n_rows=None, stream=None):
     """One row each: row r of the inputs is the next row of slot[r] (None: slot r)."""
+    dev = _device()
     R, f32 = inp.rows, torch.float32
-    _fit(inp, d, R, "the scan's inputs")
-    yp, ldy = _rows(y, _DT[d.dtype], "y", R, d.d)
+    _fit(inp, d, R, "the scan's inputs", dev)
+    yp, ldy = _rows(y, _DT[d.dtype], "y", R, d.d, dev=dev)
     n = _n_slots(state_in, state_out)
     st = (n, d.n, d.d)
-    _check(lib().mtgnn_selective_scan_step(_count(slot, R, "slot"), _count(n_rows, 1, "n_rows"), R, n, C.byref(inp),
-                                           C.byref(d), _table(state_in, f32, "state_in", st, True),
-                                           _table(state_out, f32, "state_out", st, True), yp, ldy, _stream(stream)),
+    _check(lib().mtgnn_selective_scan_step(_count(slot, R, "slot", dev=dev), _count(n_rows, 1, "n_rows", dev=dev), R, n,
+                                           C.byref(inp), C.byref(d), _table(state_in, f32, "state_in", st, True, dev=dev),
+                                           _table(state_out, f32, "state_out", st, True, dev=dev), yp, ldy, _stream(stream)),
            "mtgnn_selective_scan_step")
 
 

@@ -322,3 +322,35 @@ def test_descriptors_keep_their_tensors(monkeypatch):
     del q, inp, g
     gc.collect()
     assert all(r() is None for r in alive)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Every kind of operand, as if the current device were another one."""
+    class Elsewhere:
+        is_cuda, device, shape, dtype = True, torch.device("cuda", 1), (4, 8), torch.float32
+        numel, dim, get_device, stride = (lambda s: 32), (lambda s: 2), (lambda s: 1), (lambda s, i: (8, 1)[i])
+
+    monkeypatch.setattr(M, "_ptr", lambda t, *a, **k: C.c_void_p(256))
+    monkeypatch.setattr(torch, "Tensor", Elsewhere)
+    monkeypatch.setattr(M, "_device", lambda: 0)
+    t = Elsewhere()
+    for call in (lambda: M._rows(t, torch.float32, "m", 4, 8, dev=0), lambda: M._work(t, 0), lambda: M.seqs(t, 4),
+                 lambda: M._table(t, torch.float32, "m", (4, 8), dev=0), lambda: M._count(t, 3, "m", dev=0),
+                 lambda: M._bytes(t, 16, "m", dev=0)):
+        with pytest.raises(M.MtgnnError, match="current device is 0"):
+            call()
+    # what holds addresses was made there, and is used here
+    monkeypatch.setattr(M, "_device", lambda: 1)
+    q, d, c = M.seqs(t, 4), M.scan_dims(8, 4), M.conv_dims(8, 4)
+    inp, g = M.ScanInputs(), M.ScanGrads()
+    inp.rows = g.rows = 4
+    inp.dims = g.dims = (8, 4, 1, M.F32)
+    inp.device = g.device = 1
+    monkeypatch.setattr(M, "_device", lambda: 0)
+    for call in (lambda: M.mtgnn_causal_conv(q, None, None, None, c, None, None, None),
+                 lambda: M.mtgnn_causal_conv_bwd(q, None, None, None, None, c, None, None, None, None, None),
+                 lambda: M.mtgnn_selective_scan(q, inp, d, None, None, None),
+                 lambda: M.mtgnn_selective_scan_step(None, inp, d, None, None, None),
+                 lambda: M.mtgnn_selective_scan_bwd(q, None, inp, d, None, g, None)):
+        with pytest.raises(M.MtgnnError, match="current device is 0"):
+            call()
