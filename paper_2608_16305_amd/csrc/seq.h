@@ -94,8 +94,10 @@ __device__ __forceinline__ SeqAt seq_find(const int32_t* off, int n, int t) {
   lo = __builtin_amdgcn_readfirstlane(lo);
   return SeqAt{lo, off[lo], off[lo + 1]};
 }
-// A walk over the sequences.  The wave holds 64 consecutive starts (lane l: off[w0 + l]) and their slots and reads
-// them from its lanes: a start costs a register read, not a dependent trip to memory.
+// A walk over the sequences that have rows.  The wave holds 64 consecutive starts (lane l: off[w0 + l], w0 <= s) and their
+// slots and reads them from its lanes: a start costs a register read, not a dependent trip to memory.  Sequences without
+// rows are passed over at once, however many they are: in the window by comparing all its starts, else by a search.  (One
+// after the other they took 0.12 us each.)
 struct SeqWalk {
   const int32_t *off, *slot;
   int64_t n_slots;
@@ -113,32 +115,33 @@ struct SeqWalk {
     v_off = off[min(w0 + lane, n)];
     v_slot = slot ? slot[min(w0 + lane, n - 1)] : w0 + lane;
   }
-  __device__ __forceinline__ int off_at(int i, bool back) {   // off[i], 0 <= i <= n
-    if (i < w0 || i > w0 + 63) window(back ? i - 63 : i - 1);
-    return __builtin_amdgcn_readlane(v_off, i - w0);
-  }
-  // To the next (previous) sequence that has rows; stays at the last (first) one.
+  // To the next (previous) sequence that has rows: the one that holds the row behind this one's last (before its first).
+  // Where there is none, to the last (first) of all, as one without rows.  Whatever the offsets hold, a step gets further
+  // or to that end, and s stays below n.
   __device__ __forceinline__ void next() {
-    do {
-      if (s + 1 >= n) {
-        beg = end;
-        return;
-      }
-      ++s;
-      beg = end;
-      end = off_at(s + 1, false);
-    } while (end <= beg);
+    beg = end;
+    uint64_t behind = __ballot(v_off > beg);
+    if (!behind) {
+      window(seq_find(off, n, beg).s);
+      behind = __ballot(v_off > beg);
+    }
+    s = n - 1;
+    if (!behind) return;
+    const int j = __builtin_ctzll(behind);
+    s = w0 + (j > 0 ? j - 1 : 0);
+    end = __builtin_amdgcn_readlane(v_off, j);
   }
   __device__ __forceinline__ void prev() {
-    do {
-      if (s == 0) {
-        end = beg;
-        return;
-      }
-      --s;
-      end = beg;
-      beg = off_at(s, true);
-    } while (end <= beg);
+    end = beg;
+    uint64_t before = s - w0 < 64 ? __ballot(v_off < end) : 0;
+    if (!before) {
+      window(seq_find(off, n, end - 1).s - 63);
+      before = __ballot(v_off < end);
+    }
+    const int j = before ? 63 - __builtin_clzll(before) : 0;
+    s = before ? min(w0 + j, n - 1) : 0;
+    beg = before ? __builtin_amdgcn_readlane(v_off, j) : 0;
+    end = before ? end : 0;
   }
   // The table row of the sequence, or -1: no carried state.
   __device__ __forceinline__ int64_t row() {

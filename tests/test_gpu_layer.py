@@ -989,3 +989,57 @@ def test_scan_of_states_that_grow(way, grown_by, d):
     dims = M.scan_dims(d, n, 1, M.F32, False)
     y, st, g, _ = _scan_run(q, v, dims, False, True, False)
     _scan_check(q, v, dims, y, st, g, False, True)
+
+
+@pytest.mark.parametrize("where", ["behind", "before", "between", "spread"])
+def test_sequences_without_rows(where):
+    """2^22 announced sequences, few of them with rows: the bits of the few alone, forward and backward, in a time that does
+    not count the others one by one (0.5 s a wave that meets them all, at 0.12 us each)."""
+    S, d, n = 1 << 22, 36, 16
+    lens = np.array([5, 1, 17, 8, 30, 2, 9, 70, 1, 1, 300])
+    m = len(lens)
+    at = {"behind": np.arange(m), "before": S - m + np.arange(m), "between": np.where(np.arange(m) < 4, 0, S - m) + np.arange(m),
+          "spread": np.sort(_gen(3).choice(S, m, replace=False))}[where]
+    full = np.zeros(S, np.int64)
+    full[at] = lens
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(full)]).astype(np.int32)).cuda()
+    few = torch.from_numpy(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)).cuda()
+    R = int(lens.sum())
+    slot = torch.arange(m, dtype=torch.int32, device="cuda")
+    slots = torch.full((S,), -1, dtype=torch.int32, device="cuda")
+    slots[torch.from_numpy(at).cuda()] = slot
+    rs = _gen(9)
+    t = {k: _dev(_vals(rs, False, R, d)) for k in ("x", "delta", "z", "dy")}
+    t.update({k: _dev(_vals(rs, False, R, n)) for k in ("B", "C")})
+    A, w, table = _dev(-rs.rand(n, d)), _dev(_vals(rs, False, 4, d)), _dev(_vals(rs, False, m, n, d))
+    conv_table = _dev(_vals(rs, False, m, 3, d))
+    ds, dc = M.scan_dims(d, n), M.conv_dims(d, 4)
+
+    def run(q, max_seq):
+        inp = M.scan_inputs(ds, t["x"], t["delta"], A, t["B"], t["C"], z=t["z"])
+        ws = M.alloc_bytes(max(M.selective_scan_ws_bytes(ds, R, max_seq, True), M.causal_conv_ws_bytes(dc, R)))
+        out = dict(y=_marked(R, d), st=torch.zeros_like(table), c=_marked(R, d))
+        save = M.alloc_bytes(M.selective_scan_save_bytes(ds, R, max_seq, False))   # (with first states 10 GB)
+        g = dict(dx=_marked(R, d), ddelta=_marked(R, d), dA=_marked(n, d), dB=_marked(R, n), dC=_marked(R, n), dz=_marked(R, d))
+        out.update(g, cdx=_marked(R, d), cdw=_marked(4, d))
+
+        def calls():
+            M.mtgnn_selective_scan(q, inp, ds, table, out["st"], out["y"], ws=ws)
+            M.mtgnn_selective_scan(q, inp, ds, None, None, g["dx"], save=save, ws=ws)
+            M.mtgnn_selective_scan_bwd(q, t["dy"], inp, ds, save, M.scan_grads(ds, **g), ws)
+            M.mtgnn_causal_conv(q, t["x"], w, None, dc, conv_table, None, out["c"])
+            M.mtgnn_causal_conv_bwd(q, t["dy"], t["x"], w, None, dc, None, out["cdx"], out["cdw"], None, ws)
+        calls()
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        calls()
+        b.record()
+        torch.cuda.synchronize()
+        return out, a.elapsed_time(b)
+
+    got, ms = run(M.seqs(off, R, slot=slots, n_slots=m), S)
+    want, _ = run(M.seqs(few, R, slot=slot, n_slots=m), m)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    assert ms < 50.0, ms
