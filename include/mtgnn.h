@@ -782,7 +782,9 @@ mtgnn_status mtgnn_build_temporal_csr(const int32_t* src, const int32_t* dst, co
  *     products).
  * mtgnn_timer_stop waits for the recorded events (host-blocking), returns
  * the summed duration in milliseconds and the number of timed launches, and
- * disarms the timer.  Host-side state: use from one host thread. */
+ * disarms the timer.  Host-side state: use from one host thread.
+ * The products of mtgnn_linear and its backward carry a second name, by the side
+ * of their tiles: linear_64, linear_128, linear_256. */
 mtgnn_status mtgnn_timer_start(const char* kernel, int max_launches);
 mtgnn_status mtgnn_timer_stop(double* total_ms, int* launches);
 

@@ -596,7 +596,7 @@ mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
       p.tc = cdiv(p.cols, BIG);
       p.tiles = cdiv(p.rows, BIG) * p.tc;
       p.split = 1;
-      TimedScope ts(site::Generic::name, s);
+      TimedScope ts(site::Generic::name, s), tile("linear_256", s);
       k_product_big<<<(unsigned)p.tiles, 512, 0, s>>>(p);
       MTGNN_CHECK_LAUNCH("product_big");
       return MTGNN_OK;
@@ -614,7 +614,7 @@ mtgnn_status product(ProdP p, void* ws, hipStream_t s) {
   }
   const unsigned grid = (unsigned)(p.tiles * p.split);
   {
-    TimedScope ts(site::Generic::name, s);
+    TimedScope ts(site::Generic::name, s), tile(q.T == 128 ? "linear_128" : "linear_64", s);
     if (q.T == 128) k_product<RF, CF, RK, CK, 128><<<grid, NT, 0, s>>>(p);
     else k_product<RF, CF, RK, CK, 64><<<grid, NT, 0, s>>>(p);
   }

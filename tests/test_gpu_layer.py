@@ -1043,3 +1043,61 @@ def test_sequences_without_rows(where):
     for k in want:
         assert torch.equal(got[k], want[k]), k
     assert ms < 50.0, ms
+
+
+# --------------------------------------------------------------------------- every kernel of the linear layer
+
+def _tile_launches(call):
+    """Products of a call by the side of their tiles."""
+    got = {}
+    for side in (64, 128, 256):
+        M.timer_start(f"linear_{side}", 16)
+        try:
+            call()
+        finally:
+            got[side] = M.timer_stop()[1]
+    return {k: v for k, v in got.items() if v}
+
+
+def _linear_tiles(case, bf16, dx=True):
+    """Which tiles forward and backward (dx, dW) of a case take."""
+    rows, pad, d_in, d_out, act, bias, residual, wide = case
+    d = M.linear_dims(d_in, d_out, M.BF16 if bf16 else M.F32, ACTS.index(act))
+    R, dt = rows + pad, torch.bfloat16 if bf16 else torch.float32
+    place = (lambda r, c: torch.zeros(r, c + 5, dtype=dt, device="cuda")[:, 3:3 + c]) if wide else (
+        lambda r, c: torch.zeros(r, c, dtype=dt, device="cuda"))
+    x, W, y = place(R, d_in), torch.zeros(d_out, d_in, dtype=dt, device="cuda"), place(R, d_out)
+    f32 = lambda *s: torch.zeros(*s, device="cuda")   # noqa: E731
+    pre, dy, g, dW = f32(R, d_out), f32(R, d_out), f32(R, d_in), f32(d_out, d_in)
+    ws = M.alloc_bytes(max(M.linear_ws_bytes(d, R), M.linear_ws_bytes(d, R, True)))
+    fwd = _tile_launches(lambda: M.mtgnn_linear(x, W, None, None, d, y, pre=pre, ws=ws))
+    both = _tile_launches(lambda: M.mtgnn_linear_bwd(dy, pre, x, W, d, g, dW, None, ws=ws))
+    only = _tile_launches(lambda: M.mtgnn_linear_bwd(dy, pre, x, W, d, None, dW, None, ws=ws))
+    assert sum(fwd.values()) == 1 and sum(only.values()) == 1 and sum(both.values()) == 2
+    side = lambda t: next(iter(t))   # noqa: E731
+    return side(fwd), side({k: both[k] - only.get(k, 0) for k in both if both[k] > only.get(k, 0)}), side(only)
+
+
+TILES = [  # case as above; sides of the tiles of the product, dx and dW; those in bfloat16 where they are others
+    ((2600, 20, 70, 2570, "silu", True, True, False), (128, 64, 64), None),          # sums of no whole step
+    ((2570, 7, 193, 2601, "silu", True, True, True), (128, 64, 64), None),           # rows at odd addresses
+    ((2600, 20, 96, 2570, "relu", False, True, False), (128, 64, 64), None),         # a whole step and half of one
+    ((2570, 7, 192, 2601, "none", True, False, True), (128, 64, 64), None),          # whole steps, rows at odd addresses
+    ((2600, 20, 2570, 70, "silu", True, False, False), (64, 128, 64), None),
+    ((2601, 3, 2573, 66, "none", True, True, True), (64, 128, 64), None),
+    ((2600, 0, 2576, 64, "silu", False, False, False), (64, 128, 64), None),
+    ((301, 5, 2570, 2601, "silu", True, False, False), (64, 64, 128), None),
+    ((320, 0, 2601, 2570, "none", True, False, True), (64, 64, 128), None),
+    ((5000, 9, 130, 141, "silu", True, True, False), (64, 64, 128), None),           # a long sum over rows in shares
+    ((200, 3, 4201, 130, "silu", True, True, False), (128, 64, 64), None),           # a long sum over d_in in shares
+    ((3584, 5, 128, 3600, "silu", True, True, False), (128, 64, 64), (256, 64, 64)),
+]
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case,sides,sides_bf16", TILES, ids=str)
+def test_linear_by_tiles(case, sides, sides_bf16, bf16):
+    """Forward, dx and dW in tiles of 64, 128 and 256, with rows, columns and sums that end inside one; which tiles a
+    case takes is part of the test."""
+    assert _linear_tiles(case, bf16) == (sides_bf16 if bf16 and sides_bf16 else sides)
+    _check_linear(case, bf16)
