@@ -1101,3 +1101,50 @@ def test_linear_by_tiles(case, sides, sides_bf16, bf16):
     case takes is part of the test."""
     assert _linear_tiles(case, bf16) == (sides_bf16 if bf16 and sides_bf16 else sides)
     _check_linear(case, bf16)
+
+
+# rows, d_in, d_out whose products take tiles of 64, 128 and (bfloat16 forward) 256; sides as above
+ONE_TERM = [((90, 64, 100), (64, 64, 64), None), ((2600, 70, 2570), (128, 64, 64), None),
+            ((2600, 2570, 70), (64, 128, 64), None), ((320, 2570, 2601), (64, 64, 128), None),
+            ((5000, 130, 141), (64, 64, 128), None), ((3584, 128, 3600), (128, 64, 64), (256, 64, 64))]
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size,sides,sides_bf16", ONE_TERM, ids=str)
+def test_linear_products_are_exact_to_float32(size, sides, sides_bf16, bf16):
+    """Sums with one term that is not zero: the product of two full mantissas, where a part of an operand that were lost
+    would show (2^-18 of it without a low part, 64 u), as it does not in sums of many.
+
+    What the split leaves out is u / 4 (two products of a middle and a low part, 2^-27 each).  Of the additions into the
+    float32 sum only the last, of the high parts' product, is of the whole's size: u, or 2 u if it is cut off and not
+    rounded; the others are 2^-8 of it.  So 3 u, and what a bfloat16 output is rounded by."""
+    rows, d_in, d_out = size
+    assert _linear_tiles((rows, 0, d_in, d_out, "none", False, False, False), bf16) == (sides_bf16 if bf16 and sides_bf16 else sides)
+    rs = _gen(41)
+    d = M.linear_dims(d_in, d_out, M.BF16 if bf16 else M.F32)
+    ws = M.alloc_bytes(max(M.linear_ws_bytes(d, rows), M.linear_ws_bytes(d, rows, True)))
+    full = lambda *s: ((1 + rs.rand(*s)) * rs.choice([-1, 1], s)).astype(np.float32)   # noqa: E731
+    held = (lambda v: round_bf16(v)) if bf16 else (lambda v: v)
+
+    def single(r, c):   # one term a row
+        v, at = np.zeros((r, c), np.float32), rs.randint(0, c, r)
+        v[np.arange(r), at] = full(r)
+        return v, at
+
+    x, at = single(rows, d_in)
+    x, W = held(x), held(full(d_out, d_in))
+    y, pre, Wd = _marked(rows, d_out, bf16), _marked(rows, d_out), _dev(W, bf16)
+    M.mtgnn_linear(_dev(x, bf16), Wd, None, None, d, y, pre=pre, ws=ws)
+    want = x[np.arange(rows), at].astype(np.float64)[:, None] * W.T.astype(np.float64)[at]
+    _close("pre", pre, want, 3 * U * np.abs(want))
+    _close("y", y, want, 3 * U * np.abs(want), bf16)
+    dy, at = single(rows, d_out)
+    dx, dW = _marked(rows, d_in), _marked(d_out, d_in)
+    dense = held(full(rows, d_in))
+    M.mtgnn_linear_bwd(_dev(dy), None, _dev(dense, bf16), Wd, d, dx, dW, None, ws=ws)
+    want = dy[np.arange(rows), at].astype(np.float64)[:, None] * W.astype(np.float64)[at]
+    _close("dx", dx, want, 3 * U * np.abs(want))
+    dyt, at = single(d_out, rows)
+    M.mtgnn_linear_bwd(_dev(np.ascontiguousarray(dyt.T)), None, _dev(dense, bf16), Wd, d, None, dW, None, ws=ws)
+    want = dyt[np.arange(d_out), at].astype(np.float64)[:, None] * dense.astype(np.float64)[at]
+    _close("dW", dW, want, 3 * U * np.abs(want))

@@ -354,3 +354,36 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
                  lambda: M.mtgnn_selective_scan_bwd(q, None, inp, d, None, g, None)):
         with pytest.raises(M.MtgnnError, match="current device is 0"):
             call()
+
+
+def test_a_lost_part_shows_in_a_single_product():
+    """What the GPU tests hold single products to (3 u): six products of bfloat16 parts keep to it, three where one operand
+    is bfloat16 itself, and none of those can be left out."""
+    from itertools import product
+
+    from oracle.bf16 import round_bf16
+    rs = np.random.RandomState(5)
+    a, b = (((1 + rs.rand(20000)) * rs.choice([-1, 1], 20000)).astype(np.float32) for _ in range(2))
+
+    def parts(v):
+        out, left = [], v.astype(np.float32)
+        for _ in range(3):
+            out.append(round_bf16(left))
+            left = (left - out[-1]).astype(np.float32)
+        return out
+
+    def off(terms, w):
+        s = np.zeros_like(a)
+        for i, j in sorted(terms, key=lambda t: -sum(t)):   # the smallest first, each sum rounded to float32
+            s = (s + parts(a)[i].astype(np.float64) * parts(w)[j].astype(np.float64)).astype(np.float32)
+        exact = a.astype(np.float64) * w.astype(np.float64)
+        return float((np.abs(s - exact) / np.abs(exact)).max()) * 2.0 ** 24
+
+    six = [(i, j) for i, j in product(range(3), range(3)) if i + j < 3]
+    assert off(six, b) < 3
+    for t in six:
+        assert off([s for s in six if s != t], b) > 30, t
+    three = [(0, 0), (1, 0), (2, 0)]
+    assert off(three, round_bf16(b)) < 3
+    for t in three:
+        assert off([s for s in three if s != t], round_bf16(b)) > 30, t
