@@ -1148,3 +1148,79 @@ def test_linear_products_are_exact_to_float32(size, sides, sides_bf16, bf16):
     M.mtgnn_linear_bwd(_dev(np.ascontiguousarray(dyt.T)), None, _dev(dense, bf16), Wd, d, None, dW, None, ws=ws)
     want = dyt[np.arange(d_out), at].astype(np.float64)[:, None] * dense.astype(np.float64)[at]
     _close("dW", dW, want, 3 * U * np.abs(want))
+
+
+# --------------------------------------------------------------------------- chunks of several tiles
+
+# sequences that end at a chunk's edge (rows 48, 72 and 96, with chunks of 16, 24 and 32), inside a tile, in a tile's
+# last row, over many chunks, and some shorter than the convolution is wide
+EDGES = [48, 1, 23, 2, 3, 19, 0, 300, 8, 1, 1, 400, 5, 0, 0, 33, 2, 350, 16, 1, 390, 7, 40]
+
+
+def _conv_check(q, d, width, act, bias, wide, bf16, slots=True):
+    rs = _gen(15)
+    x, w = _vals(rs, bf16, q.rows, d), _vals(rs, bf16, width, d)
+    b = _vals(rs, False, d) if bias else None
+    dy, table = _vals(rs, False, q.rows, d), _vals(rs, bf16, q.n_slots, width - 1, d)
+    dims = M.conv_dims(d, width, M.BF16 if bf16 else M.F32, ACTS.index(act))
+    place = _in_wide if wide else _dev
+    X, Wd, bd = place(q.rows_of(x), bf16), _dev(w, bf16), None if b is None else _dev(b)
+    y, st_in = _marked(q.total, d, bf16, wide), _dev(table, bf16)
+    st_out, save = torch.full_like(st_in, MARK), M.alloc_bytes(M.causal_conv_save_bytes(dims, q.max_seq))
+    M.mtgnn_causal_conv(q.q, X, Wd, bd, dims, st_in, st_out, y, save=save)
+    dx, dw, db = _marked(q.total, d, wide=wide), _marked(width, d), _marked(1, d)[0] if bias else None
+    ws = M.alloc_bytes(M.causal_conv_ws_bytes(dims, q.total))
+    M.mtgnn_causal_conv_bwd(q.q, place(q.rows_of(dy), False), X, Wd, bd, dims, save, dx, dw, db, ws)
+    first = q.first(table)
+    want = layer.conv(q.lens, x, w, b, act, first, dy.astype(np.float64))
+    mag = layer.conv(q.lens, x, w, b, act, first, dy.astype(np.float64), magnitude=True)
+    k = (2 * width + 12) * U
+    _close("y", q.cut(y), want["y"], k * mag["y"], bf16)
+    _close("dx", q.cut(dx), want["dx"], k * mag["dx"])
+    _close("dw", dw, want["dw"], (k + q.rows * U) * mag["dw"])
+    if bias:
+        _close("db", db, want["db"], (k + q.rows * U) * mag["db"])
+    q.untouched(y, dx)
+    q.check_table("state", st_out, want["state"], 0.0)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d,width,act,bias,wide", [
+    (8192, 4, "silu", True, False),     # 8,192 waves share the 1,650 rows: chunks of 32
+    (16384, 3, "silu", False, False),   # 56
+    (8191, 2, "none", True, True),      # a channel a lane
+    (4096, 4, "silu", True, True)])     # 16
+@pytest.mark.parametrize("lead", [0, 5])
+def test_conv_of_several_tiles_a_chunk(lead, d, width, act, bias, wide, bf16):
+    q = Layout(EDGES, lead, 3, 2)
+    _conv_check(q, d, width, act, bias, wide, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d,n,groups,lead", [(2048, 16, 1, 0), (1024, 33, 2, 3), (768, 64, 1, 0), (2048, 5, 1, 3), (1088, 40, 1, 0)])
+def test_scan_of_several_tiles_a_chunk(d, n, groups, lead, bf16):
+    """4,096 waves share the rows: chunks of two tiles and more, with one wave a channel or two, and one to four of the
+    backward's; states read and written in one table give the same bits."""
+    q = Layout(EDGES, lead, 3, 2)
+    v = _scan_case(q, d, n, groups, True, True, True, True, bf16)
+    dims = M.scan_dims(d, n, groups, M.BF16 if bf16 else M.F32)
+    y, st_out, g, (keep, st_in, ws) = _scan_run(q, v, dims, bf16, True, False)
+    _scan_check(q, v, dims, y, st_out, g, bf16, True)
+    _, inp = _scan_inputs(q, v, dims, bf16, False)
+    y2 = _marked(q.total, d, bf16)
+    M.mtgnn_selective_scan(q.q, inp, dims, st_in, st_in, y2, ws=ws)
+    moved = torch.from_numpy(q.slot[q.has & (np.asarray(q.lens) > 0)]).cuda()
+    assert torch.equal(q.cut(y2), q.cut(y)) and torch.equal(st_in[moved], st_out[moved])
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d,n,groups", [(70, 16, 1), (40, 33, 1), (128, 8, 4)])
+def test_scan_of_many_chunks(d, n, groups, bf16):
+    """Chunks of eight rows, more than 256 of them: 64 runs of chunks hand on to each other, both ways."""
+    q = Layout(EDGES + [300, 1, 2, 399, 0, 64, 300], 2, 3, 2)
+    assert (q.total + 7) // 8 > 256
+    v = _scan_case(q, d, n, groups, True, True, True, True, bf16)
+    v["A"] *= np.float32(0.02)   # slow decays: what enters a sequence's first chunk is still there in its last
+    dims = M.scan_dims(d, n, groups, M.BF16 if bf16 else M.F32)
+    y, st_out, g, _ = _scan_run(q, v, dims, bf16, True, False)
+    _scan_check(q, v, dims, y, st_out, g, bf16, True)
