@@ -545,9 +545,10 @@ mtgnn_status mtgnn_time_projection_bwd(const int32_t* q_node, const float* q_t, 
                                        float* db_p, float* d_mem, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------ a state-space layer over sequences
- * A third kind of memory update beside the GRU (mtgnn_gru_update) and the recurrent cell (mtgnn_rnn_update):
- * instead of a node's last message it takes all of them, in time order.  Its operators are a linear layer, a
- * short causal convolution per channel and a selective state space scan; a layer is
+ * Operators of a memory update beside the GRU (mtgnn_gru_update) and the recurrent cell (mtgnn_rnn_update) that
+ * takes all of a node's messages, in time order, instead of its last one: a linear layer, a short causal
+ * convolution per channel and a selective state space scan.  The caller chains them and lays the messages out by
+ * node; no step of this library does.  A layer is
  *   linear -> conv -> linear (delta, B, C) -> scan with gate -> linear with residual.
  * Activations, weights of products and of the convolution, and the convolution's states are in the dims'
  * dtype; biases, A, D, the scan's states and every gradient are float32; every sum and state is held in
@@ -581,7 +582,7 @@ typedef struct {
  *   pre -- [max_rows, d_out] float32 out for mtgnn_linear_bwd, or NULL.
  * act: silu(p) = p / (1 + e^-p), gelu(p) = p (1 + erf(p / sqrt 2)) / 2.  y may be residual (same stride); it
  * may not overlap x.  A product is exact to float32: bfloat16 operands multiply on the bfloat16 matrix
- * instructions; float32 ones there too, as three bfloat16 parts each.
+ * instructions; float32 ones there too, as three bfloat16 parts each (below 2^-109 the parts hold fewer bits).
  * Workspace: mtgnn_linear_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too.  Rows at or beyond
  * n_rows are left untouched. */
 typedef struct {

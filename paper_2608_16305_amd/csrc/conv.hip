@@ -6,9 +6,9 @@
 // W - 1 before it are requested together, and a row is read again only as another tile's margin (11 reads for 8, from
 // the caches).  Where a sequence starts, its first W - 1 rows take the values that are missing from its slot's
 // state instead of from the rows above.  Reading and writing the rows bounds it: 32,768 rows x 2,048 in bfloat16 take
-// 75 us forward (3.6 TB/s) and 173 us backward (3.9 TB/s: x, dy in, dx out); 4,000 single rows 28 us with their
-// states in the caches, 38 without.  8,000 rows x 100 of 6,000 sequences take 15 us, a chain of dependent reads (offsets, slot, state)
-// in one wave a SIMD, and 4 us for the new states.
+// 80 us forward (3.4 TB/s) and 164 us backward (4.1 TB/s: x, dy in, dx out); 4,000 single rows 28 us with their
+// states in the caches, 38 without.  8,000 rows x 100 of 6,000 sequences take 9 us, a chain of dependent reads (count, search,
+// offsets, rows, state) in one wave a SIMD, and 4 us for the new states.
 #include <algorithm>
 #include <initializer_list>
 

@@ -14,10 +14,10 @@
 // first operand is C: a lane then holds four neighbouring columns of a row.  Tiles leave through LDS, so that
 // rows are written in 128 to 256 bytes, and the epilogue is a loop and not 64 copies of it.
 //
-// Measured (each alone, us): data gradient 8,192 x 2,048 -> 1,024 from a float32 slope (three products) 138, 747
-// TFLOP/s of products; weight gradient 145 + 11 for the shares; there the LDS traffic of the three parts (reads and
-// writes as long as the matrix instructions) bounds it.  Float32 8,000 x 300 -> 200: 20 us, five dependent steps of
-// 500 blocks, so latency.
+// Measured (us, kernel trace, median of 53; calls in a row hide 1 or 2 of each): data gradient 8,192 x 2,048 -> 1,024 from a
+// float32 slope (three products) 134, 770 TFLOP/s of products; weight gradient 137 + 11 for the shares; there the LDS
+// traffic of the three parts (reads and writes as long as the matrix instructions) bounds it.  Float32 8,000 x 300 -> 200:
+// 19 (17 in a row), five dependent steps of 500 blocks, so latency.
 #include <algorithm>
 
 #include "bf16_split.h"
@@ -410,8 +410,8 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
 }
 
 // The same for bfloat16 operands that are contiguous along k, K a multiple of 64, where there are enough tiles of
-// 256 x 256 for the card: 326 us alone, 844 TFLOP/s, at 16,384 x 4,096 -> 2,048 with a residual (512 tiles), 452 in tiles of
-// 128; 68 against 82 us at 8,192 x 1,024 -> 2,048 with pre (256 tiles: one a CU, 96 MB written at its end).  What is
+// 256 x 256 for the card: 304 us in a row, 904 TFLOP/s, at 16,384 x 4,096 -> 2,048 with a residual (512 tiles; in a kernel
+// trace 319, 305 at the least), 452 in tiles of 128; 67 against 82 us at 8,192 x 1,024 -> 2,048 with pre (256 tiles: one a CU, 96 MB written at its end).  What is
 // left: waits for LDS, whose reads take 0.75 of the cycles of the matrix instructions, and the epilogue, which no other block
 // of the CU hides.  Eight waves, 128 rows x 64 columns each: a matrix instruction needs 0.75 of the LDS bytes
 // that it needs with 64 x 64.  Rows go straight to LDS, lane l of a load to unit l % 8 of row l / 8; the units'
@@ -569,6 +569,10 @@ size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 // against 46 at 272, 36 against 20 at 126.  Long sums with few tiles (weight gradients) take 128 and share the sum:
 // 170 + 11 us against 280 (2,048 x 1,024 from 8,192 rows).  Shares have 128 k or more: 2,399 x 472 -> 100 takes 11 + 4.5 us
 // in shares of 157, 13 + 5 in shares of 67, 22 without.
+// Where these rules do not hold: they count tiles, not columns, so from 51,073 rows on a few outputs take the large tiles
+// too (60,000 x 100 -> 32 24 us in float32, 16 in bfloat16; 40,000 rows 13 and 13); and forward calls of 4,096 inputs and more
+// take 128 as weight gradients do, which costs those of few tiles up to half (1,000 x 8,192 -> 300 in bfloat16 34 against
+// 24 us in tiles of 64, 300 x 4,096 -> 100 in float32 20 against 15) and gains with many (2,000 x 8,192 -> 600 63 against 87).
 struct Plan {
   int T, split;
   int64_t tr, tc;

@@ -22,9 +22,10 @@
 // Vector instructions bound it: per row, channel and state an exponential (four times an ordinary instruction's
 // cycles) and three or four products and sums, once in k_scan_local and once in k_scan_out, against 8 bytes per row and
 // channel in bfloat16.  Measured with 16 states, bfloat16, gate and skip: 32,768 rows x 2,048 of 5 sequences take
-// 234 (local) + 13 (carry) + 370 us (out), 1.07e9 exponentials in each of local and out, 70 to 85% of the cycles issue vector
-// instructions.  Training, 16,384 x 1,024: 66 + 14 + 113 forward, backward 84 + 14 + 352 + 22 for the sums.  8,000
-// rows x 100 of 6,000 sequences: 14 + 16 + 28 us, reads of states at scattered slots, one after the other.
+// 224 (local) + 14 (carry) + 363 us (out), 1.07e9 exponentials in each of local and out, 70 to 85% of the cycles issue vector
+// instructions; in out some of them move scalar registers that B and C leave no room for.  Training, 16,384 x 1,024:
+// 65 + 15 + 112 forward, backward 82 + 15 + 347 + 22 for the sums.  8,000 rows x 100 of 6,000 sequences: 14 + 17 + 26 us, a
+// chain of dependent reads (count, search, offsets, rows, states), and the carry's latency.
 #include <algorithm>
 
 #include "bf16_split.h"
@@ -424,7 +425,8 @@ __device__ __forceinline__ float carried(float s, float h, float own) {
 // first.  A block has 1024 / RUNS states and channels; each of RUNS threads to one takes a run of chunks, once for
 // what the run hands on, h -> own + decay h, and, after a scan over the runs, once with what enters it.  (One
 // thread over all chunks waited for memory 127 times in turn at 1,013 chunks: 144 us, against 16.)  Latency bounds it.
-// 64 runs from 256 chunks on, else 16: 16.3 against 36 us at 1,013 chunks x 1,600; 29.7 against 13.4 at 128 x 32,768.
+// 64 runs from 256 chunks on, else 16: 16.3 against 36 us at 1,013 chunks x 1,600; 29.7 against 13.4 at 128 x 32,768 (1 us
+// less each than now, with decays in place of their exponents).
 template <int RUNS>
 __global__ __launch_bounds__(1024) void k_scan_carry(ScanP p, int back) {
   constexpr int RUN_COLS = 1024 / RUNS;

@@ -17,7 +17,7 @@ __device__ __forceinline__ float exp_neg(float x) {
   return fmaf(e, r * LN2, e);
 }
 // softplus(u) = max(u, 0) + log1p(e^-|u|).  log1p(v) = 2 atanh(s) with s = v / (2 + v) <= 1/3; atanh(s) / s as the
-// polynomial in s^2 that a Chebyshev fit over [0, 1/9] gives (4e-9 off at most): exact to a few units of the last
+// polynomial in s^2 that a Chebyshev fit over [0, 1/9] gives (8e-9 off at most): exact to a few units of the last
 // place for every v, small ones too, where log(1 + v) has lost v's low bits.
 __device__ __forceinline__ float softplus_(float u) {
   const float v = exp_neg(-fabsf(u));
