@@ -415,10 +415,12 @@ __global__ __launch_bounds__(64 * NW) void k_scan_local(ScanP p) {
 
 // own + 2^s h.  The power's whole part goes to h's exponent: past float32's range it still meets a small h as it would row
 // after row, and a zero one stays zero (an infinite decay times zero is NaN).  h spans 2^277, so s past +-1000 is as at
-// it; where s is NaN own is too.  1 us of k_scan_carry's 14 against a product with exp2(s).
+// it; an infinite one is an infinite step's, 2^s then 0 or infinite (NaN with an infinite or a zero h, as there); where s
+// is NaN own is too.  1 us of k_scan_carry's 14 against a product with exp2(s).
 __device__ __forceinline__ float carried(float s, float h, float own) {
-  s = __builtin_amdgcn_fmed3f(s, -1000.f, 1000.f);
-  return fmaf(__builtin_amdgcn_exp2f(__builtin_amdgcn_fractf(s)), ldexpf(h, (int)floorf(s)), own);
+  const float t = __builtin_amdgcn_fmed3f(s, -1000.f, 1000.f);
+  const float e = __builtin_amdgcn_exp2f(fabsf(s) == INFINITY ? s : __builtin_amdgcn_fractf(t));
+  return fmaf(e, ldexpf(h, (int)floorf(t)), own);
 }
 
 // The state that enters each chunk, in place of E.  back: the same for the flow that runs from the last chunk to the

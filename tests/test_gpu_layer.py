@@ -684,6 +684,20 @@ def test_linear_gradient_in_the_place_of_dy():
     assert torch.equal(wide[:, k:], dx)
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [12, 16])
+def test_scan_of_an_infinite_state_and_an_infinite_step(n, bf16):
+    """A decay of 0 that meets an infinite state (a flow) is NaN in that row, and so in the chunks behind it (before it)."""
+    q, v, dims = _ends_case(n, False, bf16)
+    v["delta"][33, 9], v["x"][33, 9] = np.inf, 1.0      # x is infinite in row 21: of the same sign as the step's own term
+    v["delta"][33, 50] = np.inf                         # dy is infinite in row 40
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = layer.scan(q.lens, *[v[k] for k in ("x", "delta", "A", "B", "C", "D", "z", "bias")], first=q.first(v["table"]),
+                          dy=v["dy"])
+    assert np.isnan(want["y"][33:50, 9]).all() and np.isnan(want["dx"][20:33, 50]).all()
+    _check_ends(q, v, dims, bf16, False)
+
+
 # --------------------------------------------------------------------------- as a layer
 
 def _layer(seed=11, bf16=False, d_msg=36, d=40, n=16, width=4):
