@@ -411,12 +411,13 @@ __global__ __launch_bounds__(NT) void k_product(ProdP p) {
 
 // The same for bfloat16 operands that are contiguous along k, K a multiple of 64, where there are enough tiles of
 // 256 x 256 for the card: 304 us in a row, 904 TFLOP/s, at 16,384 x 4,096 -> 2,048 with a residual (512 tiles; in a kernel
-// trace 319, 305 at the least), 452 in tiles of 128; 67 against 82 us at 8,192 x 1,024 -> 2,048 with pre (256 tiles: one a CU, 96 MB written at its end).  What is
-// left: waits for LDS, whose reads take 0.75 of the cycles of the matrix instructions, and the epilogue, which no other block
-// of the CU hides.  Eight waves, 128 rows x 64 columns each: a matrix instruction needs 0.75 of the LDS bytes
-// that it needs with 64 x 64.  Rows go straight to LDS, lane l of a load to unit l % 8 of row l / 8; the units'
-// swizzle is in the address that the lane reads.  Two buffers, which are two objects, so that the compiler knows that the
-// reads of one do not wait for the loads into the other; a step's loads are a whole step's work ahead.
+// trace 319, 305 at the least), 452 in tiles of 128; 67 against 82 us at 8,192 x 1,024 -> 2,048 with pre (256 tiles: one a
+// CU, 96 MB written at its end).  What is left: waits for LDS, whose reads take 0.75 of the cycles of the matrix
+// instructions, and the epilogue, which no other block of the CU hides.  Eight waves, 128 rows x 64 columns each: a matrix
+// instruction needs 0.75 of the LDS bytes that it needs with 64 x 64.  Rows go straight to LDS, lane l of a load to unit
+// l % 8 of row l / 8; the units' swizzle is in the address that the lane reads.  Two buffers, which are two objects, so that
+// the compiler knows that the reads of one do not wait for the loads into the other; a step's loads are a whole step's work
+// ahead.
 constexpr int BIG = 256, BIG_KS = 64;
 __global__ __launch_bounds__(512, 2) void k_product_big(ProdP p) {
   constexpr int WR = 8, WC = 4, OP = BIG * BIG_KS / 2;   // words of an operand's tile
