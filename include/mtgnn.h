@@ -690,6 +690,88 @@ mtgnn_status mtgnn_selective_scan_step(const int32_t* slot, const int32_t* n_row
                                        const float* state_in, float* state_out, void* y, int64_t ldy,
                                        hipStream_t stream);
 
+/* ------------------------------------------------------------------ a model over all nodes
+ * Operators of a model that is trained to name an event's destination among all nodes, where mtgnn_link_loss tells it from
+ * one other: rows of a table by id, a layer norm, the softmax cross entropy over all nodes, and (below, at mtgnn_adam_step) a
+ * parameter update over any number of tensors.  The caller chains them with the state-space layer's operators, whose
+ * conventions hold: activations and tables in the dims' dtype, norm parameters, biases and every gradient float32, sums in
+ * float32 or more, one rounding of an output; row strides in elements; rows at or beyond n_rows (device count, or NULL:
+ * max_rows) are neither read nor written; workspaces 16-byte aligned.  All results are deterministic.
+ * Calls whose launches would have 2^32 threads or more are refused (MTGNN_EUNSUPPORTED). */
+
+/* Rows of a table by id:  y_r = scale table[ids[r]],  zeros where ids[r] is outside [0, n).
+ *   table [n, d], y [max_rows, d] (dtype; y may not overlap the table); ids [max_rows]. */
+typedef struct {
+  int64_t n;                 /* rows of the table, < 2^31 - 64 */
+  int32_t d, dtype;          /* d <= 2^20 */
+  float scale;               /* finite */
+} mtgnn_embedding_dims;
+mtgnn_status mtgnn_embedding(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
+                             const mtgnn_embedding_dims* dims, void* y, int64_t ldy, hipStream_t stream);
+
+/* Gradient of the table for dy [max_rows, d] float32:  dtable_i = scale sum of dy_r over the rows with ids[r] = i, in a
+ * fixed order; dtable [n, d] is overwritten (zeros for the ids that no row has) and may not overlap dy.
+ * Workspace: mtgnn_embedding_ws_bytes(dims, max_rows). */
+size_t mtgnn_embedding_ws_bytes(const mtgnn_embedding_dims* dims, int64_t max_rows);
+mtgnn_status mtgnn_embedding_bwd(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,
+                                 const mtgnn_embedding_dims* dims, float* dtable, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
+/* Layer norm of each row:  m = mean x,  q = 1 / sqrt(mean (x - m)^2 + eps),  h = (x - m) q,  y = gamma h + beta.
+ *   x, y [max_rows, d] (dtype; y may be x with the same stride where no backward follows, else no overlap);
+ *   gamma, beta [d] float32, each or NULL (ones, zeros);
+ *   stats -- [max_rows, 2] float32 out, m and q, for mtgnn_layer_norm_bwd, or NULL. */
+typedef struct {
+  int32_t d, dtype;          /* d <= 2^20 */
+  float eps;                 /* finite, >= 0 */
+} mtgnn_norm_dims;
+mtgnn_status mtgnn_layer_norm(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const float* gamma,
+                              const float* beta, const mtgnn_norm_dims* dims, void* y, int64_t ldy, float* stats,
+                              hipStream_t stream);
+
+/* Backward of mtgnn_layer_norm for dy [max_rows, d] float32: with g = dy gamma,
+ *   dx = q (g - mean g - h mean(g h)) + past,  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy.
+ *   x, stats -- the forward's;  past -- [max_rows, d] float32, a gradient that reaches x beside the norm (a residual
+ *           stream's), or NULL;  dx [max_rows, d] float32 may be in dy's or past's place (same stride), else it may not
+ *           overlap dy, past or x;  dgamma, dbeta [d] each or NULL, overwritten (zeros without rows).
+ * Workspace: mtgnn_layer_norm_ws_bytes(dims, max_rows) (none where dgamma and dbeta are NULL). */
+size_t mtgnn_layer_norm_ws_bytes(const mtgnn_norm_dims* dims, int64_t max_rows);
+mtgnn_status mtgnn_layer_norm_bwd(const float* dy, int64_t lddy, const void* x, int64_t ldx, const float* stats,
+                                  const int32_t* n_rows, int64_t max_rows, const float* gamma, const float* past, int64_t ldp,
+                                  const mtgnn_norm_dims* dims, float* dx, int64_t lddx, float* dgamma, float* dbeta, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/* Softmax cross entropy of each row's label over all n classes:
+ *   l_r = x_r W^T + b,  loss_r = log sum_c exp l_rc - l_r,label[r],  loss = mean of loss_r over the rows that have a label.
+ *   x [max_rows, d], W [n, d] (rows dense) in the dtype; b [n] float32 or NULL (-inf takes a class out);
+ *   label [max_rows]: a row whose label is outside [0, n) has none, counts nothing (whatever its x holds) and has the loss 0;
+ *   loss -- [1] float32 out (0 where no row has a label);  row_loss -- [max_rows] float32 out, or NULL;
+ *   save -- mtgnn_softmax_loss_save_bytes bytes for the backward (it keeps a copy of x's rows), or NULL.
+ * A row all of whose logits are -inf has the loss NaN; an infinite or NaN element of x or W makes the logits that it enters
+ * infinite or NaN.  Logits are exact to float32, formed as mtgnn_linear's products are; they are not kept: memory beside
+ * the copies of x (and of W where it is float32 or d % 8 != 0) grows with max_rows n / 128.
+ * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too. */
+typedef struct {
+  int32_t n, d, dtype;       /* n < 2^31 - 64, d <= 2^20 */
+} mtgnn_loss_dims;
+size_t mtgnn_softmax_loss_save_bytes(const mtgnn_loss_dims* dims, int64_t max_rows);
+size_t mtgnn_softmax_loss_ws_bytes(const mtgnn_loss_dims* dims, int64_t max_rows, int32_t backward);
+mtgnn_status mtgnn_softmax_loss(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W,
+                                const float* b, const int32_t* label, const mtgnn_loss_dims* dims, float* loss,
+                                float* row_loss, void* save, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Backward of mtgnn_softmax_loss for the loss's gradient dloss ([1] float32, device, or NULL: 1): with
+ *   P_rc = (exp(l_rc) / sum exp l_r - [c = label[r]]) dloss / rows with a label  (0 in the rows without one),
+ *   dx = P W [max_rows, d],  dW = P^T x [n, d],  db = column sums of P [n],  float32, each or NULL, overwritten (dx in the
+ * rows below n_rows).  n_rows, W, b, label, save: the forward's, W and b unchanged.  dx may not overlap W or dW.
+ * The classes are taken in pieces: a piece's P, in bfloat16 parts (two beside bfloat16 operands: 2^-17 of an element; three
+ * beside float32), takes a gigabyte of the workspace at most where that is 256 classes or more.
+ * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 1). */
+mtgnn_status mtgnn_softmax_loss_bwd(const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
+                                    const int32_t* label, const mtgnn_loss_dims* dims, const void* save, const float* dloss,
+                                    float* dx, int64_t lddx, float* dW, float* db, void* ws, size_t ws_bytes,
+                                    hipStream_t stream);
+
 /* ------------------------------------------------------------------ adaptive runtime controller
  * The decisions of one worker's runtime controller (Section V, Algorithm 2), kept on the host:
  *   gradient-norm EMA (Eq. 6):   g_bar = g_r if g_bar was 0, else alpha g_r + (1 - alpha) g_bar;
@@ -756,6 +838,31 @@ mtgnn_status mtgnn_adam_step(float* const* params, const float* const* grads, fl
                              void* const* shadow, const int64_t* sizes, int32_t n, const mtgnn_adam_config* cfg,
                              hipStream_t stream);
 
+/* One AdamW step (decoupled weight decay, bias-corrected) over n tensors, any number, in place:
+ *   m = beta1 m + (1 - beta1) grad,  v = beta2 v + (1 - beta2) grad^2,
+ *   param = param (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * A tensor (n elements, dense, at any float's address; no two share memory; n = 0: skipped):
+ *   param, grad -- float32;  shadow -- bfloat16 copy of the updated parameter, or NULL;  decay -- its weight decay;
+ *   m_exp, v_exp NULL: m, v are float32;
+ *   m_exp, v_exp given: the states take 8 bits.  m holds codes of m, v codes of sqrt(v), in e4m3 (4 bits of exponent, bias 7;
+ *           3 of mantissa; 448 the largest; 0x7f NaN), in units of 2^(e - 127) for each 32 elements, e = m_exp[i / 32],
+ *           v_exp[i / 32] ([ceil(n / 32)], the least e that keeps the block's largest within 448).  Codes are rounded to the
+ *           nearest (ties to even) from m and v in 64 bits, a v that is not zero never to zero; what is not finite becomes
+ *           NaN.  Zeroed bytes are zeros.  The parameter is updated from m and v before that rounding.
+ * The descriptions (host) are read during the call.  t of cfg, or where step is given the device count *step (>= 1; a captured
+ * call then follows it). */
+typedef struct {
+  float* param;
+  const float* grad;
+  void *m, *v;
+  uint8_t *m_exp, *v_exp;
+  uint16_t* shadow;
+  int64_t n;
+  float decay;
+} mtgnn_adamw_tensor;
+mtgnn_status mtgnn_adamw_step(const mtgnn_adamw_tensor* tensors, int64_t n, const mtgnn_adam_config* cfg,
+                              const int32_t* step, hipStream_t stream);
+
 /* Temporal adjacency of a whole stream (built once, offline; outside the step).
  * Event e = (src[e], dst[e], t[e]) with eid e gives two entries: (node src,
  * nbr dst, role 0) and (node dst, nbr src, role 1).  Entries are grouped by
@@ -785,7 +892,8 @@ mtgnn_status mtgnn_build_temporal_csr(const int32_t* src, const int32_t* dst, co
  * the summed duration in milliseconds and the number of timed launches, and
  * disarms the timer.  Host-side state: use from one host thread.
  * The products of mtgnn_linear and its backward carry a second name, by the side
- * of their tiles: linear_64, linear_128, linear_256. */
+ * of their tiles: linear_64, linear_128, linear_256; those of mtgnn_softmax_loss
+ * and its backward by what they make: loss_stat, loss_prob, loss_dx, loss_dw. */
 mtgnn_status mtgnn_timer_start(const char* kernel, int max_launches);
 mtgnn_status mtgnn_timer_stop(double* total_ms, int* launches);
 

@@ -282,4 +282,31 @@ mtgnn_status scan_step_impl(const int32_t* slot, const int32_t* n_rows, int64_t 
                             const mtgnn_scan_inputs* in, const mtgnn_scan_dims* d, const float* state_in,
                             float* state_out, void* y, int64_t ldy, hipStream_t s);
 
+// a model over all nodes (embed.hip, norm.hip, softmax_loss.hip, adamw.hip; arguments as in mtgnn.h, validated)
+bool embed_fits(const mtgnn_embedding_dims* d, int64_t rows, bool back);
+size_t embed_ws(const mtgnn_embedding_dims* d, int64_t rows);
+mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
+                        const mtgnn_embedding_dims* d, void* y, int64_t ldy, hipStream_t s);
+mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,
+                            const mtgnn_embedding_dims* d, float* dtable, void* ws, size_t ws_bytes, hipStream_t s);
+int64_t norm_threads(const mtgnn_norm_dims* d);   // the most threads of a launch to a row
+size_t norm_ws(const mtgnn_norm_dims* d, int64_t rows);
+mtgnn_status norm_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const float* gamma,
+                       const float* beta, const mtgnn_norm_dims* d, void* y, int64_t ldy, float* stats, hipStream_t s);
+mtgnn_status norm_bwd_impl(const float* dy, int64_t lddy, const void* x, int64_t ldx, const float* stats,
+                           const int32_t* n_rows, int64_t max_rows, const float* gamma, const float* past, int64_t ldp,
+                           const mtgnn_norm_dims* d, float* dx, int64_t lddx, float* dgamma, float* dbeta, void* ws,
+                           hipStream_t s);
+bool loss_fits(const mtgnn_loss_dims* d, int64_t rows);
+size_t loss_save(const mtgnn_loss_dims* d, int64_t rows);
+size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back);
+mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
+                       const int32_t* label, const mtgnn_loss_dims* d, float* loss, float* row_loss, void* save, void* ws,
+                       hipStream_t s);
+mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* W, const float* b, const int32_t* label,
+                           const mtgnn_loss_dims* d, const void* save, const float* dloss, float* dx, int64_t lddx, float* dW,
+                           float* db, void* ws, hipStream_t s);
+mtgnn_status adamw_impl(const mtgnn_adamw_tensor* tensors, int64_t n, const mtgnn_adam_config* cfg, const int32_t* step,
+                        hipStream_t s);
+
 }  // namespace mtgnn

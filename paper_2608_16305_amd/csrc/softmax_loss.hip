@@ -1,0 +1,746 @@
+// Softmax cross entropy of each row's label over all classes, and its gradients, without the rows x classes logits:
+//   l = x W^T + b,  loss_r = log sum_c exp l_rc - l_r,label,  loss = their mean over the rows with a label;
+//   P = softmax(l) - [c is the row's label],  dx = P W,  dW = P^T x,  db = column sums of P, each times dloss / rows.
+//
+// The forward's product leaves per tile of columns each row's largest logit and the sum of exponentials relative to it; a row's
+// are then joined.  The backward takes the classes in pieces: a piece's logits are formed again, become P in the workspace, and
+// two products with W and x take it from there.  So 8 rows x classes x width operations are done where 6 are needed, and a
+// piece of P, not all of it, is in memory.
+//
+// All products run on the bfloat16 matrix instructions with float32 sums.  bfloat16 x and W enter as they are; float32 ones as
+// three bfloat16 parts (24 bits), six products of parts for one of theirs.  P is held as two parts beside bfloat16 (16
+// bits: an element is off by 2^-17 of itself at most, where the exponential of a float32 logit is off by |l| 2^-24 or more; one
+// part would be 2^-9), as three beside float32.
+//
+// Rows without a label are left out before anything is computed: the others' x is copied, row after row, padded with
+// zeros to whole steps.  A W that is not a multiple of 16 bytes wide, or float32, is copied into parts likewise.
+#include <algorithm>
+#include <cmath>
+
+#include "gemm.h"
+#include "ops.h"
+#include "words.h"
+
+namespace mtgnn {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+
+constexpr int KS = 64;          // a step of the sums
+constexpr int CHUNK = 1024;     // rows whose labels are counted together
+constexpr int ROWS = 16;        // rows that a block copies
+constexpr float LOG2E = 1.4426950408889634f;
+
+__host__ __device__ inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+// --------------------------------------------------------------------------- rows with a label
+
+__device__ __forceinline__ bool has_label(const int32_t* label, int64_t r, int64_t rows, int n) {
+  return r < rows && (uint32_t)label[r] < (uint32_t)n;
+}
+
+__global__ __launch_bounds__(CHUNK) void k_loss_count(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n,
+                                                      int32_t* counts) {
+  __shared__ int s[CHUNK / 64];
+  const int64_t r = (int64_t)blockIdx.x * CHUNK + threadIdx.x;
+  const uint64_t have = __ballot(has_label(label, r, eff_count(max_rows, n_rows), n));
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __popcll(have);
+  __syncthreads();
+  if (threadIdx.x) return;
+  int v = 0;
+  for (int w = 0; w < CHUNK / 64; ++w) v += s[w];
+  counts[blockIdx.x] = v;
+}
+
+__device__ __forceinline__ int block_sum(int v, int* s) {   // over 256 threads
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = s[0] + s[1] + s[2] + s[3];
+  __syncthreads();
+  return v;
+}
+
+// A row's eight elements from c on (zeros from d on) as the parts of a padded matrix.
+template <typename T>
+__device__ __forceinline__ void put_parts(const T* row, int c, int d, uint16_t* to, int64_t plane) {
+  float v[8];
+  load_some(row + c, d - c, v);
+  if constexpr (sizeof(T) == 2) {
+    *(uint4*)to = make_uint4(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]), cvt2_bf16(v[4], v[5]), cvt2_bf16(v[6], v[7]));
+  } else {
+    uint32_t h[4], m[4], l[4];
+    split_words<true>(v, h, m, l);
+    *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
+    *(uint4*)(to + plane) = make_uint4(m[0], m[1], m[2], m[3]);
+    *(uint4*)(to + 2 * plane) = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+// The rows with a label, one after the other: idx (which rows), lab, xc (their x in parts, zeros behind the last one to a
+// whole step); their number.  Blocks past those of the rows fill in the zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
+                                                   int64_t max_rows, int n, int d, int dp, const int32_t* counts,
+                                                   int32_t* count, int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane,
+                                                   float* row_loss) {
+  __shared__ int s[4], src[ROWS];
+  const int64_t rows = eff_count(max_rows, n_rows), r0 = (int64_t)blockIdx.x * ROWS;
+  const int chunks = (int)cdiv(max_rows, CHUNK), units = dp / 8;
+  const bool behind = r0 >= max_rows;
+  const int mine = behind ? chunks : (int)(r0 / CHUNK);
+  int v = 0;
+  for (int i = threadIdx.x; i < mine; i += 256) v += counts[i];
+  if (!behind)
+    for (int64_t r = (int64_t)mine * CHUNK + threadIdx.x; r < r0; r += 256) v += has_label(label, r, rows, n);
+  const int first = block_sum(v, s);
+  if (behind) {
+    const int j0 = (int)(r0 - up(max_rows, ROWS));
+    if (j0 == 0 && threadIdx.x == 0) *count = first;
+    const int64_t end = up(first, KS);
+    for (int e = threadIdx.x; e < ROWS * units; e += 256) {
+      const int64_t r = first + j0 + e / units;
+      if (r >= end) break;
+#pragma unroll
+      for (int p = 0; p < (sizeof(T) == 2 ? 1 : 3); ++p)
+        *(uint4*)(xc + p * plane + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    return;
+  }
+  int here = 0;
+  if (threadIdx.x < 64) {
+    const int64_t r = r0 + threadIdx.x;
+    const bool ok = threadIdx.x < ROWS && has_label(label, r, rows, n);
+    const uint64_t have = __ballot(ok);
+    const int at = __popcll(have & ((uint64_t(1) << threadIdx.x) - 1));
+    here = __popcll(have);
+    if (ok) {
+      src[at] = (int)threadIdx.x;
+      idx[first + at] = (int32_t)r;
+      lab[first + at] = label[r];
+    } else if (threadIdx.x < ROWS && r < rows && row_loss) {
+      row_loss[r] = 0.f;
+    }
+    if (threadIdx.x == 0) s[0] = here;
+  }
+  __syncthreads();
+  here = s[0];
+  for (int e = threadIdx.x; e < here * units; e += 256) {
+    const int k = e / units, c = e % units * 8;
+    put_parts(x + (r0 + src[k]) * ldx, c, d, xc + (int64_t)(first + k) * dp + c, plane);
+  }
+}
+
+// W in parts, padded.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_table(const T* W, int64_t n, int d, int dp, uint16_t* to, int64_t plane) {
+  const uint32_t units = dp / 8, e = blockIdx.x * 256 + threadIdx.x;
+  const int64_t c = e / units;
+  const int u = (int)(e % units) * 8;
+  if (c < n) put_parts(W + c * d, u, d, to + c * dp + u, plane);
+}
+
+// --------------------------------------------------------------------------- the products
+
+enum { STAT, PROB, DX, DW };
+
+struct Prod {
+  const uint16_t *A, *B;         // A: the result's rows, B: its columns
+  int64_t lda, ldb, planeA, planeB;
+  uint32_t codeA, codeB;         // the parts of each segment, two bits each
+  int segs;
+  int64_t rows, cols, K;         // the most rows; K: of a segment
+  int64_t dimA, dimB;            // elements of an operand's line that may be read (A's along the sum are whole steps)
+  int64_t tr, tc;                // tiles
+  const int32_t* count;          // rows with a label: bounds the rows (STAT, PROB, DX) or K (DW)
+  // epilogue
+  const float* b;                // of the first column on
+  const int32_t *lab, *idx;
+  int64_t c0;                    // first column's class
+  float2* part;                  // STAT: [tc][ld_part]
+  int64_t ld_part;
+  float* at_label;
+  const float2* stat;            // PROB: largest logit, 1 / sum
+  uint16_t* P;
+  int64_t ldp, planeP;
+  int parts;
+  float* cols_part;              // [rows / 64][ldp] column sums of P, or NULL
+  float* out;
+  int64_t ldo;
+  const float* dloss;
+  int add;
+};
+
+// A's lines are contiguous along the sum (AK) or across it; so are B's (BK).  T x T tiles, a wave has 16 WR x 64 of one.
+// Lines go straight to LDS, 16 bytes a lane.  Along the sum: a line's eight units are swizzled by the line, as in
+// linear.hip.  Across it: a k's 32-byte units by k, and the transposing read of 4 k x 16 columns gives a lane its four k;
+// the 16 lanes of such a read, and their neighbours, meet every bank once.
+template <bool AK, bool BK, int T>
+struct Tiles {
+  static constexpr int NW = T == 256 ? 8 : 4, WCOLS = T / 64, WR = T == 256 ? 8 : 4, WC = 4;
+  static constexpr int OP = T * KS / 2;   // words of an operand's tile
+  typedef __attribute__((address_space(3))) void* lds_ptr;
+  typedef __attribute__((address_space(3))) s16x4* lds_tr;
+
+  // A lane's place in its wave's load i: line (row) and k of a step.
+  __device__ __forceinline__ static int k_of(bool along, int wid, int lane, int i) {
+    constexpr int UPR = T / 8, KR = 64 / UPR;
+    return along ? 8 * ((lane & 7) ^ (lane >> 3 & 7)) : (4 * wid + i) * KR + lane / UPR;
+  }
+  // This wave's four loads of an operand: bytes from the tile's first line at a step's first k.  (Below 2^32: 256 lines of
+  // 2^22 elements, or 64 of them.)
+  template <bool K_>
+  __device__ __forceinline__ static void sources(int64_t ld, int64_t lines, int64_t dim, int wid, int lane, uint32_t (&off)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k_of(K_, wid, lane, i);
+      if constexpr (K_) {
+        const int row = 32 * wid + 8 * i + (lane >> 3);
+        off[i] = 2u * ((uint32_t)min((int64_t)row, lines - 1) * (uint32_t)ld + k);
+      } else {
+        constexpr int UPR = T / 8;
+        const int q = lane % UPR, col = ((q >> 1 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 2 + (q & 1)) * 8;
+        off[i] = 2u * ((uint32_t)k * (uint32_t)ld + (uint32_t)min((int64_t)col, dim - 8));
+      }
+    }
+  }
+  // The loads of a step that starts at `p`.  `left`: how many of its k may be read; the lanes past them read the step's first
+  // (it meets zeros of the other operand).
+  template <bool K_, bool END>
+  __device__ __forceinline__ static void fill(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[4], int64_t ld, int64_t left,
+                                              int wid, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t o = off[i];
+      if (END && left < KS) {
+        const int k = k_of(K_, wid, lane, i);
+        if (k >= left) o -= 2u * (uint32_t)k * (K_ ? 1u : (uint32_t)ld);
+      }
+      __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (4 * wid + i) * 256), 16, 0, 0);
+    }
+  }
+  // A lane's byte in an operand's tile for line 0 and the step's first half, and what a line of 16 l and the half add to it.
+  template <bool K_>
+  __device__ __forceinline__ static uint32_t place(int fr, int fg) {
+    if (K_) return fr * (2 * KS) + (fg ^ (fr & 7)) * 16;
+    return (8 * fg + (fr >> 2)) * (2 * T) + ((fr >> 2) | (fg & 1) << 2) * 32 + (fr & 3) * 8;
+  }
+  template <bool K_>
+  __device__ __forceinline__ static bf16x8_t frag(uint32_t* buf, uint32_t at, int l, int kk) {
+    if constexpr (K_) {
+      return __builtin_bit_cast(bf16x8_t, *(const uint4*)((char*)buf + ((at ^ 64 * kk) + l * 16 * 2 * KS)));
+    } else {
+      char* a = (char*)buf + ((at ^ 32 * l) + kk * 32 * 2 * T);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)a);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(a + 4 * 2 * T));
+      return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// Blocks run on the 8 XCDs in turn, each with its own L2: a contiguous eighth of the tiles to each, in groups of eight tiles of
+// rows by all of columns, so that the blocks that run together share lines of both operands.
+__device__ __forceinline__ void my_tile(const Prod& p, int64_t& tr, int64_t& tc) {
+  const int64_t L = blockIdx.x, n = p.tr * p.tc, full = n & ~int64_t(7);
+  const int64_t V = L < full ? (L & 7) * (full >> 3) + (L >> 3) : L;
+  constexpr int64_t G = 8;
+  const int64_t group = V / (G * p.tc), in = V % (G * p.tc), h = min(G, p.tr - group * G);
+  tr = group * G + in % h;
+  tc = in / h;
+}
+
+template <int KIND, bool AK, bool BK, int T>
+__global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss_product(Prod p) {
+  using X = Tiles<AK, BK, T>;
+  constexpr int WR = X::WR, WC = X::WC;
+  __shared__ __align__(1024) uint32_t bufA[2 * X::OP], bufB[2 * X::OP];
+  int64_t tr, tc;
+  my_tile(p, tr, tc);
+  const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
+  const int64_t K = KIND == DW ? up(count, KS) : p.K;
+  const int64_t r0 = tr * T, c0 = tc * T;
+  if (r0 >= rows) return;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wid / X::WCOLS * (16 * WR), wc = wid % X::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
+  uint32_t offA[4], offB[4];
+  X::template sources<AK>(p.lda, rows - r0, p.dimA - (AK ? 0 : r0), wid, lane, offA);
+  X::template sources<BK>(p.ldb, p.cols - c0, p.dimB - (BK ? 0 : c0), wid, lane, offB);
+  const uint16_t *fromA = p.A + r0 * (AK ? p.lda : 1), *fromB = p.B + c0 * (BK ? p.ldb : 1);
+  f32x4 acc[WR][WC];
+#pragma unroll
+  for (int i = 0; i < WR; ++i)
+#pragma unroll
+    for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int per = (int)cdiv(K, KS), steps = per * p.segs;
+  int seg = 0, k = 0;   // of the next step to load
+  const auto fill = [&](uint32_t* buf) {
+    const int64_t k0 = (int64_t)k * KS;
+    X::template fill<AK, false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane);
+    X::template fill<BK, KIND != DW>(buf + X::OP, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
+                                     (BK ? p.dimB : p.K) - k0, wid, lane);
+    if (++k == per) {
+      k = 0;
+      ++seg;
+    }
+  };
+  uint32_t atA = X::template place<AK>(fr, fg), atB = X::template place<BK>(fr, fg);
+  if (AK) atA += wr * 2 * KS;
+  else atA ^= 2 * wr;
+  if (BK) atB += wc * 2 * KS;
+  else atB ^= 2 * wc;
+  const auto multiply = [&](uint32_t* buf) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      // (formed again each time: kept for every line, the places would not leave the sums their registers)
+      asm volatile("" : "+v"(atA), "+v"(atB));
+      bf16x8_t cf[WC];
+#pragma unroll
+      for (int j = 0; j < WC; ++j) cf[j] = X::template frag<BK>(buf + X::OP, atB, j, kk);
+#pragma unroll
+      for (int i = 0; i < WR; ++i) {
+        const bf16x8_t rf = X::template frag<AK>(buf, atA, i, kk);
+#pragma unroll
+        for (int j = 0; j < WC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cf[j], rf, acc[i][j], 0, 0, 0);
+      }
+    }
+  };
+  const auto ready = [] {   // this wave's loads have arrived and its reads are done, then everybody's
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (steps > 0) fill(bufA);
+  int step = 0;
+  for (; step + 1 < steps; step += 2) {
+    ready();
+    fill(bufB);
+    multiply(bufA);
+    ready();
+    if (step + 2 < steps) fill(bufA);
+    multiply(bufB);
+  }
+  if (step < steps) {
+    ready();
+    multiply(bufA);
+  }
+  __syncthreads();
+
+  // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.
+  const int64_t ca = c0 + wc + 4 * fg;
+  if constexpr (KIND == STAT || KIND == PROB) {
+#pragma unroll
+    for (int j = 0; j < WC; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t c = ca + 16 * j + e;
+        const float b = c >= p.cols ? -INFINITY : p.b ? p.b[c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < WR; ++i) acc[i][j][e] = c >= p.cols ? b : acc[i][j][e] + b;
+      }
+  }
+  if constexpr (KIND == STAT) {
+    float2* s = (float2*)bufA;   // [columns' waves][T]
+#pragma unroll
+    for (int i = 0; i < WR; ++i) {
+      const int64_t r = r0 + wr + 16 * i + fr;
+      const int64_t at = r < rows ? p.lab[r] - p.c0 - ca : -1;
+      float m = -INFINITY, v = 0.f;
+#pragma unroll
+      for (int j = 0; j < WC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m = fmaxf(m, acc[i][j][e]);
+          if (at == 16 * j + e) p.at_label[r] = acc[i][j][e];
+        }
+      m = fmaxf(m, __shfl_xor(m, 16, 64));
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float from = m == -INFINITY ? 0.f : m;   // (nothing but classes of logit -inf: a sum of zeros)
+#pragma unroll
+      for (int j = 0; j < WC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * LOG2E);
+      v += __shfl_xor(v, 16, 64);
+      v += __shfl_xor(v, 32, 64);
+      if (fg == 0) s[wid % X::WCOLS * T + wr + 16 * i + fr] = make_float2(m, v);
+    }
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t >= T || r0 + t >= rows) return;
+    float2 q = s[t];
+#pragma unroll
+    for (int w = 1; w < X::WCOLS; ++w) {
+      const float2 o = s[w * T + t];
+      const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;
+      q.y = q.y * __builtin_amdgcn_exp2f((q.x - from) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - from) * LOG2E);
+      q.x = m;
+    }
+    p.part[tc * p.ld_part + r0 + t] = q;
+  }
+  if constexpr (KIND == PROB) {
+    float sum[WC][4];
+#pragma unroll
+    for (int j = 0; j < WC; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[j][e] = 0.f;
+    const int64_t end = up(rows, KS);   // zeros in the rows behind the last, to a whole step
+#pragma unroll
+    for (int i = 0; i < WR; ++i) {
+      const int64_t r = r0 + wr + 16 * i + fr;
+      const bool live = r < rows;
+      const float2 st = live ? p.stat[r] : make_float2(0.f, 0.f);
+      const int64_t at = live ? p.lab[r] - p.c0 - ca : -1;
+#pragma unroll
+      for (int j = 0; j < WC; ++j) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = __builtin_amdgcn_exp2f((acc[i][j][e] - st.x) * LOG2E) * st.y - (at == 16 * j + e ? 1.f : 0.f);
+          if (!live) v[e] = 0.f;
+          sum[j][e] += v[e];
+        }
+        if (r >= end || ca + 16 * j >= p.ldp) continue;
+        uint16_t* to = p.P + r * p.ldp + ca + 16 * j;
+        uint2 h = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+        *(uint2*)to = h;
+        for (int q = 1; q < p.parts; ++q) {
+          v[0] -= lo_bf16(h.x); v[1] -= hi_bf16(h.x); v[2] -= lo_bf16(h.y); v[3] -= hi_bf16(h.y);
+          h = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+          *(uint2*)(to + q * p.planeP) = h;
+        }
+      }
+    }
+    if (p.cols_part) {
+#pragma unroll
+      for (int j = 0; j < WC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) sum[j][e] += __shfl_xor(sum[j][e], o, 64);
+        }
+      if (fr == 0 && r0 + wr < rows)
+#pragma unroll
+        for (int j = 0; j < WC; ++j)
+          if (ca + 16 * j < p.ldp)
+            *(float4*)(p.cols_part + (r0 + wr) / (16 * WR) * p.ldp + ca + 16 * j) =
+                make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
+    }
+  }
+  if constexpr (KIND == DX || KIND == DW) {
+    const float scale = count > 0 ? (p.dloss ? *p.dloss : 1.f) / (float)count : 0.f;
+#pragma unroll
+    for (int i = 0; i < WR; ++i) {
+      const int64_t r = r0 + wr + 16 * i + fr;
+      if (r >= rows) continue;
+      float* o = p.out + (KIND == DX ? (int64_t)p.idx[r] : r) * p.ldo + ca;
+#pragma unroll
+      for (int j = 0; j < WC; ++j) {
+        const int n = (int)min((int64_t)4, p.cols - ca - 16 * j);
+        if (n <= 0) continue;
+        float v[4], w[4];
+        if (KIND == DX && p.add) load_some(o + 16 * j, n, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * scale + (KIND == DX && p.add ? w[e] : 0.f);
+        store_some(o + 16 * j, n, v);
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------- rows' sums
+
+// 16 rows a block, 16 threads to each: joins the tiles' (largest, sum) and leaves the row's, its loss, and the block's sum.
+__global__ __launch_bounds__(256) void k_loss_join(const int32_t* count, const int32_t* idx, const float2* part, int tiles,
+                                                   int64_t ld_part, const float* at_label, float2* stat, float* row_loss,
+                                                   double* sums) {
+  __shared__ float2 s[16][17];
+  __shared__ double l[16];
+  const int64_t n = *count, r = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+  const int k = threadIdx.x >> 4;
+  if ((int64_t)blockIdx.x * 16 >= n) return;
+  float2 q = make_float2(-INFINITY, 0.f);
+  const auto add = [&](float2 o) {
+    const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;
+    q.y = q.y * expf(q.x - from) + o.y * expf(o.x - from);
+    q.x = m;
+  };
+  if (r < n)
+    for (int t = k; t < tiles; t += 16) add(part[t * ld_part + r]);
+  s[k][threadIdx.x & 15] = q;
+  __syncthreads();
+  if (k == 0) {
+    for (int j = 1; j < 16; ++j) add(s[j][threadIdx.x]);
+    double loss = 0.0;
+    if (r < n) {
+      // a logit of +inf: the others' exponentials are 0 beside it
+      if (q.x == INFINITY) q.y = 1.f;
+      const float v = (q.x - at_label[r]) + logf(q.y);
+      stat[r] = make_float2(q.x, 1.f / q.y);
+      if (row_loss) row_loss[idx[r]] = v;
+      loss = v;
+    }
+    l[threadIdx.x] = loss;
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  double v = 0.0;
+  for (int j = 0; j < 16; ++j) v += l[j];
+  sums[blockIdx.x] = v;
+}
+
+__global__ __launch_bounds__(256) void k_loss_mean(const int32_t* count, const double* sums, float* loss) {
+  __shared__ double s[256];
+  const int64_t n = *count, blocks = cdiv(n, 16);
+  double v = 0.0;
+  for (int64_t i = threadIdx.x; i < blocks; i += 256) v += sums[i];
+  s[threadIdx.x] = v;
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
+    if (threadIdx.x < o) s[threadIdx.x] += s[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = n > 0 ? (float)(s[0] / (double)n) : 0.f;
+}
+
+// db of a piece, from the column sums of each `per` rows.
+__global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const float* part, int64_t ld, int64_t per, int64_t cols,
+                                                 const float* dloss, float* db) {
+  __shared__ float s[16][17];
+  const int j = threadIdx.x & 15, k = threadIdx.x >> 4;
+  const int64_t c = (int64_t)blockIdx.x * 16 + j, n = *count, parts = cdiv(n, per);
+  float v = 0.f;
+  if (c < cols)
+    for (int64_t i = k; i < parts; i += 16) v += part[i * ld + c];
+  s[k][j] = v;
+  __syncthreads();
+  if (k || c >= cols) return;
+  v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v += s[i][j];
+  db[c] = n > 0 ? v * ((dloss ? *dloss : 1.f) / (float)n) : 0.f;
+}
+
+// dx of the rows without a label (all rows where dx is not made by the products).
+__global__ __launch_bounds__(256) void k_loss_zero(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n, int d,
+                                                   float* dx, int64_t lddx) {
+  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = e / dv;
+  const int c = (int)(e % dv) * 4;
+  if (r >= eff_count(max_rows, n_rows) || (uint32_t)label[r] < (uint32_t)n) return;
+  const float z[4] = {0.f, 0.f, 0.f, 0.f};
+  store_some(dx + r * lddx + c, d - c, z);
+}
+
+// --------------------------------------------------------------------------- memory
+
+size_t al(size_t b) { return (b + 255) & ~size_t(255); }
+
+constexpr size_t PIECE = size_t(1) << 30;   // bytes of P in memory at a time (where a piece is more than 256 classes wide)
+
+struct Plan {
+  int dp, parts;             // padded width; parts of x and W
+  int p_parts;               // of P
+  bool copy;                 // W is copied
+  int64_t Rp, width;         // padded rows; classes of a piece
+};
+Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
+  Plan p;
+  const bool bf = d->dtype == MTGNN_BF16;
+  p.dp = (int)up(d->d, KS);
+  p.parts = bf ? 1 : 3;
+  p.p_parts = bf ? 2 : 3;
+  p.copy = !bf || d->d % 8 != 0;
+  p.Rp = up(rows, KS);
+  const int64_t most = (int64_t)(PIECE / (2 * (size_t)p.p_parts * (size_t)p.Rp)) / 256 * 256;
+  p.width = std::min<int64_t>(up(d->n, KS), std::max<int64_t>(256, most));
+  return p;
+}
+
+struct Kept {                // what the forward leaves for the backward
+  int32_t *count, *idx, *lab;
+  float2* stat;
+  uint16_t* xc;
+};
+size_t kept_bytes(const Plan& p) { return 256 + 2 * al(4 * p.Rp) + al(8 * p.Rp) + al(2 * (size_t)p.parts * p.Rp * p.dp); }
+Kept kept(void* at, const Plan& p) {
+  Kept k;
+  char* w = (char*)at;
+  k.count = (int32_t*)w;
+  k.idx = (int32_t*)(w += 256);
+  k.lab = (int32_t*)(w += al(4 * p.Rp));
+  k.stat = (float2*)(w += al(4 * p.Rp));
+  k.xc = (uint16_t*)(w += al(8 * p.Rp));
+  return k;
+}
+size_t table_bytes(const mtgnn_loss_dims* d, const Plan& p) {
+  return p.copy ? al(2 * (size_t)p.parts * d->n * p.dp) : 0;
+}
+
+// Tiles of 256 where there are enough of them for the card.
+bool large(int64_t rows, int64_t cols) { return cdiv(rows, 256) * cdiv(cols, 256) >= 192; }
+
+template <int KIND, bool AK, bool BK>
+mtgnn_status product(Prod p, hipStream_t s) {
+  const bool big = large(p.rows, p.cols);
+  const int T = big ? 256 : 128;
+  p.tr = cdiv(p.rows, T);
+  p.tc = cdiv(p.cols, T);
+  {
+    TimedScope ts(site::Generic::name, s),
+        kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
+    if (big) k_loss_product<KIND, AK, BK, 256><<<(unsigned)(p.tr * p.tc), 512, 0, s>>>(p);
+    else k_loss_product<KIND, AK, BK, 128><<<(unsigned)(p.tr * p.tc), 256, 0, s>>>(p);
+  }
+  MTGNN_CHECK_LAUNCH("loss_product");
+  return MTGNN_OK;
+}
+
+// W as the products read it: copied into `to`, or in place.
+mtgnn_status table(const void* W, const mtgnn_loss_dims* d, const Plan& p, void* to, const uint16_t*& t, int64_t& ld,
+                   int64_t& dim, hipStream_t s) {
+  t = (const uint16_t*)W;
+  ld = dim = d->d;
+  if (!p.copy) return MTGNN_OK;
+  t = (const uint16_t*)to;
+  ld = dim = p.dp;
+  const unsigned grid = (unsigned)cdiv(d->n * (p.dp / 8), 256);
+  if (d->dtype == MTGNN_BF16) k_loss_table<<<grid, 256, 0, s>>>((const uint16_t*)W, d->n, d->d, p.dp, (uint16_t*)to, d->n * p.dp);
+  else k_loss_table<<<grid, 256, 0, s>>>((const float*)W, d->n, d->d, p.dp, (uint16_t*)to, d->n * p.dp);
+  MTGNN_CHECK_LAUNCH("loss_table");
+  return MTGNN_OK;
+}
+
+// The parts of a product of two operands of `a` and `b` parts, the smallest ones first.
+void segments(Prod& p, int a, int b) {
+  p.segs = a == 3 && b == 3 ? 6 : std::max(a, b);
+  if (p.segs == 6) {
+    const int x[6] = {1, 2, 0, 1, 0, 0}, y[6] = {1, 0, 2, 0, 1, 0};
+    for (int i = 0; i < 6; ++i) p.codeA |= x[i] << 2 * i, p.codeB |= y[i] << 2 * i;
+  } else if (a == 2) {
+    p.codeA = 1;
+  }
+}
+
+}  // namespace
+
+bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
+  constexpr int64_t MAX = int64_t(1) << 32;
+  const auto tiles = [](int64_t r, int64_t c) { return large(r, c) ? cdiv(r, 256) * cdiv(c, 256) * 512 : cdiv(r, 128) * cdiv(c, 128) * 256; };
+  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX &&
+         cdiv(d->n * (up(d->d, KS) / 8), 256) * 256 < MAX && cdiv(rows * cdiv(d->d, 4), 256) * 256 < MAX &&
+         rows / ROWS * 256 < MAX / 2;
+}
+
+size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows)); }
+
+size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
+  const Plan p = plan(d, rows);
+  const size_t t = table_bytes(d, p);
+  if (back) return t + al(2 * (size_t)p.p_parts * p.Rp * p.width) + al(4 * (size_t)cdiv(p.Rp, 64) * p.width);
+  return kept_bytes(p) + t + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * (size_t)cdiv(d->n, 128) * p.Rp) + al(4 * p.Rp) +
+         al(8 * cdiv(p.Rp, 16));
+}
+
+mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
+                       const int32_t* label, const mtgnn_loss_dims* d, float* loss, float* row_loss, void* save, void* ws,
+                       hipStream_t s) {
+  const Plan p = plan(d, max_rows);
+  const Kept k = kept(save ? save : ws, p);
+  char* w = (char*)ws + kept_bytes(p);
+  const auto take = [&](size_t bytes) {
+    char* at = w;
+    w += al(bytes);
+    return at;
+  };
+  void* tbl = take(table_bytes(d, p));
+  int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
+  float2* part = (float2*)take(8 * (size_t)cdiv(d->n, 128) * p.Rp);
+  float* at_label = (float*)take(4 * p.Rp);
+  double* sums = (double*)take(8 * cdiv(p.Rp, 16));
+  k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), CHUNK, 0, s>>>(label, n_rows, max_rows, d->n, counts);
+  MTGNN_CHECK_LAUNCH("loss_count");
+  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + KS / ROWS);
+  if (d->dtype == MTGNN_BF16)
+    k_loss_rows<<<blocks, 256, 0, s>>>((const uint16_t*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
+                                       k.lab, k.xc, p.Rp * p.dp, row_loss);
+  else
+    k_loss_rows<<<blocks, 256, 0, s>>>((const float*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
+                                       k.lab, k.xc, p.Rp * p.dp, row_loss);
+  MTGNN_CHECK_LAUNCH("loss_rows");
+  Prod q{};
+  MTGNN_TRY(table(W, d, p, tbl, q.B, q.ldb, q.dimB, s));
+  q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp; q.planeB = d->n * (int64_t)p.dp;
+  segments(q, p.parts, p.parts);
+  q.rows = max_rows; q.cols = d->n; q.K = p.dp; q.count = k.count;
+  q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
+  MTGNN_TRY((product<STAT, true, true>(q, s)));
+  const int tiles = (int)cdiv(d->n, large(max_rows, d->n) ? 256 : 128);
+  k_loss_join<<<(unsigned)cdiv(max_rows, 16), 256, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums);
+  MTGNN_CHECK_LAUNCH("loss_join");
+  k_loss_mean<<<1, 256, 0, s>>>(k.count, sums, loss);
+  MTGNN_CHECK_LAUNCH("loss_mean");
+  return MTGNN_OK;
+}
+
+mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* W, const float* b, const int32_t* label,
+                           const mtgnn_loss_dims* d, const void* save, const float* dloss, float* dx, int64_t lddx, float* dW,
+                           float* db, void* ws, hipStream_t s) {
+  const Plan p = plan(d, max_rows);
+  const Kept k = kept((void*)save, p);
+  char* w = (char*)ws;
+  const auto take = [&](size_t bytes) {
+    char* at = w;
+    w += al(bytes);
+    return at;
+  };
+  void* tbl = take(table_bytes(d, p));
+  uint16_t* P = (uint16_t*)take(2 * (size_t)p.p_parts * p.Rp * p.width);
+  float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * p.width);
+  const uint16_t* B;
+  int64_t ldb, dimB;
+  MTGNN_TRY(table(W, d, p, tbl, B, ldb, dimB, s));
+  if (dx) {
+    k_loss_zero<<<(unsigned)cdiv(max_rows * cdiv(d->d, 4), 256), 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx);
+    MTGNN_CHECK_LAUNCH("loss_zero");
+  }
+  for (int64_t c = 0; c < d->n; c += p.width) {
+    const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = up(cols, KS);
+    Prod q{};
+    q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
+    q.B = B + c * ldb; q.ldb = ldb; q.dimB = dimB; q.planeB = d->n * (int64_t)p.dp;
+    segments(q, p.parts, p.parts);
+    q.rows = max_rows; q.cols = cols; q.K = p.dp; q.count = k.count;
+    q.b = b ? b + c : nullptr; q.lab = k.lab; q.c0 = c; q.stat = k.stat;
+    q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp; q.parts = p.p_parts;
+    q.cols_part = db ? cols_part : nullptr;
+    MTGNN_TRY((product<PROB, true, true>(q, s)));
+    if (db) {
+      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, large(max_rows, cols) ? 128 : 64, cols, dloss, db + c);
+      MTGNN_CHECK_LAUNCH("loss_db");
+    }
+    if (dx) {
+      Prod r{};
+      r.A = P; r.lda = r.dimA = ldp; r.planeA = p.Rp * ldp;
+      r.B = B + c * ldb; r.ldb = ldb; r.dimB = dimB; r.planeB = q.planeB;
+      segments(r, p.p_parts, p.parts);
+      r.rows = max_rows; r.cols = d->d; r.K = cols; r.count = k.count;
+      r.idx = k.idx; r.out = dx; r.ldo = lddx; r.dloss = dloss; r.add = c > 0;
+      MTGNN_TRY((product<DX, true, false>(r, s)));
+    }
+    if (dW) {
+      Prod r{};
+      r.A = P; r.lda = r.dimA = ldp; r.planeA = p.Rp * ldp;
+      r.B = k.xc; r.ldb = r.dimB = p.dp; r.planeB = p.Rp * p.dp;
+      segments(r, p.p_parts, p.parts);
+      r.rows = cols; r.cols = d->d; r.count = k.count;
+      r.out = dW + c * d->d; r.ldo = d->d; r.dloss = dloss;
+      MTGNN_TRY((product<DW, false, false>(r, s)));
+    }
+  }
+  return MTGNN_OK;
+}
+
+}  // namespace mtgnn

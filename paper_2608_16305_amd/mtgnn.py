@@ -37,6 +37,9 @@ ENTRY_POINTS = (
     "mtgnn_causal_conv_ws_bytes", "mtgnn_causal_conv", "mtgnn_causal_conv_bwd", "mtgnn_causal_conv_step",
     "mtgnn_selective_scan_ws_bytes", "mtgnn_selective_scan_save_bytes", "mtgnn_selective_scan",
     "mtgnn_selective_scan_bwd", "mtgnn_selective_scan_step",
+    "mtgnn_embedding", "mtgnn_embedding_ws_bytes", "mtgnn_embedding_bwd", "mtgnn_layer_norm", "mtgnn_layer_norm_ws_bytes",
+    "mtgnn_layer_norm_bwd", "mtgnn_softmax_loss_save_bytes", "mtgnn_softmax_loss_ws_bytes", "mtgnn_softmax_loss",
+    "mtgnn_softmax_loss_bwd", "mtgnn_adamw_step",
     "mtgnn_status_string", "mtgnn_last_error", "mtgnn_version", "mtgnn_timer_start", "mtgnn_timer_stop",
 )
 
@@ -120,6 +123,23 @@ class ScanGrads(C.Structure):
                 + [(n, C.c_void_p) for n in ("dA", "dD", "ddelta_bias")])
 
 
+class EmbeddingDims(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class NormDims(C.Structure):
+    _fields_ = [("d", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class LossDims(C.Structure):
+    _fields_ = [("n", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_exp", "v_exp", "shadow")]
+                + [("n", C.c_int64), ("decay", C.c_float)])
+
+
 _P = C.c_void_p
 _I64 = C.c_int64
 _I32 = C.c_int32
@@ -178,6 +198,17 @@ _SIGS = {
     "mtgnn_cache_refresh": [_P, _I64, _P, _P, C.POINTER(Dims), _P, _P, _P],
     "mtgnn_adam_step": [C.POINTER(C.c_void_p)] * 5 + [C.POINTER(C.c_int64), _I32, C.POINTER(AdamConfig), _P],
     "mtgnn_mixed_batches": [_P, _I64, _I64, _P, _P, _P, _P, _SZ, _P],
+    "mtgnn_embedding": [_P, _P, _I64, _P, C.POINTER(EmbeddingDims), _P, _I64, _P],
+    "mtgnn_embedding_ws_bytes": [C.POINTER(EmbeddingDims), _I64],
+    "mtgnn_embedding_bwd": [_P, _P, _I64, _P, _I64, C.POINTER(EmbeddingDims), _P, _P, _SZ, _P],
+    "mtgnn_layer_norm": [_P, _I64, _P, _I64, _P, _P, C.POINTER(NormDims), _P, _I64, _P, _P],
+    "mtgnn_layer_norm_ws_bytes": [C.POINTER(NormDims), _I64],
+    "mtgnn_layer_norm_bwd": [_P, _I64, _P, _I64, _P, _P, _I64, _P, _P, _I64, C.POINTER(NormDims), _P, _I64, _P, _P, _P, _SZ, _P],
+    "mtgnn_softmax_loss_save_bytes": [C.POINTER(LossDims), _I64],
+    "mtgnn_softmax_loss_ws_bytes": [C.POINTER(LossDims), _I64, _I32],
+    "mtgnn_softmax_loss": [_P, _I64, _P, _I64, _P, _P, _P, C.POINTER(LossDims), _P, _P, _P, _P, _SZ, _P],
+    "mtgnn_softmax_loss_bwd": [_P, _I64, _P, _P, _P, C.POINTER(LossDims), _P, _P, _P, _I64, _P, _P, _P, _SZ, _P],
+    "mtgnn_adamw_step": [C.POINTER(AdamwTensor), _I64, C.POINTER(AdamConfig), _P, _P],
     "mtgnn_linear_ws_bytes": [C.POINTER(LinearDims), _I64, _I32],
     "mtgnn_linear": [_P, _I64, _P, _I64, _P, _P, _P, _I64, C.POINTER(LinearDims), _P, _I64, _P, _P, _SZ, _P],
     "mtgnn_linear_bwd": [_P, _I64, _P, _P, _I64, _P, _I64, _P, C.POINTER(LinearDims), _P, _I64, _P, _P, _P, _SZ, _P],
@@ -206,6 +237,8 @@ _SIGS = {
 _RES = {"mtgnn_workspace_bytes": _SZ, "mtgnn_save_bytes": _SZ, "mtgnn_grad_norm_ws_bytes": _SZ,
         "mtgnn_linear_ws_bytes": _SZ, "mtgnn_causal_conv_save_bytes": _SZ, "mtgnn_causal_conv_ws_bytes": _SZ,
         "mtgnn_selective_scan_ws_bytes": _SZ, "mtgnn_selective_scan_save_bytes": _SZ,
+        "mtgnn_embedding_ws_bytes": _SZ, "mtgnn_layer_norm_ws_bytes": _SZ, "mtgnn_softmax_loss_save_bytes": _SZ,
+        "mtgnn_softmax_loss_ws_bytes": _SZ,
         "mtgnn_controller_destroy": None, "mtgnn_status_string": C.c_char_p,
         "mtgnn_last_error": C.c_char_p, "mtgnn_version": C.c_int}
 
@@ -1000,6 +1033,164 @@ def mtgnn_selective_scan_step(slot, inp: ScanInputs, d: ScanDims, state_in, stat
                                            C.byref(inp), C.byref(d), _table(state_in, f32, "state_in", st, True, dev=dev),
                                            _table(state_out, f32, "state_out", st, True, dev=dev), yp, ldy, _stream(stream)),
            "mtgnn_selective_scan_step")
+
+
+# ----------------------------------------------------------------------------- a model over all nodes
+
+def embedding_dims(n, d, dtype=F32, scale=1.0) -> EmbeddingDims:
+    return EmbeddingDims(int(n), int(d), int(dtype), float(scale))
+
+
+def norm_dims(d, dtype=F32, eps=1e-5) -> NormDims:
+    return NormDims(int(d), int(dtype), float(eps))
+
+
+def loss_dims(n, d, dtype=F32) -> LossDims:
+    """n classes, rows of width d."""
+    return LossDims(int(n), int(d), int(dtype))
+
+
+def embedding_ws_bytes(d: EmbeddingDims, max_rows) -> int:
+    return int(lib().mtgnn_embedding_ws_bytes(C.byref(d), int(max_rows)))
+
+
+def layer_norm_ws_bytes(d: NormDims, max_rows) -> int:
+    return int(lib().mtgnn_layer_norm_ws_bytes(C.byref(d), int(max_rows)))
+
+
+def softmax_loss_save_bytes(d: LossDims, max_rows) -> int:
+    return int(lib().mtgnn_softmax_loss_save_bytes(C.byref(d), int(max_rows)))
+
+
+def softmax_loss_ws_bytes(d: LossDims, max_rows, backward=False) -> int:
+    return int(lib().mtgnn_softmax_loss_ws_bytes(C.byref(d), int(max_rows), int(backward)))
+
+
+def _ids(t, name, dev):
+    if t is None or t.dim() != 1:
+        raise MtgnnError(f"{name} must be a vector of int32")
+    return _count(t, 0, name, dev=dev), int(t.shape[0])
+
+
+def mtgnn_embedding(ids, table, d: EmbeddingDims, y, n_rows=None, stream=None):
+    """y[r] = scale table[ids[r]], zeros for an id outside the table."""
+    dev = _device()
+    md = _DT[d.dtype]
+    ip, R = _ids(ids, "ids", dev)
+    yp, ldy = _rows(y, md, "y", R, d.d, dev=dev)
+    _check(lib().mtgnn_embedding(ip, _count(n_rows, 1, "n_rows", dev=dev), R, _table(table, md, "table", (d.n, d.d), dev=dev),
+                                 C.byref(d), yp, ldy, _stream(stream)), "mtgnn_embedding")
+
+
+def mtgnn_embedding_bwd(ids, dy, d: EmbeddingDims, dtable, ws, n_rows=None, stream=None):
+    dev = _device()
+    f32 = torch.float32
+    ip, R = _ids(ids, "ids", dev)
+    gp, lddy = _rows(dy, f32, "dy", R, d.d, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_embedding_bwd(ip, _count(n_rows, 1, "n_rows", dev=dev), R, gp, lddy, C.byref(d),
+                                     _table(dtable, f32, "dtable", (d.n, d.d), dev=dev), wp, wb, _stream(stream)),
+           "mtgnn_embedding_bwd")
+
+
+def mtgnn_layer_norm(x, gamma, beta, d: NormDims, y, stats=None, n_rows=None, stream=None):
+    """Each row normed; stats [rows, 2]: where the backward will find the rows' means and scales."""
+    dev = _device()
+    md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
+    xp, ldx = _rows(x, md, "x", R, d.d, dev=dev)
+    yp, ldy = _rows(y, md, "y", R, d.d, dev=dev)
+    _check(lib().mtgnn_layer_norm(xp, ldx, _count(n_rows, 1, "n_rows", dev=dev), R,
+                                  _table(gamma, f32, "gamma", (d.d,), True, dev=dev),
+                                  _table(beta, f32, "beta", (d.d,), True, dev=dev), C.byref(d), yp, ldy,
+                                  _table(stats, f32, "stats", (R, 2), True, dev=dev), _stream(stream)), "mtgnn_layer_norm")
+
+
+def mtgnn_layer_norm_bwd(dy, x, gamma, stats, d: NormDims, dx, dgamma, dbeta, past=None, n_rows=None, ws=None, stream=None):
+    """past: a gradient that reaches x beside the norm, added to dx."""
+    dev = _device()
+    md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
+    gp, lddy = _rows(dy, f32, "dy", R, d.d, dev=dev)
+    xp, ldx = _rows(x, md, "x", R, d.d, dev=dev)
+    pp, ldp = _rows(past, f32, "past", R, d.d, optional=True, dev=dev)
+    dp, lddx = _rows(dx, f32, "dx", R, d.d, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_layer_norm_bwd(gp, lddy, xp, ldx, _table(stats, f32, "stats", (R, 2), dev=dev),
+                                      _count(n_rows, 1, "n_rows", dev=dev), R,
+                                      _table(gamma, f32, "gamma", (d.d,), True, dev=dev), pp, ldp, C.byref(d), dp, lddx,
+                                      _table(dgamma, f32, "dgamma", (d.d,), True, dev=dev),
+                                      _table(dbeta, f32, "dbeta", (d.d,), True, dev=dev), wp, wb, _stream(stream)),
+           "mtgnn_layer_norm_bwd")
+
+
+def mtgnn_softmax_loss(x, W, b, label, d: LossDims, loss, ws, row_loss=None, save=None, n_rows=None, stream=None):
+    """loss[0] = mean over the rows with a label of log sum exp(x W^T + b) - the label's."""
+    dev = _device()
+    md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
+    xp, ldx = _rows(x, md, "x", R, d.d, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_softmax_loss(xp, ldx, _count(n_rows, 1, "n_rows", dev=dev), R, _table(W, md, "W", (d.n, d.d), dev=dev),
+                                    _table(b, f32, "b", (d.n,), True, dev=dev),
+                                    _table(label, torch.int32, "label", (R,), dev=dev), C.byref(d),
+                                    _table(loss, f32, "loss", (1,), dev=dev),
+                                    _table(row_loss, f32, "row_loss", (R,), True, dev=dev),
+                                    _bytes(save, softmax_loss_save_bytes(d, R), "save", True, dev=dev), wp, wb,
+                                    _stream(stream)), "mtgnn_softmax_loss")
+
+
+def mtgnn_softmax_loss_bwd(x, W, b, label, d: LossDims, save, dx, dW, db, ws, dloss=None, n_rows=None, stream=None):
+    """dx, dW, db (each or None) of the loss times dloss ([1] or None: 1).  Of x only the rows count: their values are in save."""
+    dev = _device()
+    md, R, f32 = _DT[d.dtype], int(x.shape[0]), torch.float32
+    _rows(x, md, "x", R, d.d, dev=dev)
+    dp, lddx = _rows(dx, f32, "dx", R, d.d, optional=True, dev=dev)
+    wp, wb = _work(ws, dev)
+    _check(lib().mtgnn_softmax_loss_bwd(_count(n_rows, 1, "n_rows", dev=dev), R, _table(W, md, "W", (d.n, d.d), dev=dev),
+                                        _table(b, f32, "b", (d.n,), True, dev=dev),
+                                        _table(label, torch.int32, "label", (R,), dev=dev), C.byref(d),
+                                        _bytes(save, softmax_loss_save_bytes(d, R), "save", dev=dev),
+                                        _table(dloss, f32, "dloss", (1,), True, dev=dev), dp, lddx,
+                                        _table(dW, f32, "dW", (d.n, d.d), True, dev=dev),
+                                        _table(db, f32, "db", (d.n,), True, dev=dev), wp, wb, _stream(stream)),
+           "mtgnn_softmax_loss_bwd")
+
+
+class AdamwTensors:
+    """The tensors of mtgnn_adamw_step, described once: lists of as many dense tensors each.  shadow: None or a list of (None |
+    bf16 tensor); decay: None or a list of numbers; m_exp, v_exp: None, or lists of (None | uint8 tensor of ceil(n / 32)),
+    where given m and v hold 8-bit codes (uint8 or float8_e4m3fn).  It keeps its tensors."""
+
+    def __init__(self, params, grads, m, v, shadow=None, decay=None, m_exp=None, v_exp=None):
+        f32, n, dev = torch.float32, len(params), _device()
+        none = [None] * n
+        lists = dict(grads=grads, m=m, v=v, shadow=shadow or none, decay=decay or [0.0] * n, m_exp=m_exp or none,
+                     v_exp=v_exp or none)
+        for name, x in lists.items():
+            if len(x) != n:
+                raise MtgnnError(f"{name}: {len(x)} tensors for {n} parameters")
+        self.array = (AdamwTensor * n)()
+        for t, p, g, a, b, sh, de, ea, eb in zip(self.array, params, *lists.values()):
+            shape, size, blocks = tuple(p.shape), int(p.numel()), -(-int(p.numel()) // 32)
+            state = f32 if ea is None else a.dtype
+            if ea is not None and (a.dtype not in (torch.uint8, torch.float8_e4m3fn) or b.dtype != a.dtype):
+                raise MtgnnError(f"m and v must be uint8 or float8_e4m3fn beside exponents, got {a.dtype} and {b.dtype}")
+            t.param, t.grad = (_table(x, f32, k, shape, dev=dev) for x, k in ((p, "param"), (g, "grad")))
+            t.m, t.v = (_table(x, state, k, shape, dev=dev) for x, k in ((a, "m"), (b, "v")))
+            t.m_exp, t.v_exp = (_table(x, torch.uint8, k, (blocks,), True, dev=dev) for x, k in ((ea, "m_exp"), (eb, "v_exp")))
+            t.shadow = _table(sh, torch.bfloat16, "shadow", shape, True, dev=dev)
+            t.n, t.decay = size, float(de)
+        self.tensors, self.device = (list(params), *(list(x) for x in lists.values())), dev
+
+
+def adamw_tensors(params, grads, m, v, shadow=None, decay=None, m_exp=None, v_exp=None) -> AdamwTensors:
+    return AdamwTensors(params, grads, m, v, shadow, decay, m_exp, v_exp)
+
+
+def mtgnn_adamw_step(tensors: AdamwTensors, lr, beta1, beta2, eps, t, step=None, stream=None):
+    """t: the step's number, or step: an int32 tensor on the device that holds it."""
+    dev = _device()
+    _made_here(tensors, "the tensors", dev)
+    _check(lib().mtgnn_adamw_step(tensors.array, len(tensors.array), C.byref(AdamConfig(lr, beta1, beta2, eps, int(t))),
+                                  _count(step, 1, "step", dev=dev), _stream(stream)), "mtgnn_adamw_step")
 
 
 def timer_start(kernel: str, max_launches: int):
