@@ -7,13 +7,16 @@
 // two products with W and x take it from there.  So 8 rows x classes x width operations are done where 6 are needed, and a
 // piece of P, not all of it, is in memory.
 //
-// All products run on the bfloat16 matrix instructions with float32 sums.  bfloat16 x and W enter as they are; float32 ones as
-// three bfloat16 parts (24 bits), six products of parts for one of theirs.  P is held as two parts beside bfloat16 (16
-// bits: an element is off by 2^-17 of itself at most, where the exponential of a float32 logit is off by |l| 2^-24 or more; one
-// part would be 2^-9), as three beside float32.
+// All products run on the 16-bit matrix instructions with float32 sums.  Logits of bfloat16 x and W are formed from them as
+// they are.  Everything else enters as float16 parts, which have 11 bits each: float32 x and W as two (within 2^-23 of an
+// element; six bfloat16 products of three parts each would take twice the time), in three products for one of theirs, without
+// that of the second parts, 2^-22 at most; bfloat16 ones, for the gradients, as one, which holds their 8 bits; P, times 2^14,
+// as two (within 2^-23 of an element or 2^-39, whichever is more; two bfloat16 parts would be 2^-17 off, and the gradients of a
+// few thousand classes then 1.3e-6, where a float32 evaluation is 1e-6 off).  What float16 lacks is range: a power of two
+// takes x's largest element, and W's, to 2^14 or above, and elements below 2^-17 of the largest are held to 2^-39 of it instead.
 //
 // Rows without a label are left out before anything is computed: the others' x is copied, row after row, padded with
-// zeros to whole steps.  A W that is not a multiple of 16 bytes wide, or float32, is copied into parts likewise.
+// zeros to whole steps.
 #include <algorithm>
 #include <cmath>
 
@@ -26,9 +29,12 @@ namespace mtgnn {
 namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 
 constexpr int KS = 64;          // a step of the sums
+constexpr float LIFT = 16384.f; // what P is multiplied by
 constexpr int CHUNK = 1024;     // rows whose labels are counted together
 constexpr int ROWS = 16;        // rows that a block copies
 constexpr float LOG2E = 1.4426950408889634f;
@@ -42,8 +48,9 @@ __device__ __forceinline__ bool has_label(const int32_t* label, int64_t r, int64
 }
 
 __global__ __launch_bounds__(CHUNK) void k_loss_count(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n,
-                                                      int32_t* counts) {
+                                                      int32_t* counts, uint32_t* largest) {
   __shared__ int s[CHUNK / 64];
+  if (blockIdx.x == 0 && threadIdx.x < 2) largest[threadIdx.x] = 0u;
   const int64_t r = (int64_t)blockIdx.x * CHUNK + threadIdx.x;
   const uint64_t have = __ballot(has_label(label, r, eff_count(max_rows, n_rows), n));
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __popcll(have);
@@ -64,29 +71,90 @@ __device__ __forceinline__ int block_sum(int v, int* s) {   // over 256 threads
   return v;
 }
 
-// A row's eight elements from c on (zeros from d on) as the parts of a padded matrix.
-template <typename T>
-__device__ __forceinline__ void put_parts(const T* row, int c, int d, uint16_t* to, int64_t plane) {
-  float v[8];
-  load_some(row + c, d - c, v);
-  if constexpr (sizeof(T) == 2) {
-    *(uint4*)to = make_uint4(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]), cvt2_bf16(v[4], v[5]), cvt2_bf16(v[6], v[7]));
-  } else {
-    uint32_t h[4], m[4], l[4];
-    split_words<true>(v, h, m, l);
-    *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
-    *(uint4*)(to + plane) = make_uint4(m[0], m[1], m[2], m[3]);
-    *(uint4*)(to + 2 * plane) = make_uint4(l[0], l[1], l[2], l[3]);
-  }
+// --------------------------------------------------------------------------- float16 parts
+
+// The bits of a finite magnitude (larger numbers, larger bits); 0 for what is not finite.
+__device__ __forceinline__ uint32_t magnitude(float v) {
+  const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+__device__ __forceinline__ void raise(uint32_t v, uint32_t* largest) {   // by all 256 threads of a block
+  __shared__ uint32_t s[4];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = max(max(s[0], s[1]), max(s[2], s[3]));
+  if (threadIdx.x == 0 && v) atomicMax(largest, v);   // (a maximum does not depend on the order)
+}
+// The power of two that takes the largest element to 2^14 .. 2^15, as far as float32 has it.
+__device__ __forceinline__ float lift(uint32_t largest) {
+  return largest ? __uint_as_float(min(268u - (largest >> 23), 254u) << 23) : 1.f;
 }
 
-// The rows with a label, one after the other: idx (which rows), lab, xc (their x in parts, zeros behind the last one to a
-// whole step); their number.  Blocks past those of the rows fill in the zeros.
+__device__ __forceinline__ uint32_t cvt2_f16(float a, float b) {   // to the nearest
+  return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+}
+__device__ __forceinline__ float lo_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).x; }
+__device__ __forceinline__ float hi_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).y; }
+__device__ __forceinline__ float left_of(float v, float h) { return fabsf(h) < INFINITY ? v - h : 0.f; }   // (what is infinite or NaN is so in its first part)
+
+// Eight elements of a row from c on (zeros from d on) in a padded matrix: as bfloat16, or times `by` in PARTS float16 parts.
+template <typename T, int PARTS>
+__device__ __forceinline__ uint32_t put_parts(const T* row, int c, int d, float by, uint16_t* to, int64_t plane) {
+  float v[8];
+  uint32_t top = 0u, h[4];
+  load_some(row + c, d - c, v);
+  if constexpr (PARTS == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = cvt2_bf16(v[2 * i], v[2 * i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= by;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = cvt2_f16(v[2 * i], v[2 * i + 1]);
+  }
+  *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
+  if constexpr (PARTS == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = cvt2_f16(left_of(v[2 * i], lo_f16(h[i])), left_of(v[2 * i + 1], hi_f16(h[i])));
+    *(uint4*)(to + plane) = make_uint4(h[0], h[1], h[2], h[3]);
+  }
+  return top;
+}
+
+// The largest elements of x's rows with a label (blocks below x_blocks) and of W.  A block takes every x_blocks-th (the others':
+// every so many) 2,048 elements: a maximum in memory for each would take longer than reading them (126 us against 17, 64 MB).
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_largest(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
+                                                      int64_t max_rows, const T* W, int64_t n, int d, unsigned x_blocks,
+                                                      uint32_t* largest) {
+  const bool table = blockIdx.x >= x_blocks;
+  const int64_t units = cdiv(d, 8), rows = table ? n : eff_count(max_rows, n_rows);
+  const int64_t step = (int64_t)(table ? gridDim.x - x_blocks : x_blocks) * 256;
+  uint32_t top = 0u;
+  for (int64_t e = (int64_t)(blockIdx.x - (table ? x_blocks : 0)) * 256 + threadIdx.x; e < rows * units; e += step) {
+    const int64_t r = e / units;
+    const int c = (int)(e - r * units) * 8;
+    if (!table && !has_label(label, r, rows, (int)n)) continue;
+    float v[8];
+    load_some(table ? W + r * d + c : x + r * ldx + c, d - c, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+  }
+  raise(top, largest + table);
+}
+
+// The rows with a label, one after the other: idx (which rows), lab, xc (their x, as it is or in parts; zeros behind the last
+// one to a whole step); their number; of bfloat16 x its largest element.  Blocks past those of the rows fill in the zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
                                                    int64_t max_rows, int n, int d, int dp, const int32_t* counts,
                                                    int32_t* count, int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane,
-                                                   float* row_loss) {
+                                                   uint32_t* largest, float* row_loss) {
+  constexpr int PARTS = sizeof(T) == 2 ? 0 : 2;
   __shared__ int s[4], src[ROWS];
   const int64_t rows = eff_count(max_rows, n_rows), r0 = (int64_t)blockIdx.x * ROWS;
   const int chunks = (int)cdiv(max_rows, CHUNK), units = dp / 8;
@@ -104,9 +172,8 @@ __global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, cons
     for (int e = threadIdx.x; e < ROWS * units; e += 256) {
       const int64_t r = first + j0 + e / units;
       if (r >= end) break;
-#pragma unroll
-      for (int p = 0; p < (sizeof(T) == 2 ? 1 : 3); ++p)
-        *(uint4*)(xc + p * plane + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
+      *(uint4*)(xc + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
+      if (PARTS == 2) *(uint4*)(xc + plane + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
     }
     return;
   }
@@ -128,30 +195,40 @@ __global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, cons
   }
   __syncthreads();
   here = s[0];
+  const float by = PARTS == 2 ? lift(*largest) : 1.f;
+  uint32_t top = 0u;
   for (int e = threadIdx.x; e < here * units; e += 256) {
     const int k = e / units, c = e % units * 8;
-    put_parts(x + (r0 + src[k]) * ldx, c, d, xc + (int64_t)(first + k) * dp + c, plane);
+    top = max(top, put_parts<T, PARTS>(x + (r0 + src[k]) * ldx, c, d, by, xc + (int64_t)(first + k) * dp + c, plane));
   }
+  if (PARTS == 0) raise(top, largest);
 }
 
-// W in parts, padded.
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_table(const T* W, int64_t n, int d, int dp, uint16_t* to, int64_t plane) {
+// Rows of d as rows of dp: as they are, or in float16 parts.
+template <typename T, int PARTS>
+__global__ __launch_bounds__(256) void k_loss_table(const T* W, int64_t n, int d, int dp, const uint32_t* largest, uint16_t* to,
+                                                    int64_t plane) {
   const uint32_t units = dp / 8, e = blockIdx.x * 256 + threadIdx.x;
   const int64_t c = e / units;
   const int u = (int)(e % units) * 8;
-  if (c < n) put_parts(W + c * d, u, d, to + c * dp + u, plane);
+  if (c < n) put_parts<T, PARTS>(W + c * d, u, d, PARTS ? lift(*largest) : 1.f, to + c * dp + u, plane);
 }
 
 // --------------------------------------------------------------------------- the products
 
 enum { STAT, PROB, DX, DW };
 
+// What P is multiplied by in the gradients: 1 / rows, times the loss's own gradient.
+__device__ __forceinline__ float loss_scale(int64_t rows, const float* dloss) {
+  return rows > 0 ? (dloss ? *dloss : 1.f) / (float)rows : 0.f;
+}
+
 struct Prod {
   const uint16_t *A, *B;         // A: the result's rows, B: its columns
   int64_t lda, ldb, planeA, planeB;
   uint32_t codeA, codeB;         // the parts of each segment, two bits each
-  int segs;
+  int segs, split;               // split: blocks that share a tile's sum, each leaving its own in `out`
+  const uint32_t *topA, *topB;   // largest elements of operands in float16 parts, or NULL
   int64_t rows, cols, K;         // the most rows; K: of a segment
   int64_t dimA, dimB;            // elements of an operand's line that may be read (A's along the sum are whole steps)
   int64_t tr, tc;                // tiles
@@ -164,9 +241,8 @@ struct Prod {
   int64_t ld_part;
   float* at_label;
   const float2* stat;            // PROB: largest logit, 1 / sum
-  uint16_t* P;
+  uint16_t* P;                   // two parts
   int64_t ldp, planeP;
-  int parts;
   float* cols_part;              // [rows / 64][ldp] column sums of P, or NULL
   float* out;
   int64_t ldo;
@@ -243,22 +319,33 @@ struct Tiles {
 
 // Blocks run on the 8 XCDs in turn, each with its own L2: a contiguous eighth of the tiles to each, in groups of eight tiles of
 // rows by all of columns, so that the blocks that run together share lines of both operands.
-__device__ __forceinline__ void my_tile(const Prod& p, int64_t& tr, int64_t& tc) {
-  const int64_t L = blockIdx.x, n = p.tr * p.tc, full = n & ~int64_t(7);
-  const int64_t V = L < full ? (L & 7) * (full >> 3) + (L >> 3) : L;
+__device__ __forceinline__ void my_tile(const Prod& p, int64_t& tr, int64_t& tc, int& share) {
+  const int64_t L = blockIdx.x, n = p.tr * p.tc * p.split, full = n & ~int64_t(7);
+  int64_t V = L < full ? (L & 7) * (full >> 3) + (L >> 3) : L;
+  share = (int)(V / (p.tr * p.tc));
+  V %= p.tr * p.tc;
   constexpr int64_t G = 8;
   const int64_t group = V / (G * p.tc), in = V % (G * p.tc), h = min(G, p.tr - group * G);
   tr = group * G + in % h;
   tc = in / h;
 }
 
-template <int KIND, bool AK, bool BK, int T>
+// HALF: float16 operands, else bfloat16 ones.
+template <bool HALF>
+__device__ __forceinline__ f32x4 mma(bf16x8_t a, bf16x8_t b, f32x4 c) {
+  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+template <int KIND, bool HALF, int T>
 __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss_product(Prod p) {
+  constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
   using X = Tiles<AK, BK, T>;
   constexpr int WR = X::WR, WC = X::WC;
   __shared__ __align__(1024) uint32_t bufA[2 * X::OP], bufB[2 * X::OP];
   int64_t tr, tc;
-  my_tile(p, tr, tc);
+  int share;
+  my_tile(p, tr, tc, share);
   const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
   const int64_t K = KIND == DW ? up(count, KS) : p.K;
   const int64_t r0 = tr * T, c0 = tc * T;
@@ -274,8 +361,9 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
   for (int i = 0; i < WR; ++i)
 #pragma unroll
     for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int per = (int)cdiv(K, KS), steps = per * p.segs;
-  int seg = 0, k = 0;   // of the next step to load
+  const int per = (int)cdiv(K, KS), all = per * p.segs, each = (all + p.split - 1) / p.split;
+  const int steps = max(0, min(each, all - share * each));
+  int seg = steps > 0 ? share * each / per : 0, k = share * each - seg * per;   // of the next step to load
   const auto fill = [&](uint32_t* buf) {
     const int64_t k0 = (int64_t)k * KS;
     X::template fill<AK, false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane);
@@ -303,7 +391,7 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
       for (int i = 0; i < WR; ++i) {
         const bf16x8_t rf = X::template frag<AK>(buf, atA, i, kk);
 #pragma unroll
-        for (int j = 0; j < WC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cf[j], rf, acc[i][j], 0, 0, 0);
+        for (int j = 0; j < WC; ++j) acc[i][j] = mma<HALF>(cf[j], rf, acc[i][j]);
       }
     }
   };
@@ -331,6 +419,7 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
 
   // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.
   const int64_t ca = c0 + wc + 4 * fg;
+  const float downA = HALF && KIND != DX ? 1.f / lift(*p.topA) : 1.f, downB = HALF && KIND != DW ? 1.f / lift(*p.topB) : 1.f;
   if constexpr (KIND == STAT || KIND == PROB) {
 #pragma unroll
     for (int j = 0; j < WC; ++j)
@@ -339,7 +428,7 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
         const int64_t c = ca + 16 * j + e;
         const float b = c >= p.cols ? -INFINITY : p.b ? p.b[c] : 0.f;
 #pragma unroll
-        for (int i = 0; i < WR; ++i) acc[i][j][e] = c >= p.cols ? b : acc[i][j][e] + b;
+        for (int i = 0; i < WR; ++i) acc[i][j][e] = c >= p.cols ? b : (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + b;
       }
   }
   if constexpr (KIND == STAT) {
@@ -404,13 +493,12 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
         }
         if (r >= end || ca + 16 * j >= p.ldp) continue;
         uint16_t* to = p.P + r * p.ldp + ca + 16 * j;
-        uint2 h = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= LIFT;
+        const uint2 h = make_uint2(cvt2_f16(v[0], v[1]), cvt2_f16(v[2], v[3]));
         *(uint2*)to = h;
-        for (int q = 1; q < p.parts; ++q) {
-          v[0] -= lo_bf16(h.x); v[1] -= hi_bf16(h.x); v[2] -= lo_bf16(h.y); v[3] -= hi_bf16(h.y);
-          h = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
-          *(uint2*)(to + q * p.planeP) = h;
-        }
+        *(uint2*)(to + p.planeP) = make_uint2(cvt2_f16(v[0] - lo_f16(h.x), v[1] - hi_f16(h.x)),
+                                              cvt2_f16(v[2] - lo_f16(h.y), v[3] - hi_f16(h.y)));
       }
     }
     if (p.cols_part) {
@@ -430,24 +518,52 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
     }
   }
   if constexpr (KIND == DX || KIND == DW) {
-    const float scale = count > 0 ? (p.dloss ? *p.dloss : 1.f) / (float)count : 0.f;
+    const bool whole = p.split == 1;   // else the sums as they are, for k_loss_shares
+    const float scale = whole ? loss_scale(count, p.dloss) / LIFT : 1.f;
+    float* const out = p.out + (whole ? 0 : share * p.rows * p.ldo);
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
       const int64_t r = r0 + wr + 16 * i + fr;
       if (r >= rows) continue;
-      float* o = p.out + (KIND == DX ? (int64_t)p.idx[r] : r) * p.ldo + ca;
+      float* o = out + (KIND == DX && whole ? (int64_t)p.idx[r] : r) * p.ldo + ca;
+      const bool add = KIND == DX && whole && p.add;
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
         const int n = (int)min((int64_t)4, p.cols - ca - 16 * j);
         if (n <= 0) continue;
-        float v[4], w[4];
-        if (KIND == DX && p.add) load_some(o + 16 * j, n, w);
+        float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
+        if (add) load_some(o + 16 * j, n, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * scale + (KIND == DX && p.add ? w[e] : 0.f);
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * (KIND == DX ? downB : downA) * scale + w[e];
         store_some(o + 16 * j, n, v);
       }
     }
   }
+}
+
+// The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.
+__global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const int32_t* idx, const float* part, int split,
+                                                     int64_t rows, int d, const float* dloss, int add, float* out, int64_t ldo) {
+  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = e / dv, n = *count;
+  const int c = (int)(e % dv) * 4;
+  if (r >= (idx ? n : rows)) return;
+  float* o = out + (idx ? (int64_t)idx[r] : r) * ldo + c;
+  const float scale = loss_scale(n, dloss) / LIFT;
+  float v[4] = {0.f, 0.f, 0.f, 0.f}, w[4];
+  for (int s = 0; s < split; ++s) {
+    load_some(part + (s * rows + r) * d + c, d - c, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] *= scale;
+  if (add) {
+    load_some(o, d - c, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += w[i];
+  }
+  store_some(o, d - c, v);
 }
 
 // --------------------------------------------------------------------------- rows' sums
@@ -520,12 +636,14 @@ __global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const flo
   v = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) v += s[i][j];
-  db[c] = n > 0 ? v * ((dloss ? *dloss : 1.f) / (float)n) : 0.f;
+  db[c] = v * loss_scale(n, dloss);
 }
 
-// dx of the rows without a label (all rows where dx is not made by the products).
+// dx of the rows without a label; clears *largest.
 __global__ __launch_bounds__(256) void k_loss_zero(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n, int d,
-                                                   float* dx, int64_t lddx) {
+                                                   float* dx, int64_t lddx, uint32_t* largest) {
+  if (blockIdx.x == 0 && threadIdx.x == 0 && largest) *largest = 0u;
+  if (!dx) return;
   const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
   const int64_t r = e / dv;
   const int c = (int)(e % dv) * 4;
@@ -541,107 +659,138 @@ size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 constexpr size_t PIECE = size_t(1) << 30;   // bytes of P in memory at a time (where a piece is more than 256 classes wide)
 
 struct Plan {
-  int dp, parts;             // padded width; parts of x and W
-  int p_parts;               // of P
-  bool copy;                 // W is copied
+  bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes)
+  int dp;                    // padded width
   int64_t Rp, width;         // padded rows; classes of a piece
 };
 Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
   Plan p;
-  const bool bf = d->dtype == MTGNN_BF16;
+  p.bf = d->dtype == MTGNN_BF16;
   p.dp = (int)up(d->d, KS);
-  p.parts = bf ? 1 : 3;
-  p.p_parts = bf ? 2 : 3;
-  p.copy = !bf || d->d % 8 != 0;
+  p.copy = p.bf && d->d % 8 != 0;
   p.Rp = up(rows, KS);
-  const int64_t most = (int64_t)(PIECE / (2 * (size_t)p.p_parts * (size_t)p.Rp)) / 256 * 256;
+  const int64_t most = (int64_t)(PIECE / (4 * (size_t)p.Rp)) / 256 * 256;
   p.width = std::min<int64_t>(up(d->n, KS), std::max<int64_t>(256, most));
   return p;
 }
 
 struct Kept {                // what the forward leaves for the backward
-  int32_t *count, *idx, *lab;
+  int32_t* count;
+  uint32_t* largest;         // of x, of W (float32)
+  int32_t *idx, *lab;
   float2* stat;
-  uint16_t* xc;
+  uint16_t* xc;              // x's rows: bfloat16, or two float16 parts
 };
-size_t kept_bytes(const Plan& p) { return 256 + 2 * al(4 * p.Rp) + al(8 * p.Rp) + al(2 * (size_t)p.parts * p.Rp * p.dp); }
+size_t kept_bytes(const Plan& p) { return 256 + 2 * al(4 * p.Rp) + al(8 * p.Rp) + al(2 * (size_t)(p.bf ? 1 : 2) * p.Rp * p.dp); }
 Kept kept(void* at, const Plan& p) {
   Kept k;
   char* w = (char*)at;
   k.count = (int32_t*)w;
+  k.largest = (uint32_t*)(w + 16);
   k.idx = (int32_t*)(w += 256);
   k.lab = (int32_t*)(w += al(4 * p.Rp));
   k.stat = (float2*)(w += al(4 * p.Rp));
   k.xc = (uint16_t*)(w += al(8 * p.Rp));
   return k;
 }
-size_t table_bytes(const mtgnn_loss_dims* d, const Plan& p) {
-  return p.copy ? al(2 * (size_t)p.parts * d->n * p.dp) : 0;
-}
 
 // Tiles of 256 where there are enough of them for the card.
 bool large(int64_t rows, int64_t cols) { return cdiv(rows, 256) * cdiv(cols, 256) >= 192; }
+// Blocks that share a tile's sum of `steps` steps.
+int shares(int64_t rows, int64_t cols, int64_t steps) {
+  const int64_t T = large(rows, cols) ? 256 : 128, t = cdiv(rows, T) * cdiv(cols, T);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, steps / 8));
+}
+struct Shares {
+  int dx, dw;                // of a piece
+  size_t bytes;
+};
+Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t cols) {
+  const int segs = p.bf ? 2 : 3;
+  Shares s;
+  s.dx = shares(rows, d->d, segs * cdiv(cols, KS));
+  s.dw = shares(cols, d->d, segs * cdiv(rows, KS));
+  s.bytes = std::max(s.dx > 1 ? 4 * (size_t)s.dx * rows * d->d : 0, s.dw > 1 ? 4 * (size_t)s.dw * cols * d->d : 0);
+  return s;
+}
 
-template <int KIND, bool AK, bool BK>
+template <int KIND, bool HALF>
 mtgnn_status product(Prod p, hipStream_t s) {
   const bool big = large(p.rows, p.cols);
   const int T = big ? 256 : 128;
   p.tr = cdiv(p.rows, T);
   p.tc = cdiv(p.cols, T);
+  p.split = std::max(1, p.split);
+  const unsigned grid = (unsigned)(p.tr * p.tc * p.split);
   {
     TimedScope ts(site::Generic::name, s),
         kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
-    if (big) k_loss_product<KIND, AK, BK, 256><<<(unsigned)(p.tr * p.tc), 512, 0, s>>>(p);
-    else k_loss_product<KIND, AK, BK, 128><<<(unsigned)(p.tr * p.tc), 256, 0, s>>>(p);
+    if (big) k_loss_product<KIND, HALF, 256><<<grid, 512, 0, s>>>(p);
+    else k_loss_product<KIND, HALF, 128><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
 }
-
-// W as the products read it: copied into `to`, or in place.
-mtgnn_status table(const void* W, const mtgnn_loss_dims* d, const Plan& p, void* to, const uint16_t*& t, int64_t& ld,
-                   int64_t& dim, hipStream_t s) {
-  t = (const uint16_t*)W;
-  ld = dim = d->d;
-  if (!p.copy) return MTGNN_OK;
-  t = (const uint16_t*)to;
-  ld = dim = p.dp;
-  const unsigned grid = (unsigned)cdiv(d->n * (p.dp / 8), 256);
-  if (d->dtype == MTGNN_BF16) k_loss_table<<<grid, 256, 0, s>>>((const uint16_t*)W, d->n, d->d, p.dp, (uint16_t*)to, d->n * p.dp);
-  else k_loss_table<<<grid, 256, 0, s>>>((const float*)W, d->n, d->d, p.dp, (uint16_t*)to, d->n * p.dp);
-  MTGNN_CHECK_LAUNCH("loss_table");
+// A gradient's product, shared by `split` blocks a tile through `part`.
+template <int KIND>
+mtgnn_status gradient(Prod p, int split, float* part, hipStream_t s) {
+  if (split <= 1) return product<KIND, true>(p, s);
+  Prod q = p;
+  q.split = split;
+  q.out = part;
+  q.ldo = p.cols;
+  MTGNN_TRY((product<KIND, true>(q, s)));
+  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256), 256, 0, s>>>(p.count, p.idx, part, split, p.rows, (int)p.cols,
+                                                                              p.dloss, p.add, p.out, p.ldo);
+  MTGNN_CHECK_LAUNCH("loss_shares");
   return MTGNN_OK;
 }
 
-// The parts of a product of two operands of `a` and `b` parts, the smallest ones first.
+// The parts of a product of two operands of `a` and `b` parts, the smaller ones first (without that of two second parts).
 void segments(Prod& p, int a, int b) {
-  p.segs = a == 3 && b == 3 ? 6 : std::max(a, b);
-  if (p.segs == 6) {
-    const int x[6] = {1, 2, 0, 1, 0, 0}, y[6] = {1, 0, 2, 0, 1, 0};
-    for (int i = 0; i < 6; ++i) p.codeA |= x[i] << 2 * i, p.codeB |= y[i] << 2 * i;
-  } else if (a == 2) {
-    p.codeA = 1;
-  }
+  p.segs = a + b - 1;
+  if (a == 2 && b == 2) p.codeA = 1, p.codeB = 1 << 2;
+  else if (a == 2) p.codeA = 1;
+}
+
+template <typename T, int PARTS>
+mtgnn_status table(const void* W, int64_t n, int d, int dp, const uint32_t* largest, uint16_t* to, hipStream_t s) {
+  k_loss_table<T, PARTS><<<(unsigned)cdiv(n * (dp / 8), 256), 256, 0, s>>>((const T*)W, n, d, dp, largest, to, n * dp);
+  MTGNN_CHECK_LAUNCH("loss_table");
+  return MTGNN_OK;
+}
+template <typename T>
+mtgnn_status largest(const void* x, int64_t ldx, const int32_t* label, const int32_t* n_rows, int64_t rows, const void* W,
+                     const mtgnn_loss_dims* d, uint32_t* to, hipStream_t s) {
+  const auto blocks = [&](int64_t r) { return (unsigned)std::min<int64_t>(1024, cdiv(r * cdiv(d->d, 8), 256)); };
+  const unsigned xb = x ? blocks(rows) : 0;
+  k_loss_largest<T><<<xb + blocks(d->n), 256, 0, s>>>((const T*)x, ldx, label, n_rows, rows, (const T*)W, d->n, d->d, xb, to);
+  MTGNN_CHECK_LAUNCH("loss_largest");
+  return MTGNN_OK;
 }
 
 }  // namespace
 
 bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
-  constexpr int64_t MAX = int64_t(1) << 32;
+  constexpr int64_t MAX = (int64_t(1) << 32) - 1024;
   const auto tiles = [](int64_t r, int64_t c) { return large(r, c) ? cdiv(r, 256) * cdiv(c, 256) * 512 : cdiv(r, 128) * cdiv(c, 128) * 256; };
-  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX &&
-         cdiv(d->n * (up(d->d, KS) / 8), 256) * 256 < MAX && cdiv(rows * cdiv(d->d, 4), 256) * 256 < MAX &&
-         rows / ROWS * 256 < MAX / 2;
+  const int64_t units = up(d->d, KS) / 4;
+  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && (d->n + rows) * units < MAX &&
+         rows * 16 < MAX;
 }
 
 size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows)); }
 
 size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const Plan p = plan(d, rows);
-  const size_t t = table_bytes(d, p);
-  if (back) return t + al(2 * (size_t)p.p_parts * p.Rp * p.width) + al(4 * (size_t)cdiv(p.Rp, 64) * p.width);
-  return kept_bytes(p) + t + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * (size_t)cdiv(d->n, 128) * p.Rp) + al(4 * p.Rp) +
-         al(8 * cdiv(p.Rp, 16));
+  const size_t t = al(2 * (size_t)d->n * p.dp);   // a part of W
+  if (!back)
+    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) +
+           al(8 * (size_t)cdiv(d->n, large(rows, d->n) ? 256 : 128) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+  const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
+  const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
+  return 256 + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * p.width) +
+         al(4 * (size_t)cdiv(p.Rp, 64) * p.width) + al(part);
 }
 
 mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
@@ -649,35 +798,49 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
                        hipStream_t s) {
   const Plan p = plan(d, max_rows);
   const Kept k = kept(save ? save : ws, p);
+  const bool big = large(max_rows, d->n);
   char* w = (char*)ws + kept_bytes(p);
   const auto take = [&](size_t bytes) {
     char* at = w;
     w += al(bytes);
     return at;
   };
-  void* tbl = take(table_bytes(d, p));
+  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)d->n * p.dp : 0) : 4 * (size_t)d->n * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
-  float2* part = (float2*)take(8 * (size_t)cdiv(d->n, 128) * p.Rp);
+  const int tiles = (int)cdiv(d->n, big ? 256 : 128);
+  float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, 16));
-  k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), CHUNK, 0, s>>>(label, n_rows, max_rows, d->n, counts);
+  k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), CHUNK, 0, s>>>(label, n_rows, max_rows, d->n, counts, k.largest);
   MTGNN_CHECK_LAUNCH("loss_count");
+  if (!p.bf) MTGNN_TRY(largest<float>(x, ldx, label, n_rows, max_rows, W, d, k.largest, s));
   const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + KS / ROWS);
-  if (d->dtype == MTGNN_BF16)
+  if (p.bf)
     k_loss_rows<<<blocks, 256, 0, s>>>((const uint16_t*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
-                                       k.lab, k.xc, p.Rp * p.dp, row_loss);
+                                       k.lab, k.xc, p.Rp * p.dp, k.largest, row_loss);
   else
     k_loss_rows<<<blocks, 256, 0, s>>>((const float*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
-                                       k.lab, k.xc, p.Rp * p.dp, row_loss);
+                                       k.lab, k.xc, p.Rp * p.dp, k.largest, row_loss);
   MTGNN_CHECK_LAUNCH("loss_rows");
   Prod q{};
-  MTGNN_TRY(table(W, d, p, tbl, q.B, q.ldb, q.dimB, s));
-  q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp; q.planeB = d->n * (int64_t)p.dp;
-  segments(q, p.parts, p.parts);
+  q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
+  q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = d->n * (int64_t)p.dp;
+  q.topA = k.largest; q.topB = k.largest + 1;
   q.rows = max_rows; q.cols = d->n; q.K = p.dp; q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
-  MTGNN_TRY((product<STAT, true, true>(q, s)));
-  const int tiles = (int)cdiv(d->n, large(max_rows, d->n) ? 256 : 128);
+  if (p.bf) {
+    if (p.copy) {
+      MTGNN_TRY((table<uint16_t, 0>(W, d->n, d->d, p.dp, nullptr, tbl, s)));
+    } else {
+      q.B = (const uint16_t*)W; q.ldb = q.dimB = d->d;
+    }
+    segments(q, 1, 1);
+    MTGNN_TRY((product<STAT, false>(q, s)));
+  } else {
+    MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, k.largest + 1, tbl, s)));
+    segments(q, 2, 2);
+    MTGNN_TRY((product<STAT, true>(q, s)));
+  }
   k_loss_join<<<(unsigned)cdiv(max_rows, 16), 256, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums);
   MTGNN_CHECK_LAUNCH("loss_join");
   k_loss_mean<<<1, 256, 0, s>>>(k.count, sums, loss);
@@ -696,48 +859,62 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     w += al(bytes);
     return at;
   };
-  void* tbl = take(table_bytes(d, p));
-  uint16_t* P = (uint16_t*)take(2 * (size_t)p.p_parts * p.Rp * p.width);
+  uint32_t* top = (uint32_t*)take(4);
+  const int64_t plane = d->n * (int64_t)p.dp, planeX = p.Rp * p.dp;
+  uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
+  uint16_t* xh = p.bf ? (uint16_t*)take(2 * (size_t)planeX) : k.xc;
+  uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * p.width);
   float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * p.width);
-  const uint16_t* B;
-  int64_t ldb, dimB;
-  MTGNN_TRY(table(W, d, p, tbl, B, ldb, dimB, s));
-  if (dx) {
-    k_loss_zero<<<(unsigned)cdiv(max_rows * cdiv(d->d, 4), 256), 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx);
-    MTGNN_CHECK_LAUNCH("loss_zero");
+  float* part = (float*)w;
+  k_loss_zero<<<(unsigned)(dx ? cdiv(max_rows * cdiv(d->d, 4), 256) : 1), 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx,
+                                                                                       p.bf ? top : nullptr);
+  MTGNN_CHECK_LAUNCH("loss_zero");
+  if (p.bf) {
+    MTGNN_TRY((largest<uint16_t>(nullptr, 0, nullptr, nullptr, 0, W, d, top - 1, s)));
+    MTGNN_TRY((table<uint16_t, 1>(W, d->n, d->d, p.dp, top, tbl, s)));
+    MTGNN_TRY((table<uint16_t, 1>(k.xc, p.Rp, p.dp, p.dp, k.largest, xh, s)));
+  } else {
+    top = k.largest + 1;
+    MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, top, tbl, s)));
   }
   for (int64_t c = 0; c < d->n; c += p.width) {
     const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = up(cols, KS);
+    const Shares sh = shares_of(d, p, max_rows, cols);
     Prod q{};
-    q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
-    q.B = B + c * ldb; q.ldb = ldb; q.dimB = dimB; q.planeB = d->n * (int64_t)p.dp;
-    segments(q, p.parts, p.parts);
+    q.A = xh; q.lda = q.dimA = p.dp; q.planeA = planeX; q.topA = k.largest;
+    q.B = tbl + c * p.dp; q.ldb = q.dimB = p.dp; q.planeB = plane; q.topB = top;
     q.rows = max_rows; q.cols = cols; q.K = p.dp; q.count = k.count;
     q.b = b ? b + c : nullptr; q.lab = k.lab; q.c0 = c; q.stat = k.stat;
-    q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp; q.parts = p.p_parts;
+    q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp;
     q.cols_part = db ? cols_part : nullptr;
-    MTGNN_TRY((product<PROB, true, true>(q, s)));
+    if (p.bf && !p.copy) {   // the logits that the forward had
+      q.A = k.xc;
+      q.B = (const uint16_t*)W + c * d->d; q.ldb = q.dimB = d->d;
+      segments(q, 1, 1);
+      MTGNN_TRY((product<PROB, false>(q, s)));
+    } else {
+      segments(q, p.bf ? 1 : 2, p.bf ? 1 : 2);
+      MTGNN_TRY((product<PROB, true>(q, s)));
+    }
     if (db) {
       k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, large(max_rows, cols) ? 128 : 64, cols, dloss, db + c);
       MTGNN_CHECK_LAUNCH("loss_db");
     }
+    Prod g{};
+    g.A = P; g.lda = g.dimA = ldp; g.planeA = p.Rp * ldp;
+    g.cols = d->d; g.count = k.count; g.dloss = dloss;
+    segments(g, 2, p.bf ? 1 : 2);
     if (dx) {
-      Prod r{};
-      r.A = P; r.lda = r.dimA = ldp; r.planeA = p.Rp * ldp;
-      r.B = B + c * ldb; r.ldb = ldb; r.dimB = dimB; r.planeB = q.planeB;
-      segments(r, p.p_parts, p.parts);
-      r.rows = max_rows; r.cols = d->d; r.K = cols; r.count = k.count;
-      r.idx = k.idx; r.out = dx; r.ldo = lddx; r.dloss = dloss; r.add = c > 0;
-      MTGNN_TRY((product<DX, true, false>(r, s)));
+      Prod r = g;
+      r.B = tbl + c * p.dp; r.ldb = r.dimB = p.dp; r.planeB = plane; r.topB = top;
+      r.rows = max_rows; r.K = cols; r.idx = k.idx; r.out = dx; r.ldo = lddx; r.add = c > 0;
+      MTGNN_TRY((gradient<DX>(r, sh.dx, part, s)));
     }
     if (dW) {
-      Prod r{};
-      r.A = P; r.lda = r.dimA = ldp; r.planeA = p.Rp * ldp;
-      r.B = k.xc; r.ldb = r.dimB = p.dp; r.planeB = p.Rp * p.dp;
-      segments(r, p.p_parts, p.parts);
-      r.rows = cols; r.cols = d->d; r.count = k.count;
-      r.out = dW + c * d->d; r.ldo = d->d; r.dloss = dloss;
-      MTGNN_TRY((product<DW, false, false>(r, s)));
+      Prod r = g;
+      r.B = xh; r.ldb = r.dimB = p.dp; r.planeB = planeX; r.topA = k.largest;
+      r.rows = cols; r.out = dW + c * d->d; r.ldo = d->d;
+      MTGNN_TRY((gradient<DW>(r, sh.dw, part, s)));
     }
   }
   return MTGNN_OK;

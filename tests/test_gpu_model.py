@@ -5,9 +5,11 @@ Tolerances are those of a 32-bit evaluation, per element, from the magnitudes th
   embedding  one product; the gradient n - 1 sums and a product for an id of n rows: (n + 1) u of the terms' magnitude;
   norm       a row's sums are chains of at most 64 + d / 256 additions: so many u of the mean magnitudes, which enter as the
              formulas say (a wrong mean moves every h by q of it), and a few u for each operation on an element;
-  loss       a logit is a sum of d products, (d + 4) u of their magnitudes; an exponential is off by that, its own two u
-             and the difference's; a row's sum is a chain of at most 64 + n / 2,048; P is held to 2^-17 beside bfloat16,
-             2^-24 beside float32; sums of K products add K u of their magnitudes;
+  loss       a logit is a sum of d products, (d + 4) u of their magnitudes, and 8 u more where each float32 factor is two
+             float16 parts (2 u each, and 4 u the product of the second parts); an exponential is off by that, its own two u
+             and the difference's; a row's sum is a chain of at most 64 + n / 2,048; P is held to 2 u of itself or 2^-39;
+             sums of K products add K u of their magnitudes; an element in float16 parts is held to 2^-39 of its
+             matrix's largest where that is more;
   adamw      a few u of each term; in 8 bits the codes and exponents are the oracle's.
 An output in bfloat16 is rounded once more, by 2^-8 of itself."""
 
@@ -255,7 +257,10 @@ def _loss_tolerances(x, W, b, label, want, dloss, bf16):
     s = abs(dloss) / max(1, len(live))
     ax, aW = np.abs(x[live]).astype(np.float64), np.abs(W).astype(np.float64)
     mag = ax @ aW.T + (0 if b is None else np.abs(b))
+    FLOOR = 2.0 ** -39
     e_l = (d + 4) * U * mag
+    if not bf16:
+        e_l = e_l + 8 * U * mag + FLOOR * (ax.max(initial=0) * aW.sum(1) + aW.max() * ax.sum(1)[:, None])
     logits = x[live].astype(np.float64) @ W.astype(np.float64).T + (0 if b is None else b)
     gap = logits.max(1, keepdims=True) - logits
     worst = e_l.max(1, keepdims=True)
@@ -264,12 +269,12 @@ def _loss_tolerances(x, W, b, label, want, dloss, bf16):
     rows[live] = 2 * worst[:, 0] + chain + 4 * U * (np.abs(logits).max(1) + 1)
     p = want["P"][live] + (np.arange(n) == label[live][:, None])
     e_p = p * (np.exp(2 * worst) * (2 * worst + chain + (8 + 4 * gap) * U)) + 2 * U * np.abs(want["P"][live])
-    e_p = e_p + (2.0 ** -17 if bf16 else U) * np.abs(want["P"][live])
+    e_p = e_p + 2 * U * np.abs(want["P"][live]) + FLOOR
     aP, R = np.abs(want["P"][live]), len(live)
     dx = np.zeros(x.shape)
-    dx[live] = s * (e_p @ aW + (n + 12) * U * (aP @ aW))
-    return dict(rows=rows, loss=rows.sum() / max(1, R) + 2 * U * abs(want["loss"]), dx=dx,
-                dW=s * (e_p.T @ ax + (R + 12) * U * (aP.T @ ax)), db=s * (e_p.sum(0) + (R + 12) * U * aP.sum(0)))
+    dx[live] = s * (e_p @ aW + (n + 20) * U * (aP @ aW) + FLOOR * aW.max() * aP.sum(1)[:, None])
+    dW = s * (e_p.T @ ax + (R + 20) * U * (aP.T @ ax) + FLOOR * ax.max(initial=0) * aP.sum(0)[:, None])
+    return dict(rows=rows, loss=rows.sum() / max(1, R) + 2 * U * abs(want["loss"]), dx=dx, dW=dW, db=s * (e_p.sum(0) + (R + 12) * U * aP.sum(0)))
 
 
 def _check_loss(case, bf16):
