@@ -33,7 +33,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 
-constexpr int KS = 64;          // a step of the sums
+constexpr int KS = 32;          // a step of the sums
+constexpr int PAD = 64;         // rows and columns are padded to whole ones
 constexpr float LIFT = 16384.f; // what P is multiplied by
 constexpr int CHUNK = 1024;     // rows whose labels are counted together
 constexpr int ROWS = 16;        // rows that a block copies
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, cons
   if (behind) {
     const int j0 = (int)(r0 - up(max_rows, ROWS));
     if (j0 == 0 && threadIdx.x == 0) *count = first;
-    const int64_t end = up(first, KS);
+    const int64_t end = up(first, PAD);
     for (int e = threadIdx.x; e < ROWS * units; e += 256) {
       const int64_t r = first + j0 + e / units;
       if (r >= end) break;
@@ -229,7 +230,7 @@ struct Prod {
   uint32_t codeA, codeB;         // the parts of each segment, two bits each
   int segs, split;               // split: blocks that share a tile's sum, each leaving its own in `out`
   const uint32_t *topA, *topB;   // largest elements of operands in float16 parts, or NULL
-  int64_t rows, cols, K;         // the most rows; K: of a segment
+  int64_t rows, cols, K;         // the most rows; K: of a segment (its last step has a k that may be read)
   int64_t dimA, dimB;            // elements of an operand's line that may be read (A's along the sum are whole steps)
   int64_t tr, tc;                // tiles
   const int32_t* count;          // rows with a label: bounds the rows (STAT, PROB, DX) or K (DW)
@@ -243,73 +244,69 @@ struct Prod {
   const float2* stat;            // PROB: largest logit, 1 / sum
   uint16_t* P;                   // two parts
   int64_t ldp, planeP;
-  float* cols_part;              // [rows / 64][ldp] column sums of P, or NULL
+  float* cols_part;              // column sums of P times LIFT, of each half tile's rows, or NULL
   float* out;
   int64_t ldo;
   const float* dloss;
   int add;
 };
 
-// A's lines are contiguous along the sum (AK) or across it; so are B's (BK).  T x T tiles, a wave has 16 WR x 64 of one.
-// Lines go straight to LDS, 16 bytes a lane.  Along the sum: a line's eight units are swizzled by the line, as in
+// Lines go straight to LDS, 16 bytes a lane.  Along the sum: a line's four units are swizzled by the line, as in
 // linear.hip.  Across it: a k's 32-byte units by k, and the transposing read of 4 k x 16 columns gives a lane its four k;
 // the 16 lanes of such a read, and their neighbours, meet every bank once.
-template <bool AK, bool BK, int T>
-struct Tiles {
-  static constexpr int NW = T == 256 ? 8 : 4, WCOLS = T / 64, WR = T == 256 ? 8 : 4, WC = 4;
-  static constexpr int OP = T * KS / 2;   // words of an operand's tile
+// An operand's T lines of a step, loaded by NW waves; its lines are contiguous along the sum (ALONG) or across it.
+template <bool ALONG, int T, int NW>
+struct Lines {
+  static constexpr int WORDS = T * KS / 2, LOADS = T * KS / 512 / NW;   // in LDS; a wave's loads
+  static constexpr int UNITS = T / 8;                                   // 16-byte units of a k
+  static_assert(LOADS >= 1, "every wave loads");
   typedef __attribute__((address_space(3))) void* lds_ptr;
   typedef __attribute__((address_space(3))) s16x4* lds_tr;
 
-  // A lane's place in its wave's load i: line (row) and k of a step.
-  __device__ __forceinline__ static int k_of(bool along, int wid, int lane, int i) {
-    constexpr int UPR = T / 8, KR = 64 / UPR;
-    return along ? 8 * ((lane & 7) ^ (lane >> 3 & 7)) : (4 * wid + i) * KR + lane / UPR;
+  // The k of a step of a lane's load i.
+  __device__ __forceinline__ static int k_of(int wid, int lane, int i) {
+    return ALONG ? 8 * ((lane & 3) ^ (lane >> 3 & 3)) : (LOADS * wid + i) * (64 / UNITS) + lane / UNITS;
   }
-  // This wave's four loads of an operand: bytes from the tile's first line at a step's first k.  (Below 2^32: 256 lines of
-  // 2^22 elements, or 64 of them.)
-  template <bool K_>
-  __device__ __forceinline__ static void sources(int64_t ld, int64_t lines, int64_t dim, int wid, int lane, uint32_t (&off)[4]) {
+  // This wave's loads: bytes from the tile's first line at a step's first k.  (Below 2^32: 256 lines of 2^22 elements, or 32 of
+  // them.)
+  __device__ __forceinline__ static void sources(int64_t ld, int64_t lines, int64_t dim, int wid, int lane, uint32_t (&off)[LOADS]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = k_of(K_, wid, lane, i);
-      if constexpr (K_) {
-        const int row = 32 * wid + 8 * i + (lane >> 3);
+    for (int i = 0; i < LOADS; ++i) {
+      const int k = k_of(wid, lane, i);
+      if constexpr (ALONG) {
+        const int row = 16 * (LOADS * wid + i) + (lane >> 2);
         off[i] = 2u * ((uint32_t)min((int64_t)row, lines - 1) * (uint32_t)ld + k);
       } else {
-        constexpr int UPR = T / 8;
-        const int q = lane % UPR, col = ((q >> 1 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 2 + (q & 1)) * 8;
+        const int q = lane % UNITS, col = ((q >> 1 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 2 + (q & 1)) * 8;
         off[i] = 2u * ((uint32_t)k * (uint32_t)ld + (uint32_t)min((int64_t)col, dim - 8));
       }
     }
   }
   // The loads of a step that starts at `p`.  `left`: how many of its k may be read; the lanes past them read the step's first
   // (it meets zeros of the other operand).
-  template <bool K_, bool END>
-  __device__ __forceinline__ static void fill(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[4], int64_t ld, int64_t left,
+  template <bool END>
+  __device__ __forceinline__ static void fill(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[LOADS], int64_t ld, int64_t left,
                                               int wid, int lane) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < LOADS; ++i) {
       uint32_t o = off[i];
       if (END && left < KS) {
-        const int k = k_of(K_, wid, lane, i);
-        if (k >= left) o -= 2u * (uint32_t)k * (K_ ? 1u : (uint32_t)ld);
+        const int k = k_of(wid, lane, i);
+        if (k >= left) o -= 2u * (uint32_t)k * (ALONG ? 1u : (uint32_t)ld);
       }
-      __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (4 * wid + i) * 256), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (LOADS * wid + i) * 256), 16, 0, 0);
     }
   }
-  // A lane's byte in an operand's tile for line 0 and the step's first half, and what a line of 16 l and the half add to it.
-  template <bool K_>
-  __device__ __forceinline__ static uint32_t place(int fr, int fg) {
-    if (K_) return fr * (2 * KS) + (fg ^ (fr & 7)) * 16;
-    return (8 * fg + (fr >> 2)) * (2 * T) + ((fr >> 2) | (fg & 1) << 2) * 32 + (fr & 3) * 8;
+  // A lane's byte for the lines from l0 (a multiple of 64) on, and what is read there of the 16 lines from l0 + 16 l.
+  __device__ __forceinline__ static uint32_t place(int l0, int fr, int fg) {
+    if (ALONG) return (l0 + fr) * (2 * KS) + (fg ^ (fr >> 1 & 3)) * 16;
+    return ((8 * fg + (fr >> 2)) * (2 * T) + ((fr >> 2) | (fg & 1) << 2) * 32 + (fr & 3) * 8) ^ 2 * l0;
   }
-  template <bool K_>
-  __device__ __forceinline__ static bf16x8_t frag(uint32_t* buf, uint32_t at, int l, int kk) {
-    if constexpr (K_) {
-      return __builtin_bit_cast(bf16x8_t, *(const uint4*)((char*)buf + ((at ^ 64 * kk) + l * 16 * 2 * KS)));
+  __device__ __forceinline__ static bf16x8_t frag(uint32_t* buf, uint32_t at, int l) {
+    if constexpr (ALONG) {
+      return __builtin_bit_cast(bf16x8_t, *(const uint4*)((char*)buf + (at + l * 16 * 2 * KS)));
     } else {
-      char* a = (char*)buf + ((at ^ 32 * l) + kk * 32 * 2 * T);
+      char* a = (char*)buf + (at ^ 32 * l);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)a);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(a + 4 * 2 * T));
       return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -337,137 +334,85 @@ __device__ __forceinline__ f32x4 mma(bf16x8_t a, bf16x8_t b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-template <int KIND, bool HALF, int T>
-__global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss_product(Prod p) {
-  constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
-  using X = Tiles<AK, BK, T>;
-  constexpr int WR = X::WR, WC = X::WC;
-  __shared__ __align__(1024) uint32_t bufA[2 * X::OP], bufB[2 * X::OP];
-  int64_t tr, tc;
-  int share;
-  my_tile(p, tr, tc, share);
-  const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
-  const int64_t K = KIND == DW ? up(count, KS) : p.K;
-  const int64_t r0 = tr * T, c0 = tc * T;
-  if (r0 >= rows) return;
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wid / X::WCOLS * (16 * WR), wc = wid % X::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
-  uint32_t offA[4], offB[4];
-  X::template sources<AK>(p.lda, rows - r0, p.dimA - (AK ? 0 : r0), wid, lane, offA);
-  X::template sources<BK>(p.ldb, p.cols - c0, p.dimB - (BK ? 0 : c0), wid, lane, offB);
-  const uint16_t *fromA = p.A + r0 * (AK ? p.lda : 1), *fromB = p.B + c0 * (BK ? p.ldb : 1);
-  f32x4 acc[WR][WC];
-#pragma unroll
-  for (int i = 0; i < WR; ++i)
-#pragma unroll
-    for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int per = (int)cdiv(K, KS), all = per * p.segs, each = (all + p.split - 1) / p.split;
-  const int steps = max(0, min(each, all - share * each));
-  int seg = steps > 0 ? share * each / per : 0, k = share * each - seg * per;   // of the next step to load
-  const auto fill = [&](uint32_t* buf) {
-    const int64_t k0 = (int64_t)k * KS;
-    X::template fill<AK, false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane);
-    X::template fill<BK, KIND != DW>(buf + X::OP, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
-                                     (BK ? p.dimB : p.K) - k0, wid, lane);
-    if (++k == per) {
-      k = 0;
-      ++seg;
-    }
-  };
-  uint32_t atA = X::template place<AK>(fr, fg), atB = X::template place<BK>(fr, fg);
-  if (AK) atA += wr * 2 * KS;
-  else atA ^= 2 * wr;
-  if (BK) atB += wc * 2 * KS;
-  else atB ^= 2 * wc;
-  const auto multiply = [&](uint32_t* buf) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      // (formed again each time: kept for every line, the places would not leave the sums their registers)
-      asm volatile("" : "+v"(atA), "+v"(atB));
-      bf16x8_t cf[WC];
-#pragma unroll
-      for (int j = 0; j < WC; ++j) cf[j] = X::template frag<BK>(buf + X::OP, atB, j, kk);
-#pragma unroll
-      for (int i = 0; i < WR; ++i) {
-        const bf16x8_t rf = X::template frag<AK>(buf, atA, i, kk);
-#pragma unroll
-        for (int j = 0; j < WC; ++j) acc[i][j] = mma<HALF>(cf[j], rf, acc[i][j]);
-      }
-    }
-  };
-  const auto ready = [] {   // this wave's loads have arrived and its reads are done, then everybody's
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  if (steps > 0) fill(bufA);
-  int step = 0;
-  for (; step + 1 < steps; step += 2) {
-    ready();
-    fill(bufB);
-    multiply(bufA);
-    ready();
-    if (step + 2 < steps) fill(bufA);
-    multiply(bufB);
-  }
-  if (step < steps) {
-    ready();
-    multiply(bufA);
-  }
-  __syncthreads();
+// TR x TC tiles, a wave has 16 WR x 64 of one; NB steps in LDS.
+template <int TR, int TC>
+struct Shape {
+  static constexpr int WR = TR / 32, WC = 4, WCOLS = TC / 64, NW = 2 * WCOLS, NB = TR == TC ? 4 : 3, LINES = TR, COLUMNS = TC;
+};
 
-  // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.
-  const int64_t ca = c0 + wc + 4 * fg;
+// Joins (largest, sum of exponentials relative to it).
+__device__ __forceinline__ void join(float2& q, float2 o) {
+  const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;   // (nothing but classes of logit -inf: a sum of zeros)
+  q.y = q.y * __builtin_amdgcn_exp2f((q.x - from) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - from) * LOG2E);
+  q.x = m;
+}
+
+// What becomes of a wave's sums.  FULL: the tile has all of its columns.  s: LDS that nothing uses any more.
+template <int KIND, bool HALF, class S, bool FULL, int WR, int WC>
+__device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], float2* s, int64_t r0, int64_t c0, int64_t rows,
+                                      int64_t count, int share, int wid, int lane) {
+  const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
+  const int64_t ca = c0 + wc + 4 * fg, ra = r0 + wr + fr;
   const float downA = HALF && KIND != DX ? 1.f / lift(*p.topA) : 1.f, downB = HALF && KIND != DW ? 1.f / lift(*p.topB) : 1.f;
+  int at[WR];          // the label's place in the lane's columns
+  float2 st[WR];
   if constexpr (KIND == STAT || KIND == PROB) {
 #pragma unroll
-    for (int j = 0; j < WC; ++j)
+    for (int i = 0; i < WR; ++i) {
+      const int64_t r = ra + 16 * i;
+      at[i] = r < rows ? (int)(p.lab[r] - p.c0 - ca) : -1;
+      // behind the last row: exponentials of -inf
+      if (KIND == PROB) st[i] = r < rows ? p.stat[r] : make_float2(INFINITY, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < WC; ++j) {
+      float b[4] = {0.f, 0.f, 0.f, 0.f};
+      if (p.b) load_some(p.b + ca + 16 * j, FULL ? 4 : (int)min((int64_t)4, max((int64_t)0, p.cols - ca - 16 * j)), b);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int64_t c = ca + 16 * j + e;
-        const float b = c >= p.cols ? -INFINITY : p.b ? p.b[c] : 0.f;
 #pragma unroll
-        for (int i = 0; i < WR; ++i) acc[i][j][e] = c >= p.cols ? b : (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + b;
+        for (int i = 0; i < WR; ++i) {
+          acc[i][j][e] = (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + b[e];
+          if (!FULL && ca + 16 * j + e >= p.cols) acc[i][j][e] = -INFINITY;
+        }
       }
+    }
   }
+  // (a row's label is in one of the waves' columns: in most there is none)
+  const auto has = [&](int i) { return __any((unsigned)at[i] < 64u && (at[i] & 15) < 4); };
   if constexpr (KIND == STAT) {
-    float2* s = (float2*)bufA;   // [columns' waves][T]
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = r0 + wr + 16 * i + fr;
-      const int64_t at = r < rows ? p.lab[r] - p.c0 - ca : -1;
       float m = -INFINITY, v = 0.f;
 #pragma unroll
       for (int j = 0; j < WC; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          m = fmaxf(m, acc[i][j][e]);
-          if (at == 16 * j + e) p.at_label[r] = acc[i][j][e];
-        }
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+      if (has(i)) {
+#pragma unroll
+        for (int j = 0; j < WC; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at[i] == 16 * j + e) p.at_label[ra + 16 * i] = acc[i][j][e];
+      }
       m = fmaxf(m, __shfl_xor(m, 16, 64));
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      const float from = m == -INFINITY ? 0.f : m;   // (nothing but classes of logit -inf: a sum of zeros)
+      const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int j = 0; j < WC; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * LOG2E);
       v += __shfl_xor(v, 16, 64);
       v += __shfl_xor(v, 32, 64);
-      if (fg == 0) s[wid % X::WCOLS * T + wr + 16 * i + fr] = make_float2(m, v);
+      if (fg == 0) s[wid % S::WCOLS * S::LINES + wr + 16 * i + fr] = make_float2(m, v);
     }
     __syncthreads();
     const int t = threadIdx.x;
-    if (t >= T || r0 + t >= rows) return;
+    if (t >= S::LINES || r0 + t >= rows) return;
     float2 q = s[t];
 #pragma unroll
-    for (int w = 1; w < X::WCOLS; ++w) {
-      const float2 o = s[w * T + t];
-      const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;
-      q.y = q.y * __builtin_amdgcn_exp2f((q.x - from) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - from) * LOG2E);
-      q.x = m;
-    }
-    p.part[tc * p.ld_part + r0 + t] = q;
+    for (int w = 1; w < S::WCOLS; ++w) join(q, s[w * S::LINES + t]);
+    p.part[c0 / S::COLUMNS * p.ld_part + r0 + t] = q;
   }
   if constexpr (KIND == PROB) {
     float sum[WC][4];
@@ -475,30 +420,38 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
     for (int j = 0; j < WC; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[j][e] = 0.f;
-    const int64_t end = up(rows, KS);   // zeros in the rows behind the last, to a whole step
+    const int64_t end = up(rows, PAD);   // zeros in the rows behind the last, to a whole step
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = r0 + wr + 16 * i + fr;
-      const bool live = r < rows;
-      const float2 st = live ? p.stat[r] : make_float2(0.f, 0.f);
-      const int64_t at = live ? p.lab[r] - p.c0 - ca : -1;
+      const int64_t r = ra + 16 * i;
+      const float by = st[i].y * LIFT;
+#pragma unroll
+      for (int j = 0; j < WC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - st[i].x) * LOG2E) * by;
+      if (has(i)) {
+#pragma unroll
+        for (int j = 0; j < WC; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at[i] == 16 * j + e) acc[i][j][e] -= LIFT;
+      }
+      if (p.cols_part) {
+#pragma unroll
+        for (int j = 0; j < WC; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[j][e] += acc[i][j][e];
+      }
+      if (r >= end) continue;
+      uint16_t* to = p.P + r * p.ldp + ca;
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = __builtin_amdgcn_exp2f((acc[i][j][e] - st.x) * LOG2E) * st.y - (at == 16 * j + e ? 1.f : 0.f);
-          if (!live) v[e] = 0.f;
-          sum[j][e] += v[e];
-        }
-        if (r >= end || ca + 16 * j >= p.ldp) continue;
-        uint16_t* to = p.P + r * p.ldp + ca + 16 * j;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= LIFT;
+        if (!FULL && ca + 16 * j >= p.ldp) continue;
+        const f32x4 v = acc[i][j];
         const uint2 h = make_uint2(cvt2_f16(v[0], v[1]), cvt2_f16(v[2], v[3]));
-        *(uint2*)to = h;
-        *(uint2*)(to + p.planeP) = make_uint2(cvt2_f16(v[0] - lo_f16(h.x), v[1] - hi_f16(h.x)),
-                                              cvt2_f16(v[2] - lo_f16(h.y), v[3] - hi_f16(h.y)));
+        *(uint2*)(to + 16 * j) = h;
+        *(uint2*)(to + 16 * j + p.planeP) = make_uint2(cvt2_f16(v[0] - lo_f16(h.x), v[1] - hi_f16(h.x)),
+                                                       cvt2_f16(v[2] - lo_f16(h.y), v[3] - hi_f16(h.y)));
       }
     }
     if (p.cols_part) {
@@ -512,33 +465,151 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, T == 256 ? 2 : 1) void k_loss
       if (fr == 0 && r0 + wr < rows)
 #pragma unroll
         for (int j = 0; j < WC; ++j)
-          if (ca + 16 * j < p.ldp)
+          if (FULL || ca + 16 * j < p.ldp)
             *(float4*)(p.cols_part + (r0 + wr) / (16 * WR) * p.ldp + ca + 16 * j) =
                 make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
     }
   }
   if constexpr (KIND == DX || KIND == DW) {
     const bool whole = p.split == 1;   // else the sums as they are, for k_loss_shares
-    const float scale = whole ? loss_scale(count, p.dloss) / LIFT : 1.f;
+    const float down = KIND == DX ? downB : downA, scale = whole ? loss_scale(count, p.dloss) / LIFT : 1.f;
     float* const out = p.out + (whole ? 0 : share * p.rows * p.ldo);
+    const bool add = KIND == DX && whole && p.add;
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = r0 + wr + 16 * i + fr;
+      const int64_t r = ra + 16 * i;
       if (r >= rows) continue;
       float* o = out + (KIND == DX && whole ? (int64_t)p.idx[r] : r) * p.ldo + ca;
-      const bool add = KIND == DX && whole && p.add;
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
-        const int n = (int)min((int64_t)4, p.cols - ca - 16 * j);
-        if (n <= 0) continue;
+        const int n = FULL ? 4 : (int)min((int64_t)4, p.cols - ca - 16 * j);
+        if (!FULL && n <= 0) continue;
         float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
         if (add) load_some(o + 16 * j, n, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * (KIND == DX ? downB : downA) * scale + w[e];
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * down * scale + w[e];
         store_some(o + 16 * j, n, v);
       }
     }
   }
+}
+
+template <int KIND, bool HALF, int TR, int TC>
+__global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
+  using S = Shape<TR, TC>;
+  constexpr int WR = S::WR, WC = S::WC, NB = S::NB;
+  using LA = Lines<KIND != DW, TR, S::NW>;
+  using LB = Lines<KIND == STAT || KIND == PROB, TC, S::NW>;
+  constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
+  constexpr int WORDS = LA::WORDS + LB::WORDS;
+  __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS], buf2[WORDS], buf3[NB > 3 ? WORDS : 1];
+  int64_t tr, tc;
+  int share;
+  my_tile(p, tr, tc, share);
+  const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
+  const int64_t K = KIND == DW ? up(count, PAD) : p.K;
+  const int64_t r0 = tr * TR, c0 = tc * TC;
+  if (r0 >= rows) return;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
+  uint32_t offA[LA::LOADS], offB[LB::LOADS];
+  LA::sources(p.lda, rows - r0, p.dimA - (AK ? 0 : r0), wid, lane, offA);
+  LB::sources(p.ldb, p.cols - c0, p.dimB - (BK ? 0 : c0), wid, lane, offB);
+  const uint16_t *fromA = p.A + r0 * (AK ? p.lda : 1), *fromB = p.B + c0 * (BK ? p.ldb : 1);
+  f32x4 acc[WR][WC];
+#pragma unroll
+  for (int i = 0; i < WR; ++i)
+#pragma unroll
+    for (int j = 0; j < WC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int per = (int)cdiv(K, KS), all = per * p.segs, each = (all + p.split - 1) / p.split;
+  const int steps = max(0, min(each, all - share * each));
+  int seg = steps > 0 ? share * each / per : 0, k = share * each - seg * per;   // of the next step to load
+  int at = 0;
+  const auto fill = [&](uint32_t* buf) {
+    const int64_t k0 = (int64_t)k * KS;
+    LA::template fill<false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane);
+    LB::template fill<KIND != DW>(buf + LA::WORDS, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
+                                  (BK ? p.dimB : p.K) - k0, wid, lane);
+    const int go = ++at < steps, turn = k + 1 == per;   // (the last step's again past it)
+    seg += go & turn;
+    k = go ? (turn ? 0 : k + 1) : k;
+  };
+  uint32_t atA = LA::place(wr, fr, fg), atB = LB::place(wc, fr, fg);
+  // This wave's loads have arrived but for the last N steps', then everybody's.
+  const auto ready = [](auto n) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (LA::LOADS + LB::LOADS) * decltype(n)::value);   // vmcnt(..)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // A step is WR groups of WC matrix instructions, a line of A by all of the wave's B; a line is read LOOK groups before it is
+  // used.  LOOK groups before the end the next step has arrived, and its operands are read; every wave is through with the
+  // step before this one, whose buffer is filled with the step NB - 1 behind it.  What is behind the barrier for a wave to
+  // do at once are matrix instructions.  (Past the last step loads and reads go on, without a branch, and what they bring is not
+  // used.)  The buffers are objects of their own, so that the compiler knows that reads of one do not wait for the loads into the others.
+  constexpr int LOOK = WR / 2;
+  bf16x8_t a[WR], b[2][WC];
+  const auto work = [&](uint32_t* prev, uint32_t* buf, uint32_t* next, auto turn) __attribute__((always_inline)) {
+    constexpr int now = decltype(turn)::value;
+    // (places formed again each time: kept for every line, they would not leave the sums their registers)
+    asm volatile("" : "+v"(atA), "+v"(atB));
+#pragma unroll
+    for (int m = 0; m < WR; ++m) {
+      if (m == WR - LOOK) ready(std::integral_constant<int, NB - 3>());
+#pragma unroll
+      for (int j = 0; j < WC; ++j) acc[m][j] = mma<HALF>(b[now][j], a[m], acc[m][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (m == WR - LOOK) fill(prev);
+      const int q = m + LOOK;
+      a[q % WR] = LA::frag(q < WR ? buf : next, atA, q % WR);
+      if (q >= WR) {
+#pragma unroll
+        for (int j = (q - WR) * WC / LOOK; j < (q - WR + 1) * WC / LOOK; ++j)
+          b[1 - now][j] = LB::frag(next + LA::WORDS, atB, j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (steps > 0) {
+    // NB steps at a time (one way out of the loop, so that the sums stay where they are): zeros stand before the first ones.
+    const int zeros = (NB - steps % NB) % NB;
+    for (int i = threadIdx.x; i < WORDS; i += 64 * S::NW) {
+      if (zeros > 0) buf0[i] = 0u;
+      if (zeros > 1) buf1[i] = 0u;
+      if (NB > 3 && zeros > 2) buf2[i] = 0u;
+    }
+    if (zeros < 1) fill(buf0);
+    if (zeros < 2) fill(buf1);
+    if (NB > 3 && zeros < 3) fill(buf2);
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    ready(std::integral_constant<int, NB - 2>());
+#pragma unroll
+    for (int i = 0; i < LOOK; ++i) a[i] = LA::frag(buf0, atA, i);
+#pragma unroll
+    for (int j = 0; j < WC; ++j) b[0][j] = LB::frag(buf0 + LA::WORDS, atB, j);
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    for (int step = 0; step < steps; step += NB) {
+      if constexpr (NB == 4) {
+        work(buf3, buf0, buf1, even);
+        work(buf0, buf1, buf2, odd);
+        work(buf1, buf2, buf3, even);
+        work(buf2, buf3, buf0, odd);
+      } else {
+        work(buf2, buf0, buf1, even);
+        work(buf0, buf1, buf2, odd);
+        work(buf1, buf2, buf0, even);
+#pragma unroll
+        for (int j = 0; j < WC; ++j) b[0][j] = b[1][j];
+      }
+    }
+  }
+  __syncthreads();   // (waits for the loads and reads that nothing used)
+
+  // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.  Most tiles have all of their columns, and
+  // no test of each.
+  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, (float2*)buf0, r0, c0, rows, count, share, wid, lane);
+  else leave<KIND, HALF, S, false>(p, acc, (float2*)buf0, r0, c0, rows, count, share, wid, lane);
 }
 
 // The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.
@@ -636,7 +707,7 @@ __global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const flo
   v = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) v += s[i][j];
-  db[c] = v * loss_scale(n, dloss);
+  db[c] = v * (loss_scale(n, dloss) / LIFT);
 }
 
 // dx of the rows without a label; clears *largest.
@@ -658,6 +729,10 @@ size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
 constexpr size_t PIECE = size_t(1) << 30;   // bytes of P in memory at a time (where a piece is more than 256 classes wide)
 
+// Elements from a row to the next one in memory of our own: whole 128 bytes, an odd number of them, so that a column of rows is
+// not in a few of the memory's channels.
+int64_t stride(int64_t width) { return up(width, PAD) | PAD; }
+
 struct Plan {
   bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes)
   int dp;                    // padded width
@@ -666,11 +741,11 @@ struct Plan {
 Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
   Plan p;
   p.bf = d->dtype == MTGNN_BF16;
-  p.dp = (int)up(d->d, KS);
+  p.dp = (int)stride(d->d);
   p.copy = p.bf && d->d % 8 != 0;
-  p.Rp = up(rows, KS);
+  p.Rp = up(rows, PAD);
   const int64_t most = (int64_t)(PIECE / (4 * (size_t)p.Rp)) / 256 * 256;
-  p.width = std::min<int64_t>(up(d->n, KS), std::max<int64_t>(256, most));
+  p.width = std::min<int64_t>(up(d->n, PAD), std::max<int64_t>(256, most));
   return p;
 }
 
@@ -694,53 +769,78 @@ Kept kept(void* at, const Plan& p) {
   return k;
 }
 
-// Tiles of 256 where there are enough of them for the card.
-bool large(int64_t rows, int64_t cols) { return cdiv(rows, 256) * cdiv(cols, 256) >= 192; }
-// Blocks that share a tile's sum of `steps` steps.
-int shares(int64_t rows, int64_t cols, int64_t steps) {
-  const int64_t T = large(rows, cols) ? 256 : 128, t = cdiv(rows, T) * cdiv(cols, T);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(t < 256 ? cdiv(512, t) : 1, steps / 8));
+#ifndef STAT_SHAPE
+#define STAT_SHAPE 2
+#endif
+#ifndef GRAD_SHAPE
+#define GRAD_SHAPE 2
+#endif
+// A product's tiles, and the blocks that share a tile's sum.
+struct Tiling {
+  int tr, tc, split;
+  int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
+};
+// Of the logits: large tiles where there are enough of them for the card.
+Tiling tiling(int64_t rows, int64_t cols) {
+  const Tiling big{256, STAT_SHAPE == 2 ? 256 : 128, 1};
+  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 128, 1};
+}
+// Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
+// enough to fill the card with shares of them; then as many shares as leave the fewest places of the last round of
+// blocks empty.
+Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
+  Tiling g{256, GRAD_SHAPE == 2 ? 256 : 128, 1};
+  const Tiling small{128, 128, 1};
+  if (g.tiles(rows, cols) * g.tr * g.tc * 100 > small.tiles(rows, cols) * small.tr * small.tc * 115 ||
+      g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192)
+    g = small;
+  const int64_t t = g.tiles(rows, cols), slots = g.tr == g.tc && g.tr == 256 ? 256 : 512;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, steps / 16));
+  double best = 0.0;
+  for (int64_t s = 1; s <= most; ++s) {
+    const double used = (double)(t * s) / (double)(slots * cdiv(t * s, slots)) - 0.01 * (double)(s - 1);
+    if (used > best) best = used, g.split = (int)s;
+  }
+  return g;
 }
 struct Shares {
-  int dx, dw;                // of a piece
+  Tiling dx, dw;             // of a piece
   size_t bytes;
 };
 Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t cols) {
   const int segs = p.bf ? 2 : 3;
   Shares s;
-  s.dx = shares(rows, d->d, segs * cdiv(cols, KS));
-  s.dw = shares(cols, d->d, segs * cdiv(rows, KS));
-  s.bytes = std::max(s.dx > 1 ? 4 * (size_t)s.dx * rows * d->d : 0, s.dw > 1 ? 4 * (size_t)s.dw * cols * d->d : 0);
+  s.dx = tiling(rows, d->d, segs * cdiv(cols, KS));
+  s.dw = tiling(cols, d->d, segs * cdiv(rows, KS));
+  s.bytes = std::max(s.dx.split > 1 ? 4 * (size_t)s.dx.split * rows * d->d : 0, s.dw.split > 1 ? 4 * (size_t)s.dw.split * cols * d->d : 0);
   return s;
 }
 
 template <int KIND, bool HALF>
-mtgnn_status product(Prod p, hipStream_t s) {
-  const bool big = large(p.rows, p.cols);
-  const int T = big ? 256 : 128;
-  p.tr = cdiv(p.rows, T);
-  p.tc = cdiv(p.cols, T);
-  p.split = std::max(1, p.split);
+mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
+  p.tr = cdiv(p.rows, t.tr);
+  p.tc = cdiv(p.cols, t.tc);
+  p.split = t.split;
   const unsigned grid = (unsigned)(p.tr * p.tc * p.split);
   {
     TimedScope ts(site::Generic::name, s),
         kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
-    if (big) k_loss_product<KIND, HALF, 256><<<grid, 512, 0, s>>>(p);
-    else k_loss_product<KIND, HALF, 128><<<grid, 256, 0, s>>>(p);
+    if (t.tc == 256) k_loss_product<KIND, HALF, 256, 256><<<grid, 512, 0, s>>>(p);
+    else if (t.tr == 256) k_loss_product<KIND, HALF, 256, 128><<<grid, 256, 0, s>>>(p);
+    else k_loss_product<KIND, HALF, 128, 128><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
 }
 // A gradient's product, shared by `split` blocks a tile through `part`.
 template <int KIND>
-mtgnn_status gradient(Prod p, int split, float* part, hipStream_t s) {
-  if (split <= 1) return product<KIND, true>(p, s);
+mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s) {
+  if (t.split <= 1) return product<KIND, true>(p, t, s);
   Prod q = p;
-  q.split = split;
   q.out = part;
   q.ldo = p.cols;
-  MTGNN_TRY((product<KIND, true>(q, s)));
-  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256), 256, 0, s>>>(p.count, p.idx, part, split, p.rows, (int)p.cols,
+  MTGNN_TRY((product<KIND, true>(q, t, s)));
+  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256), 256, 0, s>>>(p.count, p.idx, part, t.split, p.rows, (int)p.cols,
                                                                               p.dloss, p.add, p.out, p.ldo);
   MTGNN_CHECK_LAUNCH("loss_shares");
   return MTGNN_OK;
@@ -773,8 +873,8 @@ mtgnn_status largest(const void* x, int64_t ldx, const int32_t* label, const int
 
 bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
   constexpr int64_t MAX = (int64_t(1) << 32) - 1024;
-  const auto tiles = [](int64_t r, int64_t c) { return large(r, c) ? cdiv(r, 256) * cdiv(c, 256) * 512 : cdiv(r, 128) * cdiv(c, 128) * 256; };
-  const int64_t units = up(d->d, KS) / 4;
+  const auto tiles = [](int64_t r, int64_t c) { return cdiv(r, 128) * cdiv(c, 128) * 256 + 512 * 512; };   // (shares only of few)
+  const int64_t units = stride(d->d) / 4;
   return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && (d->n + rows) * units < MAX &&
          rows * 16 < MAX;
 }
@@ -786,11 +886,11 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const size_t t = al(2 * (size_t)d->n * p.dp);   // a part of W
   if (!back)
     return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) +
-           al(8 * (size_t)cdiv(d->n, large(rows, d->n) ? 256 : 128) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).tc) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
-  return 256 + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * p.width) +
-         al(4 * (size_t)cdiv(p.Rp, 64) * p.width) + al(part);
+  return 256 + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
+         al(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width)) + al(part);
 }
 
 mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
@@ -798,7 +898,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
                        hipStream_t s) {
   const Plan p = plan(d, max_rows);
   const Kept k = kept(save ? save : ws, p);
-  const bool big = large(max_rows, d->n);
+  const Tiling tl = tiling(max_rows, d->n);
   char* w = (char*)ws + kept_bytes(p);
   const auto take = [&](size_t bytes) {
     char* at = w;
@@ -807,14 +907,14 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   };
   uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)d->n * p.dp : 0) : 4 * (size_t)d->n * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
-  const int tiles = (int)cdiv(d->n, big ? 256 : 128);
+  const int tiles = (int)cdiv(d->n, tl.tc);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, 16));
   k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), CHUNK, 0, s>>>(label, n_rows, max_rows, d->n, counts, k.largest);
   MTGNN_CHECK_LAUNCH("loss_count");
   if (!p.bf) MTGNN_TRY(largest<float>(x, ldx, label, n_rows, max_rows, W, d, k.largest, s));
-  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + KS / ROWS);
+  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS);
   if (p.bf)
     k_loss_rows<<<blocks, 256, 0, s>>>((const uint16_t*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
                                        k.lab, k.xc, p.Rp * p.dp, k.largest, row_loss);
@@ -826,7 +926,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
   q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = d->n * (int64_t)p.dp;
   q.topA = k.largest; q.topB = k.largest + 1;
-  q.rows = max_rows; q.cols = d->n; q.K = p.dp; q.count = k.count;
+  q.rows = max_rows; q.cols = d->n; q.K = up(d->d, KS); q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
   if (p.bf) {
     if (p.copy) {
@@ -835,11 +935,11 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
       q.B = (const uint16_t*)W; q.ldb = q.dimB = d->d;
     }
     segments(q, 1, 1);
-    MTGNN_TRY((product<STAT, false>(q, s)));
+    MTGNN_TRY((product<STAT, false>(q, tl, s)));
   } else {
     MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, k.largest + 1, tbl, s)));
     segments(q, 2, 2);
-    MTGNN_TRY((product<STAT, true>(q, s)));
+    MTGNN_TRY((product<STAT, true>(q, tl, s)));
   }
   k_loss_join<<<(unsigned)cdiv(max_rows, 16), 256, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums);
   MTGNN_CHECK_LAUNCH("loss_join");
@@ -863,8 +963,8 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
   const int64_t plane = d->n * (int64_t)p.dp, planeX = p.Rp * p.dp;
   uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
   uint16_t* xh = p.bf ? (uint16_t*)take(2 * (size_t)planeX) : k.xc;
-  uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * p.width);
-  float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * p.width);
+  uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * stride(p.width));
+  float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width));
   float* part = (float*)w;
   k_loss_zero<<<(unsigned)(dx ? cdiv(max_rows * cdiv(d->d, 4), 256) : 1), 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx,
                                                                                        p.bf ? top : nullptr);
@@ -878,12 +978,13 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, top, tbl, s)));
   }
   for (int64_t c = 0; c < d->n; c += p.width) {
-    const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = up(cols, KS);
+    const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = stride(cols);
     const Shares sh = shares_of(d, p, max_rows, cols);
+    const Tiling tl = tiling(max_rows, cols);
     Prod q{};
     q.A = xh; q.lda = q.dimA = p.dp; q.planeA = planeX; q.topA = k.largest;
     q.B = tbl + c * p.dp; q.ldb = q.dimB = p.dp; q.planeB = plane; q.topB = top;
-    q.rows = max_rows; q.cols = cols; q.K = p.dp; q.count = k.count;
+    q.rows = max_rows; q.cols = cols; q.K = up(d->d, KS); q.count = k.count;
     q.b = b ? b + c : nullptr; q.lab = k.lab; q.c0 = c; q.stat = k.stat;
     q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp;
     q.cols_part = db ? cols_part : nullptr;
@@ -891,13 +992,13 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
       q.A = k.xc;
       q.B = (const uint16_t*)W + c * d->d; q.ldb = q.dimB = d->d;
       segments(q, 1, 1);
-      MTGNN_TRY((product<PROB, false>(q, s)));
+      MTGNN_TRY((product<PROB, false>(q, tl, s)));
     } else {
       segments(q, p.bf ? 1 : 2, p.bf ? 1 : 2);
-      MTGNN_TRY((product<PROB, true>(q, s)));
+      MTGNN_TRY((product<PROB, true>(q, tl, s)));
     }
     if (db) {
-      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, large(max_rows, cols) ? 128 : 64, cols, dloss, db + c);
+      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.tr / 2, cols, dloss, db + c);
       MTGNN_CHECK_LAUNCH("loss_db");
     }
     Prod g{};
