@@ -347,40 +347,60 @@ __device__ __forceinline__ void join(float2& q, float2 o) {
   q.x = m;
 }
 
+// What the end of a tile needs of its rows and columns, requested before the products so that it need not be waited for.
+template <int KIND, class S>
+struct Ahead {
+  int at[S::WR];         // the label's place in the lane's columns
+  float2 st[S::WR];      // the row's largest logit, 1 / sum
+  float b[S::WC][4];
+  __device__ __forceinline__ void load(const Prod& p, int64_t ra, int64_t ca, int64_t rows) {
+    if constexpr (KIND == STAT || KIND == PROB) {
+#pragma unroll
+      for (int i = 0; i < S::WR; ++i) {
+        const int64_t r = min(ra + 16 * i, rows - 1);
+        at[i] = p.lab[r];
+        if (KIND == PROB) st[i] = p.stat[r];
+      }
+#pragma unroll
+      for (int j = 0; j < S::WC; ++j) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[j][e] = 0.f;
+        if (p.b) load_some(p.b + ca + 16 * j, (int)max((int64_t)0, min((int64_t)4, p.cols - ca - 16 * j)), b[j]);
+      }
+    }
+  }
+};
+
 // What becomes of a wave's sums.  FULL: the tile has all of its columns.  s: LDS that nothing uses any more.
 template <int KIND, bool HALF, class S, bool FULL, int WR, int WC>
-__device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], float2* s, int64_t r0, int64_t c0, int64_t rows,
-                                      int64_t count, int share, int wid, int lane) {
+__device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead<KIND, S>& h, uint32_t* lds, int64_t r0, int64_t c0,
+                                      int64_t rows, int64_t count, int share, int wid, int lane) {
   const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
   const int64_t ca = c0 + wc + 4 * fg, ra = r0 + wr + fr;
   const float downA = HALF && KIND != DX ? 1.f / lift(*p.topA) : 1.f, downB = HALF && KIND != DW ? 1.f / lift(*p.topB) : 1.f;
-  int at[WR];          // the label's place in the lane's columns
-  float2 st[WR];
+  auto &at = h.at;
+  auto &st = h.st;
   if constexpr (KIND == STAT || KIND == PROB) {
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = ra + 16 * i;
-      at[i] = r < rows ? (int)(p.lab[r] - p.c0 - ca) : -1;
-      // behind the last row: exponentials of -inf
-      if (KIND == PROB) st[i] = r < rows ? p.stat[r] : make_float2(INFINITY, 0.f);
+      const bool live = ra + 16 * i < rows;
+      at[i] = live ? (int)(at[i] - p.c0 - ca) : -1;
+      if (KIND == PROB && !live) st[i] = make_float2(INFINITY, 0.f);   // behind the last row: exponentials of -inf
     }
 #pragma unroll
-    for (int j = 0; j < WC; ++j) {
-      float b[4] = {0.f, 0.f, 0.f, 0.f};
-      if (p.b) load_some(p.b + ca + 16 * j, FULL ? 4 : (int)min((int64_t)4, max((int64_t)0, p.cols - ca - 16 * j)), b);
+    for (int j = 0; j < WC; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < WR; ++i) {
-          acc[i][j][e] = (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + b[e];
+          acc[i][j][e] = (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + h.b[j][e];
           if (!FULL && ca + 16 * j + e >= p.cols) acc[i][j][e] = -INFINITY;
         }
-      }
-    }
   }
   // (a row's label is in one of the waves' columns: in most there is none)
   const auto has = [&](int i) { return __any((unsigned)at[i] < 64u && (at[i] & 15) < 4); };
   if constexpr (KIND == STAT) {
+    float2* s = (float2*)lds;   // [columns' waves][lines]
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
       float m = -INFINITY, v = 0.f;
@@ -423,7 +443,6 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], float
     const int64_t end = up(rows, PAD);   // zeros in the rows behind the last, to a whole step
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = ra + 16 * i;
       const float by = st[i].y * LIFT;
 #pragma unroll
       for (int j = 0; j < WC; ++j)
@@ -442,17 +461,28 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], float
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[j][e] += acc[i][j][e];
       }
-      if (r >= end) continue;
-      uint16_t* to = p.P + r * p.ldp + ca;
+      // sixteen rows through LDS (the wave's own place): written as they lie there, in whole 128 bytes (in the lanes'
+      // order 32 bytes a row at a time took 823 us for 612, 7,373 x 32,768 x 1,024)
+      char* w = (char*)lds + wid * (2 * 16 * 144);
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
-        if (!FULL && ca + 16 * j >= p.ldp) continue;
         const f32x4 v = acc[i][j];
-        const uint2 h = make_uint2(cvt2_f16(v[0], v[1]), cvt2_f16(v[2], v[3]));
-        *(uint2*)(to + 16 * j) = h;
-        *(uint2*)(to + 16 * j + p.planeP) = make_uint2(cvt2_f16(v[0] - lo_f16(h.x), v[1] - hi_f16(h.x)),
-                                                       cvt2_f16(v[2] - lo_f16(h.y), v[3] - hi_f16(h.y)));
+        const uint2 hi = make_uint2(cvt2_f16(v[0], v[1]), cvt2_f16(v[2], v[3]));
+        *(uint2*)(w + fr * 144 + 32 * j + 8 * fg) = hi;
+        *(uint2*)(w + 16 * 144 + fr * 144 + 32 * j + 8 * fg) =
+            make_uint2(cvt2_f16(v[0] - lo_f16(hi.x), v[1] - hi_f16(hi.x)), cvt2_f16(v[2] - lo_f16(hi.y), v[3] - hi_f16(hi.y)));
       }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int h8 = 0; h8 < 2; ++h8) {
+          const int line = 8 * h8 + (lane >> 3);
+          const uint4 v = *(const uint4*)(w + q * 16 * 144 + line * 144 + (lane & 7) * 16);
+          const int64_t rr = r0 + wr + 16 * i + line, cc = c0 + wc + (lane & 7) * 8;
+          if (rr < end && (FULL || cc < p.ldp)) *(uint4*)(p.P + q * p.planeP + rr * p.ldp + cc) = v;
+        }
+      __builtin_amdgcn_wave_barrier();
     }
     if (p.cols_part) {
 #pragma unroll
@@ -475,21 +505,27 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], float
     const float down = KIND == DX ? downB : downA, scale = whole ? loss_scale(count, p.dloss) / LIFT : 1.f;
     float* const out = p.out + (whole ? 0 : share * p.rows * p.ldo);
     const bool add = KIND == DX && whole && p.add;
+    float* w = (float*)lds + wid * (16 * 68);   // (as above: whole 256 bytes of a row)
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const int64_t r = ra + 16 * i;
-      if (r >= rows) continue;
-      float* o = out + (KIND == DX && whole ? (int64_t)p.idx[r] : r) * p.ldo + ca;
 #pragma unroll
-      for (int j = 0; j < WC; ++j) {
-        const int n = FULL ? 4 : (int)min((int64_t)4, p.cols - ca - 16 * j);
-        if (!FULL && n <= 0) continue;
-        float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
-        if (add) load_some(o + 16 * j, n, w);
+      for (int j = 0; j < WC; ++j) *(f32x4*)(w + fr * 68 + 16 * j + 4 * fg) = acc[i][j];
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * down * scale + w[e];
-        store_some(o + 16 * j, n, v);
+      for (int q = 0; q < 4; ++q) {
+        const int line = 4 * q + fg;
+        const f32x4 f = *(const f32x4*)(w + line * 68 + 4 * fr);
+        const int64_t r = r0 + wr + 16 * i + line, c = c0 + wc + 4 * fr;
+        const int n = FULL ? 4 : (int)min((int64_t)4, p.cols - c);
+        if (r >= rows || n <= 0) continue;
+        float* o = out + (KIND == DX && whole ? (int64_t)p.idx[r] : r) * p.ldo + c;
+        float v[4], old[4] = {0.f, 0.f, 0.f, 0.f};
+        if (add) load_some(o, n, old);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f[e] * down * scale + old[e];
+        store_some(o, n, v);
       }
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -516,6 +552,8 @@ __global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   LA::sources(p.lda, rows - r0, p.dimA - (AK ? 0 : r0), wid, lane, offA);
   LB::sources(p.ldb, p.cols - c0, p.dimB - (BK ? 0 : c0), wid, lane, offB);
   const uint16_t *fromA = p.A + r0 * (AK ? p.lda : 1), *fromB = p.B + c0 * (BK ? p.ldb : 1);
+  Ahead<KIND, S> ahead;
+  ahead.load(p, r0 + wr + fr, c0 + wc + 4 * fg, rows);
   f32x4 acc[WR][WC];
 #pragma unroll
   for (int i = 0; i < WR; ++i)
@@ -608,8 +646,8 @@ __global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod 
 
   // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.  Most tiles have all of their columns, and
   // no test of each.
-  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, (float2*)buf0, r0, c0, rows, count, share, wid, lane);
-  else leave<KIND, HALF, S, false>(p, acc, (float2*)buf0, r0, c0, rows, count, share, wid, lane);
+  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
+  else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
 // The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.
