@@ -334,10 +334,10 @@ __device__ __forceinline__ f32x4 mma(bf16x8_t a, bf16x8_t b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// TR x TC tiles, a wave has 16 WR x 64 of one; NB steps in LDS.
-template <int TR, int TC>
+// T x T tiles, a wave has 16 WR x 64 of one.
+template <int T>
 struct Shape {
-  static constexpr int WR = TR / 32, WC = 4, WCOLS = TC / 64, NW = 2 * WCOLS, NB = TR == TC ? 4 : 3, LINES = TR, COLUMNS = TC;
+  static constexpr int WR = T / 32, WC = 4, WCOLS = T / 64, NW = 2 * WCOLS, LINES = T;
 };
 
 // Joins (largest, sum of exponentials relative to it).
@@ -432,7 +432,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
     float2 q = s[t];
 #pragma unroll
     for (int w = 1; w < S::WCOLS; ++w) join(q, s[w * S::LINES + t]);
-    p.part[c0 / S::COLUMNS * p.ld_part + r0 + t] = q;
+    p.part[c0 / S::LINES * p.ld_part + r0 + t] = q;
   }
   if constexpr (KIND == PROB) {
     float sum[WC][4];
@@ -530,21 +530,21 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
   }
 }
 
-template <int KIND, bool HALF, int TR, int TC>
-__global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
-  using S = Shape<TR, TC>;
-  constexpr int WR = S::WR, WC = S::WC, NB = S::NB;
-  using LA = Lines<KIND != DW, TR, S::NW>;
-  using LB = Lines<KIND == STAT || KIND == PROB, TC, S::NW>;
+template <int KIND, bool HALF, int T>
+__global__ __launch_bounds__(T == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
+  using S = Shape<T>;
   constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
-  constexpr int WORDS = LA::WORDS + LB::WORDS;
-  __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS], buf2[WORDS], buf3[NB > 3 ? WORDS : 1];
+  constexpr int WR = S::WR, WC = S::WC;
+  using LA = Lines<AK, T, S::NW>;
+  using LB = Lines<BK, T, S::NW>;
+  constexpr int WORDS = LA::WORDS + LB::WORDS, LOADS = LA::LOADS + LB::LOADS;
+  __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS], buf2[WORDS], buf3[WORDS];
   int64_t tr, tc;
   int share;
   my_tile(p, tr, tc, share);
   const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
   const int64_t K = KIND == DW ? up(count, PAD) : p.K;
-  const int64_t r0 = tr * TR, c0 = tc * TC;
+  const int64_t r0 = tr * T, c0 = tc * T;
   if (r0 >= rows) return;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
@@ -576,13 +576,13 @@ __global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   // This wave's loads have arrived but for the last N steps', then everybody's.
   const auto ready = [](auto n) {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (LA::LOADS + LB::LOADS) * decltype(n)::value);   // vmcnt(..)
+    __builtin_amdgcn_s_waitcnt(0x0f70 | LOADS * decltype(n)::value);   // vmcnt(..)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
   // A step is WR groups of WC matrix instructions, a line of A by all of the wave's B; a line is read LOOK groups before it is
   // used.  LOOK groups before the end the next step has arrived, and its operands are read; every wave is through with the
-  // step before this one, whose buffer is filled with the step NB - 1 behind it.  What is behind the barrier for a wave to
+  // step before this one, whose buffer is filled with the step three behind it.  What is behind the barrier for a wave to
   // do at once are matrix instructions.  (Past the last step loads and reads go on, without a branch, and what they bring is not
   // used.)  The buffers are objects of their own, so that the compiler knows that reads of one do not wait for the loads into the others.
   constexpr int LOOK = WR / 2;
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod 
     asm volatile("" : "+v"(atA), "+v"(atB));
 #pragma unroll
     for (int m = 0; m < WR; ++m) {
-      if (m == WR - LOOK) ready(std::integral_constant<int, NB - 3>());
+      if (m == WR - LOOK) ready(std::integral_constant<int, 1>());
 #pragma unroll
       for (int j = 0; j < WC; ++j) acc[m][j] = mma<HALF>(b[now][j], a[m], acc[m][j]);
       __builtin_amdgcn_sched_barrier(0);
@@ -609,44 +609,36 @@ __global__ __launch_bounds__(TC == 256 ? 512 : 256, 2) void k_loss_product(Prod 
     }
   };
   if (steps > 0) {
-    // NB steps at a time (one way out of the loop, so that the sums stay where they are): zeros stand before the first ones.
-    const int zeros = (NB - steps % NB) % NB;
+    // Four steps at a time (one way out of the loop, so that the sums stay where they are): zeros stand before the first ones.
+    const int zeros = -steps & 3;
     for (int i = threadIdx.x; i < WORDS; i += 64 * S::NW) {
       if (zeros > 0) buf0[i] = 0u;
       if (zeros > 1) buf1[i] = 0u;
-      if (NB > 3 && zeros > 2) buf2[i] = 0u;
+      if (zeros > 2) buf2[i] = 0u;
     }
     if (zeros < 1) fill(buf0);
     if (zeros < 2) fill(buf1);
-    if (NB > 3 && zeros < 3) fill(buf2);
+    if (zeros < 3) fill(buf2);
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-    ready(std::integral_constant<int, NB - 2>());
+    ready(std::integral_constant<int, 2>());
 #pragma unroll
     for (int i = 0; i < LOOK; ++i) a[i] = LA::frag(buf0, atA, i);
 #pragma unroll
     for (int j = 0; j < WC; ++j) b[0][j] = LB::frag(buf0 + LA::WORDS, atB, j);
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
-    for (int step = 0; step < steps; step += NB) {
-      if constexpr (NB == 4) {
-        work(buf3, buf0, buf1, even);
-        work(buf0, buf1, buf2, odd);
-        work(buf1, buf2, buf3, even);
-        work(buf2, buf3, buf0, odd);
-      } else {
-        work(buf2, buf0, buf1, even);
-        work(buf0, buf1, buf2, odd);
-        work(buf1, buf2, buf0, even);
-#pragma unroll
-        for (int j = 0; j < WC; ++j) b[0][j] = b[1][j];
-      }
+    for (int step = 0; step < steps; step += 4) {
+      work(buf3, buf0, buf1, even);
+      work(buf0, buf1, buf2, odd);
+      work(buf1, buf2, buf3, even);
+      work(buf2, buf3, buf0, odd);
     }
   }
   __syncthreads();   // (waits for the loads and reads that nothing used)
 
   // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.  Most tiles have all of their columns, and
   // no test of each.
-  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
+  if (c0 + T <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
   else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
@@ -807,32 +799,24 @@ Kept kept(void* at, const Plan& p) {
   return k;
 }
 
-#ifndef STAT_SHAPE
-#define STAT_SHAPE 2
-#endif
-#ifndef GRAD_SHAPE
-#define GRAD_SHAPE 2
-#endif
-// A product's tiles, and the blocks that share a tile's sum.
+// A product's tiles, T wide and high, and the blocks that share a tile's sum.
 struct Tiling {
-  int tr, tc, split;
-  int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
+  int T, split;
+  int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, T) * cdiv(cols, T); }
 };
 // Of the logits: large tiles where there are enough of them for the card.
 Tiling tiling(int64_t rows, int64_t cols) {
-  const Tiling big{256, STAT_SHAPE == 2 ? 256 : 128, 1};
-  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 128, 1};
+  const Tiling big{256, 1};
+  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 1};
 }
 // Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
 // enough to fill the card with shares of them; then as many shares as leave the fewest places of the last round of
 // blocks empty.
 Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
-  Tiling g{256, GRAD_SHAPE == 2 ? 256 : 128, 1};
-  const Tiling small{128, 128, 1};
-  if (g.tiles(rows, cols) * g.tr * g.tc * 100 > small.tiles(rows, cols) * small.tr * small.tc * 115 ||
-      g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192)
-    g = small;
-  const int64_t t = g.tiles(rows, cols), slots = g.tr == g.tc && g.tr == 256 ? 256 : 512;
+  Tiling g{256, 1};
+  const Tiling small{128, 1};
+  if (g.tiles(rows, cols) * 4 * 100 > small.tiles(rows, cols) * 115 || g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192) g = small;
+  const int64_t t = g.tiles(rows, cols), slots = g.T == 256 ? 256 : 512;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, steps / 16));
   double best = 0.0;
   for (int64_t s = 1; s <= most; ++s) {
@@ -856,16 +840,15 @@ Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t 
 
 template <int KIND, bool HALF>
 mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
-  p.tr = cdiv(p.rows, t.tr);
-  p.tc = cdiv(p.cols, t.tc);
+  p.tr = cdiv(p.rows, t.T);
+  p.tc = cdiv(p.cols, t.T);
   p.split = t.split;
   const unsigned grid = (unsigned)(p.tr * p.tc * p.split);
   {
     TimedScope ts(site::Generic::name, s),
         kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
-    if (t.tc == 256) k_loss_product<KIND, HALF, 256, 256><<<grid, 512, 0, s>>>(p);
-    else if (t.tr == 256) k_loss_product<KIND, HALF, 256, 128><<<grid, 256, 0, s>>>(p);
-    else k_loss_product<KIND, HALF, 128, 128><<<grid, 256, 0, s>>>(p);
+    if (t.T == 256) k_loss_product<KIND, HALF, 256><<<grid, 512, 0, s>>>(p);
+    else k_loss_product<KIND, HALF, 128><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
@@ -924,7 +907,7 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const size_t t = al(2 * (size_t)d->n * p.dp);   // a part of W
   if (!back)
     return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) +
-           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).tc) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).T) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
   return 256 + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
@@ -945,7 +928,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   };
   uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)d->n * p.dp : 0) : 4 * (size_t)d->n * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
-  const int tiles = (int)cdiv(d->n, tl.tc);
+  const int tiles = (int)cdiv(d->n, tl.T);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, 16));
@@ -1036,7 +1019,7 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
       MTGNN_TRY((product<PROB, true>(q, tl, s)));
     }
     if (db) {
-      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.tr / 2, cols, dloss, db + c);
+      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.T / 2, cols, dloss, db + c);
       MTGNN_CHECK_LAUNCH("loss_db");
     }
     Prod g{};
