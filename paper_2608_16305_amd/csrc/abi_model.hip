@@ -78,7 +78,7 @@ mtgnn_status mtgnn_embedding_bwd(const int32_t* ids, const int32_t* n_rows, int6
   MTGNN_TRY(check_aligned(ws, "ws is not 16-byte aligned"));
   const int64_t to = d->n * d->d * 4, from = ((max_rows - 1) * lddy + d->d) * 4;
   if (overlap(Rows{dtable, to, to}, Rows{dy, from, from}, 1)) return fail(MTGNN_EINVAL, "dtable overlaps dy");
-  return embed_bwd_impl(ids, n_rows, max_rows, dy, lddy, d, dtable, ws, ws_bytes, stream);
+  return embed_bwd_impl(ids, n_rows, max_rows, dy, lddy, d, dtable, ws, stream);
 }
 
 mtgnn_status mtgnn_layer_norm(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const float* gamma,

@@ -8,8 +8,8 @@
 //
 // The 8-bit states hold the root of v, whose range is half as many binades: e4m3 has 2^17 between its largest and smallest
 // number, so a v 2^-35 of its block's largest is still held.  They are formed in 64 bits and rounded once (m + (1 - b1) g
-// near the border of two codes is decided as the formula says, whatever float32 would make of it); a root that is
-// not zero never becomes zero, for m / sqrt(v) has no bound there.  The parameter's step uses m and v before that rounding.
+// near the border of two codes is decided as the formula says, whatever float32 would make of it; away from one float32
+// decides, which is half of the instructions); a root that is not zero never becomes zero, for m / sqrt(v) has no bound there.  The parameter's step uses m and v before that rounding.
 #include <algorithm>
 #include <cmath>
 
@@ -36,6 +36,7 @@ struct Coef {
 };
 
 typedef uint32_t word_at1 __attribute__((aligned(1)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ double pow_int(double b, int t) {   // by squares
   double r = 1.0;
@@ -45,29 +46,83 @@ __device__ __forceinline__ double pow_int(double b, int t) {   // by squares
 }
 
 // e4m3: sign, four bits of exponent (bias 7), three of mantissa; 448 the largest, 2^-9 the least; no infinity, 0x7f is NaN.
-__device__ __forceinline__ float of_e4m3(uint32_t c) {
-  return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
-}
-// The nearest code (ties to even) of a >= 0 that is at most 448.
-__device__ __forceinline__ uint32_t to_e4m3(double a) {
-  if (!(a >= 0.015625)) return a != a ? 0x7fu : (uint32_t)rint(a * 512.0);   // multiples of 2^-9 below 2^-6 (8 of them: 2^-6)
+// The nearest code (ties to even) of a >= 0 that is at most 448; of what is not finite NaN.
+__device__ __attribute__((noinline)) uint32_t exact_code(double a) {
+  if (!(a < INFINITY)) return 0x7fu;
+  if (a < 0.015625) return (uint32_t)rint(a * 512.0);   // multiples of 2^-9 below 2^-6 (8 of them: 2^-6)
   const uint64_t u = (uint64_t)__double_as_longlong(a);
-  const uint32_t c = (uint32_t)((u + 0xffffffffffffull + (u >> 49 & 1)) >> 49) - (1016u << 3);
-  return c < 0x7fu ? c : 0x7fu;
+  return (uint32_t)((u + 0xffffffffffffull + (u >> 49 & 1)) >> 49) - (1016u << 3);
+}
+// Whether a float32 value that is off by a few units in its last place may be on the wrong side of a border of two codes: the 20
+// bits behind a code's are near a half.  (Below 2^-6 the codes are 2^-9 apart: as far as they are from 2^-6 on.)
+__device__ __forceinline__ bool near_border(float a) {
+  const uint32_t u = __float_as_uint(a < 0.015625f ? a + 0.015625f : a);
+  return (u & 0xfffffu) - 0x7fff8u <= 0x10u || !(a < 448.f);
 }
 // The biased exponent e of a block whose largest magnitude is `top`: top <= 448 2^(e - 127), the least such e.
-__device__ __forceinline__ int block_exponent(double top) {
+__device__ __forceinline__ int exact_exponent(double top) {
   if (!(top > 0.0)) return 0;
   const uint64_t u = (uint64_t)__double_as_longlong(top);
   const int x = (int)(u >> 52) - 1022;   // top = f 2^x, f in [0.5, 1) (a subnormal one: x = -1022)
   const int e = x - 9 + ((u & 0xfffffffffffffull) > 0xc000000000000ull);
   return min(max(e, -127), 127) + 127;
 }
+__device__ __forceinline__ int block_exponent(float top) {
+  const uint32_t u = __float_as_uint(top);
+  return min(max((int)(u >> 23) - 126 - 9 + (int)((u & 0x7fffffu) > 0x600000u) + 127, 0), 254);
+}
+__device__ __forceinline__ bool exponent_unsure(float top) {   // near 448 times a power of two
+  return (__float_as_uint(top) & 0x7fffffu) - 0x5ffff8u <= 0x10u;
+}
 __device__ __forceinline__ double pow2(int e) { return __longlong_as_double((long long)(e + 1023) << 52); }   // |e| < 1023
-__device__ __forceinline__ double max8(double v) {   // over eight lanes; NaN stays out (its codes say it)
+__device__ __forceinline__ float pow2f(int e) { return e > -127 ? __uint_as_float((uint32_t)(e + 127) << 23) : __uint_as_float(0x400000u); }   // -127 .. 127
+__device__ __forceinline__ float max8(float v) {   // over eight lanes
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ double max8(double v) {
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) v = fmax(v, __shfl_xor(v, o, 64));
   return v;
+}
+__device__ __forceinline__ float finite(float v) { return v < INFINITY ? v : 0.f; }   // (v >= 0 or NaN)
+__device__ __forceinline__ double finite(double v) { return v < INFINITY ? v : 0.0; }
+
+// The codes and the exponent of four elements' magnitudes, x in 64 bits and f as float32 (of the block's eight lanes).
+// Decided in float32; what is near a border, from x itself (root: from its root).
+template <bool ROOT>
+__device__ __forceinline__ void encode(const double (&x)[PER], const float (&f)[PER], uint32_t& codes, int& exponent) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) top = fmaxf(top, finite(f[j]));
+  top = max8(top);
+  exponent = block_exponent(top);
+  if (__any(exponent_unsure(top))) {
+    double t = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) t = fmax(t, finite(fabs(x[j])));
+    t = max8(t);
+    exponent = exact_exponent(ROOT ? sqrt(t) : t);
+  }
+  const float by = pow2f(127 - exponent);
+  float a[PER];
+  bool unsure = false;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    a[j] = f[j] * by;
+    unsure |= near_border(a[j]);
+  }
+  int c = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false);
+  c = __builtin_amdgcn_cvt_pk_fp8_f32(a[2], a[3], c, true);
+  codes = (uint32_t)c;
+  if (__any(unsure)) {
+    uint32_t sure = 0u;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      sure |= (near_border(a[j]) ? exact_code((ROOT ? sqrt(x[j]) : fabs(x[j])) * pow2(127 - exponent)) : codes >> 8 * j & 255u) << 8 * j;
+    codes = sure;
+  }
 }
 
 template <bool BITS8>
@@ -86,7 +141,7 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
     ibc1 = (float)(1.0 / (1.0 - pow_int(c.b1, n)));
     ibc2 = (float)(1.0 / (1.0 - pow_int(c.b2, n)));
   }
-  const float keep = c.lr * t.decay;
+  const float keep = c.lr * t.decay, sbc2 = sqrtf(ibc2);
   const double o1 = 1.0 - c.b1, o2 = 1.0 - c.b2;
   float p[4][PER], g[4][PER], m[4][PER], v[4][PER];
   uint32_t mc[4], vc[4];
@@ -122,29 +177,28 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
     const int64_t e = e0 + i * NT * PER;
     const int n = (int)min((int64_t)PER, t.n - e);
     if constexpr (BITS8) {
-      double md[PER], vd[PER], mt = 0.0, vt = 0.0;
-      const double ms = pow2(me[i] - 127), vs = pow2(ve[i] - 127);
+      double md[PER], vd[PER];
+      const float ms = pow2f(me[i] - 127), vs = pow2f(ve[i] - 127);
+      float am[PER], mo[PER], ro[PER];
+      const f32x2 m01 = __builtin_amdgcn_cvt_pk_f32_fp8(mc[i], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(mc[i], true);
+      const f32x2 r01 = __builtin_amdgcn_cvt_pk_f32_fp8(vc[i], false), r23 = __builtin_amdgcn_cvt_pk_f32_fp8(vc[i], true);
+      mo[0] = m01.x; mo[1] = m01.y; mo[2] = m23.x; mo[3] = m23.y;
+      ro[0] = r01.x; ro[1] = r01.y; ro[2] = r23.x; ro[3] = r23.y;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const double r = (double)of_e4m3(vc[i] >> 8 * j & 255u) * vs, x = j < n ? (double)g[i][j] : 0.0;
-        md[j] = c.b1 * ((double)of_e4m3(mc[i] >> 8 * j & 255u) * ms) + o1 * x;
-        vd[j] = c.b2 * (r * r) + o2 * (x * x);
-        mt = fmax(mt, fabs(md[j]) < INFINITY ? fabs(md[j]) : 0.0);   // (what is infinite has a code of its own: NaN)
-        vt = fmax(vt, vd[j] < INFINITY ? vd[j] : 0.0);
+      for (int j = 0; j < PER; ++j) {   // (codes times their units are exact)
+        const double r = (double)(ro[j] * vs), x = j < n ? (double)g[i][j] : 0.0;
+        md[j] = fma(c.b1, (double)(mo[j] * ms), o1 * x);
+        vd[j] = fma(c.b2, r * r, o2 * (x * x));
         m[i][j] = (float)md[j];
-        v[i][j] = (float)vd[j];
+        am[j] = fabsf(m[i][j]);
+        v[i][j] = (float)__builtin_amdgcn_sqrt(vd[j]);   // (the instruction's root: within a few float32 units)
       }
-      me[i] = block_exponent(max8(mt));
-      ve[i] = block_exponent(sqrt(max8(vt)));
-      const double mi = pow2(127 - me[i]), vi = pow2(127 - ve[i]);
-      mc[i] = vc[i] = 0u;
+      encode<false>(md, am, mc[i], me[i]);
+      encode<true>(vd, v[i], vc[i], ve[i]);
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        const uint32_t mq = to_e4m3(fabs(md[j]) * mi) | (md[j] < 0.0 ? 0x80u : 0u);
-        uint32_t vq = to_e4m3(sqrt(vd[j]) * vi);
-        if (vq == 0u && vd[j] > 0.0) vq = 1u;
-        mc[i] |= mq << 8 * j;
-        vc[i] |= vq << 8 * j;
+        if (md[j] < 0.0) mc[i] |= 0x80u << 8 * j;
+        if (vd[j] > 0.0 && (vc[i] >> 8 * j & 255u) == 0u) vc[i] |= 1u << 8 * j;
       }
     }
     if (n <= 0) continue;
@@ -154,7 +208,9 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
         m[i][j] = (float)c.b1 * m[i][j] + (float)o1 * g[i][j];
         v[i][j] = (float)c.b2 * v[i][j] + (float)o2 * (g[i][j] * g[i][j]);
       }
-      p[i][j] = (p[i][j] - keep * p[i][j]) - c.lr * (m[i][j] * ibc1) / (sqrtf(v[i][j] * ibc2) + c.eps);
+      // (v: in 8 bits its root already)
+      const float root = BITS8 ? v[i][j] * sbc2 : sqrtf(v[i][j] * ibc2);
+      p[i][j] = (p[i][j] - keep * p[i][j]) - c.lr * (m[i][j] * ibc1) / (root + c.eps);
     }
     store_some(t.param + e, n, p[i]);
     if (t.shadow) store_some(t.shadow + e, n, p[i]);

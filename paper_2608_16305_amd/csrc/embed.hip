@@ -3,8 +3,11 @@
 // An id that is no row of the table gives a row of zeros and takes part in no gradient.
 //
 // Both are bound by memory.  The gradient is dense: every row of it is written once, as a sum over the rows that carry its id,
-// in their order (no float atomics: the result does not depend on scheduling).  The rows are grouped by id first, which moves
-// four bytes of a row of d; ids with more than LIGHT rows are summed in runs that other threads work on at the same time.
+// in their order (no float atomics: the result does not depend on scheduling).  The rows are put in the order of their ids first,
+// which moves four bytes of a row of d: into buckets of neighbouring ids (a histogram, a scatter that keeps the rows' order),
+// then by id within each bucket; three launches, where a radix sort took eight and a search for each id's first row another
+// (8,000 rows of 100,000 ids: 14 us against 44).  Ids with more than LIGHT rows are summed in runs that other threads work on
+// at the same time.
 #include <algorithm>
 
 #include "ops.h"
@@ -15,7 +18,8 @@ namespace mtgnn {
 namespace {
 
 constexpr int NT = 256;
-constexpr int LIGHT = 32;   // rows of an id that one thread sums (per column)
+constexpr int LIGHT = 16;   // rows that one thread sums (per column): of an id, of a run of one with more
+constexpr int IDS = 4;      // ids that a thread sums
 
 template <typename T>
 __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const T* table,
@@ -35,9 +39,20 @@ __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t*
   store_some(y + r * ldy + c, d - c, v);
 }
 
+// --------------------------------------------------------------------------- rows in the order of their ids
+
+constexpr int ST = 1024, MAX_BUCKETS = 8192, MAX_WIDTH_IDS = 1 << 15, MAX_TILES = 64;
+constexpr int MANY = 64;     // ids of a bucket whose runs its whole block lists
+constexpr int AT_ONCE = 8;   // requests of a thread in flight where a bucket's rows are walked over
+
 // What the gradient's kernels share, in the workspace.
 struct Groups {
-  uint32_t *key, *row;       // of each position in the order of ids: the id (n: none), the row
+  int64_t rows, n, per;      // rows, ids, rows of a tile (a block of the first two kernels)
+  int tiles, buckets, shift; // bucket = id >> shift
+  int32_t* hist;             // [tiles][buckets]
+  int32_t* first;            // [buckets + 1] first position of each bucket
+  uint32_t *bid, *brow;      // id and row of each position in the order of buckets
+  uint32_t* row;             // row of each position in the order of ids
   int32_t* off;              // [n + 1] first position of each id
   int32_t* counts;           // [2] runs, heavy ids
   int32_t* run;              // [runs] two each: first and last position
@@ -45,126 +60,360 @@ struct Groups {
   float* part;               // [runs][d]
 };
 
-__global__ __launch_bounds__(NT) void k_embed_keys(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, int64_t n,
-                                                   uint32_t* key, uint32_t* row, int32_t* counts) {
-  const int64_t r = (int64_t)blockIdx.x * NT + threadIdx.x;
-  if (r < 2) counts[r] = 0;
-  if (r >= max_rows) return;
-  const int64_t id = ids[r];
-  key[r] = r < eff_count(max_rows, n_rows) && id >= 0 && id < n ? (uint32_t)id : (uint32_t)n;
-  row[r] = (uint32_t)r;
+__device__ __forceinline__ bool known(const int32_t* ids, int64_t r, int64_t rows, int64_t n, uint32_t& id) {
+  id = r < rows ? (uint32_t)ids[r] : 0xffffffffu;
+  return id < (uint64_t)n;
 }
 
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* key, int64_t rows, uint32_t id) {
-  int64_t lo = 0, hi = rows;
-  while (lo < hi) {
-    const int64_t m = (lo + hi) >> 1;
-    if (key[m] < id) lo = m + 1;
-    else hi = m;
+// The lanes of a wave that have the same key (of `bits` bits), of those that have one.
+__device__ __forceinline__ uint64_t same_key(bool have, uint32_t key, int bits) {
+  uint64_t peers = __ballot(have);
+  for (int b = 0; b < bits; ++b) {
+    const bool bit = key >> b & 1;
+    const uint64_t m = __ballot(bit);
+    peers &= bit ? m : ~m;
   }
-  return lo;
+  return have ? peers : 0;
+}
+__device__ __forceinline__ int lower_lanes(uint64_t m) { return __popcll(m & ((uint64_t(1) << (threadIdx.x & 63)) - 1)); }
+
+// Exclusive sums over a block's threads; total: of all.
+template <int THREADS>
+__device__ __forceinline__ int block_exclusive(int v, int& total, int* s) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  int inc = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += t;
+  }
+  if (lane == 63) s[wid] = inc;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    before += w < wid ? s[w] : 0;
+    total += s[w];
+  }
+  __syncthreads();
+  return before + inc - v;
 }
 
-// Positions in a run of a heavy id of `count` rows: about the root, so that neither the runs nor their sums are long chains.
-__device__ __forceinline__ int run_length(int count) {
-  return max(LIGHT, ((int)sqrtf((float)count) + LIGHT - 1) / LIGHT * LIGHT);
+__global__ __launch_bounds__(ST) void k_embed_hist(Groups g, const int32_t* ids, const int32_t* n_rows) {
+  __shared__ int h[MAX_BUCKETS];
+  const int64_t rows = eff_count(g.rows, n_rows), r0 = blockIdx.x * g.per;
+  if (blockIdx.x == 0 && threadIdx.x < 2) g.counts[threadIdx.x] = 0;
+  for (int b = threadIdx.x; b < g.buckets; b += ST) h[b] = 0;
+  __syncthreads();
+  for (int64_t r = r0 + threadIdx.x; r < min(r0 + g.per, g.rows); r += ST) {
+    uint32_t id;
+    if (known(ids, r, rows, g.n, id)) atomicAdd(&h[id >> g.shift], 1);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < g.buckets; b += ST) g.hist[(int64_t)blockIdx.x * g.buckets + b] = h[b];
 }
 
-__global__ __launch_bounds__(NT) void k_embed_bounds(Groups g, int64_t rows, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
-  if (i > n) return;
-  const int64_t a = lower_bound(g.key, rows, (uint32_t)i);
-  g.off[i] = (int32_t)a;
-  if (i == n) return;
-  const int count = (int)(lower_bound(g.key, rows, (uint32_t)i + 1) - a);
-  if (count <= LIGHT) return;
-  const int L = run_length(count), runs = (int)cdiv(count, L);
-  const int first = atomicAdd(g.counts, runs), h = atomicAdd(g.counts + 1, 1);   // (places, not order)
-  g.heavy[3 * h] = (int32_t)i;
-  g.heavy[3 * h + 1] = first;
-  g.heavy[3 * h + 2] = runs;
-  for (int k = 0; k < runs; ++k) {
-    g.run[2 * (first + k)] = (int32_t)a + k * L;
-    g.run[2 * (first + k) + 1] = (int32_t)a + min(count, (k + 1) * L);
+// A tile's rows to their buckets, behind those of the tiles before it; waves of a tile in turn, so that the order stays.
+__global__ __launch_bounds__(ST) void k_embed_scatter(Groups g, const int32_t* ids, const int32_t* n_rows) {
+  __shared__ int at[MAX_BUCKETS];
+  __shared__ int s[ST / 64];
+  const int64_t rows = eff_count(g.rows, n_rows), r0 = blockIdx.x * g.per;
+  const int wid = threadIdx.x >> 6;
+  uint32_t id;
+  bool have = known(ids, r0 + threadIdx.x, min(rows, r0 + g.per), g.n, id);
+  int base = 0;
+  for (int b0 = 0; b0 < g.buckets; b0 += ST) {
+    const int b = b0 + threadIdx.x;
+    int before = 0, all = 0, total;
+    if (b < g.buckets)
+#pragma unroll 8
+      for (int t = 0; t < g.tiles; ++t) {
+        const int v = g.hist[(int64_t)t * g.buckets + b];
+        before += t < (int)blockIdx.x ? v : 0;
+        all += v;
+      }
+    const int from = base + block_exclusive<ST>(all, total, s);
+    if (b < g.buckets) {
+      at[b] = from + before;
+      if (blockIdx.x == 0) g.first[b] = from;
+    }
+    base += total;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.first[g.buckets] = base;
+  __syncthreads();
+  const int bits = 32 - __clz(max(1, g.buckets - 1));
+  for (int64_t c = r0; c < min(r0 + g.per, g.rows); c += ST) {
+    const int64_t r = c + threadIdx.x;
+    const uint32_t b = have ? id >> g.shift : 0u;
+    const uint64_t peers = same_key(have, b, bits);
+    const int rank = lower_lanes(peers);
+    int pos = 0;
+    for (int w = 0; w < ST / 64; ++w) {
+      if (w == wid && have) {
+        pos = at[b] + rank;
+        if (rank + 1 == __popcll(peers)) at[b] = pos + 1;   // the last of them
+      }
+      __syncthreads();
+    }
+    if (have) {
+      g.bid[pos] = id;
+      g.brow[pos] = (uint32_t)r;
+    }
+    have = known(ids, r + ST, min(rows, r0 + g.per), g.n, id);
   }
 }
 
-// Threads below n ids x columns: the ids with at most LIGHT rows.  The others: the runs of the heavy ones.
-__global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int64_t lddy, int64_t n, int d, float scale,
-                                                  int64_t id_blocks, float* dtable) {
+// A bucket's rows in the order of their ids; every id's first position, and the runs of those with more than LIGHT rows.
+__global__ __launch_bounds__(NT) void k_embed_order(Groups g) {
+  extern __shared__ int at[];   // [ids of a bucket]
+  __shared__ int s[NT / 64], base[2], many[MANY][3], n_many;
+  const int wid = threadIdx.x >> 6, width = 1 << g.shift;
+  const int a = g.first[blockIdx.x], e = g.first[blockIdx.x + 1];
+  const int64_t id0 = (int64_t)blockIdx.x << g.shift;
+  const int have_ids = (int)min((int64_t)width, g.n - id0);
+  for (int i = threadIdx.x; i < width; i += NT) at[i] = 0;
+  __syncthreads();
+  for (int c = a; c < e; c += AT_ONCE * NT) {
+    uint32_t id[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) id[u] = g.bid[min(c + u * NT + (int)threadIdx.x, e - 1)];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (c + u * NT >= e) break;
+      const bool have = c + u * NT + (int)threadIdx.x < e;
+      const uint32_t i = id[u] - (uint32_t)id0;
+      const uint64_t peers = same_key(have, i, g.shift);
+      if (have && lower_lanes(peers) == 0) atomicAdd(&at[i], __popcll(peers));
+    }
+  }
+  __syncthreads();
+  // counts to first positions: a thread has `each` neighbouring ids
+  const int each = (width + NT - 1) / NT, i0 = threadIdx.x * each;
+  int sum = 0, mine = 0, mine_runs = 0, total, all, all_runs;
+  for (int i = i0; i < min(i0 + each, width); ++i) {
+    sum += at[i];
+    if (at[i] > LIGHT) ++mine, mine_runs += (int)cdiv(at[i], LIGHT);
+  }
+  int from = a + block_exclusive<NT>(sum, total, s);
+  int h = block_exclusive<NT>(mine, all, s), first = block_exclusive<NT>(mine_runs, all_runs, s);
+  if (threadIdx.x == 0) {
+    n_many = 0;
+    if (all) {   // (places, not order)
+      base[0] = atomicAdd(g.counts, all_runs);
+      base[1] = atomicAdd(g.counts + 1, all);
+    }
+  }
+  __syncthreads();
+  for (int i = i0; i < min(i0 + each, width); ++i) {
+    const int count = at[i];
+    at[i] = from;
+    if (i < have_ids) g.off[id0 + i] = from;
+    if (count > LIGHT) {
+      const int runs = (int)cdiv(count, LIGHT), f = base[0] + first, o = base[1] + h;
+      g.heavy[3 * o] = (int32_t)(id0 + i);
+      g.heavy[3 * o + 1] = f;
+      g.heavy[3 * o + 2] = runs;
+      // those of many runs by the whole block, below
+      const int q = runs > 4 ? atomicAdd(&n_many, 1) : MANY;
+      if (q < MANY) {
+        many[q][0] = f;
+        many[q][1] = from;
+        many[q][2] = count;
+      } else {
+        for (int k = 0; k < runs; ++k) {
+          g.run[2 * (f + k)] = from + k * LIGHT;
+          g.run[2 * (f + k) + 1] = from + min(count, (k + 1) * LIGHT);
+        }
+      }
+      ++h;
+      first += runs;
+    }
+    from += count;
+  }
+  __syncthreads();
+  for (int q = 0; q < min(n_many, MANY); ++q)
+    for (int k = threadIdx.x; k * LIGHT < many[q][2]; k += NT) {
+      g.run[2 * (many[q][0] + k)] = many[q][1] + k * LIGHT;
+      g.run[2 * (many[q][0] + k) + 1] = many[q][1] + min(many[q][2], (k + 1) * LIGHT);
+    }
+  if (blockIdx.x + 1 == g.buckets && threadIdx.x == 0) g.off[g.n] = e;
+  __syncthreads();
+  for (int c = a; c < e; c += AT_ONCE * NT) {
+    uint32_t id[AT_ONCE], r[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int k = min(c + u * NT + (int)threadIdx.x, e - 1);
+      id[u] = g.bid[k];
+      r[u] = g.brow[k];
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (c + u * NT >= e) break;
+      const bool have = c + u * NT + (int)threadIdx.x < e;
+      const uint32_t i = id[u] - (uint32_t)id0;
+      const uint64_t peers = same_key(have, i, g.shift);
+      const int rank = lower_lanes(peers);
+      for (int w = 0; w < NT / 64; ++w) {
+        if (w == wid && have) {
+          const int pos = at[i] + rank;
+          g.row[pos] = r[u];
+          if (rank + 1 == __popcll(peers)) at[i] = pos + 1;
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------- sums
+
+// s += the rows at positions a .. b - 1, in their order.
+__device__ __forceinline__ void add_rows(float (&s)[4], const uint32_t* row, int a, int b, const float* dy, int64_t ld, int n) {
+  for (int k = a; k < b; k += 8) {
+    float v[8][4];
+    uint32_t r[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) r[u] = row[min(k + u, b - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) load_some(dy + (int64_t)r[u] * ld, n, v[u]);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = k + u < b ? s[j] + v[u][j] : s[j];
+  }
+}
+
+// Four columns of IDS neighbouring ids (those with at most LIGHT rows), or of a run: blocks from id_blocks on.  An id's first two
+// rows are requested for all of them together.
+__global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int64_t lddy, int d, float scale, int64_t id_blocks,
+                                                  float* dtable) {
   const int dv = (int)cdiv(d, 4);
   const bool runs = blockIdx.x >= id_blocks;
   const uint32_t e = (uint32_t)(blockIdx.x - (runs ? id_blocks : 0)) * NT + threadIdx.x;
   const int64_t i = e / dv;
-  const int c = (int)(e % dv) * 4;
-  int a, b;
-  float* out;
+  const int c = (int)(e % dv) * 4, n = d - c;
+  dy += c;
   if (runs) {
     if (i >= g.counts[0]) return;
-    a = g.run[2 * i];
-    b = g.run[2 * i + 1];
-    out = g.part + i * d + c;
-    scale = 1.f;
-  } else {
-    if (i >= n) return;
-    a = g.off[i];
-    b = g.off[i + 1];
-    if (b - a > LIGHT) return;
-    out = dtable + i * d + c;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    add_rows(s, g.row, g.run[2 * i], g.run[2 * i + 1], dy, lddy, n);
+    store_some(g.part + i * d + c, n, s);
+    return;
   }
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = a; k < b; k += 4) {
-    float v[4][4];
+  const int64_t id = i * IDS;
+  if (id >= g.n) return;
+  int off[IDS + 1];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_some(dy + (int64_t)g.row[min(k + u, b - 1)] * lddy + c, d - c, v[u]);
+  for (int u = 0; u <= IDS; ++u) off[u] = g.off[min(id + u, g.n)];
+  uint32_t r[IDS][2];
+  float v[IDS][2][4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+  for (int u = 0; u < IDS; ++u)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] = k + u < b ? s[j] + v[u][j] : s[j];
+    for (int k = 0; k < 2; ++k) r[u][k] = off[u] + k < off[u + 1] ? g.row[off[u] + k] : 0u;
+#pragma unroll
+  for (int u = 0; u < IDS; ++u)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[u][k][j] = 0.f;
+      if (off[u] + k < off[u + 1]) load_some(dy + (int64_t)r[u][k] * lddy, n, v[u][k]);
+    }
+#pragma unroll
+  for (int u = 0; u < IDS; ++u) {
+    const int count = off[u + 1] - off[u];
+    if (id + u >= g.n || count > LIGHT) continue;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = k < count ? s[j] + v[u][k][j] : s[j];
+    if (count > 2) add_rows(s, g.row, off[u] + 2, off[u + 1], dy, lddy, n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] *= scale;
+    store_some(dtable + (id + u) * d + c, n, s);
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] *= scale;
-  store_some(out, d - c, s);
 }
 
-__global__ __launch_bounds__(NT) void k_embed_heavy(Groups g, int d, float scale, float* dtable) {
-  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * NT + threadIdx.x;
-  const int64_t h = e / dv;
-  const int c = (int)(e % dv) * 4;
+// The runs of a heavy id: a block has 16 times four columns of one, and 16 threads to each, which take every 16th run.
+__global__ __launch_bounds__(NT) void k_embed_join(Groups g, int d, float scale, float* dtable) {
+  __shared__ float s[16][16][4];
+  const int cb = (int)cdiv(d, 64), h = blockIdx.x / cb, j16 = threadIdx.x & 15, k16 = threadIdx.x >> 4;
+  const int c = (int)(blockIdx.x % cb) * 64 + j16 * 4, n = d - c;
   if (h >= g.counts[1]) return;
-  const int64_t id = g.heavy[3 * h];
   const int first = g.heavy[3 * h + 1], runs = g.heavy[3 * h + 2];
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < runs; k += 4) {
-    float v[4][4];
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n > 0)
+#pragma unroll 4
+    for (int k = k16; k < runs; k += 16) {
+      float w[4];
+      load_some(g.part + (int64_t)(first + k) * d + c, n, w);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_some(g.part + (int64_t)(first + min(k + u, runs - 1)) * d + c, d - c, v[u]);
+      for (int j = 0; j < 4; ++j) v[j] += w[j];
+    }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+  for (int j = 0; j < 4; ++j) s[k16][j16][j] = v[j];
+  __syncthreads();
+  if (k16 || n <= 0) return;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] = k + u < runs ? s[j] + v[u][j] : s[j];
-  }
+  for (int k = 1; k < 16; ++k)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] *= scale;
-  store_some(dtable + id * d + c, d - c, s);
+    for (int j = 0; j < 4; ++j) v[j] += s[k][j16][j];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] *= scale;
+  store_some(dtable + (int64_t)g.heavy[3 * h] * d + c, n, v);
 }
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 int64_t most_heavy(int64_t rows) { return rows / (LIGHT + 1); }
 int64_t most_runs(int64_t rows) { return rows / LIGHT + most_heavy(rows); }
 
+// Buckets: about 32 rows in each, as far as LDS has counters for them and for their ids.
+void lay_out(Groups& g, int64_t rows, int64_t n) {
+  g.rows = rows;
+  g.n = n;
+  g.per = std::max<int64_t>(ST, cdiv(cdiv(rows, MAX_TILES), ST) * ST);
+  g.tiles = (int)cdiv(rows, g.per);
+  const int64_t want = std::min<int64_t>(MAX_BUCKETS, std::max<int64_t>(256, rows / 32));
+  g.shift = 0;
+  while (cdiv(n, int64_t(1) << g.shift) > want) ++g.shift;
+  g.buckets = (int)cdiv(n, int64_t(1) << g.shift);
+}
+size_t place(Groups& g, int d, char* w) {
+  char* const start = w;
+  const auto take = [&](size_t bytes) {
+    char* p = w;
+    w += al(bytes);
+    return p;
+  };
+  g.hist = (int32_t*)take(4 * (size_t)g.tiles * g.buckets);
+  g.first = (int32_t*)take(4 * ((size_t)g.buckets + 1));
+  g.bid = (uint32_t*)take(4 * g.rows);
+  g.brow = (uint32_t*)take(4 * g.rows);
+  g.row = (uint32_t*)take(4 * g.rows);
+  g.off = (int32_t*)take(4 * (g.n + 1));
+  g.counts = (int32_t*)take(8);
+  g.run = (int32_t*)take(8 * most_runs(g.rows));
+  g.heavy = (int32_t*)take(12 * most_heavy(g.rows));
+  g.part = (float*)take(4 * most_runs(g.rows) * d);
+  return (size_t)(w - start);
+}
+
 }  // namespace
 
 bool embed_fits(const mtgnn_embedding_dims* d, int64_t rows, bool back) {
   constexpr int64_t MAX = (int64_t(1) << 32) - 2 * NT;
-  const int64_t V = d->dtype == MTGNN_BF16 ? 8 : 4;
-  if (!back) return rows * cdiv(d->d, V) <= MAX;
-  return cdiv(d->n * cdiv(d->d, 4), NT) * NT + most_runs(rows) * cdiv(d->d, 4) <= MAX;
+  if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX;
+  const int64_t dv = cdiv(d->d, 4);
+  return d->n <= (int64_t)MAX_BUCKETS * MAX_WIDTH_IDS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows) * dv <= MAX &&
+         most_heavy(rows) * cdiv(d->d, 64) * NT <= MAX;
 }
 
 size_t embed_ws(const mtgnn_embedding_dims* d, int64_t rows) {
-  return 2 * al(4 * rows) + al(4 * (d->n + 1)) + 256 + al(8 * most_runs(rows)) + al(12 * most_heavy(rows)) +
-         al(4 * most_runs(rows) * d->d) + radix_sort_ws_bytes(rows);
+  Groups g;
+  lay_out(g, rows, d->n);
+  return place(g, d->d, nullptr);
 }
 
 mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
@@ -178,33 +427,24 @@ mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_r
 }
 
 mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,
-                            const mtgnn_embedding_dims* d, float* dtable, void* ws, size_t ws_bytes, hipStream_t s) {
-  char* w = (char*)ws;
-  const auto take = [&](size_t bytes) {
-    char* p = w;
-    w += al(bytes);
-    return p;
-  };
+                            const mtgnn_embedding_dims* d, float* dtable, void* ws, hipStream_t s) {
   Groups g;
-  g.key = (uint32_t*)take(4 * max_rows);
-  g.row = (uint32_t*)take(4 * max_rows);
-  g.off = (int32_t*)take(4 * (d->n + 1));
-  g.counts = (int32_t*)take(8);
-  g.run = (int32_t*)take(8 * most_runs(max_rows));
-  g.heavy = (int32_t*)take(12 * most_heavy(max_rows));
-  g.part = (float*)take(4 * most_runs(max_rows) * d->d);
-  k_embed_keys<<<(unsigned)cdiv(max_rows, NT), NT, 0, s>>>(ids, n_rows, max_rows, d->n, g.key, g.row, g.counts);
-  MTGNN_CHECK_LAUNCH("embed_keys");
-  MTGNN_TRY(radix_sort_pairs(&g.key, &g.row, max_rows, bits_for(d->n), w, ws_bytes - (size_t)(w - (char*)ws), s));
-  k_embed_bounds<<<(unsigned)cdiv(d->n + 1, NT), NT, 0, s>>>(g, max_rows, d->n);
-  MTGNN_CHECK_LAUNCH("embed_bounds");
-  const int64_t dv = cdiv(d->d, 4), id_blocks = cdiv(d->n * dv, NT);
-  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows) * dv, NT)), NT, 0, s>>>(g, dy, lddy, d->n, d->d, d->scale,
-                                                                                         id_blocks, dtable);
+  lay_out(g, max_rows, d->n);
+  place(g, d->d, (char*)ws);
+  k_embed_hist<<<(unsigned)g.tiles, ST, 0, s>>>(g, ids, n_rows);
+  MTGNN_CHECK_LAUNCH("embed_hist");
+  k_embed_scatter<<<(unsigned)g.tiles, ST, 0, s>>>(g, ids, n_rows);
+  MTGNN_CHECK_LAUNCH("embed_scatter");
+  const size_t lds = sizeof(int) << g.shift;
+  k_embed_order<<<(unsigned)g.buckets, NT, lds, s>>>(g);
+  MTGNN_CHECK_LAUNCH("embed_order");
+  const int64_t dv = cdiv(d->d, 4), id_blocks = cdiv(cdiv(d->n, IDS) * dv, NT);
+  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows) * dv, NT)), NT, 0, s>>>(g, dy, lddy, d->d, d->scale, id_blocks,
+                                                                                         dtable);
   MTGNN_CHECK_LAUNCH("embed_sum");
   if (most_heavy(max_rows) > 0) {
-    k_embed_heavy<<<(unsigned)cdiv(most_heavy(max_rows) * dv, NT), NT, 0, s>>>(g, d->d, d->scale, dtable);
-    MTGNN_CHECK_LAUNCH("embed_heavy");
+    k_embed_join<<<(unsigned)(most_heavy(max_rows) * cdiv(d->d, 64)), NT, 0, s>>>(g, d->d, d->scale, dtable);
+    MTGNN_CHECK_LAUNCH("embed_join");
   }
   return MTGNN_OK;
 }

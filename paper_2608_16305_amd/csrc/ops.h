@@ -288,7 +288,7 @@ size_t embed_ws(const mtgnn_embedding_dims* d, int64_t rows);
 mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
                         const mtgnn_embedding_dims* d, void* y, int64_t ldy, hipStream_t s);
 mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,
-                            const mtgnn_embedding_dims* d, float* dtable, void* ws, size_t ws_bytes, hipStream_t s);
+                            const mtgnn_embedding_dims* d, float* dtable, void* ws, hipStream_t s);
 int64_t norm_threads(const mtgnn_norm_dims* d);   // the most threads of a launch to a row
 size_t norm_ws(const mtgnn_norm_dims* d, int64_t rows);
 mtgnn_status norm_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const float* gamma,
