@@ -21,22 +21,36 @@ constexpr int NT = 256;
 constexpr int LIGHT = 16;   // rows that one thread sums (per column): of an id, of a run of one with more
 constexpr int IDS = 4;      // ids that a thread sums
 
-template <typename T>
+// U elements of 16 bytes a thread, requested together.
+template <typename T, int U>
 __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const T* table,
                                               int64_t n, int d, float scale, T* y, int64_t ldy) {
   constexpr int V = 16 / sizeof(T);
-  const uint32_t dv = (uint32_t)cdiv(d, V), e = blockIdx.x * NT + threadIdx.x;
-  const int64_t r = e / dv;
-  const int c = (int)(e % dv) * V;
-  if (r >= eff_count(max_rows, n_rows)) return;
-  const int64_t id = ids[r];
-  float v[V];
+  const uint32_t dv = (uint32_t)cdiv(d, V), e0 = blockIdx.x * (U * NT) + threadIdx.x;
+  const int64_t rows = eff_count(max_rows, n_rows);
+  int64_t r[U], id[U];
+  int c[U];
+  float v[U][V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = 0.f;
-  if (id >= 0 && id < n) load_some(table + id * d + c, d - c, v);
+  for (int u = 0; u < U; ++u) {
+    const uint32_t e = e0 + u * NT;
+    r[u] = e / dv;
+    c[u] = (int)(e % dv) * V;
+    id[u] = r[u] < rows ? ids[r[u]] : -1;
+  }
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] *= scale;
-  store_some(y + r * ldy + c, d - c, v);
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[u][i] = 0.f;
+    if (id[u] >= 0 && id[u] < n) load_some(table + id[u] * d + c[u], d - c[u], v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (r[u] >= rows) continue;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[u][i] *= scale;
+    store_some(y + r[u] * ldy + c[u], d - c[u], v[u]);
+  }
 }
 
 // --------------------------------------------------------------------------- rows in the order of their ids
@@ -404,7 +418,7 @@ size_t place(Groups& g, int d, char* w) {
 
 bool embed_fits(const mtgnn_embedding_dims* d, int64_t rows, bool back) {
   constexpr int64_t MAX = (int64_t(1) << 32) - 2 * NT;
-  if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX;
+  if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX - 4 * NT;
   const int64_t dv = cdiv(d->d, 4);
   return d->n <= (int64_t)MAX_BUCKETS * MAX_WIDTH_IDS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows) * dv <= MAX &&
          most_heavy(rows) * cdiv(d->d, 64) * NT <= MAX;
@@ -416,14 +430,23 @@ size_t embed_ws(const mtgnn_embedding_dims* d, int64_t rows) {
   return place(g, d->d, nullptr);
 }
 
-mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
-                        const mtgnn_embedding_dims* d, void* y, int64_t ldy, hipStream_t s) {
-  const bool bf = d->dtype == MTGNN_BF16;
-  const unsigned grid = (unsigned)cdiv(max_rows * cdiv(d->d, bf ? 8 : 4), NT);
-  if (bf) k_embed<<<grid, NT, 0, s>>>(ids, n_rows, max_rows, (const uint16_t*)table, d->n, d->d, d->scale, (uint16_t*)y, ldy);
-  else k_embed<<<grid, NT, 0, s>>>(ids, n_rows, max_rows, (const float*)table, d->n, d->d, d->scale, (float*)y, ldy);
+template <typename T>
+mtgnn_status embed_t(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const T* table, const mtgnn_embedding_dims* d,
+                     T* y, int64_t ldy, hipStream_t s) {
+  const int64_t items = max_rows * cdiv(d->d, 16 / (int)sizeof(T));
+  // four elements a thread where that leaves eight blocks a CU
+  if (items >= int64_t(4) * NT * 2048)
+    k_embed<T, 4><<<(unsigned)cdiv(items, 4 * NT), NT, 0, s>>>(ids, n_rows, max_rows, table, d->n, d->d, d->scale, y, ldy);
+  else
+    k_embed<T, 1><<<(unsigned)cdiv(items, NT), NT, 0, s>>>(ids, n_rows, max_rows, table, d->n, d->d, d->scale, y, ldy);
   MTGNN_CHECK_LAUNCH("embed");
   return MTGNN_OK;
+}
+
+mtgnn_status embed_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const void* table,
+                        const mtgnn_embedding_dims* d, void* y, int64_t ldy, hipStream_t s) {
+  if (d->dtype == MTGNN_BF16) return embed_t(ids, n_rows, max_rows, (const uint16_t*)table, d, (uint16_t*)y, ldy, s);
+  return embed_t(ids, n_rows, max_rows, (const float*)table, d, (float*)y, ldy, s);
 }
 
 mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,

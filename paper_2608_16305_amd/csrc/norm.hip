@@ -9,7 +9,6 @@
 #include <algorithm>
 
 #include "ops.h"
-#include "seq.h"
 #include "words.h"
 
 namespace mtgnn {
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(1024) void k_norm_wide(const T* x, int64_t ldx, con
   }
 }
 
-// A team of G threads takes every `teams`-th row.  part: [teams][2 d], dgamma's columns before dbeta's.
+// A team of G threads takes every `teams`-th row.  part: [blocks][2 d], a block's shares of dgamma before those of dbeta.
 template <typename T, int G, int N>
 __global__ __launch_bounds__(G == 64 ? 256 : G) void k_norm_back(const float* dy, int64_t lddy, const T* x, int64_t ldx,
                                                                  const float2* stats, const int32_t* n_rows,
@@ -137,7 +136,6 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void k_norm_back(const float* dy
   const int64_t rows = eff_count(max_rows, n_rows);
   const int t = threadIdx.x % G;
   const int64_t team = G == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (team >= teams) return;
   float dg[N][V], db[N][V], w[N][V];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -147,7 +145,7 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void k_norm_back(const float* dy
     if (gamma && c < d) load_some(gamma + c, d - c, w[i]);
   }
   int turn = 0;
-  for (int64_t r = team; r < rows; r += teams, turn ^= 1) {
+  for (int64_t r = team < teams ? team : rows; r < rows; r += teams, turn ^= 1) {
     const float2 st = stats[r];
     float h[N][V], g[N][V];
 #pragma unroll
@@ -199,12 +197,64 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void k_norm_back(const float* dy
     }
   }
   if (!part) return;
+  if constexpr (G == 64) {   // the block's four teams
+    __shared__ float4 q[3][2 * N][64];
+    const int wid = threadIdx.x >> 6;
+    if (wid) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        q[wid - 1][i][t] = make_float4(dg[i][0], dg[i][1], dg[i][2], dg[i][3]);
+        q[wid - 1][N + i][t] = make_float4(db[i][0], db[i][1], db[i][2], db[i][3]);
+      }
+    }
+    __syncthreads();
+    if (wid) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float4 a = q[w][i][t], b = q[w][N + i][t];
+        dg[i][0] += a.x; dg[i][1] += a.y; dg[i][2] += a.z; dg[i][3] += a.w;
+        db[i][0] += b.x; db[i][1] += b.y; db[i][2] += b.z; db[i][3] += b.w;
+      }
+  }
+  part += (int64_t)blockIdx.x * 2 * d;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int c = (i * G + t) * V;
     if (c >= d) continue;
-    store_some(part + team * 2 * d + c, d - c, dg[i]);
-    store_some(part + team * 2 * d + d + c, d - c, db[i]);
+    store_some(part + c, d - c, dg[i]);
+    store_some(part + d + c, d - c, db[i]);
+  }
+}
+
+// The blocks' shares: 64 columns a block, four to each of 16 threads, and 32 times 16 threads that take every 32nd share.
+__global__ __launch_bounds__(512) void k_norm_join(const float* part, int shares, int d, float* dgamma, float* dbeta) {
+  __shared__ float s[32][16][4];
+  const int j16 = threadIdx.x & 15, k32 = threadIdx.x >> 4, c = blockIdx.x * 64 + j16 * 4, n = 2 * d - c;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n > 0)
+    for (int k = k32; k < shares; k += 256) {
+      float w[8][4];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) load_some(part + (int64_t)min(k + 32 * u, shares - 1) * 2 * d + c, n, w[u]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = k + 32 * u < shares ? v[j] + w[u][j] : v[j];
+    }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[k32][j16][j] = v[j];
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const int col = blockIdx.x * 64 + threadIdx.x;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 32; ++k) sum += s[k][threadIdx.x >> 2][threadIdx.x & 3];
+  if (col < d) {
+    if (dgamma) dgamma[col] = sum;
+  } else if (col < 2 * d) {
+    if (dbeta) dbeta[col - d] = sum;
   }
 }
 
@@ -284,8 +334,13 @@ mtgnn_status norm_t(const T* x, int64_t ldx, const int32_t* n_rows, int64_t max_
   const int d = dims->d;
   const float eps = dims->eps;
   const unsigned few = (unsigned)cdiv(max_rows, 4), all = (unsigned)max_rows;
+  // A wave to a row, 32 elements a lane at most, where that leaves eight waves a CU; a block to one of few rows, in which less
+  // follows one after the other.
+  const bool many = max_rows >= 2048;
   if (d <= 64 * V) k_norm<T, 64, 1><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 128 * V) k_norm<T, 64, 2><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
+  else if (many && d <= 256 * V) k_norm<T, 64, 4><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
+  else if (many && d <= 2048) k_norm<T, 64, 32 / V><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 256 * V) k_norm<T, 256, 1><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 512 * V) k_norm<T, 256, 2><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 8192) k_norm<T, 256, 32 / V><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
@@ -325,8 +380,9 @@ mtgnn_status norm_bwd_t(const float* dy, int64_t lddy, const T* x, int64_t ldx, 
 #undef MTGNN_BACK
   MTGNN_CHECK_LAUNCH("layer_norm_back");
   if (part) {
-    k_sum_parts<<<(unsigned)cdiv(2 * d, 16), 256, 0, s>>>(Seqs{}, 0, teams, part, 2 * d, d, dgamma, d, dbeta, nullptr);
-    MTGNN_CHECK_LAUNCH("layer_norm_sum_parts");
+    const int shares = d <= 512 ? (int)cdiv(teams, 4) : teams;
+    k_norm_join<<<(unsigned)cdiv(2 * d, 64), 512, 0, s>>>(part, shares, d, dgamma, dbeta);
+    MTGNN_CHECK_LAUNCH("layer_norm_join");
   }
   return MTGNN_OK;
 }

@@ -267,7 +267,13 @@ def _check(status: int, name: str):
                          f"({L.mtgnn_last_error().decode()})")
 
 
+# The current stream's handle without a Stream object around it (2.5 us less a call), where torch offers it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
+    if stream is None and _raw_stream is not None:
+        return C.c_void_p(_raw_stream(torch.cuda.current_device()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
 
@@ -783,31 +789,36 @@ def _rows(t, dtype, name, rows, cols, optional=False, dev=-1):
         raise MtgnnError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise MtgnnError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols:
-        raise MtgnnError(f"{name} must be [{rows}, {cols}], got {tuple(t.shape)}")
-    if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
-        raise MtgnnError(f"{name} must have dense rows, got strides {t.stride()}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
+        raise MtgnnError(f"{name} must be [{rows}, {cols}], got {tuple(shape)}")
+    if (cols > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < cols):
+        raise MtgnnError(f"{name} must have dense rows, got strides {stride}")
     if t.get_device() != dev:
         _elsewhere(t, name, dev)
-    return C.c_void_p(t.data_ptr()), max(int(t.stride(0)), cols)
+    return C.c_void_p(t.data_ptr()), max(stride[0], cols)
 
 
 def _table(t, dtype, name, shape, optional=False, dev=-1):
     """Pointer of a dense tensor of the given shape."""
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is None:
+        return _ptr(t, dtype, name, optional)
+    if t.shape != shape:
         raise MtgnnError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    p = _ptr(t, dtype, name, optional)
-    if t is not None and t.get_device() != dev:
+    p = _ptr(t, dtype, name)
+    if t.get_device() != dev:
         _elsewhere(t, name, dev)
     return p
 
 
 def _count(t, n, name, dev=-1):
     """Pointer of an int32 tensor of n entries or more, or NULL."""
-    if t is not None and t.numel() < n:
+    if t is None:
+        return None
+    if t.numel() < n:
         raise MtgnnError(f"{name} must have {n} entries, got {t.numel()}")
-    p = _ptr(t, torch.int32, name, optional=True)
-    if t is not None and t.get_device() != dev:
+    p = _ptr(t, torch.int32, name)
+    if t.get_device() != dev:
         _elsewhere(t, name, dev)
     return p
 
