@@ -48,20 +48,6 @@ __device__ __forceinline__ bool has_label(const int32_t* label, int64_t r, int64
   return r < rows && (uint32_t)label[r] < (uint32_t)n;
 }
 
-__global__ __launch_bounds__(CHUNK) void k_loss_count(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n,
-                                                      int32_t* counts, uint32_t* largest) {
-  __shared__ int s[CHUNK / 64];
-  if (blockIdx.x == 0 && threadIdx.x < 2) largest[threadIdx.x] = 0u;
-  const int64_t r = (int64_t)blockIdx.x * CHUNK + threadIdx.x;
-  const uint64_t have = __ballot(has_label(label, r, eff_count(max_rows, n_rows), n));
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __popcll(have);
-  __syncthreads();
-  if (threadIdx.x) return;
-  int v = 0;
-  for (int w = 0; w < CHUNK / 64; ++w) v += s[w];
-  counts[blockIdx.x] = v;
-}
-
 __device__ __forceinline__ int block_sum(int v, int* s) {   // over 256 threads
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -79,14 +65,21 @@ __device__ __forceinline__ uint32_t magnitude(float v) {
   const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
   return u < 0x7f800000u ? u : 0u;
 }
-__device__ __forceinline__ void raise(uint32_t v, uint32_t* largest) {   // by all 256 threads of a block
+__device__ __forceinline__ uint32_t block_largest(uint32_t v) {   // over 256 threads
   __shared__ uint32_t s[4];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
   v = max(max(s[0], s[1]), max(s[2], s[3]));
-  if (threadIdx.x == 0 && v) atomicMax(largest, v);   // (a maximum does not depend on the order)
+  __syncthreads();
+  return v;
+}
+// The largest of the shares that blocks have left (`n` of them, at most MAX_SHARES).
+__device__ __forceinline__ uint32_t largest_of(const uint32_t* share, int n) {
+  uint32_t v = 0u;
+  for (int i = threadIdx.x; i < n; i += 256) v = max(v, share[i]);
+  return block_largest(v);
 }
 // The power of two that takes the largest element to 2^14 .. 2^15, as far as float32 has it.
 __device__ __forceinline__ float lift(uint32_t largest) {
@@ -126,37 +119,84 @@ __device__ __forceinline__ uint32_t put_parts(const T* row, int c, int d, float 
   return top;
 }
 
-// The largest elements of x's rows with a label (blocks below x_blocks) and of W.  A block takes every x_blocks-th (the others':
-// every so many) 2,048 elements: a maximum in memory for each would take longer than reading them (126 us against 17, 64 MB).
+// The largest element of the rows (of those with a label, where labels are given) that fall to block b of `blocks`.
+constexpr int MAX_SHARES = 1024;
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_largest(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
-                                                      int64_t max_rows, const T* W, int64_t n, int d, unsigned x_blocks,
-                                                      uint32_t* largest) {
-  const bool table = blockIdx.x >= x_blocks;
-  const int64_t units = cdiv(d, 8), rows = table ? n : eff_count(max_rows, n_rows);
-  const int64_t step = (int64_t)(table ? gridDim.x - x_blocks : x_blocks) * 256;
+__device__ __forceinline__ uint32_t largest_share(const T* M, int64_t ld, int64_t rows, int d, const int32_t* label, int n, unsigned b,
+                                                  unsigned blocks) {
+  const int64_t units = cdiv(d, 8);
   uint32_t top = 0u;
-  for (int64_t e = (int64_t)(blockIdx.x - (table ? x_blocks : 0)) * 256 + threadIdx.x; e < rows * units; e += step) {
+  for (int64_t e = (int64_t)b * 256 + threadIdx.x; e < rows * units; e += (int64_t)blocks * 256) {
     const int64_t r = e / units;
     const int c = (int)(e - r * units) * 8;
-    if (!table && !has_label(label, r, rows, (int)n)) continue;
+    if (label && !has_label(label, r, rows, n)) continue;
     float v[8];
-    load_some(table ? W + r * d + c : x + r * ldx + c, d - c, v);
+    load_some(M + r * ld + c, d - c, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
   }
-  raise(top, largest + table);
+  return block_largest(top);
 }
 
-// The rows with a label, one after the other: idx (which rows), lab, xc (their x, as it is or in parts; zeros behind the last
-// one to a whole step); their number; of bfloat16 x its largest element.  Blocks past those of the rows fill in the zeros.
+// The forward's first launch.  A block each: the labels of CHUNK rows are counted; then, of float32 operands, shares of x's rows
+// with a label and of W in search of the largest elements.
+struct First {
+  const int32_t *label, *n_rows;
+  int64_t max_rows;
+  int n, d;
+  int32_t* counts;             // of each chunk
+  uint32_t *largest, *share;   // [2] cleared; [x_blocks + w_blocks] what they found
+  unsigned chunks, x_blocks, w_blocks;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
-                                                   int64_t max_rows, int n, int d, int dp, const int32_t* counts,
-                                                   int32_t* count, int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane,
-                                                   uint32_t* largest, float* row_loss) {
+__global__ __launch_bounds__(256) void k_loss_first(First f, const T* x, int64_t ldx, const T* W) {
+  __shared__ int s[4];
+  const int64_t rows = eff_count(f.max_rows, f.n_rows);
+  if (blockIdx.x < f.chunks) {
+    if (blockIdx.x == 0 && threadIdx.x < 2) f.largest[threadIdx.x] = 0u;
+    int v = 0;
+#pragma unroll
+    for (int u = 0; u < CHUNK / 256; ++u) v += has_label(f.label, (int64_t)blockIdx.x * CHUNK + u * 256 + threadIdx.x, rows, f.n);
+    v = block_sum(v, s);
+    if (threadIdx.x == 0) f.counts[blockIdx.x] = v;
+    return;
+  }
+  const unsigned b = blockIdx.x - f.chunks;
+  const uint32_t top = b < f.x_blocks ? largest_share(x, ldx, rows, f.d, f.label, f.n, b, f.x_blocks)
+                                      : largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b - f.x_blocks, f.w_blocks);
+  if (threadIdx.x == 0) f.share[b] = top;
+}
+
+// Rows of d as rows of dp: as they are, or in float16 parts.  Block b.
+template <typename T, int PARTS>
+__device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, float by, uint16_t* to, int64_t plane, unsigned b) {
+  const uint32_t units = dp / 8, e = b * 256 + threadIdx.x;
+  const int64_t c = e / units;
+  const int u = (int)(e % units) * 8;
+  if (c < n) put_parts<T, PARTS>(W + c * d, u, d, by, to + c * dp + u, plane);
+}
+
+// The forward's second launch.  Blocks below `blocks`: the rows with a label, one after the other: idx (which rows), lab, xc (their x,
+// as it is or in parts; zeros behind the last one to a whole step); their number; of bfloat16 x its largest element.  The last of
+// them, past those of the rows, fill in the zeros.  The other blocks: W in parts, or padded.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
+                                                  int64_t max_rows, int n, int d, int dp, const int32_t* counts, int32_t* count,
+                                                  int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane, uint32_t* largest,
+                                                  const uint32_t* share, unsigned x_shares, unsigned w_shares, float* row_loss,
+                                                  unsigned blocks, const T* W, uint16_t* table) {
   constexpr int PARTS = sizeof(T) == 2 ? 0 : 2;
   __shared__ int s[4], src[ROWS];
+  if (blockIdx.x >= blocks) {
+    float by = 1.f;
+    if (PARTS) {
+      const uint32_t top = largest_of(share + x_shares, (int)w_shares);
+      if (blockIdx.x == blocks && threadIdx.x == 0) largest[1] = top;
+      by = lift(top);
+    }
+    lay_table<T, PARTS>(W, n, d, dp, by, table, (int64_t)n * dp, blockIdx.x - blocks);
+    return;
+  }
   const int64_t rows = eff_count(max_rows, n_rows), r0 = (int64_t)blockIdx.x * ROWS;
   const int chunks = (int)cdiv(max_rows, CHUNK), units = dp / 8;
   const bool behind = r0 >= max_rows;
@@ -196,23 +236,57 @@ __global__ __launch_bounds__(256) void k_loss_rows(const T* x, int64_t ldx, cons
   }
   __syncthreads();
   here = s[0];
-  const float by = PARTS == 2 ? lift(*largest) : 1.f;
   uint32_t top = 0u;
+  if (PARTS) {
+    top = largest_of(share, (int)x_shares);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = top;
+  }
+  const float by = PARTS ? lift(top) : 1.f;
   for (int e = threadIdx.x; e < here * units; e += 256) {
     const int k = e / units, c = e % units * 8;
     top = max(top, put_parts<T, PARTS>(x + (r0 + src[k]) * ldx, c, d, by, xc + (int64_t)(first + k) * dp + c, plane));
   }
-  if (PARTS == 0) raise(top, largest);
+  if (PARTS == 0) {
+    top = block_largest(top);
+    if (threadIdx.x == 0 && top) atomicMax(largest, top);   // (a maximum does not depend on the order)
+  }
 }
 
-// Rows of d as rows of dp: as they are, or in float16 parts.
-template <typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_loss_table(const T* W, int64_t n, int d, int dp, const uint32_t* largest, uint16_t* to,
-                                                    int64_t plane) {
-  const uint32_t units = dp / 8, e = blockIdx.x * 256 + threadIdx.x;
-  const int64_t c = e / units;
-  const int u = (int)(e % units) * 8;
-  if (c < n) put_parts<T, PARTS>(W + c * d, u, d, PARTS ? lift(*largest) : 1.f, to + c * dp + u, plane);
+// The backward's first launch: dx of the rows without a label (blocks below `blocks`), and of bfloat16 operands the search of W.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W) {
+  if (blockIdx.x >= blocks) {
+    const unsigned b = blockIdx.x - blocks;
+    const uint32_t top = largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b, f.w_blocks);
+    if (threadIdx.x == 0) f.share[b] = top;
+    return;
+  }
+  const uint32_t dv = (uint32_t)cdiv(f.d, 4), e = blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = e / dv;
+  const int c = (int)(e % dv) * 4;
+  if (r >= eff_count(f.max_rows, f.n_rows) || (uint32_t)f.label[r] < (uint32_t)f.n) return;
+  const float z[4] = {0.f, 0.f, 0.f, 0.f};
+  store_some(dx + r * lddx + c, f.d - c, z);
+}
+
+// Its second: W in float16 parts (blocks below `blocks`), and of bfloat16 operands x's rows.
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_back_lay(const T* W, int64_t n, int d, int dp, uint32_t* largest, const uint32_t* share,
+                                                       unsigned shares, uint16_t* table, unsigned blocks, const uint16_t* xc,
+                                                       int64_t Rp, const uint32_t* largest_x, uint16_t* xh) {
+  constexpr int PARTS = sizeof(T) == 2 ? 1 : 2;
+  if (blockIdx.x >= blocks) {
+    lay_table<uint16_t, 1>(xc, Rp, dp, dp, lift(*largest_x), xh, 0, blockIdx.x - blocks);
+    return;
+  }
+  uint32_t top;
+  if (PARTS == 1) {
+    top = largest_of(share, (int)shares);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = top;
+  } else {
+    top = *largest;
+  }
+  lay_table<T, PARTS>(W, n, d, dp, lift(top), table, n * dp, blockIdx.x);
 }
 
 // --------------------------------------------------------------------------- the products
@@ -334,10 +408,11 @@ __device__ __forceinline__ f32x4 mma(bf16x8_t a, bf16x8_t b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// T x T tiles, a wave has 16 WR x 64 of one.
-template <int T>
+// TR x TC tiles, a wave has 16 WR x 64 of one: all of its rows where they are 64, else half of them.
+template <int TR, int TC>
 struct Shape {
-  static constexpr int WR = T / 32, WC = 4, WCOLS = T / 64, NW = 2 * WCOLS, LINES = T;
+  static constexpr int WCOLS = TC / 64, WROWS = TR == 64 ? 1 : 2, NW = WROWS * WCOLS;
+  static constexpr int WR = TR / 16 / WROWS, WC = 4, LINES = TR, COLUMNS = TC;
 };
 
 // Joins (largest, sum of exponentials relative to it).
@@ -432,7 +507,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
     float2 q = s[t];
 #pragma unroll
     for (int w = 1; w < S::WCOLS; ++w) join(q, s[w * S::LINES + t]);
-    p.part[c0 / S::LINES * p.ld_part + r0 + t] = q;
+    p.part[c0 / S::COLUMNS * p.ld_part + r0 + t] = q;
   }
   if constexpr (KIND == PROB) {
     float sum[WC][4];
@@ -530,13 +605,13 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
   }
 }
 
-template <int KIND, bool HALF, int T>
-__global__ __launch_bounds__(T == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
-  using S = Shape<T>;
+template <int KIND, bool HALF, int TR, int TC>
+__global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
+  using S = Shape<TR, TC>;
   constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
   constexpr int WR = S::WR, WC = S::WC;
-  using LA = Lines<AK, T, S::NW>;
-  using LB = Lines<BK, T, S::NW>;
+  using LA = Lines<AK, TR, S::NW>;
+  using LB = Lines<BK, TC, S::NW>;
   constexpr int WORDS = LA::WORDS + LB::WORDS, LOADS = LA::LOADS + LB::LOADS;
   __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS], buf2[WORDS], buf3[WORDS];
   int64_t tr, tc;
@@ -544,7 +619,7 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, 2) void k_loss_product(Prod p
   my_tile(p, tr, tc, share);
   const int64_t count = *p.count, rows = KIND == DW ? p.rows : min(p.rows, count);
   const int64_t K = KIND == DW ? up(count, PAD) : p.K;
-  const int64_t r0 = tr * T, c0 = tc * T;
+  const int64_t r0 = tr * TR, c0 = tc * TC;
   if (r0 >= rows) return;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
@@ -638,7 +713,7 @@ __global__ __launch_bounds__(T == 256 ? 512 : 256, 2) void k_loss_product(Prod p
 
   // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.  Most tiles have all of their columns, and
   // no test of each.
-  if (c0 + T <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
+  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
   else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
@@ -669,7 +744,9 @@ __global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const
 
 // --------------------------------------------------------------------------- rows' sums
 
-// 16 rows a block, 16 threads to each: joins the tiles' (largest, sum) and leaves the row's, its loss, and the block's sum.
+// 16 rows a block, 16 threads to each: joins the tiles' (largest, sum) and leaves the row's, its loss, and the block's sum.  (A mean by
+// the last block to be done in the same launch needs a fence of each, which took longer than the launch: 18 us for 9 + 5,
+// 7,373 rows.)
 __global__ __launch_bounds__(256) void k_loss_join(const int32_t* count, const int32_t* idx, const float2* part, int tiles,
                                                    int64_t ld_part, const float* at_label, float2* stat, float* row_loss,
                                                    double* sums) {
@@ -685,7 +762,13 @@ __global__ __launch_bounds__(256) void k_loss_join(const int32_t* count, const i
     q.x = m;
   };
   if (r < n)
-    for (int t = k; t < tiles; t += 16) add(part[t * ld_part + r]);
+    for (int t = k; t < tiles; t += 128) {   // (those past the last one: nothing)
+      float2 o[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) o[u] = t + 16 * u < tiles ? part[(t + 16 * u) * ld_part + r] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) add(o[u]);
+    }
   s[k][threadIdx.x & 15] = q;
   __syncthreads();
   if (k == 0) {
@@ -740,19 +823,6 @@ __global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const flo
   db[c] = v * (loss_scale(n, dloss) / LIFT);
 }
 
-// dx of the rows without a label; clears *largest.
-__global__ __launch_bounds__(256) void k_loss_zero(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n, int d,
-                                                   float* dx, int64_t lddx, uint32_t* largest) {
-  if (blockIdx.x == 0 && threadIdx.x == 0 && largest) *largest = 0u;
-  if (!dx) return;
-  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
-  const int64_t r = e / dv;
-  const int c = (int)(e % dv) * 4;
-  if (r >= eff_count(max_rows, n_rows) || (uint32_t)label[r] < (uint32_t)n) return;
-  const float z[4] = {0.f, 0.f, 0.f, 0.f};
-  store_some(dx + r * lddx + c, d - c, z);
-}
-
 // --------------------------------------------------------------------------- memory
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
@@ -799,24 +869,26 @@ Kept kept(void* at, const Plan& p) {
   return k;
 }
 
-// A product's tiles, T wide and high, and the blocks that share a tile's sum.
+// A product's tiles, and the blocks that share a tile's sum.
 struct Tiling {
-  int T, split;
-  int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, T) * cdiv(cols, T); }
+  int tr, tc, split;
+  int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
 };
-// Of the logits: large tiles where there are enough of them for the card.
+// Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 27 us, 3.8 TB/s, in tiles of 256 x 256 48), else large ones where there are enough
+// of them for the card.
 Tiling tiling(int64_t rows, int64_t cols) {
-  const Tiling big{256, 1};
-  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 1};
+  if (rows <= 64) return Tiling{64, 256, 1};
+  const Tiling big{256, 256, 1};
+  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 128, 1};
 }
 // Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
 // enough to fill the card with shares of them; then as many shares as leave the fewest places of the last round of
 // blocks empty.
 Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
-  Tiling g{256, 1};
-  const Tiling small{128, 1};
+  Tiling g{256, 256, 1};
+  const Tiling small{128, 128, 1};
   if (g.tiles(rows, cols) * 4 * 100 > small.tiles(rows, cols) * 115 || g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192) g = small;
-  const int64_t t = g.tiles(rows, cols), slots = g.T == 256 ? 256 : 512;
+  const int64_t t = g.tiles(rows, cols), slots = g.tr == 256 ? 256 : 512;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, steps / 16));
   double best = 0.0;
   for (int64_t s = 1; s <= most; ++s) {
@@ -840,15 +912,16 @@ Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t 
 
 template <int KIND, bool HALF>
 mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
-  p.tr = cdiv(p.rows, t.T);
-  p.tc = cdiv(p.cols, t.T);
+  p.tr = cdiv(p.rows, t.tr);
+  p.tc = cdiv(p.cols, t.tc);
   p.split = t.split;
   const unsigned grid = (unsigned)(p.tr * p.tc * p.split);
   {
     TimedScope ts(site::Generic::name, s),
         kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
-    if (t.T == 256) k_loss_product<KIND, HALF, 256><<<grid, 512, 0, s>>>(p);
-    else k_loss_product<KIND, HALF, 128><<<grid, 256, 0, s>>>(p);
+    if (t.tr == 256) k_loss_product<KIND, HALF, 256, 256><<<grid, 512, 0, s>>>(p);
+    else if (t.tr == 128) k_loss_product<KIND, HALF, 128, 128><<<grid, 256, 0, s>>>(p);
+    else if constexpr (KIND == STAT || KIND == PROB) k_loss_product<KIND, HALF, 64, 256><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
@@ -874,21 +947,8 @@ void segments(Prod& p, int a, int b) {
   else if (a == 2) p.codeA = 1;
 }
 
-template <typename T, int PARTS>
-mtgnn_status table(const void* W, int64_t n, int d, int dp, const uint32_t* largest, uint16_t* to, hipStream_t s) {
-  k_loss_table<T, PARTS><<<(unsigned)cdiv(n * (dp / 8), 256), 256, 0, s>>>((const T*)W, n, d, dp, largest, to, n * dp);
-  MTGNN_CHECK_LAUNCH("loss_table");
-  return MTGNN_OK;
-}
-template <typename T>
-mtgnn_status largest(const void* x, int64_t ldx, const int32_t* label, const int32_t* n_rows, int64_t rows, const void* W,
-                     const mtgnn_loss_dims* d, uint32_t* to, hipStream_t s) {
-  const auto blocks = [&](int64_t r) { return (unsigned)std::min<int64_t>(1024, cdiv(r * cdiv(d->d, 8), 256)); };
-  const unsigned xb = x ? blocks(rows) : 0;
-  k_loss_largest<T><<<xb + blocks(d->n), 256, 0, s>>>((const T*)x, ldx, label, n_rows, rows, (const T*)W, d->n, d->d, xb, to);
-  MTGNN_CHECK_LAUNCH("loss_largest");
-  return MTGNN_OK;
-}
+unsigned table_blocks(int64_t n, const Plan& p) { return (unsigned)cdiv(n * (p.dp / 8), 256); }
+unsigned search_blocks(int64_t rows, int d) { return (unsigned)std::min<int64_t>(MAX_SHARES, cdiv(rows * cdiv(d, 8), 256)); }
 
 }  // namespace
 
@@ -906,11 +966,11 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const Plan p = plan(d, rows);
   const size_t t = al(2 * (size_t)d->n * p.dp);   // a part of W
   if (!back)
-    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) +
-           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).T) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
+           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).tc) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
-  return 256 + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
+  return 256 + al(4 * MAX_SHARES) + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
          al(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width)) + al(part);
 }
 
@@ -928,21 +988,23 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   };
   uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)d->n * p.dp : 0) : 4 * (size_t)d->n * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
-  const int tiles = (int)cdiv(d->n, tl.T);
+  const int tiles = (int)cdiv(d->n, tl.tc);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, 16));
-  k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), CHUNK, 0, s>>>(label, n_rows, max_rows, d->n, counts, k.largest);
-  MTGNN_CHECK_LAUNCH("loss_count");
-  if (!p.bf) MTGNN_TRY(largest<float>(x, ldx, label, n_rows, max_rows, W, d, k.largest, s));
-  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS);
-  if (p.bf)
-    k_loss_rows<<<blocks, 256, 0, s>>>((const uint16_t*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
-                                       k.lab, k.xc, p.Rp * p.dp, k.largest, row_loss);
-  else
-    k_loss_rows<<<blocks, 256, 0, s>>>((const float*)x, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx,
-                                       k.lab, k.xc, p.Rp * p.dp, k.largest, row_loss);
-  MTGNN_CHECK_LAUNCH("loss_rows");
+  uint32_t* share = (uint32_t*)take(8 * MAX_SHARES);
+  First f{label, n_rows, max_rows, d->n, d->d, counts, k.largest, share, (unsigned)cdiv(max_rows, CHUNK), 0, 0};
+  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS), tb = p.bf && !p.copy ? 0 : table_blocks(d->n, p);
+  const auto lay = [&](auto* xt, auto* Wt) -> mtgnn_status {
+    if (!p.bf) f.x_blocks = search_blocks(max_rows, d->d), f.w_blocks = search_blocks(d->n, d->d);
+    k_loss_first<<<f.chunks + f.x_blocks + f.w_blocks, 256, 0, s>>>(f, xt, ldx, Wt);
+    MTGNN_CHECK_LAUNCH("loss_first");
+    k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx, k.lab, k.xc,
+                                           p.Rp * p.dp, k.largest, share, f.x_blocks, f.w_blocks, row_loss, blocks, Wt, tbl);
+    MTGNN_CHECK_LAUNCH("loss_lay");
+    return MTGNN_OK;
+  };
+  MTGNN_TRY(p.bf ? lay((const uint16_t*)x, (const uint16_t*)W) : lay((const float*)x, (const float*)W));
   Prod q{};
   q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
   q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = d->n * (int64_t)p.dp;
@@ -950,15 +1012,10 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   q.rows = max_rows; q.cols = d->n; q.K = up(d->d, KS); q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
   if (p.bf) {
-    if (p.copy) {
-      MTGNN_TRY((table<uint16_t, 0>(W, d->n, d->d, p.dp, nullptr, tbl, s)));
-    } else {
-      q.B = (const uint16_t*)W; q.ldb = q.dimB = d->d;
-    }
+    if (!p.copy) q.B = (const uint16_t*)W, q.ldb = q.dimB = d->d;
     segments(q, 1, 1);
     MTGNN_TRY((product<STAT, false>(q, tl, s)));
   } else {
-    MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, k.largest + 1, tbl, s)));
     segments(q, 2, 2);
     MTGNN_TRY((product<STAT, true>(q, tl, s)));
   }
@@ -981,23 +1038,26 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     return at;
   };
   uint32_t* top = (uint32_t*)take(4);
+  uint32_t* share = (uint32_t*)take(4 * MAX_SHARES);
   const int64_t plane = d->n * (int64_t)p.dp, planeX = p.Rp * p.dp;
   uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
   uint16_t* xh = p.bf ? (uint16_t*)take(2 * (size_t)planeX) : k.xc;
   uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * stride(p.width));
   float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width));
   float* part = (float*)w;
-  k_loss_zero<<<(unsigned)(dx ? cdiv(max_rows * cdiv(d->d, 4), 256) : 1), 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx,
-                                                                                       p.bf ? top : nullptr);
-  MTGNN_CHECK_LAUNCH("loss_zero");
-  if (p.bf) {
-    MTGNN_TRY((largest<uint16_t>(nullptr, 0, nullptr, nullptr, 0, W, d, top - 1, s)));
-    MTGNN_TRY((table<uint16_t, 1>(W, d->n, d->d, p.dp, top, tbl, s)));
-    MTGNN_TRY((table<uint16_t, 1>(k.xc, p.Rp, p.dp, p.dp, k.largest, xh, s)));
-  } else {
-    top = k.largest + 1;
-    MTGNN_TRY((table<float, 2>(W, d->n, d->d, p.dp, top, tbl, s)));
-  }
+  // (the sizes a float32 W was searched for are the forward's)
+  if (!p.bf) top = k.largest + 1;
+  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, 0, p.bf ? search_blocks(d->n, d->d) : 0};
+  const unsigned zb = dx ? (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256) : 0, tb = table_blocks(d->n, p);
+  const auto lay = [&](auto* Wt) -> mtgnn_status {
+    if (zb + f.w_blocks > 0) k_loss_back_first<<<zb + f.w_blocks, 256, 0, s>>>(f, dx, lddx, zb, Wt);
+    MTGNN_CHECK_LAUNCH("loss_back_first");
+    k_loss_back_lay<<<tb + (p.bf ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(Wt, d->n, d->d, p.dp, top, share, f.w_blocks, tbl, tb, k.xc,
+                                                                            p.Rp, k.largest, xh);
+    MTGNN_CHECK_LAUNCH("loss_back_lay");
+    return MTGNN_OK;
+  };
+  MTGNN_TRY(p.bf ? lay((const uint16_t*)W) : lay((const float*)W));
   for (int64_t c = 0; c < d->n; c += p.width) {
     const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = stride(cols);
     const Shares sh = shares_of(d, p, max_rows, cols);
@@ -1019,7 +1079,7 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
       MTGNN_TRY((product<PROB, true>(q, tl, s)));
     }
     if (db) {
-      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.T / 2, cols, dloss, db + c);
+      k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.tr == 64 ? 64 : tl.tr / 2, cols, dloss, db + c);
       MTGNN_CHECK_LAUNCH("loss_db");
     }
     Prod g{};
