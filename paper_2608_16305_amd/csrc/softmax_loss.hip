@@ -33,7 +33,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 
-constexpr int KS = 32;          // a step of the sums
+constexpr int KS = 64;          // a step of the sums: 128 bytes of a line
 constexpr int PAD = 64;         // rows and columns are padded to whole ones
 constexpr float LIFT = 16384.f; // what P is multiplied by
 constexpr int CHUNK = 1024;     // rows whose labels are counted together
@@ -173,7 +173,7 @@ __device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, 
   const uint32_t units = dp / 8, e = b * 256 + threadIdx.x;
   const int64_t c = e / units;
   const int u = (int)(e % units) * 8;
-  if (c < n) put_parts<T, PARTS>(W + c * d, u, d, by, to + c * dp + u, plane);
+  if (c < up(n, PAD)) put_parts<T, PARTS>(W + c * d, u, c < n ? d : 0, by, to + c * dp + u, plane);   // (zeros behind the last)
 }
 
 // The forward's second launch.  Blocks below `blocks`: the rows with a label, one after the other: idx (which rows), lab, xc (their x,
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
       if (blockIdx.x == blocks && threadIdx.x == 0) largest[1] = top;
       by = lift(top);
     }
-    lay_table<T, PARTS>(W, n, d, dp, by, table, (int64_t)n * dp, blockIdx.x - blocks);
+    lay_table<T, PARTS>(W, n, d, dp, by, table, up(n, PAD) * dp, blockIdx.x - blocks);
     return;
   }
   const int64_t rows = eff_count(max_rows, n_rows), r0 = (int64_t)blockIdx.x * ROWS;
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(256) void k_loss_back_lay(const T* W, int64_t n, in
   } else {
     top = *largest;
   }
-  lay_table<T, PARTS>(W, n, d, dp, lift(top), table, n * dp, blockIdx.x);
+  lay_table<T, PARTS>(W, n, d, dp, lift(top), table, up(n, PAD) * dp, blockIdx.x);
 }
 
 // --------------------------------------------------------------------------- the products
@@ -305,7 +305,7 @@ struct Prod {
   int segs, split;               // split: blocks that share a tile's sum, each leaving its own in `out`
   const uint32_t *topA, *topB;   // largest elements of operands in float16 parts, or NULL
   int64_t rows, cols, K;         // the most rows; K: of a segment (its last step has a k that may be read)
-  int64_t dimA, dimB;            // elements of an operand's line that may be read (A's along the sum are whole steps)
+  int64_t dimA, dimB;            // elements of an operand's line that may be read (along the sum whole steps, but of a W in place)
   int64_t tr, tc;                // tiles
   const int32_t* count;          // rows with a label: bounds the rows (STAT, PROB, DX) or K (DW)
   // epilogue
@@ -325,7 +325,7 @@ struct Prod {
   int add;
 };
 
-// Lines go straight to LDS, 16 bytes a lane.  Along the sum: a line's four units are swizzled by the line, as in
+// Lines go straight to LDS, 16 bytes a lane.  Along the sum: a line's eight units are swizzled by the line, as in
 // linear.hip.  Across it: a k's 32-byte units by k, and the transposing read of 4 k x 16 columns gives a lane its four k;
 // the 16 lanes of such a read, and their neighbours, meet every bank once.
 // An operand's T lines of a step, loaded by NW waves; its lines are contiguous along the sum (ALONG) or across it.
@@ -339,7 +339,7 @@ struct Lines {
 
   // The k of a step of a lane's load i.
   __device__ __forceinline__ static int k_of(int wid, int lane, int i) {
-    return ALONG ? 8 * ((lane & 3) ^ (lane >> 3 & 3)) : (LOADS * wid + i) * (64 / UNITS) + lane / UNITS;
+    return ALONG ? 8 * ((lane & 7) ^ (lane >> 3)) : (LOADS * wid + i) * (64 / UNITS) + lane / UNITS;
   }
   // This wave's loads: bytes from the tile's first line at a step's first k.  (Below 2^32: 256 lines of 2^22 elements, or 32 of
   // them.)
@@ -348,7 +348,7 @@ struct Lines {
     for (int i = 0; i < LOADS; ++i) {
       const int k = k_of(wid, lane, i);
       if constexpr (ALONG) {
-        const int row = 16 * (LOADS * wid + i) + (lane >> 2);
+        const int row = 8 * (LOADS * wid + i) + (lane >> 3);
         off[i] = 2u * ((uint32_t)min((int64_t)row, lines - 1) * (uint32_t)ld + k);
       } else {
         const int q = lane % UNITS, col = ((q >> 1 ^ ((k & 3) | (k >> 3 & 1) << 2)) * 2 + (q & 1)) * 8;
@@ -356,31 +356,28 @@ struct Lines {
       }
     }
   }
-  // The loads of a step that starts at `p`.  `left`: how many of its k may be read; the lanes past them read the step's first
-  // (it meets zeros of the other operand).
+  // Load i of a step that starts at `p`.  `left`: how many of its k may be read; the lanes past them read the step's first (it meets
+  // zeros of the other operand).
   template <bool END>
-  __device__ __forceinline__ static void fill(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[LOADS], int64_t ld, int64_t left,
-                                              int wid, int lane) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      uint32_t o = off[i];
-      if (END && left < KS) {
-        const int k = k_of(wid, lane, i);
-        if (k >= left) o -= 2u * (uint32_t)k * (ALONG ? 1u : (uint32_t)ld);
-      }
-      __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (LOADS * wid + i) * 256), 16, 0, 0);
+  __device__ __forceinline__ static void load(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[LOADS], int64_t ld, int64_t left,
+                                              int wid, int lane, int i) {
+    uint32_t o = off[i];
+    if (END && left < KS) {
+      const int k = k_of(wid, lane, i);
+      if (k >= left) o -= 2u * (uint32_t)k * (ALONG ? 1u : (uint32_t)ld);
     }
+    __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (LOADS * wid + i) * 256), 16, 0, 0);
   }
-  // A lane's byte for the lines from l0 (a multiple of 64) on, and what is read there of the 16 lines from l0 + 16 l.
+  // A lane's byte for the lines from l0 (a multiple of 64) on, and what is read there of the 16 lines from l0 + 16 l, half kk.
   __device__ __forceinline__ static uint32_t place(int l0, int fr, int fg) {
-    if (ALONG) return (l0 + fr) * (2 * KS) + (fg ^ (fr >> 1 & 3)) * 16;
+    if (ALONG) return (l0 + fr) * (2 * KS) + (fg ^ (fr & 7)) * 16;
     return ((8 * fg + (fr >> 2)) * (2 * T) + ((fr >> 2) | (fg & 1) << 2) * 32 + (fr & 3) * 8) ^ 2 * l0;
   }
-  __device__ __forceinline__ static bf16x8_t frag(uint32_t* buf, uint32_t at, int l) {
+  __device__ __forceinline__ static bf16x8_t frag(uint32_t* buf, uint32_t at, int l, int kk) {
     if constexpr (ALONG) {
-      return __builtin_bit_cast(bf16x8_t, *(const uint4*)((char*)buf + (at + l * 16 * 2 * KS)));
+      return __builtin_bit_cast(bf16x8_t, *(const uint4*)((char*)buf + ((at ^ 64 * kk) + l * 16 * 2 * KS)));
     } else {
-      char* a = (char*)buf + (at ^ 32 * l);
+      char* a = (char*)buf + ((at ^ 32 * l) + kk * 32 * 2 * T);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)a);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(a + 4 * 2 * T));
       return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -426,7 +423,6 @@ __device__ __forceinline__ void join(float2& q, float2 o) {
 template <int KIND, class S>
 struct Ahead {
   int at[S::WR];         // the label's place in the lane's columns
-  float2 st[S::WR];      // the row's largest logit, 1 / sum
   float b[S::WC][4];
   __device__ __forceinline__ void load(const Prod& p, int64_t ra, int64_t ca, int64_t rows) {
     if constexpr (KIND == STAT || KIND == PROB) {
@@ -434,7 +430,6 @@ struct Ahead {
       for (int i = 0; i < S::WR; ++i) {
         const int64_t r = min(ra + 16 * i, rows - 1);
         at[i] = p.lab[r];
-        if (KIND == PROB) st[i] = p.stat[r];
       }
 #pragma unroll
       for (int j = 0; j < S::WC; ++j) {
@@ -454,21 +449,23 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
   const int64_t ca = c0 + wc + 4 * fg, ra = r0 + wr + fr;
   const float downA = HALF && KIND != DX ? 1.f / lift(*p.topA) : 1.f, downB = HALF && KIND != DW ? 1.f / lift(*p.topB) : 1.f;
   auto &at = h.at;
-  auto &st = h.st;
+  float2 st[WR];         // the row's largest logit, 1 / sum
   if constexpr (KIND == STAT || KIND == PROB) {
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
       const bool live = ra + 16 * i < rows;
       at[i] = live ? (int)(at[i] - p.c0 - ca) : -1;
-      if (KIND == PROB && !live) st[i] = make_float2(INFINITY, 0.f);   // behind the last row: exponentials of -inf
+      if (KIND == PROB) st[i] = live ? p.stat[ra + 16 * i] : make_float2(INFINITY, 0.f);   // behind the last row: exponentials of -inf
     }
+    // (powers of two: the product is exact, and the sum rounded as it was)
+    const float down = fminf(downA * downB, 3e38f);
 #pragma unroll
     for (int j = 0; j < WC; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < WR; ++i) {
-          acc[i][j][e] = (HALF ? acc[i][j][e] * downA * downB : acc[i][j][e]) + h.b[j][e];
+          acc[i][j][e] = HALF ? fmaf(acc[i][j][e], down, h.b[j][e]) : acc[i][j][e] + h.b[j][e];
           if (!FULL && ca + 16 * j + e >= p.cols) acc[i][j][e] = -INFINITY;
         }
   }
@@ -613,7 +610,7 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   using LA = Lines<AK, TR, S::NW>;
   using LB = Lines<BK, TC, S::NW>;
   constexpr int WORDS = LA::WORDS + LB::WORDS, LOADS = LA::LOADS + LB::LOADS;
-  __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS], buf2[WORDS], buf3[WORDS];
+  __shared__ __align__(1024) uint32_t buf0[WORDS], buf1[WORDS];
   int64_t tr, tc;
   int share;
   my_tile(p, tr, tc, share);
@@ -638,75 +635,78 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   const int steps = max(0, min(each, all - share * each));
   int seg = steps > 0 ? share * each / per : 0, k = share * each - seg * per;   // of the next step to load
   int at = 0;
-  const auto fill = [&](uint32_t* buf) {
+  const auto load = [&](uint32_t* buf, int u) __attribute__((always_inline)) {
     const int64_t k0 = (int64_t)k * KS;
-    LA::template fill<false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane);
-    LB::template fill<KIND != DW>(buf + LA::WORDS, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
-                                  (BK ? p.dimB : p.K) - k0, wid, lane);
+    if (u < LA::LOADS)
+      LA::template load<false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane, u);
+    else
+      LB::template load<BK && !HALF>(buf + LA::WORDS, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
+                                      p.dimB - k0, wid, lane, u - LA::LOADS);
+    if (u + 1 < LOADS) return;
     const int go = ++at < steps, turn = k + 1 == per;   // (the last step's again past it)
     seg += go & turn;
     k = go ? (turn ? 0 : k + 1) : k;
   };
   uint32_t atA = LA::place(wr, fr, fg), atB = LB::place(wc, fr, fg);
-  // This wave's loads have arrived but for the last N steps', then everybody's.
-  const auto ready = [](auto n) {
+  // This wave's loads have arrived and its reads are done, then everybody's.
+  const auto ready = [] {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | LOADS * decltype(n)::value);   // vmcnt(..)
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  // A step is WR groups of WC matrix instructions, a line of A by all of the wave's B; a line is read LOOK groups before it is
-  // used.  LOOK groups before the end the next step has arrived, and its operands are read; every wave is through with the
-  // step before this one, whose buffer is filled with the step three behind it.  What is behind the barrier for a wave to
-  // do at once are matrix instructions.  (Past the last step loads and reads go on, without a branch, and what they bring is not
-  // used.)  The buffers are objects of their own, so that the compiler knows that reads of one do not wait for the loads into the others.
-  constexpr int LOOK = WR / 2;
+  // A step is 2 WR groups of WC matrix instructions, a line of A by all of the wave's B; a line is read LOOK groups before it is
+  // used, the B of a half step in the half step before.  WR / 2 groups before the end, and a group after the step's last reads, every
+  // wave has read the whole step and the next one has arrived: the next one's operands are read, and the buffer is filled with the
+  // step after it.  What is behind the barrier for a wave to do at once are matrix instructions.  (Past the last step loads and
+  // reads go on, without a branch, and what they bring is not used.)  The buffers are two objects, so that the compiler knows that
+  // reads of one do not wait for the loads into the other.
+  constexpr int GROUPS = 2 * WR, READY = GROUPS - WR / 2, LOOK = WR / 2 + 1;
   bf16x8_t a[WR], b[2][WC];
-  const auto work = [&](uint32_t* prev, uint32_t* buf, uint32_t* next, auto turn) __attribute__((always_inline)) {
-    constexpr int now = decltype(turn)::value;
+  const auto work = [&](uint32_t* buf, uint32_t* next) __attribute__((always_inline)) {
     // (places formed again each time: kept for every line, they would not leave the sums their registers)
     asm volatile("" : "+v"(atA), "+v"(atB));
 #pragma unroll
-    for (int m = 0; m < WR; ++m) {
-      if (m == WR - LOOK) ready(std::integral_constant<int, 1>());
+    for (int m = 0; m < GROUPS; ++m) {
+      if (m == READY) ready();
 #pragma unroll
-      for (int j = 0; j < WC; ++j) acc[m][j] = mma<HALF>(b[now][j], a[m], acc[m][j]);
+      for (int j = 0; j < WC; ++j) acc[m % WR][j] = mma<HALF>(b[m / WR][j], a[m % WR], acc[m % WR][j]);
       __builtin_amdgcn_sched_barrier(0);
-      if (m == WR - LOOK) fill(prev);
-      const int q = m + LOOK;
-      a[q % WR] = LA::frag(q < WR ? buf : next, atA, q % WR);
-      if (q >= WR) {
+      if (m >= READY) {
+        constexpr int PER = LOADS / (WR / 2);
 #pragma unroll
-        for (int j = (q - WR) * WC / LOOK; j < (q - WR + 1) * WC / LOOK; ++j)
-          b[1 - now][j] = LB::frag(next + LA::WORDS, atB, j);
+        for (int u = 0; u < PER; ++u) load(buf, (m - READY) * PER + u);
+      }
+      const int q = m + LOOK;   // line of this step, or (from READY on, two of them at first) of the next
+      if (q < GROUPS) a[q % WR] = LA::frag(buf, atA, q % WR, q / WR);
+      if (m == READY) a[0] = LA::frag(next, atA, 0, 0);
+      if (m >= READY) a[m - READY + 1] = LA::frag(next, atA, m - READY + 1, 0);
+      const int half = m < WR / 2 ? 1 : 0, first = half ? m : m - READY;
+      if (half || m >= READY) {
+#pragma unroll
+        for (int j = first * 2 * WC / WR; j < (first + 1) * 2 * WC / WR; ++j) b[half][j] = LB::frag((half ? buf : next) + LA::WORDS, atB, j, half);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  static_assert(LOADS % (WR / 2) == 0 && 2 * WC % WR == 0, "loads and reads of B of a group");
   if (steps > 0) {
-    // Four steps at a time (one way out of the loop, so that the sums stay where they are): zeros stand before the first ones.
-    const int zeros = -steps & 3;
-    for (int i = threadIdx.x; i < WORDS; i += 64 * S::NW) {
-      if (zeros > 0) buf0[i] = 0u;
-      if (zeros > 1) buf1[i] = 0u;
-      if (zeros > 2) buf2[i] = 0u;
-    }
-    if (zeros < 1) fill(buf0);
-    if (zeros < 2) fill(buf1);
-    if (zeros < 3) fill(buf2);
-    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-    ready(std::integral_constant<int, 2>());
+    // Two steps at a time (one way out of the loop, so that the sums stay where they are): an odd number has zeros before the first.
+    const bool zeros = steps & 1;
+    for (int i = threadIdx.x; zeros && i < WORDS; i += 64 * S::NW) buf0[i] = 0u;
+    if (!zeros)
 #pragma unroll
-    for (int i = 0; i < LOOK; ++i) a[i] = LA::frag(buf0, atA, i);
+      for (int u = 0; u < LOADS; ++u) load(buf0, u);
+    ready();
 #pragma unroll
-    for (int j = 0; j < WC; ++j) b[0][j] = LB::frag(buf0 + LA::WORDS, atB, j);
-    constexpr std::integral_constant<int, 0> even;
-    constexpr std::integral_constant<int, 1> odd;
-    for (int step = 0; step < steps; step += 4) {
-      work(buf3, buf0, buf1, even);
-      work(buf0, buf1, buf2, odd);
-      work(buf1, buf2, buf3, even);
-      work(buf2, buf3, buf0, odd);
+    for (int u = 0; u < LOADS; ++u) load(buf1, u);
+#pragma unroll
+    for (int i = 0; i < LOOK; ++i) a[i] = LA::frag(buf0, atA, i, 0);
+#pragma unroll
+    for (int j = 0; j < WC; ++j) b[0][j] = LB::frag(buf0 + LA::WORDS, atB, j, 0);
+    for (int step = 0; step < steps; step += 2) {
+      work(buf0, buf1);
+      work(buf1, buf0);
     }
   }
   __syncthreads();   // (waits for the loads and reads that nothing used)
@@ -947,7 +947,7 @@ void segments(Prod& p, int a, int b) {
   else if (a == 2) p.codeA = 1;
 }
 
-unsigned table_blocks(int64_t n, const Plan& p) { return (unsigned)cdiv(n * (p.dp / 8), 256); }
+unsigned table_blocks(int64_t n, const Plan& p) { return (unsigned)cdiv(up(n, PAD) * (p.dp / 8), 256); }
 unsigned search_blocks(int64_t rows, int d) { return (unsigned)std::min<int64_t>(MAX_SHARES, cdiv(rows * cdiv(d, 8), 256)); }
 
 }  // namespace
@@ -964,7 +964,7 @@ size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(pla
 
 size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const Plan p = plan(d, rows);
-  const size_t t = al(2 * (size_t)d->n * p.dp);   // a part of W
+  const size_t t = al(2 * (size_t)up(d->n, PAD) * p.dp);   // a part of W
   if (!back)
     return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
            al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).tc) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
@@ -986,7 +986,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     w += al(bytes);
     return at;
   };
-  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)d->n * p.dp : 0) : 4 * (size_t)d->n * p.dp);
+  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)up(d->n, PAD) * p.dp : 0) : 4 * (size_t)up(d->n, PAD) * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
   const int tiles = (int)cdiv(d->n, tl.tc);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
@@ -1007,7 +1007,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   MTGNN_TRY(p.bf ? lay((const uint16_t*)x, (const uint16_t*)W) : lay((const float*)x, (const float*)W));
   Prod q{};
   q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
-  q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = d->n * (int64_t)p.dp;
+  q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = up(d->n, PAD) * p.dp;
   q.topA = k.largest; q.topB = k.largest + 1;
   q.rows = max_rows; q.cols = d->n; q.K = up(d->d, KS); q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
@@ -1039,7 +1039,7 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
   };
   uint32_t* top = (uint32_t*)take(4);
   uint32_t* share = (uint32_t*)take(4 * MAX_SHARES);
-  const int64_t plane = d->n * (int64_t)p.dp, planeX = p.Rp * p.dp;
+  const int64_t plane = up(d->n, PAD) * p.dp, planeX = p.Rp * p.dp;
   uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
   uint16_t* xh = p.bf ? (uint16_t*)take(2 * (size_t)planeX) : k.xc;
   uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * stride(p.width));
