@@ -20,7 +20,7 @@ namespace mtgnn {
 
 namespace {
 
-constexpr int NT = 256, PER = 4, TILE = NT * PER * 4;   // elements of a block: four vectors of four a thread
+constexpr int NT = 256, PER = 4;   // threads; elements of a vector
 constexpr int TENSORS = 40;
 
 struct Set {
@@ -125,8 +125,15 @@ __device__ __forceinline__ void encode(const double (&x)[PER], const float (&f)[
   }
 }
 
+// Vectors of a thread, all requested before the first is used.  Few, and many waves instead, which hide the arithmetic of one by
+// the loads of others: 537 us with one, 587 with two and 728 with four in 8 bits (151M elements, 5.1 TB/s); 394, 404 and 416 with
+// two, four and eight in 32 (69M, 5.2 TB/s).
+template <bool BITS8>
+constexpr int VECTORS = BITS8 ? 1 : 2;
+
 template <bool BITS8>
 __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
+  constexpr int N = VECTORS<BITS8>, TILE = NT * PER * N;
   int lo = 0, hi = a.count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -143,11 +150,11 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
   }
   const float keep = c.lr * t.decay, sbc2 = sqrtf(ibc2);
   const double o1 = 1.0 - c.b1, o2 = 1.0 - c.b2;
-  float p[4][PER], g[4][PER], m[4][PER], v[4][PER];
-  uint32_t mc[4], vc[4];
-  int me[4], ve[4];
+  float p[N][PER], g[N][PER], m[N][PER], v[N][PER];
+  uint32_t mc[N], vc[N];
+  int me[N], ve[N];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int64_t e = e0 + i * NT * PER;
     const int n = (int)min((int64_t)PER, t.n - e);
     mc[i] = vc[i] = 0u;
@@ -173,7 +180,7 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int64_t e = e0 + i * NT * PER;
     const int n = (int)min((int64_t)PER, t.n - e);
     if constexpr (BITS8) {
@@ -263,7 +270,7 @@ mtgnn_status adamw_impl(const mtgnn_adamw_tensor* tensors, int64_t n, const mtgn
     };
     for (int64_t i = 0; i < n; ++i) {
       if (tensors[i].n == 0 || (tensors[i].m_exp != nullptr) != (kind == 1)) continue;
-      const int64_t need = cdiv(tensors[i].n, TILE);
+      const int64_t need = cdiv(tensors[i].n, NT * PER * (kind ? VECTORS<true> : VECTORS<false>));
       if (a.count == TENSORS || blocks + need > (int64_t(1) << 24) - 1) MTGNN_TRY(launch());
       a.t[a.count] = tensors[i];
       a.first[a.count++] = (uint32_t)blocks;
