@@ -710,7 +710,7 @@ mtgnn_status mtgnn_embedding(const int32_t* ids, const int32_t* n_rows, int64_t 
                              const mtgnn_embedding_dims* dims, void* y, int64_t ldy, hipStream_t stream);
 
 /* Gradient of the table for dy [max_rows, d] float32:  dtable_i = scale sum of dy_r over the rows with ids[r] = i, in a
- * fixed order; dtable [n, d] is overwritten (zeros for the ids that no row has) and may not overlap dy.
+ * fixed order; dtable [n, d] is overwritten (zeros for the ids that no row has) and may not overlap dy.  n <= 2^26.
  * Workspace: mtgnn_embedding_ws_bytes(dims, max_rows). */
 size_t mtgnn_embedding_ws_bytes(const mtgnn_embedding_dims* dims, int64_t max_rows);
 mtgnn_status mtgnn_embedding_bwd(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const float* dy, int64_t lddy,
@@ -841,7 +841,7 @@ mtgnn_status mtgnn_adam_step(float* const* params, const float* const* grads, fl
 /* One AdamW step (decoupled weight decay, bias-corrected) over n tensors, any number, in place:
  *   m = beta1 m + (1 - beta1) grad,  v = beta2 v + (1 - beta2) grad^2,
  *   param = param (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
- * A tensor (n elements, dense, at any float's address; no two share memory; n = 0: skipped):
+ * A tensor (n <= 2^33 elements, dense, at any float's address; no two share memory; n = 0: skipped):
  *   param, grad -- float32;  shadow -- bfloat16 copy of the updated parameter, or NULL;  decay -- its weight decay;
  *   m_exp, v_exp NULL: m, v are float32;
  *   m_exp, v_exp given: the states take 8 bits.  m holds codes of m, v codes of sqrt(v), in e4m3 (4 bits of exponent, bias 7;

@@ -199,7 +199,8 @@ mtgnn_status mtgnn_adamw_step(const mtgnn_adamw_tensor* tensors, int64_t n, cons
   if (n > 0) REQ(tensors, "tensors");
   for (int64_t i = 0; i < n; ++i) {
     const mtgnn_adamw_tensor& t = tensors[i];
-    if (t.n < 0 || t.n >= int64_t(1) << 36) return fail(MTGNN_EINVAL, "a tensor's n");
+    if (t.n < 0) return fail(MTGNN_EINVAL, "a tensor's n");
+    if (t.n > int64_t(1) << 33) return fail(MTGNN_EUNSUPPORTED, "a tensor's n > 2^33");
     if (!std::isfinite(t.decay)) return fail(MTGNN_EINVAL, "a tensor's decay is not finite");
     if ((t.m_exp == nullptr) != (t.v_exp == nullptr)) return fail(MTGNN_EINVAL, "one of m_exp and v_exp is NULL");
     if (t.n == 0) continue;

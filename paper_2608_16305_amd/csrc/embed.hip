@@ -55,7 +55,7 @@ __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t*
 
 // --------------------------------------------------------------------------- rows in the order of their ids
 
-constexpr int ST = 1024, MAX_BUCKETS = 8192, MAX_WIDTH_IDS = 1 << 15, MAX_TILES = 64;
+constexpr int ST = 1024, MAX_BUCKETS = 8192, MAX_WIDTH_IDS = 8192, MAX_TILES = 64;
 constexpr int MANY = 64;     // ids of a bucket whose runs its whole block lists
 constexpr int AT_ONCE = 8;   // requests of a thread in flight where a bucket's rows are walked over
 
@@ -389,7 +389,7 @@ void lay_out(Groups& g, int64_t rows, int64_t n) {
   g.n = n;
   g.per = std::max<int64_t>(ST, cdiv(cdiv(rows, MAX_TILES), ST) * ST);
   g.tiles = (int)cdiv(rows, g.per);
-  const int64_t want = std::min<int64_t>(MAX_BUCKETS, std::max<int64_t>(256, rows / 32));
+  const int64_t want = std::min<int64_t>(MAX_BUCKETS, std::max({int64_t(256), rows / 32, cdiv(n, MAX_WIDTH_IDS)}));
   g.shift = 0;
   while (cdiv(n, int64_t(1) << g.shift) > want) ++g.shift;
   g.buckets = (int)cdiv(n, int64_t(1) << g.shift);

@@ -324,7 +324,7 @@ int back_teams(const mtgnn_norm_dims* d, int64_t rows) { return (int)std::min<in
 
 }  // namespace
 
-int64_t norm_threads(const mtgnn_norm_dims* d) { return d->d <= 8192 ? 256 : 1024; }
+int64_t norm_threads(const mtgnn_norm_dims* d) { return d->d <= 2048 ? 64 : d->d <= 8192 ? 256 : 1024; }   // (of many rows)
 size_t norm_ws(const mtgnn_norm_dims* d, int64_t rows) { return (size_t)back_teams(d, rows) * 2 * d->d * 4; }
 
 template <typename T>

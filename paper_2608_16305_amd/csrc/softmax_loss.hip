@@ -953,11 +953,11 @@ unsigned search_blocks(int64_t rows, int d) { return (unsigned)std::min<int64_t>
 }  // namespace
 
 bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
-  constexpr int64_t MAX = (int64_t(1) << 32) - 1024;
-  const auto tiles = [](int64_t r, int64_t c) { return cdiv(r, 128) * cdiv(c, 128) * 256 + 512 * 512; };   // (shares only of few)
-  const int64_t units = stride(d->d) / 4;
-  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && (d->n + rows) * units < MAX &&
-         rows * 16 < MAX;
+  constexpr int64_t MAX = (int64_t(1) << 32) - (int64_t(1) << 20);
+  const auto tiles = [](int64_t r, int64_t c) { return cdiv(r, 128) * cdiv(c, 128) * 256; };   // (shares only of few)
+  const int64_t units = stride(d->d) / 8, W = (d->n + PAD) * units, x = (rows + PAD) * units;   // threads that lay out a matrix
+  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && W + x < MAX && W + rows * 16 < MAX &&
+         std::max<int64_t>(rows, d->n) * cdiv(d->d, 4) < MAX;
 }
 
 size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows)); }

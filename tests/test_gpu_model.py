@@ -508,3 +508,221 @@ def test_adamw_step_count_on_the_device():
     M.mtgnn_adamw_step(M.adamw_tensors(*made[1]), 1e-2, 0.9, 0.999, 1e-8, 41)
     assert torch.allclose(made[0][0][0], made[1][0][0], rtol=4 * U, atol=1e-9)
     assert torch.equal(made[0][2][0], made[1][2][0])
+
+
+# --------------------------------------------------------------------------- together
+
+class Model:
+    """ids -> embedding -> norm -> linear with silu and residual -> norm -> loss over all n, as a program keeps it."""
+
+    def __init__(self, rows, n, d, seed=0):
+        rs = np.random.RandomState(seed)
+        self.rows, self.n, self.d = rows, n, d
+        self.ids, self.label = rs.randint(0, n, rows).astype(np.int32), rs.randint(-1, n, rows).astype(np.int32)
+        self.ids[3] = -1
+        host = dict(table=rs.randn(n, d) * 0.3, g1=1 + 0.1 * rs.randn(d), b1=0.1 * rs.randn(d), W=rs.randn(d, d) / np.sqrt(d),
+                    b=0.1 * rs.randn(d), g2=1 + 0.1 * rs.randn(d), b2=0.1 * rs.randn(d), out=rs.randn(n, d) / np.sqrt(d),
+                    bias=0.1 * rs.randn(n))
+        self.host = {k: v.astype(np.float32) for k, v in host.items()}
+        self.p = {k: _dev(v) for k, v in self.host.items()}
+        z = lambda *s: torch.zeros(*s, device="cuda")   # noqa: E731
+        self.g = {k: torch.zeros_like(v) for k, v in self.p.items()}
+        self.ids_d, self.label_d = torch.from_numpy(self.ids).cuda(), torch.from_numpy(self.label).cuda()
+        self.e, self.nd, self.ld = M.embedding_dims(n, d, scale=2.0), M.norm_dims(d), M.linear_dims(d, d, act=M.ACT_SILU)
+        self.od = M.loss_dims(n, d)
+        r = rows
+        self.x0, self.h1, self.x1, self.h2, self.pre = (z(r, d) for _ in range(5))
+        self.s1, self.s2, self.loss, self.row_loss = z(r, 2), z(r, 2), z(1), z(r)
+        self.da, self.db, self.dc = z(r, d), z(r, d), z(r, d)
+        need = max(M.embedding_ws_bytes(self.e, r), M.layer_norm_ws_bytes(self.nd, r), M.linear_ws_bytes(self.ld, r, True),
+                   M.softmax_loss_ws_bytes(self.od, r, True))
+        self.ws, self.save = M.alloc_bytes(need), M.alloc_bytes(M.softmax_loss_save_bytes(self.od, r))
+        names = list(self.p)
+        self.m, self.v = ({k: torch.zeros_like(self.p[k]) for k in names} for _ in range(2))
+        self.tensors = M.adamw_tensors(*([x[k] for k in names] for x in (self.p, self.g, self.m, self.v)),
+                                       decay=[0.01 if self.p[k].dim() > 1 else 0.0 for k in names])
+        self.step = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def gradients(self):
+        p, g, ws = self.p, self.g, self.ws
+        M.mtgnn_embedding(self.ids_d, p["table"], self.e, self.x0)
+        M.mtgnn_layer_norm(self.x0, p["g1"], p["b1"], self.nd, self.h1, stats=self.s1)
+        M.mtgnn_linear(self.h1, p["W"], p["b"], self.x0, self.ld, self.x1, pre=self.pre, ws=ws)
+        M.mtgnn_layer_norm(self.x1, p["g2"], p["b2"], self.nd, self.h2, stats=self.s2)
+        M.mtgnn_softmax_loss(self.h2, p["out"], p["bias"], self.label_d, self.od, self.loss, ws, row_loss=self.row_loss, save=self.save)
+        M.mtgnn_softmax_loss_bwd(self.h2, p["out"], p["bias"], self.label_d, self.od, self.save, self.da, g["out"], g["bias"], ws)
+        M.mtgnn_layer_norm_bwd(self.da, self.x1, p["g2"], self.s2, self.nd, self.db, g["g2"], g["b2"], ws=ws)
+        M.mtgnn_linear_bwd(self.db, self.pre, self.h1, p["W"], self.ld, self.dc, g["W"], g["b"], ws=ws)
+        # x0 reaches the loss through the norm and through the residual
+        M.mtgnn_layer_norm_bwd(self.dc, self.x0, p["g1"], self.s1, self.nd, self.da, g["g1"], g["b1"], past=self.db, ws=ws)
+        M.mtgnn_embedding_bwd(self.ids_d, self.da, self.e, g["table"], ws)
+
+    def train(self):
+        self.gradients()
+        self.step.add_(1)
+        M.mtgnn_adamw_step(self.tensors, 1e-2, 0.9, 0.99, 1e-8, 0, step=self.step)
+
+    def reference(self):
+        """Loss and gradients in 64 bits by torch's differentiation on the CPU."""
+        p = {k: torch.from_numpy(v).double().requires_grad_() for k, v in self.host.items()}
+        ids = torch.from_numpy(self.ids).long()
+        x0 = 2.0 * p["table"][ids.clamp(min=0)] * (ids >= 0)[:, None]
+        norm = lambda x, g, b: (x - x.mean(1, keepdim=True)) / torch.sqrt(x.var(1, correction=0, keepdim=True) + float(np.float32(1e-5))) * g + b   # noqa: E731
+        x1 = torch.nn.functional.silu(norm(x0, p["g1"], p["b1"]) @ p["W"].T + p["b"]) + x0
+        logits = norm(x1, p["g2"], p["b2"]) @ p["out"].T + p["bias"]
+        loss = torch.nn.functional.cross_entropy(logits, torch.from_numpy(self.label).long(), ignore_index=-1)
+        loss.backward()
+        return loss.item(), {k: v.grad.numpy() for k, v in p.items()}
+
+
+@pytest.mark.parametrize("rows,n,d", [(50, 70, 24), (300, 411, 64)])
+def test_a_model_of_them(rows, n, d):
+    """The gradients of the whole against 64 bits.  Each of seven stages adds a relative error of its sums, at most max(d, n, rows) u
+    of terms that are up to about 8 times the sum in norm (they cancel like random ones): 56 max(d, n, rows) u of the norm."""
+    m = Model(rows, n, d)
+    m.gradients()
+    loss, want = m.reference()
+    rel = 56 * max(rows, n, d) * U
+    assert abs(float(m.loss) - loss) <= rel * loss
+    for k, g in want.items():
+        off = np.linalg.norm(_np(m.g[k]) - g) / np.linalg.norm(g)
+        assert off <= rel, (k, off, rel)
+    assert (m.g["table"][[i for i in range(n) if i not in m.ids]] == 0).all()
+
+
+def test_training_steps_in_a_graph():
+    """A captured step, replayed between eager work and synchronizations, is the eager step bit for bit, its step count too."""
+    a, b = Model(200, 300, 40), Model(200, 300, 40)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.gradients()             # (warms up; changes no parameter)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.train()
+    losses = []
+    for k in range(4):
+        a.train()
+        graph.replay()
+        torch.cuda.synchronize()
+        torch.randn(1000, device="cuda").sum()
+        assert torch.equal(a.loss, b.loss), k
+        for name in a.p:
+            assert torch.equal(a.g[name], b.g[name]) and torch.equal(a.p[name], b.p[name]), (k, name)
+        losses.append(float(a.loss))
+    assert int(a.step) == int(b.step) == 4 and len(set(losses)) == 4
+
+
+def test_two_streams_at_once():
+    """Two models on two streams, each with a workspace of its own, give what one after the other gives."""
+    want, got = [Model(257, 500, 33, s) for s in (1, 2)], [Model(257, 500, 33, s) for s in (1, 2)]
+    for m in want:
+        m.gradients()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in got]
+    for _ in range(3):
+        for m, s in zip(got, streams):
+            with torch.cuda.stream(s):
+                m.gradients()
+    torch.cuda.synchronize()
+    for x, y in zip(want, got):
+        assert torch.equal(x.loss, y.loss)
+        for k in x.g:
+            assert torch.equal(x.g[k], y.g[k]), k
+
+
+# --------------------------------------------------------------------------- far offsets and limits
+
+def test_rows_past_32_bits():
+    """Elements behind the 2^31st of a table, a gradient, a norm's rows and an optimizer's tensor."""
+    n, d = 2_200_000, 1024
+    table = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    table[-1], table[0] = 3.0, 1.0
+    ids = torch.tensor([n - 1, 0, n - 1], dtype=torch.int32, device="cuda")
+    e, y = M.embedding_dims(n, d, M.BF16), torch.empty(3, d, dtype=torch.bfloat16, device="cuda")
+    M.mtgnn_embedding(ids, table, e, y)
+    assert (y[0] == 3).all() and (y[1] == 1).all()
+    del table
+    dtable = torch.full((n, d), MARK, device="cuda")
+    dy = torch.ones(3, d, device="cuda")
+    M.mtgnn_embedding_bwd(ids, dy, e, dtable, M.alloc_bytes(M.embedding_ws_bytes(e, 3)))
+    assert (dtable[-1] == 2).all() and (dtable[0] == 1).all() and (dtable[1:-1] == 0).all()
+    m, v = torch.zeros_like(dtable), torch.zeros_like(dtable)
+    p = torch.ones_like(dtable)
+    M.mtgnn_adamw_step(M.adamw_tensors([p], [dtable], [m], [v]), 0.5, 0.5, 0.5, 0.0, 1)
+    assert (m[-1] == 1).all() and (v[-1] == 2).all() and (p[-1] == 0.5).all() and torch.isnan(p[-2]).all()   # (0 / 0: eps is 0)
+    del dtable, m, v, p
+    wide = torch.zeros(2100, 1 << 20, device="cuda")   # rows 2^20 elements apart
+    x, y = wide[:, :64], wide[:, 64:128]
+    x.copy_(torch.arange(64, device="cuda"))
+    M.mtgnn_layer_norm(x, None, None, M.norm_dims(64), y)
+    assert torch.equal(y[0], y[-1]) and y[-1].std() > 0.9
+
+
+def test_embedding_of_the_most_ids():
+    n = 1 << 26
+    ids = torch.tensor([n - 1, 5, n - 1, n, 8192], dtype=torch.int32, device="cuda")
+    e, dtable = M.embedding_dims(n, 1, scale=2.0), torch.full((n, 1), MARK, device="cuda")
+    M.mtgnn_embedding_bwd(ids, torch.ones(5, 1, device="cuda"), e, dtable, M.alloc_bytes(M.embedding_ws_bytes(e, 5)))
+    assert dtable[n - 1] == 4 and dtable[5] == 2 and dtable[8192] == 2 and int((dtable != 0).sum()) == 3
+
+
+def _check_loss_large(rows, n, d, bf16, scale):
+    """Against torch's float64 products on the GPU, with the tolerances of _loss_tolerances."""
+    rs = np.random.RandomState(rows + n)
+    x, W, b = _vals(rs, bf16, rows, d), _vals(rs, bf16, n, d) * np.float32(scale), _vals(rs, False, n)
+    label = rs.randint(0, n, rows).astype(np.int32)
+    label[rs.rand(rows) < 0.02] = -1
+    e, L = M.loss_dims(n, d, M.BF16 if bf16 else M.F32), torch.from_numpy(label).cuda()
+    X, Wd, bd = _dev(x, bf16), _dev(W, bf16), _dev(b)
+    ws, save = M.alloc_bytes(M.softmax_loss_ws_bytes(e, rows, True)).fill_(255), M.alloc_bytes(M.softmax_loss_save_bytes(e, rows)).fill_(255)
+    loss, per_row, dx, dW, db = _marked(1, 1)[0], _marked(rows, 1)[:, 0], _marked(rows, d), _marked(n, d), _marked(1, n)[0]
+    M.mtgnn_softmax_loss(X, Wd, bd, L, e, loss, ws, row_loss=per_row, save=save)
+    M.mtgnn_softmax_loss_bwd(X, Wd, bd, L, e, save, dx, dW, db, ws)
+    live = torch.nonzero(L >= 0)[:, 0]
+    at, R = L[live].long(), int(live.numel())
+    xd, Wq = X.double()[live], Wd.double()
+    ax, aW = xd.abs(), Wq.abs()
+    floor = 2.0 ** -39
+    logits = xd @ Wq.t().contiguous() + bd.double()
+    e_l = (d + (4 if bf16 else 12)) * U * (ax @ aW.t().contiguous() + bd.double().abs())
+    if not bf16:
+        e_l += floor * (ax.max() * aW.sum(1) + aW.max() * ax.sum(1)[:, None])
+    lse = torch.logsumexp(logits, 1)
+    rows_want = lse - logits[torch.arange(R, device="cuda"), at]
+    worst, chain = e_l.max(1).values, (64 + n / 2048) * U
+    tol = 2 * worst + chain + 4 * U * (logits.abs().max(1).values + 1)
+    assert bool(((per_row[live].double() - rows_want).abs() <= tol + U * rows_want).all())
+    assert abs(float(loss) - float(rows_want.mean())) <= float(tol.mean()) + 4 * U * float(rows_want.mean())
+    P = torch.exp(logits - lse[:, None])
+    e_p = P * (torch.exp(2 * worst)[:, None] * (2 * worst[:, None] + chain + (8 + 4 * (logits.max(1, keepdim=True).values - logits)) * U))
+    del logits, e_l
+    P[torch.arange(R, device="cuda"), at] -= 1
+    aP = P.abs()
+    e_p += 4 * U * aP + floor
+    t = lambda m: m.t().contiguous()   # noqa: E731
+    full = torch.zeros(rows, d, dtype=torch.float64, device="cuda")
+    full[live] = P @ Wq
+    room = torch.zeros_like(full)
+    room[live] = e_p @ aW + (n + 20) * U * (aP @ aW) + floor * aW.max() * aP.sum(1)[:, None]
+    for name, got, want, tol in (("dx", dx, full, room),
+                                 ("dW", dW, t(P) @ xd, t(e_p) @ ax + (R + 20) * U * (t(aP) @ ax) + floor * ax.max() * aP.sum(0)[:, None]),
+                                 ("db", db, P.sum(0), e_p.sum(0) + (R + 12) * U * aP.sum(0))):
+        off = (got.double() - want / R).abs()
+        assert bool((off <= tol / R + 4 * U * want.abs() / R).all()), (name, float((off / tol * R).max()))
+
+
+@BOTH
+def test_softmax_loss_in_pieces(bf16):
+    """More rows and classes than one piece of P holds: 66,000 rows of 3,840 classes at a time, the last piece not a whole one."""
+    e = M.loss_dims(4_500, 8, M.BF16 if bf16 else M.F32)
+    assert M.softmax_loss_ws_bytes(e, 66_000, True) < 4 * 66_000 * 4_600   # (P of all classes would take more)
+    _check_loss_large(66_000, 4_500, 8, bf16, 0.5)
+
+
+@BOTH
+@pytest.mark.parametrize("rows,n,d", [(2100, 16500, 1000), (2304, 16384, 1024)])
+def test_softmax_loss_large_tiles(rows, n, d, bf16):
+    """The gradients' products in tiles of 256, their sums shared by blocks; ragged and whole."""
+    _check_loss_large(rows, n, d, bf16, 2 / np.sqrt(d))
