@@ -4,10 +4,9 @@
 //
 // Both are bound by memory.  The gradient is dense: every row of it is written once, as a sum over the rows that carry its id,
 // in their order (no float atomics: the result does not depend on scheduling).  The rows are put in the order of their ids first,
-// which moves four bytes of a row of d: into buckets of neighbouring ids (a histogram, a scatter that keeps the rows' order),
-// then by id within each bucket; three launches, where a radix sort took eight and a search for each id's first row another
-// (8,000 rows of 100,000 ids: 14 us against 44).  Ids with more than LIGHT rows are summed in runs that other threads work on
-// at the same time.
+// which moves eight bytes of a row of d: one or two passes, each a histogram of tiles and a scatter that keeps the rows' order
+// within a digit of up to 13 bits, so two launches a pass where a sort by 8-bit digits takes three, and no rule by which many rows
+// of one id would fall to one block.  Ids with more than LIGHT rows are summed in runs that other threads work on at the same time.
 #include <algorithm>
 
 #include "ops.h"
@@ -55,28 +54,35 @@ __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t*
 
 // --------------------------------------------------------------------------- rows in the order of their ids
 
-constexpr int ST = 1024, MAX_BUCKETS = 8192, MAX_WIDTH_IDS = 8192, MAX_TILES = 64;
-constexpr int MANY = 64;     // ids of a bucket whose runs its whole block lists
-constexpr int AT_ONCE = 8;   // requests of a thread in flight where a bucket's rows are walked over
+constexpr int ST = 1024, MAX_DIGITS = 8192, MAX_TILES = 64;
+constexpr int MANY = 64;     // ids of a block whose runs all of its threads list
 
 // What the gradient's kernels share, in the workspace.
 struct Groups {
-  int64_t rows, n, per;      // rows, ids, rows of a tile (a block of the first two kernels)
-  int tiles, buckets, shift; // bucket = id >> shift
-  int32_t* hist;             // [tiles][buckets]
-  int32_t* first;            // [buckets + 1] first position of each bucket
-  uint32_t *bid, *brow;      // id and row of each position in the order of buckets
-  uint32_t* row;             // row of each position in the order of ids
+  int64_t rows, n, per;      // rows, ids, rows of a tile (a block of the passes)
+  int tiles, low;            // low: bits of an id that the first of two passes sorts by (0: one pass)
+  int32_t* hist;             // [tiles][digits]
+  int32_t *first, *firsts;   // [digits + 1] first position of each digit of the last pass; the same of the first one
+  uint32_t *id[2], *row[2];  // id and row of each position after a pass
   int32_t* off;              // [n + 1] first position of each id
   int32_t* counts;           // [2] runs, heavy ids
   int32_t* run;              // [runs] two each: first and last position
   int32_t* heavy;            // [heavy ids] three each: id, first run, runs
   float* part;               // [runs][d]
 };
-
-__device__ __forceinline__ bool known(const int32_t* ids, int64_t r, int64_t rows, int64_t n, uint32_t& id) {
-  id = r < rows ? (uint32_t)ids[r] : 0xffffffffu;
-  return id < (uint64_t)n;
+// A pass: position i of its input has an id, or (the first pass) is a row that may have none.
+struct Pass {
+  const uint32_t *id, *row;  // NULL: the first pass, `ids`
+  const int32_t *ids, *n_rows, *count;   // count: positions of the input of the second
+  int shift, digits;
+  uint32_t mask;
+  uint32_t *to_id, *to_row;
+  int32_t* first;
+};
+__device__ __forceinline__ int64_t length(const Groups& g, const Pass& p) { return p.count ? (int64_t)*p.count : eff_count(g.rows, p.n_rows); }
+__device__ __forceinline__ bool get(const Groups& g, const Pass& p, int64_t i, int64_t end, uint32_t& id) {
+  id = i < end ? (p.id ? p.id[i] : (uint32_t)p.ids[i]) : 0xffffffffu;
+  return id < (uint64_t)g.n;
 }
 
 // The lanes of a wave that have the same key (of `bits` bits), of those that have one.
@@ -114,52 +120,53 @@ __device__ __forceinline__ int block_exclusive(int v, int& total, int* s) {
   return before + inc - v;
 }
 
-__global__ __launch_bounds__(ST) void k_embed_hist(Groups g, const int32_t* ids, const int32_t* n_rows) {
-  __shared__ int h[MAX_BUCKETS];
-  const int64_t rows = eff_count(g.rows, n_rows), r0 = blockIdx.x * g.per;
+__global__ __launch_bounds__(ST) void k_embed_hist(Groups g, Pass p) {
+  __shared__ int h[MAX_DIGITS];
+  const int64_t i0 = blockIdx.x * g.per, end = min(length(g, p), i0 + g.per);
   if (blockIdx.x == 0 && threadIdx.x < 2) g.counts[threadIdx.x] = 0;
-  for (int b = threadIdx.x; b < g.buckets; b += ST) h[b] = 0;
+  for (int b = threadIdx.x; b < p.digits; b += ST) h[b] = 0;
   __syncthreads();
-  for (int64_t r = r0 + threadIdx.x; r < min(r0 + g.per, g.rows); r += ST) {
+  for (int64_t i = i0 + threadIdx.x; i < end; i += ST) {
     uint32_t id;
-    if (known(ids, r, rows, g.n, id)) atomicAdd(&h[id >> g.shift], 1);
+    if (get(g, p, i, end, id)) atomicAdd(&h[id >> p.shift & p.mask], 1);
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < g.buckets; b += ST) g.hist[(int64_t)blockIdx.x * g.buckets + b] = h[b];
+  for (int b = threadIdx.x; b < p.digits; b += ST) g.hist[(int64_t)blockIdx.x * p.digits + b] = h[b];
 }
 
-// A tile's rows to their buckets, behind those of the tiles before it; waves of a tile in turn, so that the order stays.
-__global__ __launch_bounds__(ST) void k_embed_scatter(Groups g, const int32_t* ids, const int32_t* n_rows) {
-  __shared__ int at[MAX_BUCKETS];
+// A tile's rows to their digits, behind those of the tiles before it; waves of a tile in turn, so that the order stays.
+__global__ __launch_bounds__(ST) void k_embed_scatter(Groups g, Pass p) {
+  __shared__ int at[MAX_DIGITS];
   __shared__ int s[ST / 64];
-  const int64_t rows = eff_count(g.rows, n_rows), r0 = blockIdx.x * g.per;
+  const int64_t i0 = blockIdx.x * g.per, end = min(length(g, p), i0 + g.per);
   const int wid = threadIdx.x >> 6;
   uint32_t id;
-  bool have = known(ids, r0 + threadIdx.x, min(rows, r0 + g.per), g.n, id);
+  bool have = get(g, p, i0 + threadIdx.x, end, id);
   int base = 0;
-  for (int b0 = 0; b0 < g.buckets; b0 += ST) {
+  for (int b0 = 0; b0 < p.digits; b0 += ST) {
     const int b = b0 + threadIdx.x;
     int before = 0, all = 0, total;
-    if (b < g.buckets)
+    if (b < p.digits)
 #pragma unroll 8
       for (int t = 0; t < g.tiles; ++t) {
-        const int v = g.hist[(int64_t)t * g.buckets + b];
+        const int v = g.hist[(int64_t)t * p.digits + b];
         before += t < (int)blockIdx.x ? v : 0;
         all += v;
       }
     const int from = base + block_exclusive<ST>(all, total, s);
-    if (b < g.buckets) {
+    if (b < p.digits) {
       at[b] = from + before;
-      if (blockIdx.x == 0) g.first[b] = from;
+      if (blockIdx.x == 0) p.first[b] = from;
     }
     base += total;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) g.first[g.buckets] = base;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.first[p.digits] = base;
   __syncthreads();
-  const int bits = 32 - __clz(max(1, g.buckets - 1));
-  for (int64_t c = r0; c < min(r0 + g.per, g.rows); c += ST) {
-    const int64_t r = c + threadIdx.x;
-    const uint32_t b = have ? id >> g.shift : 0u;
+  const int bits = 32 - __clz(max(1, p.digits - 1));
+  for (int64_t c = i0; c < end; c += ST) {
+    const int64_t i = c + threadIdx.x;
+    const uint32_t b = have ? id >> p.shift & p.mask : 0u;
+    const uint32_t r = have ? (p.row ? p.row[i] : (uint32_t)i) : 0u;
     const uint64_t peers = same_key(have, b, bits);
     const int rank = lower_lanes(peers);
     int pos = 0;
@@ -171,79 +178,56 @@ __global__ __launch_bounds__(ST) void k_embed_scatter(Groups g, const int32_t* i
       __syncthreads();
     }
     if (have) {
-      g.bid[pos] = id;
-      g.brow[pos] = (uint32_t)r;
+      p.to_id[pos] = id;
+      p.to_row[pos] = r;
     }
-    have = known(ids, r + ST, min(rows, r0 + g.per), g.n, id);
+    have = get(g, p, i + ST, end, id);
   }
 }
 
-// A bucket's rows in the order of their ids; every id's first position, and the runs of those with more than LIGHT rows.
-__global__ __launch_bounds__(NT) void k_embed_order(Groups g) {
-  extern __shared__ int at[];   // [ids of a bucket]
+// Every id's first position (a search among those that share its high digit), and the runs of those with more than LIGHT rows.
+__global__ __launch_bounds__(NT) void k_embed_bounds(Groups g, const uint32_t* key) {
   __shared__ int s[NT / 64], base[2], many[MANY][3], n_many;
-  const int wid = threadIdx.x >> 6, width = 1 << g.shift;
-  const int a = g.first[blockIdx.x], e = g.first[blockIdx.x + 1];
-  const int64_t id0 = (int64_t)blockIdx.x << g.shift;
-  const int have_ids = (int)min((int64_t)width, g.n - id0);
-  for (int i = threadIdx.x; i < width; i += NT) at[i] = 0;
-  __syncthreads();
-  for (int c = a; c < e; c += AT_ONCE * NT) {
-    uint32_t id[AT_ONCE];
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) id[u] = g.bid[min(c + u * NT + (int)threadIdx.x, e - 1)];
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      if (c + u * NT >= e) break;
-      const bool have = c + u * NT + (int)threadIdx.x < e;
-      const uint32_t i = id[u] - (uint32_t)id0;
-      const uint64_t peers = same_key(have, i, g.shift);
-      if (have && lower_lanes(peers) == 0) atomicAdd(&at[i], __popcll(peers));
+  const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
+  const auto first_of = [&](int64_t id) {
+    int lo = g.first[id >> g.low], hi = id < g.n ? g.first[(id >> g.low) + 1] : lo;
+    while (lo < hi) {
+      const int m = (lo + hi) >> 1;
+      if (key[m] < id) lo = m + 1;
+      else hi = m;
     }
-  }
-  __syncthreads();
-  // counts to first positions: a thread has `each` neighbouring ids
-  const int each = (width + NT - 1) / NT, i0 = threadIdx.x * each;
-  int sum = 0, mine = 0, mine_runs = 0, total, all, all_runs;
-  for (int i = i0; i < min(i0 + each, width); ++i) {
-    sum += at[i];
-    if (at[i] > LIGHT) ++mine, mine_runs += (int)cdiv(at[i], LIGHT);
-  }
-  int from = a + block_exclusive<NT>(sum, total, s);
-  int h = block_exclusive<NT>(mine, all, s), first = block_exclusive<NT>(mine_runs, all_runs, s);
-  if (threadIdx.x == 0) {
+    return lo;
+  };
+  int from = 0, count = 0;
+  if (i <= g.n) g.off[i] = from = i < g.n ? first_of(i) : g.first[(g.n - 1 >> g.low) + 1];
+  if (i < g.n) count = (i + 1 < g.n ? first_of(i + 1) : g.first[(g.n - 1 >> g.low) + 1]) - from;
+  const int runs = count > LIGHT ? (int)cdiv(count, LIGHT) : 0;
+  int all, all_runs;
+  const int h = block_exclusive<NT>(runs > 0, all, s), f = block_exclusive<NT>(runs, all_runs, s);
+  if (all == 0) return;
+  if (threadIdx.x == 0) {   // (places, not order)
     n_many = 0;
-    if (all) {   // (places, not order)
-      base[0] = atomicAdd(g.counts, all_runs);
-      base[1] = atomicAdd(g.counts + 1, all);
-    }
+    base[0] = atomicAdd(g.counts, all_runs);
+    base[1] = atomicAdd(g.counts + 1, all);
   }
   __syncthreads();
-  for (int i = i0; i < min(i0 + each, width); ++i) {
-    const int count = at[i];
-    at[i] = from;
-    if (i < have_ids) g.off[id0 + i] = from;
-    if (count > LIGHT) {
-      const int runs = (int)cdiv(count, LIGHT), f = base[0] + first, o = base[1] + h;
-      g.heavy[3 * o] = (int32_t)(id0 + i);
-      g.heavy[3 * o + 1] = f;
-      g.heavy[3 * o + 2] = runs;
-      // those of many runs by the whole block, below
-      const int q = runs > 4 ? atomicAdd(&n_many, 1) : MANY;
-      if (q < MANY) {
-        many[q][0] = f;
-        many[q][1] = from;
-        many[q][2] = count;
-      } else {
-        for (int k = 0; k < runs; ++k) {
-          g.run[2 * (f + k)] = from + k * LIGHT;
-          g.run[2 * (f + k) + 1] = from + min(count, (k + 1) * LIGHT);
-        }
+  if (runs) {
+    const int o = base[1] + h;
+    g.heavy[3 * o] = (int32_t)i;
+    g.heavy[3 * o + 1] = base[0] + f;
+    g.heavy[3 * o + 2] = runs;
+    // those of many runs by the whole block, below
+    const int q = runs > 4 ? atomicAdd(&n_many, 1) : MANY;
+    if (q < MANY) {
+      many[q][0] = base[0] + f;
+      many[q][1] = from;
+      many[q][2] = count;
+    } else {
+      for (int k = 0; k < runs; ++k) {
+        g.run[2 * (base[0] + f + k)] = from + k * LIGHT;
+        g.run[2 * (base[0] + f + k) + 1] = from + min(count, (k + 1) * LIGHT);
       }
-      ++h;
-      first += runs;
     }
-    from += count;
   }
   __syncthreads();
   for (int q = 0; q < min(n_many, MANY); ++q)
@@ -251,33 +235,6 @@ __global__ __launch_bounds__(NT) void k_embed_order(Groups g) {
       g.run[2 * (many[q][0] + k)] = many[q][1] + k * LIGHT;
       g.run[2 * (many[q][0] + k) + 1] = many[q][1] + min(many[q][2], (k + 1) * LIGHT);
     }
-  if (blockIdx.x + 1 == g.buckets && threadIdx.x == 0) g.off[g.n] = e;
-  __syncthreads();
-  for (int c = a; c < e; c += AT_ONCE * NT) {
-    uint32_t id[AT_ONCE], r[AT_ONCE];
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      const int k = min(c + u * NT + (int)threadIdx.x, e - 1);
-      id[u] = g.bid[k];
-      r[u] = g.brow[k];
-    }
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      if (c + u * NT >= e) break;
-      const bool have = c + u * NT + (int)threadIdx.x < e;
-      const uint32_t i = id[u] - (uint32_t)id0;
-      const uint64_t peers = same_key(have, i, g.shift);
-      const int rank = lower_lanes(peers);
-      for (int w = 0; w < NT / 64; ++w) {
-        if (w == wid && have) {
-          const int pos = at[i] + rank;
-          g.row[pos] = r[u];
-          if (rank + 1 == __popcll(peers)) at[i] = pos + 1;
-        }
-        __syncthreads();
-      }
-    }
-  }
 }
 
 // --------------------------------------------------------------------------- sums
@@ -300,7 +257,7 @@ __device__ __forceinline__ void add_rows(float (&s)[4], const uint32_t* row, int
 
 // Four columns of IDS neighbouring ids (those with at most LIGHT rows), or of a run: blocks from id_blocks on.  An id's first two
 // rows are requested for all of them together.
-__global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int64_t lddy, int d, float scale, int64_t id_blocks,
+__global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const uint32_t* row, const float* dy, int64_t lddy, int d, float scale, int64_t id_blocks,
                                                   float* dtable) {
   const int dv = (int)cdiv(d, 4);
   const bool runs = blockIdx.x >= id_blocks;
@@ -311,7 +268,7 @@ __global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int
   if (runs) {
     if (i >= g.counts[0]) return;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    add_rows(s, g.row, g.run[2 * i], g.run[2 * i + 1], dy, lddy, n);
+    add_rows(s, row, g.run[2 * i], g.run[2 * i + 1], dy, lddy, n);
     store_some(g.part + i * d + c, n, s);
     return;
   }
@@ -325,7 +282,7 @@ __global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int
 #pragma unroll
   for (int u = 0; u < IDS; ++u)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) r[u][k] = off[u] + k < off[u + 1] ? g.row[off[u] + k] : 0u;
+    for (int k = 0; k < 2; ++k) r[u][k] = off[u] + k < off[u + 1] ? row[off[u] + k] : 0u;
 #pragma unroll
   for (int u = 0; u < IDS; ++u)
 #pragma unroll
@@ -343,7 +300,7 @@ __global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const float* dy, int
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[j] = k < count ? s[j] + v[u][k][j] : s[j];
-    if (count > 2) add_rows(s, g.row, off[u] + 2, off[u + 1], dy, lddy, n);
+    if (count > 2) add_rows(s, row, off[u] + 2, off[u + 1], dy, lddy, n);
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[j] *= scale;
     store_some(dtable + (id + u) * d + c, n, s);
@@ -383,16 +340,13 @@ size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 int64_t most_heavy(int64_t rows) { return rows / (LIGHT + 1); }
 int64_t most_runs(int64_t rows) { return rows / LIGHT + most_heavy(rows); }
 
-// Buckets: about 32 rows in each, as far as LDS has counters for them and for their ids.
+// One pass where every id can be a digit, else two of about half of an id's bits.
 void lay_out(Groups& g, int64_t rows, int64_t n) {
   g.rows = rows;
   g.n = n;
   g.per = std::max<int64_t>(ST, cdiv(cdiv(rows, MAX_TILES), ST) * ST);
   g.tiles = (int)cdiv(rows, g.per);
-  const int64_t want = std::min<int64_t>(MAX_BUCKETS, std::max({int64_t(256), rows / 32, cdiv(n, MAX_WIDTH_IDS)}));
-  g.shift = 0;
-  while (cdiv(n, int64_t(1) << g.shift) > want) ++g.shift;
-  g.buckets = (int)cdiv(n, int64_t(1) << g.shift);
+  g.low = n <= MAX_DIGITS ? 0 : bits_for(n - 1) / 2;
 }
 size_t place(Groups& g, int d, char* w) {
   char* const start = w;
@@ -401,11 +355,14 @@ size_t place(Groups& g, int d, char* w) {
     w += al(bytes);
     return p;
   };
-  g.hist = (int32_t*)take(4 * (size_t)g.tiles * g.buckets);
-  g.first = (int32_t*)take(4 * ((size_t)g.buckets + 1));
-  g.bid = (uint32_t*)take(4 * g.rows);
-  g.brow = (uint32_t*)take(4 * g.rows);
-  g.row = (uint32_t*)take(4 * g.rows);
+  const size_t high = (size_t)cdiv(g.n, int64_t(1) << g.low), low = g.low ? size_t(1) << g.low : 0;
+  g.hist = (int32_t*)take(4 * (size_t)g.tiles * std::max(high, low));
+  g.first = (int32_t*)take(4 * (high + 1));
+  g.firsts = (int32_t*)take(4 * (low + 1));
+  for (int k = 0; k < 2; ++k) {
+    g.id[k] = (uint32_t*)take(4 * g.rows);
+    g.row[k] = (uint32_t*)take(4 * g.rows);
+  }
   g.off = (int32_t*)take(4 * (g.n + 1));
   g.counts = (int32_t*)take(8);
   g.run = (int32_t*)take(8 * most_runs(g.rows));
@@ -420,7 +377,7 @@ bool embed_fits(const mtgnn_embedding_dims* d, int64_t rows, bool back) {
   constexpr int64_t MAX = (int64_t(1) << 32) - 2 * NT;
   if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX - 4 * NT;
   const int64_t dv = cdiv(d->d, 4);
-  return d->n <= (int64_t)MAX_BUCKETS * MAX_WIDTH_IDS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows) * dv <= MAX &&
+  return d->n <= (int64_t)MAX_DIGITS * MAX_DIGITS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows) * dv <= MAX &&
          most_heavy(rows) * cdiv(d->d, 64) * NT <= MAX;
 }
 
@@ -454,15 +411,25 @@ mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t m
   Groups g;
   lay_out(g, max_rows, d->n);
   place(g, d->d, (char*)ws);
-  k_embed_hist<<<(unsigned)g.tiles, ST, 0, s>>>(g, ids, n_rows);
-  MTGNN_CHECK_LAUNCH("embed_hist");
-  k_embed_scatter<<<(unsigned)g.tiles, ST, 0, s>>>(g, ids, n_rows);
-  MTGNN_CHECK_LAUNCH("embed_scatter");
-  const size_t lds = sizeof(int) << g.shift;
-  k_embed_order<<<(unsigned)g.buckets, NT, lds, s>>>(g);
-  MTGNN_CHECK_LAUNCH("embed_order");
+  const auto pass = [&](const Pass& p) -> mtgnn_status {
+    k_embed_hist<<<(unsigned)g.tiles, ST, 0, s>>>(g, p);
+    MTGNN_CHECK_LAUNCH("embed_hist");
+    k_embed_scatter<<<(unsigned)g.tiles, ST, 0, s>>>(g, p);
+    MTGNN_CHECK_LAUNCH("embed_scatter");
+    return MTGNN_OK;
+  };
+  const int high = (int)cdiv(d->n, int64_t(1) << g.low), last = g.low ? 1 : 0;
+  if (g.low) {
+    const int digits = 1 << g.low;
+    MTGNN_TRY(pass(Pass{nullptr, nullptr, ids, n_rows, nullptr, 0, digits, (uint32_t)digits - 1, g.id[0], g.row[0], g.firsts}));
+    MTGNN_TRY(pass(Pass{g.id[0], g.row[0], nullptr, nullptr, g.firsts + digits, g.low, high, ~0u, g.id[1], g.row[1], g.first}));
+  } else {
+    MTGNN_TRY(pass(Pass{nullptr, nullptr, ids, n_rows, nullptr, 0, high, ~0u, g.id[0], g.row[0], g.first}));
+  }
+  k_embed_bounds<<<(unsigned)cdiv(d->n + 1, NT), NT, 0, s>>>(g, g.id[last]);
+  MTGNN_CHECK_LAUNCH("embed_bounds");
   const int64_t dv = cdiv(d->d, 4), id_blocks = cdiv(cdiv(d->n, IDS) * dv, NT);
-  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows) * dv, NT)), NT, 0, s>>>(g, dy, lddy, d->d, d->scale, id_blocks,
+  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows) * dv, NT)), NT, 0, s>>>(g, g.row[last], dy, lddy, d->d, d->scale, id_blocks,
                                                                                          dtable);
   MTGNN_CHECK_LAUNCH("embed_sum");
   if (most_heavy(max_rows) > 0) {
