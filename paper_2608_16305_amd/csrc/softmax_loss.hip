@@ -19,6 +19,7 @@
 // zeros to whole steps.
 #include <algorithm>
 #include <cmath>
+#include <cmath>
 
 #include "gemm.h"
 #include "ops.h"
@@ -717,21 +718,32 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
-// The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.
-__global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const int32_t* idx, const float* part, int split,
+// The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.  `by` threads of a
+// block add up every by-th share of the same four elements.
+__global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const int32_t* idx, const float* part, int split, int by,
                                                      int64_t rows, int d, const float* dloss, int add, float* out, int64_t ldo) {
-  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
+  __shared__ float4 sums[256];
+  const uint32_t dv = (uint32_t)cdiv(d, 4), each = 256 / by, at = threadIdx.x % each, k = threadIdx.x / each, e = blockIdx.x * each + at;
   const int64_t r = e / dv, n = *count;
   const int c = (int)(e % dv) * 4;
-  if (r >= (idx ? n : rows)) return;
-  float* o = out + (idx ? (int64_t)idx[r] : r) * ldo + c;
-  const float scale = loss_scale(n, dloss) / LIFT;
+  const bool mine = r < (idx ? n : rows);
   float v[4] = {0.f, 0.f, 0.f, 0.f}, w[4];
-  for (int s = 0; s < split; ++s) {
+  for (int s = (int)k; mine && s < split; s += by) {
     load_some(part + (s * rows + r) * d + c, d - c, w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += w[i];
   }
+  if (by > 1) {
+    sums[threadIdx.x] = make_float4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+    for (int j = 1; k == 0 && j < by; ++j) {
+      const float4 o = sums[j * each + at];
+      v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+    }
+  }
+  if (!mine || k) return;
+  float* o = out + (idx ? (int64_t)idx[r] : r) * ldo + c;
+  const float scale = loss_scale(n, dloss) / LIFT;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] *= scale;
   if (add) {
@@ -874,27 +886,32 @@ struct Tiling {
   int tr, tc, split;
   int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
 };
-// Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 27 us, 3.8 TB/s, in tiles of 256 x 256 48), else large ones where there are enough
-// of them for the card.
+// Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 27 us, 3.8 TB/s, in tiles of 256 x 256 48; for few
+// classes they took as long as small ones), else large ones where there are enough of them for the card.
 Tiling tiling(int64_t rows, int64_t cols) {
   if (rows <= 64) return Tiling{64, 256, 1};
   const Tiling big{256, 256, 1};
   return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 128, 1};
 }
 // Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
-// enough to fill the card with shares of them; then as many shares as leave the fewest places of the last round of
-// blocks empty.
+// enough to fill the card with shares of them.  The shares are those that are done first, counted in steps (1.3 to 1.5 us each): rounds of
+// blocks, each with 6 steps beside its own, and the shares' way to memory and back, with a launch.
 Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
   Tiling g{256, 256, 1};
   const Tiling small{128, 128, 1};
   if (g.tiles(rows, cols) * 4 * 100 > small.tiles(rows, cols) * 115 || g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192) g = small;
   const int64_t t = g.tiles(rows, cols), slots = g.tr == 256 ? 256 : 512;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, steps / 16));
-  double best = 0.0;
-  for (int64_t s = 1; s <= most; ++s) {
-    const double used = (double)(t * s) / (double)(slots * cdiv(t * s, slots)) - 0.01 * (double)(s - 1);
-    if (used > best) best = used, g.split = (int)s;
-  }
+  const double size = (double)rows * (double)cols / 8e5;
+  const auto cost = [&](int64_t s) {
+    return (double)(cdiv(t * s, slots) * (cdiv(steps, s) + 6)) + (s > 1 ? 6. + (double)s * size : 0.);
+  };
+  double best = cost(1);
+  const auto look = [&](int64_t s) {
+    s = std::min(s, steps / 8);
+    if (s > 1 && cost(s) < best) best = cost(s), g.split = (int)s;
+  };
+  for (int k = 1; k <= 4; ++k) look(k * slots / t);   // whole rounds,
+  if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));   // or so many that more would gain less than they cost
   return g;
 }
 struct Shares {
@@ -934,8 +951,9 @@ mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s
   q.out = part;
   q.ldo = p.cols;
   MTGNN_TRY((product<KIND, true>(q, t, s)));
-  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256), 256, 0, s>>>(p.count, p.idx, part, t.split, p.rows, (int)p.cols,
-                                                                              p.dloss, p.add, p.out, p.ldo);
+  const int by = t.split > 32 ? 16 : t.split > 8 ? 4 : 1;   // (many shares are of few elements)
+  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256 / by), 256, 0, s>>>(p.count, p.idx, part, t.split, by, p.rows,
+                                                                                   (int)p.cols, p.dloss, p.add, p.out, p.ldo);
   MTGNN_CHECK_LAUNCH("loss_shares");
   return MTGNN_OK;
 }

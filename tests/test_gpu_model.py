@@ -89,6 +89,8 @@ EMBED = [  # rows, pad, n, d, scale, ids (how many different), share that is no 
     (5000, 100, 300, 20, 0.125, 300, 0.05, True),
     (4099, 0, 70000, 12, 1.0, 70000, 0.0, False),
     (9000, 0, 1025, 260, 1.0, 5, 0.01, False),
+    (20000, 0, 9001, 3, 1.0, 2, 0.0, False),
+    (30000, 11, 8192, 9, 1.0, 1, 0.0, True),
 ]
 
 
@@ -137,6 +139,8 @@ NORM = [  # rows, pad, d, affine, past, wide
     (3, 0, 8193, True, False, True),
     (70, 2, 9000, True, True, False),
     (2, 0, 33000, True, True, True),
+    (9000, 30, 21, True, True, True),
+    (17001, 0, 8, True, False, False),
 ]
 
 
@@ -234,6 +238,8 @@ LOSS = [  # rows, pad, n, d, bias, share without a label, wide, dloss
     (300, 0, 257, 520, False, 0.2, False, None),
     (2100, 30, 40, 16, True, 0.1, False, None),
     (5, 0, 4000, 200, True, 0.0, False, None),
+    (3, 2, 70000, 20, True, 0.0, True, None),
+    (9000, 0, 5, 33, True, 0.1, True, 0.25),
 ]
 # enough tiles of 256 for the larger kernels, forward and backward; whole and ragged ones
 LOSS_BIG = [(3333, 40, 3800, 72, True, 0.03, True, None), (3584, 0, 3584, 64, False, 0.0, False, 1.5)]
