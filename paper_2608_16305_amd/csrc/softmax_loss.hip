@@ -19,7 +19,6 @@
 // zeros to whole steps.
 #include <algorithm>
 #include <cmath>
-#include <cmath>
 
 #include "gemm.h"
 #include "ops.h"
@@ -32,7 +31,6 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 
 constexpr int KS = 64;          // a step of the sums: 128 bytes of a line
 constexpr int PAD = 64;         // rows and columns are padded to whole ones
@@ -718,6 +716,331 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
+// --------------------------------------------------------------------------- few rows of float32
+
+// At most 64 rows of float32.  For so few every product is reading W or writing dW, and W is read as it is, on the float32 matrix
+// instructions (256 operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in
+// float16 parts it is searched, laid out and read (14 x 142,281 x 1,024 forward 592 us for 143).  A block has 64 CF classes; a
+// lane reads 16 bytes of a class at a k four apart from its neighbours', and x, through LDS, in the same order, so that the
+// fragments need no more than that.  The forward leaves what STAT does, and x's rows with a label as they are; the backward
+// forms the logits again, leaves P times LIFT [classes][16 RF] for dx, and writes db and, from P and x in LDS, dW.
+struct Few {
+  const float *x, *W, *b;
+  int64_t ldx;
+  const int32_t *label, *n_rows;
+  int64_t max_rows;
+  int n, d;
+  int32_t *count, *idx, *lab;
+  float* xc;                // x's rows with a label, dp apart, zeros behind d; the forward's may be NULL
+  int dp;
+  float2* part;             // forward
+  int64_t ld_part;
+  float *at_label, *row_loss;
+  const float2* stat;       // backward
+  const float* dloss;
+  float *P, *db, *dW;       // each or NULL
+};
+constexpr int FEW = 64, KC = 64, LDC = KC + 4;
+template <int RF, int CF, bool BACK>
+__global__ __launch_bounds__(256) void k_loss_few(Few p) {
+  __shared__ __align__(16) float xs[2][16 * RF][LDC];
+  __shared__ __align__(16) float ps[BACK ? 64 * CF : 1][16 * RF + 4], out[BACK ? 4 : 1][16][LDC];
+  __shared__ int src[FEW], lab[FEW];
+  __shared__ float2 st[4][16 * RF];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fg = lane >> 4;
+  int count;
+  if constexpr (BACK) {
+    count = *p.count;
+    if (wid == 0 && lane < count) lab[lane] = p.lab[lane];
+  } else {
+    const int64_t rows = eff_count(p.max_rows, p.n_rows);
+    const bool ok = has_label(p.label, lane, rows, p.n);
+    const uint64_t have = __ballot(ok);
+    count = __popcll(have);
+    if (wid == 0) {
+      const int at = __popcll(have & ((uint64_t(1) << lane) - 1));
+      if (ok) src[at] = lane, lab[at] = p.label[lane];
+      if (blockIdx.x == 0) {
+        if (lane == 0) *p.count = count;
+        if (ok) p.idx[at] = lane, p.lab[at] = p.label[lane];
+        else if (lane < rows && p.row_loss) p.row_loss[lane] = 0.f;
+      }
+    }
+  }
+  const int c0 = (int)blockIdx.x * 64 * CF + wid * 16 * CF, steps = (int)cdiv(p.d, KC);
+  if (!BACK && count == 0) return;
+  __syncthreads();
+
+  const float* w[CF];
+#pragma unroll
+  for (int j = 0; j < CF; ++j) w[j] = p.W + (int64_t)min(c0 + 16 * j + fr, p.n - 1) * p.d + 4 * fg;
+  const int xl = threadIdx.x >> 4, xk = 4 * (threadIdx.x & 15);
+  const float* xr[RF];
+#pragma unroll
+  for (int u = 0; u < RF; ++u) {
+    const int r = 16 * u + xl;
+    if constexpr (BACK) xr[u] = r < count ? p.xc + (int64_t)r * p.dp + xk : nullptr;
+    else xr[u] = r < count ? p.x + (int64_t)src[r] * p.ldx + xk : nullptr;
+  }
+  float xv[RF][4];
+  const auto load_x = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < RF; ++u)
+      if (!xr[u]) xv[u][0] = xv[u][1] = xv[u][2] = xv[u][3] = 0.f;
+      else load_some(xr[u] + k, BACK || k + KC <= p.d ? 4 : p.d - k - xk, xv[u]);
+  };
+  const auto put_x = [&](float (*xb)[LDC]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < RF; ++u) *(float4*)&xb[16 * u + xl][xk] = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
+  };
+  float wv[CF][4][4];
+  const auto load = [&](int k) __attribute__((always_inline)) {
+    const bool whole = k + KC <= p.d;
+#pragma unroll
+    for (int j = 0; j < CF; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) load_some(w[j] + k + 16 * t, whole ? 4 : p.d - k - 16 * t - 4 * fg, wv[j][t]);
+    load_x(k);
+  };
+  f32x4 acc[RF][CF];
+#pragma unroll
+  for (int i = 0; i < RF; ++i)
+#pragma unroll
+    for (int j = 0; j < CF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load(0);
+  for (int step = 0; step < steps; ++step) {
+    float (*xb)[LDC] = xs[step & 1];
+    float now[CF][4][4];
+#pragma unroll
+    for (int j = 0; j < CF; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) now[j][t][e] = wv[j][t][e];
+    put_x(xb);
+    if (!BACK && p.xc && blockIdx.x == 0) {
+#pragma unroll
+      for (int u = 0; u < RF; ++u) *(float4*)(p.xc + (int64_t)(16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
+    }
+    if (step + 1 < steps) load((step + 1) * KC);
+    __syncthreads();   // (every wave has read what the step before last left here)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 f[RF];
+#pragma unroll
+      for (int i = 0; i < RF; ++i) f[i] = *(const f32x4*)&xb[16 * i + fr][16 * t + 4 * fg];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < CF; ++j)
+#pragma unroll
+          for (int i = 0; i < RF; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(now[j][t][e], f[i][e], acc[i][j], 0, 0, 0);
+    }
+  }
+
+  // A lane has classes c0 + 16 j + 4 fg .. + 3 of the rows 16 i + fr.
+  float bias[CF][4];
+#pragma unroll
+  for (int j = 0; j < CF; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = c0 + 16 * j + 4 * fg + e;
+      bias[j][e] = p.b && c < p.n ? p.b[c] : 0.f;
+    }
+  if constexpr (!BACK) {
+#pragma unroll
+    for (int i = 0; i < RF; ++i) {
+      const int r = 16 * i + fr, at = r < count ? lab[r] : -1;
+      float m = -INFINITY, v = 0.f;
+#pragma unroll
+      for (int j = 0; j < CF; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = c0 + 16 * j + 4 * fg + e;
+          const float l = c < p.n ? acc[i][j][e] + bias[j][e] : -INFINITY;
+          acc[i][j][e] = l;
+          if (c == at) p.at_label[r] = l;
+          m = fmaxf(m, l);
+        }
+      m = fmaxf(m, __shfl_xor(m, 16, 64));
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int j = 0; j < CF; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * LOG2E);
+      v += __shfl_xor(v, 16, 64);
+      v += __shfl_xor(v, 32, 64);
+      if (fg == 0) st[wid][r] = make_float2(m, v);
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= min(count, 16 * RF)) return;
+    float2 q = st[0][r];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) join(q, st[k][r]);
+    p.part[blockIdx.x * p.ld_part + r] = q;
+  } else {
+    const float scale = loss_scale(count, p.dloss) / LIFT;
+    float sum[CF][4];
+#pragma unroll
+    for (int i = 0; i < RF; ++i) {
+      const int r = 16 * i + fr, at = r < count ? lab[r] : -1;
+      const float2 s = r < count ? p.stat[r] : make_float2(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < CF; ++j) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = c0 + 16 * j + 4 * fg + e;
+          float v = __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - s.x) * LOG2E) * (s.y * LIFT);
+          if (c == at) v -= LIFT;
+          if (r >= count) v = 0.f;
+          sum[j][e] = i ? sum[j][e] + v : v;
+          if (p.P && c < p.n) p.P[(int64_t)c * (16 * RF) + r] = v;
+          ps[wid * 16 * CF + 16 * j + 4 * fg + e][r] = v;
+        }
+      }
+    }
+    if (p.db) {
+#pragma unroll
+      for (int j = 0; j < CF; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) sum[j][e] += __shfl_xor(sum[j][e], o, 64);
+          const int c = c0 + 16 * j + 4 * fg + e;
+          if (fr == 0 && c < p.n) p.db[c] = sum[j][e] * scale;
+        }
+    }
+    if (!p.dW) return;
+    // dW of the wave's classes, 64 k at a time: P's rows, and x's, four apart in a lane; out through LDS in whole 256 bytes.
+    f32x4 pf[CF][RF];
+    __syncthreads();   // (of xs too)
+#pragma unroll
+    for (int j = 0; j < CF; ++j)
+#pragma unroll
+      for (int t = 0; t < RF; ++t) pf[j][t] = *(const f32x4*)&ps[wid * 16 * CF + 16 * j + fr][16 * t + 4 * fg];
+    load_x(0);
+    for (int step = 0; step < steps; ++step) {
+      float (*xb)[LDC] = xs[step & 1];
+      put_x(xb);
+      if (step + 1 < steps) load_x((step + 1) * KC);
+      __syncthreads();
+      f32x4 g[CF][4];
+#pragma unroll
+      for (int j = 0; j < CF; ++j)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) g[j][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < RF; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const float f = xb[16 * t + 4 * fg + e][16 * h + fr];
+#pragma unroll
+            for (int j = 0; j < CF; ++j) g[j][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(f, pf[j][t][e], g[j][h], 0, 0, 0);
+          }
+#pragma unroll
+      for (int j = 0; j < CF; ++j) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) *(f32x4*)&out[wid][fr][16 * h + 4 * fg] = g[j][h];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = c0 + 16 * j + 4 * q + fg, k = step * KC + 4 * fr;
+          const f32x4 f = *(const f32x4*)&out[wid][4 * q + fg][4 * fr];
+          const float v[4] = {f[0] * scale, f[1] * scale, f[2] * scale, f[3] * scale};
+          if (c < p.n) store_some(p.dW + (int64_t)c * p.d + k, p.d - k, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+}
+
+// A share of dx = P W: 64 columns (blockIdx.x of them) of the classes from blockIdx.y `per` on, 16 a step of a wave.  A lane reads 16
+// bytes of a class, four columns of the matrix instructions', and the classes' P.
+template <int RF>
+__global__ __launch_bounds__(256) void k_loss_few_dx(const int32_t* n_have, const float* P, const float* W, int n, int d, int per,
+                                                     int64_t rows, float* part) {
+  __shared__ __align__(16) float sums[2][16 * RF][LDC];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fg = lane >> 4;
+  const int k = (int)blockIdx.x * KC + 4 * fr, count = *n_have;
+  if (count == 0) return;
+  const int64_t first = (int64_t)blockIdx.y * per, end = min(first + per, (int64_t)n);
+  float wv[4][4], pv[4][RF];
+  const auto load = [&](int64_t c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t at = c + 4 * t + fg, use = min(at, (int64_t)n - 1);
+      load_some(W + use * d + k, d - k, wv[t]);
+#pragma unroll
+      for (int i = 0; i < RF; ++i) {
+        pv[t][i] = P[use * (16 * RF) + 16 * i + fr];
+        if (at >= end) pv[t][i] = 0.f;
+      }
+      if (at >= end) wv[t][0] = wv[t][1] = wv[t][2] = wv[t][3] = 0.f;
+    }
+  };
+  f32x4 acc[RF][4];
+#pragma unroll
+  for (int i = 0; i < RF; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int64_t c = first + 16 * wid;
+  if (c < end) load(c);
+  for (; c < end; c += 64) {
+    float w[4][4], q[4][RF];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[t][e] = wv[t][e];
+#pragma unroll
+      for (int i = 0; i < RF; ++i) q[t][i] = pv[t][i];
+    }
+    if (c + 64 < end) load(c + 64);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < RF; ++i) acc[i][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(q[t][i], w[t][e], acc[i][e], 0, 0, 0);
+  }
+  // (a lane has columns k .. k + 3 of the rows 16 i + 4 fg + q; the waves' sums are added by halves)
+#pragma unroll
+  for (int half = 2; half > 0; half >>= 1) {
+    if (wid >= half && wid < 2 * half) {
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(f32x4*)&sums[wid - half][16 * i + 4 * fg + q][4 * fr] = f32x4{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
+    }
+    __syncthreads();
+    if (wid < half) {
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 o = *(const f32x4*)&sums[wid][16 * i + 4 * fg + q][4 * fr];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][e][q] += o[e];
+        }
+    }
+    __syncthreads();
+  }
+  if (wid) return;
+#pragma unroll
+  for (int i = 0; i < RF; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = 16 * i + 4 * fg + q;
+      const float v[4] = {acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
+      if (r < count) store_some(part + ((int64_t)blockIdx.y * rows + r) * d + k, d - k, v);
+    }
+}
+
 // The sums of the blocks that shared a product's: rows of dx (idx given: the rows with a label) or of dW.  `by` threads of a
 // block add up every by-th share of the same four elements.
 __global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const int32_t* idx, const float* part, int split, int by,
@@ -847,6 +1170,7 @@ int64_t stride(int64_t width) { return up(width, PAD) | PAD; }
 
 struct Plan {
   bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes)
+  bool few;                  // float32 operands of so few rows that the forward reads W itself
   int dp;                    // padded width
   int64_t Rp, width;         // padded rows; classes of a piece
 };
@@ -855,6 +1179,7 @@ Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
   p.bf = d->dtype == MTGNN_BF16;
   p.dp = (int)stride(d->d);
   p.copy = p.bf && d->d % 8 != 0;
+  p.few = !p.bf && rows <= FEW;
   p.Rp = up(rows, PAD);
   const int64_t most = (int64_t)(PIECE / (4 * (size_t)p.Rp)) / 256 * 256;
   p.width = std::min<int64_t>(up(d->n, PAD), std::max<int64_t>(256, most));
@@ -914,6 +1239,19 @@ Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
   if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));   // or so many that more would gain less than they cost
   return g;
 }
+int row_frags(int64_t rows) { return rows > 32 ? 4 : rows > 16 ? 2 : 1; }
+// Classes of a share of k_loss_few_dx: enough blocks to fill the card, each of a few steps at least.
+int few_per(const mtgnn_loss_dims* d) {
+  const int64_t chunks = cdiv(d->d, KC), shares = std::max<int64_t>(1, std::min<int64_t>(cdiv(2048, chunks), d->n / 256));
+  return (int)up(cdiv(d->n, shares), 64);
+}
+// Classes of a block of the forward's k_loss_few: more for short rows of many classes, whose tiles then take less time to join (128 and 64, the
+// whole forward: 16 x 190,000 x 200 51 and 61 us, 14 x 142,281 x 1,024 152 and 143, 64 x 9,000 x 1,024 55 and 38).
+int few_classes(const mtgnn_loss_dims* d) { return d->n >= 32768 && d->d < 512 ? 128 : 64; }
+// A forward's tiles of classes.
+int64_t class_tiles(const mtgnn_loss_dims* d, const Plan& p, int64_t rows) {
+  return cdiv(d->n, p.few ? few_classes(d) : tiling(rows, d->n).tc);
+}
 struct Shares {
   Tiling dx, dw;             // of a piece
   size_t bytes;
@@ -943,6 +1281,13 @@ mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
 }
+mtgnn_status join_shares(const Prod& p, int split, const float* part, hipStream_t s) {
+  const int by = split > 32 ? 16 : split > 8 ? 4 : 1;   // (many shares are of few elements)
+  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256 / by), 256, 0, s>>>(p.count, p.idx, part, split, by, p.rows, (int)p.cols,
+                                                                                   p.dloss, p.add, p.out, p.ldo);
+  MTGNN_CHECK_LAUNCH("loss_shares");
+  return MTGNN_OK;
+}
 // A gradient's product, shared by `split` blocks a tile through `part`.
 template <int KIND>
 mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s) {
@@ -951,10 +1296,23 @@ mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s
   q.out = part;
   q.ldo = p.cols;
   MTGNN_TRY((product<KIND, true>(q, t, s)));
-  const int by = t.split > 32 ? 16 : t.split > 8 ? 4 : 1;   // (many shares are of few elements)
-  k_loss_shares<<<(unsigned)cdiv(p.rows * cdiv(p.cols, 4), 256 / by), 256, 0, s>>>(p.count, p.idx, part, t.split, by, p.rows,
-                                                                                   (int)p.cols, p.dloss, p.add, p.out, p.ldo);
-  MTGNN_CHECK_LAUNCH("loss_shares");
+  return join_shares(p, t.split, part, s);
+}
+template <bool BACK>
+mtgnn_status few(const Few& p, int tc, hipStream_t s) {
+  const int rf = row_frags(p.max_rows);
+  const unsigned grid = (unsigned)cdiv(p.n, tc);
+  {
+    TimedScope ts(site::Generic::name, s), kind(BACK ? "loss_prob" : "loss_stat", s);
+    if (!BACK && tc == 128) {
+      if (rf == 4) k_loss_few<4, 2, false><<<grid, 256, 0, s>>>(p);
+      else if (rf == 2) k_loss_few<2, 2, false><<<grid, 256, 0, s>>>(p);
+      else k_loss_few<1, 2, false><<<grid, 256, 0, s>>>(p);
+    } else if (rf == 4) k_loss_few<4, 1, BACK><<<grid, 256, 0, s>>>(p);
+    else if (rf == 2) k_loss_few<2, 1, BACK><<<grid, 256, 0, s>>>(p);
+    else k_loss_few<1, 1, BACK><<<grid, 256, 0, s>>>(p);
+  }
+  MTGNN_CHECK_LAUNCH("loss_few");
   return MTGNN_OK;
 }
 
@@ -984,8 +1342,9 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const Plan p = plan(d, rows);
   const size_t t = al(2 * (size_t)up(d->n, PAD) * p.dp);   // a part of W
   if (!back)
-    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
-           al(8 * (size_t)cdiv(d->n, tiling(rows, d->n).tc) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
+           al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+  if (p.few) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
   return 256 + al(4 * MAX_SHARES) + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
@@ -1004,9 +1363,9 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     w += al(bytes);
     return at;
   };
-  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)up(d->n, PAD) * p.dp : 0) : 4 * (size_t)up(d->n, PAD) * p.dp);
+  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)up(d->n, PAD) * p.dp : 0) : p.few ? 0 : 4 * (size_t)up(d->n, PAD) * p.dp);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
-  const int tiles = (int)cdiv(d->n, tl.tc);
+  const int tiles = (int)class_tiles(d, p, max_rows);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, 16));
@@ -1022,14 +1381,21 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     MTGNN_CHECK_LAUNCH("loss_lay");
     return MTGNN_OK;
   };
-  MTGNN_TRY(p.bf ? lay((const uint16_t*)x, (const uint16_t*)W) : lay((const float*)x, (const float*)W));
+  if (!p.few) MTGNN_TRY(p.bf ? lay((const uint16_t*)x, (const uint16_t*)W) : lay((const float*)x, (const float*)W));
   Prod q{};
   q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
   q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = up(d->n, PAD) * p.dp;
   q.topA = k.largest; q.topB = k.largest + 1;
   q.rows = max_rows; q.cols = d->n; q.K = up(d->d, KS); q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
-  if (p.bf) {
+  if (p.few) {
+    Few f{};
+    f.x = (const float*)x; f.ldx = ldx; f.W = (const float*)W; f.b = b;
+    f.label = label; f.n_rows = n_rows; f.max_rows = max_rows; f.n = d->n; f.d = d->d;
+    f.count = k.count; f.idx = k.idx; f.lab = k.lab; f.xc = save ? (float*)k.xc : nullptr; f.dp = p.dp;
+    f.part = part; f.ld_part = p.Rp; f.at_label = at_label; f.row_loss = row_loss;
+    MTGNN_TRY(few<false>(f, few_classes(d), s));
+  } else if (p.bf) {
     if (!p.copy) q.B = (const uint16_t*)W, q.ldb = q.dimB = d->d;
     segments(q, 1, 1);
     MTGNN_TRY((product<STAT, false>(q, tl, s)));
@@ -1055,6 +1421,31 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     w += al(bytes);
     return at;
   };
+  if (p.few) {
+    const int rf = row_frags(max_rows), per = few_per(d);
+    float* P = (float*)take(4 * (size_t)d->n * 16 * rf);
+    Few f{};
+    f.W = (const float*)W; f.b = b; f.max_rows = max_rows; f.n = d->n; f.d = d->d;
+    f.count = k.count; f.idx = k.idx; f.lab = k.lab; f.xc = (float*)k.xc; f.dp = p.dp;
+    f.stat = k.stat; f.dloss = dloss; f.P = dx ? P : nullptr; f.db = db; f.dW = dW;
+    MTGNN_TRY(few<true>(f, 64, s));
+    if (!dx) return MTGNN_OK;
+    First none{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, nullptr, 0, 0, 0};
+    const unsigned zb = (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256);
+    k_loss_back_first<float><<<zb, 256, 0, s>>>(none, dx, lddx, zb, nullptr);
+    MTGNN_CHECK_LAUNCH("loss_back_first");
+    Prod r{};
+    r.rows = max_rows; r.cols = d->d; r.count = k.count; r.idx = k.idx; r.dloss = dloss; r.out = dx; r.ldo = lddx;
+    const dim3 grid((unsigned)cdiv(d->d, KC), (unsigned)cdiv(d->n, per));
+    {
+      TimedScope ts(site::Generic::name, s), kind("loss_dx", s);
+      if (rf == 4) k_loss_few_dx<4><<<grid, 256, 0, s>>>(k.count, P, (const float*)W, d->n, d->d, per, max_rows, (float*)w);
+      else if (rf == 2) k_loss_few_dx<2><<<grid, 256, 0, s>>>(k.count, P, (const float*)W, d->n, d->d, per, max_rows, (float*)w);
+      else k_loss_few_dx<1><<<grid, 256, 0, s>>>(k.count, P, (const float*)W, d->n, d->d, per, max_rows, (float*)w);
+    }
+    MTGNN_CHECK_LAUNCH("loss_few_dx");
+    return join_shares(r, (int)grid.y, (float*)w, s);
+  }
   uint32_t* top = (uint32_t*)take(4);
   uint32_t* share = (uint32_t*)take(4 * MAX_SHARES);
   const int64_t plane = up(d->n, PAD) * p.dp, planeX = p.Rp * p.dp;

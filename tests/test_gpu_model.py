@@ -240,6 +240,10 @@ LOSS = [  # rows, pad, n, d, bias, share without a label, wide, dloss
     (5, 0, 4000, 200, True, 0.0, False, None),
     (3, 2, 70000, 20, True, 0.0, True, None),
     (9000, 0, 5, 33, True, 0.1, True, 0.25),
+    (5, 3, 9, 12, True, 1.0, False, None),
+    (33, 5, 65, 130, True, 0.2, True, None),
+    (64, 0, 33000, 100, True, 0.0, False, 2.0),
+    (20, 0, 40000, 65, False, 0.1, True, None),
 ]
 # enough tiles of 256 for the larger kernels, forward and backward; whole and ragged ones
 LOSS_BIG = [(3333, 40, 3800, 72, True, 0.03, True, None), (3584, 0, 3584, 64, False, 0.0, False, 1.5)]
