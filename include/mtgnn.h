@@ -849,8 +849,8 @@ mtgnn_status mtgnn_adam_step(float* const* params, const float* const* grads, fl
  *   m_exp, v_exp given: the states take 8 bits.  m holds codes of m, v codes of sqrt(v), in e4m3 (4 bits of exponent, bias 7;
  *           3 of mantissa; 448 the largest; 0x7f NaN), in units of 2^(e - 127) for each 32 elements, e = m_exp[i / 32],
  *           v_exp[i / 32] ([ceil(n / 32)], the least e that keeps the block's largest within 448).  Codes are rounded to the
- *           nearest (ties to even) from m and v in 64 bits, a v that is not zero never to zero; what is not finite becomes
- *           NaN.  Zeroed bytes are zeros.  The parameter is updated from m and v before that rounding.
+ *           nearest (ties to even) from m and v in 64 bits (each operation of the formulas rounded), a v that is not zero
+ *           never to zero; what is not finite becomes NaN.  Zeroed bytes are zeros.  The parameter is updated from m and v before that rounding.
  * The descriptions (host) are read during the call.  t of cfg, or where step is given the device count *step (>= 1; a captured
  * call then follows it). */
 typedef struct {

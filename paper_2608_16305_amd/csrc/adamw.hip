@@ -89,6 +89,14 @@ __device__ __forceinline__ double max8(double v) {
 __device__ __forceinline__ float finite(float v) { return v < INFINITY ? v : 0.f; }   // (v >= 0 or NaN)
 __device__ __forceinline__ double finite(double v) { return v < INFINITY ? v : 0.0; }
 
+// a x + b y, each operation rounded: a sum may be meant to lie on a border (0.9 times a code is one now and then), and is there
+// only if its products are what 64 bits make of them.
+__device__ __forceinline__ double sum64(double a, double x, double b, double y) {
+#pragma clang fp contract(off)
+  const double p = a * x, q = b * y;
+  return p + q;
+}
+
 // The codes and the exponent of four elements' magnitudes, x in 64 bits and f as float32 (of the block's eight lanes).
 // Decided in float32; what is near a border, from x itself (root: from its root).
 template <bool ROOT>
@@ -194,8 +202,8 @@ __global__ __launch_bounds__(NT) void k_adamw(Set a, Coef c) {
 #pragma unroll
       for (int j = 0; j < PER; ++j) {   // (codes times their units are exact)
         const double r = (double)(ro[j] * vs), x = j < n ? (double)g[i][j] : 0.0;
-        md[j] = fma(c.b1, (double)(mo[j] * ms), o1 * x);
-        vd[j] = fma(c.b2, r * r, o2 * (x * x));
+        md[j] = sum64(c.b1, (double)(mo[j] * ms), o1, x);
+        vd[j] = sum64(c.b2, r * r, o2, x * x);
         m[i][j] = (float)md[j];
         am[j] = fabsf(m[i][j]);
         v[i][j] = (float)__builtin_amdgcn_sqrt(vd[j]);   // (the instruction's root: within a few float32 units)

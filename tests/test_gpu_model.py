@@ -509,6 +509,31 @@ def test_adamw_8_bit_borders():
         assert torch.equal(a[ok], b[ok])
 
 
+def test_adamw_8_bit_sums_on_borders():
+    """beta1 = 0.9: old codes and gradients whose new m is a border of two codes in decimals.  Which side it falls on is decided by
+    the roundings of the formula's operations in 64 bits, which the oracle's are."""
+    c = np.asarray(model.E4M3[:127], np.float64)
+    border = (c[:-1] + c[1:]) / 2
+    old, to = (x.ravel() for x in np.meshgrid(c[1:], np.concatenate([border, -border])))
+    g = (10 * to - 9 * old)              # (exact: a few bits each)
+    assert np.array_equal(g, g.astype(np.float32))
+    rows = np.stack([old, g], 1)[: len(old) // 31 * 31].reshape(-1, 31, 2)
+    lead = np.full((len(rows), 1, 2), [448.0, 448.0])      # holds each block's exponent where it is
+    rows = np.concatenate([lead, rows], 1).reshape(-1, 2) * 2.0 ** -20
+    old, g = rows[:, 0], rows[:, 1].astype(np.float32)
+    codes, exps = model.to8(old, False)
+    assert np.array_equal(model.from8(codes, exps), old)
+    dev = lambda x: torch.from_numpy(x.copy()).cuda()   # noqa: E731
+    p, m, me = dev(np.zeros(len(g), np.float32)), dev(codes), dev(exps)
+    v, ve = dev(np.zeros(len(g), np.uint8)), dev(np.zeros(len(exps), np.uint8))
+    M.mtgnn_adamw_step(M.adamw_tensors([p], [dev(g)], [m], [v], m_exp=[me], v_exp=[ve]), 1e-3, 0.9, 0.999, 1e-8, 1)
+    _, wm, wv = model.adamw(np.zeros(len(g)), g, old, np.zeros(len(g)), 1e-3, 0.9, 0.999, 1e-8, 1, 0.0)
+    for got, e, x, root in ((m, me, wm, False), (v, ve, wv, True)):
+        want, we = model.to8(x, root)
+        assert np.array_equal(e.cpu().numpy(), we)
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
 def test_adamw_step_count_on_the_device():
     rs = np.random.RandomState(9)
     p, g = torch.from_numpy(rs.randn(1000).astype(np.float32)).cuda(), torch.from_numpy(rs.randn(1000).astype(np.float32)).cuda()
