@@ -1212,11 +1212,13 @@ struct Tiling {
   int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
 };
 // Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 27 us, 3.8 TB/s, in tiles of 256 x 256 48; for few
-// classes they took as long as small ones), else large ones where there are enough of them for the card.
+// classes they took as long as small ones); else large ones unless the last round of them leaves too much of the card empty: the
+// forward in large and small ones, us, 3,000 x 6,000 x 512 in float32 (288 large tiles) 106 and 91, 4,000 x 9,001 x 512 in
+// bfloat16 (576) 82 and 79, 4,000 x 16,000 x 512 (1,008) 108 and 113, 4,000 x 30,000 x 1,024 (1,888) 269 and 292.
 Tiling tiling(int64_t rows, int64_t cols) {
   if (rows <= 64) return Tiling{64, 256, 1};
-  const Tiling big{256, 256, 1};
-  return big.tiles(rows, cols) >= 192 ? big : Tiling{128, 128, 1};
+  const Tiling big{256, 256, 1}, small{128, 128, 1};
+  return cdiv(big.tiles(rows, cols), 256) * 100 <= cdiv(small.tiles(rows, cols), 512) * 56 ? big : small;
 }
 // Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
 // enough to fill the card with shares of them.  The shares are those that are done first, counted in steps (1.3 to 1.5 us each): rounds of
