@@ -1189,6 +1189,10 @@ class AdamwTensors:
             t.m_exp, t.v_exp = (_table(x, torch.uint8, k, (blocks,), True, dev=dev) for x, k in ((ea, "m_exp"), (eb, "v_exp")))
             t.shadow = _table(sh, torch.bfloat16, "shadow", shape, True, dev=dev)
             t.n, t.decay = size, float(de)
+        written = sorted((x.data_ptr(), x.numel() * x.element_size())
+                         for x in (*params, *m, *v, *lists["shadow"], *lists["m_exp"], *lists["v_exp"]) if x is not None and x.numel())
+        if any(a + size > b for (a, size), (b, _) in zip(written, written[1:])):
+            raise MtgnnError("two of the tensors share memory (a parameter may be listed once)")
         self.tensors, self.device = (list(params), *(list(x) for x in lists.values())), dev
 
 

@@ -534,6 +534,18 @@ def test_adamw_8_bit_sums_on_borders():
         assert np.array_equal(got.cpu().numpy(), want)
 
 
+def test_adamw_refuses_a_tensor_listed_twice():
+    x = [torch.ones(8, device="cuda") for _ in range(7)]
+    M.adamw_tensors(x[:2], [x[6]] * 2, x[2:4], x[4:6])      # (a gradient is only read)
+    with pytest.raises(M.MtgnnError, match="share memory"):
+        M.adamw_tensors([x[0], x[0]], x[6:] * 2, x[2:4], x[4:6])
+    with pytest.raises(M.MtgnnError, match="share memory"):
+        M.adamw_tensors(x[:2], x[6:] * 2, x[2:4], [x[4], x[3]])
+    wide = torch.ones(15, device="cuda")
+    with pytest.raises(M.MtgnnError, match="share memory"):
+        M.adamw_tensors([wide[:8], wide[7:]], x[6:] * 2, x[2:4], x[4:6])
+
+
 def test_adamw_step_count_on_the_device():
     rs = np.random.RandomState(9)
     p, g = torch.from_numpy(rs.randn(1000).astype(np.float32)).cuda(), torch.from_numpy(rs.randn(1000).astype(np.float32)).cuda()
