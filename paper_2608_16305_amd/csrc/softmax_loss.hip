@@ -1079,17 +1079,22 @@ __global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const
 
 // --------------------------------------------------------------------------- rows' sums
 
-// 16 rows a block, 16 threads to each: joins the tiles' (largest, sum) and leaves the row's, its loss, and the block's sum.  (A mean by
-// the last block to be done in the same launch needs a fence of each, which took longer than the launch: 18 us for 9 + 5,
-// 7,373 rows.)
-__global__ __launch_bounds__(256) void k_loss_join(const int32_t* count, const int32_t* idx, const float2* part, int tiles,
-                                                   int64_t ld_part, const float* at_label, float2* stat, float* row_loss,
-                                                   double* sums) {
-  __shared__ float2 s[16][17];
-  __shared__ double l[16];
-  const int64_t n = *count, r = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
-  const int k = threadIdx.x >> 4;
-  if ((int64_t)blockIdx.x * 16 >= n) return;
+// R rows a block, THREADS / R threads to each: joins the tiles' (largest, sum) and leaves the row's, its loss, and the block's sum;
+// of one block the mean too.  (A mean by the last of many blocks to be done in the same launch needs a fence of each, which took
+// longer than the launch: 18 us for 9 + 5, 7,373 rows.)
+template <int R, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_loss_join(const int32_t* count, const int32_t* idx, const float2* part, int tiles,
+                                                       int64_t ld_part, const float* at_label, float2* stat, float* row_loss,
+                                                       double* sums, float* loss) {
+  constexpr int EACH = THREADS / R;
+  __shared__ float2 s[EACH][R + 1];
+  __shared__ double l[R];
+  const int j = threadIdx.x % R, k = threadIdx.x / R;
+  const int64_t n = *count, r = (int64_t)blockIdx.x * R + j;
+  if ((int64_t)blockIdx.x * R >= n) {
+    if (gridDim.x == 1 && threadIdx.x == 0) *loss = 0.f;
+    return;
+  }
   float2 q = make_float2(-INFINITY, 0.f);
   const auto add = [&](float2 o) {
     const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;
@@ -1097,38 +1102,45 @@ __global__ __launch_bounds__(256) void k_loss_join(const int32_t* count, const i
     q.x = m;
   };
   if (r < n)
-    for (int t = k; t < tiles; t += 128) {   // (those past the last one: nothing)
+    for (int t = k; t < tiles; t += 8 * EACH) {   // (those past the last one: nothing)
       float2 o[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) o[u] = t + 16 * u < tiles ? part[(t + 16 * u) * ld_part + r] : make_float2(-INFINITY, 0.f);
+      for (int u = 0; u < 8; ++u) o[u] = t + EACH * u < tiles ? part[(t + EACH * u) * ld_part + r] : make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int u = 0; u < 8; ++u) add(o[u]);
     }
-  s[k][threadIdx.x & 15] = q;
-  __syncthreads();
+  s[k][j] = q;
+  for (int h = EACH / 2; h > 0; h >>= 1) {
+    __syncthreads();
+    if (k < h) {
+      add(s[k + h][j]);
+      s[k][j] = q;
+    }
+  }
   if (k == 0) {
-    for (int j = 1; j < 16; ++j) add(s[j][threadIdx.x]);
-    double loss = 0.0;
+    double v = 0.0;
     if (r < n) {
       // a logit of +inf: the others' exponentials are 0 beside it
       if (q.x == INFINITY) q.y = 1.f;
-      const float v = (q.x - at_label[r]) + logf(q.y);
+      const float f = (q.x - at_label[r]) + logf(q.y);
       stat[r] = make_float2(q.x, 1.f / q.y);
-      if (row_loss) row_loss[idx[r]] = v;
-      loss = v;
+      if (row_loss) row_loss[idx[r]] = f;
+      v = f;
     }
-    l[threadIdx.x] = loss;
+    l[j] = v;
   }
   __syncthreads();
   if (threadIdx.x) return;
   double v = 0.0;
-  for (int j = 0; j < 16; ++j) v += l[j];
-  sums[blockIdx.x] = v;
+  for (int i = 0; i < R; ++i) v += l[i];
+  if (gridDim.x == 1) *loss = (float)(v / (double)n);
+  else sums[blockIdx.x] = v;
 }
 
+constexpr int JOIN = 16;   // rows of a block of k_loss_join where there are several
 __global__ __launch_bounds__(256) void k_loss_mean(const int32_t* count, const double* sums, float* loss) {
   __shared__ double s[256];
-  const int64_t n = *count, blocks = cdiv(n, 16);
+  const int64_t n = *count, blocks = cdiv(n, JOIN);
   double v = 0.0;
   for (int64_t i = threadIdx.x; i < blocks; i += 256) v += sums[i];
   s[threadIdx.x] = v;
@@ -1345,7 +1357,7 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const size_t t = al(2 * (size_t)up(d->n, PAD) * p.dp);   // a part of W
   if (!back)
     return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
-           al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, 16));
+           al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, JOIN));
   if (p.few) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
@@ -1370,7 +1382,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   const int tiles = (int)class_tiles(d, p, max_rows);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
-  double* sums = (double*)take(8 * cdiv(p.Rp, 16));
+  double* sums = (double*)take(8 * cdiv(p.Rp, JOIN));
   uint32_t* share = (uint32_t*)take(8 * MAX_SHARES);
   First f{label, n_rows, max_rows, d->n, d->d, counts, k.largest, share, (unsigned)cdiv(max_rows, CHUNK), 0, 0};
   const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS), tb = p.bf && !p.copy ? 0 : table_blocks(d->n, p);
@@ -1405,8 +1417,17 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     segments(q, 2, 2);
     MTGNN_TRY((product<STAT, true>(q, tl, s)));
   }
-  k_loss_join<<<(unsigned)cdiv(max_rows, 16), 256, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums);
-  MTGNN_CHECK_LAUNCH("loss_join");
+  // The whole forward, us: with 64 threads to a row, not 16, where there are more tiles than those request at once, 33 x 100,003 x 520
+  // (391 tiles) 54 -> 40; with one block, and no launch for the mean, 17 x 9,000 x 100 (141 tiles) 17.4 -> 15.4, but
+  // 14 x 142,281 x 1,024 (2,224 tiles) 130 -> 156.
+  const auto join = [&](auto kernel, int rows, int threads) -> mtgnn_status {
+    kernel<<<(unsigned)cdiv(max_rows, rows), threads, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums, loss);
+    MTGNN_CHECK_LAUNCH("loss_join");
+    return MTGNN_OK;
+  };
+  if (max_rows <= 64 && tiles <= 256) return join(k_loss_join<64, 1024>, 64, 1024);
+  MTGNN_TRY(tiles > 128 ? join(k_loss_join<JOIN, 1024>, JOIN, 1024) : join(k_loss_join<JOIN, 256>, JOIN, 256));
+  if (max_rows <= JOIN) return MTGNN_OK;
   k_loss_mean<<<1, 256, 0, s>>>(k.count, sums, loss);
   MTGNN_CHECK_LAUNCH("loss_mean");
   return MTGNN_OK;
