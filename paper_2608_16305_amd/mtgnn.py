@@ -789,14 +789,14 @@ def _rows(t, dtype, name, rows, cols, optional=False, dev=-1):
         raise MtgnnError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise MtgnnError(f"{name} must be {dtype}, got {t.dtype}")
-    shape, stride = t.shape, t.stride()
+    shape, ld = t.shape, t.stride(0) if t.dim() == 2 else 0
     if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
         raise MtgnnError(f"{name} must be [{rows}, {cols}], got {tuple(shape)}")
-    if (cols > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < cols):
-        raise MtgnnError(f"{name} must have dense rows, got strides {stride}")
+    if (cols > 1 and t.stride(1) != 1) or (shape[0] > 1 and ld < cols):
+        raise MtgnnError(f"{name} must have dense rows, got strides {t.stride()}")
     if t.get_device() != dev:
         _elsewhere(t, name, dev)
-    return C.c_void_p(t.data_ptr()), max(stride[0], cols)
+    return C.c_void_p(t.data_ptr()), max(ld, cols)
 
 
 def _table(t, dtype, name, shape, optional=False, dev=-1):
