@@ -749,8 +749,8 @@ mtgnn_status mtgnn_layer_norm_bwd(const float* dy, int64_t lddy, const void* x, 
  *   save -- mtgnn_softmax_loss_save_bytes bytes for the backward (it keeps a copy of x's rows), or NULL.
  * A row all of whose logits are -inf has the loss NaN; an infinite or NaN element of x or W makes the logits that it enters
  * infinite or NaN.  Logits are exact to float32 (float32 elements within 2^-23 of themselves, or 2^-39 of x's or W's
- * largest where that is more); they are not kept: memory beside the copies of x and W (none of at most
- * 64 rows of float32) grows with max_rows n / 64.
+ * largest where that is more); they are not kept: memory beside the copies of x and W (of W none for few
+ * rows of float32) grows with max_rows n / 64.
  * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too. */
 typedef struct {
   int32_t n, d, dtype;       /* n < 2^31 - 64, d <= 2^20 */

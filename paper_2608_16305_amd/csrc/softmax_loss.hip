@@ -251,12 +251,15 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
   }
 }
 
-// The backward's first launch: dx of the rows without a label (blocks below `blocks`), and of bfloat16 operands the search of W.
+// The backward's first launch: dx of the rows without a label (blocks below `blocks`), and the search of the operands that the
+// forward has not searched.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W) {
+__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W, const T* xc, int dp,
+                                                         const int32_t* count) {
   if (blockIdx.x >= blocks) {
     const unsigned b = blockIdx.x - blocks;
-    const uint32_t top = largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b, f.w_blocks);
+    const uint32_t top = b < f.x_blocks ? largest_share(xc, (int64_t)dp, (int64_t)*count, f.d, nullptr, 0, b, f.x_blocks)
+                                        : largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b - f.x_blocks, f.w_blocks);
     if (threadIdx.x == 0) f.share[b] = top;
     return;
   }
@@ -268,24 +271,23 @@ __global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int
   store_some(dx + r * lddx + c, f.d - c, z);
 }
 
-// Its second: W in float16 parts (blocks below `blocks`), and of bfloat16 operands x's rows.
+// Its second: W in float16 parts (blocks below `blocks`), and x's rows where the forward has left them as they are.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_lay(const T* W, int64_t n, int d, int dp, uint32_t* largest, const uint32_t* share,
-                                                       unsigned shares, uint16_t* table, unsigned blocks, const uint16_t* xc,
-                                                       int64_t Rp, const uint32_t* largest_x, uint16_t* xh) {
+__global__ __launch_bounds__(256) void k_loss_back_lay(First f, const T* W, int dp, uint16_t* table, unsigned blocks, const T* xc, int64_t Rp,
+                                                       uint32_t* topA, uint32_t* topB, uint16_t* xh) {
   constexpr int PARTS = sizeof(T) == 2 ? 1 : 2;
-  if (blockIdx.x >= blocks) {
-    lay_table<uint16_t, 1>(xc, Rp, dp, dp, lift(*largest_x), xh, 0, blockIdx.x - blocks);
-    return;
-  }
+  const bool of_x = blockIdx.x >= blocks;
+  uint32_t* const at = of_x ? topA : topB;
+  const unsigned shares = of_x ? f.x_blocks : f.w_blocks, first = of_x ? blocks : 0;
   uint32_t top;
-  if (PARTS == 1) {
-    top = largest_of(share, (int)shares);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = top;
+  if (shares) {
+    top = largest_of(f.share + (of_x ? 0 : f.x_blocks), (int)shares);
+    if (blockIdx.x == first && threadIdx.x == 0) *at = top;
   } else {
-    top = *largest;
+    top = *at;
   }
-  lay_table<T, PARTS>(W, n, d, dp, lift(top), table, up(n, PAD) * dp, blockIdx.x);
+  if (of_x) lay_table<T, PARTS>(xc, Rp, dp, dp, lift(top), xh, Rp * dp, blockIdx.x - first);
+  else lay_table<T, PARTS>(W, f.n, f.d, dp, lift(top), table, up(f.n, PAD) * dp, blockIdx.x);
 }
 
 // --------------------------------------------------------------------------- the products
@@ -718,9 +720,9 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
 
 // --------------------------------------------------------------------------- few rows of float32
 
-// At most 64 rows of float32.  For so few every product is reading W or writing dW, and W is read as it is, on the float32 matrix
-// instructions (256 operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in
-// float16 parts it is searched, laid out and read (14 x 142,281 x 1,024 forward 592 us for 143).  A block has 64 CF classes; a
+// For few rows every product is reading W or writing dW.  Those of float32 take W as it is, on the float32 matrix instructions (256
+// operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in float16 parts it is
+// searched, laid out and read (14 x 142,281 x 1,024 forward 592 us for 130).  A block has 64 CF classes and up to 64 rows; a
 // lane reads 16 bytes of a class at a k four apart from its neighbours', and x, through LDS, in the same order, so that the
 // fragments need no more than that.  The forward leaves what STAT does, and x's rows with a label as they are; the backward
 // forms the logits again, leaves P times LIFT [classes][16 RF] for dx, and writes db and, from P and x in LDS, dW.
@@ -739,36 +741,45 @@ struct Few {
   const float2* stat;       // backward
   const float* dloss;
   float *P, *db, *dW;       // each or NULL
+  int groups;               // of 64 rows: blocks that follow each other have a tile's
 };
-constexpr int FEW = 64, KC = 64, LDC = KC + 4;
+constexpr int FEW = 256, KC = 64, LDC = KC + 4;
 template <int RF, int CF, bool BACK>
 __global__ __launch_bounds__(256) void k_loss_few(Few p) {
   __shared__ __align__(16) float xs[2][16 * RF][LDC];
   __shared__ __align__(16) float ps[BACK ? 64 * CF : 1][16 * RF + 4], out[BACK ? 4 : 1][16][LDC];
-  __shared__ int src[FEW], lab[FEW];
+  __shared__ int src[16 * RF], lab[16 * RF], in_wave[4];
   __shared__ float2 st[4][16 * RF];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fg = lane >> 4;
-  int count;
+  const int tile = blockIdx.x / p.groups, group = blockIdx.x % p.groups, r0 = group * 16 * RF;
+  int all = 0;
   if constexpr (BACK) {
-    count = *p.count;
-    if (wid == 0 && lane < count) lab[lane] = p.lab[lane];
+    all = *p.count;
+    if (threadIdx.x < all) lab[threadIdx.x] = p.lab[threadIdx.x];
   } else {
     const int64_t rows = eff_count(p.max_rows, p.n_rows);
-    const bool ok = has_label(p.label, lane, rows, p.n);
+    const int t = threadIdx.x;
+    const bool ok = has_label(p.label, t, rows, p.n);
     const uint64_t have = __ballot(ok);
-    count = __popcll(have);
-    if (wid == 0) {
-      const int at = __popcll(have & ((uint64_t(1) << lane) - 1));
-      if (ok) src[at] = lane, lab[at] = p.label[lane];
-      if (blockIdx.x == 0) {
-        if (lane == 0) *p.count = count;
-        if (ok) p.idx[at] = lane, p.lab[at] = p.label[lane];
-        else if (lane < rows && p.row_loss) p.row_loss[lane] = 0.f;
-      }
+    if (lane == 0) in_wave[wid] = __popcll(have);
+    __syncthreads();
+    int at = __popcll(have & ((uint64_t(1) << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      at += w < wid ? in_wave[w] : 0;
+      all += in_wave[w];
+    }
+    const int here = at - r0;
+    if (ok && here >= 0 && here < 16 * RF) src[here] = t, lab[here] = p.label[t];
+    if (blockIdx.x == 0) {
+      if (t == 0) *p.count = all;
+      if (ok) p.idx[at] = t, p.lab[at] = p.label[t];
+      else if (t < rows && p.row_loss) p.row_loss[t] = 0.f;
     }
   }
-  const int c0 = (int)blockIdx.x * 64 * CF + wid * 16 * CF, steps = (int)cdiv(p.d, KC);
-  if (!BACK && count == 0) return;
+  const int c0 = tile * 64 * CF + wid * 16 * CF, steps = (int)cdiv(p.d, KC);
+  const int count = min(all - r0, 16 * RF);   // rows of the group
+  if (!BACK && count <= 0) return;
   __syncthreads();
 
   const float* w[CF];
@@ -818,9 +829,9 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) now[j][t][e] = wv[j][t][e];
     put_x(xb);
-    if (!BACK && p.xc && blockIdx.x == 0) {
+    if (!BACK && p.xc && tile == 0) {
 #pragma unroll
-      for (int u = 0; u < RF; ++u) *(float4*)(p.xc + (int64_t)(16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
+      for (int u = 0; u < RF; ++u) *(float4*)(p.xc + (int64_t)(r0 + 16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
     }
     if (step + 1 < steps) load((step + 1) * KC);
     __syncthreads();   // (every wave has read what the step before last left here)
@@ -859,7 +870,7 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
           const int c = c0 + 16 * j + 4 * fg + e;
           const float l = c < p.n ? acc[i][j][e] + bias[j][e] : -INFINITY;
           acc[i][j][e] = l;
-          if (c == at) p.at_label[r] = l;
+          if (c == at) p.at_label[r0 + r] = l;
           m = fmaxf(m, l);
         }
       m = fmaxf(m, __shfl_xor(m, 16, 64));
@@ -875,11 +886,11 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
     }
     __syncthreads();
     const int r = threadIdx.x;
-    if (r >= min(count, 16 * RF)) return;
+    if (r >= count) return;
     float2 q = st[0][r];
 #pragma unroll
     for (int k = 1; k < 4; ++k) join(q, st[k][r]);
-    p.part[blockIdx.x * p.ld_part + r] = q;
+    p.part[tile * p.ld_part + r0 + r] = q;
   } else {
     const float scale = loss_scale(count, p.dloss) / LIFT;
     float sum[CF][4];
@@ -1182,16 +1193,24 @@ int64_t stride(int64_t width) { return up(width, PAD) | PAD; }
 
 struct Plan {
   bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes)
-  bool few;                  // float32 operands of so few rows that the forward reads W itself
+  bool few, few_back;        // float32 operands of so few rows that the forward, and the backward too, read W as it is
   int dp;                    // padded width
   int64_t Rp, width;         // padded rows; classes of a piece
 };
+// Rows of float32 that k_loss_few's forward takes: up to 128, or 256 where its blocks are all on the card at once (three a CU).  The
+// forward in float16 parts and by it, us: 92 x 48,988 x 1,024 186 and 136, 128 x 30,000 x 512 65 and 65; 200 x 9,000 x 100 26 and
+// 22, 250 x 3,000 x 1,024 57 and 38; 250 x 16,000 x 1,024 (1,000 blocks) 81 and 101.  The backward by it takes up to 64: 92 x
+// 48,988 x 1,024 312 and 507.
+bool few_rows(const mtgnn_loss_dims* d, int64_t rows) {
+  return rows <= 128 || (rows <= FEW && cdiv(d->n, 64) * cdiv(rows, 64) <= 768);
+}
 Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
   Plan p;
   p.bf = d->dtype == MTGNN_BF16;
   p.dp = (int)stride(d->d);
   p.copy = p.bf && d->d % 8 != 0;
-  p.few = !p.bf && rows <= FEW;
+  p.few = !p.bf && few_rows(d, rows);
+  p.few_back = p.few && rows <= 64;
   p.Rp = up(rows, PAD);
   const int64_t most = (int64_t)(PIECE / (4 * (size_t)p.Rp)) / 256 * 256;
   p.width = std::min<int64_t>(up(d->n, PAD), std::max<int64_t>(256, most));
@@ -1312,21 +1331,32 @@ mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s
   MTGNN_TRY((product<KIND, true>(q, t, s)));
   return join_shares(p, t.split, part, s);
 }
-template <bool BACK>
 mtgnn_status few(const Few& p, int tc, hipStream_t s) {
   const int rf = row_frags(p.max_rows);
-  const unsigned grid = (unsigned)cdiv(p.n, tc);
+  const unsigned grid = (unsigned)(cdiv(p.n, tc) * p.groups);
   {
-    TimedScope ts(site::Generic::name, s), kind(BACK ? "loss_prob" : "loss_stat", s);
-    if (!BACK && tc == 128) {
+    TimedScope ts(site::Generic::name, s), kind("loss_stat", s);
+    if (tc == 128) {
       if (rf == 4) k_loss_few<4, 2, false><<<grid, 256, 0, s>>>(p);
       else if (rf == 2) k_loss_few<2, 2, false><<<grid, 256, 0, s>>>(p);
       else k_loss_few<1, 2, false><<<grid, 256, 0, s>>>(p);
-    } else if (rf == 4) k_loss_few<4, 1, BACK><<<grid, 256, 0, s>>>(p);
-    else if (rf == 2) k_loss_few<2, 1, BACK><<<grid, 256, 0, s>>>(p);
-    else k_loss_few<1, 1, BACK><<<grid, 256, 0, s>>>(p);
+    } else if (rf == 4) k_loss_few<4, 1, false><<<grid, 256, 0, s>>>(p);
+    else if (rf == 2) k_loss_few<2, 1, false><<<grid, 256, 0, s>>>(p);
+    else k_loss_few<1, 1, false><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_few");
+  return MTGNN_OK;
+}
+mtgnn_status few_back(const Few& p, hipStream_t s) {
+  const int rf = row_frags(p.max_rows);
+  const unsigned grid = (unsigned)cdiv(p.n, 64);
+  {
+    TimedScope ts(site::Generic::name, s), kind("loss_prob", s);
+    if (rf == 4) k_loss_few<4, 1, true><<<grid, 256, 0, s>>>(p);
+    else if (rf == 2) k_loss_few<2, 1, true><<<grid, 256, 0, s>>>(p);
+    else k_loss_few<1, 1, true><<<grid, 256, 0, s>>>(p);
+  }
+  MTGNN_CHECK_LAUNCH("loss_few_back");
   return MTGNN_OK;
 }
 
@@ -1358,10 +1388,11 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   if (!back)
     return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
            al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, JOIN));
-  if (p.few) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
+  if (p.few_back) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
-  return 256 + al(4 * MAX_SHARES) + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t) + al(4 * (size_t)p.Rp * stride(p.width)) +
+  return 256 + al(8 * MAX_SHARES) + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t + (p.few ? al(4 * (size_t)p.Rp * p.dp) : 0)) +
+         al(4 * (size_t)p.Rp * stride(p.width)) +
          al(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width)) + al(part);
 }
 
@@ -1408,7 +1439,8 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     f.label = label; f.n_rows = n_rows; f.max_rows = max_rows; f.n = d->n; f.d = d->d;
     f.count = k.count; f.idx = k.idx; f.lab = k.lab; f.xc = save ? (float*)k.xc : nullptr; f.dp = p.dp;
     f.part = part; f.ld_part = p.Rp; f.at_label = at_label; f.row_loss = row_loss;
-    MTGNN_TRY(few<false>(f, few_classes(d), s));
+    f.groups = (int)cdiv(max_rows, 64);
+    MTGNN_TRY(few(f, few_classes(d), s));
   } else if (p.bf) {
     if (!p.copy) q.B = (const uint16_t*)W, q.ldb = q.dimB = d->d;
     segments(q, 1, 1);
@@ -1444,18 +1476,19 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     w += al(bytes);
     return at;
   };
-  if (p.few) {
+  if (p.few_back) {
     const int rf = row_frags(max_rows), per = few_per(d);
     float* P = (float*)take(4 * (size_t)d->n * 16 * rf);
     Few f{};
     f.W = (const float*)W; f.b = b; f.max_rows = max_rows; f.n = d->n; f.d = d->d;
     f.count = k.count; f.idx = k.idx; f.lab = k.lab; f.xc = (float*)k.xc; f.dp = p.dp;
     f.stat = k.stat; f.dloss = dloss; f.P = dx ? P : nullptr; f.db = db; f.dW = dW;
-    MTGNN_TRY(few<true>(f, 64, s));
+    f.groups = 1;
+    MTGNN_TRY(few_back(f, s));
     if (!dx) return MTGNN_OK;
     First none{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, nullptr, 0, 0, 0};
     const unsigned zb = (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256);
-    k_loss_back_first<float><<<zb, 256, 0, s>>>(none, dx, lddx, zb, nullptr);
+    k_loss_back_first<float><<<zb, 256, 0, s>>>(none, dx, lddx, zb, nullptr, nullptr, 0, nullptr);
     MTGNN_CHECK_LAUNCH("loss_back_first");
     Prod r{};
     r.rows = max_rows; r.cols = d->d; r.count = k.count; r.idx = k.idx; r.dloss = dloss; r.out = dx; r.ldo = lddx;
@@ -1469,23 +1502,25 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     MTGNN_CHECK_LAUNCH("loss_few_dx");
     return join_shares(r, (int)grid.y, (float*)w, s);
   }
-  uint32_t* top = (uint32_t*)take(4);
-  uint32_t* share = (uint32_t*)take(4 * MAX_SHARES);
+  uint32_t* top = (uint32_t*)take(8);   // of x, of W, where they are searched here
+  uint32_t* share = (uint32_t*)take(8 * MAX_SHARES);
   const int64_t plane = up(d->n, PAD) * p.dp, planeX = p.Rp * p.dp;
   uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
-  uint16_t* xh = p.bf ? (uint16_t*)take(2 * (size_t)planeX) : k.xc;
+  const bool lay_x = p.bf || p.few;
+  uint16_t* xh = lay_x ? (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * planeX) : k.xc;
   uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * stride(p.width));
   float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width));
   float* part = (float*)w;
-  // (the sizes a float32 W was searched for are the forward's)
-  if (!p.bf) top = k.largest + 1;
-  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, 0, p.bf ? search_blocks(d->n, d->d) : 0};
+  // (the sizes that the forward has searched operands for are kept: a bfloat16 x's, both of what it laid out in parts)
+  uint32_t* const topA = p.few ? top : k.largest;
+  uint32_t* const topB = lay_x ? top + 1 : k.largest + 1;
+  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, p.few ? search_blocks(max_rows, d->d) : 0, lay_x ? search_blocks(d->n, d->d) : 0};
   const unsigned zb = dx ? (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256) : 0, tb = table_blocks(d->n, p);
   const auto lay = [&](auto* Wt) -> mtgnn_status {
-    if (zb + f.w_blocks > 0) k_loss_back_first<<<zb + f.w_blocks, 256, 0, s>>>(f, dx, lddx, zb, Wt);
+    const unsigned grid = zb + f.x_blocks + f.w_blocks;
+    if (grid > 0) k_loss_back_first<<<grid, 256, 0, s>>>(f, dx, lddx, zb, Wt, (decltype(Wt))k.xc, p.dp, k.count);
     MTGNN_CHECK_LAUNCH("loss_back_first");
-    k_loss_back_lay<<<tb + (p.bf ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(Wt, d->n, d->d, p.dp, top, share, f.w_blocks, tbl, tb, k.xc,
-                                                                            p.Rp, k.largest, xh);
+    k_loss_back_lay<<<tb + (lay_x ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(f, Wt, p.dp, tbl, tb, (decltype(Wt))k.xc, p.Rp, topA, topB, xh);
     MTGNN_CHECK_LAUNCH("loss_back_lay");
     return MTGNN_OK;
   };
@@ -1495,8 +1530,8 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     const Shares sh = shares_of(d, p, max_rows, cols);
     const Tiling tl = tiling(max_rows, cols);
     Prod q{};
-    q.A = xh; q.lda = q.dimA = p.dp; q.planeA = planeX; q.topA = k.largest;
-    q.B = tbl + c * p.dp; q.ldb = q.dimB = p.dp; q.planeB = plane; q.topB = top;
+    q.A = xh; q.lda = q.dimA = p.dp; q.planeA = planeX; q.topA = topA;
+    q.B = tbl + c * p.dp; q.ldb = q.dimB = p.dp; q.planeB = plane; q.topB = topB;
     q.rows = max_rows; q.cols = cols; q.K = up(d->d, KS); q.count = k.count;
     q.b = b ? b + c : nullptr; q.lab = k.lab; q.c0 = c; q.stat = k.stat;
     q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp;
@@ -1520,13 +1555,13 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     segments(g, 2, p.bf ? 1 : 2);
     if (dx) {
       Prod r = g;
-      r.B = tbl + c * p.dp; r.ldb = r.dimB = p.dp; r.planeB = plane; r.topB = top;
+      r.B = tbl + c * p.dp; r.ldb = r.dimB = p.dp; r.planeB = plane; r.topB = topB;
       r.rows = max_rows; r.K = cols; r.idx = k.idx; r.out = dx; r.ldo = lddx; r.add = c > 0;
       MTGNN_TRY((gradient<DX>(r, sh.dx, part, s)));
     }
     if (dW) {
       Prod r = g;
-      r.B = xh; r.ldb = r.dimB = p.dp; r.planeB = planeX; r.topA = k.largest;
+      r.B = xh; r.ldb = r.dimB = p.dp; r.planeB = planeX; r.topA = topA;
       r.rows = cols; r.out = dW + c * d->d; r.ldo = d->d;
       MTGNN_TRY((gradient<DW>(r, sh.dw, part, s)));
     }

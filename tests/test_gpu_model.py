@@ -242,6 +242,9 @@ LOSS = [  # rows, pad, n, d, bias, share without a label, wide, dloss
     (9000, 0, 5, 33, True, 0.1, True, 0.25),
     (5, 3, 9, 12, True, 1.0, False, None),
     (33, 5, 65, 130, True, 0.2, True, None),
+    (100, 0, 70, 33, True, 1.0, False, None),
+    (256, 0, 500, 129, True, 0.0, True, None),
+    (250, 6, 33, 68, False, 0.6, False, -1.0),
     (64, 0, 33000, 100, True, 0.0, False, 2.0),
     (20, 0, 40000, 65, False, 0.1, True, None),
 ]
