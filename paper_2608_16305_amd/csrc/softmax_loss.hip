@@ -175,7 +175,7 @@ __device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, 
   if (c < up(n, PAD)) put_parts<T, PARTS>(W + c * d, u, c < n ? d : 0, by, to + c * dp + u, plane);   // (zeros behind the last)
 }
 
-// The forward's second launch.  Blocks below `blocks`: the rows with a label, one after the other: idx (which rows), lab, xc (their x,
+// The forward's second launch (counts NULL: its only one, of so few rows that each block counts them).  Blocks below `blocks`: the rows with a label, one after the other: idx (which rows), lab, xc (their x,
 // as it is or in parts; zeros behind the last one to a whole step); their number; of bfloat16 x its largest element.  The last of
 // them, past those of the rows, fill in the zeros.  The other blocks: W in parts, or padded.
 template <typename T>
@@ -201,9 +201,8 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
   const bool behind = r0 >= max_rows;
   const int mine = behind ? chunks : (int)(r0 / CHUNK);
   int v = 0;
-  for (int i = threadIdx.x; i < mine; i += 256) v += counts[i];
-  if (!behind)
-    for (int64_t r = (int64_t)mine * CHUNK + threadIdx.x; r < r0; r += 256) v += has_label(label, r, rows, n);
+  for (int i = threadIdx.x; counts && i < mine; i += 256) v += counts[i];
+  for (int64_t r = (counts ? (int64_t)mine * CHUNK : 0) + threadIdx.x; r < min(r0, max_rows); r += 256) v += has_label(label, r, rows, n);
   const int first = block_sum(v, s);
   if (behind) {
     const int j0 = (int)(r0 - up(max_rows, ROWS));
@@ -247,7 +246,7 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
   }
   if (PARTS == 0) {
     top = block_largest(top);
-    if (threadIdx.x == 0 && top) atomicMax(largest, top);   // (a maximum does not depend on the order)
+    if (threadIdx.x == 0 && top && largest) atomicMax(largest, top);   // (a maximum does not depend on the order)
   }
 }
 
@@ -1419,10 +1418,12 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS), tb = p.bf && !p.copy ? 0 : table_blocks(d->n, p);
   const auto lay = [&](auto* xt, auto* Wt) -> mtgnn_status {
     if (!p.bf) f.x_blocks = search_blocks(max_rows, d->d), f.w_blocks = search_blocks(d->n, d->d);
-    k_loss_first<<<f.chunks + f.x_blocks + f.w_blocks, 256, 0, s>>>(f, xt, ldx, Wt);
+    // (a bfloat16 x's largest element is the backward's)
+    const bool alone = p.bf && !save && max_rows <= CHUNK;
+    if (!alone) k_loss_first<<<f.chunks + f.x_blocks + f.w_blocks, 256, 0, s>>>(f, xt, ldx, Wt);
     MTGNN_CHECK_LAUNCH("loss_first");
-    k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, counts, k.count, k.idx, k.lab, k.xc,
-                                           p.Rp * p.dp, k.largest, share, f.x_blocks, f.w_blocks, row_loss, blocks, Wt, tbl);
+    k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, alone ? nullptr : counts, k.count, k.idx, k.lab,
+                                           k.xc, p.Rp * p.dp, alone ? nullptr : k.largest, share, f.x_blocks, f.w_blocks, row_loss, blocks, Wt, tbl);
     MTGNN_CHECK_LAUNCH("loss_lay");
     return MTGNN_OK;
   };
