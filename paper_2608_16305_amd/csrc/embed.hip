@@ -6,7 +6,7 @@
 // in their order (no float atomics: the result does not depend on scheduling).  The rows are put in the order of their ids first,
 // which moves eight bytes of a row of d: one or two passes, each a histogram of tiles and a scatter that keeps the rows' order
 // within a digit of up to 13 bits, so two launches a pass where a sort by 8-bit digits takes three, and no rule by which many rows
-// of one id would fall to one block.  Ids with more than LIGHT rows are summed in runs that other threads work on at the same time.
+// of one id would fall to one block.  Ids with many rows are summed in runs that other threads work on at the same time.
 #include <algorithm>
 
 #include "ops.h"
@@ -17,39 +17,26 @@ namespace mtgnn {
 namespace {
 
 constexpr int NT = 256;
-constexpr int LIGHT = 16;   // rows that one thread sums (per column): of an id, of a run of one with more
 constexpr int IDS = 4;      // ids that a thread sums
 
-// U elements of 16 bytes a thread, requested together.
-template <typename T, int U>
+// 16 bytes a thread (four a thread, requested together, took as long: 17 us for 32,768 rows of 1,024 in bfloat16, 7.9 TB/s, some of it
+// from the caches).
+template <typename T>
 __global__ __launch_bounds__(NT) void k_embed(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const T* table,
                                               int64_t n, int d, float scale, T* y, int64_t ldy) {
   constexpr int V = 16 / sizeof(T);
-  const uint32_t dv = (uint32_t)cdiv(d, V), e0 = blockIdx.x * (U * NT) + threadIdx.x;
-  const int64_t rows = eff_count(max_rows, n_rows);
-  int64_t r[U], id[U];
-  int c[U];
-  float v[U][V];
+  const uint32_t dv = (uint32_t)cdiv(d, V), e = blockIdx.x * NT + threadIdx.x;
+  const int64_t r = e / dv;
+  const int c = (int)(e % dv) * V;
+  if (r >= eff_count(max_rows, n_rows)) return;
+  const int64_t id = ids[r];
+  float v[V];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t e = e0 + u * NT;
-    r[u] = e / dv;
-    c[u] = (int)(e % dv) * V;
-    id[u] = r[u] < rows ? ids[r[u]] : -1;
-  }
+  for (int i = 0; i < V; ++i) v[i] = 0.f;
+  if (id >= 0 && id < n) load_some(table + id * d + c, d - c, v);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[u][i] = 0.f;
-    if (id[u] >= 0 && id[u] < n) load_some(table + id[u] * d + c[u], d - c[u], v[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (r[u] >= rows) continue;
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[u][i] *= scale;
-    store_some(y + r[u] * ldy + c[u], d - c[u], v[u]);
-  }
+  for (int i = 0; i < V; ++i) v[i] *= scale;
+  store_some(y + r * ldy + c, d - c, v);
 }
 
 // --------------------------------------------------------------------------- rows in the order of their ids
@@ -61,6 +48,7 @@ constexpr int MANY = 64;     // ids of a block whose runs all of its threads lis
 struct Groups {
   int64_t rows, n, per;      // rows, ids, rows of a tile (a block of the passes)
   int tiles, low;            // low: bits of an id that the first of two passes sorts by (0: one pass)
+  int light;                 // rows that one thread sums (per column): of an id, of a run of one with more
   int32_t* hist;             // [tiles][digits]
   int32_t *first, *firsts;   // [digits + 1] first position of each digit of the last pass; the same of the first one
   uint32_t *id[2], *row[2];  // id and row of each position after a pass
@@ -185,7 +173,7 @@ __global__ __launch_bounds__(ST) void k_embed_scatter(Groups g, Pass p) {
   }
 }
 
-// Every id's first position (a search among those that share its high digit), and the runs of those with more than LIGHT rows.
+// Every id's first position (a search among those that share its high digit), and the runs of those with more than `light` rows.
 __global__ __launch_bounds__(NT) void k_embed_bounds(Groups g, const uint32_t* key) {
   __shared__ int s[NT / 64], base[2], many[MANY][3], n_many;
   const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
@@ -201,7 +189,7 @@ __global__ __launch_bounds__(NT) void k_embed_bounds(Groups g, const uint32_t* k
   int from = 0, count = 0;
   if (i <= g.n) g.off[i] = from = i < g.n ? first_of(i) : g.first[(g.n - 1 >> g.low) + 1];
   if (i < g.n) count = (i + 1 < g.n ? first_of(i + 1) : g.first[(g.n - 1 >> g.low) + 1]) - from;
-  const int runs = count > LIGHT ? (int)cdiv(count, LIGHT) : 0;
+  const int light = g.light, runs = count > light ? (count + light - 1) / light : 0;
   int all, all_runs;
   const int h = block_exclusive<NT>(runs > 0, all, s), f = block_exclusive<NT>(runs, all_runs, s);
   if (all == 0) return;
@@ -224,16 +212,16 @@ __global__ __launch_bounds__(NT) void k_embed_bounds(Groups g, const uint32_t* k
       many[q][2] = count;
     } else {
       for (int k = 0; k < runs; ++k) {
-        g.run[2 * (base[0] + f + k)] = from + k * LIGHT;
-        g.run[2 * (base[0] + f + k) + 1] = from + min(count, (k + 1) * LIGHT);
+        g.run[2 * (base[0] + f + k)] = from + k * light;
+        g.run[2 * (base[0] + f + k) + 1] = from + min(count, (k + 1) * light);
       }
     }
   }
   __syncthreads();
   for (int q = 0; q < min(n_many, MANY); ++q)
-    for (int k = threadIdx.x; k * LIGHT < many[q][2]; k += NT) {
-      g.run[2 * (many[q][0] + k)] = many[q][1] + k * LIGHT;
-      g.run[2 * (many[q][0] + k) + 1] = many[q][1] + min(many[q][2], (k + 1) * LIGHT);
+    for (int k = threadIdx.x; k * light < many[q][2]; k += NT) {
+      g.run[2 * (many[q][0] + k)] = many[q][1] + k * light;
+      g.run[2 * (many[q][0] + k) + 1] = many[q][1] + min(many[q][2], (k + 1) * light);
     }
 }
 
@@ -255,7 +243,7 @@ __device__ __forceinline__ void add_rows(float (&s)[4], const uint32_t* row, int
   }
 }
 
-// Four columns of IDS neighbouring ids (those with at most LIGHT rows), or of a run: blocks from id_blocks on.  An id's first two
+// Four columns of IDS neighbouring ids (those with at most `light` rows), or of a run: blocks from id_blocks on.  An id's first two
 // rows are requested for all of them together.
 __global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const uint32_t* row, const float* dy, int64_t lddy, int d, float scale, int64_t id_blocks,
                                                   float* dtable) {
@@ -294,7 +282,7 @@ __global__ __launch_bounds__(NT) void k_embed_sum(Groups g, const uint32_t* row,
 #pragma unroll
   for (int u = 0; u < IDS; ++u) {
     const int count = off[u + 1] - off[u];
-    if (id + u >= g.n || count > LIGHT) continue;
+    if (id + u >= g.n || count > g.light) continue;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -337,8 +325,11 @@ __global__ __launch_bounds__(NT) void k_embed_join(Groups g, int d, float scale,
 }
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
-int64_t most_heavy(int64_t rows) { return rows / (LIGHT + 1); }
-int64_t most_runs(int64_t rows) { return rows / LIGHT + most_heavy(rows); }
+// Shorter runs where there is little work for threads to share: 16 and 32, us, with the forward, 8,000 rows of 100,000 x 100 in float32 43.9
+// and 46.6, 32,768 of 50,000 x 1,024 in bfloat16 143 and 138, 200,000 of 9,000 x 200 126 and 112 (64: 143 and 111).
+int light_rows(int64_t rows, int d) { return rows * cdiv(d, 4) >= int64_t(1) << 20 ? 32 : 16; }
+int64_t most_heavy(int64_t rows, int d) { return rows / (light_rows(rows, d) + 1); }
+int64_t most_runs(int64_t rows, int d) { return rows / light_rows(rows, d) + most_heavy(rows, d); }
 
 // One pass where every id can be a digit, else two of about half of an id's bits.
 void lay_out(Groups& g, int64_t rows, int64_t n) {
@@ -365,9 +356,10 @@ size_t place(Groups& g, int d, char* w) {
   }
   g.off = (int32_t*)take(4 * (g.n + 1));
   g.counts = (int32_t*)take(8);
-  g.run = (int32_t*)take(8 * most_runs(g.rows));
-  g.heavy = (int32_t*)take(12 * most_heavy(g.rows));
-  g.part = (float*)take(4 * most_runs(g.rows) * d);
+  g.light = light_rows(g.rows, d);
+  g.run = (int32_t*)take(8 * most_runs(g.rows, d));
+  g.heavy = (int32_t*)take(12 * most_heavy(g.rows, d));
+  g.part = (float*)take(4 * most_runs(g.rows, d) * d);
   return (size_t)(w - start);
 }
 
@@ -375,10 +367,10 @@ size_t place(Groups& g, int d, char* w) {
 
 bool embed_fits(const mtgnn_embedding_dims* d, int64_t rows, bool back) {
   constexpr int64_t MAX = (int64_t(1) << 32) - 2 * NT;
-  if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX - 4 * NT;
+  if (!back) return rows * cdiv(d->d, d->dtype == MTGNN_BF16 ? 8 : 4) <= MAX;
   const int64_t dv = cdiv(d->d, 4);
-  return d->n <= (int64_t)MAX_DIGITS * MAX_DIGITS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows) * dv <= MAX &&
-         most_heavy(rows) * cdiv(d->d, 64) * NT <= MAX;
+  return d->n <= (int64_t)MAX_DIGITS * MAX_DIGITS && cdiv(cdiv(d->n, IDS) * dv, NT) * NT + most_runs(rows, d->d) * dv <= MAX &&
+         most_heavy(rows, d->d) * cdiv(d->d, 64) * NT <= MAX;
 }
 
 size_t embed_ws(const mtgnn_embedding_dims* d, int64_t rows) {
@@ -391,11 +383,7 @@ template <typename T>
 mtgnn_status embed_t(const int32_t* ids, const int32_t* n_rows, int64_t max_rows, const T* table, const mtgnn_embedding_dims* d,
                      T* y, int64_t ldy, hipStream_t s) {
   const int64_t items = max_rows * cdiv(d->d, 16 / (int)sizeof(T));
-  // four elements a thread where that leaves eight blocks a CU
-  if (items >= int64_t(4) * NT * 2048)
-    k_embed<T, 4><<<(unsigned)cdiv(items, 4 * NT), NT, 0, s>>>(ids, n_rows, max_rows, table, d->n, d->d, d->scale, y, ldy);
-  else
-    k_embed<T, 1><<<(unsigned)cdiv(items, NT), NT, 0, s>>>(ids, n_rows, max_rows, table, d->n, d->d, d->scale, y, ldy);
+  k_embed<T><<<(unsigned)cdiv(items, NT), NT, 0, s>>>(ids, n_rows, max_rows, table, d->n, d->d, d->scale, y, ldy);
   MTGNN_CHECK_LAUNCH("embed");
   return MTGNN_OK;
 }
@@ -429,11 +417,11 @@ mtgnn_status embed_bwd_impl(const int32_t* ids, const int32_t* n_rows, int64_t m
   k_embed_bounds<<<(unsigned)cdiv(d->n + 1, NT), NT, 0, s>>>(g, g.id[last]);
   MTGNN_CHECK_LAUNCH("embed_bounds");
   const int64_t dv = cdiv(d->d, 4), id_blocks = cdiv(cdiv(d->n, IDS) * dv, NT);
-  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows) * dv, NT)), NT, 0, s>>>(g, g.row[last], dy, lddy, d->d, d->scale, id_blocks,
+  k_embed_sum<<<(unsigned)(id_blocks + cdiv(most_runs(max_rows, d->d) * dv, NT)), NT, 0, s>>>(g, g.row[last], dy, lddy, d->d, d->scale, id_blocks,
                                                                                          dtable);
   MTGNN_CHECK_LAUNCH("embed_sum");
-  if (most_heavy(max_rows) > 0) {
-    k_embed_join<<<(unsigned)(most_heavy(max_rows) * cdiv(d->d, 64)), NT, 0, s>>>(g, d->d, d->scale, dtable);
+  if (most_heavy(max_rows, d->d) > 0) {
+    k_embed_join<<<(unsigned)(most_heavy(max_rows, d->d) * cdiv(d->d, 64)), NT, 0, s>>>(g, d->d, d->scale, dtable);
     MTGNN_CHECK_LAUNCH("embed_join");
   }
   return MTGNN_OK;

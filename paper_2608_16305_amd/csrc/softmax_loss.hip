@@ -7,7 +7,7 @@
 // two products with W and x take it from there.  So 8 rows x classes x width operations are done where 6 are needed, and a
 // piece of P, not all of it, is in memory.
 //
-// All products run on the 16-bit matrix instructions with float32 sums.  Logits of bfloat16 x and W are formed from them as
+// All products but those of few rows of float32 (k_loss_few) run on the 16-bit matrix instructions with float32 sums.  Logits of bfloat16 x and W are formed from them as
 // they are.  Everything else enters as float16 parts, which have 11 bits each: float32 x and W as two (within 2^-23 of an
 // element; six bfloat16 products of three parts each would take twice the time), in three products for one of theirs, without
 // that of the second parts, 2^-22 at most; bfloat16 ones, for the gradients, as one, which holds their 8 bits; P, times 2^14,

@@ -91,6 +91,7 @@ EMBED = [  # rows, pad, n, d, scale, ids (how many different), share that is no 
     (9000, 0, 1025, 260, 1.0, 5, 0.01, False),
     (20000, 0, 9001, 3, 1.0, 2, 0.0, False),
     (30000, 11, 8192, 9, 1.0, 1, 0.0, True),
+    (17000, 3, 3000, 260, 0.5, 700, 0.01, True),
 ]
 
 
