@@ -1250,26 +1250,27 @@ Tiling tiling(int64_t rows, int64_t cols) {
   const Tiling big{256, 256, 1}, small{128, 128, 1};
   return cdiv(big.tiles(rows, cols), 256) * 100 <= cdiv(small.tiles(rows, cols), 512) * 56 ? big : small;
 }
-// Of a gradient, with sums of `steps` steps.  Large tiles where they cover little more than the small ones would and sums are long
-// enough to fill the card with shares of them.  The shares are those that are done first, counted in steps (1.3 to 1.5 us each): rounds of
-// blocks, each with 6 steps beside its own, and the shares' way to memory and back, with a launch.
+// Of a gradient, with sums of `steps` steps: the tiles and shares that are done first, in us: rounds of blocks, a step of 1.53 in large
+// tiles and 1 in small ones, two of which a compute unit has, 6 steps a block beside its own, and the shares' way to memory and
+// back, with a launch.  (Gradients and logits, us, in small tiles alone, large ones alone and as chosen here: 4,000 x 9,001 x 100
+// in float32 249, 284, 249; 8,192 x 32,768 x 1,024 in bfloat16 3,444, 3,077, 3,047; 1,000 x 30,000 x 1,024 488, 459, 459.)
 Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
-  Tiling g{256, 256, 1};
-  const Tiling small{128, 128, 1};
-  if (g.tiles(rows, cols) * 4 * 100 > small.tiles(rows, cols) * 115 || g.tiles(rows, cols) * std::min<int64_t>(8, steps / 64) < 192) g = small;
-  const int64_t t = g.tiles(rows, cols), slots = g.tr == 256 ? 256 : 512;
+  Tiling best{256, 256, 1};
+  double least = INFINITY;
   const double size = (double)rows * (double)cols / 8e5;
-  const auto cost = [&](int64_t s) {
-    return (double)(cdiv(t * s, slots) * (cdiv(steps, s) + 6)) + (s > 1 ? 6. + (double)s * size : 0.);
-  };
-  double best = cost(1);
-  const auto look = [&](int64_t s) {
-    s = std::min(s, steps / 8);
-    if (s > 1 && cost(s) < best) best = cost(s), g.split = (int)s;
-  };
-  for (int k = 1; k <= 4; ++k) look(k * slots / t);   // whole rounds,
-  if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));   // or so many that more would gain less than they cost
-  return g;
+  for (const Tiling g : {Tiling{256, 256, 1}, Tiling{128, 128, 1}}) {
+    const int64_t t = g.tiles(rows, cols), slots = g.tr == 256 ? 256 : 512;
+    const double step = g.tr == 256 ? 1.53 : 1.;
+    const auto look = [&](int64_t s) {
+      s = std::max<int64_t>(1, std::min(s, steps / 8));
+      const double cost = step * (double)(cdiv(t * s, slots) * (cdiv(steps, s) + 6)) + (s > 1 ? 1.4 * (6. + (double)s * size) : 0.);
+      if (cost < least) least = cost, best = g, best.split = (int)s;
+    };
+    look(1);
+    for (int k = 1; k <= 4; ++k) look(k * slots / t);   // whole rounds,
+    if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));   // or so many that more would gain less than they cost
+  }
+  return best;
 }
 int row_frags(int64_t rows) { return rows > 32 ? 4 : rows > 16 ? 2 : 1; }
 // Classes of a share of k_loss_few_dx: enough blocks to fill the card, each of a few steps at least.
