@@ -9,7 +9,8 @@
 // The 8-bit states hold the root of v, whose range is half as many binades: e4m3 has 2^17 between its largest and smallest
 // number, so a v 2^-35 of its block's largest is still held.  They are formed in 64 bits and rounded once (m + (1 - b1) g
 // near the border of two codes is decided as the formula says, whatever float32 would make of it; away from one float32
-// decides, which is half of the instructions); a root that is not zero never becomes zero, for m / sqrt(v) has no bound there.  The parameter's step uses m and v before that rounding.
+// decides, which is half of the instructions); a root that is not zero never becomes zero, for m / sqrt(v) has no bound there.
+// The parameter's step uses m and v before that rounding.
 #include <algorithm>
 #include <cmath>
 
@@ -75,7 +76,9 @@ __device__ __forceinline__ bool exponent_unsure(float top) {   // near 448 times
   return (__float_as_uint(top) & 0x7fffffu) - 0x5ffff8u <= 0x10u;
 }
 __device__ __forceinline__ double pow2(int e) { return __longlong_as_double((long long)(e + 1023) << 52); }   // |e| < 1023
-__device__ __forceinline__ float pow2f(int e) { return e > -127 ? __uint_as_float((uint32_t)(e + 127) << 23) : __uint_as_float(0x400000u); }   // -127 .. 127
+__device__ __forceinline__ float pow2f(int e) {   // -127 .. 127
+  return e > -127 ? __uint_as_float((uint32_t)(e + 127) << 23) : __uint_as_float(0x400000u);
+}
 __device__ __forceinline__ float max8(float v) {   // over eight lanes
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));

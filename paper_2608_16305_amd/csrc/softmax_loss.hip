@@ -7,8 +7,8 @@
 // two products with W and x take it from there.  So 8 rows x classes x width operations are done where 6 are needed, and a
 // piece of P, not all of it, is in memory.
 //
-// All products but those of few rows of float32 (k_loss_few) run on the 16-bit matrix instructions with float32 sums.  Logits of bfloat16 x and W are formed from them as
-// they are.  Everything else enters as float16 parts, which have 11 bits each: float32 x and W as two (within 2^-23 of an
+// All products but those of few rows of float32 (k_loss_few) run on the 16-bit matrix instructions with float32 sums.  Logits of
+// bfloat16 x and W are formed from them as they are.  Everything else enters as float16 parts, which have 11 bits each: float32 x and W as two (within 2^-23 of an
 // element; six bfloat16 products of three parts each would take twice the time), in three products for one of theirs, without
 // that of the second parts, 2^-22 at most; bfloat16 ones, for the gradients, as one, which holds their 8 bits; P, times 2^14,
 // as two (within 2^-23 of an element or 2^-39, whichever is more; two bfloat16 parts would be 2^-17 off, and the gradients of a
@@ -90,7 +90,9 @@ __device__ __forceinline__ uint32_t cvt2_f16(float a, float b) {   // to the nea
 }
 __device__ __forceinline__ float lo_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).x; }
 __device__ __forceinline__ float hi_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).y; }
-__device__ __forceinline__ float left_of(float v, float h) { return fabsf(h) < INFINITY ? v - h : 0.f; }   // (what is infinite or NaN is so in its first part)
+__device__ __forceinline__ float left_of(float v, float h) {   // (what is infinite or NaN is so in its first part)
+  return fabsf(h) < INFINITY ? v - h : 0.f;
+}
 
 // Eight elements of a row from c on (zeros from d on) in a padded matrix: as bfloat16, or times `by` in PARTS float16 parts.
 template <typename T, int PARTS>
@@ -175,7 +177,8 @@ __device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, 
   if (c < up(n, PAD)) put_parts<T, PARTS>(W + c * d, u, c < n ? d : 0, by, to + c * dp + u, plane);   // (zeros behind the last)
 }
 
-// The forward's second launch (counts NULL: its only one, of so few rows that each block counts them).  Blocks below `blocks`: the rows with a label, one after the other: idx (which rows), lab, xc (their x,
+// The forward's second launch (counts NULL: its only one, of so few rows that each block counts them).  Blocks below `blocks`:
+// the rows with a label, one after the other: idx (which rows), lab, xc (their x,
 // as it is or in parts; zeros behind the last one to a whole step); their number; of bfloat16 x its largest element.  The last of
 // them, past those of the rows, fill in the zeros.  The other blocks: W in parts, or padded.
 template <typename T>
@@ -202,7 +205,8 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
   const int mine = behind ? chunks : (int)(r0 / CHUNK);
   int v = 0;
   for (int i = threadIdx.x; counts && i < mine; i += 256) v += counts[i];
-  for (int64_t r = (counts ? (int64_t)mine * CHUNK : 0) + threadIdx.x; r < min(r0, max_rows); r += 256) v += has_label(label, r, rows, n);
+  for (int64_t r = (counts ? (int64_t)mine * CHUNK : 0) + threadIdx.x; r < min(r0, max_rows); r += 256)
+    v += has_label(label, r, rows, n);
   const int first = block_sum(v, s);
   if (behind) {
     const int j0 = (int)(r0 - up(max_rows, ROWS));
@@ -253,8 +257,8 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
 // The backward's first launch: dx of the rows without a label (blocks below `blocks`), and the search of the operands that the
 // forward has not searched.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W, const T* xc, int dp,
-                                                         const int32_t* count) {
+__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W,
+                                                         const T* xc, int dp, const int32_t* count) {
   if (blockIdx.x >= blocks) {
     const unsigned b = blockIdx.x - blocks;
     const uint32_t top = b < f.x_blocks ? largest_share(xc, (int64_t)dp, (int64_t)*count, f.d, nullptr, 0, b, f.x_blocks)
@@ -272,8 +276,8 @@ __global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int
 
 // Its second: W in float16 parts (blocks below `blocks`), and x's rows where the forward has left them as they are.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_lay(First f, const T* W, int dp, uint16_t* table, unsigned blocks, const T* xc, int64_t Rp,
-                                                       uint32_t* topA, uint32_t* topB, uint16_t* xh) {
+__global__ __launch_bounds__(256) void k_loss_back_lay(First f, const T* W, int dp, uint16_t* table, unsigned blocks, const T* xc,
+                                                       int64_t Rp, uint32_t* topA, uint32_t* topB, uint16_t* xh) {
   constexpr int PARTS = sizeof(T) == 2 ? 1 : 2;
   const bool of_x = blockIdx.x >= blocks;
   uint32_t* const at = of_x ? topA : topB;
@@ -830,7 +834,8 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
     put_x(xb);
     if (!BACK && p.xc && tile == 0) {
 #pragma unroll
-      for (int u = 0; u < RF; ++u) *(float4*)(p.xc + (int64_t)(r0 + 16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
+      for (int u = 0; u < RF; ++u)
+        *(float4*)(p.xc + (int64_t)(r0 + 16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
     }
     if (step + 1 < steps) load((step + 1) * KC);
     __syncthreads();   // (every wave has read what the step before last left here)
@@ -1056,7 +1061,8 @@ __global__ __launch_bounds__(256) void k_loss_few_dx(const int32_t* n_have, cons
 __global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const int32_t* idx, const float* part, int split, int by,
                                                      int64_t rows, int d, const float* dloss, int add, float* out, int64_t ldo) {
   __shared__ float4 sums[256];
-  const uint32_t dv = (uint32_t)cdiv(d, 4), each = 256 / by, at = threadIdx.x % each, k = threadIdx.x / each, e = blockIdx.x * each + at;
+  const uint32_t dv = (uint32_t)cdiv(d, 4), each = 256 / by, at = threadIdx.x % each, k = threadIdx.x / each;
+  const uint32_t e = blockIdx.x * each + at;
   const int64_t r = e / dv, n = *count;
   const int c = (int)(e % dv) * 4;
   const bool mine = r < (idx ? n : rows);
@@ -1268,7 +1274,8 @@ Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
     };
     look(1);
     for (int k = 1; k <= 4; ++k) look(k * slots / t);   // whole rounds,
-    if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));   // or so many that more would gain less than they cost
+    // or so many that more would gain less than they cost
+    if (t < slots) look(std::min(slots / t, (int64_t)std::sqrt((double)steps / size)));
   }
   return best;
 }
@@ -1278,8 +1285,8 @@ int few_per(const mtgnn_loss_dims* d) {
   const int64_t chunks = cdiv(d->d, KC), shares = std::max<int64_t>(1, std::min<int64_t>(cdiv(2048, chunks), d->n / 256));
   return (int)up(cdiv(d->n, shares), 64);
 }
-// Classes of a block of the forward's k_loss_few: more for short rows of many classes, whose tiles then take less time to join (128 and 64, the
-// whole forward: 16 x 190,000 x 200 51 and 61 us, 14 x 142,281 x 1,024 152 and 143, 64 x 9,000 x 1,024 55 and 38).
+// Classes of a block of the forward's k_loss_few: more for short rows of many classes, whose tiles then take less time to join
+// (128 and 64, the whole forward: 16 x 190,000 x 200 51 and 61 us, 14 x 142,281 x 1,024 152 and 143, 64 x 9,000 x 1,024 55 and 38).
 int few_classes(const mtgnn_loss_dims* d) { return d->n >= 32768 && d->d < 512 ? 128 : 64; }
 // A forward's tiles of classes.
 int64_t class_tiles(const mtgnn_loss_dims* d, const Plan& p, int64_t rows) {
@@ -1294,7 +1301,8 @@ Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t 
   Shares s;
   s.dx = tiling(rows, d->d, segs * cdiv(cols, KS));
   s.dw = tiling(cols, d->d, segs * cdiv(rows, KS));
-  s.bytes = std::max(s.dx.split > 1 ? 4 * (size_t)s.dx.split * rows * d->d : 0, s.dw.split > 1 ? 4 * (size_t)s.dw.split * cols * d->d : 0);
+  s.bytes = std::max(s.dx.split > 1 ? 4 * (size_t)s.dx.split * rows * d->d : 0,
+                     s.dw.split > 1 ? 4 * (size_t)s.dw.split * cols * d->d : 0);
   return s;
 }
 
@@ -1408,7 +1416,8 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     w += al(bytes);
     return at;
   };
-  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * (size_t)up(d->n, PAD) * p.dp : 0) : p.few ? 0 : 4 * (size_t)up(d->n, PAD) * p.dp);
+  const size_t plane = (size_t)up(d->n, PAD) * p.dp;
+  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * plane : 0) : p.few ? 0 : 4 * plane);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
   const int tiles = (int)class_tiles(d, p, max_rows);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
@@ -1423,8 +1432,9 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     const bool alone = p.bf && !save && max_rows <= CHUNK;
     if (!alone) k_loss_first<<<f.chunks + f.x_blocks + f.w_blocks, 256, 0, s>>>(f, xt, ldx, Wt);
     MTGNN_CHECK_LAUNCH("loss_first");
-    k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, alone ? nullptr : counts, k.count, k.idx, k.lab,
-                                           k.xc, p.Rp * p.dp, alone ? nullptr : k.largest, share, f.x_blocks, f.w_blocks, row_loss, blocks, Wt, tbl);
+    k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, alone ? nullptr : counts, k.count,
+                                           k.idx, k.lab, k.xc, p.Rp * p.dp, alone ? nullptr : k.largest, share, f.x_blocks,
+                                           f.w_blocks, row_loss, blocks, Wt, tbl);
     MTGNN_CHECK_LAUNCH("loss_lay");
     return MTGNN_OK;
   };
@@ -1455,7 +1465,8 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
   // (391 tiles) 54 -> 40; with one block, and no launch for the mean, 17 x 9,000 x 100 (141 tiles) 17.4 -> 15.4, but
   // 14 x 142,281 x 1,024 (2,224 tiles) 130 -> 156.
   const auto join = [&](auto kernel, int rows, int threads) -> mtgnn_status {
-    kernel<<<(unsigned)cdiv(max_rows, rows), threads, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums, loss);
+    kernel<<<(unsigned)cdiv(max_rows, rows), threads, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums,
+                                                              loss);
     MTGNN_CHECK_LAUNCH("loss_join");
     return MTGNN_OK;
   };
@@ -1516,13 +1527,15 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
   // (the sizes that the forward has searched operands for are kept: a bfloat16 x's, both of what it laid out in parts)
   uint32_t* const topA = p.few ? top : k.largest;
   uint32_t* const topB = lay_x ? top + 1 : k.largest + 1;
-  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, p.few ? search_blocks(max_rows, d->d) : 0, lay_x ? search_blocks(d->n, d->d) : 0};
+  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, p.few ? search_blocks(max_rows, d->d) : 0,
+          lay_x ? search_blocks(d->n, d->d) : 0};
   const unsigned zb = dx ? (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256) : 0, tb = table_blocks(d->n, p);
   const auto lay = [&](auto* Wt) -> mtgnn_status {
     const unsigned grid = zb + f.x_blocks + f.w_blocks;
     if (grid > 0) k_loss_back_first<<<grid, 256, 0, s>>>(f, dx, lddx, zb, Wt, (decltype(Wt))k.xc, p.dp, k.count);
     MTGNN_CHECK_LAUNCH("loss_back_first");
-    k_loss_back_lay<<<tb + (lay_x ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(f, Wt, p.dp, tbl, tb, (decltype(Wt))k.xc, p.Rp, topA, topB, xh);
+    k_loss_back_lay<<<tb + (lay_x ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(f, Wt, p.dp, tbl, tb, (decltype(Wt))k.xc, p.Rp, topA,
+                                                                             topB, xh);
     MTGNN_CHECK_LAUNCH("loss_back_lay");
     return MTGNN_OK;
   };
