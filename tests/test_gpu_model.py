@@ -665,6 +665,48 @@ def test_training_steps_in_a_graph():
     assert int(a.step) == int(b.step) == 4 and len(set(losses)) == 4
 
 
+@BOTH
+@pytest.mark.parametrize("rows,n,d", [(60, 700, 36), (200, 90, 130), (300, 40, 65)])
+def test_captured_losses_follow_the_count(rows, n, d, bf16):
+    """One capture of the loss and its gradients, replayed for other counts of rows (none, too), is the eager call's bits each time."""
+    rs = np.random.RandomState(rows)
+    x, W, b = _dev(_vals(rs, bf16, rows, d), bf16), _dev(_vals(rs, bf16, n, d), bf16), _dev(_vals(rs, False, n))
+    L = torch.from_numpy(rs.randint(-1, n, rows).astype(np.int32)).cuda()
+    e, c = M.loss_dims(n, d, M.BF16 if bf16 else M.F32), torch.tensor([rows], dtype=torch.int32, device="cuda")
+    ws, save = M.alloc_bytes(M.softmax_loss_ws_bytes(e, rows, True)), M.alloc_bytes(M.softmax_loss_save_bytes(e, rows))
+    out = [_marked(1, 1)[0], _marked(1, rows)[0], _marked(rows, d), _marked(n, d), _marked(1, n)[0]]
+    marked = [t.clone() for t in out]
+
+    def both():
+        M.mtgnn_softmax_loss(x, W, b, L, e, out[0], ws, row_loss=out[1], save=save, n_rows=c)
+        M.mtgnn_softmax_loss_bwd(x, W, b, L, e, save, out[2], out[3], out[4], ws, n_rows=c)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for count in (rows, 1, 0, 33, rows - 1, 0, rows):
+        got = []
+        for run in (graph.replay, both):
+            c.fill_(count)
+            for t, m in zip(out, marked):
+                t.copy_(m)
+            ws.fill_(255)
+            save.fill_(255)
+            run()
+            torch.cuda.synchronize()
+            got.append([t.clone() for t in out])
+        for k, (a, w) in enumerate(zip(*got)):
+            assert torch.equal(a.view(torch.int32), w.view(torch.int32)), (count, k)
+        assert torch.equal(got[0][1][count:], marked[1][count:]) and torch.equal(got[0][2][count:], marked[2][count:])
+        if count == 0:
+            assert float(got[0][0]) == 0 and not got[0][3].any() and not got[0][4].any()
+
+
 def test_two_streams_at_once():
     """Two models on two streams, each with a workspace of its own, give what one after the other gives."""
     want, got = [Model(257, 500, 33, s) for s in (1, 2)], [Model(257, 500, 33, s) for s in (1, 2)]
