@@ -755,6 +755,25 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
   __shared__ float2 st[4][16 * RF];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fg = lane >> 4;
   const int tile = blockIdx.x / p.groups, group = blockIdx.x % p.groups, r0 = group * 16 * RF;
+  const int c0 = tile * 64 * CF + wid * 16 * CF, steps = (int)cdiv(p.d, KC);
+  // the first step of W and the bias do not wait for the labels
+  const float* w[CF];
+#pragma unroll
+  for (int j = 0; j < CF; ++j) w[j] = p.W + (int64_t)min(c0 + 16 * j + fr, p.n - 1) * p.d + 4 * fg;
+  float wv[CF][4][4], bias[CF][4];
+  const auto load_w = [&](int k) __attribute__((always_inline)) {
+    const bool whole = k + KC <= p.d;
+#pragma unroll
+    for (int j = 0; j < CF; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) load_some(w[j] + k + 16 * t, whole ? 4 : p.d - k - 16 * t - 4 * fg, wv[j][t]);
+  };
+  load_w(0);
+#pragma unroll
+  for (int j = 0; j < CF; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[j][e] = p.b ? p.b[min(c0 + 16 * j + 4 * fg + e, p.n - 1)] : 0.f;
+
   int all = 0;
   if constexpr (BACK) {
     all = *p.count;
@@ -780,14 +799,10 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
       else if (t < rows && p.row_loss) p.row_loss[t] = 0.f;
     }
   }
-  const int c0 = tile * 64 * CF + wid * 16 * CF, steps = (int)cdiv(p.d, KC);
   const int count = min(all - r0, 16 * RF);   // rows of the group
   if (!BACK && count <= 0) return;
   __syncthreads();
 
-  const float* w[CF];
-#pragma unroll
-  for (int j = 0; j < CF; ++j) w[j] = p.W + (int64_t)min(c0 + 16 * j + fr, p.n - 1) * p.d + 4 * fg;
   const int xl = threadIdx.x >> 4, xk = 4 * (threadIdx.x & 15);
   const float* xr[RF];
 #pragma unroll
@@ -807,21 +822,12 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
 #pragma unroll
     for (int u = 0; u < RF; ++u) *(float4*)&xb[16 * u + xl][xk] = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
   };
-  float wv[CF][4][4];
-  const auto load = [&](int k) __attribute__((always_inline)) {
-    const bool whole = k + KC <= p.d;
-#pragma unroll
-    for (int j = 0; j < CF; ++j)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) load_some(w[j] + k + 16 * t, whole ? 4 : p.d - k - 16 * t - 4 * fg, wv[j][t]);
-    load_x(k);
-  };
   f32x4 acc[RF][CF];
 #pragma unroll
   for (int i = 0; i < RF; ++i)
 #pragma unroll
     for (int j = 0; j < CF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  load(0);
+  load_x(0);
   for (int step = 0; step < steps; ++step) {
     float (*xb)[LDC] = xs[step & 1];
     float now[CF][4][4];
@@ -837,7 +843,10 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
       for (int u = 0; u < RF; ++u)
         *(float4*)(p.xc + (int64_t)(r0 + 16 * u + xl) * p.dp + step * KC + xk) = make_float4(xv[u][0], xv[u][1], xv[u][2], xv[u][3]);
     }
-    if (step + 1 < steps) load((step + 1) * KC);
+    if (step + 1 < steps) {
+      load_w((step + 1) * KC);
+      load_x((step + 1) * KC);
+    }
     __syncthreads();   // (every wave has read what the step before last left here)
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -854,14 +863,6 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
   }
 
   // A lane has classes c0 + 16 j + 4 fg .. + 3 of the rows 16 i + fr.
-  float bias[CF][4];
-#pragma unroll
-  for (int j = 0; j < CF; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = c0 + 16 * j + 4 * fg + e;
-      bias[j][e] = p.b && c < p.n ? p.b[c] : 0.f;
-    }
   if constexpr (!BACK) {
 #pragma unroll
     for (int i = 0; i < RF; ++i) {
