@@ -743,7 +743,8 @@ mtgnn_status mtgnn_layer_norm_bwd(const float* dy, int64_t lddy, const void* x, 
 
 /* Softmax cross entropy of each row's label over all n classes:
  *   l_r = x_r W^T + b,  loss_r = log sum_c exp l_rc - l_r,label[r],  loss = mean of loss_r over the rows that have a label.
- *   x [max_rows, d], W [n, d] (rows dense) in the dtype; b [n] float32 or NULL (-inf takes a class out);
+ *   x [max_rows, d], W [n, d] (rows dense; at any element's address, in bfloat16 it is copied where its rows are not whole 16
+ *           bytes at 16-byte addresses) in the dtype; b [n] float32 or NULL (-inf takes a class out);
  *   label [max_rows]: a row whose label is outside [0, n) has none, counts nothing (whatever its x holds) and has the loss 0;
  *   loss -- [1] float32 out (0 where no row has a label);  row_loss -- [max_rows] float32 out, or NULL;
  *   save -- mtgnn_softmax_loss_save_bytes bytes for the backward (it keeps a copy of x's rows), or NULL.

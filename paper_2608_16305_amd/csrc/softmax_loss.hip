@@ -1198,7 +1198,7 @@ constexpr size_t PIECE = size_t(1) << 30;   // bytes of P in memory at a time (w
 int64_t stride(int64_t width) { return up(width, PAD) | PAD; }
 
 struct Plan {
-  bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes)
+  bool bf, copy;             // bfloat16 operands; their W is copied (its rows are not whole 16 bytes at 16-byte addresses)
   bool few, few_back;        // float32 operands of so few rows that the forward, and the backward too, read W as it is
   int dp;                    // padded width
   int64_t Rp, width;         // padded rows; classes of a piece
@@ -1210,11 +1210,11 @@ struct Plan {
 bool few_rows(const mtgnn_loss_dims* d, int64_t rows) {
   return rows <= 128 || (rows <= FEW && cdiv(d->n, 64) * cdiv(rows, 64) <= 768);
 }
-Plan plan(const mtgnn_loss_dims* d, int64_t rows) {
+Plan plan(const mtgnn_loss_dims* d, int64_t rows, const void* W) {
   Plan p;
   p.bf = d->dtype == MTGNN_BF16;
   p.dp = (int)stride(d->d);
-  p.copy = p.bf && d->d % 8 != 0;
+  p.copy = p.bf && (d->d % 8 != 0 || (uintptr_t)W % 16 != 0);
   p.few = !p.bf && few_rows(d, rows);
   p.few_back = p.few && rows <= 64;
   p.Rp = up(rows, PAD);
@@ -1389,13 +1389,13 @@ bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
          std::max<int64_t>(rows, d->n) * cdiv(d->d, 4) < MAX;
 }
 
-size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows)); }
+size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows, nullptr)); }
 
 size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
-  const Plan p = plan(d, rows);
+  const Plan p = plan(d, rows, nullptr);   // (W's address is not known yet: there is room for its copy whatever it is)
   const size_t t = al(2 * (size_t)up(d->n, PAD) * p.dp);   // a part of W
   if (!back)
-    return kept_bytes(p) + (p.bf ? (p.copy ? t : 0) : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
+    return kept_bytes(p) + (p.bf ? t : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
            al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, JOIN));
   if (p.few_back) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
@@ -1408,7 +1408,7 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
 mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
                        const int32_t* label, const mtgnn_loss_dims* d, float* loss, float* row_loss, void* save, void* ws,
                        hipStream_t s) {
-  const Plan p = plan(d, max_rows);
+  const Plan p = plan(d, max_rows, W);
   const Kept k = kept(save ? save : ws, p);
   const Tiling tl = tiling(max_rows, d->n);
   char* w = (char*)ws + kept_bytes(p);
@@ -1482,7 +1482,7 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
 mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* W, const float* b, const int32_t* label,
                            const mtgnn_loss_dims* d, const void* save, const float* dloss, float* dx, int64_t lddx, float* dW,
                            float* db, void* ws, hipStream_t s) {
-  const Plan p = plan(d, max_rows);
+  const Plan p = plan(d, max_rows, W);
   const Kept k = kept((void*)save, p);
   char* w = (char*)ws;
   const auto take = [&](size_t bytes) {

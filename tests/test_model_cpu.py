@@ -195,6 +195,14 @@ def test_softmax_loss_memory():
 
 
 @built
+def test_softmax_loss_has_room_for_a_copy_of_w():
+    """Of a bfloat16 W at any address, which the workspace's size does not know, in the forward and the backward."""
+    for n, d, rows in ((100_000, 64, 5), (3000, 520, 200), (70, 8, 1)):
+        for back in (False, True):
+            assert M.softmax_loss_ws_bytes(M.loss_dims(n, d, M.BF16), rows, back) >= 2 * n * d
+
+
+@built
 def test_adamw_refusals():
     L = M.lib()
     t = (M.AdamwTensor * 2)()
