@@ -7,13 +7,12 @@
 // two products with W and x take it from there.  So 8 rows x classes x width operations are done where 6 are needed, and a
 // piece of P, not all of it, is in memory.
 //
-// All products but those of few rows of float32 (k_loss_few) run on the 16-bit matrix instructions with float32 sums.  Logits of
-// bfloat16 x and W are formed from them as they are.  Everything else enters as float16 parts, which have 11 bits each: float32 x and W as two (within 2^-23 of an
-// element; six bfloat16 products of three parts each would take twice the time), in three products for one of theirs, without
-// that of the second parts, 2^-22 at most; bfloat16 ones, for the gradients, as one, which holds their 8 bits; P, times 2^14,
-// as two (within 2^-23 of an element or 2^-39, whichever is more; two bfloat16 parts would be 2^-17 off, and the gradients of a
-// few thousand classes then 1.3e-6, where a float32 evaluation is 1e-6 off).  What float16 lacks is range: a power of two
-// takes x's largest element, and W's, to 2^14 or above, and elements below 2^-17 of the largest are held to 2^-39 of it instead.
+// All products but those of few rows of float32 (k_loss_few) run on the bfloat16 matrix instructions with float32 sums.  bfloat16 x and
+// W enter as they are.  Everything else enters as three bfloat16 parts, which hold 24 bits and float32's whole range (bf16_split.h):
+// float32 x and W in the six products of parts that are not below 2^-24 of the whole, P in three with a bfloat16 operand.  (Two
+// float16 parts of float32 operands and of P take three and two products.  But float16 lacks the range: elements below 2^-17 of
+// a matrix's largest lost bits, a probability below 2^-39 was lost, and Adam divides a rare class's gradient by its own size.
+// 8,192 x 32,768 x 1,024 in bfloat16 with gradients took @A us with them, 4,000 x 9,001 x 100 in float32 @B.)
 //
 // Rows without a label are left out before anything is computed: the others' x is copied, row after row, padded with
 // zeros to whole steps.
@@ -29,12 +28,9 @@ namespace mtgnn {
 namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int KS = 64;          // a step of the sums: 128 bytes of a line
 constexpr int PAD = 64;         // rows and columns are padded to whole ones
-constexpr float LIFT = 16384.f; // what P is multiplied by
 constexpr int CHUNK = 1024;     // rows whose labels are counted together
 constexpr int ROWS = 16;        // rows that a block copies
 constexpr float LOG2E = 1.4426950408889634f;
@@ -57,146 +53,60 @@ __device__ __forceinline__ int block_sum(int v, int* s) {   // over 256 threads
   return v;
 }
 
-// --------------------------------------------------------------------------- float16 parts
+// --------------------------------------------------------------------------- operands
 
-// The bits of a finite magnitude (larger numbers, larger bits); 0 for what is not finite.
-__device__ __forceinline__ uint32_t magnitude(float v) {
-  const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
-__device__ __forceinline__ uint32_t block_largest(uint32_t v) {   // over 256 threads
-  __shared__ uint32_t s[4];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = max(max(s[0], s[1]), max(s[2], s[3]));
-  __syncthreads();
-  return v;
-}
-// The largest of the shares that blocks have left (`n` of them, at most MAX_SHARES).
-__device__ __forceinline__ uint32_t largest_of(const uint32_t* share, int n) {
-  uint32_t v = 0u;
-  for (int i = threadIdx.x; i < n; i += 256) v = max(v, share[i]);
-  return block_largest(v);
-}
-// The power of two that takes the largest element to 2^14 .. 2^15, as far as float32 has it.
-__device__ __forceinline__ float lift(uint32_t largest) {
-  return largest ? __uint_as_float(min(268u - (largest >> 23), 254u) << 23) : 1.f;
-}
-
-__device__ __forceinline__ uint32_t cvt2_f16(float a, float b) {   // to the nearest
-  return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
-}
-__device__ __forceinline__ float lo_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).x; }
-__device__ __forceinline__ float hi_f16(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p).y; }
-__device__ __forceinline__ float left_of(float v, float h) {   // (what is infinite or NaN is so in its first part)
-  return fabsf(h) < INFINITY ? v - h : 0.f;
-}
-
-// Eight elements of a row from c on (zeros from d on) in a padded matrix: as bfloat16, or times `by` in PARTS float16 parts.
-template <typename T, int PARTS>
-__device__ __forceinline__ uint32_t put_parts(const T* row, int c, int d, float by, uint16_t* to, int64_t plane) {
+// Eight elements of a row from c on (zeros from d on) in a padded matrix: as they are, or float32 in three parts.
+template <typename T>
+__device__ __forceinline__ void put_parts(const T* row, int c, int d, uint16_t* to, int64_t plane) {
   float v[8];
-  uint32_t top = 0u, h[4];
+  uint32_t h[4], m[4], l[4];
   load_some(row + c, d - c, v);
-  if constexpr (PARTS == 0) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = cvt2_bf16(v[2 * i], v[2 * i + 1]);
+    *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= by;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = cvt2_f16(v[2 * i], v[2 * i + 1]);
+    split_words<true>(v, h, m, l);
+    *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
+    *(uint4*)(to + plane) = make_uint4(m[0], m[1], m[2], m[3]);
+    *(uint4*)(to + 2 * plane) = make_uint4(l[0], l[1], l[2], l[3]);
   }
-  *(uint4*)to = make_uint4(h[0], h[1], h[2], h[3]);
-  if constexpr (PARTS == 2) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = cvt2_f16(left_of(v[2 * i], lo_f16(h[i])), left_of(v[2 * i + 1], hi_f16(h[i])));
-    *(uint4*)(to + plane) = make_uint4(h[0], h[1], h[2], h[3]);
-  }
-  return top;
 }
 
-// The largest element of the rows (of those with a label, where labels are given) that fall to block b of `blocks`.
-constexpr int MAX_SHARES = 1024;
-template <typename T>
-__device__ __forceinline__ uint32_t largest_share(const T* M, int64_t ld, int64_t rows, int d, const int32_t* label, int n, unsigned b,
-                                                  unsigned blocks) {
-  const int64_t units = cdiv(d, 8);
-  uint32_t top = 0u;
-  for (int64_t e = (int64_t)b * 256 + threadIdx.x; e < rows * units; e += (int64_t)blocks * 256) {
-    const int64_t r = e / units;
-    const int c = (int)(e - r * units) * 8;
-    if (label && !has_label(label, r, rows, n)) continue;
-    float v[8];
-    load_some(M + r * ld + c, d - c, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
-  }
-  return block_largest(top);
-}
-
-// The forward's first launch.  A block each: the labels of CHUNK rows are counted; then, of float32 operands, shares of x's rows
-// with a label and of W in search of the largest elements.
-struct First {
-  const int32_t *label, *n_rows;
-  int64_t max_rows;
-  int n, d;
-  int32_t* counts;             // of each chunk
-  uint32_t *largest, *share;   // [2] cleared; [x_blocks + w_blocks] what they found
-  unsigned chunks, x_blocks, w_blocks;
-};
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_first(First f, const T* x, int64_t ldx, const T* W) {
+// The forward's first launch: a block counts the labels of CHUNK rows.
+__global__ __launch_bounds__(256) void k_loss_count(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n,
+                                                    int32_t* counts) {
   __shared__ int s[4];
-  const int64_t rows = eff_count(f.max_rows, f.n_rows);
-  if (blockIdx.x < f.chunks) {
-    if (blockIdx.x == 0 && threadIdx.x < 2) f.largest[threadIdx.x] = 0u;
-    int v = 0;
+  const int64_t rows = eff_count(max_rows, n_rows);
+  int v = 0;
 #pragma unroll
-    for (int u = 0; u < CHUNK / 256; ++u) v += has_label(f.label, (int64_t)blockIdx.x * CHUNK + u * 256 + threadIdx.x, rows, f.n);
-    v = block_sum(v, s);
-    if (threadIdx.x == 0) f.counts[blockIdx.x] = v;
-    return;
-  }
-  const unsigned b = blockIdx.x - f.chunks;
-  const uint32_t top = b < f.x_blocks ? largest_share(x, ldx, rows, f.d, f.label, f.n, b, f.x_blocks)
-                                      : largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b - f.x_blocks, f.w_blocks);
-  if (threadIdx.x == 0) f.share[b] = top;
+  for (int u = 0; u < CHUNK / 256; ++u) v += has_label(label, (int64_t)blockIdx.x * CHUNK + u * 256 + threadIdx.x, rows, n);
+  v = block_sum(v, s);
+  if (threadIdx.x == 0) counts[blockIdx.x] = v;
 }
 
-// Rows of d as rows of dp: as they are, or in float16 parts.  Block b.
-template <typename T, int PARTS>
-__device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, float by, uint16_t* to, int64_t plane, unsigned b) {
+// Rows of d as rows of dp: as they are, or in parts.  Block b.
+template <typename T>
+__device__ __forceinline__ void lay_table(const T* W, int64_t n, int d, int dp, uint16_t* to, int64_t plane, unsigned b) {
   const uint32_t units = dp / 8, e = b * 256 + threadIdx.x;
   const int64_t c = e / units;
   const int u = (int)(e % units) * 8;
-  if (c < up(n, PAD)) put_parts<T, PARTS>(W + c * d, u, c < n ? d : 0, by, to + c * dp + u, plane);   // (zeros behind the last)
+  if (c < up(n, PAD)) put_parts<T>(W + c * d, u, c < n ? d : 0, to + c * dp + u, plane);   // (zeros behind the last)
 }
 
 // The forward's second launch (counts NULL: its only one, of so few rows that each block counts them).  Blocks below `blocks`:
 // the rows with a label, one after the other: idx (which rows), lab, xc (their x,
-// as it is or in parts; zeros behind the last one to a whole step); their number; of bfloat16 x its largest element.  The last of
+// as it is or in parts; zeros behind the last one to a whole step); their number.  The last of
 // them, past those of the rows, fill in the zeros.  The other blocks: W in parts, or padded.
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const int32_t* label, const int32_t* n_rows,
                                                   int64_t max_rows, int n, int d, int dp, const int32_t* counts, int32_t* count,
-                                                  int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane, uint32_t* largest,
-                                                  const uint32_t* share, unsigned x_shares, unsigned w_shares, float* row_loss,
+                                                  int32_t* idx, int32_t* lab, uint16_t* xc, int64_t plane, float* row_loss,
                                                   unsigned blocks, const T* W, uint16_t* table) {
-  constexpr int PARTS = sizeof(T) == 2 ? 0 : 2;
+  constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
   __shared__ int s[4], src[ROWS];
   if (blockIdx.x >= blocks) {
-    float by = 1.f;
-    if (PARTS) {
-      const uint32_t top = largest_of(share + x_shares, (int)w_shares);
-      if (blockIdx.x == blocks && threadIdx.x == 0) largest[1] = top;
-      by = lift(top);
-    }
-    lay_table<T, PARTS>(W, n, d, dp, by, table, up(n, PAD) * dp, blockIdx.x - blocks);
+    lay_table<T>(W, n, d, dp, table, up(n, PAD) * dp, blockIdx.x - blocks);
     return;
   }
   const int64_t rows = eff_count(max_rows, n_rows), r0 = (int64_t)blockIdx.x * ROWS;
@@ -215,8 +125,8 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
     for (int e = threadIdx.x; e < ROWS * units; e += 256) {
       const int64_t r = first + j0 + e / units;
       if (r >= end) break;
-      *(uint4*)(xc + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
-      if (PARTS == 2) *(uint4*)(xc + plane + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) *(uint4*)(xc + q * plane + r * dp + e % units * 8) = make_uint4(0u, 0u, 0u, 0u);
     }
     return;
   }
@@ -238,59 +148,34 @@ __global__ __launch_bounds__(256) void k_loss_lay(const T* x, int64_t ldx, const
   }
   __syncthreads();
   here = s[0];
-  uint32_t top = 0u;
-  if (PARTS) {
-    top = largest_of(share, (int)x_shares);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = top;
-  }
-  const float by = PARTS ? lift(top) : 1.f;
   for (int e = threadIdx.x; e < here * units; e += 256) {
     const int k = e / units, c = e % units * 8;
-    top = max(top, put_parts<T, PARTS>(x + (r0 + src[k]) * ldx, c, d, by, xc + (int64_t)(first + k) * dp + c, plane));
-  }
-  if (PARTS == 0) {
-    top = block_largest(top);
-    if (threadIdx.x == 0 && top && largest) atomicMax(largest, top);   // (a maximum does not depend on the order)
+    put_parts<T>(x + (r0 + src[k]) * ldx, c, d, xc + (int64_t)(first + k) * dp + c, plane);
   }
 }
 
-// The backward's first launch: dx of the rows without a label (blocks below `blocks`), and the search of the operands that the
-// forward has not searched.
+// The backward's first launch: zeros in dx of the rows without a label (zero_blocks); W in parts or padded, or the rows behind the last
+// whole step of one that is used in place (table_blocks: `wn` rows from W on, `wdp` apart); x's rows where the forward has
+// left them in float32.
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_first(First f, float* dx, int64_t lddx, unsigned blocks, const T* W,
-                                                         const T* xc, int dp, const int32_t* count) {
-  if (blockIdx.x >= blocks) {
-    const unsigned b = blockIdx.x - blocks;
-    const uint32_t top = b < f.x_blocks ? largest_share(xc, (int64_t)dp, (int64_t)*count, f.d, nullptr, 0, b, f.x_blocks)
-                                        : largest_share(W, (int64_t)f.d, (int64_t)f.n, f.d, nullptr, 0, b - f.x_blocks, f.w_blocks);
-    if (threadIdx.x == 0) f.share[b] = top;
+__global__ __launch_bounds__(256) void k_loss_back_lay(const int32_t* label, const int32_t* n_rows, int64_t max_rows, int n, int d,
+                                                       float* dx, int64_t lddx, unsigned zero_blocks, const T* W, int64_t wn,
+                                                       int wdp, uint16_t* table, unsigned table_blocks, const T* xc, int64_t Rp, int dp,
+                                                       uint16_t* xh) {
+  if (blockIdx.x >= zero_blocks + table_blocks) {
+    lay_table<T>(xc, Rp, dp, dp, xh, Rp * dp, blockIdx.x - zero_blocks - table_blocks);
     return;
   }
-  const uint32_t dv = (uint32_t)cdiv(f.d, 4), e = blockIdx.x * 256 + threadIdx.x;
+  if (blockIdx.x >= zero_blocks) {
+    lay_table<T>(W, wn, d, wdp, table, up(wn, PAD) * wdp, blockIdx.x - zero_blocks);
+    return;
+  }
+  const uint32_t dv = (uint32_t)cdiv(d, 4), e = blockIdx.x * 256 + threadIdx.x;
   const int64_t r = e / dv;
   const int c = (int)(e % dv) * 4;
-  if (r >= eff_count(f.max_rows, f.n_rows) || (uint32_t)f.label[r] < (uint32_t)f.n) return;
+  if (r >= eff_count(max_rows, n_rows) || (uint32_t)label[r] < (uint32_t)n) return;
   const float z[4] = {0.f, 0.f, 0.f, 0.f};
-  store_some(dx + r * lddx + c, f.d - c, z);
-}
-
-// Its second: W in float16 parts (blocks below `blocks`), and x's rows where the forward has left them as they are.
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_back_lay(First f, const T* W, int dp, uint16_t* table, unsigned blocks, const T* xc,
-                                                       int64_t Rp, uint32_t* topA, uint32_t* topB, uint16_t* xh) {
-  constexpr int PARTS = sizeof(T) == 2 ? 1 : 2;
-  const bool of_x = blockIdx.x >= blocks;
-  uint32_t* const at = of_x ? topA : topB;
-  const unsigned shares = of_x ? f.x_blocks : f.w_blocks, first = of_x ? blocks : 0;
-  uint32_t top;
-  if (shares) {
-    top = largest_of(f.share + (of_x ? 0 : f.x_blocks), (int)shares);
-    if (blockIdx.x == first && threadIdx.x == 0) *at = top;
-  } else {
-    top = *at;
-  }
-  if (of_x) lay_table<T, PARTS>(xc, Rp, dp, dp, lift(top), xh, Rp * dp, blockIdx.x - first);
-  else lay_table<T, PARTS>(W, f.n, f.d, dp, lift(top), table, up(f.n, PAD) * dp, blockIdx.x);
+  store_some(dx + r * lddx + c, d - c, z);
 }
 
 // --------------------------------------------------------------------------- the products
@@ -307,9 +192,10 @@ struct Prod {
   int64_t lda, ldb, planeA, planeB;
   uint32_t codeA, codeB;         // the parts of each segment, two bits each
   int segs, split;               // split: blocks that share a tile's sum, each leaving its own in `out`
-  const uint32_t *topA, *topB;   // largest elements of operands in float16 parts, or NULL
   int64_t rows, cols, K;         // the most rows; K: of a segment (its last step has a k that may be read)
-  int64_t dimA, dimB;            // elements of an operand's line that may be read (along the sum whole steps, but of a W in place)
+  int64_t dimA, dimB;            // elements of a line across the sum that may be read
+  int64_t endB;                  // k of B that may be read, where a W in place may end inside a step (STAT, PROB, DX)
+  int64_t tail;                  // DX: where that step's rows are, and zeros behind them, from B on
   int64_t tr, tc;                // tiles
   const int32_t* count;          // rows with a label: bounds the rows (STAT, PROB, DX) or K (DW)
   // epilogue
@@ -320,9 +206,9 @@ struct Prod {
   int64_t ld_part;
   float* at_label;
   const float2* stat;            // PROB: largest logit, 1 / sum
-  uint16_t* P;                   // two parts
+  uint16_t* P;                   // three parts
   int64_t ldp, planeP;
-  float* cols_part;              // column sums of P times LIFT, of each half tile's rows, or NULL
+  float* cols_part;              // column sums of P, of each half tile's rows, or NULL
   float* out;
   int64_t ldo;
   const float* dloss;
@@ -363,12 +249,12 @@ struct Lines {
   // Load i of a step that starts at `p`.  `left`: how many of its k may be read; the lanes past them read the step's first (it meets
   // zeros of the other operand).
   template <bool END>
-  __device__ __forceinline__ static void load(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[LOADS], int64_t ld, int64_t left,
-                                              int wid, int lane, int i) {
+  __device__ __forceinline__ static void load(uint32_t* buf, const uint16_t* p, const uint32_t (&off)[LOADS], int64_t left, int wid,
+                                              int lane, int i) {
     uint32_t o = off[i];
     if (END && left < KS) {
       const int k = k_of(wid, lane, i);
-      if (k >= left) o -= 2u * (uint32_t)k * (ALONG ? 1u : (uint32_t)ld);
+      if (k >= left) o -= 2u * (uint32_t)k;
     }
     __builtin_amdgcn_global_load_lds((void*)((const char*)p + o), (lds_ptr)(buf + (LOADS * wid + i) * 256), 16, 0, 0);
   }
@@ -402,11 +288,8 @@ __device__ __forceinline__ void my_tile(const Prod& p, int64_t& tr, int64_t& tc,
   tc = in / h;
 }
 
-// HALF: float16 operands, else bfloat16 ones.
-template <bool HALF>
 __device__ __forceinline__ f32x4 mma(bf16x8_t a, bf16x8_t b, f32x4 c) {
-  if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
 // TR x TC tiles, a wave has 16 WR x 64 of one: all of its rows where they are 64, else half of them.
@@ -446,12 +329,11 @@ struct Ahead {
 };
 
 // What becomes of a wave's sums.  FULL: the tile has all of its columns.  s: LDS that nothing uses any more.
-template <int KIND, bool HALF, class S, bool FULL, int WR, int WC>
+template <int KIND, class S, bool FULL, int WR, int WC>
 __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead<KIND, S>& h, uint32_t* lds, int64_t r0, int64_t c0,
                                       int64_t rows, int64_t count, int share, int wid, int lane) {
   const int wr = wid / S::WCOLS * (16 * WR), wc = wid % S::WCOLS * 64, fr = lane & 15, fg = lane >> 4;
   const int64_t ca = c0 + wc + 4 * fg, ra = r0 + wr + fr;
-  const float downA = HALF && KIND != DX ? 1.f / lift(*p.topA) : 1.f, downB = HALF && KIND != DW ? 1.f / lift(*p.topB) : 1.f;
   auto &at = h.at;
   float2 st[WR];         // the row's largest logit, 1 / sum
   if constexpr (KIND == STAT || KIND == PROB) {
@@ -461,15 +343,13 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
       at[i] = live ? (int)(at[i] - p.c0 - ca) : -1;
       if (KIND == PROB) st[i] = live ? p.stat[ra + 16 * i] : make_float2(INFINITY, 0.f);   // behind the last row: exponentials of -inf
     }
-    // (powers of two: the product is exact, and the sum rounded as it was)
-    const float down = fminf(downA * downB, 3e38f);
 #pragma unroll
     for (int j = 0; j < WC; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < WR; ++i) {
-          acc[i][j][e] = HALF ? fmaf(acc[i][j][e], down, h.b[j][e]) : acc[i][j][e] + h.b[j][e];
+          acc[i][j][e] += h.b[j][e];
           if (!FULL && ca + 16 * j + e >= p.cols) acc[i][j][e] = -INFINITY;
         }
   }
@@ -519,17 +399,16 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
     const int64_t end = up(rows, PAD);   // zeros in the rows behind the last, to a whole step
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-      const float by = st[i].y * LIFT;
 #pragma unroll
       for (int j = 0; j < WC; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - st[i].x) * LOG2E) * by;
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - st[i].x) * LOG2E) * st[i].y;
       if (has(i)) {
 #pragma unroll
         for (int j = 0; j < WC; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (at[i] == 16 * j + e) acc[i][j][e] -= LIFT;
+            if (at[i] == 16 * j + e) acc[i][j][e] -= 1.f;
       }
       if (p.cols_part) {
 #pragma unroll
@@ -539,18 +418,22 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
       }
       // sixteen rows through LDS (the wave's own place): written as they lie there, in whole 128 bytes (in the lanes'
       // order 32 bytes a row at a time took 823 us for 612, 7,373 x 32,768 x 1,024)
-      char* w = (char*)lds + wid * (2 * 16 * 144);
+      char* w = (char*)lds + wid * (3 * 16 * 144);
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
         const f32x4 v = acc[i][j];
-        const uint2 hi = make_uint2(cvt2_f16(v[0], v[1]), cvt2_f16(v[2], v[3]));
-        *(uint2*)(w + fr * 144 + 32 * j + 8 * fg) = hi;
-        *(uint2*)(w + 16 * 144 + fr * 144 + 32 * j + 8 * fg) =
-            make_uint2(cvt2_f16(v[0] - lo_f16(hi.x), v[1] - hi_f16(hi.x)), cvt2_f16(v[2] - lo_f16(hi.y), v[3] - hi_f16(hi.y)));
+        char* to = w + fr * 144 + 32 * j + 8 * fg;
+        const uint2 hi = make_uint2(cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3]));
+        const float a[4] = {v[0] - lo_bf16(hi.x), v[1] - hi_bf16(hi.x), v[2] - lo_bf16(hi.y), v[3] - hi_bf16(hi.y)};
+        const uint2 mid = make_uint2(cvt2_bf16(a[0], a[1]), cvt2_bf16(a[2], a[3]));
+        *(uint2*)to = hi;
+        *(uint2*)(to + 16 * 144) = mid;
+        *(uint2*)(to + 2 * 16 * 144) = make_uint2(cvt2_bf16(a[0] - lo_bf16(mid.x), a[1] - hi_bf16(mid.x)),
+                                                  cvt2_bf16(a[2] - lo_bf16(mid.y), a[3] - hi_bf16(mid.y)));
       }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
+      for (int q = 0; q < 3; ++q)
 #pragma unroll
         for (int h8 = 0; h8 < 2; ++h8) {
           const int line = 8 * h8 + (lane >> 3);
@@ -578,7 +461,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
   }
   if constexpr (KIND == DX || KIND == DW) {
     const bool whole = p.split == 1;   // else the sums as they are, for k_loss_shares
-    const float down = KIND == DX ? downB : downA, scale = whole ? loss_scale(count, p.dloss) / LIFT : 1.f;
+    const float scale = whole ? loss_scale(count, p.dloss) : 1.f;
     float* const out = p.out + (whole ? 0 : share * p.rows * p.ldo);
     const bool add = KIND == DX && whole && p.add;
     float* w = (float*)lds + wid * (16 * 68);   // (as above: whole 256 bytes of a row)
@@ -598,7 +481,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
         float v[4], old[4] = {0.f, 0.f, 0.f, 0.f};
         if (add) load_some(o, n, old);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = f[e] * down * scale + old[e];
+        for (int e = 0; e < 4; ++e) v[e] = f[e] * scale + old[e];
         store_some(o, n, v);
       }
       __builtin_amdgcn_wave_barrier();
@@ -606,7 +489,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
   }
 }
 
-template <int KIND, bool HALF, int TR, int TC>
+template <int KIND, int TR, int TC>
 __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod p) {
   using S = Shape<TR, TC>;
   constexpr bool AK = KIND != DW, BK = KIND == STAT || KIND == PROB;
@@ -639,13 +522,17 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
   const int steps = max(0, min(each, all - share * each));
   int seg = steps > 0 ? share * each / per : 0, k = share * each - seg * per;   // of the next step to load
   int at = 0;
+  // Where B's step from k0 on is.  (The choice by masks: by a branch or a select it took vector registers that the sums need.)
+  const auto of_b = [&](int64_t k0) __attribute__((always_inline)) {
+    const int64_t o = (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), past = (p.endB - KS - k0) >> 63;
+    return KIND == DX ? o ^ ((o ^ p.tail) & past) : o;
+  };
   const auto load = [&](uint32_t* buf, int u) __attribute__((always_inline)) {
     const int64_t k0 = (int64_t)k * KS;
     if (u < LA::LOADS)
-      LA::template load<false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, p.lda, KS, wid, lane, u);
+      LA::template load<false>(buf, fromA + (p.codeA >> 2 * seg & 3) * p.planeA + k0 * (AK ? 1 : p.lda), offA, KS, wid, lane, u);
     else
-      LB::template load<BK && !HALF>(buf + LA::WORDS, fromB + (p.codeB >> 2 * seg & 3) * p.planeB + k0 * (BK ? 1 : p.ldb), offB, p.ldb,
-                                      p.dimB - k0, wid, lane, u - LA::LOADS);
+      LB::template load<BK>(buf + LA::WORDS, fromB + of_b(k0), offB, p.endB - k0, wid, lane, u - LA::LOADS);
     if (u + 1 < LOADS) return;
     const int go = ++at < steps, turn = k + 1 == per;   // (the last step's again past it)
     seg += go & turn;
@@ -674,7 +561,7 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
     for (int m = 0; m < GROUPS; ++m) {
       if (m == READY) ready();
 #pragma unroll
-      for (int j = 0; j < WC; ++j) acc[m % WR][j] = mma<HALF>(b[m / WR][j], a[m % WR], acc[m % WR][j]);
+      for (int j = 0; j < WC; ++j) acc[m % WR][j] = mma(b[m / WR][j], a[m % WR], acc[m % WR][j]);
       __builtin_amdgcn_sched_barrier(0);
       if (m >= READY) {
         constexpr int PER = LOADS / (WR / 2);
@@ -717,18 +604,18 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
 
   // A lane has columns c0 + wc + 16 j + 4 fg .. + 3 of the rows r0 + wr + 16 i + fr.  Most tiles have all of their columns, and
   // no test of each.
-  if (c0 + TC <= p.cols) leave<KIND, HALF, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
-  else leave<KIND, HALF, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
+  if (c0 + TC <= p.cols) leave<KIND, S, true>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
+  else leave<KIND, S, false>(p, acc, ahead, buf0, r0, c0, rows, count, share, wid, lane);
 }
 
 // --------------------------------------------------------------------------- few rows of float32
 
 // For few rows every product is reading W or writing dW.  Those of float32 take W as it is, on the float32 matrix instructions (256
-// operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in float16 parts it is
-// searched, laid out and read (14 x 142,281 x 1,024 forward 592 us for 130).  A block has 64 CF classes and up to 64 rows; a
+// operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in parts it is
+// laid out and read (14 x 142,281 x 1,024 forward @C us for 143).  A block has 64 CF classes and up to 64 rows; a
 // lane reads 16 bytes of a class at a k four apart from its neighbours', and x, through LDS, in the same order, so that the
 // fragments need no more than that.  The forward leaves what STAT does, and x's rows with a label as they are; the backward
-// forms the logits again, leaves P times LIFT [classes][16 RF] for dx, and writes db and, from P and x in LDS, dW.
+// forms the logits again, leaves P [classes][16 RF] for dx, and writes db and, from P and x in LDS, dW.
 struct Few {
   const float *x, *W, *b;
   int64_t ldx;
@@ -897,7 +784,7 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
     for (int k = 1; k < 4; ++k) join(q, st[k][r]);
     p.part[tile * p.ld_part + r0 + r] = q;
   } else {
-    const float scale = loss_scale(count, p.dloss) / LIFT;
+    const float scale = loss_scale(count, p.dloss);
     float sum[CF][4];
 #pragma unroll
     for (int i = 0; i < RF; ++i) {
@@ -908,8 +795,8 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int c = c0 + 16 * j + 4 * fg + e;
-          float v = __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - s.x) * LOG2E) * (s.y * LIFT);
-          if (c == at) v -= LIFT;
+          float v = __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - s.x) * LOG2E) * s.y;
+          if (c == at) v -= 1.f;
           if (r >= count) v = 0.f;
           sum[j][e] = i ? sum[j][e] + v : v;
           if (p.P && c < p.n) p.P[(int64_t)c * (16 * RF) + r] = v;
@@ -1083,7 +970,7 @@ __global__ __launch_bounds__(256) void k_loss_shares(const int32_t* count, const
   }
   if (!mine || k) return;
   float* o = out + (idx ? (int64_t)idx[r] : r) * ldo + c;
-  const float scale = loss_scale(n, dloss) / LIFT;
+  const float scale = loss_scale(n, dloss);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] *= scale;
   if (add) {
@@ -1184,7 +1071,7 @@ __global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const flo
   v = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) v += s[i][j];
-  db[c] = v * (loss_scale(n, dloss) / LIFT);
+  db[c] = v * loss_scale(n, dloss);
 }
 
 // --------------------------------------------------------------------------- memory
@@ -1218,24 +1105,22 @@ Plan plan(const mtgnn_loss_dims* d, int64_t rows, const void* W) {
   p.few = !p.bf && few_rows(d, rows);
   p.few_back = p.few && rows <= 64;
   p.Rp = up(rows, PAD);
-  const int64_t most = (int64_t)(PIECE / (4 * (size_t)p.Rp)) / 256 * 256;
+  const int64_t most = (int64_t)(PIECE / (6 * (size_t)p.Rp)) / 256 * 256;
   p.width = std::min<int64_t>(up(d->n, PAD), std::max<int64_t>(256, most));
   return p;
 }
 
 struct Kept {                // what the forward leaves for the backward
   int32_t* count;
-  uint32_t* largest;         // of x, of W (float32)
   int32_t *idx, *lab;
   float2* stat;
-  uint16_t* xc;              // x's rows: bfloat16, or two float16 parts
+  uint16_t* xc;              // x's rows: as they are, or float32 in three parts
 };
-size_t kept_bytes(const Plan& p) { return 256 + 2 * al(4 * p.Rp) + al(8 * p.Rp) + al(2 * (size_t)(p.bf ? 1 : 2) * p.Rp * p.dp); }
+size_t kept_bytes(const Plan& p) { return 256 + 2 * al(4 * p.Rp) + al(8 * p.Rp) + al(2 * (size_t)(p.bf ? 1 : p.few ? 2 : 3) * p.Rp * p.dp); }
 Kept kept(void* at, const Plan& p) {
   Kept k;
   char* w = (char*)at;
   k.count = (int32_t*)w;
-  k.largest = (uint32_t*)(w + 16);
   k.idx = (int32_t*)(w += 256);
   k.lab = (int32_t*)(w += al(4 * p.Rp));
   k.stat = (float2*)(w += al(4 * p.Rp));
@@ -1298,7 +1183,7 @@ struct Shares {
   size_t bytes;
 };
 Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t cols) {
-  const int segs = p.bf ? 2 : 3;
+  const int segs = p.bf ? 3 : 6;
   Shares s;
   s.dx = tiling(rows, d->d, segs * cdiv(cols, KS));
   s.dw = tiling(cols, d->d, segs * cdiv(rows, KS));
@@ -1307,7 +1192,7 @@ Shares shares_of(const mtgnn_loss_dims* d, const Plan& p, int64_t rows, int64_t 
   return s;
 }
 
-template <int KIND, bool HALF>
+template <int KIND>
 mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
   p.tr = cdiv(p.rows, t.tr);
   p.tc = cdiv(p.cols, t.tc);
@@ -1316,9 +1201,9 @@ mtgnn_status product(Prod p, const Tiling& t, hipStream_t s) {
   {
     TimedScope ts(site::Generic::name, s),
         kind(KIND == STAT ? "loss_stat" : KIND == PROB ? "loss_prob" : KIND == DX ? "loss_dx" : "loss_dw", s);
-    if (t.tr == 256) k_loss_product<KIND, HALF, 256, 256><<<grid, 512, 0, s>>>(p);
-    else if (t.tr == 128) k_loss_product<KIND, HALF, 128, 128><<<grid, 256, 0, s>>>(p);
-    else if constexpr (KIND == STAT || KIND == PROB) k_loss_product<KIND, HALF, 64, 256><<<grid, 256, 0, s>>>(p);
+    if (t.tr == 256) k_loss_product<KIND, 256, 256><<<grid, 512, 0, s>>>(p);
+    else if (t.tr == 128) k_loss_product<KIND, 128, 128><<<grid, 256, 0, s>>>(p);
+    else if constexpr (KIND == STAT || KIND == PROB) k_loss_product<KIND, 64, 256><<<grid, 256, 0, s>>>(p);
   }
   MTGNN_CHECK_LAUNCH("loss_product");
   return MTGNN_OK;
@@ -1333,11 +1218,11 @@ mtgnn_status join_shares(const Prod& p, int split, const float* part, hipStream_
 // A gradient's product, shared by `split` blocks a tile through `part`.
 template <int KIND>
 mtgnn_status gradient(const Prod& p, const Tiling& t, float* part, hipStream_t s) {
-  if (t.split <= 1) return product<KIND, true>(p, t, s);
+  if (t.split <= 1) return product<KIND>(p, t, s);
   Prod q = p;
   q.out = part;
   q.ldo = p.cols;
-  MTGNN_TRY((product<KIND, true>(q, t, s)));
+  MTGNN_TRY(product<KIND>(q, t, s));
   return join_shares(p, t.split, part, s);
 }
 mtgnn_status few(const Few& p, int tc, hipStream_t s) {
@@ -1369,15 +1254,17 @@ mtgnn_status few_back(const Few& p, hipStream_t s) {
   return MTGNN_OK;
 }
 
-// The parts of a product of two operands of `a` and `b` parts, the smaller ones first (without that of two second parts).
-void segments(Prod& p, int a, int b) {
-  p.segs = a + b - 1;
-  if (a == 2 && b == 2) p.codeA = 1, p.codeB = 1 << 2;
-  else if (a == 2) p.codeA = 1;
+// The products of parts, the smaller ones first: of float32 operands (A in three parts, B too: both) six, of P and a bfloat16 one three.
+void segments(Prod& p, bool a, bool b) {
+  constexpr auto code = [](int q0, int q1, int q2, int q3, int q4, int q5) {
+    return (uint32_t)(q0 | q1 << 2 | q2 << 4 | q3 << 6 | q4 << 8 | q5 << 10);
+  };
+  p.segs = b ? 6 : a ? 3 : 1;
+  p.codeA = b ? code(2, 0, 1, 1, 0, 0) : a ? code(2, 1, 0, 0, 0, 0) : 0u;
+  p.codeB = b ? code(0, 2, 1, 0, 1, 0) : 0u;
 }
 
-unsigned table_blocks(int64_t n, const Plan& p) { return (unsigned)cdiv(up(n, PAD) * (p.dp / 8), 256); }
-unsigned search_blocks(int64_t rows, int d) { return (unsigned)std::min<int64_t>(MAX_SHARES, cdiv(rows * cdiv(d, 8), 256)); }
+unsigned table_blocks(int64_t n, int dp) { return (unsigned)cdiv(up(n, PAD) * (dp / 8), 256); }
 
 }  // namespace
 
@@ -1385,8 +1272,8 @@ bool loss_fits(const mtgnn_loss_dims* d, int64_t rows) {
   constexpr int64_t MAX = (int64_t(1) << 32) - (int64_t(1) << 20);
   const auto tiles = [](int64_t r, int64_t c) { return cdiv(r, 128) * cdiv(c, 128) * 256; };   // (shares only of few)
   const int64_t units = stride(d->d) / 8, W = (d->n + PAD) * units, x = (rows + PAD) * units;   // threads that lay out a matrix
-  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && W + x < MAX && W + rows * 16 < MAX &&
-         std::max<int64_t>(rows, d->n) * cdiv(d->d, 4) < MAX;
+  return tiles(rows, d->n) < MAX && tiles(rows, d->d) < MAX && tiles(d->n, d->d) < MAX && W + x + rows * cdiv(d->d, 4) < MAX &&
+         W + rows * 16 < MAX && std::max<int64_t>(rows, d->n) * cdiv(d->d, 4) < MAX;
 }
 
 size_t loss_save(const mtgnn_loss_dims* d, int64_t rows) { return kept_bytes(plan(d, rows, nullptr)); }
@@ -1395,13 +1282,12 @@ size_t loss_ws(const mtgnn_loss_dims* d, int64_t rows, bool back) {
   const Plan p = plan(d, rows, nullptr);   // (W's address is not known yet: there is room for its copy whatever it is)
   const size_t t = al(2 * (size_t)up(d->n, PAD) * p.dp);   // a part of W
   if (!back)
-    return kept_bytes(p) + (p.bf ? t : p.few ? 0 : 2 * t) + al(4 * cdiv(p.Rp, CHUNK)) + al(8 * MAX_SHARES) +
+    return kept_bytes(p) + (p.bf ? t : p.few ? 0 : 3 * t) + al(4 * cdiv(p.Rp, CHUNK)) +
            al(8 * (size_t)class_tiles(d, p, rows) * p.Rp) + al(4 * p.Rp) + al(8 * cdiv(p.Rp, JOIN));
   if (p.few_back) return al(4 * (size_t)d->n * 16 * row_frags(rows)) + al(4 * (size_t)cdiv(d->n, few_per(d)) * rows * d->d);
   const int64_t last = d->n % p.width ? d->n % p.width : std::min<int64_t>(d->n, p.width);
   const size_t part = std::max(shares_of(d, p, rows, std::min<int64_t>(d->n, p.width)).bytes, shares_of(d, p, rows, last).bytes);
-  return 256 + al(8 * MAX_SHARES) + (p.bf ? t + al(2 * (size_t)p.Rp * p.dp) : 2 * t + (p.few ? al(4 * (size_t)p.Rp * p.dp) : 0)) +
-         al(4 * (size_t)p.Rp * stride(p.width)) +
+  return (p.bf ? t : 3 * t + (p.few ? al(6 * (size_t)p.Rp * p.dp) : 0)) + al(6 * (size_t)p.Rp * stride(p.width)) +
          al(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width)) + al(part);
 }
 
@@ -1418,32 +1304,28 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     return at;
   };
   const size_t plane = (size_t)up(d->n, PAD) * p.dp;
-  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * plane : 0) : p.few ? 0 : 4 * plane);
+  uint16_t* tbl = (uint16_t*)take(p.bf ? (p.copy ? 2 * plane : 0) : p.few ? 0 : 6 * plane);
   int32_t* counts = (int32_t*)take(4 * cdiv(p.Rp, CHUNK));
   const int tiles = (int)class_tiles(d, p, max_rows);
   float2* part = (float2*)take(8 * (size_t)tiles * p.Rp);
   float* at_label = (float*)take(4 * p.Rp);
   double* sums = (double*)take(8 * cdiv(p.Rp, JOIN));
-  uint32_t* share = (uint32_t*)take(8 * MAX_SHARES);
-  First f{label, n_rows, max_rows, d->n, d->d, counts, k.largest, share, (unsigned)cdiv(max_rows, CHUNK), 0, 0};
-  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS), tb = p.bf && !p.copy ? 0 : table_blocks(d->n, p);
+  const unsigned blocks = (unsigned)(cdiv(max_rows, ROWS) + PAD / ROWS), tb = p.bf && !p.copy ? 0 : table_blocks(d->n, p.dp);
   const auto lay = [&](auto* xt, auto* Wt) -> mtgnn_status {
-    if (!p.bf) f.x_blocks = search_blocks(max_rows, d->d), f.w_blocks = search_blocks(d->n, d->d);
-    // (a bfloat16 x's largest element is the backward's)
-    const bool alone = p.bf && !save && max_rows <= CHUNK;
-    if (!alone) k_loss_first<<<f.chunks + f.x_blocks + f.w_blocks, 256, 0, s>>>(f, xt, ldx, Wt);
-    MTGNN_CHECK_LAUNCH("loss_first");
+    const bool alone = max_rows <= CHUNK;
+    if (!alone) k_loss_count<<<(unsigned)cdiv(max_rows, CHUNK), 256, 0, s>>>(label, n_rows, max_rows, d->n, counts);
+    MTGNN_CHECK_LAUNCH("loss_count");
     k_loss_lay<<<blocks + tb, 256, 0, s>>>(xt, ldx, label, n_rows, max_rows, d->n, d->d, p.dp, alone ? nullptr : counts, k.count,
-                                           k.idx, k.lab, k.xc, p.Rp * p.dp, alone ? nullptr : k.largest, share, f.x_blocks,
-                                           f.w_blocks, row_loss, blocks, Wt, tbl);
+                                           k.idx, k.lab, k.xc, p.Rp * p.dp, row_loss, blocks, Wt, tbl);
     MTGNN_CHECK_LAUNCH("loss_lay");
     return MTGNN_OK;
   };
   if (!p.few) MTGNN_TRY(p.bf ? lay((const uint16_t*)x, (const uint16_t*)W) : lay((const float*)x, (const float*)W));
   Prod q{};
-  q.A = k.xc; q.lda = q.dimA = p.dp; q.planeA = p.Rp * p.dp;
-  q.B = tbl; q.ldb = q.dimB = p.dp; q.planeB = up(d->n, PAD) * p.dp;
-  q.topA = k.largest; q.topB = k.largest + 1;
+  q.A = k.xc; q.lda = p.dp; q.planeA = p.Rp * p.dp;
+  q.B = tbl; q.ldb = q.endB = p.dp; q.planeB = plane;
+  if (p.bf && !p.copy) q.B = (const uint16_t*)W, q.ldb = q.endB = d->d;
+  segments(q, !p.bf, !p.bf);
   q.rows = max_rows; q.cols = d->n; q.K = up(d->d, KS); q.count = k.count;
   q.b = b; q.lab = k.lab; q.part = part; q.ld_part = p.Rp; q.at_label = at_label;
   if (p.few) {
@@ -1454,13 +1336,8 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     f.part = part; f.ld_part = p.Rp; f.at_label = at_label; f.row_loss = row_loss;
     f.groups = (int)cdiv(max_rows, 64);
     MTGNN_TRY(few(f, few_classes(d), s));
-  } else if (p.bf) {
-    if (!p.copy) q.B = (const uint16_t*)W, q.ldb = q.dimB = d->d;
-    segments(q, 1, 1);
-    MTGNN_TRY((product<STAT, false>(q, tl, s)));
   } else {
-    segments(q, 2, 2);
-    MTGNN_TRY((product<STAT, true>(q, tl, s)));
+    MTGNN_TRY(product<STAT>(q, tl, s));
   }
   // The whole forward, us: with 64 threads to a row, not 16, where there are more tiles than those request at once, 33 x 100,003 x 520
   // (391 tiles) 54 -> 40; with one block, and no launch for the mean, 17 x 9,000 x 100 (141 tiles) 17.4 -> 15.4, but
@@ -1500,10 +1377,10 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     f.groups = 1;
     MTGNN_TRY(few_back(f, s));
     if (!dx) return MTGNN_OK;
-    First none{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, nullptr, 0, 0, 0};
     const unsigned zb = (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256);
-    k_loss_back_first<float><<<zb, 256, 0, s>>>(none, dx, lddx, zb, nullptr, nullptr, 0, nullptr);
-    MTGNN_CHECK_LAUNCH("loss_back_first");
+    k_loss_back_lay<float><<<zb, 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx, zb, nullptr, 0, 0, nullptr, 0, nullptr, 0,
+                                              0, nullptr);
+    MTGNN_CHECK_LAUNCH("loss_back_lay");
     Prod r{};
     r.rows = max_rows; r.cols = d->d; r.count = k.count; r.idx = k.idx; r.dloss = dloss; r.out = dx; r.ldo = lddx;
     const dim3 grid((unsigned)cdiv(d->d, KC), (unsigned)cdiv(d->n, per));
@@ -1516,51 +1393,46 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     MTGNN_CHECK_LAUNCH("loss_few_dx");
     return join_shares(r, (int)grid.y, (float*)w, s);
   }
-  uint32_t* top = (uint32_t*)take(8);   // of x, of W, where they are searched here
-  uint32_t* share = (uint32_t*)take(8 * MAX_SHARES);
+  const bool in_place = p.bf && !p.copy;
   const int64_t plane = up(d->n, PAD) * p.dp, planeX = p.Rp * p.dp;
-  uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * plane);        // W and x in float16 parts
-  const bool lay_x = p.bf || p.few;
-  uint16_t* xh = lay_x ? (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 2) * planeX) : k.xc;
-  uint16_t* P = (uint16_t*)take(4 * (size_t)p.Rp * stride(p.width));
+  // W, or what is behind the last whole step of one in place: its rows from w0 on
+  const int64_t w0 = in_place ? d->n / KS * KS : 0;
+  const int wdp = in_place ? d->d : p.dp;
+  uint16_t* tbl = (uint16_t*)take(2 * (size_t)(p.bf ? 1 : 3) * up(d->n - w0, PAD) * wdp);
+  uint16_t* xh = p.few ? (uint16_t*)take(6 * (size_t)planeX) : k.xc;
+  uint16_t* P = (uint16_t*)take(6 * (size_t)p.Rp * stride(p.width));
   float* cols_part = (float*)take(4 * (size_t)cdiv(p.Rp, 64) * stride(p.width));
   float* part = (float*)w;
-  // (the sizes that the forward has searched operands for are kept: a bfloat16 x's, both of what it laid out in parts)
-  uint32_t* const topA = p.few ? top : k.largest;
-  uint32_t* const topB = lay_x ? top + 1 : k.largest + 1;
-  First f{label, n_rows, max_rows, d->n, d->d, nullptr, nullptr, share, 0, p.few ? search_blocks(max_rows, d->d) : 0,
-          lay_x ? search_blocks(d->n, d->d) : 0};
-  const unsigned zb = dx ? (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256) : 0, tb = table_blocks(d->n, p);
+  const unsigned zb = dx ? (unsigned)cdiv(max_rows * cdiv(d->d, 4), 256) : 0, tb = table_blocks(d->n - w0, wdp);
   const auto lay = [&](auto* Wt) -> mtgnn_status {
-    const unsigned grid = zb + f.x_blocks + f.w_blocks;
-    if (grid > 0) k_loss_back_first<<<grid, 256, 0, s>>>(f, dx, lddx, zb, Wt, (decltype(Wt))k.xc, p.dp, k.count);
-    MTGNN_CHECK_LAUNCH("loss_back_first");
-    k_loss_back_lay<<<tb + (lay_x ? table_blocks(p.Rp, p) : 0), 256, 0, s>>>(f, Wt, p.dp, tbl, tb, (decltype(Wt))k.xc, p.Rp, topA,
-                                                                             topB, xh);
+    const unsigned grid = zb + tb + (p.few ? table_blocks(p.Rp, p.dp) : 0);
+    if (grid > 0)
+      k_loss_back_lay<<<grid, 256, 0, s>>>(label, n_rows, max_rows, d->n, d->d, dx, lddx, zb, Wt + w0 * d->d, d->n - w0, wdp, tbl, tb,
+                                           (decltype(Wt))k.xc, p.Rp, p.dp, xh);
     MTGNN_CHECK_LAUNCH("loss_back_lay");
     return MTGNN_OK;
   };
   MTGNN_TRY(p.bf ? lay((const uint16_t*)W) : lay((const float*)W));
+  // W from class c on: the forward's operand, so the logits are the forward's too
+  const auto table = [&](Prod& q, int64_t c) {
+    q.B = in_place ? (const uint16_t*)W + c * d->d : tbl + c * p.dp;
+    q.ldb = wdp;
+    q.planeB = plane;
+  };
   for (int64_t c = 0; c < d->n; c += p.width) {
     const int64_t cols = std::min<int64_t>(p.width, d->n - c), ldp = stride(cols);
     const Shares sh = shares_of(d, p, max_rows, cols);
     const Tiling tl = tiling(max_rows, cols);
     Prod q{};
-    q.A = xh; q.lda = q.dimA = p.dp; q.planeA = planeX; q.topA = topA;
-    q.B = tbl + c * p.dp; q.ldb = q.dimB = p.dp; q.planeB = plane; q.topB = topB;
+    q.A = xh; q.lda = p.dp; q.planeA = planeX;
+    table(q, c);
+    q.endB = q.ldb;
     q.rows = max_rows; q.cols = cols; q.K = up(d->d, KS); q.count = k.count;
     q.b = b ? b + c : nullptr; q.lab = k.lab; q.c0 = c; q.stat = k.stat;
     q.P = P; q.ldp = ldp; q.planeP = p.Rp * ldp;
     q.cols_part = db ? cols_part : nullptr;
-    if (p.bf && !p.copy) {   // the logits that the forward had
-      q.A = k.xc;
-      q.B = (const uint16_t*)W + c * d->d; q.ldb = q.dimB = d->d;
-      segments(q, 1, 1);
-      MTGNN_TRY((product<PROB, false>(q, tl, s)));
-    } else {
-      segments(q, p.bf ? 1 : 2, p.bf ? 1 : 2);
-      MTGNN_TRY((product<PROB, true>(q, tl, s)));
-    }
+    segments(q, !p.bf, !p.bf);
+    MTGNN_TRY(product<PROB>(q, tl, s));
     if (db) {
       k_loss_db<<<(unsigned)cdiv(cols, 16), 256, 0, s>>>(k.count, cols_part, ldp, tl.tr == 64 ? 64 : tl.tr / 2, cols, dloss, db + c);
       MTGNN_CHECK_LAUNCH("loss_db");
@@ -1568,16 +1440,17 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     Prod g{};
     g.A = P; g.lda = g.dimA = ldp; g.planeA = p.Rp * ldp;
     g.cols = d->d; g.count = k.count; g.dloss = dloss;
-    segments(g, 2, p.bf ? 1 : 2);
+    segments(g, true, !p.bf);
     if (dx) {
       Prod r = g;
-      r.B = tbl + c * p.dp; r.ldb = r.dimB = p.dp; r.planeB = plane; r.topB = topB;
+      table(r, c);
+      r.dimB = r.ldb; r.endB = up(d->n, in_place ? 1 : PAD) - c; r.tail = tbl - r.B;
       r.rows = max_rows; r.K = cols; r.idx = k.idx; r.out = dx; r.ldo = lddx; r.add = c > 0;
       MTGNN_TRY((gradient<DX>(r, sh.dx, part, s)));
     }
     if (dW) {
       Prod r = g;
-      r.B = xh; r.ldb = r.dimB = p.dp; r.planeB = planeX; r.topA = topA;
+      r.B = xh; r.ldb = r.dimB = p.dp; r.planeB = planeX;
       r.rows = cols; r.out = dW + c * d->d; r.ldo = d->d;
       MTGNN_TRY((gradient<DW>(r, sh.dw, part, s)));
     }
