@@ -1105,8 +1105,9 @@ Plan plan(const mtgnn_loss_dims* d, int64_t rows, const void* W) {
   p.few = !p.bf && few_rows(d, rows);
   p.few_back = p.few && rows <= 64;
   p.Rp = up(rows, PAD);
-  const int64_t most = (int64_t)(PIECE / (6 * (size_t)p.Rp)) / 256 * 256;
-  p.width = std::min<int64_t>(up(d->n, PAD), std::max<int64_t>(256, most));
+  // (rows of P are up to 64 elements longer than a piece is wide)
+  const int64_t most = std::max<int64_t>(256, ((int64_t)(PIECE / (6 * (size_t)p.Rp)) - PAD) / 256 * 256), pieces = cdiv(d->n, most);
+  p.width = pieces == 1 ? up(d->n, PAD) : up(cdiv(d->n, pieces), 256);
   return p;
 }
 

@@ -203,6 +203,14 @@ def test_softmax_loss_has_room_for_a_copy_of_w():
 
 
 @built
+@pytest.mark.parametrize("rows", [8_000, 16_384, 100_000, 262_144, 349_500])
+def test_softmax_loss_takes_a_gigabyte_for_p(rows):
+    """The padding of P's rows counts too.  A twentieth more for what else is there: copies of 8 columns, tiles' and columns' sums."""
+    for n in (2000, 30_000):
+        assert M.softmax_loss_ws_bytes(M.loss_dims(n, 8, M.BF16), rows, True) < 1.05 * 2 ** 30 + rows * n // 16
+
+
+@built
 def test_adamw_refusals():
     L = M.lib()
     t = (M.AdamwTensor * 2)()
