@@ -720,7 +720,7 @@ mtgnn_status mtgnn_embedding_bwd(const int32_t* ids, const int32_t* n_rows, int6
 /* Layer norm of each row:  m = mean x,  q = 1 / sqrt(mean (x - m)^2 + eps),  h = (x - m) q,  y = gamma h + beta.
  *   x, y [max_rows, d] (dtype; y may be x with the same stride where no backward follows, else no overlap);
  *   gamma, beta [d] float32, each or NULL (ones, zeros);
- *   stats -- [max_rows, 2] float32 out, m and q, for mtgnn_layer_norm_bwd, or NULL. */
+ *   stats -- [max_rows, 2] float32 out, 8-byte aligned, m and q, for mtgnn_layer_norm_bwd, or NULL. */
 typedef struct {
   int32_t d, dtype;          /* d <= 2^20 */
   float eps;                 /* finite, >= 0 */

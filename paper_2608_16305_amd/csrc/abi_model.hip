@@ -34,6 +34,11 @@ mtgnn_status check_loss(const mtgnn_loss_dims* d) {
   return MTGNN_OK;
 }
 
+// Written and read two floats at a time.
+mtgnn_status check_stats(const float* stats) {
+  return (uintptr_t)stats % 8 ? fail(MTGNN_EINVAL, "stats is not 8-byte aligned") : MTGNN_OK;
+}
+
 // A block of `threads` to each row.
 mtgnn_status check_blocks(int64_t rows, int64_t threads, const char* what) { return check_items(rows, threads, what); }
 
@@ -91,6 +96,7 @@ mtgnn_status mtgnn_layer_norm(const void* x, int64_t ldx, const int32_t* n_rows,
   REQ(y, "y");
   STRIDE(ldx, d->d, "ldx");
   STRIDE(ldy, d->d, "ldy");
+  MTGNN_TRY(check_stats(stats));
   MTGNN_TRY(check_blocks(max_rows, norm_threads(d), "max_rows"));
   const int64_t e = bytes_of(d->dtype), w = d->d * e;
   if ((x != y || ldx != ldy || stats) && overlap(Rows{x, ldx * e, w}, Rows{y, ldy * e, w}, max_rows))
@@ -118,7 +124,7 @@ mtgnn_status mtgnn_layer_norm_bwd(const float* dy, int64_t lddy, const void* x, 
   STRIDE(ldx, d->d, "ldx");
   STRIDE(lddx, d->d, "lddx");
   if (past) STRIDE(ldp, d->d, "ldp");
-  MTGNN_TRY(check_aligned((uintptr_t)stats % 8 ? (const void*)1 : nullptr, "stats is not 8-byte aligned"));
+  MTGNN_TRY(check_stats(stats));
   MTGNN_TRY(check_blocks(max_rows, norm_threads(d), "max_rows"));
   if (dgamma || dbeta) {
     if (ws_bytes < norm_ws(d, max_rows)) return fail(MTGNN_EWORKSPACE, "layer_norm_bwd ws");

@@ -157,6 +157,17 @@ def test_layer_norm_refusals():
 
 
 @built
+def test_layer_norm_stats_are_aligned_in_both_directions():
+    """What the backward would refuse, the forward does too."""
+    L, d = M.lib(), M.norm_dims(8)
+    for at, want in ((4, -1), (12, -1), (1, -1)):
+        stats, far = C.c_void_p((1 << 32) + at), C.c_void_p(1 << 30)
+        assert L.mtgnn_layer_norm(P, 8, None, 10, None, None, C.byref(d), far, 8, stats, None) == want
+        assert L.mtgnn_layer_norm_bwd(P, 8, far, 8, stats, None, 10, None, None, 8, C.byref(d), C.c_void_p(1 << 34), 8, None, None, None, 0,
+                                      None) == want
+
+
+@built
 def test_softmax_loss_refusals():
     L = M.lib()
     good = M.loss_dims(100, 8)
