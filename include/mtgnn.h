@@ -844,7 +844,8 @@ mtgnn_status mtgnn_adam_step(float* const* params, const float* const* grads, fl
 /* One AdamW step (decoupled weight decay, bias-corrected) over n tensors, any number, in place:
  *   m = beta1 m + (1 - beta1) grad,  v = beta2 v + (1 - beta2) grad^2,
  *   param = param (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
- * A tensor (n <= 2^33 elements, dense, at any float's address; no two share memory; n = 0: skipped):
+ * A tensor (n <= 2^33 elements, dense, at any float's address; n = 0: skipped).  What is written shares
+ * memory with nothing else of the call; two gradients may be one:
  *   param, grad -- float32;  shadow -- bfloat16 copy of the updated parameter, or NULL;  decay -- its weight decay;
  *   m_exp, v_exp NULL: m, v are float32;
  *   m_exp, v_exp given: the states take 8 bits.  m holds codes of m, v codes of sqrt(v), in e4m3 (4 bits of exponent, bias 7;

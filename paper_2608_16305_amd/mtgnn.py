@@ -7,6 +7,7 @@ current HIP stream to the C entry point of the same name, and raises
 is no fallback: if the library is missing, the first call raises.
 """
 
+import bisect
 import ctypes as C
 import os
 
@@ -1193,6 +1194,10 @@ class AdamwTensors:
                          for x in (*params, *m, *v, *lists["shadow"], *lists["m_exp"], *lists["v_exp"]) if x is not None and x.numel())
         if any(a + size > b for (a, size), (b, _) in zip(written, written[1:])):
             raise MtgnnError("two of the tensors share memory (a parameter may be listed once)")
+        for g in grads:   # (only read: two may be one)
+            k = bisect.bisect_left(written, (g.data_ptr() + g.numel() * 4,)) - 1   # the last that starts before its end
+            if g.numel() and k >= 0 and sum(written[k]) > g.data_ptr():
+                raise MtgnnError("a gradient shares memory with a parameter or a state")
         self.tensors, self.device = (list(params), *(list(x) for x in lists.values())), dev
 
 

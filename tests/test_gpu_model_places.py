@@ -45,3 +45,22 @@ def test_softmax_loss_of_a_packed_w(rows, n, d, at, bf16):
     for t in (dW, db):      # what lies around a result stays
         around = torch.as_strided(t, (at + t.numel() + 5,), (1,), t.storage_offset() - at)
         assert torch.isnan(around[:at]).all() and torch.isnan(around[-5:]).all()
+
+
+def test_adamw_refuses_a_gradient_in_what_is_written():
+    p, g, m, v, sh = (torch.ones(24, device="cuda") for _ in range(5))
+    sh = sh.bfloat16()
+    lists = lambda g, **k: M.adamw_tensors([p[:8], p[8:16]], g, [m[:8], m[8:16]], [v[:8], v[8:16]], **k)   # noqa: E731
+    lists([g[:8], g[4:12]])                              # gradients are only read
+    lists([p[16:], v[16:]])                              # beside a parameter, not in it
+    lists([g[:8], m[16:]], shadow=[sh[:8], None])
+    for bad in (p[:8], p[15:23], p[8:16], m[7:15], v[:8], v[15:23]):
+        with pytest.raises(M.MtgnnError, match="gradient shares memory"):
+            lists([g[:8], bad])
+        with pytest.raises(M.MtgnnError, match="gradient shares memory"):
+            lists([bad, g[:8]])
+    in_shadow = sh.view(torch.float32)[:8]
+    with pytest.raises(M.MtgnnError, match="gradient shares memory"):
+        lists([g[:8], in_shadow], shadow=[None, sh[8:16]])
+    empty = torch.empty(0, device="cuda")
+    M.adamw_tensors([empty, p[:8]], [empty, g[:8]], [empty, m[:8]], [empty, v[:8]])
