@@ -299,9 +299,13 @@ struct Shape {
   static constexpr int WR = TR / 16 / WROWS, WC = 4, LINES = TR, COLUMNS = TC;
 };
 
+// What exponentials are relative to, where m is the largest logit: m, but not an infinite one, whose difference from itself is NaN.
+// Nothing but classes of logit -inf have a sum of zeros so, and one of +inf an infinite sum, in which a NaN still shows.
+__device__ __forceinline__ float base_of(float m) { return fabsf(m) < INFINITY ? m : 0.f; }
+
 // Joins (largest, sum of exponentials relative to it).
 __device__ __forceinline__ void join(float2& q, float2 o) {
-  const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;   // (nothing but classes of logit -inf: a sum of zeros)
+  const float m = fmaxf(q.x, o.x), from = base_of(m);
   q.y = q.y * __builtin_amdgcn_exp2f((q.x - from) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - from) * LOG2E);
   q.x = m;
 }
@@ -373,7 +377,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
       }
       m = fmaxf(m, __shfl_xor(m, 16, 64));
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      const float from = m == -INFINITY ? 0.f : m;
+      const float from = base_of(m);
 #pragma unroll
       for (int j = 0; j < WC; ++j)
 #pragma unroll
@@ -767,7 +771,7 @@ __global__ __launch_bounds__(256) void k_loss_few(Few p) {
         }
       m = fmaxf(m, __shfl_xor(m, 16, 64));
       m = fmaxf(m, __shfl_xor(m, 32, 64));
-      const float from = m == -INFINITY ? 0.f : m;
+      const float from = base_of(m);
 #pragma unroll
       for (int j = 0; j < CF; ++j)
 #pragma unroll
@@ -1001,7 +1005,7 @@ __global__ __launch_bounds__(THREADS) void k_loss_join(const int32_t* count, con
   }
   float2 q = make_float2(-INFINITY, 0.f);
   const auto add = [&](float2 o) {
-    const float m = fmaxf(q.x, o.x), from = m == -INFINITY ? 0.f : m;
+    const float m = fmaxf(q.x, o.x), from = base_of(m);
     q.y = q.y * expf(q.x - from) + o.y * expf(o.x - from);
     q.x = m;
   };
@@ -1024,8 +1028,6 @@ __global__ __launch_bounds__(THREADS) void k_loss_join(const int32_t* count, con
   if (k == 0) {
     double v = 0.0;
     if (r < n) {
-      // a logit of +inf: the others' exponentials are 0 beside it
-      if (q.x == INFINITY) q.y = 1.f;
       const float f = (q.x - at_label[r]) + logf(q.y);
       stat[r] = make_float2(q.x, 1.f / q.y);
       if (row_loss) row_loss[idx[r]] = f;

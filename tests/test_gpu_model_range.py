@@ -90,3 +90,27 @@ def test_rare_classes_have_their_gradient(rows, n, d, bf16):
     label = label % (n // 3) * 3 + 1 + label % 2
     want = _check(x, W, b, label.astype(np.int32), bf16)
     assert 0 < np.abs(want["dW"][::3]).max() < 1e-20
+
+
+@BOTH
+@pytest.mark.parametrize("rows", [10, 70, 200, 1100])
+@pytest.mark.parametrize("at", [5, 500])
+def test_a_nan_beside_an_infinite_logit_is_nan(rows, at, bf16):
+    """log sum exp of an infinite logit is infinite, of one and a NaN, in the same tile or in another, NaN; a row without a label is 0."""
+    rs = np.random.RandomState(rows)
+    n, d = 600, 24
+    x, W, b = _vals(rs, bf16, rows, d), _vals(rs, bf16, n, d), _vals(rs, False, n)
+    label = rs.randint(4, n, rows).astype(np.int32)
+    label[0], label[1] = -1, 3
+    e, L = M.loss_dims(n, d, M.BF16 if bf16 else M.F32), torch.from_numpy(label).cuda()
+    loss, per_row, dx = _marked(1, 1)[0], _marked(rows, 1)[:, 0], _marked(rows, d)
+    ws, save = M.alloc_bytes(M.softmax_loss_ws_bytes(e, rows, True)), M.alloc_bytes(M.softmax_loss_save_bytes(e, rows))
+    for nan in (False, True):
+        b[3] = np.inf
+        b[at] = np.nan if nan else 0.5
+        X, Wd, bd = _dev(x, bf16), _dev(W, bf16), _dev(b)
+        M.mtgnn_softmax_loss(X, Wd, bd, L, e, loss, ws, row_loss=per_row, save=save)
+        M.mtgnn_softmax_loss_bwd(X, Wd, bd, L, e, save, dx, None, None, ws)
+        assert per_row[0] == 0 and torch.isnan(per_row[1]) and torch.isnan(loss).all()
+        assert torch.isnan(per_row[2:]).all() if nan else (per_row[2:] == np.inf).all()
+        assert torch.isnan(dx[1:]).all() and not dx[0].any()
