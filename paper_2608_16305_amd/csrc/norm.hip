@@ -352,7 +352,7 @@ mtgnn_status norm_t(const T* x, int64_t ldx, const int32_t* n_rows, int64_t max_
   if (d <= 64 * V) k_norm<T, 64, 1><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 128 * V) k_norm<T, 64, 2><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (many && d <= 256 * V) k_norm<T, 64, 4><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
-  else if (many && d <= 2048) k_norm<T, 64, 32 / V><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
+  else if (many && d <= 2048 && V == 4) k_norm<T, 64, 32 / V><<<few, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 256 * V) k_norm<T, 256, 1><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 512 * V) k_norm<T, 256, 2><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
   else if (d <= 8192) k_norm<T, 256, 32 / V><<<all, 256, 0, s>>>(x, ldx, n_rows, max_rows, gamma, beta, d, eps, y, ldy, st);
