@@ -12,7 +12,7 @@
 // float32 x and W in the six products of parts that are not below 2^-24 of the whole, P in three with a bfloat16 operand.  (Two
 // float16 parts of float32 operands and of P take three and two products.  But float16 lacks the range: elements below 2^-17 of
 // a matrix's largest lost bits, a probability below 2^-39 was lost, and Adam divides a rare class's gradient by its own size.
-// 8,192 x 32,768 x 1,024 in bfloat16 with gradients took @A us with them, 4,000 x 9,001 x 100 in float32 @B.)
+// 8,192 x 32,768 x 1,024 in bfloat16 with gradients took 3,080 us with them for @A, 4,000 x 9,001 x 100 in float32 234 for @B.)
 //
 // Rows without a label are left out before anything is computed: the others' x is copied, row after row, padded with
 // zeros to whole steps.
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(TR == 256 ? 512 : 256, 2) void k_loss_product(Prod 
 
 // For few rows every product is reading W or writing dW.  Those of float32 take W as it is, on the float32 matrix instructions (256
 // operations a cycle of a compute unit: 64 rows take about as long as the reading, 16 a quarter); in parts it is
-// laid out and read (14 x 142,281 x 1,024 forward @C us for 143).  A block has 64 CF classes and up to 64 rows; a
+// laid out and read (14 x 142,281 x 1,024 forward 665 us for 130).  A block has 64 CF classes and up to 64 rows; a
 // lane reads 16 bytes of a class at a k four apart from its neighbours', and x, through LDS, in the same order, so that the
 // fragments need no more than that.  The forward leaves what STAT does, and x's rows with a label as they are; the backward
 // forms the logits again, leaves P [classes][16 RF] for dx, and writes db and, from P and x in LDS, dW.
@@ -1092,12 +1092,13 @@ struct Plan {
   int dp;                    // padded width
   int64_t Rp, width;         // padded rows; classes of a piece
 };
-// Rows of float32 that k_loss_few's forward takes: up to 128, or 256 where its blocks are all on the card at once (three a CU).  The
-// forward in float16 parts and by it, us: 92 x 48,988 x 1,024 186 and 136, 128 x 30,000 x 512 65 and 65; 200 x 9,000 x 100 26 and
-// 22, 250 x 3,000 x 1,024 57 and 38; 250 x 16,000 x 1,024 (1,000 blocks) 81 and 101.  The backward by it takes up to 64: 92 x
-// 48,988 x 1,024 312 and 507.
+// Rows of float32 that k_loss_few's forward takes: up to 192, or 256 where its blocks are all on the card at once (three a CU).  The
+// forward in parts and by it, us: 92 x 48,988 x 1,024 215 and 137, 129 x 38,544 x 1,024 222 and 174, 192 x 60,000 x 200 79 and 83,
+// 192 x 150,000 x 512 403 and 319; 200 x 9,000 x 100 26 and 20, 250 x 3,000 x 1,024 81 and 38; 256 x 20,000 x 768 (1,252 blocks) 94
+// and 101, 256 x 60,000 x 200 81 and 107, 256 x 150,000 x 1,024 824 and 766.  The backward by it takes up to 64: 64 x 30,000 x
+// 512 with the forward 218 and 130; 92 x 48,988 x 1,024 alone 414, and in groups of 64 rows 507.
 bool few_rows(const mtgnn_loss_dims* d, int64_t rows) {
-  return rows <= 128 || (rows <= FEW && cdiv(d->n, 64) * cdiv(rows, 64) <= 768);
+  return rows <= 192 || (rows <= FEW && cdiv(d->n, 64) * cdiv(rows, 64) <= 768);
 }
 Plan plan(const mtgnn_loss_dims* d, int64_t rows, const void* W) {
   Plan p;
