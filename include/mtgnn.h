@@ -748,10 +748,11 @@ mtgnn_status mtgnn_layer_norm_bwd(const float* dy, int64_t lddy, const void* x, 
  *   label [max_rows]: a row whose label is outside [0, n) has none, counts nothing (whatever its x holds) and has the loss 0;
  *   loss -- [1] float32 out (0 where no row has a label);  row_loss -- [max_rows] float32 out, or NULL;
  *   save -- mtgnn_softmax_loss_save_bytes bytes for the backward (it keeps a copy of x's rows), or NULL.
- * A row all of whose logits are -inf has the loss NaN; an infinite or NaN element of x or W makes the logits that it enters
- * infinite or NaN.  Logits are exact to float32 (float32 elements within 2^-23 of themselves, or 2^-39 of x's or W's
- * largest where that is more); they are not kept: memory beside the copies of x and W (of W none for few
- * rows of float32) grows with max_rows n / 64.
+ * A row all of whose logits are -inf has the loss NaN, one with a logit of +inf the loss inf (NaN where it is the label's, or another is
+ * NaN); an infinite or NaN element of x or W makes the logits that it enters infinite or NaN.  Logits are those of a float32
+ * evaluation, over float32's range: float32 elements are held to 2^-24 of themselves.  They are not kept: memory beside the copies
+ * of x and W (of W none for few rows of float32; float32 ones take 6 bytes an element, and there is room for a bfloat16 W's in any
+ * case) grows with max_rows n / 64.
  * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 0), or with 1 enough for the backward too. */
 typedef struct {
   int32_t n, d, dtype;       /* n < 2^31 - 64, d <= 2^20 */
@@ -766,9 +767,9 @@ mtgnn_status mtgnn_softmax_loss(const void* x, int64_t ldx, const int32_t* n_row
  *   P_rc = (exp(l_rc) / sum exp l_r - [c = label[r]]) dloss / rows with a label  (0 in the rows without one),
  *   dx = P W [max_rows, d],  dW = P^T x [n, d],  db = column sums of P [n],  float32, each or NULL, overwritten (dx in the
  * rows below n_rows).  n_rows, W, b, label, save: the forward's, W and b unchanged.  dx may not overlap W or dW.
- * P is held within 2^-23 of an element or 2^-39, whichever is more, before that scale, x and W as for the logits.  The
- * classes are taken in pieces: a piece's P takes a gigabyte of the workspace at most, where that is 256 classes or more.
- * Of at most 64 rows of float32 everything is in float32, and all of P in the workspace (256 n bytes at most).
+ * The logits are formed again as the forward had them; P is held to 2^-24 of each element, x and W as for the logits.  The
+ * classes are taken in pieces: a piece's P, 6 bytes an element, takes a gigabyte of the workspace at most, where that is 256 classes
+ * or more.  Of at most 64 rows of float32 all of P is in the workspace (256 n bytes at most).
  * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 1). */
 mtgnn_status mtgnn_softmax_loss_bwd(const int32_t* n_rows, int64_t max_rows, const void* W, const float* b,
                                     const int32_t* label, const mtgnn_loss_dims* dims, const void* save, const float* dloss,

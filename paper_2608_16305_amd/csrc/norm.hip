@@ -322,7 +322,12 @@ constexpr int WIDE = 32768, WIDE_BACK = 8192;
 // Teams of the backward: enough to fill the card, few enough that their shares of the sums over rows are few.  Rows that fit a
 // wave have a wave each, 1,024 to 4,096 of them by the rows (backward and joining of 200,000 x 160 in float32: 209 us with
 // 1,024, 124 with 2,048, 79 with 4,096, 80 with 8,192; of 7,997 x 445: 18.7, 15.7, 17.0 and 22.3), and four of them leave one share
-// (forward and backward of 7,997 x 445 and 60,000 x 445 by waves 24.7 and 101, by blocks 27.7 and 138).
+// (forward and backward of 7,997 x 445 and 60,000 x 445 by waves 24.7 and 101, by blocks 27.7 and 138).  Wider ones have 1,024 blocks; with
+// 256, 512, 1,024 and 2,048, forward and backward in bfloat16, us: 16,384 x 600 95, 61, 45 and 44; 16,384 x 2,048 190, 140, 103 and
+// 114; 4,096 x 1,024 32, 25, 24 and 27; 4,096 x 4,096 72, 56, 63 and 70.  Where a block has a row or two of 4,096 and more, its shares
+// outweigh them, and fewer blocks would be faster: 1,000 x 4,096 28, 27, 31 and 31; 1,000 x 8,192 35, 41, 52 and 52; 4,096 x
+// 8,192 125, 131, 145 and 183.  Above 8,192 x and dy are read again for the sums over rows, by 64 teams (with 32, 64 and
+// 256: 500 x 16,384 47, 49 and 58; 2,000 x 16,384 162, 169 and 181; 64 x 33,000 39, 44 and 43; 2,000 x 33,000 373, 363 and 379).
 int back_teams(const mtgnn_norm_dims* d, int64_t rows) {
   if (d->d > WIDE_BACK) return (int)std::min<int64_t>(rows, 64);
   if (d->d > 512) return (int)std::min<int64_t>(rows, 1024);

@@ -12,7 +12,7 @@
 // float32 x and W in the six products of parts that are not below 2^-24 of the whole, P in three with a bfloat16 operand.  (Two
 // float16 parts of float32 operands and of P take three and two products.  But float16 lacks the range: elements below 2^-17 of
 // a matrix's largest lost bits, a probability below 2^-39 was lost, and Adam divides a rare class's gradient by its own size.
-// 8,192 x 32,768 x 1,024 in bfloat16 with gradients took 3,080 us with them for @A, 4,000 x 9,001 x 100 in float32 234 for @B.)
+// 8,192 x 32,768 x 1,024 in bfloat16 with gradients took 3,080 us with them for 3,980, 4,000 x 9,001 x 100 in float32 234 for 342.)
 //
 // Rows without a label are left out before anything is computed: the others' x is copied, row after row, padded with
 // zeros to whole steps.
@@ -421,7 +421,7 @@ __device__ __forceinline__ void leave(const Prod& p, f32x4 (&acc)[WR][WC], Ahead
           for (int e = 0; e < 4; ++e) sum[j][e] += acc[i][j][e];
       }
       // sixteen rows through LDS (the wave's own place): written as they lie there, in whole 128 bytes (in the lanes'
-      // order 32 bytes a row at a time took 823 us for 612, 7,373 x 32,768 x 1,024)
+      // order 32 bytes a row at a time P in two parts took 823 us for 612, 7,373 x 32,768 x 1,024)
       char* w = (char*)lds + wid * (3 * 16 * 144);
 #pragma unroll
       for (int j = 0; j < WC; ++j) {
@@ -1080,7 +1080,9 @@ __global__ __launch_bounds__(256) void k_loss_db(const int32_t* count, const flo
 
 size_t al(size_t b) { return (b + 255) & ~size_t(255); }
 
-constexpr size_t PIECE = size_t(1) << 30;   // bytes of P in memory at a time (where a piece is more than 256 classes wide)
+// Bytes of P in memory at a time (where a piece is more than 256 classes wide).  With 2^28, 2^30 and 2^31, gradients of 8,192 x 32,768 x
+// 1,024 in bfloat16 4,586, 4,033 and 4,006 us.
+constexpr size_t PIECE = size_t(1) << 30;
 
 // Elements from a row to the next one in memory of our own: whole 128 bytes, an odd number of them, so that a column of rows is
 // not in a few of the memory's channels.
@@ -1137,10 +1139,10 @@ struct Tiling {
   int tr, tc, split;
   int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
 };
-// Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 27 us, 3.8 TB/s, in tiles of 256 x 256 48; for few
-// classes they took as long as small ones); else large ones unless the last round of them leaves too much of the card empty: the
-// forward in large and small ones, us, 3,000 x 6,000 x 512 in float32 (288 large tiles) 106 and 91, 4,000 x 9,001 x 512 in
-// bfloat16 (576) 82 and 79, 4,000 x 16,000 x 512 (1,008) 108 and 113, 4,000 x 30,000 x 1,024 (1,888) 269 and 292.
+// Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 24 us, 4.3 TB/s; the whole forward in wide, small and large
+// tiles 38, 47 and 58 us, 64 x 30,000 x 1,024 33, 32 and 41, 40 x 9,000 x 100 19, 19 and 21); else large ones unless the last round of them leaves too much of the card empty: the
+// forward in large and small ones, us, 3,000 x 6,000 x 512 in float32 (288 large tiles) 160 and 136, 2,000 x 30,000 x
+// 512 (944) 332 and 374, 4,000 x 9,001 x 512 in bfloat16 (576) 75 and 72, 4,000 x 16,000 x 512 (1,008) 100 and 107.
 Tiling tiling(int64_t rows, int64_t cols) {
   if (rows <= 64) return Tiling{64, 256, 1};
   const Tiling big{256, 256, 1}, small{128, 128, 1};
@@ -1149,7 +1151,8 @@ Tiling tiling(int64_t rows, int64_t cols) {
 // Of a gradient, with sums of `steps` steps: the tiles and shares that are done first, in us: rounds of blocks, a step of 1.53 in large
 // tiles and 1 in small ones, two of which a compute unit has, 6 steps a block beside its own, and the shares' way to memory and
 // back, with a launch.  (Gradients and logits, us, in small tiles alone, large ones alone and as chosen here: 4,000 x 9,001 x 100
-// in float32 249, 284, 249; 8,192 x 32,768 x 1,024 in bfloat16 3,444, 3,077, 3,047; 1,000 x 30,000 x 1,024 488, 459, 459.)
+// in float32 344, 386, 342; 500 x 20,000 x 512 345, 350, 341; 3,000 x 6,000 x 512 523, 485, 488; 8,192 x 32,768 x 1,024 in
+// bfloat16 4,639, 3,985, 3,980; 1,000 x 30,000 x 1,024 574, 526, 519.)
 Tiling tiling(int64_t rows, int64_t cols, int64_t steps) {
   Tiling best{256, 256, 1};
   double least = INFINITY;
@@ -1176,7 +1179,7 @@ int few_per(const mtgnn_loss_dims* d) {
   return (int)up(cdiv(d->n, shares), 64);
 }
 // Classes of a block of the forward's k_loss_few: more for short rows of many classes, whose tiles then take less time to join
-// (128 and 64, the whole forward: 16 x 190,000 x 200 51 and 61 us, 14 x 142,281 x 1,024 152 and 143, 64 x 9,000 x 1,024 55 and 38).
+// (128 and 64, the whole forward: 16 x 190,000 x 200 42 and 47 us, 14 x 142,281 x 1,024 145 and 129, 64 x 9,000 x 1,024 53 and 38).
 int few_classes(const mtgnn_loss_dims* d) { return d->n >= 32768 && d->d < 512 ? 128 : 64; }
 // A forward's tiles of classes.
 int64_t class_tiles(const mtgnn_loss_dims* d, const Plan& p, int64_t rows) {
@@ -1344,8 +1347,8 @@ mtgnn_status loss_impl(const void* x, int64_t ldx, const int32_t* n_rows, int64_
     MTGNN_TRY(product<STAT>(q, tl, s));
   }
   // The whole forward, us: with 64 threads to a row, not 16, where there are more tiles than those request at once, 33 x 100,003 x 520
-  // (391 tiles) 54 -> 40; with one block, and no launch for the mean, 17 x 9,000 x 100 (141 tiles) 17.4 -> 15.4, but
-  // 14 x 142,281 x 1,024 (2,224 tiles) 130 -> 156.
+  // (391 tiles) 42 -> 38; with one block, and no launch for the mean, 17 x 9,000 x 100 (141 tiles) 18.4 -> 15.5, but
+  // 14 x 142,281 x 1,024 (2,224 tiles) 130 -> 157.
   const auto join = [&](auto kernel, int rows, int threads) -> mtgnn_status {
     kernel<<<(unsigned)cdiv(max_rows, rows), threads, 0, s>>>(k.count, k.idx, part, tiles, p.Rp, at_label, k.stat, row_loss, sums,
                                                               loss);

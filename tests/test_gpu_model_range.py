@@ -93,6 +93,15 @@ def test_rare_classes_have_their_gradient(rows, n, d, bf16):
 
 
 @BOTH
+@SIZES
+@pytest.mark.parametrize("power", [-80, 60])
+def test_operands_of_unlike_sizes(rows, n, d, power, bf16):
+    """Rows of x larger or smaller by a power of two than W's are smaller or larger: the logits are ordinary ones."""
+    x, W, b, label = _inputs(rows, n, d, bf16)
+    _check(np.ldexp(x, power), np.ldexp(W, -power), b, label, bf16)
+
+
+@BOTH
 @pytest.mark.parametrize("rows", [10, 70, 200, 1100])
 @pytest.mark.parametrize("at", [5, 500])
 def test_a_nan_beside_an_infinite_logit_is_nan(rows, at, bf16):
