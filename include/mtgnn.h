@@ -767,7 +767,7 @@ mtgnn_status mtgnn_softmax_loss(const void* x, int64_t ldx, const int32_t* n_row
  *   P_rc = (exp(l_rc) / sum exp l_r - [c = label[r]]) dloss / rows with a label  (0 in the rows without one),
  *   dx = P W [max_rows, d],  dW = P^T x [n, d],  db = column sums of P [n],  float32, each or NULL, overwritten (dx in the
  * rows below n_rows).  n_rows, W, b, label, save: the forward's, W and b unchanged.  dx may not overlap W or dW.
- * The logits are formed again as the forward had them; P is held to 2^-24 of each element, x and W as for the logits.  The
+ * The logits are formed again; P is held to 2^-24 of each element, x and W as for the logits.  The
  * classes are taken in pieces: a piece's P, 6 bytes an element, takes a gigabyte of the workspace at most, where that is 256 classes
  * or more.  Of at most 64 rows of float32 all of P is in the workspace (256 n bytes at most).
  * Workspace: mtgnn_softmax_loss_ws_bytes(dims, max_rows, 1). */

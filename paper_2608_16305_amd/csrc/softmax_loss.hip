@@ -1140,9 +1140,10 @@ struct Tiling {
   int64_t tiles(int64_t rows, int64_t cols) const { return cdiv(rows, tr) * cdiv(cols, tc); }
 };
 // Of the logits: wide tiles for few rows (33 x 100,003 x 520 is reading W: 24 us, 4.3 TB/s; the whole forward in wide, small and large
-// tiles 38, 47 and 58 us, 64 x 30,000 x 1,024 33, 32 and 41, 40 x 9,000 x 100 19, 19 and 21); else large ones unless the last round of them leaves too much of the card empty: the
-// forward in large and small ones, us, 3,000 x 6,000 x 512 in float32 (288 large tiles) 160 and 136, 2,000 x 30,000 x
-// 512 (944) 332 and 374, 4,000 x 9,001 x 512 in bfloat16 (576) 75 and 72, 4,000 x 16,000 x 512 (1,008) 100 and 107.
+// tiles 38, 47 and 58 us, 64 x 30,000 x 1,024 33, 32 and 41, 40 x 9,000 x 100 19, 19 and 21); else large ones unless the last
+// round of them leaves too much of the card empty: the forward in large and small ones, us, 3,000 x 6,000 x 512 in float32 (288
+// large tiles) 160 and 136, 2,000 x 30,000 x 512 (944) 332 and 374, 4,000 x 9,001 x 512 in bfloat16 (576) 75 and 72, 4,000 x
+// 16,000 x 512 (1,008) 100 and 107.
 Tiling tiling(int64_t rows, int64_t cols) {
   if (rows <= 64) return Tiling{64, 256, 1};
   const Tiling big{256, 256, 1}, small{128, 128, 1};
@@ -1420,7 +1421,7 @@ mtgnn_status loss_bwd_impl(const int32_t* n_rows, int64_t max_rows, const void* 
     return MTGNN_OK;
   };
   MTGNN_TRY(p.bf ? lay((const uint16_t*)W) : lay((const float*)W));
-  // W from class c on: the forward's operand, so the logits are the forward's too
+  // W from class c on: what the forward's product has, so its logits are formed again (those of k_loss_few differ by their rounding)
   const auto table = [&](Prod& q, int64_t c) {
     q.B = in_place ? (const uint16_t*)W + c * d->d : tbl + c * p.dp;
     q.ldb = wdp;

@@ -9,7 +9,8 @@ import torch
 from oracle import model
 from paper_2608_16305_amd import mtgnn as M
 from tests._gpu import needs_gpu
-from tests.test_gpu_model import (BOTH, CFG, U, _adamw_tolerance, _close, _dev, _loss_tolerances, _marked, _norm_tolerances, _vals)
+from tests.test_gpu_model import (BOTH, CFG, U, _adamw_tolerance, _check_loss, _close, _dev, _loss_tolerances, _marked, _norm_tolerances,
+                                  _vals)
 from tests.test_gpu_model import test_embedding as _embedding_case
 from tests.test_gpu_model import test_layer_norm as _norm_case
 
@@ -67,6 +68,14 @@ def test_adamw_refuses_a_gradient_in_what_is_written():
         lists([g[:8], in_shadow], shadow=[None, sh[8:16]])
     empty = torch.empty(0, device="cuda")
     M.adamw_tensors([empty, p[:8]], [empty, g[:8]], [empty, m[:8]], [empty, v[:8]])
+
+
+# float32: three groups of 64 rows that share W, more blocks than the card has at once; and one row more, by parts
+@BOTH
+@pytest.mark.parametrize("case", [(150, 42, 17_003, 40, True, 0.1, True, None), (192, 0, 20_000, 33, False, 0.0, False, 2.0),
+                                  (193, 0, 20_000, 33, True, 0.0, False, None), (3, 189, 17_000, 64, True, 0.0, False, None)], ids=str)
+def test_softmax_loss_of_three_groups_of_rows(case, bf16):
+    _check_loss(case, bf16)
 
 
 # 2,048 rows and more of these widths have a wave each forward, of 16 or 32 elements a lane
